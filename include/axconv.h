@@ -372,6 +372,203 @@ int ax_conv2d_backward(const ax_conv_desc_t* desc, const ax_quant_t* q, const vo
                        size_t workspace_bytes, void* hip_stream);
 size_t ax_conv2d_backward_workspace_bytes(const ax_conv_desc_t* desc);
 
+/* ---- feed-forward operators ----------------------------------------------------------------
+ *
+ * What a network needs around its quantized layers to be trained and to answer: the norm in front
+ * of a feed-forward block with an output in 8-bit codes, matrix products with bias, activation and
+ * residual in their epilogue on float tensors or on 8-bit codes, the gated block, and the step of
+ * the optimizer.  They work on exact products (the matrix cores), next to the table-lookup layers.
+ *
+ * Element types are named by the values below.  Matrices are row major; *_ld are row pitches in
+ * elements (at least the row's length).  Sums, norms and optimizer states are held in float32 (int32
+ * for products of codes); results are rounded once, to nearest even, where they are stored.  Zero
+ * rows (M or rows = 0) are valid: nothing is written but the sums over rows, which are zero.
+ * Everything else follows the conventions above: the calls only enqueue work, outputs are
+ * overwritten completely and alias no input unless that is said, 16-bit and 32-bit pointers are
+ * aligned to their element.
+ */
+#define AX_F32 0
+#define AX_BF16 1
+
+#define AX_ACT_NONE 0
+#define AX_ACT_RELU 1
+#define AX_ACT_SILU 2 /* z / (1 + exp(-z)) */
+#define AX_ACT_GELU 3 /* z * (1 + erf(z / sqrt 2)) / 2 */
+
+/*
+ * Root-mean-square norm of rows with the residual's addition in front:
+ *   t = x + residual            (x alone where residual is NULL), in float32
+ *   rstd = 1 / sqrt(mean of t^2 over the row + eps)
+ *   y = t * rstd * weight
+ */
+typedef struct {
+  int64_t rows, cols; /* rows >= 0, 1 <= cols < 2^31                                            */
+  int64_t x_ld, residual_ld, sum_ld, y_ld;
+  int32_t dtype;      /* of x, residual, sum and y; in the backward pass of all the matrices    */
+  int32_t w_dtype;    /* of weight                                                              */
+  float eps;          /* >= 0 and finite                                                        */
+  int32_t normalize;  /* 1.  0 (ax_rmsnorm_q8 alone): rstd = 1, plain quantization of rows      */
+} ax_norm_desc_t;
+
+/* sum_out (may be NULL; needs a residual): t, the residual stream behind the addition, rounded to
+ * dtype (the norm itself takes it unrounded); it may be x or residual itself, with that tensor's
+ * row pitch.  rstd_out [rows] (may be NULL): kept for the backward pass. */
+int ax_rmsnorm(const ax_norm_desc_t* desc, const void* x, const void* residual, const void* weight,
+               void* sum_out, void* y_out, float* rstd_out, void* hip_stream);
+
+/*
+ * The same rows as 8-bit codes, symmetric, one scale a row: with v = t * weight (one float32
+ * product; v = t where weight is NULL) and amax the row's largest |v|,
+ *   codes = round(v * (127 / amax)), ties to even, in [-127, 127]        scales = amax * rstd / 127
+ * The codes do not depend on the order of the norm's sum: rstd scales the whole row.  A row whose
+ * amax is below 2^-120 (where 127 / amax leaves float32) has codes zero.  A row that holds a NaN or an infinity has scale NaN or
+ * infinity and codes zero.  codes_out [rows, cols] and scales_out [rows] are what ax_matmul_q8 and
+ * ax_gated_q8 take.  values_out (may be NULL) [rows, cols] float32, pitch cols: code * scale.
+ */
+int ax_rmsnorm_q8(const ax_norm_desc_t* desc, const void* x, const void* residual, const void* weight,
+                  void* sum_out, int8_t* codes_out, float* scales_out, float* values_out, void* hip_stream);
+
+/*
+ * Gradients of ax_rmsnorm.  t: the sum (x where there was no residual) and rstd as the forward pass
+ * left them; gy [rows, cols]; gsum (may be NULL) [rows, cols]: the gradient that reaches t from the
+ * residual stream.  With h = t * rstd and q = gy * weight:
+ *   gx_out = rstd * (q - h * mean over the row of (q * h)) + gsum       for x and residual alike
+ *   gw_out [cols] float32 = sum over the rows of gy * h
+ * Pitches: desc->x_ld (t), residual_ld (gsum), sum_ld (gx_out), y_ld (gy).  gx_out may be gsum.
+ * Either output may be NULL (not both).  The sum over rows is taken in a fixed order.
+ * workspace: ax_rmsnorm_backward_workspace_bytes(desc) bytes, 256-byte aligned.
+ */
+int ax_rmsnorm_backward(const ax_norm_desc_t* desc, const void* gy, const void* gsum, const void* t,
+                        const void* weight, const float* rstd, void* gx_out, float* gw_out,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t ax_rmsnorm_backward_workspace_bytes(const ax_norm_desc_t* desc);
+
+/*
+ * Matrix product with its epilogue:  z = x w + bias,  y = act(z) + residual.
+ *   x [M, K], w [K, N] (or [N, K] where w_transposed is 1), bias [N], residual and y [M, N],
+ *   z_out (may be NULL) [M, N] with pitch N, kept for the backward pass
+ * bias and residual may be NULL.  dtype is the type of x and w, out_dtype that of bias, residual, z
+ * and y.  AX_BF16 products are exact in float32 and summed there.  AX_F32 operands are taken as three
+ * bf16 pieces each (exact together) and six of their nine products; what is dropped is below 2^-24
+ * of a product, so results are those of a float32 product.
+ * Operands that the kernels cannot read in place (AX_F32; rows that are not 16-byte aligned or whose
+ * length is no multiple of 16 bytes) are copied into the workspace first.
+ * workspace: ax_matmul_workspace_bytes(desc) bytes, 256-byte aligned.
+ */
+typedef struct {
+  int64_t M, N, K;    /* M >= 0; N, K >= 1; each below 2^31, row pitches below 2^22 bytes        */
+  int64_t x_ld, w_ld, residual_ld, y_ld;
+  int32_t dtype, out_dtype;
+  int32_t act;
+  int32_t w_transposed;
+  int32_t unaligned;  /* 0: x, w (and gy where act is AX_ACT_NONE) start on 16 bytes wherever their rows do
+                         (AX_ERR_ALIGN otherwise).  1: they may start anywhere; they are copied   */
+} ax_matmul_desc_t;
+
+int ax_matmul(const ax_matmul_desc_t* desc, const void* x, const void* w, const void* bias,
+              const void* residual, void* y_out, void* z_out, void* workspace, size_t workspace_bytes,
+              void* hip_stream);
+size_t ax_matmul_workspace_bytes(const ax_matmul_desc_t* desc);
+
+/*
+ * The product of 8-bit codes: z = (x_scales[m] * w_scales[n]) * sum over k of x[m,k] w[n,k] + bias,
+ * y = act(z) + residual, the sum exact in int32.  x [M, K] and w [N, K] int8 (desc->w_transposed must
+ * be 1, desc->dtype is ignored), K <= 131071 (AX_ERR_K_OVERFLOW).
+ * workspace: ax_matmul_q8_workspace_bytes(desc) bytes, 256-byte aligned.
+ */
+int ax_matmul_q8(const ax_matmul_desc_t* desc, const int8_t* x, const float* x_scales, const int8_t* w,
+                 const float* w_scales, const void* bias, const void* residual, void* y_out,
+                 void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t ax_matmul_q8_workspace_bytes(const ax_matmul_desc_t* desc);
+
+/*
+ * Gradients of ax_matmul (of its residual: gy itself).  With gz = gy * act'(z), act'(0) = 0 for relu:
+ *   gx_out [M, K] = gz w^T     gw_out (the shape and pitch of w) = x^T gz     gb_out [N] float32 = sum of gz
+ * gy and z [M, N] have the type desc->dtype and the pitches y_ld and N; gx_out (pitch x_ld) and gw_out
+ * (pitch w_ld) too; desc->out_dtype must be desc->dtype.  z may be NULL where act is AX_ACT_NONE.  bf16: gz is rounded to bf16
+ * for the two products (their matrix instructions take 16-bit operands), not for gb_out.  Any output
+ * may be NULL (not all).  workspace: ax_matmul_backward_workspace_bytes(desc) bytes.
+ */
+int ax_matmul_backward(const ax_matmul_desc_t* desc, const void* gy, const void* x, const void* w,
+                       const void* z, void* gx_out, void* gw_out, float* gb_out, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
+size_t ax_matmul_backward_workspace_bytes(const ax_matmul_desc_t* desc);
+
+/*
+ * Gated feed-forward block up to the product back:  g = x wg,  u = x wu,  h = act(g) * u,
+ * both projections, the activation and the product in one kernel.
+ *   x [M, K], wg and wu [K, N], h [M, N]; g_out, u_out [M, N] (pitch N, both or neither NULL): kept
+ *   for the backward pass
+ * The descriptor is that of ax_matmul: w_ld is the pitch of both weights, w_transposed must be 0,
+ * residual_ld is ignored.  workspace: ax_gated_workspace_bytes(desc) bytes, 256-byte aligned.
+ */
+int ax_gated(const ax_matmul_desc_t* desc, const void* x, const void* wg, const void* wu, void* h_out,
+             void* g_out, void* u_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t ax_gated_workspace_bytes(const ax_matmul_desc_t* desc);
+
+/* On 8-bit codes, as ax_matmul_q8: x [M, K], wg and wu [N, K] int8, w_transposed must be 1. */
+int ax_gated_q8(const ax_matmul_desc_t* desc, const int8_t* x, const float* x_scales, const int8_t* wg,
+                const float* wg_scales, const int8_t* wu, const float* wu_scales, void* h_out,
+                void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t ax_gated_q8_workspace_bytes(const ax_matmul_desc_t* desc);
+
+/*
+ * Gradients of ax_gated.  With gg = gh * u * act'(g) and gu = gh * act(g):
+ *   gx_out [M, K] = gg wg^T + gu wu^T     gwg_out = x^T gg,  gwu_out = x^T gu     [K, N], pitch w_ld
+ * gh (pitch y_ld), g, u (pitch N), gx_out (pitch x_ld): type desc->dtype; desc->out_dtype must be
+ * desc->dtype.  bf16: gg and gu are rounded to bf16 for the products.  gx_out may be NULL, or both
+ * weight gradients.  workspace: ax_gated_backward_workspace_bytes(desc) bytes.
+ */
+int ax_gated_backward(const ax_matmul_desc_t* desc, const void* gh, const void* x, const void* wg,
+                      const void* wu, const void* g, const void* u, void* gx_out, void* gwg_out,
+                      void* gwu_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t ax_gated_backward_workspace_bytes(const ax_matmul_desc_t* desc);
+
+/*
+ * One AdamW step over many tensors (decoupled weight decay, bias correction for step = 1, 2, ...).
+ * For every element, each line a float32 operation at a time, factors rounded once from double:
+ *   g = gradient * *grad_scale          (the gradient itself where grad_scale is NULL)
+ *   m = beta1 * m + (1 - beta1) * g            v = beta2 * v + (1 - beta2) * (g * g)
+ *   p = p * (1 - lr * weight_decay) - (lr / (1 - beta1^step)) * (m / (sqrt(v) * (1 / sqrt(1 - beta2^step)) + eps))
+ * state_bits 32: m and v are float32.  state_bits 8: codes, one float32 scale for every 256 elements
+ * in their order (AX_STATE_BLOCK; the last block of a tensor may be shorter):
+ *   m = scale * r |r|, r = code / 127, code in [-127, 127], scale the block's largest |m|
+ *   v = scale * (r r)^2, r = code / 255, code in [0, 255], scale the block's largest v
+ * with the codes rounded to nearest in r; a v above zero never gets code 0, so that no update divides
+ * by eps alone.  A block with a NaN gets scale NaN: it shows in every parameter of the block.
+ */
+#define AX_STATE_BLOCK 256
+
+typedef struct {
+  void* p;        /* parameters, updated in place                                              */
+  const void* g;  /* gradients                                                                 */
+  void* m;        /* float32, or int8 codes                                                    */
+  void* v;        /* float32, or uint8 codes                                                   */
+  float* m_scale; /* 8 bits: one a block                                                       */
+  float* v_scale;
+  void* copy;     /* may be NULL: the updated parameters once more, rounded to bf16            */
+  int64_t n;      /* elements, >= 0                                                            */
+} ax_adamw_tensor_t;
+
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;            /* >= 1                                                             */
+  const float* grad_scale; /* device float, may be NULL                                        */
+  int32_t p_dtype, g_dtype;
+  int32_t state_bits;      /* 32 or 8                                                          */
+  int32_t reserved;        /* 0                                                                */
+} ax_adamw_desc_t;
+
+/* tensors: HOST array, read before the call returns (it travels in the kernels' arguments: one launch
+ * for every AX_ADAMW_LAUNCH tensors that are not empty).  Tensors must not overlap. */
+#define AX_ADAMW_LAUNCH 48
+int ax_adamw(const ax_adamw_desc_t* desc, const ax_adamw_tensor_t* tensors, int count, void* hip_stream);
+
+/* The values that 8-bit states stand for, float32: m_out[i] and v_out[i] (host arrays of device
+ * pointers) for tensors[i], of which p, g and copy are not looked at. */
+int ax_adamw_states(const ax_adamw_tensor_t* tensors, int count, float* const* m_out, float* const* v_out,
+                    void* hip_stream);
+
 const char* ax_strerror(int code);
 
 /* Library version, major * 10000 + minor * 100 + patch. */

@@ -49,6 +49,11 @@ EXPORTS = [  # include/axconv.h
     "ax_conv2d_f32_ex_workspace_bytes", "ax_layer_create", "ax_layer_destroy", "ax_layer_prepared_bytes",
     "ax_layer_workspace_bytes", "ax_layer_prepare", "ax_layer_run", "ax_layer_plan", "ax_layer_plan_paths", "ax_layer_run_static",
     "ax_static_scratch_bytes", "ax_conv2d_backward", "ax_conv2d_backward_workspace_bytes",
+    "ax_rmsnorm", "ax_rmsnorm_q8", "ax_rmsnorm_backward", "ax_rmsnorm_backward_workspace_bytes",
+    "ax_matmul", "ax_matmul_workspace_bytes", "ax_matmul_q8", "ax_matmul_q8_workspace_bytes",
+    "ax_matmul_backward", "ax_matmul_backward_workspace_bytes", "ax_gated", "ax_gated_workspace_bytes",
+    "ax_gated_q8", "ax_gated_q8_workspace_bytes", "ax_gated_backward", "ax_gated_backward_workspace_bytes",
+    "ax_adamw", "ax_adamw_states",
 ]
 PROBE_EXPORTS = [  # include/axconv_probe.h
     "ax_probe_lds_gather", "ax_probe_copy", "ax_probe_mac", "ax_probe_layer_kernel_ms",
@@ -67,6 +72,31 @@ class ax_conv_desc_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "N", "H", "W", "Cin", "KH", "KW", "Cout", "stride_h", "stride_w", "pad_h", "pad_w", "dilation_h", "dilation_w",
         "depthwise", "signed_codes", "groups")]
+
+
+AX_F32, AX_BF16 = 0, 1
+AX_ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+AX_STATE_BLOCK = 256
+
+
+class ax_norm_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "cols", "x_ld", "residual_ld", "sum_ld", "y_ld")] + [
+        ("dtype", ctypes.c_int32), ("w_dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("normalize", ctypes.c_int32)]
+
+
+class ax_matmul_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("M", "N", "K", "x_ld", "w_ld", "residual_ld", "y_ld")] + [
+        (n, ctypes.c_int32) for n in ("dtype", "out_dtype", "act", "w_transposed", "unaligned")]
+
+
+class ax_adamw_tensor_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("p", "g", "m", "v", "m_scale", "v_scale", "copy")] + [("n", ctypes.c_int64)]
+
+
+class ax_adamw_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [
+        ("step", ctypes.c_int64), ("grad_scale", ctypes.c_void_p)] + [
+        (n, ctypes.c_int32) for n in ("p_dtype", "g_dtype", "state_bits", "reserved")]
 
 
 def lib():
@@ -161,6 +191,21 @@ def lib():
     L.ax_dense_f32.restype = ci
     L.ax_dense_f32_workspace_bytes.argtypes = [ci, ci, ci]
     L.ax_dense_f32_workspace_bytes.restype = sz
+    nd, md = ctypes.POINTER(ax_norm_desc_t), ctypes.POINTER(ax_matmul_desc_t)
+    for name, args in (
+            ("ax_rmsnorm", [nd] + [vp] * 7), ("ax_rmsnorm_q8", [nd] + [vp] * 8),
+            ("ax_rmsnorm_backward", [nd] + [vp] * 8 + [sz, vp]),
+            ("ax_matmul", [md] + [vp] * 7 + [sz, vp]), ("ax_matmul_q8", [md] + [vp] * 8 + [sz, vp]),
+            ("ax_matmul_backward", [md] + [vp] * 8 + [sz, vp]),
+            ("ax_gated", [md] + [vp] * 7 + [sz, vp]), ("ax_gated_q8", [md] + [vp] * 8 + [sz, vp]),
+            ("ax_gated_backward", [md] + [vp] * 10 + [sz, vp]),
+            ("ax_adamw", [ctypes.POINTER(ax_adamw_desc_t), ctypes.POINTER(ax_adamw_tensor_t), ci, vp]),
+            ("ax_adamw_states", [ctypes.POINTER(ax_adamw_tensor_t), ci, ctypes.POINTER(vp), ctypes.POINTER(vp), vp])):
+        getattr(L, name).argtypes, getattr(L, name).restype = args, ci
+    L.ax_rmsnorm_backward_workspace_bytes.argtypes, L.ax_rmsnorm_backward_workspace_bytes.restype = [nd], sz
+    for name in ("ax_matmul", "ax_matmul_q8", "ax_matmul_backward", "ax_gated", "ax_gated_q8", "ax_gated_backward"):
+        f = getattr(L, name + "_workspace_bytes")
+        f.argtypes, f.restype = [md], sz
     _lib = L
     return L
 
@@ -805,6 +850,415 @@ def ax_dense_f32(x, w, lut, x_range=None, w_range=None, relu=False, round_mode=0
                         ctypes.c_void_p(_stream_ptr(stream)))
     _check(rc)
     return (None if acc_out is False else acc_out), (None if y_out is False else y_out)
+
+
+# ---- feed-forward operators: norm, products, gated block, optimizer step -----------------------------------------------
+#
+# Matrices are torch tensors whose last dimension is contiguous; the leading dimensions are rows, at any pitch where there is
+# one of them, contiguous where there are more.  Outputs that are not handed in are allocated with torch.
+
+
+_DT = {torch.float32: AX_F32, torch.bfloat16: AX_BF16}
+
+
+def _float_dtype(t, name: str) -> int:
+    dt = _DT.get(t.dtype)
+    if dt is None:
+        raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    return dt
+
+
+def _mat(t, dtype, name: str) -> Tuple[int, int, int]:
+    """(rows, columns, row pitch) of a matrix."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % name)
+    if t.dtype != dtype:
+        raise TypeError("%s must have dtype %s, got %s" % (name, dtype, t.dtype))
+    n = t.dim()
+    if n == 2:
+        r, c = t.shape
+        if c > 1 and t.stride(1) != 1:
+            raise ValueError("%s must have contiguous rows" % name)
+        if r <= 1:
+            return r, c, c
+        ld = t.stride(0)
+        if ld < c:
+            raise ValueError("%s must not overlap itself" % name)
+        return r, c, ld
+    if n == 0 or not t.is_contiguous():
+        raise ValueError("%s must be a matrix with contiguous rows, or contiguous" % name)
+    c = t.shape[-1]
+    r = 1
+    for v in t.shape[:-1]:
+        r *= v
+    return r, c, c
+
+
+def _mat_of(t, dtype, rows: int, cols: int, name: str) -> int:
+    """Row pitch of a matrix that has to be [rows, cols]."""
+    r, c, ld = _mat(t, dtype, name)
+    if r != rows or c != cols:
+        raise ValueError("%s must be [%d, %d], got [%d, %d]" % (name, rows, cols, r, c))
+    return ld
+
+
+def _vec_of(t, dtype, n: int, name: str) -> None:
+    _dev(t, dtype, name)
+    if t.numel() != n:
+        raise ValueError("%s must have %d elements" % (name, n))
+
+
+def _act_code(act: str) -> int:
+    if act not in AX_ACTS:
+        raise ValueError("act must be one of %s" % ", ".join(AX_ACTS))
+    return AX_ACTS[act]
+
+
+def _norm_desc(x, residual, sum_out, weight, eps, normalize) -> Tuple[ax_norm_desc_t, torch.Tensor]:
+    dt = _float_dtype(x, "x")
+    rows, cols, ld = _mat(x, x.dtype, "x")
+    d = ax_norm_desc_t(rows, cols, ld, cols, cols, cols, dt, dt, float(eps), int(bool(normalize)))
+    if weight is not None:
+        d.w_dtype = _float_dtype(weight, "weight")
+        _vec_of(weight, weight.dtype, cols, "weight")
+    if residual is not None:
+        d.residual_ld = _mat_of(residual, x.dtype, rows, cols, "residual")
+        if sum_out is None:
+            sum_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    elif sum_out is not None and sum_out is not False:
+        raise ValueError("sum_out needs a residual")
+    if sum_out is False:
+        sum_out = None
+    if sum_out is not None:
+        d.sum_ld = _mat_of(sum_out, x.dtype, rows, cols, "sum_out")
+    return d, sum_out
+
+
+def ax_rmsnorm(x, weight, residual=None, eps=1e-5, sum_out=None, y_out=None, rstd_out=None, stream=None):
+    """Root-mean-square norm of rows: t = x + residual, y = t * rstd * weight.  Returns (y, t, rstd); t is None without
+    a residual.  sum_out may be x or residual themselves; False skips t (or rstd)."""
+    d, sum_out = _norm_desc(x, residual, sum_out, weight, eps, True)
+    if y_out is None:
+        y_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    d.y_ld = _mat_of(y_out, x.dtype, d.rows, d.cols, "y_out")
+    if rstd_out is None:
+        rstd_out = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    if rstd_out is False:
+        rstd_out = None
+    else:
+        _vec_of(rstd_out, torch.float32, d.rows, "rstd_out")
+    _check(lib().ax_rmsnorm(ctypes.byref(d), _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_out), _ptr(y_out),
+                            _ptr(rstd_out), _stream_ptr(stream)))
+    return y_out, sum_out, rstd_out
+
+
+def ax_rmsnorm_q8(x, weight=None, residual=None, eps=1e-5, normalize=True, sum_out=None, codes_out=None, scales_out=None,
+                  values_out=None, values=False, stream=None):
+    """The norm's output as int8 codes with a scale a row: y = codes * scales[:, None].  normalize False: the rows
+    themselves (times weight).  Returns (codes, scales, t, values); values, the float32 values that the codes stand for,
+    is None unless asked for."""
+    d, sum_out = _norm_desc(x, residual, sum_out, weight, eps, normalize)
+    if codes_out is None:
+        codes_out = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    _vec_of(codes_out, torch.int8, d.rows * d.cols, "codes_out")
+    if scales_out is None:
+        scales_out = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    _vec_of(scales_out, torch.float32, d.rows, "scales_out")
+    if values_out is None and values:
+        values_out = torch.empty(x.shape, dtype=torch.float32, device=x.device)
+    if values_out is not None:
+        _vec_of(values_out, torch.float32, d.rows * d.cols, "values_out")
+    _check(lib().ax_rmsnorm_q8(ctypes.byref(d), _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_out), _ptr(codes_out),
+                               _ptr(scales_out), _ptr(values_out), _stream_ptr(stream)))
+    return codes_out, scales_out, sum_out, values_out
+
+
+def _scratch(need: int, workspace, device, stream):
+    if workspace is None:
+        return _workspace(need, device, stream) if need else None
+    return _dev(workspace, torch.uint8, "workspace")
+
+
+def _ws_args(ws):
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
+
+
+def ax_rmsnorm_backward(gy, t, weight, rstd, gsum=None, gx_out=None, gw_out=None, workspace=None, stream=None):
+    """Gradients of ax_rmsnorm: (gx, gw), gx for x and residual alike, gw float32.  t, rstd: what the forward pass
+    returned (t = x without a residual); gsum: the gradient that reaches t from the residual stream.  False skips one."""
+    L = lib()
+    dt = _float_dtype(t, "t")
+    rows, cols, ld = _mat(t, t.dtype, "t")
+    _vec_of(weight, weight.dtype, cols, "weight")
+    _vec_of(rstd, torch.float32, rows, "rstd")
+    d = ax_norm_desc_t(rows, cols, ld, cols, cols, _mat_of(gy, t.dtype, rows, cols, "gy"), dt, _float_dtype(weight, "weight"),
+                       0.0, 1)
+    if gsum is not None:
+        d.residual_ld = _mat_of(gsum, t.dtype, rows, cols, "gsum")
+    if gx_out is None:
+        gx_out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    if gw_out is None:
+        gw_out = torch.empty(weight.shape, dtype=torch.float32, device=t.device)
+    if gx_out is not False:
+        d.sum_ld = _mat_of(gx_out, t.dtype, rows, cols, "gx_out")
+    if gw_out is not False:
+        _vec_of(gw_out, torch.float32, cols, "gw_out")
+    gx_out, gw_out = (None if o is False else o for o in (gx_out, gw_out))
+    ws = _scratch(int(L.ax_rmsnorm_backward_workspace_bytes(ctypes.byref(d))), workspace, t.device, stream)
+    _check(L.ax_rmsnorm_backward(ctypes.byref(d), _ptr(gy), _ptr(gsum), _ptr(t), _ptr(weight), _ptr(rstd), _ptr(gx_out),
+                                 _ptr(gw_out), *_ws_args(ws), _stream_ptr(stream)))
+    return gx_out, gw_out
+
+
+def _matmul_desc(x, w, act, transposed, out_dtype, names=("x", "w")) -> ax_matmul_desc_t:
+    M, K, x_ld = _mat(x, x.dtype, names[0])
+    wr, wc, w_ld = _mat(w, x.dtype, names[1])
+    if w.dim() != 2 or (wc if transposed else wr) != K:
+        raise ValueError("%s must be %s for %s [M,K]" % (names[1], "[N,K]" if transposed else "[K,N]", names[0]))
+    N = wr if transposed else wc
+    dt = AX_BF16 if x.dtype == torch.int8 else _float_dtype(x, names[0])
+    odt = _DT.get(out_dtype)
+    if odt is None:
+        raise TypeError("out_dtype must be float32 or bfloat16")
+    return ax_matmul_desc_t(M, N, K, x_ld, w_ld, N, N, dt, odt, _act_code(act), int(bool(transposed)),
+                            int((x.data_ptr() | w.data_ptr()) % 16 != 0))
+
+
+def _matmul_out(d, out, x, dtype, name):
+    if out is None:
+        out = torch.empty(x.shape[:-1] + (d.N,), dtype=dtype, device=x.device)
+    d.y_ld = _mat_of(out, dtype, d.M, d.N, name)
+    return out
+
+
+def _epilogue_args(d, bias, residual, dtype):
+    if bias is not None:
+        _vec_of(bias, dtype, d.N, "bias")
+    if residual is not None:
+        d.residual_ld = _mat_of(residual, dtype, d.M, d.N, "residual")
+
+
+def ax_matmul(x, w, bias=None, residual=None, act="none", transposed=False, out_dtype=None, save=False, y_out=None, z_out=None,
+              workspace=None, stream=None):
+    """y = act(x w + bias) + residual.  x: [M,K]; w: [K,N], or [N,K] with transposed; float32 or bfloat16 both; bias,
+    residual and the outputs have out_dtype (x's by default).  Returns (y, z): z, the value before the activation, with
+    save or z_out, otherwise None."""
+    L = lib()
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    d = _matmul_desc(x, w, act, transposed, out_dtype)
+    y_out = _matmul_out(d, y_out, x, out_dtype, "y_out")
+    _epilogue_args(d, bias, residual, out_dtype)
+    if z_out is None and save:
+        z_out = torch.empty(x.shape[:-1] + (d.N,), dtype=out_dtype, device=x.device)
+    if z_out is not None:
+        _vec_of(z_out, out_dtype, d.M * d.N, "z_out")
+    ws = _scratch(int(L.ax_matmul_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
+    _check(L.ax_matmul(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(y_out), _ptr(z_out), *_ws_args(ws),
+                       _stream_ptr(stream)))
+    return y_out, z_out
+
+
+def ax_matmul_q8(x, x_scales, w, w_scales, bias=None, residual=None, act="none", out_dtype=torch.bfloat16, y_out=None,
+                 workspace=None, stream=None):
+    """y = act((x * x_scales) (w * w_scales)^T + bias) + residual on int8 codes: x [M,K] with a scale a row (what
+    ax_rmsnorm_q8 returns), w [N,K] with a scale a row."""
+    L = lib()
+    for t, name in ((x, "x"), (w, "w")):
+        if t.dtype != torch.int8:
+            raise TypeError("%s must have dtype torch.int8, got %s" % (name, t.dtype))
+    d = _matmul_desc(x, w, act, True, out_dtype)
+    _vec_of(x_scales, torch.float32, d.M, "x_scales")
+    _vec_of(w_scales, torch.float32, d.N, "w_scales")
+    y_out = _matmul_out(d, y_out, x, out_dtype, "y_out")
+    _epilogue_args(d, bias, residual, out_dtype)
+    ws = _scratch(int(L.ax_matmul_q8_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
+    _check(L.ax_matmul_q8(ctypes.byref(d), _ptr(x), _ptr(x_scales), _ptr(w), _ptr(w_scales), _ptr(bias), _ptr(residual),
+                          _ptr(y_out), *_ws_args(ws), _stream_ptr(stream)))
+    return y_out
+
+
+def ax_matmul_backward(gy, x, w, z=None, act="none", transposed=False, gx_out=None, gw_out=None, gb_out=None, workspace=None,
+                       stream=None):
+    """Gradients of ax_matmul: (gx, gw, gb), gb float32; False skips one.  z: the value before the activation."""
+    L = lib()
+    d = _matmul_desc(x, w, act, transposed, x.dtype)
+    d.y_ld = _mat_of(gy, x.dtype, d.M, d.N, "gy")
+    if z is not None:
+        _vec_of(z, x.dtype, d.M * d.N, "z")
+    elif d.act:
+        raise ValueError("the gradient of an activation needs z")
+    if d.act == 0 and gy.data_ptr() % 16:
+        d.unaligned = 1
+    gx_out = _grad_out(gx_out, x, "gx_out", d.x_ld)
+    gw_out = _grad_out(gw_out, w, "gw_out", d.w_ld)
+    if gb_out is None:
+        gb_out = torch.empty(d.N, dtype=torch.float32, device=x.device)
+    elif gb_out is not False:
+        _vec_of(gb_out, torch.float32, d.N, "gb_out")
+    gb_out = None if gb_out is False else gb_out
+    ws = _scratch(int(L.ax_matmul_backward_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
+    _check(L.ax_matmul_backward(ctypes.byref(d), _ptr(gy), _ptr(x), _ptr(w), _ptr(z), _ptr(gx_out), _ptr(gw_out), _ptr(gb_out),
+                                *_ws_args(ws), _stream_ptr(stream)))
+    return gx_out, gw_out, gb_out
+
+
+def _grad_out(out, like, name, ld):
+    """A gradient with the shape and the row pitch of the tensor that it belongs to."""
+    if out is False:
+        return None
+    if out is None:
+        return torch.empty_strided(like.shape, like.stride(), dtype=like.dtype, device=like.device)
+    r, c, _ = _mat(like, like.dtype, name)
+    if _mat_of(out, like.dtype, r, c, name) != ld:
+        raise ValueError("%s must have the row pitch of its tensor" % name)
+    return out
+
+
+def _gated_desc(x, wg, wu, act, transposed, out_dtype) -> ax_matmul_desc_t:
+    d = _matmul_desc(x, wg, act, transposed, out_dtype, ("x", "wg"))
+    wr, wc, ld = _mat(wu, x.dtype, "wu")
+    if wu.shape != wg.shape or ld != d.w_ld:
+        raise ValueError("wg and wu must have one shape and one row pitch")
+    if wu.data_ptr() % 16:
+        d.unaligned = 1
+    return d
+
+
+def ax_gated(x, wg, wu, act="silu", out_dtype=None, save=False, h_out=None, g_out=None, u_out=None, workspace=None, stream=None):
+    """h = act(x wg) * (x wu).  x [M,K]; wg, wu [K,F]; float32 or bfloat16.  Returns (h, g, u): both projections with
+    save (or g_out and u_out), otherwise None."""
+    L = lib()
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    d = _gated_desc(x, wg, wu, act, False, out_dtype)
+    h_out = _matmul_out(d, h_out, x, out_dtype, "h_out")
+    if save:
+        g_out, u_out = (torch.empty(x.shape[:-1] + (d.N,), dtype=out_dtype, device=x.device) if o is None else o
+                        for o in (g_out, u_out))
+    for o, name in ((g_out, "g_out"), (u_out, "u_out")):
+        if o is not None:
+            _vec_of(o, out_dtype, d.M * d.N, name)
+    ws = _scratch(int(L.ax_gated_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
+    _check(L.ax_gated(ctypes.byref(d), _ptr(x), _ptr(wg), _ptr(wu), _ptr(h_out), _ptr(g_out), _ptr(u_out), *_ws_args(ws),
+                      _stream_ptr(stream)))
+    return h_out, g_out, u_out
+
+
+def ax_gated_q8(x, x_scales, wg, wg_scales, wu, wu_scales, act="silu", out_dtype=torch.bfloat16, h_out=None, workspace=None,
+                stream=None):
+    """The gated block on int8 codes: x [M,K] and wg, wu [F,K], each with a scale a row."""
+    L = lib()
+    for t, name in ((x, "x"), (wg, "wg"), (wu, "wu")):
+        if t.dtype != torch.int8:
+            raise TypeError("%s must have dtype torch.int8, got %s" % (name, t.dtype))
+    d = _gated_desc(x, wg, wu, act, True, out_dtype)
+    _vec_of(x_scales, torch.float32, d.M, "x_scales")
+    _vec_of(wg_scales, torch.float32, d.N, "wg_scales")
+    _vec_of(wu_scales, torch.float32, d.N, "wu_scales")
+    h_out = _matmul_out(d, h_out, x, out_dtype, "h_out")
+    ws = _scratch(int(L.ax_gated_q8_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
+    _check(L.ax_gated_q8(ctypes.byref(d), _ptr(x), _ptr(x_scales), _ptr(wg), _ptr(wg_scales), _ptr(wu), _ptr(wu_scales),
+                         _ptr(h_out), *_ws_args(ws), _stream_ptr(stream)))
+    return h_out
+
+
+def ax_gated_backward(gh, x, wg, wu, g, u, act="silu", gx_out=None, gwg_out=None, gwu_out=None, workspace=None, stream=None):
+    """Gradients of ax_gated: (gx, gwg, gwu); gx_out False, or gwg_out and gwu_out False, skips them."""
+    L = lib()
+    d = _gated_desc(x, wg, wu, act, False, x.dtype)
+    d.y_ld = _mat_of(gh, x.dtype, d.M, d.N, "gh")
+    _vec_of(g, x.dtype, d.M * d.N, "g")
+    _vec_of(u, x.dtype, d.M * d.N, "u")
+    gx_out = _grad_out(gx_out, x, "gx_out", d.x_ld)
+    gwg_out = _grad_out(gwg_out, wg, "gwg_out", d.w_ld)
+    gwu_out = _grad_out(gwu_out, wu, "gwu_out", d.w_ld)
+    ws = _scratch(int(L.ax_gated_backward_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
+    _check(L.ax_gated_backward(ctypes.byref(d), _ptr(gh), _ptr(x), _ptr(wg), _ptr(wu), _ptr(g), _ptr(u), _ptr(gx_out),
+                               _ptr(gwg_out), _ptr(gwu_out), *_ws_args(ws), _stream_ptr(stream)))
+    return gx_out, gwg_out, gwu_out
+
+
+class AxAdamW:
+    """The AdamW step over a list of tensors (ax_adamw), with the list checked and marshalled once.
+
+    params, grads: lists of contiguous tensors, each list of one type (float32 or bfloat16).  States: None, None allocates
+    them (bits = 32 or 8); otherwise lists m and v, float32, or int8 and uint8 codes together with their scales m_scales and
+    v_scales (ceil(n / 256) float32 a tensor).  copies: bfloat16 tensors that receive the updated parameters as well.
+    The tensors are held, and their addresses used, until the object is dropped; set_grads exchanges the gradients."""
+
+    def __init__(self, params, grads, m=None, v=None, m_scales=None, v_scales=None, copies=None, bits=32):
+        self.params, self.copies = list(params), None if copies is None else list(copies)
+        n = len(self.params)
+        if not n:
+            raise ValueError("no parameters")
+        dev, pdt = self.params[0].device, self.params[0].dtype
+        sizes = [t.numel() for t in self.params]
+        blocks = [-(-k // AX_STATE_BLOCK) for k in sizes]
+        if (m is None) != (v is None) or (m_scales is None) != (v_scales is None):
+            raise ValueError("both states or neither, both lists of scales or neither")
+        if m is None:
+            if bits not in (32, 8) or m_scales is not None:
+                raise ValueError("bits must be 32 or 8, and scales come with their codes")
+            make = lambda shapes, dt: [torch.zeros(s, dtype=dt, device=dev) for s in shapes]  # noqa: E731
+            shapes = [t.shape for t in self.params]
+            if bits == 8:
+                m, v = make(shapes, torch.int8), make(shapes, torch.uint8)
+                m_scales, v_scales = make(blocks, torch.float32), make(blocks, torch.float32)
+            else:
+                m, v = make(shapes, torch.float32), make(shapes, torch.float32)
+        self.bits = 32 if m_scales is None else 8
+        self.m, self.v = list(m), list(v)
+        self.m_scales, self.v_scales = (None if s is None else list(s) for s in (m_scales, v_scales))
+        mt, vt = (torch.int8, torch.uint8) if self.bits == 8 else (torch.float32, torch.float32)
+        for what, ts, dt, counts in (("params", self.params, pdt, sizes), ("m", self.m, mt, sizes), ("v", self.v, vt, sizes),
+                                     ("m_scales", self.m_scales, torch.float32, blocks),
+                                     ("v_scales", self.v_scales, torch.float32, blocks),
+                                     ("copies", self.copies, torch.bfloat16, sizes)):
+            if ts is None:
+                continue
+            if len(ts) != n:
+                raise ValueError("%s must hold %d tensors" % (what, n))
+            for t, k in zip(ts, counts):
+                _vec_of(t, dt, k, what)
+        self._d = ax_adamw_desc_t()
+        self._d.p_dtype, self._d.state_bits = _float_dtype(self.params[0], "params"), self.bits
+        self._t = (ax_adamw_tensor_t * n)()
+        for i, e in enumerate(self._t):
+            e.p, e.m, e.v, e.n = self.params[i].data_ptr(), self.m[i].data_ptr(), self.v[i].data_ptr(), sizes[i]
+            if self.bits == 8:
+                e.m_scale, e.v_scale = self.m_scales[i].data_ptr(), self.v_scales[i].data_ptr()
+            if self.copies is not None:
+                e.copy = self.copies[i].data_ptr()
+        self.set_grads(grads)
+
+    def set_grads(self, grads):
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError("grads must hold %d tensors" % len(self.params))
+        for t, p in zip(grads, self.params):
+            _vec_of(t, grads[0].dtype, p.numel(), "grads")
+        self._d.g_dtype = _float_dtype(grads[0], "grads")
+        for e, t in zip(self._t, grads):
+            e.g = t.data_ptr()
+        self.grads = grads
+
+    def step(self, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, grad_scale=None, stream=None):
+        """One step, the step-th (from 1).  grad_scale: None, or a float32 CUDA tensor of one element that multiplies the
+        gradients (what clipping by a norm that was computed on the device gives)."""
+        d = self._d
+        d.lr, d.beta1, d.beta2, d.eps, d.weight_decay, d.step = lr, beta1, beta2, eps, weight_decay, int(step)
+        if grad_scale is not None:
+            _vec_of(grad_scale, torch.float32, 1, "grad_scale")
+        d.grad_scale = _ptr(grad_scale)
+        _check(lib().ax_adamw(ctypes.byref(d), self._t, len(self._t), _stream_ptr(stream)))
+
+    def states(self, stream=None):
+        """(m, v) as lists of float32 tensors: the values that 8-bit states stand for, or the 32-bit states themselves."""
+        if self.bits == 32:
+            return self.m, self.v
+        out = [[torch.empty(t.shape, dtype=torch.float32, device=t.device) for t in self.params] for _ in range(2)]
+        ptrs = [(ctypes.c_void_p * len(o))(*[t.data_ptr() for t in o]) for o in out]
+        _check(lib().ax_adamw_states(self._t, len(self._t), ptrs[0], ptrs[1], _stream_ptr(stream)))
+        return out[0], out[1]
 
 
 def ax_probe_lds_gather(width_bytes: int, pattern: int, table_bytes: int, threads: int = 1024, iters: int = 2000,

@@ -1,0 +1,642 @@
+// Matrix products with a fused epilogue, the gated feed-forward block, and their gradients: validation, operand
+// preparation and the launches of ax_gemm.hip.
+//
+//   z = x w + bias,  y = act(z) + residual         gz = gy act'(z),  gx = gz w^T,  gw = x^T gz,  gb = sum of gz
+//   g = x wg,  u = x wu,  h = act(g) u             gg = gh u act'(g),  gu = gh act(g),  gx = gg wg^T + gu wu^T, ...
+//
+// The matrix instructions take bf16 (or int8) operands.  float32 operands are cut into three bf16 pieces,
+// a = a1 + a2 + a3 exactly (eight significant bits each), and the product runs over the six pairs of pieces whose
+// product can reach 2^-24 of a b, smallest first, as six segments of one contraction: 6 / 16 of the cost of the float32
+// matrix instruction, at its precision.
+#include <algorithm>
+
+#include "ax_float.h"
+#include "ax_gemm.h"
+#include "ax_norm.h"
+
+namespace ax {
+namespace {
+
+constexpr size_t kAlign = 256;
+
+// Hands out pieces of the workspace; with base 0 it only counts.
+struct Arena {
+  uintptr_t base;
+  size_t used = 0;
+  explicit Arena(void* p) : base((uintptr_t)p) {}
+  void* take(size_t bytes) {
+    void* p = (void*)(base + used);
+    used += (bytes + kAlign - 1) / kAlign * kAlign;
+    return p;
+  }
+};
+
+inline int elem_bytes(int dtype) { return dtype == AX_F32 ? 4 : 2; }
+
+// A matrix as the products read it: planes of bf16 (or int8) rows whose length is a multiple of 16 bytes.
+struct Operand {
+  const void* p[3];
+  int planes;      // 3 for float32
+  long long ld;    // bytes
+  long long cols;  // row length, rounded up to whole 16-byte chunks (zeros behind the given columns)
+};
+
+struct PackJob {
+  const void* src;
+  void* dst;  // planes back to back; null: read in place
+  long long rows, cols, ld;  // of the source, elements
+  long long pcols;
+  int dtype;  // AX_F32, AX_BF16, or kI8
+};
+constexpr int kI8 = 2;
+
+// a = p0 + p1 + p2 exactly: each piece is what is left, cut after eight significant bits.  An infinity or a NaN goes into
+// the first piece alone; what it meets comes out as NaN or infinity (not always the one that float32 gives: a piece of the
+// other factor may be zero).
+__device__ __forceinline__ void split3(float a, uint32_t& p0, uint32_t& p1, uint32_t& p2) {
+  const uint32_t b = __float_as_uint(a);
+  if ((b & 0x7f800000u) == 0x7f800000u) {
+    p0 = (b >> 16) | ((b & 0x7fffffu) ? 0x40u : 0u);
+    p1 = p2 = 0;
+    return;
+  }
+  const float r1 = a - __uint_as_float(b & 0xffff0000u);
+  const uint32_t b1 = __float_as_uint(r1);
+  const float r2 = r1 - __uint_as_float(b1 & 0xffff0000u);
+  p0 = b >> 16;
+  p1 = b1 >> 16;
+  p2 = __float_as_uint(r2) >> 16;
+}
+
+// Rows copied into the form the products read: eight elements (16 bytes of output; int8: 16) a thread.  Bound by
+// memory: 4 bytes read and 6 written per float32 element.
+template <int DT>
+__global__ __launch_bounds__(256) void pack_kernel(const void* __restrict__ src, void* __restrict__ dst, long long rows,
+                                                    long long cols, long long ld, long long pcols) {
+  constexpr int E = DT == kI8 ? 16 : 8;
+  const long long groups = pcols / E, total = rows * groups;
+  const bool wide = DT == AX_F32 && ((uintptr_t)src & 15) == 0 && (ld & 3) == 0;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+    const long long r = i / groups, c = (i - r * groups) * E;
+    const long long left = cols - c;
+    if (DT == AX_F32) {
+      const float* s = (const float*)src + r * ld + c;
+      float v[8];
+      if (wide && left >= 8) {
+        const float4 a = *(const float4*)s, b = *(const float4*)(s + 4);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      } else {
+        for (int e = 0; e < 8; ++e) v[e] = e < left ? s[e] : 0.f;
+      }
+      uint32_t q[3][4];
+      for (int e = 0; e < 4; ++e) {
+        uint32_t a[3], b[3];
+        split3(v[2 * e], a[0], a[1], a[2]);
+        split3(v[2 * e + 1], b[0], b[1], b[2]);
+        for (int k = 0; k < 3; ++k) q[k][e] = a[k] | (b[k] << 16);
+      }
+      for (int k = 0; k < 3; ++k)
+        *(uint4*)((uint16_t*)dst + (k * rows + r) * pcols + c) = make_uint4(q[k][0], q[k][1], q[k][2], q[k][3]);
+    } else if (DT == AX_BF16) {
+      const uint16_t* s = (const uint16_t*)src + r * ld + c;
+      uint32_t q[4];
+      for (int e = 0; e < 4; ++e)
+        q[e] = (2 * e < left ? (uint32_t)s[2 * e] : 0u) | ((2 * e + 1 < left ? (uint32_t)s[2 * e + 1] : 0u) << 16);
+      *(uint4*)((uint16_t*)dst + r * pcols + c) = make_uint4(q[0], q[1], q[2], q[3]);
+    } else {
+      const uint8_t* s = (const uint8_t*)src + r * ld + c;
+      uint32_t q[4];
+      for (int e = 0; e < 4; ++e) {
+        q[e] = 0;
+        for (int b = 0; b < 4; ++b) q[e] |= (4 * e + b < left ? (uint32_t)s[4 * e + b] : 0u) << (8 * b);
+      }
+      *(uint4*)((uint8_t*)dst + r * pcols + c) = make_uint4(q[0], q[1], q[2], q[3]);
+    }
+  }
+}
+
+int grid_for(long long items) { return (int)std::max<long long>(1, std::min<long long>((items + 255) / 256, 8192)); }
+
+hipError_t run_pack(const PackJob& j, hipStream_t s) {
+  if (!j.dst || j.rows == 0) return hipSuccess;
+  const int grid = grid_for(j.rows * (j.pcols / (j.dtype == kI8 ? 16 : 8)));
+  if (j.dtype == AX_F32) pack_kernel<AX_F32><<<grid, 256, 0, s>>>(j.src, j.dst, j.rows, j.cols, j.ld, j.pcols);
+  else if (j.dtype == AX_BF16) pack_kernel<AX_BF16><<<grid, 256, 0, s>>>(j.src, j.dst, j.rows, j.cols, j.ld, j.pcols);
+  else pack_kernel<kI8><<<grid, 256, 0, s>>>(j.src, j.dst, j.rows, j.cols, j.ld, j.pcols);
+  return hipGetLastError();
+}
+
+// Whether the matrix is read in place or copied is decided by its description alone, so that the workspace query knows.
+Operand make_operand(const void* p, long long rows, long long cols, long long ld, int dtype, bool unaligned, Arena& ar, PackJob* job) {
+  Operand o{};
+  const int chunk = dtype == kI8 ? 16 : 8, esz = dtype == kI8 ? 1 : 2;
+  const long long pcols = (cols + chunk - 1) / chunk * chunk;
+  *job = PackJob{p, nullptr, rows, cols, ld, pcols, dtype};
+  o.cols = pcols;
+  if (dtype != AX_F32 && !unaligned && pcols == cols && ld % chunk == 0) {
+    o.planes = 1;
+    o.p[0] = p;
+    o.ld = ld * esz;
+    return o;
+  }
+  o.planes = dtype == AX_F32 ? 3 : 1;
+  o.ld = pcols * esz;
+  const size_t plane = (size_t)rows * pcols * esz;
+  job->dst = ar.take(plane * o.planes);
+  for (int k = 0; k < o.planes; ++k) o.p[k] = (const char*)job->dst + k * plane;
+  return o;
+}
+
+// Factor pairs of a product of two operands: one, or six pairs of pieces, smallest products first.
+void add_segments(GemmArgs* g, const Operand& a, const Operand& b, const Operand* b2) {
+  if (a.planes == 1) {
+    g->seg[g->nseg++] = GemmSeg{a.p[0], b.p[0], b2 ? b2->p[0] : nullptr};
+    return;
+  }
+  static const int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
+  for (int i = 0; i < 6; ++i) g->seg[g->nseg++] = GemmSeg{a.p[pa[i]], b.p[pb[i]], b2 ? b2->p[pb[i]] : nullptr};
+}
+
+// ---- elementwise part of the gradients ---------------------------------------------------------------------------
+//
+// gz = gy act'(z) (GATED: gg and gu) in the form the products read, and the sums of gz over blocks of rows.  A
+// workgroup takes 256 columns (eight a thread) and `rows_per` rows, eight at a time.  Bound by memory.
+struct GradArgs {
+  const void* gy;  // [M, N], pitch ldy (GATED: gh)
+  const void* z;   // [M, N], pitch N (may be NULL; GATED: the gate projection)
+  const void* u;   // GATED
+  void* gz;        // planes [M, pcols] (may be NULL: gy itself is read by the products)
+  void* gu;        // GATED
+  float* part;     // [row blocks][N] (may be NULL)
+  long long ldy, pcols;
+  int M, N, act, rows_per;
+};
+
+template <int DT>
+__device__ __forceinline__ void read8(const void* p, long long i, bool wide, int left, float (&v)[8]) {
+  if (wide && left >= 8) {
+    if (DT == AX_F32) {
+      const float4 a = *(const float4*)((const float*)p + i), b = *(const float4*)((const float*)p + i + 4);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+      const uint4 a = *(const uint4*)((const uint16_t*)p + i);
+      const uint32_t q[4] = {a.x, a.y, a.z, a.w};
+      for (int e = 0; e < 4; ++e) {
+        v[2 * e] = bf16_to_f32(q[e] & 0xffffu);
+        v[2 * e + 1] = bf16_to_f32(q[e] >> 16);
+      }
+    }
+    return;
+  }
+  for (int e = 0; e < 8; ++e)
+    v[e] = e >= left ? 0.f : DT == AX_F32 ? ((const float*)p)[i + e] : bf16_to_f32(((const uint16_t*)p)[i + e]);
+}
+template <int DT>
+__device__ __forceinline__ void write_planes(void* dst, long long rows, long long pcols, long long r, long long c, const float (&v)[8]) {
+  if (DT == AX_F32) {
+    uint32_t q[3][4];
+    for (int e = 0; e < 4; ++e) {
+      uint32_t a[3], b[3];
+      split3(v[2 * e], a[0], a[1], a[2]);
+      split3(v[2 * e + 1], b[0], b[1], b[2]);
+      for (int k = 0; k < 3; ++k) q[k][e] = a[k] | (b[k] << 16);
+    }
+    for (int k = 0; k < 3; ++k)
+      *(uint4*)((uint16_t*)dst + (k * rows + r) * pcols + c) = make_uint4(q[k][0], q[k][1], q[k][2], q[k][3]);
+  } else {
+    *(uint4*)((uint16_t*)dst + r * pcols + c) =
+        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  }
+}
+
+template <int DT, bool GATED>
+__global__ __launch_bounds__(256) void act_grad_kernel(const GradArgs a) {
+  const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
+  const long long c = ((long long)blockIdx.x * 32 + cx) * 8;
+  const int r0 = blockIdx.y * a.rows_per, r1 = min(a.M, r0 + a.rows_per);
+  const int left = (int)max(0ll, min(8ll, a.N - c));
+  constexpr int am = 15, lm = DT == AX_F32 ? 3 : 7;
+  const bool wy = ((uintptr_t)a.gy & am) == 0 && (a.ldy & lm) == 0;
+  const bool wz = ((uintptr_t)a.z & am) == 0 && (a.N & lm) == 0, wu = ((uintptr_t)a.u & am) == 0 && (a.N & lm) == 0;
+  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (c < a.pcols) {
+    for (int r = r0 + ry; r < r1; r += 8) {
+      float gy[8], z[8], u[8];
+      read8<DT>(a.gy, (long long)r * a.ldy + c, wy, left, gy);
+      if (GATED || a.z) read8<DT>(a.z, (long long)r * a.N + c, wz, left, z);
+      if (GATED) {
+        float gu[8];
+        read8<DT>(a.u, (long long)r * a.N + c, wu, left, u);
+        for (int e = 0; e < 8; ++e) {
+          gu[e] = gy[e] * act_of(z[e], a.act);
+          gy[e] = gy[e] * u[e] * act_slope(z[e], a.act);
+        }
+        write_planes<DT>(a.gu, a.M, a.pcols, r, c, gu);
+      } else if (a.z) {
+        for (int e = 0; e < 8; ++e) gy[e] *= act_slope(z[e], a.act);
+      }
+      if (a.gz) write_planes<DT>(a.gz, a.M, a.pcols, r, c, gy);
+      if (!GATED)
+        for (int e = 0; e < 8; ++e) sum[e] += gy[e];
+    }
+  }
+  if (GATED || !a.part) return;
+  __shared__ float red[8][32][9];
+  for (int e = 0; e < 8; ++e) red[ry][cx][e] = sum[e];
+  __syncthreads();
+  const int x = threadIdx.x >> 3, e = threadIdx.x & 7;
+  const long long col = ((long long)blockIdx.x * 32 + x) * 8 + e;
+  if (col >= a.N) return;
+  float t = 0.f;
+  for (int y = 0; y < 8; ++y) t += red[y][x][e];
+  a.part[(long long)blockIdx.y * a.N + col] = t;
+}
+
+// rows x cols elements of `bytes` bytes at pitch ld set to zero.
+__global__ __launch_bounds__(256) void zero_rows_kernel(uint8_t* p, long long rows, long long row_bytes, long long ld_bytes) {
+  const long long total = rows * (row_bytes / 2);
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+    const long long r = i / (row_bytes / 2);
+    *(uint16_t*)(p + r * ld_bytes + (i - r * (row_bytes / 2)) * 2) = 0;
+  }
+}
+
+int rows_per_block(int M, int N) {  // about eight workgroups per compute unit, at least eight rows each
+  const long long cols = (N + 255) / 256;
+  const long long want = std::max(1ll, 2048 / cols);
+  return (int)std::max(8ll, ((M + want - 1) / want + 7) / 8 * 8);
+}
+
+// ---- checks ------------------------------------------------------------------------------------------------------
+
+constexpr long long kMaxDim = 0x7fffffff, kMaxPitch = 1 << 22;
+
+bool dtype_ok(int d) { return d == AX_F32 || d == AX_BF16; }
+bool pitch_ok(long long ld, long long cols, int esz) { return ld >= cols && ld * esz < kMaxPitch; }
+
+int check_desc(const ax_matmul_desc_t* d, bool q8, bool backward, bool gated) {
+  if (!d) return AX_ERR_NULL;
+  if (!dtype_ok(d->out_dtype) || (!q8 && !dtype_ok(d->dtype))) return AX_ERR_OPTION;
+  if (backward && d->out_dtype != d->dtype) return AX_ERR_OPTION;
+  if (d->act < AX_ACT_NONE || d->act > AX_ACT_GELU) return AX_ERR_OPTION;
+  if ((d->w_transposed & ~1) || (d->unaligned & ~1)) return AX_ERR_OPTION;
+  if (q8 && !d->w_transposed) return AX_ERR_OPTION;
+  if (gated && !q8 && d->w_transposed) return AX_ERR_OPTION;
+  if (d->M < 0 || d->N < 1 || d->K < 1 || d->M > kMaxDim || d->N > kMaxDim || d->K > kMaxDim) return AX_ERR_SHAPE;
+  const int e = q8 ? 1 : elem_bytes(d->dtype), oe = elem_bytes(d->out_dtype);
+  if (!pitch_ok(d->x_ld, d->K, e) || !pitch_ok(d->w_ld, d->w_transposed ? d->K : d->N, e) || !pitch_ok(d->y_ld, d->N, oe)) return AX_ERR_SHAPE;
+  if (q8 && d->K > 131071) return AX_ERR_K_OVERFLOW;  // 131072 * 128 * 128 = 2^31
+  return AX_OK;
+}
+// 16-byte operands where the description promises them, element alignment otherwise.
+bool operand_aligned(const void* p, int esz, bool unaligned, long long cols, long long ld, int dtype) {
+  if ((uintptr_t)p % esz) return false;
+  const int chunk = 16 / esz;
+  const bool in_place = dtype != AX_F32 && !unaligned && cols % chunk == 0 && ld % chunk == 0;
+  return !in_place || (uintptr_t)p % 16 == 0;
+}
+bool aligned_to(const void* p, int esz) { return (uintptr_t)p % esz == 0; }
+bool ws_ok(const void* ws, size_t have, size_t need) {
+  return need == 0 || (ws && (uintptr_t)ws % kAlign == 0 && have >= need);
+}
+
+// ---- forward -----------------------------------------------------------------------------------------------------
+
+struct Forward {
+  PackJob jobs[3];
+  int njobs;
+  GemmArgs g;
+  GemmPlan plan;
+  void* part;
+  size_t bytes;
+};
+
+Forward make_forward(const ax_matmul_desc_t* d, bool q8, bool gated, const void* x, const void* w, const void* w2, void* ws) {
+  Forward f{};
+  Arena ar(ws);
+  const int dt = q8 ? kI8 : d->dtype;
+  const long long wr = d->w_transposed ? d->N : d->K, wc = d->w_transposed ? d->K : d->N;
+  const Operand a = make_operand(x, d->M, d->K, d->x_ld, dt, d->unaligned, ar, &f.jobs[0]);
+  const Operand b = make_operand(w, wr, wc, d->w_ld, dt, d->unaligned, ar, &f.jobs[1]);
+  Operand b2{};
+  f.njobs = 2;
+  if (gated) b2 = make_operand(w2, wr, wc, d->w_ld, dt, d->unaligned, ar, &f.jobs[f.njobs++]);
+  GemmArgs& g = f.g;
+  add_segments(&g, a, b, gated ? &b2 : nullptr);
+  g.i8 = q8;
+  g.la = 0;
+  g.lb = d->w_transposed ? 0 : 1;
+  g.M = (int)d->M;
+  g.N = (int)d->N;
+  // contraction: whole chunks where both operands have them contiguous (zeros behind the end), rows of w otherwise
+  g.K = (int)(d->w_transposed ? a.cols : d->K);
+  g.lda = a.ld;
+  g.ldb = b.ld;
+  g.gated = gated;
+  g.odt = d->out_dtype;
+  g.act = d->act;
+  g.ldy = d->y_ld;
+  g.ldr = d->residual_ld;
+  f.plan = plan_gemm(g);
+  f.part = ar.take(f.plan.part_bytes);
+  f.bytes = ar.used;
+  return f;
+}
+
+int run_forward(Forward& f, hipStream_t s) {
+  for (int i = 0; i < f.njobs; ++i)
+    if (run_pack(f.jobs[i], s) != hipSuccess) return AX_ERR_HIP;
+  return launch_gemm(f.g, f.plan, f.part, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
+}
+
+// ---- backward ----------------------------------------------------------------------------------------------------
+
+struct Backward {
+  PackJob jobs[3];  // x, w, wu
+  GradArgs ga;
+  bool elementwise;  // act_grad_kernel runs for the products (it runs for gb alone too)
+  int row_blocks;
+  float* part;       // of gb
+  GemmArgs gx, gw;
+  GemmPlan px, pw;
+  void *partx, *partw;
+  size_t bytes;
+};
+
+Backward make_backward(const ax_matmul_desc_t* d, bool gated, const void* gy, const void* x, const void* w, const void* w2,
+                       const void* z, const void* u, void* ws) {
+  Backward b{};
+  Arena ar(ws);
+  const int dt = d->dtype;
+  const long long wr = d->w_transposed ? d->N : d->K, wc = d->w_transposed ? d->K : d->N;
+  const Operand ox = make_operand(x, d->M, d->K, d->x_ld, dt, d->unaligned, ar, &b.jobs[0]);
+  const Operand ow = make_operand(w, wr, wc, d->w_ld, dt, d->unaligned, ar, &b.jobs[1]);
+  Operand ow2{};
+  if (gated) ow2 = make_operand(w2, wr, wc, d->w_ld, dt, d->unaligned, ar, &b.jobs[2]);
+  // gz as an operand: gy itself where nothing is multiplied to it and it can be read in place
+  PackJob unused;
+  Operand oz{}, ou{};
+  const bool plain = !gated && d->act == AX_ACT_NONE;
+  const bool in_place = plain && dt == AX_BF16 && !d->unaligned && d->N % 8 == 0 && d->y_ld % 8 == 0;
+  const long long pcols = (d->N + 7) / 8 * 8;
+  if (in_place) {
+    oz = make_operand(gy, d->M, d->N, d->y_ld, dt, false, ar, &unused);
+  } else {  // (unaligned: a buffer of its own)
+    oz = make_operand(gy, d->M, d->N, d->y_ld, dt, true, ar, &unused);
+    b.ga.gz = unused.dst;
+    if (gated) {
+      ou = make_operand(gy, d->M, d->N, d->y_ld, dt, true, ar, &unused);
+      b.ga.gu = unused.dst;
+    }
+  }
+  b.elementwise = !in_place;
+  b.ga.gy = gy;
+  b.ga.z = plain ? nullptr : z;
+  b.ga.u = u;
+  b.ga.ldy = d->y_ld;
+  b.ga.pcols = pcols;
+  b.ga.M = (int)d->M;
+  b.ga.N = (int)d->N;
+  b.ga.act = d->act;
+  b.ga.rows_per = rows_per_block((int)d->M, (int)d->N);
+  b.row_blocks = (int)((d->M + b.ga.rows_per - 1) / b.ga.rows_per);
+  if (!gated) b.part = (float*)ar.take((size_t)b.row_blocks * d->N * 4);
+
+  GemmArgs& gx = b.gx;  // gx [M, K] = gz [M, N] w^T
+  add_segments(&gx, oz, ow, nullptr);
+  if (gated) add_segments(&gx, ou, ow2, nullptr);
+  gx.la = 0;
+  gx.lb = d->w_transposed ? 1 : 0;
+  gx.M = (int)d->M;
+  gx.N = (int)d->K;
+  gx.K = (int)(d->w_transposed ? d->N : pcols);
+  gx.lda = oz.ld;
+  gx.ldb = ow.ld;
+  gx.odt = dt;
+  gx.ldy = d->x_ld;
+  b.px = plan_gemm(gx);
+
+  GemmArgs& gw = b.gw;  // gw [K, N] = x^T gz, or [N, K] = gz^T x
+  if (d->w_transposed) add_segments(&gw, oz, ox, nullptr);
+  else add_segments(&gw, ox, oz, gated ? &ou : nullptr);
+  gw.la = gw.lb = 1;
+  gw.M = (int)(d->w_transposed ? d->N : d->K);
+  gw.N = (int)(d->w_transposed ? d->K : d->N);
+  gw.K = (int)d->M;
+  gw.lda = d->w_transposed ? oz.ld : ox.ld;
+  gw.ldb = d->w_transposed ? ox.ld : oz.ld;
+  gw.dual = gated;
+  gw.odt = dt;
+  gw.ldy = d->w_ld;
+  if (d->M > 0) b.pw = plan_gemm(gw);
+  // one after the other on one stream: the partial sums may share their place
+  b.partx = b.partw = ar.take(std::max(b.px.part_bytes, b.pw.part_bytes));
+  b.bytes = ar.used;
+  return b;
+}
+
+template <bool GATED>
+hipError_t run_act_grad(const GradArgs& a, int row_blocks, int dtype, hipStream_t s) {
+  const dim3 grid((unsigned)((a.pcols + 255) / 256), (unsigned)row_blocks);
+  if (dtype == AX_F32) act_grad_kernel<AX_F32, GATED><<<grid, 256, 0, s>>>(a);
+  else act_grad_kernel<AX_BF16, GATED><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t zero_rows(void* p, long long rows, long long cols, long long ld, int esz, hipStream_t s) {
+  zero_rows_kernel<<<grid_for(rows * cols * esz / 2), 256, 0, s>>>((uint8_t*)p, rows, cols * esz, ld * esz);
+  return hipGetLastError();
+}
+
+int backward_common(const ax_matmul_desc_t* d, bool gated, const void* gy, const void* x, const void* w, const void* w2,
+                    const void* z, const void* u, void* gx_out, void* gw_out, void* gw2_out, float* gb_out, void* ws,
+                    size_t ws_bytes, hipStream_t s) {
+  const int esz = elem_bytes(d->dtype);
+  const long long wr = d->w_transposed ? d->N : d->K, wc = d->w_transposed ? d->K : d->N;
+  if (d->M == 0) {
+    hipError_t rc = hipSuccess;
+    for (void* p : {gw_out, gw2_out})
+      if (p && rc == hipSuccess) rc = zero_rows(p, wr, wc, d->w_ld, esz, s);
+    if (gb_out && rc == hipSuccess) rc = zero_rows(gb_out, 1, d->N, d->N, 4, s);
+    return rc == hipSuccess ? AX_OK : AX_ERR_HIP;
+  }
+  Backward b = make_backward(d, gated, gy, x, w, w2, z, u, ws);
+  if (!ws_ok(ws, ws_bytes, b.bytes)) return AX_ERR_WORKSPACE;
+  const bool products = gx_out || gw_out;
+  if (gw_out && run_pack(b.jobs[0], s) != hipSuccess) return AX_ERR_HIP;
+  if (gx_out && run_pack(b.jobs[1], s) != hipSuccess) return AX_ERR_HIP;
+  if (gx_out && gated && run_pack(b.jobs[2], s) != hipSuccess) return AX_ERR_HIP;
+  if (gated) {
+    if (run_act_grad<true>(b.ga, b.row_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
+  } else if ((b.elementwise && products) || gb_out) {
+    if (!products) b.ga.gz = nullptr;
+    b.ga.part = gb_out ? b.part : nullptr;
+    if (run_act_grad<false>(b.ga, b.row_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
+    if (gb_out) {
+      if (launch_column_sum(b.part, b.row_blocks, (int)d->N, gb_out, s) != hipSuccess) return AX_ERR_HIP;
+    }
+  }
+  if (gx_out) {
+    b.gx.y = gx_out;
+    if (launch_gemm(b.gx, b.px, b.partx, s) != hipSuccess) return AX_ERR_HIP;
+  }
+  if (gw_out) {
+    b.gw.y = gw_out;
+    b.gw.y2 = gw2_out;
+    if (launch_gemm(b.gw, b.pw, b.partw, s) != hipSuccess) return AX_ERR_HIP;
+  }
+  return AX_OK;
+}
+
+}  // namespace
+}  // namespace ax
+
+using namespace ax;
+
+extern "C" size_t ax_matmul_workspace_bytes(const ax_matmul_desc_t* d) {
+  if (check_desc(d, false, false, false) != AX_OK || d->M == 0) return 0;
+  return make_forward(d, false, false, nullptr, nullptr, nullptr, nullptr).bytes;
+}
+
+extern "C" int ax_matmul(const ax_matmul_desc_t* d, const void* x, const void* w, const void* bias, const void* residual,
+                         void* y_out, void* z_out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (int rc = check_desc(d, false, false, false)) return rc;
+  if (residual && !pitch_ok(d->residual_ld, d->N, elem_bytes(d->out_dtype))) return AX_ERR_SHAPE;
+  if (d->M == 0) return AX_OK;
+  if (!x || !w || !y_out) return AX_ERR_NULL;
+  const int e = elem_bytes(d->dtype), oe = elem_bytes(d->out_dtype);
+  if (!operand_aligned(x, e, d->unaligned, d->K, d->x_ld, d->dtype) ||
+      !operand_aligned(w, e, d->unaligned, d->w_transposed ? d->K : d->N, d->w_ld, d->dtype))
+    return AX_ERR_ALIGN;
+  for (const void* p : {bias, residual, (const void*)y_out, (const void*)z_out})
+    if (!aligned_to(p, oe)) return AX_ERR_ALIGN;
+  Forward f = make_forward(d, false, false, x, w, nullptr, workspace);
+  if (!ws_ok(workspace, workspace_bytes, f.bytes)) return AX_ERR_WORKSPACE;
+  f.g.y = y_out;
+  f.g.z = z_out;
+  f.g.bias = bias;
+  f.g.res = residual;
+  return run_forward(f, (hipStream_t)hip_stream);
+}
+
+extern "C" size_t ax_matmul_q8_workspace_bytes(const ax_matmul_desc_t* d) {
+  if (check_desc(d, true, false, false) != AX_OK || d->M == 0) return 0;
+  return make_forward(d, true, false, nullptr, nullptr, nullptr, nullptr).bytes;
+}
+
+extern "C" int ax_matmul_q8(const ax_matmul_desc_t* d, const int8_t* x, const float* x_scales, const int8_t* w,
+                            const float* w_scales, const void* bias, const void* residual, void* y_out, void* workspace,
+                            size_t workspace_bytes, void* hip_stream) {
+  if (int rc = check_desc(d, true, false, false)) return rc;
+  if (residual && !pitch_ok(d->residual_ld, d->N, elem_bytes(d->out_dtype))) return AX_ERR_SHAPE;
+  if (d->M == 0) return AX_OK;
+  if (!x || !x_scales || !w || !w_scales || !y_out) return AX_ERR_NULL;
+  const int oe = elem_bytes(d->out_dtype);
+  if (!operand_aligned(x, 1, d->unaligned, d->K, d->x_ld, kI8) || !operand_aligned(w, 1, d->unaligned, d->K, d->w_ld, kI8) ||
+      !aligned_to(x_scales, 4) || !aligned_to(w_scales, 4))
+    return AX_ERR_ALIGN;
+  for (const void* p : {bias, residual, (const void*)y_out})
+    if (!aligned_to(p, oe)) return AX_ERR_ALIGN;
+  Forward f = make_forward(d, true, false, x, w, nullptr, workspace);
+  if (!ws_ok(workspace, workspace_bytes, f.bytes)) return AX_ERR_WORKSPACE;
+  f.g.y = y_out;
+  f.g.bias = bias;
+  f.g.res = residual;
+  f.g.xs = x_scales;
+  f.g.ws = w_scales;
+  return run_forward(f, (hipStream_t)hip_stream);
+}
+
+extern "C" size_t ax_matmul_backward_workspace_bytes(const ax_matmul_desc_t* d) {
+  if (check_desc(d, false, true, false) != AX_OK || d->M == 0) return 0;
+  return make_backward(d, false, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr).bytes;
+}
+
+extern "C" int ax_matmul_backward(const ax_matmul_desc_t* d, const void* gy, const void* x, const void* w, const void* z,
+                                  void* gx_out, void* gw_out, float* gb_out, void* workspace, size_t workspace_bytes,
+                                  void* hip_stream) {
+  if (int rc = check_desc(d, false, true, false)) return rc;
+  if (!gx_out && !gw_out && !gb_out) return AX_ERR_NULL;
+  if (d->M > 0 && (!gy || (gw_out && !x) || (gx_out && !w) || (d->act != AX_ACT_NONE && !z))) return AX_ERR_NULL;
+  const int e = elem_bytes(d->dtype);
+  if (!operand_aligned(x, e, d->unaligned, d->K, d->x_ld, d->dtype) ||
+      !operand_aligned(w, e, d->unaligned, d->w_transposed ? d->K : d->N, d->w_ld, d->dtype) ||
+      !operand_aligned(gy, e, d->unaligned || d->act != AX_ACT_NONE, d->N, d->y_ld, d->dtype))
+    return AX_ERR_ALIGN;
+  for (const void* p : {z, (const void*)gx_out, (const void*)gw_out})
+    if (!aligned_to(p, e)) return AX_ERR_ALIGN;
+  if (!aligned_to(gb_out, 4)) return AX_ERR_ALIGN;
+  return backward_common(d, false, gy, x, w, nullptr, z, nullptr, gx_out, gw_out, nullptr, gb_out, workspace, workspace_bytes,
+                         (hipStream_t)hip_stream);
+}
+
+extern "C" size_t ax_gated_workspace_bytes(const ax_matmul_desc_t* d) {
+  if (check_desc(d, false, false, true) != AX_OK || d->M == 0) return 0;
+  return make_forward(d, false, true, nullptr, nullptr, nullptr, nullptr).bytes;
+}
+
+extern "C" int ax_gated(const ax_matmul_desc_t* d, const void* x, const void* wg, const void* wu, void* h_out, void* g_out,
+                        void* u_out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (int rc = check_desc(d, false, false, true)) return rc;
+  if (!g_out != !u_out) return AX_ERR_NULL;
+  if (d->M == 0) return AX_OK;
+  if (!x || !wg || !wu || !h_out) return AX_ERR_NULL;
+  const int e = elem_bytes(d->dtype), oe = elem_bytes(d->out_dtype);
+  if (!operand_aligned(x, e, d->unaligned, d->K, d->x_ld, d->dtype)) return AX_ERR_ALIGN;
+  for (const void* p : {wg, wu})
+    if (!operand_aligned(p, e, d->unaligned, d->N, d->w_ld, d->dtype)) return AX_ERR_ALIGN;
+  for (const void* p : {(const void*)h_out, (const void*)g_out, (const void*)u_out})
+    if (!aligned_to(p, oe)) return AX_ERR_ALIGN;
+  Forward f = make_forward(d, false, true, x, wg, wu, workspace);
+  if (!ws_ok(workspace, workspace_bytes, f.bytes)) return AX_ERR_WORKSPACE;
+  f.g.y = h_out;
+  f.g.z = g_out;
+  f.g.z2 = u_out;
+  return run_forward(f, (hipStream_t)hip_stream);
+}
+
+extern "C" size_t ax_gated_q8_workspace_bytes(const ax_matmul_desc_t* d) {
+  if (check_desc(d, true, false, true) != AX_OK || d->M == 0) return 0;
+  return make_forward(d, true, true, nullptr, nullptr, nullptr, nullptr).bytes;
+}
+
+extern "C" int ax_gated_q8(const ax_matmul_desc_t* d, const int8_t* x, const float* x_scales, const int8_t* wg,
+                           const float* wg_scales, const int8_t* wu, const float* wu_scales, void* h_out, void* workspace,
+                           size_t workspace_bytes, void* hip_stream) {
+  if (int rc = check_desc(d, true, false, true)) return rc;
+  if (d->M == 0) return AX_OK;
+  if (!x || !x_scales || !wg || !wg_scales || !wu || !wu_scales || !h_out) return AX_ERR_NULL;
+  if (!operand_aligned(x, 1, d->unaligned, d->K, d->x_ld, kI8) || !aligned_to(x_scales, 4) || !aligned_to(wg_scales, 4) ||
+      !aligned_to(wu_scales, 4) || !aligned_to(h_out, elem_bytes(d->out_dtype)))
+    return AX_ERR_ALIGN;
+  for (const void* p : {(const void*)wg, (const void*)wu})
+    if (!operand_aligned(p, 1, d->unaligned, d->K, d->w_ld, kI8)) return AX_ERR_ALIGN;
+  Forward f = make_forward(d, true, true, x, wg, wu, workspace);
+  if (!ws_ok(workspace, workspace_bytes, f.bytes)) return AX_ERR_WORKSPACE;
+  f.g.y = h_out;
+  f.g.xs = x_scales;
+  f.g.ws = wg_scales;
+  f.g.ws2 = wu_scales;
+  return run_forward(f, (hipStream_t)hip_stream);
+}
+
+extern "C" size_t ax_gated_backward_workspace_bytes(const ax_matmul_desc_t* d) {
+  if (check_desc(d, false, true, true) != AX_OK || d->M == 0) return 0;
+  return make_backward(d, true, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr).bytes;
+}
+
+extern "C" int ax_gated_backward(const ax_matmul_desc_t* d, const void* gh, const void* x, const void* wg, const void* wu,
+                                 const void* g, const void* u, void* gx_out, void* gwg_out, void* gwu_out, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream) {
+  if (int rc = check_desc(d, false, true, true)) return rc;
+  if ((!gwg_out != !gwu_out) || (!gx_out && !gwg_out)) return AX_ERR_NULL;
+  if (d->M > 0 && (!gh || !g || !u || (gwg_out && !x) || (gx_out && (!wg || !wu)))) return AX_ERR_NULL;
+  const int e = elem_bytes(d->dtype);
+  if (!operand_aligned(x, e, d->unaligned, d->K, d->x_ld, d->dtype)) return AX_ERR_ALIGN;
+  for (const void* p : {wg, wu})
+    if (!operand_aligned(p, e, d->unaligned, d->N, d->w_ld, d->dtype)) return AX_ERR_ALIGN;
+  for (const void* p : {gh, g, u, (const void*)gx_out, (const void*)gwg_out, (const void*)gwu_out})
+    if (!aligned_to(p, e)) return AX_ERR_ALIGN;
+  return backward_common(d, true, gh, x, wg, wu, g, u, gx_out, gwg_out, gwu_out, nullptr, workspace, workspace_bytes,
+                         (hipStream_t)hip_stream);
+}

@@ -1,0 +1,591 @@
+// Root-mean-square norm of rows with the residual's addition, its output in 8-bit codes, and its gradients.
+//
+//   t = x + residual,  rstd = 1 / sqrt(mean t^2 + eps),  y = t rstd w
+//   codes = round(t w * (127 / max |t w|)),  scale = max |t w| * rstd / 127
+//   gx = rstd (gy w - h mean(gy w h)) + gsum,  gw = sum over rows of gy h,  h = t rstd
+//
+// All kernels are bound by memory.  One pass: a row's values stay in registers between the reduction and the output
+// (rows of up to 32768 columns; longer ones are read twice, the second time mostly from the caches).  Few rows get more
+// lanes each, since their time is the latency of one row.
+//
+// Codes are reproducible bit for bit: t, t w, the division and the product in front of the rounding are single float32
+// operations, the maximum is exact, and rstd, the only quantity that depends on the order of a sum, is in the scale alone.
+#include <algorithm>
+#include <cmath>
+
+#include "ax_float.h"
+#include "ax_internal.h"
+#include "ax_norm.h"
+
+#pragma clang fp contract(off)
+
+namespace ax {
+namespace {
+
+enum Mode { kValues, kCodes };
+
+struct NormArgs {
+  const void* x;
+  const void* res;  // may be null
+  const void* w;    // may be null (codes)
+  void* sum;        // may be null
+  void* y;
+  int8_t* codes;
+  float* scales;
+  float* values;  // may be null
+  float* rstd;    // may be null
+  long long rows;
+  long long x_ld, r_ld, s_ld, y_ld;
+  int cols, w_f32, normalize;
+  float eps;
+};
+
+// Eight elements of a row: contiguous where rows are wide-aligned, TPR apart otherwise (so that neighbouring lanes read
+// neighbouring elements either way).
+template <bool WIDE, int TPR>
+__device__ __forceinline__ int col_of(int it, int t, int e) {
+  return WIDE ? (it * TPR + t) * 8 + e : (it * 8 + e) * TPR + t;
+}
+template <bool WIDE, int TPR, bool F32>
+__device__ __forceinline__ void load_row(const void* p, long long row, int it, int t, int cols, float (&v)[8]) {
+  if (WIDE) {
+    const int c = (it * TPR + t) * 8;
+    if (c >= cols) {
+      for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    } else if (F32) {
+      const float4 a = *(const float4*)((const float*)p + row + c), b = *(const float4*)((const float*)p + row + c + 4);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+      const uint4 a = *(const uint4*)((const uint16_t*)p + row + c);
+      const uint32_t q[4] = {a.x, a.y, a.z, a.w};
+      for (int e = 0; e < 4; ++e) {
+        v[2 * e] = bf16_to_f32(q[e] & 0xffffu);
+        v[2 * e + 1] = bf16_to_f32(q[e] >> 16);
+      }
+    }
+  } else {
+    for (int e = 0; e < 8; ++e) {
+      const int c = col_of<WIDE, TPR>(it, t, e);
+      v[e] = c >= cols ? 0.f : F32 ? ((const float*)p)[row + c] : bf16_to_f32(((const uint16_t*)p)[row + c]);
+    }
+  }
+}
+template <bool WIDE, int TPR, bool F32>
+__device__ __forceinline__ void store_row(void* p, long long row, int it, int t, int cols, const float (&v)[8]) {
+  if (WIDE) {
+    const int c = (it * TPR + t) * 8;
+    if (c >= cols) return;
+    if (F32) {
+      *(float4*)((float*)p + row + c) = make_float4(v[0], v[1], v[2], v[3]);
+      *(float4*)((float*)p + row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+      *(uint4*)((uint16_t*)p + row + c) =
+          make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    }
+  } else {
+    for (int e = 0; e < 8; ++e) {
+      const int c = col_of<WIDE, TPR>(it, t, e);
+      if (c >= cols) continue;
+      if (F32) ((float*)p)[row + c] = v[e];
+      else ((uint16_t*)p)[row + c] = (uint16_t)f32_to_bf16(v[e]);
+    }
+  }
+}
+
+// Sum and largest value over the TPR lanes of a row, in a fixed order.  red: 2 * TPR / 64 words of LDS.
+template <int TPR>
+__device__ __forceinline__ void reduce_row(float& sum, uint32_t& top, float* red) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    sum += __shfl_xor(sum, off, 64);
+    top = max(top, (uint32_t)__shfl_xor((int)top, off, 64));
+  }
+  if (TPR == 64) return;
+  constexpr int W = TPR / 64;
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    red[wave] = sum;
+    red[W + wave] = __uint_as_float(top);
+  }
+  __syncthreads();
+  sum = 0.f;
+  top = 0;
+  for (int i = 0; i < W; ++i) {
+    sum += red[i];
+    top = max(top, __float_as_uint(red[W + i]));
+  }
+}
+
+// TPR lanes a row, NV passes of eight elements in registers (0: any number of columns, read twice).
+template <int MODE, bool F32, bool WIDE, int TPR, int NV>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const NormArgs a) {
+  constexpr int THREADS = TPR < 256 ? 256 : TPR;
+  __shared__ float red[2 * (TPR / 64)];
+  const int t = threadIdx.x % TPR;
+  const long long row = (long long)blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
+  if (row >= a.rows) return;  // uniform over a row's lanes (and over the workgroup where it has one row)
+  const long long xo = row * a.x_ld, ro = row * a.r_ld, so = row * a.s_ld, yo = row * a.y_ld, co = row * (long long)a.cols;
+  const int iters = NV ? NV : (a.cols + TPR * 8 - 1) / (TPR * 8);
+  float v[NV ? NV : 1][8], w[NV ? NV : 1][8];
+
+  auto load = [&](int it, float (&tv)[8], float (&wv)[8]) {
+    load_row<WIDE, TPR, F32>(a.x, xo, it, t, a.cols, tv);
+    if (a.res) {
+      float r[8];
+      load_row<WIDE, TPR, F32>(a.res, ro, it, t, a.cols, r);
+      for (int e = 0; e < 8; ++e) tv[e] += r[e];
+    }
+    if (a.w) {
+      if (a.w_f32) load_row<WIDE, TPR, true>(a.w, 0, it, t, a.cols, wv);
+      else load_row<WIDE, TPR, false>(a.w, 0, it, t, a.cols, wv);
+    } else {
+      for (int e = 0; e < 8; ++e) wv[e] = 1.f;
+    }
+  };
+  float ss = 0.f;
+  uint32_t top = 0;  // bit pattern of the largest |t w|: as integers, NaN is above infinity and both above all numbers
+  auto take = [&](int it, float (&tv)[8], float (&wv)[8]) {
+    for (int e = 0; e < 8; ++e) {
+      ss = __builtin_fmaf(tv[e], tv[e], ss);
+      if (MODE == kCodes) {
+        tv[e] = tv[e] * wv[e];
+        top = max(top, __float_as_uint(tv[e]) & 0x7fffffffu);
+      }
+    }
+  };
+  if (NV) {
+#pragma unroll
+    for (int it = 0; it < iters; ++it) load(it, v[it], w[it]);
+#pragma unroll
+    for (int it = 0; it < iters; ++it) {
+      if (a.sum) store_row<WIDE, TPR, F32>(a.sum, so, it, t, a.cols, v[it]);
+      take(it, v[it], w[it]);
+    }
+  } else {
+    for (int it = 0; it < iters; ++it) {
+      load(it, v[0], w[0]);
+      take(it, v[0], w[0]);
+    }
+  }
+  reduce_row<TPR>(ss, top, red);
+  const float rstd = a.normalize ? 1.f / sqrtf(ss / (float)a.cols + a.eps) : 1.f;
+  const float amax = __uint_as_float(top);
+  const float inv = amax >= 0x1p-120f && top < 0x7f800000u ? 127.f / amax : 0.f;
+  const float scale = amax * rstd / 127.f;
+  if (t == 0) {
+    if (a.rstd) a.rstd[row] = rstd;
+    if (MODE == kCodes) a.scales[row] = scale;
+  }
+  auto put = [&](int it, const float (&tv)[8], const float (&wv)[8]) {
+    if (MODE == kValues) {
+      float y[8];
+      for (int e = 0; e < 8; ++e) y[e] = tv[e] * rstd * wv[e];
+      store_row<WIDE, TPR, F32>(a.y, yo, it, t, a.cols, y);
+    } else {
+      float c[8];
+      for (int e = 0; e < 8; ++e) c[e] = inv > 0.f ? rintf(tv[e] * inv) : 0.f;
+      if (WIDE) {
+        const int col = (it * TPR + t) * 8;
+        if (col < a.cols) {
+          uint32_t q[2] = {0, 0};
+          for (int e = 0; e < 8; ++e) q[e >> 2] |= ((uint32_t)(int)c[e] & 0xffu) << (8 * (e & 3));
+          *(uint2*)(a.codes + co + col) = make_uint2(q[0], q[1]);
+        }
+      } else {
+        for (int e = 0; e < 8; ++e) {
+          const int col = col_of<WIDE, TPR>(it, t, e);
+          if (col < a.cols) a.codes[co + col] = (int8_t)(int)c[e];
+        }
+      }
+      if (a.values) {
+        for (int e = 0; e < 8; ++e) c[e] *= scale;
+        store_row<WIDE, TPR, true>(a.values, co, it, t, a.cols, c);
+      }
+    }
+  };
+  if (NV) {
+#pragma unroll
+    for (int it = 0; it < iters; ++it) put(it, v[it], w[it]);
+  } else {
+    for (int it = 0; it < iters; ++it) {
+      load(it, v[0], w[0]);
+      // (sum may be x or the residual: written only now, behind this lane's last read of the place)
+      if (a.sum) store_row<WIDE, TPR, F32>(a.sum, so, it, t, a.cols, v[0]);
+      if (MODE == kCodes)
+        for (int e = 0; e < 8; ++e) v[0][e] = v[0][e] * w[0][e];
+      put(it, v[0], w[0]);
+    }
+  }
+}
+
+struct NormGradArgs {
+  const void* gy;
+  const void* gsum;  // may be null
+  const void* t;
+  const void* w;
+  const float* rstd;
+  void* gx;     // may be null
+  float* part;  // [workgroups][cols], may be null
+  long long rows;
+  long long t_ld, gs_ld, gx_ld, gy_ld;
+  int cols, w_f32;
+};
+
+// A workgroup takes every gridDim.x-th group of THREADS / TPR rows and keeps its share of gw in registers until the end.
+template <bool F32, bool WIDE, int TPR, int NV>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(const NormGradArgs a) {
+  constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
+  __shared__ float red[2 * 2 * (TPR / 64)];
+  __shared__ float share[ROWS > 1 ? NV * 8 * THREADS : 1];
+  const int t = threadIdx.x % TPR;
+  float gw[NV][8], w[NV][8];
+#pragma unroll
+  for (int it = 0; it < NV; ++it) {
+    if (a.w_f32) load_row<WIDE, TPR, true>(a.w, 0, it, t, a.cols, w[it]);
+    else load_row<WIDE, TPR, false>(a.w, 0, it, t, a.cols, w[it]);
+    for (int e = 0; e < 8; ++e) gw[it][e] = 0.f;
+  }
+  int turn = 0;
+  for (long long base = (long long)blockIdx.x * ROWS; base < a.rows; base += (long long)gridDim.x * ROWS) {
+    const long long row = base + threadIdx.x / TPR;
+    if (ROWS > 1 && row >= a.rows) break;  // uniform over the wave, which has the row to itself
+    const float rstd = a.rstd[row];
+    float gy[NV][8], h[NV][8];
+#pragma unroll
+    for (int it = 0; it < NV; ++it) {
+      load_row<WIDE, TPR, F32>(a.gy, row * a.gy_ld, it, t, a.cols, gy[it]);
+      load_row<WIDE, TPR, F32>(a.t, row * a.t_ld, it, t, a.cols, h[it]);
+    }
+    float dot = 0.f;
+#pragma unroll
+    for (int it = 0; it < NV; ++it)
+      for (int e = 0; e < 8; ++e) {
+        h[it][e] = h[it][e] * rstd;
+        gw[it][e] = __builtin_fmaf(gy[it][e], h[it][e], gw[it][e]);
+        gy[it][e] = gy[it][e] * w[it][e];
+        dot = __builtin_fmaf(gy[it][e], h[it][e], dot);
+      }
+    if (!a.gx) continue;  // uniform
+    uint32_t none = 0;
+    // two turns' words apart: a wave may write the next row's while another still reads this one's
+    reduce_row<TPR>(dot, none, red + turn * 2 * (TPR / 64));
+    turn ^= 1;
+    const float mean = dot / (float)a.cols;
+#pragma unroll
+    for (int it = 0; it < NV; ++it) {
+      float o[8];
+      for (int e = 0; e < 8; ++e) o[e] = rstd * (gy[it][e] - h[it][e] * mean);
+      if (a.gsum) {
+        float s[8];
+        load_row<WIDE, TPR, F32>(a.gsum, row * a.gs_ld, it, t, a.cols, s);
+        for (int e = 0; e < 8; ++e) o[e] += s[e];
+      }
+      store_row<WIDE, TPR, F32>(a.gx, row * a.gx_ld, it, t, a.cols, o);
+    }
+  }
+  if (!a.part) return;
+  if (ROWS > 1) {  // the waves' shares, in their order
+#pragma unroll
+    for (int it = 0; it < NV; ++it)
+      for (int e = 0; e < 8; ++e) share[(it * 8 + e) * THREADS + threadIdx.x] = gw[it][e];
+    __syncthreads();
+    if (threadIdx.x >= TPR) return;
+#pragma unroll
+    for (int it = 0; it < NV; ++it)
+      for (int e = 0; e < 8; ++e)
+        for (int r = 1; r < ROWS; ++r) gw[it][e] += share[(it * 8 + e) * THREADS + r * TPR + t];
+  }
+#pragma unroll
+  for (int it = 0; it < NV; ++it) {
+    for (int e = 0; e < 8; ++e) {
+      const int c = col_of<WIDE, TPR>(it, t, e);
+      if (c < a.cols) a.part[(long long)blockIdx.x * a.cols + c] = gw[it][e];
+    }
+  }
+}
+
+// Rows of more columns than a workgroup's registers hold: one pass for the row's mean, one for the outputs; gw from a
+// kernel of its own.
+template <bool F32>
+__global__ __launch_bounds__(1024) void norm_grad_long_kernel(const NormGradArgs a) {
+  constexpr int TPR = 1024;
+  __shared__ float red[2 * (TPR / 64)];
+  const int t = threadIdx.x;
+  const long long row = blockIdx.x;
+  const float rstd = a.rstd[row];
+  const int iters = (a.cols + TPR * 8 - 1) / (TPR * 8);
+  float dot = 0.f;
+  for (int pass = 0; pass < 2; ++pass) {
+    const float mean = dot / (float)a.cols;
+    for (int it = 0; it < iters; ++it) {
+      float gy[8], h[8], w[8];
+      load_row<false, TPR, F32>(a.gy, row * a.gy_ld, it, t, a.cols, gy);
+      load_row<false, TPR, F32>(a.t, row * a.t_ld, it, t, a.cols, h);
+      if (a.w_f32) load_row<false, TPR, true>(a.w, 0, it, t, a.cols, w);
+      else load_row<false, TPR, false>(a.w, 0, it, t, a.cols, w);
+      for (int e = 0; e < 8; ++e) {
+        h[e] = h[e] * rstd;
+        gy[e] = gy[e] * w[e];
+        if (pass == 0) dot = __builtin_fmaf(gy[e], h[e], dot);
+      }
+      if (pass == 1) {
+        for (int e = 0; e < 8; ++e) gy[e] = rstd * (gy[e] - h[e] * mean);
+        if (a.gsum) {
+          load_row<false, TPR, F32>(a.gsum, row * a.gs_ld, it, t, a.cols, w);
+          for (int e = 0; e < 8; ++e) gy[e] += w[e];
+        }
+        store_row<false, TPR, F32>(a.gx, row * a.gx_ld, it, t, a.cols, gy);
+      }
+    }
+    if (pass == 0) {
+      uint32_t none = 0;
+      reduce_row<TPR>(dot, none, red);
+    }
+  }
+}
+template <bool F32>
+__global__ __launch_bounds__(256) void norm_gw_long_kernel(const NormGradArgs a) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= a.cols) return;
+  float s = 0.f;
+  for (long long row = blockIdx.y; row < a.rows; row += gridDim.y) {
+    const long long g = row * a.gy_ld + c, x = row * a.t_ld + c;
+    const float gy = F32 ? ((const float*)a.gy)[g] : bf16_to_f32(((const uint16_t*)a.gy)[g]);
+    const float t = F32 ? ((const float*)a.t)[x] : bf16_to_f32(((const uint16_t*)a.t)[x]);
+    s = __builtin_fmaf(gy, t * a.rstd[row], s);
+  }
+  a.part[(long long)blockIdx.y * a.cols + c] = s;
+}
+
+// out[c] = sum over the rows of part: 64 lanes a column, 16 columns a workgroup.
+__global__ __launch_bounds__(1024) void column_sum_kernel(const float* __restrict__ part, int rows, int cols, float* __restrict__ out) {
+  __shared__ float red[64][17];
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+  const int c = blockIdx.x * 16 + x;
+  float s = 0.f;
+  if (c < cols)
+    for (int r = y; r < rows; r += 64) s += part[(long long)r * cols + c];
+  red[y][x] = s;
+  __syncthreads();
+  for (int h = 32; h > 0; h >>= 1) {
+    if (y < h) red[y][x] += red[y + h][x];
+    __syncthreads();
+  }
+  if (y == 0 && c < cols) out[c] = red[0][x];
+}
+
+// ---- dispatch ----------------------------------------------------------------------------------------------------
+
+// Lanes a row and passes: as few lanes as hold the row in four passes; four times as many for few rows, whose time is one row's latency
+// rather than bandwidth.
+struct Shape {
+  int tpr, nv;
+};
+Shape shape_of(long long rows, long long cols) {
+  const bool few = rows <= 512;
+  if (cols <= (few ? 512 : 2048)) return {64, (int)((cols + 511) / 512)};
+  if (cols <= (few ? 2048 : 8192)) return {256, (int)((cols + 2047) / 2048)};
+  if (cols <= 32768) return {1024, (int)((cols + 8191) / 8192)};
+  return {1024, 0};
+}
+
+template <int MODE, bool F32, bool WIDE>
+void norm_launch(const NormArgs& a, hipStream_t s) {
+  const Shape sh = shape_of(a.rows, a.cols);
+  const int per = sh.tpr == 64 ? 4 : 1;
+  const unsigned grid = (unsigned)((a.rows + per - 1) / per);
+  const int threads = sh.tpr < 256 ? 256 : sh.tpr;
+#define AX_NORM(T, V) norm_kernel<MODE, F32, WIDE, T, V><<<grid, threads, 0, s>>>(a)
+#define AX_NORM_T(T)                         \
+  switch (sh.nv) {                           \
+    case 1: AX_NORM(T, 1); break;            \
+    case 2: AX_NORM(T, 2); break;            \
+    default: AX_NORM(T, 4); break;           \
+  }
+  if (sh.nv == 0) AX_NORM(1024, 0);
+  else if (sh.tpr == 64) AX_NORM_T(64)
+  else if (sh.tpr == 256) AX_NORM_T(256)
+  else AX_NORM_T(1024)
+#undef AX_NORM_T
+#undef AX_NORM
+}
+template <bool F32, bool WIDE>
+void norm_grad_launch(const NormGradArgs& a, const Shape& sh, int groups, hipStream_t s) {
+  const int threads = sh.tpr < 256 ? 256 : sh.tpr;
+#define AX_NG(T, V) norm_grad_kernel<F32, WIDE, T, V><<<groups, threads, 0, s>>>(a)
+#define AX_NG_T(T)                           \
+  switch (sh.nv) {                           \
+    case 1: AX_NG(T, 1); break;              \
+    case 2: AX_NG(T, 2); break;              \
+    default: AX_NG(T, 4); break;             \
+  }
+  if (sh.tpr == 64) AX_NG_T(64)
+  else if (sh.tpr == 256) AX_NG_T(256)
+  else if (sh.nv == 1) AX_NG(1024, 1);
+  else AX_NG(1024, 2);
+#undef AX_NG_T
+#undef AX_NG
+}
+
+bool wide_ptr(const void* p, long long ld, int esz) { return (uintptr_t)p % 16 == 0 && (ld * esz) % 16 == 0; }
+
+// The gradient keeps four values a column in registers: 1024 lanes hold 16384 columns.
+bool grad_is_long(const Shape& sh) { return sh.nv == 0 || (sh.tpr == 1024 && sh.nv > 2); }
+
+int grad_groups(long long rows, long long cols) {
+  const Shape sh = shape_of(rows, cols);
+  if (grad_is_long(sh)) return (int)std::min<long long>(rows, 64);
+  const long long per = sh.tpr == 64 ? 4 : 1;
+  return (int)std::min<long long>((rows + per - 1) / per, sh.tpr == 1024 ? 512 : 1024);
+}
+
+int check_norm(const ax_norm_desc_t* d) {
+  if (!d) return AX_ERR_NULL;
+  if ((d->dtype != AX_F32 && d->dtype != AX_BF16) || (d->w_dtype != AX_F32 && d->w_dtype != AX_BF16)) return AX_ERR_OPTION;
+  if (d->normalize & ~1) return AX_ERR_OPTION;
+  if (!(d->eps >= 0.f) || !std::isfinite(d->eps)) return AX_ERR_OPTION;
+  if (d->rows < 0 || d->cols < 1 || d->rows > 0x7fffffff || d->cols > 0x7fffffff - 32768) return AX_ERR_SHAPE;
+  return AX_OK;
+}
+
+bool aligned_to(const void* p, int esz) { return (uintptr_t)p % esz == 0; }
+
+int norm_common(const ax_norm_desc_t* d, NormArgs& a, bool codes, hipStream_t s) {
+  const int e = d->dtype == AX_F32 ? 4 : 2, we = d->w_dtype == AX_F32 ? 4 : 2;
+  if (d->x_ld < d->cols || (a.res && d->residual_ld < d->cols) || (a.sum && d->sum_ld < d->cols) ||
+      (a.y && d->y_ld < d->cols))
+    return AX_ERR_SHAPE;
+  if (d->rows == 0) return AX_OK;
+  if (!a.x || (a.sum && !a.res)) return AX_ERR_NULL;
+  for (const void* p : {a.x, a.res, (const void*)a.sum, (const void*)a.y})
+    if (!aligned_to(p, e)) return AX_ERR_ALIGN;
+  for (const void* p : {(const void*)a.scales, (const void*)a.values, (const void*)a.rstd})
+    if (!aligned_to(p, 4)) return AX_ERR_ALIGN;
+  if (!aligned_to(a.w, we)) return AX_ERR_ALIGN;
+  a.rows = d->rows;
+  a.cols = (int)d->cols;
+  a.x_ld = d->x_ld;
+  a.r_ld = d->residual_ld;
+  a.s_ld = d->sum_ld;
+  a.y_ld = d->y_ld;
+  a.w_f32 = d->w_dtype == AX_F32;
+  a.normalize = d->normalize;
+  a.eps = d->eps;
+  const bool wide = d->cols % 8 == 0 && wide_ptr(a.x, a.x_ld, e) && (!a.res || wide_ptr(a.res, a.r_ld, e)) &&
+                    (!a.sum || wide_ptr(a.sum, a.s_ld, e)) && (!a.y || wide_ptr(a.y, a.y_ld, e)) &&
+                    (!a.w || wide_ptr(a.w, 0, we)) && (!a.codes || (uintptr_t)a.codes % 8 == 0) &&
+                    (!a.values || wide_ptr(a.values, d->cols, 4));
+  const bool f32 = d->dtype == AX_F32;
+  if (codes) {
+    if (f32) wide ? norm_launch<kCodes, true, true>(a, s) : norm_launch<kCodes, true, false>(a, s);
+    else wide ? norm_launch<kCodes, false, true>(a, s) : norm_launch<kCodes, false, false>(a, s);
+  } else {
+    if (f32) wide ? norm_launch<kValues, true, true>(a, s) : norm_launch<kValues, true, false>(a, s);
+    else wide ? norm_launch<kValues, false, true>(a, s) : norm_launch<kValues, false, false>(a, s);
+  }
+  return hipGetLastError() == hipSuccess ? AX_OK : AX_ERR_HIP;
+}
+
+}  // namespace
+
+hipError_t launch_column_sum(const float* part, int rows, int cols, float* out, hipStream_t s) {
+  column_sum_kernel<<<(cols + 15) / 16, 1024, 0, s>>>(part, rows, cols, out);
+  return hipGetLastError();
+}
+
+}  // namespace ax
+
+using namespace ax;
+
+extern "C" int ax_rmsnorm(const ax_norm_desc_t* d, const void* x, const void* residual, const void* weight, void* sum_out,
+                          void* y_out, float* rstd_out, void* hip_stream) {
+  if (int rc = check_norm(d)) return rc;
+  if (!d->normalize) return AX_ERR_OPTION;
+  if (d->rows > 0 && (!weight || !y_out)) return AX_ERR_NULL;
+  NormArgs a{};
+  a.x = x;
+  a.res = residual;
+  a.w = weight;
+  a.sum = sum_out;
+  a.y = y_out;
+  a.rstd = rstd_out;
+  return norm_common(d, a, false, (hipStream_t)hip_stream);
+}
+
+extern "C" int ax_rmsnorm_q8(const ax_norm_desc_t* d, const void* x, const void* residual, const void* weight, void* sum_out,
+                             int8_t* codes_out, float* scales_out, float* values_out, void* hip_stream) {
+  if (int rc = check_norm(d)) return rc;
+  if (d->rows > 0 && (!codes_out || !scales_out)) return AX_ERR_NULL;
+  NormArgs a{};
+  a.x = x;
+  a.res = residual;
+  a.w = weight;
+  a.sum = sum_out;
+  a.codes = codes_out;
+  a.scales = scales_out;
+  a.values = values_out;
+  return norm_common(d, a, true, (hipStream_t)hip_stream);
+}
+
+extern "C" size_t ax_rmsnorm_backward_workspace_bytes(const ax_norm_desc_t* d) {
+  if (check_norm(d) != AX_OK || d->rows == 0) return 0;
+  return ((size_t)grad_groups(d->rows, d->cols) * d->cols * 4 + 255) / 256 * 256;
+}
+
+extern "C" int ax_rmsnorm_backward(const ax_norm_desc_t* d, const void* gy, const void* gsum, const void* t, const void* weight,
+                                   const float* rstd, void* gx_out, float* gw_out, void* workspace, size_t workspace_bytes,
+                                   void* hip_stream) {
+  if (int rc = check_norm(d)) return rc;
+  if (!d->normalize) return AX_ERR_OPTION;
+  if (!gx_out && !gw_out) return AX_ERR_NULL;
+  if (d->x_ld < d->cols || d->y_ld < d->cols || (gsum && d->residual_ld < d->cols) || (gx_out && d->sum_ld < d->cols))
+    return AX_ERR_SHAPE;
+  const int e = d->dtype == AX_F32 ? 4 : 2, we = d->w_dtype == AX_F32 ? 4 : 2;
+  for (const void* p : {gy, gsum, t, (const void*)gx_out})
+    if (!aligned_to(p, e)) return AX_ERR_ALIGN;
+  if (!aligned_to(weight, we) || !aligned_to(rstd, 4) || !aligned_to(gw_out, 4)) return AX_ERR_ALIGN;
+  const hipStream_t s = (hipStream_t)hip_stream;
+  if (d->rows == 0) {  // no rows: their sum
+    if (gw_out && launch_column_sum(gw_out, 0, (int)d->cols, gw_out, s) != hipSuccess) return AX_ERR_HIP;
+    return AX_OK;
+  }
+  if (!gy || !t || !weight || !rstd) return AX_ERR_NULL;
+  if (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < ax_rmsnorm_backward_workspace_bytes(d)) return AX_ERR_WORKSPACE;
+  NormGradArgs a{};
+  a.gy = gy;
+  a.gsum = gsum;
+  a.t = t;
+  a.w = weight;
+  a.rstd = rstd;
+  a.gx = gx_out;
+  a.part = gw_out ? (float*)workspace : nullptr;
+  a.rows = d->rows;
+  a.t_ld = d->x_ld;
+  a.gs_ld = d->residual_ld;
+  a.gx_ld = d->sum_ld;
+  a.gy_ld = d->y_ld;
+  a.cols = (int)d->cols;
+  a.w_f32 = d->w_dtype == AX_F32;
+  const bool f32 = d->dtype == AX_F32;
+  const Shape sh = shape_of(d->rows, d->cols);
+  const int groups = grad_groups(d->rows, d->cols);
+  if (grad_is_long(sh)) {
+    if (gx_out) {
+      if (f32) norm_grad_long_kernel<true><<<(unsigned)d->rows, 1024, 0, s>>>(a);
+      else norm_grad_long_kernel<false><<<(unsigned)d->rows, 1024, 0, s>>>(a);
+    }
+    if (gw_out) {
+      const dim3 grid((a.cols + 255) / 256, groups);
+      if (f32) norm_gw_long_kernel<true><<<grid, 256, 0, s>>>(a);
+      else norm_gw_long_kernel<false><<<grid, 256, 0, s>>>(a);
+    }
+  } else {
+    const bool wide = d->cols % 8 == 0 && wide_ptr(gy, a.gy_ld, e) && wide_ptr(t, a.t_ld, e) && (!gsum || wide_ptr(gsum, a.gs_ld, e)) &&
+                      (!gx_out || wide_ptr(gx_out, a.gx_ld, e)) && wide_ptr(weight, 0, we);
+    if (f32) wide ? norm_grad_launch<true, true>(a, sh, groups, s) : norm_grad_launch<true, false>(a, sh, groups, s);
+    else wide ? norm_grad_launch<false, true>(a, sh, groups, s) : norm_grad_launch<false, false>(a, sh, groups, s);
+  }
+  if (hipGetLastError() != hipSuccess) return AX_ERR_HIP;
+  if (gw_out && launch_column_sum(a.part, groups, a.cols, gw_out, s) != hipSuccess) return AX_ERR_HIP;
+  return AX_OK;
+}
