@@ -41,43 +41,27 @@ struct Batch {
 };
 static_assert(sizeof(Batch) <= 4096, "kernel arguments");
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 template <bool F32>
-__device__ __forceinline__ f32x4 get4(const void* p, long long i, bool wide, int left) {
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (wide && left >= 4) {
-    if (F32) return *(const f32x4*)((const float*)p + i);
-    const uint2 q = *(const uint2*)((const uint16_t*)p + i);
-    return f32x4{bf16_to_f32(q.x & 0xffffu), bf16_to_f32(q.x >> 16), bf16_to_f32(q.y & 0xffffu), bf16_to_f32(q.y >> 16)};
-  }
-  for (int e = 0; e < 4; ++e)
-    if (e < left) v[e] = F32 ? ((const float*)p)[i + e] : bf16_to_f32(((const uint16_t*)p)[i + e]);
-  return v;
+__device__ __forceinline__ f32x4 get4(const void* p, long long i, int left) {
+  float v[4];
+  load_elems<F32, 4>(p, i, left, v);
+  return f32x4{v[0], v[1], v[2], v[3]};
 }
 template <bool F32>
-__device__ __forceinline__ void put4(void* p, long long i, bool wide, int left, const f32x4& v) {
-  if (wide && left >= 4) {
-    if (F32) *(f32x4*)((float*)p + i) = v;
-    else *(uint2*)((uint16_t*)p + i) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-    return;
-  }
-  for (int e = 0; e < 4; ++e)
-    if (e < left) {
-      if (F32) ((float*)p)[i + e] = v[e];
-      else ((uint16_t*)p)[i + e] = (uint16_t)f32_to_bf16(v[e]);
-    }
+__device__ __forceinline__ void put4(void* p, long long i, int left, const f32x4& v) {
+  const float t[4] = {v[0], v[1], v[2], v[3]};
+  store_elems<F32, 4>(p, i, left, t);
 }
-__device__ __forceinline__ uint32_t get_codes(const uint8_t* p, long long i, bool wide, int left) {
-  if (wide && left >= 4) return *(const uint32_t*)(p + i);
+__device__ __forceinline__ uint32_t get_codes(const uint8_t* p, long long i, int left) {
+  if (left >= 4) return load_any<uint32_t>(p + i);
   uint32_t q = 0;
   for (int e = 0; e < 4; ++e)
     if (e < left) q |= (uint32_t)p[i + e] << (8 * e);
   return q;
 }
-__device__ __forceinline__ void put_codes(uint8_t* p, long long i, bool wide, int left, uint32_t q) {
-  if (wide && left >= 4) {
-    *(uint32_t*)(p + i) = q;
+__device__ __forceinline__ void put_codes(uint8_t* p, long long i, int left, uint32_t q) {
+  if (left >= 4) {
+    store_any(p + i, q);
     return;
   }
   for (int e = 0; e < 4; ++e)
@@ -126,9 +110,6 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Batch b) {
   const long long base = (long long)(blockIdx.x - b.first[ti]) * kChunk;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const float gs = s.grad_scale ? *s.grad_scale : 1.f;
-  const bool wp = (uintptr_t)T.p % (PF32 ? 16 : 8) == 0, wg = (uintptr_t)T.g % (GF32 ? 16 : 8) == 0;
-  const bool wm = (uintptr_t)T.m % (Q8 ? 4 : 16) == 0, wv = (uintptr_t)T.v % (Q8 ? 4 : 16) == 0;
-  const bool wc = (uintptr_t)T.copy % 8 == 0;
 #pragma unroll
   for (int it = 0; it < kChunk / 1024; ++it) {
     // a wave's 256 elements of this pass are one block of the 8-bit states
@@ -136,14 +117,14 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Batch b) {
     const long long more = T.n - i;
     const int left = more >= 4 ? 4 : more > 0 ? (int)more : 0;
     if (T.n - (i - lane * 4) <= 0) break;  // uniform over the wave
-    f32x4 p = get4<PF32>(T.p, i, wp, left), g = get4<GF32>(T.g, i, wg, left), m, v;
+    f32x4 p = get4<PF32>(T.p, i, left), g = get4<GF32>(T.g, i, left), m, v;
     const long long blk = i / AX_STATE_BLOCK;
     if (Q8) {
-      m = decode_m(get_codes((const uint8_t*)T.m, i, wm, left), T.ms[blk]);
-      v = decode_v(get_codes((const uint8_t*)T.v, i, wv, left), T.vs[blk]);
+      m = decode_m(get_codes((const uint8_t*)T.m, i, left), T.ms[blk]);
+      v = decode_v(get_codes((const uint8_t*)T.v, i, left), T.vs[blk]);
     } else {
-      m = get4<true>(T.m, i, wm, left);
-      v = get4<true>(T.v, i, wv, left);
+      m = get4<true>(T.m, i, left);
+      v = get4<true>(T.v, i, left);
     }
     uint32_t tm = 0, tv = 0;
     for (int e = 0; e < 4; ++e) {
@@ -157,8 +138,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Batch b) {
         tv = max(tv, __float_as_uint(v[e]) & 0x7fffffffu);
       }
     }
-    put4<PF32>(T.p, i, wp, left, p);
-    if (T.copy) put4<false>(T.copy, i, wc, left, p);
+    put4<PF32>(T.p, i, left, p);
+    if (T.copy) put4<false>(T.copy, i, left, p);
     if (Q8) {
       const float sm = __uint_as_float(wave_max(tm)), sv = __uint_as_float(wave_max(tv));
       const float im = inverse_of(sm), iv = inverse_of(sv);
@@ -171,15 +152,15 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Batch b) {
         if (v[e] > 0.f && iv > 0.f) k = max(k, 1);
         qv |= ((uint32_t)k & 0xffu) << (8 * e);
       }
-      put_codes((uint8_t*)T.m, i, wm, left, qm);
-      put_codes((uint8_t*)T.v, i, wv, left, qv);
+      put_codes((uint8_t*)T.m, i, left, qm);
+      put_codes((uint8_t*)T.v, i, left, qv);
       if (lane == 0) {
         T.ms[blk] = sm;
         T.vs[blk] = sv;
       }
     } else {
-      put4<true>(T.m, i, wm, left, m);
-      put4<true>(T.v, i, wv, left, v);
+      put4<true>(T.m, i, left, m);
+      put4<true>(T.v, i, left, v);
     }
   }
 }
@@ -189,8 +170,6 @@ __global__ __launch_bounds__(kThreads) void states_kernel(const Batch b) {
   const int ti = tensor_of(b.first, blockIdx.x);
   const Tensor& T = b.t[ti];
   const long long base = (long long)(blockIdx.x - b.first[ti]) * kChunk;
-  const bool wm = (uintptr_t)T.m % 4 == 0, wv = (uintptr_t)T.v % 4 == 0;
-  const bool om = (uintptr_t)T.p % 16 == 0, ov = (uintptr_t)T.copy % 16 == 0;
 #pragma unroll
   for (int it = 0; it < kChunk / 1024; ++it) {
     const long long i = base + it * 1024 + threadIdx.x * 4;
@@ -198,8 +177,8 @@ __global__ __launch_bounds__(kThreads) void states_kernel(const Batch b) {
     const int left = more >= 4 ? 4 : more > 0 ? (int)more : 0;
     if (left == 0) break;
     const long long blk = i / AX_STATE_BLOCK;
-    put4<true>(T.p, i, om, left, decode_m(get_codes((const uint8_t*)T.m, i, wm, left), T.ms[blk]));
-    put4<true>(T.copy, i, ov, left, decode_v(get_codes((const uint8_t*)T.v, i, wv, left), T.vs[blk]));
+    put4<true>(T.p, i, left, decode_m(get_codes((const uint8_t*)T.m, i, left), T.ms[blk]));
+    put4<true>(T.copy, i, left, decode_v(get_codes((const uint8_t*)T.v, i, left), T.vs[blk]));
   }
 }
 

@@ -4,9 +4,20 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "axconv.h"
+#include "ax_internal.h"
 
 namespace ax {
+
+// Stores, like load_any, at an address of any alignment: rows of odd length start anywhere, and global memory takes
+// accesses of 16 bytes there too, at the cost of the extra lines that they touch.
+template <typename T>
+__device__ __forceinline__ void store_any(void* p, const T& v) {
+  __builtin_memcpy(p, &v, sizeof(T));
+}
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float bf16_to_f32(uint32_t b) { return __uint_as_float(b << 16); }
 // To nearest, ties to even; NaN stays NaN.
@@ -15,6 +26,53 @@ __device__ __forceinline__ uint32_t f32_to_bf16(float f) {
   return (uint32_t)__builtin_bit_cast(unsigned short, h);
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) { return f32_to_bf16(lo) | (f32_to_bf16(hi) << 16); }
+
+// E (4 or 8) elements from element i of p on, `left` of them in the row (zeros behind).
+template <bool F32, int E>
+__device__ __forceinline__ void load_elems(const void* p, long long i, int left, float (&v)[E]) {
+  if (left >= E) {
+    if (F32) {
+#pragma unroll
+      for (int h = 0; h < E / 4; ++h) {
+        const f32x4 t = load_any<f32x4>((const float*)p + i + 4 * h);
+        for (int e = 0; e < 4; ++e) v[4 * h + e] = t[e];
+      }
+    } else if (E == 8) {
+      const u32x4 t = load_any<u32x4>((const uint16_t*)p + i);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = bf16_to_f32((t[e >> 1] >> (16 * (e & 1))) & 0xffffu);
+    } else {
+      const u32x2 t = load_any<u32x2>((const uint16_t*)p + i);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = bf16_to_f32((t[(e >> 1) & 1] >> (16 * (e & 1))) & 0xffffu);
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    v[e] = e >= left ? 0.f : F32 ? ((const float*)p)[i + e] : bf16_to_f32(((const uint16_t*)p)[i + e]);
+}
+template <bool F32, int E>
+__device__ __forceinline__ void store_elems(void* p, long long i, int left, const float (&v)[E]) {
+  if (left >= E) {
+    if (F32) {
+#pragma unroll
+      for (int h = 0; h < E / 4; ++h) store_any((float*)p + i + 4 * h, f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]});
+    } else if (E == 8) {
+      store_any((uint16_t*)p + i, u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4 % E], v[5 % E]),
+                                        pack_bf16(v[6 % E], v[7 % E])});
+    } else {
+      store_any((uint16_t*)p + i, u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])});
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (e < left) {
+      if (F32) ((float*)p)[i + e] = v[e];
+      else ((uint16_t*)p)[i + e] = (uint16_t)f32_to_bf16(v[e]);
+    }
+}
 
 // Activations in float32: one exponential and one reciprocal (both good to a few units in the last place), against
 // results that are rounded to bf16 or compared at 2e-5.

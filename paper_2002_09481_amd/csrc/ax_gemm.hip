@@ -11,8 +11,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 #define AX_LDS(T) __attribute__((address_space(3))) T
 
@@ -30,88 +28,43 @@ struct Args {
 
 // ---- epilogue ----------------------------------------------------------------------------------
 
-__device__ __forceinline__ float load_elem(const void* p, long long i, int dt) {
-  return dt == AX_F32 ? ((const float*)p)[i] : bf16_to_f32(((const uint16_t*)p)[i]);
+__device__ __forceinline__ void load4(const void* p, long long i, int dt, int left, float (&v)[4]) {
+  if (dt == AX_F32) load_elems<true, 4>(p, i, left, v);
+  else load_elems<false, 4>(p, i, left, v);
 }
-__device__ __forceinline__ void load4(const void* p, long long i, int dt, bool vec, int left, float v[4]) {
-  if (vec) {
-    if (dt == AX_F32) {
-      const f32x4 t = *(const f32x4*)((const float*)p + i);
-      for (int e = 0; e < 4; ++e) v[e] = t[e];
-    } else {
-      const uint2 t = *(const uint2*)((const uint16_t*)p + i);
-      v[0] = bf16_to_f32(t.x & 0xffffu); v[1] = bf16_to_f32(t.x >> 16);
-      v[2] = bf16_to_f32(t.y & 0xffffu); v[3] = bf16_to_f32(t.y >> 16);
-    }
-  } else {
-    for (int e = 0; e < 4; ++e) v[e] = e < left ? load_elem(p, i + e, dt) : 0.f;
-  }
-}
-__device__ __forceinline__ void store4(void* p, long long i, int dt, bool vec, int left, const float v[4]) {
-  if (vec) {
-    if (dt == AX_F32) {
-      *(f32x4*)((float*)p + i) = f32x4{v[0], v[1], v[2], v[3]};
-    } else {
-      *(uint2*)((uint16_t*)p + i) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-    }
-  } else {
-    for (int e = 0; e < 4; ++e)
-      if (e < left) {
-        if (dt == AX_F32) ((float*)p)[i + e] = v[e];
-        else ((uint16_t*)p)[i + e] = (uint16_t)f32_to_bf16(v[e]);
-      }
-  }
-}
-
-// What of the epilogue allows four columns in one access.
-struct Wide {
-  bool y, y2, z, z2, res, bias;
-};
-__device__ __forceinline__ bool wide_ok(const void* p, long long ld, int dt) {
-  const int b = dt == AX_F32 ? 15 : 7;
-  return (((uintptr_t)p & b) == 0) && (ld & 3) == 0;
-}
-__device__ __forceinline__ Wide make_wide(const GemmArgs& g) {
-  Wide w;
-  w.y = wide_ok(g.y, g.ldy, g.odt);
-  w.y2 = wide_ok(g.y2, g.ldy, g.odt);
-  w.z = wide_ok(g.z, g.N, g.odt);
-  w.z2 = wide_ok(g.z2, g.N, g.odt);
-  w.res = wide_ok(g.res, g.ldr, g.odt);
-  w.bias = wide_ok(g.bias, 0, g.odt);
-  return w;
+__device__ __forceinline__ void store4(void* p, long long i, int dt, int left, const float (&v)[4]) {
+  if (dt == AX_F32) store_elems<true, 4>(p, i, left, v);
+  else store_elems<false, 4>(p, i, left, v);
 }
 
 // Columns n .. n + 3 of row m from the finished sums (int8: already scaled).  second: the second output of a dual launch.
-__device__ __forceinline__ void finish(const GemmArgs& g, const Wide& w, int m, int n, const float (&s)[4], int second) {
+__device__ __forceinline__ void finish(const GemmArgs& g, int m, int n, const float (&s)[4], int second) {
   const int left = g.N - n;
-  const bool four = left >= 4;
   float v[4];
   for (int e = 0; e < 4; ++e) v[e] = s[e];
   if (g.bias) {
     float b[4];
-    load4(g.bias, n, g.odt, four && w.bias, left, b);
+    load4(g.bias, n, g.odt, left, b);
     for (int e = 0; e < 4; ++e) v[e] += b[e];
   }
-  if (g.z) store4(g.z, (long long)m * g.N + n, g.odt, four && w.z, left, v);
+  if (g.z) store4(g.z, (long long)m * g.N + n, g.odt, left, v);
   if (g.act != AX_ACT_NONE)
     for (int e = 0; e < 4; ++e) v[e] = act_of(v[e], g.act);
   if (g.res) {
     float r[4];
-    load4(g.res, (long long)m * g.ldr + n, g.odt, four && w.res, left, r);
+    load4(g.res, (long long)m * g.ldr + n, g.odt, left, r);
     for (int e = 0; e < 4; ++e) v[e] += r[e];
   }
-  if (second) store4(g.y2, (long long)m * g.ldy + n, g.odt, four && w.y2, left, v);
-  else store4(g.y, (long long)m * g.ldy + n, g.odt, four && w.y, left, v);
+  if (second) store4(g.y2, (long long)m * g.ldy + n, g.odt, left, v);
+  else store4(g.y, (long long)m * g.ldy + n, g.odt, left, v);
 }
-__device__ __forceinline__ void finish_gated(const GemmArgs& g, const Wide& w, int m, int n, const float (&a)[4], const float (&u)[4]) {
+__device__ __forceinline__ void finish_gated(const GemmArgs& g, int m, int n, const float (&a)[4], const float (&u)[4]) {
   const int left = g.N - n;
-  const bool four = left >= 4;
-  if (g.z) store4(g.z, (long long)m * g.N + n, g.odt, four && w.z, left, a);
-  if (g.z2) store4(g.z2, (long long)m * g.N + n, g.odt, four && w.z2, left, u);
+  if (g.z) store4(g.z, (long long)m * g.N + n, g.odt, left, a);
+  if (g.z2) store4(g.z2, (long long)m * g.N + n, g.odt, left, u);
   float v[4];
   for (int e = 0; e < 4; ++e) v[e] = act_of(a[e], g.act) * u[e];
-  store4(g.y, (long long)m * g.ldy + n, g.odt, four && w.y, left, v);
+  store4(g.y, (long long)m * g.ldy + n, g.odt, left, v);
 }
 // int8: scales of four columns and of a row.
 __device__ __forceinline__ void scaled4(const int32_t (&c)[4], float xs, const float* ws, int n, int N, float (&v)[4]) {
@@ -342,7 +295,6 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
 
   // lane: row m, columns n .. n + 3 of every 16 x 16 block
   const int lm = lane & 15, ln = (lane >> 4) * 4;
-  const Wide w = make_wide(g);
 #pragma unroll
   for (int i = 0; i < MF; ++i) {
     const int m = m0 + wrow + 16 * i + lm;
@@ -375,8 +327,8 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
           u[e] = (float)acc[i][j + NB - 1][e];
         }
       }
-      if (NB == 2) finish_gated(g, w, m, n, v, u);
-      else finish(g, w, m, n, v, second);
+      if (NB == 2) finish_gated(g, m, n, v, u);
+      else finish(g, m, n, v, second);
     }
   }
 }
@@ -389,7 +341,6 @@ __global__ __launch_bounds__(256) void gemm_join_kernel(const Args a) {
   const int planes = g.gated || g.dual ? 2 : 1;
   const int outs = g.dual ? 2 : 1;
   const long long plane = (long long)g.M * a.ldp;
-  const Wide w = make_wide(g);
   const long long total = (long long)outs * g.M * quads;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
     const int second = i >= (long long)g.M * quads;
@@ -411,8 +362,8 @@ __global__ __launch_bounds__(256) void gemm_join_kernel(const Args a) {
         for (int e = 0; e < 4; ++e) v[pl][e] = s[e];
       }
     }
-    if (g.gated) finish_gated(g, w, m, n, v[0], v[1]);
-    else finish(g, w, m, n, v[0], second);
+    if (g.gated) finish_gated(g, m, n, v[0], v[1]);
+    else finish(g, m, n, v[0], second);
   }
 }
 

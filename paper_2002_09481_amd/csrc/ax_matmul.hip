@@ -75,19 +75,12 @@ __global__ __launch_bounds__(256) void pack_kernel(const void* __restrict__ src,
                                                     long long cols, long long ld, long long pcols) {
   constexpr int E = DT == kI8 ? 16 : 8;
   const long long groups = pcols / E, total = rows * groups;
-  const bool wide = DT == AX_F32 && ((uintptr_t)src & 15) == 0 && (ld & 3) == 0;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
     const long long r = i / groups, c = (i - r * groups) * E;
     const long long left = cols - c;
     if (DT == AX_F32) {
-      const float* s = (const float*)src + r * ld + c;
       float v[8];
-      if (wide && left >= 8) {
-        const float4 a = *(const float4*)s, b = *(const float4*)(s + 4);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-      } else {
-        for (int e = 0; e < 8; ++e) v[e] = e < left ? s[e] : 0.f;
-      }
+      load_elems<true, 8>(src, r * ld + c, (int)min(left, 8ll), v);
       uint32_t q[3][4];
       for (int e = 0; e < 4; ++e) {
         uint32_t a[3], b[3];
@@ -99,18 +92,20 @@ __global__ __launch_bounds__(256) void pack_kernel(const void* __restrict__ src,
         *(uint4*)((uint16_t*)dst + (k * rows + r) * pcols + c) = make_uint4(q[k][0], q[k][1], q[k][2], q[k][3]);
     } else if (DT == AX_BF16) {
       const uint16_t* s = (const uint16_t*)src + r * ld + c;
-      uint32_t q[4];
-      for (int e = 0; e < 4; ++e)
+      u32x4 q;
+      if (left >= 8) q = load_any<u32x4>(s);
+      else for (int e = 0; e < 4; ++e)
         q[e] = (2 * e < left ? (uint32_t)s[2 * e] : 0u) | ((2 * e + 1 < left ? (uint32_t)s[2 * e + 1] : 0u) << 16);
-      *(uint4*)((uint16_t*)dst + r * pcols + c) = make_uint4(q[0], q[1], q[2], q[3]);
+      *(u32x4*)((uint16_t*)dst + r * pcols + c) = q;
     } else {
       const uint8_t* s = (const uint8_t*)src + r * ld + c;
-      uint32_t q[4];
-      for (int e = 0; e < 4; ++e) {
+      u32x4 q;
+      if (left >= 16) q = load_any<u32x4>(s);
+      else for (int e = 0; e < 4; ++e) {
         q[e] = 0;
         for (int b = 0; b < 4; ++b) q[e] |= (4 * e + b < left ? (uint32_t)s[4 * e + b] : 0u) << (8 * b);
       }
-      *(uint4*)((uint8_t*)dst + r * pcols + c) = make_uint4(q[0], q[1], q[2], q[3]);
+      *(u32x4*)((uint8_t*)dst + r * pcols + c) = q;
     }
   }
 }
@@ -173,25 +168,6 @@ struct GradArgs {
 };
 
 template <int DT>
-__device__ __forceinline__ void read8(const void* p, long long i, bool wide, int left, float (&v)[8]) {
-  if (wide && left >= 8) {
-    if (DT == AX_F32) {
-      const float4 a = *(const float4*)((const float*)p + i), b = *(const float4*)((const float*)p + i + 4);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-      const uint4 a = *(const uint4*)((const uint16_t*)p + i);
-      const uint32_t q[4] = {a.x, a.y, a.z, a.w};
-      for (int e = 0; e < 4; ++e) {
-        v[2 * e] = bf16_to_f32(q[e] & 0xffffu);
-        v[2 * e + 1] = bf16_to_f32(q[e] >> 16);
-      }
-    }
-    return;
-  }
-  for (int e = 0; e < 8; ++e)
-    v[e] = e >= left ? 0.f : DT == AX_F32 ? ((const float*)p)[i + e] : bf16_to_f32(((const uint16_t*)p)[i + e]);
-}
-template <int DT>
 __device__ __forceinline__ void write_planes(void* dst, long long rows, long long pcols, long long r, long long c, const float (&v)[8]) {
   if (DT == AX_F32) {
     uint32_t q[3][4];
@@ -215,18 +191,15 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const GradArgs a) {
   const long long c = ((long long)blockIdx.x * 32 + cx) * 8;
   const int r0 = blockIdx.y * a.rows_per, r1 = min(a.M, r0 + a.rows_per);
   const int left = (int)max(0ll, min(8ll, a.N - c));
-  constexpr int am = 15, lm = DT == AX_F32 ? 3 : 7;
-  const bool wy = ((uintptr_t)a.gy & am) == 0 && (a.ldy & lm) == 0;
-  const bool wz = ((uintptr_t)a.z & am) == 0 && (a.N & lm) == 0, wu = ((uintptr_t)a.u & am) == 0 && (a.N & lm) == 0;
   float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   if (c < a.pcols) {
     for (int r = r0 + ry; r < r1; r += 8) {
       float gy[8], z[8], u[8];
-      read8<DT>(a.gy, (long long)r * a.ldy + c, wy, left, gy);
-      if (GATED || a.z) read8<DT>(a.z, (long long)r * a.N + c, wz, left, z);
+      load_elems<DT == AX_F32, 8>(a.gy, (long long)r * a.ldy + c, left, gy);
+      if (GATED || a.z) load_elems<DT == AX_F32, 8>(a.z, (long long)r * a.N + c, left, z);
       if (GATED) {
         float gu[8];
-        read8<DT>(a.u, (long long)r * a.N + c, wu, left, u);
+        load_elems<DT == AX_F32, 8>(a.u, (long long)r * a.N + c, left, u);
         for (int e = 0; e < 8; ++e) {
           gu[e] = gy[e] * act_of(z[e], a.act);
           gy[e] = gy[e] * u[e] * act_slope(z[e], a.act);

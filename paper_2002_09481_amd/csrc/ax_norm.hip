@@ -40,56 +40,16 @@ struct NormArgs {
   float eps;
 };
 
-// Eight elements of a row: contiguous where rows are wide-aligned, TPR apart otherwise (so that neighbouring lanes read
-// neighbouring elements either way).
-template <bool WIDE, int TPR>
-__device__ __forceinline__ int col_of(int it, int t, int e) {
-  return WIDE ? (it * TPR + t) * 8 + e : (it * 8 + e) * TPR + t;
-}
-template <bool WIDE, int TPR, bool F32>
+// Eight consecutive elements of a row a lane and pass.
+template <int TPR, bool F32>
 __device__ __forceinline__ void load_row(const void* p, long long row, int it, int t, int cols, float (&v)[8]) {
-  if (WIDE) {
-    const int c = (it * TPR + t) * 8;
-    if (c >= cols) {
-      for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    } else if (F32) {
-      const float4 a = *(const float4*)((const float*)p + row + c), b = *(const float4*)((const float*)p + row + c + 4);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-      const uint4 a = *(const uint4*)((const uint16_t*)p + row + c);
-      const uint32_t q[4] = {a.x, a.y, a.z, a.w};
-      for (int e = 0; e < 4; ++e) {
-        v[2 * e] = bf16_to_f32(q[e] & 0xffffu);
-        v[2 * e + 1] = bf16_to_f32(q[e] >> 16);
-      }
-    }
-  } else {
-    for (int e = 0; e < 8; ++e) {
-      const int c = col_of<WIDE, TPR>(it, t, e);
-      v[e] = c >= cols ? 0.f : F32 ? ((const float*)p)[row + c] : bf16_to_f32(((const uint16_t*)p)[row + c]);
-    }
-  }
+  const int c = (it * TPR + t) * 8;
+  load_elems<F32, 8>(p, row + c, cols - c, v);
 }
-template <bool WIDE, int TPR, bool F32>
+template <int TPR, bool F32>
 __device__ __forceinline__ void store_row(void* p, long long row, int it, int t, int cols, const float (&v)[8]) {
-  if (WIDE) {
-    const int c = (it * TPR + t) * 8;
-    if (c >= cols) return;
-    if (F32) {
-      *(float4*)((float*)p + row + c) = make_float4(v[0], v[1], v[2], v[3]);
-      *(float4*)((float*)p + row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-      *(uint4*)((uint16_t*)p + row + c) =
-          make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-    }
-  } else {
-    for (int e = 0; e < 8; ++e) {
-      const int c = col_of<WIDE, TPR>(it, t, e);
-      if (c >= cols) continue;
-      if (F32) ((float*)p)[row + c] = v[e];
-      else ((uint16_t*)p)[row + c] = (uint16_t)f32_to_bf16(v[e]);
-    }
-  }
+  const int c = (it * TPR + t) * 8;
+  store_elems<F32, 8>(p, row + c, cols - c, v);
 }
 
 // Sum and largest value over the TPR lanes of a row, in a fixed order.  red: 2 * TPR / 64 words of LDS.
@@ -117,7 +77,7 @@ __device__ __forceinline__ void reduce_row(float& sum, uint32_t& top, float* red
 }
 
 // TPR lanes a row, NV passes of eight elements in registers (0: any number of columns, read twice).
-template <int MODE, bool F32, bool WIDE, int TPR, int NV>
+template <int MODE, bool F32, int TPR, int NV>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const NormArgs a) {
   constexpr int THREADS = TPR < 256 ? 256 : TPR;
   __shared__ float red[2 * (TPR / 64)];
@@ -129,15 +89,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const NormA
   float v[NV ? NV : 1][8], w[NV ? NV : 1][8];
 
   auto load = [&](int it, float (&tv)[8], float (&wv)[8]) {
-    load_row<WIDE, TPR, F32>(a.x, xo, it, t, a.cols, tv);
+    load_row<TPR, F32>(a.x, xo, it, t, a.cols, tv);
     if (a.res) {
       float r[8];
-      load_row<WIDE, TPR, F32>(a.res, ro, it, t, a.cols, r);
+      load_row<TPR, F32>(a.res, ro, it, t, a.cols, r);
       for (int e = 0; e < 8; ++e) tv[e] += r[e];
     }
     if (a.w) {
-      if (a.w_f32) load_row<WIDE, TPR, true>(a.w, 0, it, t, a.cols, wv);
-      else load_row<WIDE, TPR, false>(a.w, 0, it, t, a.cols, wv);
+      if (a.w_f32) load_row<TPR, true>(a.w, 0, it, t, a.cols, wv);
+      else load_row<TPR, false>(a.w, 0, it, t, a.cols, wv);
     } else {
       for (int e = 0; e < 8; ++e) wv[e] = 1.f;
     }
@@ -158,7 +118,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const NormA
     for (int it = 0; it < iters; ++it) load(it, v[it], w[it]);
 #pragma unroll
     for (int it = 0; it < iters; ++it) {
-      if (a.sum) store_row<WIDE, TPR, F32>(a.sum, so, it, t, a.cols, v[it]);
+      if (a.sum) store_row<TPR, F32>(a.sum, so, it, t, a.cols, v[it]);
       take(it, v[it], w[it]);
     }
   } else {
@@ -180,26 +140,22 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const NormA
     if (MODE == kValues) {
       float y[8];
       for (int e = 0; e < 8; ++e) y[e] = tv[e] * rstd * wv[e];
-      store_row<WIDE, TPR, F32>(a.y, yo, it, t, a.cols, y);
+      store_row<TPR, F32>(a.y, yo, it, t, a.cols, y);
     } else {
       float c[8];
       for (int e = 0; e < 8; ++e) c[e] = inv > 0.f ? rintf(tv[e] * inv) : 0.f;
-      if (WIDE) {
-        const int col = (it * TPR + t) * 8;
-        if (col < a.cols) {
-          uint32_t q[2] = {0, 0};
-          for (int e = 0; e < 8; ++e) q[e >> 2] |= ((uint32_t)(int)c[e] & 0xffu) << (8 * (e & 3));
-          *(uint2*)(a.codes + co + col) = make_uint2(q[0], q[1]);
-        }
+      const int col = (it * TPR + t) * 8;
+      if (col + 8 <= a.cols) {
+        u32x2 q = {0, 0};
+        for (int e = 0; e < 8; ++e) q[e >> 2] |= ((uint32_t)(int)c[e] & 0xffu) << (8 * (e & 3));
+        store_any(a.codes + co + col, q);
       } else {
-        for (int e = 0; e < 8; ++e) {
-          const int col = col_of<WIDE, TPR>(it, t, e);
-          if (col < a.cols) a.codes[co + col] = (int8_t)(int)c[e];
-        }
+        for (int e = 0; e < 8; ++e)
+          if (col + e < a.cols) a.codes[co + col + e] = (int8_t)(int)c[e];
       }
       if (a.values) {
         for (int e = 0; e < 8; ++e) c[e] *= scale;
-        store_row<WIDE, TPR, true>(a.values, co, it, t, a.cols, c);
+        store_row<TPR, true>(a.values, co, it, t, a.cols, c);
       }
     }
   };
@@ -210,7 +166,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const NormA
     for (int it = 0; it < iters; ++it) {
       load(it, v[0], w[0]);
       // (sum may be x or the residual: written only now, behind this lane's last read of the place)
-      if (a.sum) store_row<WIDE, TPR, F32>(a.sum, so, it, t, a.cols, v[0]);
+      if (a.sum) store_row<TPR, F32>(a.sum, so, it, t, a.cols, v[0]);
       if (MODE == kCodes)
         for (int e = 0; e < 8; ++e) v[0][e] = v[0][e] * w[0][e];
       put(it, v[0], w[0]);
@@ -232,7 +188,7 @@ struct NormGradArgs {
 };
 
 // A workgroup takes every gridDim.x-th group of THREADS / TPR rows and keeps its share of gw in registers until the end.
-template <bool F32, bool WIDE, int TPR, int NV>
+template <bool F32, int TPR, int NV>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(const NormGradArgs a) {
   constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
   __shared__ float red[2 * 2 * (TPR / 64)];
@@ -241,8 +197,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(const 
   float gw[NV][8], w[NV][8];
 #pragma unroll
   for (int it = 0; it < NV; ++it) {
-    if (a.w_f32) load_row<WIDE, TPR, true>(a.w, 0, it, t, a.cols, w[it]);
-    else load_row<WIDE, TPR, false>(a.w, 0, it, t, a.cols, w[it]);
+    if (a.w_f32) load_row<TPR, true>(a.w, 0, it, t, a.cols, w[it]);
+    else load_row<TPR, false>(a.w, 0, it, t, a.cols, w[it]);
     for (int e = 0; e < 8; ++e) gw[it][e] = 0.f;
   }
   int turn = 0;
@@ -253,8 +209,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(const 
     float gy[NV][8], h[NV][8];
 #pragma unroll
     for (int it = 0; it < NV; ++it) {
-      load_row<WIDE, TPR, F32>(a.gy, row * a.gy_ld, it, t, a.cols, gy[it]);
-      load_row<WIDE, TPR, F32>(a.t, row * a.t_ld, it, t, a.cols, h[it]);
+      load_row<TPR, F32>(a.gy, row * a.gy_ld, it, t, a.cols, gy[it]);
+      load_row<TPR, F32>(a.t, row * a.t_ld, it, t, a.cols, h[it]);
     }
     float dot = 0.f;
 #pragma unroll
@@ -277,10 +233,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(const 
       for (int e = 0; e < 8; ++e) o[e] = rstd * (gy[it][e] - h[it][e] * mean);
       if (a.gsum) {
         float s[8];
-        load_row<WIDE, TPR, F32>(a.gsum, row * a.gs_ld, it, t, a.cols, s);
+        load_row<TPR, F32>(a.gsum, row * a.gs_ld, it, t, a.cols, s);
         for (int e = 0; e < 8; ++e) o[e] += s[e];
       }
-      store_row<WIDE, TPR, F32>(a.gx, row * a.gx_ld, it, t, a.cols, o);
+      store_row<TPR, F32>(a.gx, row * a.gx_ld, it, t, a.cols, o);
     }
   }
   if (!a.part) return;
@@ -297,10 +253,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(const 
   }
 #pragma unroll
   for (int it = 0; it < NV; ++it) {
-    for (int e = 0; e < 8; ++e) {
-      const int c = col_of<WIDE, TPR>(it, t, e);
-      if (c < a.cols) a.part[(long long)blockIdx.x * a.cols + c] = gw[it][e];
-    }
+    store_row<TPR, true>(a.part, (long long)blockIdx.x * a.cols, it, t, a.cols, gw[it]);
   }
 }
 
@@ -319,10 +272,10 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const NormGradArgs
     const float mean = dot / (float)a.cols;
     for (int it = 0; it < iters; ++it) {
       float gy[8], h[8], w[8];
-      load_row<false, TPR, F32>(a.gy, row * a.gy_ld, it, t, a.cols, gy);
-      load_row<false, TPR, F32>(a.t, row * a.t_ld, it, t, a.cols, h);
-      if (a.w_f32) load_row<false, TPR, true>(a.w, 0, it, t, a.cols, w);
-      else load_row<false, TPR, false>(a.w, 0, it, t, a.cols, w);
+      load_row<TPR, F32>(a.gy, row * a.gy_ld, it, t, a.cols, gy);
+      load_row<TPR, F32>(a.t, row * a.t_ld, it, t, a.cols, h);
+      if (a.w_f32) load_row<TPR, true>(a.w, 0, it, t, a.cols, w);
+      else load_row<TPR, false>(a.w, 0, it, t, a.cols, w);
       for (int e = 0; e < 8; ++e) {
         h[e] = h[e] * rstd;
         gy[e] = gy[e] * w[e];
@@ -331,10 +284,10 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const NormGradArgs
       if (pass == 1) {
         for (int e = 0; e < 8; ++e) gy[e] = rstd * (gy[e] - h[e] * mean);
         if (a.gsum) {
-          load_row<false, TPR, F32>(a.gsum, row * a.gs_ld, it, t, a.cols, w);
+          load_row<TPR, F32>(a.gsum, row * a.gs_ld, it, t, a.cols, w);
           for (int e = 0; e < 8; ++e) gy[e] += w[e];
         }
-        store_row<false, TPR, F32>(a.gx, row * a.gx_ld, it, t, a.cols, gy);
+        store_row<TPR, F32>(a.gx, row * a.gx_ld, it, t, a.cols, gy);
       }
     }
     if (pass == 0) {
@@ -389,13 +342,13 @@ Shape shape_of(long long rows, long long cols) {
   return {1024, 0};
 }
 
-template <int MODE, bool F32, bool WIDE>
+template <int MODE, bool F32>
 void norm_launch(const NormArgs& a, hipStream_t s) {
   const Shape sh = shape_of(a.rows, a.cols);
   const int per = sh.tpr == 64 ? 4 : 1;
   const unsigned grid = (unsigned)((a.rows + per - 1) / per);
   const int threads = sh.tpr < 256 ? 256 : sh.tpr;
-#define AX_NORM(T, V) norm_kernel<MODE, F32, WIDE, T, V><<<grid, threads, 0, s>>>(a)
+#define AX_NORM(T, V) norm_kernel<MODE, F32, T, V><<<grid, threads, 0, s>>>(a)
 #define AX_NORM_T(T)                         \
   switch (sh.nv) {                           \
     case 1: AX_NORM(T, 1); break;            \
@@ -409,10 +362,10 @@ void norm_launch(const NormArgs& a, hipStream_t s) {
 #undef AX_NORM_T
 #undef AX_NORM
 }
-template <bool F32, bool WIDE>
+template <bool F32>
 void norm_grad_launch(const NormGradArgs& a, const Shape& sh, int groups, hipStream_t s) {
   const int threads = sh.tpr < 256 ? 256 : sh.tpr;
-#define AX_NG(T, V) norm_grad_kernel<F32, WIDE, T, V><<<groups, threads, 0, s>>>(a)
+#define AX_NG(T, V) norm_grad_kernel<F32, T, V><<<groups, threads, 0, s>>>(a)
 #define AX_NG_T(T)                           \
   switch (sh.nv) {                           \
     case 1: AX_NG(T, 1); break;              \
@@ -426,8 +379,6 @@ void norm_grad_launch(const NormGradArgs& a, const Shape& sh, int groups, hipStr
 #undef AX_NG_T
 #undef AX_NG
 }
-
-bool wide_ptr(const void* p, long long ld, int esz) { return (uintptr_t)p % 16 == 0 && (ld * esz) % 16 == 0; }
 
 // The gradient keeps four values a column in registers: 1024 lanes hold 16384 columns.
 bool grad_is_long(const Shape& sh) { return sh.nv == 0 || (sh.tpr == 1024 && sh.nv > 2); }
@@ -471,18 +422,9 @@ int norm_common(const ax_norm_desc_t* d, NormArgs& a, bool codes, hipStream_t s)
   a.w_f32 = d->w_dtype == AX_F32;
   a.normalize = d->normalize;
   a.eps = d->eps;
-  const bool wide = d->cols % 8 == 0 && wide_ptr(a.x, a.x_ld, e) && (!a.res || wide_ptr(a.res, a.r_ld, e)) &&
-                    (!a.sum || wide_ptr(a.sum, a.s_ld, e)) && (!a.y || wide_ptr(a.y, a.y_ld, e)) &&
-                    (!a.w || wide_ptr(a.w, 0, we)) && (!a.codes || (uintptr_t)a.codes % 8 == 0) &&
-                    (!a.values || wide_ptr(a.values, d->cols, 4));
   const bool f32 = d->dtype == AX_F32;
-  if (codes) {
-    if (f32) wide ? norm_launch<kCodes, true, true>(a, s) : norm_launch<kCodes, true, false>(a, s);
-    else wide ? norm_launch<kCodes, false, true>(a, s) : norm_launch<kCodes, false, false>(a, s);
-  } else {
-    if (f32) wide ? norm_launch<kValues, true, true>(a, s) : norm_launch<kValues, true, false>(a, s);
-    else wide ? norm_launch<kValues, false, true>(a, s) : norm_launch<kValues, false, false>(a, s);
-  }
+  if (codes) f32 ? norm_launch<kCodes, true>(a, s) : norm_launch<kCodes, false>(a, s);
+  else f32 ? norm_launch<kValues, true>(a, s) : norm_launch<kValues, false>(a, s);
   return hipGetLastError() == hipSuccess ? AX_OK : AX_ERR_HIP;
 }
 
@@ -580,10 +522,7 @@ extern "C" int ax_rmsnorm_backward(const ax_norm_desc_t* d, const void* gy, cons
       else norm_gw_long_kernel<false><<<grid, 256, 0, s>>>(a);
     }
   } else {
-    const bool wide = d->cols % 8 == 0 && wide_ptr(gy, a.gy_ld, e) && wide_ptr(t, a.t_ld, e) && (!gsum || wide_ptr(gsum, a.gs_ld, e)) &&
-                      (!gx_out || wide_ptr(gx_out, a.gx_ld, e)) && wide_ptr(weight, 0, we);
-    if (f32) wide ? norm_grad_launch<true, true>(a, sh, groups, s) : norm_grad_launch<true, false>(a, sh, groups, s);
-    else wide ? norm_grad_launch<false, true>(a, sh, groups, s) : norm_grad_launch<false, false>(a, sh, groups, s);
+    f32 ? norm_grad_launch<true>(a, sh, groups, s) : norm_grad_launch<false>(a, sh, groups, s);
   }
   if (hipGetLastError() != hipSuccess) return AX_ERR_HIP;
   if (gw_out && launch_column_sum(a.part, groups, a.cols, gw_out, s) != hipSuccess) return AX_ERR_HIP;

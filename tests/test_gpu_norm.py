@@ -1,0 +1,169 @@
+"""Root-mean-square norm: values, 8-bit codes and gradients against 64-bit forms, at the row lengths and pitches where lanes,
+passes and kernels change."""
+
+import numpy as np
+import pytest
+import torch
+
+import ff_common as F
+from paper_2002_09481_amd import binding as ax
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-5
+
+# (rows, cols): one element, odd, either side of the register shapes, more columns than registers hold
+SHAPES = [(1, 1), (3, 7), (1, 2048), (5, 513), (600, 512), (700, 2056), (2, 8200), (513, 8191), (3, 16392), (2, 40007), (1, 65536)]
+
+
+def _operands(rows, cols, dtype, wdtype, seed, residual=True):
+    g = F.gen(seed)
+    x = torch.randn((rows, cols), generator=g)
+    x[:, ::17] *= 10
+    return (x.to(dtype).cuda(), (1 + 0.2 * torch.randn(cols, generator=g)).to(wdtype).cuda(),
+            F.randn(g, (rows, cols), 1.0, dtype).cuda() if residual else None)
+
+
+@pytest.mark.parametrize("wdt", ["same", "f32"])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_values(rows, cols, dt, wdt):
+    dtype = F.DT[dt]
+    x, w, r = _operands(rows, cols, dtype, dtype if wdt == "same" else torch.float32, rows * 31 + cols, residual=rows % 2 == 1)
+    y, t, rstd = ax.ax_rmsnorm(x, w, residual=r, eps=EPS)
+    td = x.cpu().double() + (r.cpu().double() if r is not None else 0)
+    k = 1 / torch.sqrt((td ** 2).mean(dim=1) + EPS)
+    want = td * k[:, None] * w.cpu().double()
+    # the sum of squares has terms of one sign: at most cols / lanes + 20 additions deep; the rest are single operations
+    rel = (cols / 64 + 24) * F.U
+    F.assert_within(rstd, k, k * rel, "rstd")
+    F.assert_within(y, want, want.abs() * (rel + 4 * F.U + F.store(dtype)) + 8 * F.U * (k * 1.0)[:, None] * w.cpu().double().abs() *
+                    (x.cpu().double().abs() + (r.cpu().double().abs() if r is not None else 0)), "y")
+    assert (t is None) == (r is None)
+    if r is not None:
+        assert torch.equal(t.cpu(), (x.cpu().float() + r.cpu().float()).to(dtype))
+
+
+def _codes_reference(t, w):
+    """Codes from float32 operations, one at a time (numpy): they do not depend on the order of the norm's sum."""
+    v = t if w is None else t * w
+    amax = np.abs(v).max(axis=1)
+    with np.errstate(divide="ignore"):
+        inv = np.where(amax >= np.float32(2.0 ** -120), np.float32(127) / amax, np.float32(0)).astype(np.float32)
+    return np.rint(v * inv[:, None]).astype(np.int8), amax
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_codes(rows, cols, dt, norm):
+    dtype = F.DT[dt]
+    x, w, r = _operands(rows, cols, dtype, dtype, 7 * rows + cols, residual=cols % 2 == 0)
+    if rows > 2:
+        x[1] = 0  # a row without a code
+        if r is not None:
+            r[1] = 0
+    codes, scales, t, values = ax.ax_rmsnorm_q8(x, w if norm else None, residual=r, eps=EPS, normalize=norm, values=True)
+    tf = x.cpu().float().numpy() + (r.cpu().float().numpy() if r is not None else np.float32(0))
+    want, amax = _codes_reference(tf, w.cpu().float().numpy() if norm else None)
+    assert np.array_equal(codes.cpu().numpy(), want)
+    k = 1 / np.sqrt((tf.astype(np.float64) ** 2).mean(axis=1) + EPS) if norm else np.ones(rows)
+    s = amax.astype(np.float64) * k / 127
+    assert np.all(np.abs(scales.cpu().numpy() - s) <= s * (cols / 64 + 28) * F.U)
+    assert torch.equal(values.cpu(), codes.cpu().float() * scales.cpu()[:, None])
+    if r is not None:
+        assert torch.equal(t.cpu(), torch.from_numpy(tf).to(dtype))
+
+
+def test_codes_of_extreme_rows():
+    big = torch.finfo(torch.float32).max
+    x = torch.ones((6, 300))
+    x[0, 5], x[1, 7], x[2, 9] = float("nan"), float("inf"), -float("inf")
+    x[3] = 2.0 ** -130  # below what 127 / amax can turn into codes
+    x[4], x[4, 0] = 1e-30, big
+    codes, scales, _, values = ax.ax_rmsnorm_q8(x.cuda(), normalize=False, values=True)
+    c, s = codes.cpu(), scales.cpu()
+    assert torch.isnan(s[0]) and torch.isinf(s[1]) and torch.isinf(s[2]) and not bool(c[:4].any())
+    assert int(c[4, 0]) == 127 and not bool(c[4, 1:].any()) and torch.equal(c[5], torch.full((300,), 127, dtype=torch.int8))
+    assert torch.isfinite(s[3:]).all() and torch.isnan(values.cpu()[0]).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (5, 513), (600, 512), (2000, 1000), (700, 2056), (2, 8200), (513, 8191),
+                                       (3, 16384), (9, 16392), (70, 20001)])
+def test_gradients(rows, cols, dt):
+    dtype = F.DT[dt]
+    t, w, gs = _operands(rows, cols, dtype, dtype, rows + 3 * cols)
+    gy = F.randn(F.gen(5), (rows, cols), 0.1, dtype).cuda()
+    rstd = (1 / torch.sqrt((t.float() ** 2).mean(dim=1) + EPS)).contiguous()
+    gs = gs if rows % 2 else None
+    gx, gw = ax.ax_rmsnorm_backward(gy, t, w, rstd, gsum=gs)
+    td, wd, gd, k = (v.cpu().double() for v in (t, w, gy, rstd))
+    h, q = td * k[:, None], gd * wd
+    want = k[:, None] * (q - h * (q * h).mean(dim=1, keepdim=True))
+    size = k[:, None] * (q.abs() + h.abs() * (q * h).abs().mean(dim=1, keepdim=True))
+    if gs is not None:
+        want, size = want + gs.cpu().double(), size + gs.cpu().double().abs()
+    F.assert_within(gx, want, size * (cols / 64 + 32) * F.U + want.abs() * F.store(dtype), "gx")
+    F.assert_within(gw, (gd * h).sum(dim=0), (gd * h).abs().sum(dim=0) * (rows / 64 + 64) * F.U, "gw")
+    assert torch.equal(gw, ax.ax_rmsnorm_backward(gy, t, w, rstd, gsum=gs)[1])  # one order of the sum over rows
+    assert torch.equal(gx, ax.ax_rmsnorm_backward(gy, t, w, rstd, gsum=gs, gw_out=False)[0])
+    assert torch.equal(gw, ax.ax_rmsnorm_backward(gy, t, w, rstd, gsum=gs, gx_out=False)[1])
+
+
+def test_gradient_against_differences():
+    g = F.gen(3)
+    x, w, c = torch.randn((4, 50), generator=g), 1 + 0.1 * torch.randn(50, generator=g), torch.randn((4, 50), generator=g)
+    dx, dw = torch.randn((4, 50), generator=g).double(), torch.randn(50, generator=g).double()
+
+    def loss(e):
+        t, v = x.double() + e * dx, w.double() + e * dw
+        return float((c.double() * t / torch.sqrt((t ** 2).mean(dim=1, keepdim=True) + EPS) * v).sum())
+
+    _, _, rstd = ax.ax_rmsnorm(x.cuda(), w.cuda(), eps=EPS)
+    gx, gw = ax.ax_rmsnorm_backward(c.cuda(), x.cuda(), w.cuda(), rstd)
+    got = float((gx.cpu().double() * dx).sum() + (gw.cpu().double() * dw).sum())
+    e = 1e-4  # differences: e^2 times a third derivative of order 200; gradients: 250 terms of order 1, float32
+    assert abs(got - (loss(e) - loss(-e)) / (2 * e)) <= 1e-5 + 250 * 40 * F.U
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("offset,pad", [(0, 8), (1, 7), (3, 6), (8, 24)])
+def test_pitches_and_places(dt, offset, pad):
+    """Rows inside wider buffers, at any element; the sum in the place of x; nothing outside the rows is touched."""
+    dtype, rows, cols = F.DT[dt], 37, 264
+    g = F.gen(9)
+    bufs = [F.randn(g, (rows, cols + pad + offset), 1.0, dtype).cuda() for _ in range(4)]
+    x, r, y, s = (b[:, offset:offset + cols] for b in bufs)
+    w = (1 + 0.1 * torch.randn(cols, generator=g)).cuda()
+    before = [b.clone() for b in bufs]
+    plain = ax.ax_rmsnorm(x.contiguous(), w, residual=r.contiguous(), eps=EPS)
+    ax.ax_rmsnorm(x, w, residual=r, eps=EPS, y_out=y, sum_out=s)
+    assert torch.equal(y, plain[0]) and torch.equal(s, plain[1])
+    gx, gw = ax.ax_rmsnorm_backward(y, s, w, plain[2], gsum=r)
+    ref = ax.ax_rmsnorm_backward(y.contiguous(), s.contiguous(), w, plain[2], gsum=r.contiguous())
+    assert torch.equal(gx, ref[0]) and torch.equal(gw, ref[1])
+    ax.ax_rmsnorm(x, w, residual=r, eps=EPS, y_out=y, sum_out=x)
+    assert torch.equal(x, plain[1]) and torch.equal(y, plain[0])
+    ax.ax_rmsnorm_backward(y, s, w, plain[2], gsum=r, gx_out=r)
+    assert torch.equal(r, ref[0])
+    for b, old in zip(bufs, before):
+        b[:, offset:offset + cols] = old[:, offset:offset + cols]
+        assert torch.equal(b, old)
+
+
+def test_no_rows():
+    x, w = torch.empty((0, 33), device="cuda"), torch.ones(33, device="cuda")
+    y, t, rstd = ax.ax_rmsnorm(x, w)
+    codes, scales, _, _ = ax.ax_rmsnorm_q8(x, w)
+    gx, gw = ax.ax_rmsnorm_backward(x, x, w, rstd, gw_out=torch.full((33,), 7.0, device="cuda"))
+    assert y.shape == (0, 33) and codes.shape == (0, 33) and scales.numel() == 0 and gx.shape == (0, 33) and not bool(gw.any())
+
+
+def test_more_elements_than_32_bits_count():
+    rows, cols = (1 << 20) + 3, 2112
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    x[-3:] = F.randn(F.gen(1), (3, cols), 1.0, torch.bfloat16).cuda()
+    w = torch.ones(cols, device="cuda", dtype=torch.bfloat16)
+    codes, scales, _, _ = ax.ax_rmsnorm_q8(x, w, eps=EPS)
+    ref = ax.ax_rmsnorm_q8(x[-3:].contiguous(), w, eps=EPS)
+    assert torch.equal(codes[-3:], ref[0]) and torch.allclose(scales[-3:], ref[1], rtol=1e-5, atol=0) and not bool(scales[:-3].any())
