@@ -296,8 +296,9 @@ def _pair(v) -> Tuple[int, int]:
 
 
 def _stream_ptr(stream) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return int(s.cuda_stream)
+    if stream is None:  # (the handle alone: building torch's stream object takes longer than all checks of a small call)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return int(stream.cuda_stream)
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -868,6 +869,25 @@ def _float_dtype(t, name: str) -> int:
     return dt
 
 
+# Descriptions of calls that were checked before, with what they need of workspace: every check of a call depends on the
+# types, shapes and pitches of its tensors alone (and on whether they start on 16 bytes).  For a call of one token the
+# checks would take longer than its kernels.
+_checked = {}
+
+
+def _remember(key, value):
+    if len(_checked) >= 4096:
+        _checked.clear()
+    _checked[key] = value
+    return value
+
+
+def _sig(t):
+    if t is None or t is False:
+        return t
+    return t.dtype, t.shape, t.stride(), t.device
+
+
 def _mat(t, dtype, name: str) -> Tuple[int, int, int]:
     """(rows, columns, row pitch) of a matrix."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -914,7 +934,7 @@ def _act_code(act: str) -> int:
     return AX_ACTS[act]
 
 
-def _norm_desc(x, residual, sum_out, weight, eps, normalize) -> Tuple[ax_norm_desc_t, torch.Tensor]:
+def _norm_desc(x, residual, sum_out, weight, eps, normalize) -> ax_norm_desc_t:
     dt = _float_dtype(x, "x")
     rows, cols, ld = _mat(x, x.dtype, "x")
     d = ax_norm_desc_t(rows, cols, ld, cols, cols, cols, dt, dt, float(eps), int(bool(normalize)))
@@ -923,32 +943,33 @@ def _norm_desc(x, residual, sum_out, weight, eps, normalize) -> Tuple[ax_norm_de
         _vec_of(weight, weight.dtype, cols, "weight")
     if residual is not None:
         d.residual_ld = _mat_of(residual, x.dtype, rows, cols, "residual")
-        if sum_out is None:
-            sum_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     elif sum_out is not None and sum_out is not False:
         raise ValueError("sum_out needs a residual")
-    if sum_out is False:
-        sum_out = None
-    if sum_out is not None:
+    if sum_out is not None and sum_out is not False:
         d.sum_ld = _mat_of(sum_out, x.dtype, rows, cols, "sum_out")
-    return d, sum_out
+    return d
 
 
 def ax_rmsnorm(x, weight, residual=None, eps=1e-5, sum_out=None, y_out=None, rstd_out=None, stream=None):
     """Root-mean-square norm of rows: t = x + residual, y = t * rstd * weight.  Returns (y, t, rstd); t is None without
     a residual.  sum_out may be x or residual themselves; False skips t (or rstd)."""
-    d, sum_out = _norm_desc(x, residual, sum_out, weight, eps, True)
+    if residual is not None and sum_out is None:
+        sum_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     if y_out is None:
         y_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    d.y_ld = _mat_of(y_out, x.dtype, d.rows, d.cols, "y_out")
     if rstd_out is None:
         rstd_out = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    if rstd_out is False:
-        rstd_out = None
-    else:
-        _vec_of(rstd_out, torch.float32, d.rows, "rstd_out")
-    _check(lib().ax_rmsnorm(ctypes.byref(d), _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_out), _ptr(y_out),
-                            _ptr(rstd_out), _stream_ptr(stream)))
+    key = ("rmsnorm", eps, _sig(x), _sig(weight), _sig(residual), _sig(sum_out), _sig(y_out), _sig(rstd_out))
+    d = _checked.get(key)
+    if d is None:
+        d = _norm_desc(x, residual, sum_out, weight, eps, True)
+        d.y_ld = _mat_of(y_out, x.dtype, d.rows, d.cols, "y_out")
+        if rstd_out is not False:
+            _vec_of(rstd_out, torch.float32, d.rows, "rstd_out")
+        _remember(key, d)
+    sum_out, rstd_out = (None if o is False else o for o in (sum_out, rstd_out))
+    _check(lib().ax_rmsnorm(d, _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_out), _ptr(y_out), _ptr(rstd_out),
+                            _stream_ptr(stream)))
     return y_out, sum_out, rstd_out
 
 
@@ -957,19 +978,28 @@ def ax_rmsnorm_q8(x, weight=None, residual=None, eps=1e-5, normalize=True, sum_o
     """The norm's output as int8 codes with a scale a row: y = codes * scales[:, None].  normalize False: the rows
     themselves (times weight).  Returns (codes, scales, t, values); values, the float32 values that the codes stand for,
     is None unless asked for."""
-    d, sum_out = _norm_desc(x, residual, sum_out, weight, eps, normalize)
+    dev = x.device
+    if residual is not None and sum_out is None:
+        sum_out = torch.empty(x.shape, dtype=x.dtype, device=dev)
     if codes_out is None:
-        codes_out = torch.empty(x.shape, dtype=torch.int8, device=x.device)
-    _vec_of(codes_out, torch.int8, d.rows * d.cols, "codes_out")
+        codes_out = torch.empty(x.shape, dtype=torch.int8, device=dev)
     if scales_out is None:
-        scales_out = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    _vec_of(scales_out, torch.float32, d.rows, "scales_out")
+        scales_out = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
     if values_out is None and values:
-        values_out = torch.empty(x.shape, dtype=torch.float32, device=x.device)
-    if values_out is not None:
-        _vec_of(values_out, torch.float32, d.rows * d.cols, "values_out")
-    _check(lib().ax_rmsnorm_q8(ctypes.byref(d), _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_out), _ptr(codes_out),
-                               _ptr(scales_out), _ptr(values_out), _stream_ptr(stream)))
+        values_out = torch.empty(x.shape, dtype=torch.float32, device=dev)
+    key = ("rmsnorm_q8", eps, normalize, _sig(x), _sig(weight), _sig(residual), _sig(sum_out), _sig(codes_out), _sig(scales_out),
+           _sig(values_out))
+    d = _checked.get(key)
+    if d is None:
+        d = _norm_desc(x, residual, sum_out, weight, eps, normalize)
+        _vec_of(codes_out, torch.int8, d.rows * d.cols, "codes_out")
+        _vec_of(scales_out, torch.float32, d.rows, "scales_out")
+        if values_out is not None:
+            _vec_of(values_out, torch.float32, d.rows * d.cols, "values_out")
+        _remember(key, d)
+    sum_out = None if sum_out is False else sum_out
+    _check(lib().ax_rmsnorm_q8(d, _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_out), _ptr(codes_out), _ptr(scales_out),
+                               _ptr(values_out), _stream_ptr(stream)))
     return codes_out, scales_out, sum_out, values_out
 
 
@@ -987,30 +1017,34 @@ def ax_rmsnorm_backward(gy, t, weight, rstd, gsum=None, gx_out=None, gw_out=None
     """Gradients of ax_rmsnorm: (gx, gw), gx for x and residual alike, gw float32.  t, rstd: what the forward pass
     returned (t = x without a residual); gsum: the gradient that reaches t from the residual stream.  False skips one."""
     L = lib()
-    dt = _float_dtype(t, "t")
-    rows, cols, ld = _mat(t, t.dtype, "t")
-    _vec_of(weight, weight.dtype, cols, "weight")
-    _vec_of(rstd, torch.float32, rows, "rstd")
-    d = ax_norm_desc_t(rows, cols, ld, cols, cols, _mat_of(gy, t.dtype, rows, cols, "gy"), dt, _float_dtype(weight, "weight"),
-                       0.0, 1)
-    if gsum is not None:
-        d.residual_ld = _mat_of(gsum, t.dtype, rows, cols, "gsum")
     if gx_out is None:
         gx_out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
     if gw_out is None:
         gw_out = torch.empty(weight.shape, dtype=torch.float32, device=t.device)
-    if gx_out is not False:
-        d.sum_ld = _mat_of(gx_out, t.dtype, rows, cols, "gx_out")
-    if gw_out is not False:
-        _vec_of(gw_out, torch.float32, cols, "gw_out")
+    key = ("rmsnorm_backward", _sig(gy), _sig(t), _sig(weight), _sig(rstd), _sig(gsum), _sig(gx_out), _sig(gw_out))
+    hit = _checked.get(key)
+    if hit is None:
+        rows, cols, ld = _mat(t, t.dtype, "t")
+        d = ax_norm_desc_t(rows, cols, ld, cols, cols, _mat_of(gy, t.dtype, rows, cols, "gy"), _float_dtype(t, "t"),
+                           _float_dtype(weight, "weight"), 0.0, 1)
+        _vec_of(weight, weight.dtype, cols, "weight")
+        _vec_of(rstd, torch.float32, rows, "rstd")
+        if gsum is not None:
+            d.residual_ld = _mat_of(gsum, t.dtype, rows, cols, "gsum")
+        if gx_out is not False:
+            d.sum_ld = _mat_of(gx_out, t.dtype, rows, cols, "gx_out")
+        if gw_out is not False:
+            _vec_of(gw_out, torch.float32, cols, "gw_out")
+        hit = _remember(key, (d, int(L.ax_rmsnorm_backward_workspace_bytes(d))))
+    d, need = hit
     gx_out, gw_out = (None if o is False else o for o in (gx_out, gw_out))
-    ws = _scratch(int(L.ax_rmsnorm_backward_workspace_bytes(ctypes.byref(d))), workspace, t.device, stream)
-    _check(L.ax_rmsnorm_backward(ctypes.byref(d), _ptr(gy), _ptr(gsum), _ptr(t), _ptr(weight), _ptr(rstd), _ptr(gx_out),
-                                 _ptr(gw_out), *_ws_args(ws), _stream_ptr(stream)))
+    ws = _scratch(need, workspace, t.device, stream)
+    _check(L.ax_rmsnorm_backward(d, _ptr(gy), _ptr(gsum), _ptr(t), _ptr(weight), _ptr(rstd), _ptr(gx_out), _ptr(gw_out),
+                                 *_ws_args(ws), _stream_ptr(stream)))
     return gx_out, gw_out
 
 
-def _matmul_desc(x, w, act, transposed, out_dtype, names=("x", "w")) -> ax_matmul_desc_t:
+def _matmul_desc(x, w, act, transposed, out_dtype, aligned, names=("x", "w")) -> ax_matmul_desc_t:
     M, K, x_ld = _mat(x, x.dtype, names[0])
     wr, wc, w_ld = _mat(w, x.dtype, names[1])
     if w.dim() != 2 or (wc if transposed else wr) != K:
@@ -1020,22 +1054,31 @@ def _matmul_desc(x, w, act, transposed, out_dtype, names=("x", "w")) -> ax_matmu
     odt = _DT.get(out_dtype)
     if odt is None:
         raise TypeError("out_dtype must be float32 or bfloat16")
-    return ax_matmul_desc_t(M, N, K, x_ld, w_ld, N, N, dt, odt, _act_code(act), int(bool(transposed)),
-                            int((x.data_ptr() | w.data_ptr()) % 16 != 0))
+    return ax_matmul_desc_t(M, N, K, x_ld, w_ld, N, N, dt, odt, _act_code(act), int(bool(transposed)), int(not aligned))
 
 
-def _matmul_out(d, out, x, dtype, name):
-    if out is None:
-        out = torch.empty(x.shape[:-1] + (d.N,), dtype=dtype, device=x.device)
-    d.y_ld = _mat_of(out, dtype, d.M, d.N, name)
-    return out
+def _columns(w, transposed) -> int:
+    if w.dim() != 2:
+        raise ValueError("weights must be matrices")
+    return w.shape[0] if transposed else w.shape[1]
 
 
-def _epilogue_args(d, bias, residual, dtype):
+def _epilogue_args(d, bias, residual, y_out, z_out, dtype, name="y_out"):
     if bias is not None:
         _vec_of(bias, dtype, d.N, "bias")
     if residual is not None:
         d.residual_ld = _mat_of(residual, dtype, d.M, d.N, "residual")
+    if z_out is not None:
+        _vec_of(z_out, dtype, d.M * d.N, "z_out")
+    d.y_ld = _mat_of(y_out, dtype, d.M, d.N, name)
+
+
+def _codes_of(x, x_scales, w, w_scales, M, N):
+    for t, name in ((x, "x"), (w, "w")):
+        if t.dtype != torch.int8:
+            raise TypeError("%s must have dtype torch.int8, got %s" % (name, t.dtype))
+    _vec_of(x_scales, torch.float32, M, "x_scales")
+    _vec_of(w_scales, torch.float32, N, "w_scales")
 
 
 def ax_matmul(x, w, bias=None, residual=None, act="none", transposed=False, out_dtype=None, save=False, y_out=None, z_out=None,
@@ -1044,17 +1087,23 @@ def ax_matmul(x, w, bias=None, residual=None, act="none", transposed=False, out_
     residual and the outputs have out_dtype (x's by default).  Returns (y, z): z, the value before the activation, with
     save or z_out, otherwise None."""
     L = lib()
+    dev = x.device
     out_dtype = x.dtype if out_dtype is None else out_dtype
-    d = _matmul_desc(x, w, act, transposed, out_dtype)
-    y_out = _matmul_out(d, y_out, x, out_dtype, "y_out")
-    _epilogue_args(d, bias, residual, out_dtype)
+    if y_out is None:
+        y_out = torch.empty(x.shape[:-1] + (_columns(w, transposed),), dtype=out_dtype, device=dev)
     if z_out is None and save:
-        z_out = torch.empty(x.shape[:-1] + (d.N,), dtype=out_dtype, device=x.device)
-    if z_out is not None:
-        _vec_of(z_out, out_dtype, d.M * d.N, "z_out")
-    ws = _scratch(int(L.ax_matmul_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
-    _check(L.ax_matmul(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(y_out), _ptr(z_out), *_ws_args(ws),
-                       _stream_ptr(stream)))
+        z_out = torch.empty(y_out.shape, dtype=out_dtype, device=dev)
+    xp, wp = x.data_ptr(), w.data_ptr()
+    aligned = (xp | wp) % 16 == 0
+    key = ("matmul", act, transposed, out_dtype, aligned, _sig(x), _sig(w), _sig(bias), _sig(residual), _sig(y_out), _sig(z_out))
+    hit = _checked.get(key)
+    if hit is None:
+        d = _matmul_desc(x, w, act, transposed, out_dtype, aligned)
+        _epilogue_args(d, bias, residual, y_out, z_out, out_dtype)
+        hit = _remember(key, (d, int(L.ax_matmul_workspace_bytes(d))))
+    d, need = hit
+    ws = _scratch(need, workspace, dev, stream)
+    _check(L.ax_matmul(d, xp, wp, _ptr(bias), _ptr(residual), y_out.data_ptr(), _ptr(z_out), *_ws_args(ws), _stream_ptr(stream)))
     return y_out, z_out
 
 
@@ -1063,64 +1112,77 @@ def ax_matmul_q8(x, x_scales, w, w_scales, bias=None, residual=None, act="none",
     """y = act((x * x_scales) (w * w_scales)^T + bias) + residual on int8 codes: x [M,K] with a scale a row (what
     ax_rmsnorm_q8 returns), w [N,K] with a scale a row."""
     L = lib()
-    for t, name in ((x, "x"), (w, "w")):
-        if t.dtype != torch.int8:
-            raise TypeError("%s must have dtype torch.int8, got %s" % (name, t.dtype))
-    d = _matmul_desc(x, w, act, True, out_dtype)
-    _vec_of(x_scales, torch.float32, d.M, "x_scales")
-    _vec_of(w_scales, torch.float32, d.N, "w_scales")
-    y_out = _matmul_out(d, y_out, x, out_dtype, "y_out")
-    _epilogue_args(d, bias, residual, out_dtype)
-    ws = _scratch(int(L.ax_matmul_q8_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
-    _check(L.ax_matmul_q8(ctypes.byref(d), _ptr(x), _ptr(x_scales), _ptr(w), _ptr(w_scales), _ptr(bias), _ptr(residual),
-                          _ptr(y_out), *_ws_args(ws), _stream_ptr(stream)))
+    dev = x.device
+    if y_out is None:
+        y_out = torch.empty(x.shape[:-1] + (_columns(w, True),), dtype=out_dtype, device=dev)
+    xp, wp = x.data_ptr(), w.data_ptr()
+    aligned = (xp | wp) % 16 == 0
+    key = ("matmul_q8", act, out_dtype, aligned, _sig(x), _sig(x_scales), _sig(w), _sig(w_scales), _sig(bias), _sig(residual),
+           _sig(y_out))
+    hit = _checked.get(key)
+    if hit is None:
+        d = _matmul_desc(x, w, act, True, out_dtype, aligned)
+        _codes_of(x, x_scales, w, w_scales, d.M, d.N)
+        _epilogue_args(d, bias, residual, y_out, None, out_dtype)
+        hit = _remember(key, (d, int(L.ax_matmul_q8_workspace_bytes(d))))
+    d, need = hit
+    ws = _scratch(need, workspace, dev, stream)
+    _check(L.ax_matmul_q8(d, xp, x_scales.data_ptr(), wp, w_scales.data_ptr(), _ptr(bias), _ptr(residual), y_out.data_ptr(),
+                          *_ws_args(ws), _stream_ptr(stream)))
     return y_out
+
+
+def _grad_out(out, like):
+    """A gradient with the shape and the row pitch of the tensor that it belongs to."""
+    if out is None:
+        return torch.empty_strided(like.shape, like.stride(), dtype=like.dtype, device=like.device)
+    return out
+
+
+def _check_grad(out, like, ld, name):
+    if out is False:
+        return
+    r, c, _ = _mat(like, like.dtype, name)
+    if _mat_of(out, like.dtype, r, c, name) != ld:
+        raise ValueError("%s must have the row pitch of its tensor" % name)
 
 
 def ax_matmul_backward(gy, x, w, z=None, act="none", transposed=False, gx_out=None, gw_out=None, gb_out=None, workspace=None,
                        stream=None):
     """Gradients of ax_matmul: (gx, gw, gb), gb float32; False skips one.  z: the value before the activation."""
     L = lib()
-    d = _matmul_desc(x, w, act, transposed, x.dtype)
-    d.y_ld = _mat_of(gy, x.dtype, d.M, d.N, "gy")
-    if z is not None:
-        _vec_of(z, x.dtype, d.M * d.N, "z")
-    elif d.act:
-        raise ValueError("the gradient of an activation needs z")
-    if d.act == 0 and gy.data_ptr() % 16:
-        d.unaligned = 1
-    gx_out = _grad_out(gx_out, x, "gx_out", d.x_ld)
-    gw_out = _grad_out(gw_out, w, "gw_out", d.w_ld)
+    dev = x.device
+    gx_out, gw_out = _grad_out(gx_out, x), _grad_out(gw_out, w)
     if gb_out is None:
-        gb_out = torch.empty(d.N, dtype=torch.float32, device=x.device)
-    elif gb_out is not False:
-        _vec_of(gb_out, torch.float32, d.N, "gb_out")
-    gb_out = None if gb_out is False else gb_out
-    ws = _scratch(int(L.ax_matmul_backward_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
-    _check(L.ax_matmul_backward(ctypes.byref(d), _ptr(gy), _ptr(x), _ptr(w), _ptr(z), _ptr(gx_out), _ptr(gw_out), _ptr(gb_out),
-                                *_ws_args(ws), _stream_ptr(stream)))
+        gb_out = torch.empty(_columns(w, transposed), dtype=torch.float32, device=dev)
+    gp, xp, wp = gy.data_ptr(), x.data_ptr(), w.data_ptr()
+    aligned = (xp | wp | (gp if act == "none" else 0)) % 16 == 0
+    key = ("matmul_backward", act, transposed, aligned, _sig(gy), _sig(x), _sig(w), _sig(z), _sig(gx_out), _sig(gw_out), _sig(gb_out))
+    hit = _checked.get(key)
+    if hit is None:
+        d = _matmul_desc(x, w, act, transposed, x.dtype, aligned)
+        d.y_ld = _mat_of(gy, x.dtype, d.M, d.N, "gy")
+        if z is not None:
+            _vec_of(z, x.dtype, d.M * d.N, "z")
+        elif d.act:
+            raise ValueError("the gradient of an activation needs z")
+        _check_grad(gx_out, x, d.x_ld, "gx_out")
+        _check_grad(gw_out, w, d.w_ld, "gw_out")
+        if gb_out is not False:
+            _vec_of(gb_out, torch.float32, d.N, "gb_out")
+        hit = _remember(key, (d, int(L.ax_matmul_backward_workspace_bytes(d))))
+    d, need = hit
+    gx_out, gw_out, gb_out = (None if o is False else o for o in (gx_out, gw_out, gb_out))
+    ws = _scratch(need, workspace, dev, stream)
+    _check(L.ax_matmul_backward(d, gp, xp, wp, _ptr(z), _ptr(gx_out), _ptr(gw_out), _ptr(gb_out), *_ws_args(ws), _stream_ptr(stream)))
     return gx_out, gw_out, gb_out
 
 
-def _grad_out(out, like, name, ld):
-    """A gradient with the shape and the row pitch of the tensor that it belongs to."""
-    if out is False:
-        return None
-    if out is None:
-        return torch.empty_strided(like.shape, like.stride(), dtype=like.dtype, device=like.device)
-    r, c, _ = _mat(like, like.dtype, name)
-    if _mat_of(out, like.dtype, r, c, name) != ld:
-        raise ValueError("%s must have the row pitch of its tensor" % name)
-    return out
-
-
-def _gated_desc(x, wg, wu, act, transposed, out_dtype) -> ax_matmul_desc_t:
-    d = _matmul_desc(x, wg, act, transposed, out_dtype, ("x", "wg"))
+def _gated_desc(x, wg, wu, act, transposed, out_dtype, aligned) -> ax_matmul_desc_t:
+    d = _matmul_desc(x, wg, act, transposed, out_dtype, aligned, ("x", "wg"))
     wr, wc, ld = _mat(wu, x.dtype, "wu")
     if wu.shape != wg.shape or ld != d.w_ld:
         raise ValueError("wg and wu must have one shape and one row pitch")
-    if wu.data_ptr() % 16:
-        d.unaligned = 1
     return d
 
 
@@ -1128,18 +1190,25 @@ def ax_gated(x, wg, wu, act="silu", out_dtype=None, save=False, h_out=None, g_ou
     """h = act(x wg) * (x wu).  x [M,K]; wg, wu [K,F]; float32 or bfloat16.  Returns (h, g, u): both projections with
     save (or g_out and u_out), otherwise None."""
     L = lib()
+    dev = x.device
     out_dtype = x.dtype if out_dtype is None else out_dtype
-    d = _gated_desc(x, wg, wu, act, False, out_dtype)
-    h_out = _matmul_out(d, h_out, x, out_dtype, "h_out")
+    if h_out is None:
+        h_out = torch.empty(x.shape[:-1] + (_columns(wg, False),), dtype=out_dtype, device=dev)
     if save:
-        g_out, u_out = (torch.empty(x.shape[:-1] + (d.N,), dtype=out_dtype, device=x.device) if o is None else o
-                        for o in (g_out, u_out))
-    for o, name in ((g_out, "g_out"), (u_out, "u_out")):
-        if o is not None:
-            _vec_of(o, out_dtype, d.M * d.N, name)
-    ws = _scratch(int(L.ax_gated_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
-    _check(L.ax_gated(ctypes.byref(d), _ptr(x), _ptr(wg), _ptr(wu), _ptr(h_out), _ptr(g_out), _ptr(u_out), *_ws_args(ws),
-                      _stream_ptr(stream)))
+        g_out, u_out = (torch.empty(h_out.shape, dtype=out_dtype, device=dev) if o is None else o for o in (g_out, u_out))
+    xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
+    aligned = (xp | gp | up) % 16 == 0
+    key = ("gated", act, out_dtype, aligned, _sig(x), _sig(wg), _sig(wu), _sig(h_out), _sig(g_out), _sig(u_out))
+    hit = _checked.get(key)
+    if hit is None:
+        d = _gated_desc(x, wg, wu, act, False, out_dtype, aligned)
+        _epilogue_args(d, None, None, h_out, g_out, out_dtype, "h_out")
+        if u_out is not None:
+            _vec_of(u_out, out_dtype, d.M * d.N, "u_out")
+        hit = _remember(key, (d, int(L.ax_gated_workspace_bytes(d))))
+    d, need = hit
+    ws = _scratch(need, workspace, dev, stream)
+    _check(L.ax_gated(d, xp, gp, up, h_out.data_ptr(), _ptr(g_out), _ptr(u_out), *_ws_args(ws), _stream_ptr(stream)))
     return h_out, g_out, u_out
 
 
@@ -1147,33 +1216,50 @@ def ax_gated_q8(x, x_scales, wg, wg_scales, wu, wu_scales, act="silu", out_dtype
                 stream=None):
     """The gated block on int8 codes: x [M,K] and wg, wu [F,K], each with a scale a row."""
     L = lib()
-    for t, name in ((x, "x"), (wg, "wg"), (wu, "wu")):
-        if t.dtype != torch.int8:
-            raise TypeError("%s must have dtype torch.int8, got %s" % (name, t.dtype))
-    d = _gated_desc(x, wg, wu, act, True, out_dtype)
-    _vec_of(x_scales, torch.float32, d.M, "x_scales")
-    _vec_of(wg_scales, torch.float32, d.N, "wg_scales")
-    _vec_of(wu_scales, torch.float32, d.N, "wu_scales")
-    h_out = _matmul_out(d, h_out, x, out_dtype, "h_out")
-    ws = _scratch(int(L.ax_gated_q8_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
-    _check(L.ax_gated_q8(ctypes.byref(d), _ptr(x), _ptr(x_scales), _ptr(wg), _ptr(wg_scales), _ptr(wu), _ptr(wu_scales),
-                         _ptr(h_out), *_ws_args(ws), _stream_ptr(stream)))
+    dev = x.device
+    if h_out is None:
+        h_out = torch.empty(x.shape[:-1] + (_columns(wg, True),), dtype=out_dtype, device=dev)
+    xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
+    aligned = (xp | gp | up) % 16 == 0
+    key = ("gated_q8", act, out_dtype, aligned, _sig(x), _sig(x_scales), _sig(wg), _sig(wg_scales), _sig(wu), _sig(wu_scales),
+           _sig(h_out))
+    hit = _checked.get(key)
+    if hit is None:
+        d = _gated_desc(x, wg, wu, act, True, out_dtype, aligned)
+        _codes_of(x, x_scales, wg, wg_scales, d.M, d.N)
+        _codes_of(x, x_scales, wu, wu_scales, d.M, d.N)
+        _epilogue_args(d, None, None, h_out, None, out_dtype, "h_out")
+        hit = _remember(key, (d, int(L.ax_gated_q8_workspace_bytes(d))))
+    d, need = hit
+    ws = _scratch(need, workspace, dev, stream)
+    _check(L.ax_gated_q8(d, xp, x_scales.data_ptr(), gp, wg_scales.data_ptr(), up, wu_scales.data_ptr(), h_out.data_ptr(),
+                         *_ws_args(ws), _stream_ptr(stream)))
     return h_out
 
 
 def ax_gated_backward(gh, x, wg, wu, g, u, act="silu", gx_out=None, gwg_out=None, gwu_out=None, workspace=None, stream=None):
     """Gradients of ax_gated: (gx, gwg, gwu); gx_out False, or gwg_out and gwu_out False, skips them."""
     L = lib()
-    d = _gated_desc(x, wg, wu, act, False, x.dtype)
-    d.y_ld = _mat_of(gh, x.dtype, d.M, d.N, "gh")
-    _vec_of(g, x.dtype, d.M * d.N, "g")
-    _vec_of(u, x.dtype, d.M * d.N, "u")
-    gx_out = _grad_out(gx_out, x, "gx_out", d.x_ld)
-    gwg_out = _grad_out(gwg_out, wg, "gwg_out", d.w_ld)
-    gwu_out = _grad_out(gwu_out, wu, "gwu_out", d.w_ld)
-    ws = _scratch(int(L.ax_gated_backward_workspace_bytes(ctypes.byref(d))), workspace, x.device, stream)
-    _check(L.ax_gated_backward(ctypes.byref(d), _ptr(gh), _ptr(x), _ptr(wg), _ptr(wu), _ptr(g), _ptr(u), _ptr(gx_out),
-                               _ptr(gwg_out), _ptr(gwu_out), *_ws_args(ws), _stream_ptr(stream)))
+    dev = x.device
+    gx_out, gwg_out, gwu_out = _grad_out(gx_out, x), _grad_out(gwg_out, wg), _grad_out(gwu_out, wu)
+    xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
+    aligned = (xp | gp | up) % 16 == 0
+    key = ("gated_backward", act, aligned, _sig(gh), _sig(x), _sig(wg), _sig(wu), _sig(g), _sig(u), _sig(gx_out), _sig(gwg_out),
+           _sig(gwu_out))
+    hit = _checked.get(key)
+    if hit is None:
+        d = _gated_desc(x, wg, wu, act, False, x.dtype, aligned)
+        d.y_ld = _mat_of(gh, x.dtype, d.M, d.N, "gh")
+        _vec_of(g, x.dtype, d.M * d.N, "g")
+        _vec_of(u, x.dtype, d.M * d.N, "u")
+        for o, like, ld, name in ((gx_out, x, d.x_ld, "gx_out"), (gwg_out, wg, d.w_ld, "gwg_out"), (gwu_out, wu, d.w_ld, "gwu_out")):
+            _check_grad(o, like, ld, name)
+        hit = _remember(key, (d, int(L.ax_gated_backward_workspace_bytes(d))))
+    d, need = hit
+    gx_out, gwg_out, gwu_out = (None if o is False else o for o in (gx_out, gwg_out, gwu_out))
+    ws = _scratch(need, workspace, dev, stream)
+    _check(L.ax_gated_backward(d, gh.data_ptr(), xp, gp, up, g.data_ptr(), u.data_ptr(), _ptr(gx_out), _ptr(gwg_out), _ptr(gwu_out),
+                               *_ws_args(ws), _stream_ptr(stream)))
     return gx_out, gwg_out, gwu_out
 
 
@@ -1249,7 +1335,7 @@ class AxAdamW:
         if grad_scale is not None:
             _vec_of(grad_scale, torch.float32, 1, "grad_scale")
         d.grad_scale = _ptr(grad_scale)
-        _check(lib().ax_adamw(ctypes.byref(d), self._t, len(self._t), _stream_ptr(stream)))
+        _check(lib().ax_adamw(d, self._t, len(self._t), _stream_ptr(stream)))
 
     def states(self, stream=None):
         """(m, v) as lists of float32 tensors: the values that 8-bit states stand for, or the 32-bit states themselves."""

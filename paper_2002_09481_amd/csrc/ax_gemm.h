@@ -49,7 +49,6 @@ struct GemmPlan {
   size_t part_bytes;  // partial sums (0 without slices)
 };
 
-// force_tile / force_splits: 0 = the automatic choice.
 GemmPlan plan_gemm(const GemmArgs& g);
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStream_t s);
 

@@ -1,5 +1,9 @@
 // Matrix products on the matrix cores: bf16 operands with float32 sums, int8 codes with int32 sums.
 #include <algorithm>
+#include <type_traits>
+#ifdef PLANENV
+#include <cstdlib>
+#endif
 
 #include "ax_float.h"
 #include "ax_gemm.h"
@@ -12,9 +16,9 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
+#define AX_INLINE __attribute__((always_inline))
 #define AX_LDS(T) __attribute__((address_space(3))) T
 
-constexpr int kStepBytes = 128;  // contraction bytes per stage: 64 bf16 or 128 int8
 constexpr uint32_t kOut = 0x80000000u;  // an offset behind every buffer: the load gives zeros
 
 struct Args {
@@ -28,50 +32,63 @@ struct Args {
 
 // ---- epilogue ----------------------------------------------------------------------------------
 
-__device__ __forceinline__ void load4(const void* p, long long i, int dt, int left, float (&v)[4]) {
-  if (dt == AX_F32) load_elems<true, 4>(p, i, left, v);
-  else load_elems<false, 4>(p, i, left, v);
+// Eight columns n .. n + 7 of a row, of which `left` are there.
+__device__ __forceinline__ void load8(const void* p, long long i, int dt, int left, float (&v)[8]) {
+  if (dt == AX_F32) load_elems<true, 8>(p, i, left, v);
+  else load_elems<false, 8>(p, i, left, v);
 }
-__device__ __forceinline__ void store4(void* p, long long i, int dt, int left, const float (&v)[4]) {
-  if (dt == AX_F32) store_elems<true, 4>(p, i, left, v);
-  else store_elems<false, 4>(p, i, left, v);
+__device__ __forceinline__ void store8(void* p, long long i, int dt, int left, const float (&v)[8]) {
+  if (dt == AX_F32) store_elems<true, 8>(p, i, left, v);
+  else store_elems<false, 8>(p, i, left, v);
 }
 
-// Columns n .. n + 3 of row m from the finished sums (int8: already scaled).  second: the second output of a dual launch.
-__device__ __forceinline__ void finish(const GemmArgs& g, int m, int n, const float (&s)[4], int second) {
+// What the epilogue needs of eight columns, the same for all rows.
+struct Columns {
+  float bias[8], ws[8], ws2[8];
+};
+template <bool I8, bool GATED>
+__device__ __forceinline__ void load_columns(const GemmArgs& g, int n, Columns& c) {
   const int left = g.N - n;
-  float v[4];
-  for (int e = 0; e < 4; ++e) v[e] = s[e];
-  if (g.bias) {
-    float b[4];
-    load4(g.bias, n, g.odt, left, b);
-    for (int e = 0; e < 4; ++e) v[e] += b[e];
-  }
-  if (g.z) store4(g.z, (long long)m * g.N + n, g.odt, left, v);
-  if (g.act != AX_ACT_NONE)
-    for (int e = 0; e < 4; ++e) v[e] = act_of(v[e], g.act);
-  if (g.res) {
-    float r[4];
-    load4(g.res, (long long)m * g.ldr + n, g.odt, left, r);
-    for (int e = 0; e < 4; ++e) v[e] += r[e];
-  }
-  if (second) store4(g.y2, (long long)m * g.ldy + n, g.odt, left, v);
-  else store4(g.y, (long long)m * g.ldy + n, g.odt, left, v);
+  if (!GATED && g.bias) load8(g.bias, n, g.odt, left, c.bias);
+  if (I8) load_elems<true, 8>(g.ws, n, left, c.ws);
+  if (I8 && GATED) load_elems<true, 8>(g.ws2, n, left, c.ws2);
 }
-__device__ __forceinline__ void finish_gated(const GemmArgs& g, int m, int n, const float (&a)[4], const float (&u)[4]) {
+// Columns n .. n + 7 of row m from their finished sums (GATED: of both projections; int8: sums as integers in s and s2).
+// second: the second output of a dual launch.
+template <bool I8, bool GATED>
+__device__ __forceinline__ void finish(const GemmArgs& g, const Columns& c, int m, int n, const f32x4 (&s)[2], const f32x4 (&s2)[2], int second) {
   const int left = g.N - n;
-  if (g.z) store4(g.z, (long long)m * g.N + n, g.odt, left, a);
-  if (g.z2) store4(g.z2, (long long)m * g.N + n, g.odt, left, u);
-  float v[4];
-  for (int e = 0; e < 4; ++e) v[e] = act_of(a[e], g.act) * u[e];
-  store4(g.y, (long long)m * g.ldy + n, g.odt, left, v);
-}
-// int8: scales of four columns and of a row.
-__device__ __forceinline__ void scaled4(const int32_t (&c)[4], float xs, const float* ws, int n, int N, float (&v)[4]) {
-  for (int e = 0; e < 4; ++e) v[e] = (float)c[e] * (xs * (n + e < N ? ws[n + e] : 0.f));
+  float v[8], u[8];
+  const float xs = I8 ? g.xs[m] : 1.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    v[e] = I8 ? (float)__float_as_int(s[e >> 2][e & 3]) * (xs * c.ws[e]) : s[e >> 2][e & 3];
+    if (GATED) u[e] = I8 ? (float)__float_as_int(s2[e >> 2][e & 3]) * (xs * c.ws2[e]) : s2[e >> 2][e & 3];
+  }
+  if (!GATED && g.bias) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += c.bias[e];
+  }
+  if (g.z) store8(g.z, (long long)m * g.N + n, g.odt, left, v);
+  if (GATED && g.z2) store8(g.z2, (long long)m * g.N + n, g.odt, left, u);
+  apply_act(v, g.act);
+  if (GATED) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= u[e];
+  }
+  if (!GATED && g.res) {
+    load8(g.res, (long long)m * g.ldr + n, g.odt, left, u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += u[e];
+  }
+  store8(!GATED && second ? g.y2 : g.y, (long long)m * g.ldy + n, g.odt, left, v);
 }
 
 // ---- main kernel -------------------------------------------------------------------------------
+
+// A value that is the same in all lanes, in a scalar register: the quotients of scalars are worked out in vector ones.
+template <typename T>
+__device__ __forceinline__ T uniform(T x) { return (T)__builtin_amdgcn_readfirstlane((int)x); }
 
 // 16 bytes per lane from memory to LDS at dst + 16 * lane (dst uniform over the wave).  Written as instructions: of a
 // copy that it knows, the compiler makes every later LDS read wait, since it cannot tell the stages apart.
@@ -79,60 +96,78 @@ __device__ __forceinline__ void lds_copy(uint32_t dst, uint32_t off, const u32x4
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :: "s"(dst), "v"(off), "s"(rsrc) : "memory");
 }
+// At most N copies under way, LDS reads done (the built-in, not an instruction: the compiler then knows that it need not
+// wait for those reads itself).
 template <int N>
 __device__ __forceinline__ void wait_copies() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | 0x70 | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
 }
 __device__ __forceinline__ void wg_barrier() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
 
-// One operand's share of the copies.  L = 0: rows of kStepBytes, contraction contiguous; a row's eight 16-byte chunks
-// are stored at chunk ^ ((row >> 1) & 7), which gives the 16 lanes of each pass of a 16-byte LDS read 16 different
-// slots of the 64 banks.  L = 1 (bf16): 64 rows (the contraction) of R elements; 32-byte chunk pairs are stored at
-// pair ^ (bits 0, 1 and 3 of the row), for the transposing 8-byte reads.
-template <int L, int R, int THREADS>
+// Where a stage keeps a row's 16-byte chunk of the contraction: at chunk ^ swizzle(row).  A 16-byte LDS read is served in
+// passes of 16 lanes, lanes 0-3, 12-15, 20-23 and 24-27 of 32 and their complement; lane l of a fragment reads row l % 16,
+// chunk l / 16, and the swizzles give the 16 lanes of a pass 16 different slots of the 64 banks.
+template <int KB>
+__device__ __forceinline__ int swizzle(int row) {
+  return KB == 128 ? (row >> 1) & 7 : (-(row >> 2)) & 3;
+}
+
+// One operand's share of the copies.  L = 0: R rows of KB bytes, contraction contiguous.  L = 1 (bf16): KB / 2 rows (the
+// contraction) of R elements; 32-byte chunk pairs are stored at pair ^ (bits 0, 1 and 3 of the row), for the transposing
+// 8-byte reads.
+template <int L, int R, int KB, int THREADS>
 struct Stager {
-  static constexpr int kLoads = R * kStepBytes / 16 / THREADS;
-  static_assert(kLoads >= 1, "a copy per thread at least");
-  static constexpr int kRowChunks = L == 0 ? 8 : R / 8;
+  static constexpr int kLoads = R * KB / 16 / THREADS;
+  static_assert(kLoads >= 1 && kLoads * 16 * THREADS == R * KB, "whole copies per thread");
+  static constexpr int kRowChunks = L == 0 ? KB / 16 : R / 8;
   static constexpr int kPairMask = R / 16 - 1;  // L = 1
-  uint32_t off[kLoads];
-  int chunk;  // L = 0: this thread's chunk (the same in all its copies)
+  static_assert(THREADS / kRowChunks % 16 == 0, "the swizzle is the same in all copies of a thread");
+  uint32_t off;   // of this thread's first copy; the others follow at `step`
+  uint32_t step;  // uniform
+  int chunk;      // L = 0: this thread's chunk (the same in all its copies)
 
   __device__ __forceinline__ void init(int t, long long ld, int cols_left) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int q = i * THREADS + t;
-      const int row = q / kRowChunks, pos = q % kRowChunks;
-      if (L == 0) {
-        chunk = pos ^ ((row >> 1) & 7);
-        off[i] = (uint32_t)(row * ld + chunk * 16);
-      } else {
-        const int sp = ((row & 3) | ((row >> 1) & 4)) & kPairMask;
-        const int c = pos ^ (sp << 1);
-        off[i] = c * 8 < cols_left ? (uint32_t)(row * ld + c * 16) : kOut;
-      }
+    const int row = t / kRowChunks, pos = t % kRowChunks;
+    step = (uint32_t)(THREADS / kRowChunks * ld);
+    if (L == 0) {
+      chunk = pos ^ swizzle<KB>(row);
+      off = (uint32_t)(row * ld + chunk * 16);
+    } else {
+      const int sp = ((row & 3) | ((row >> 1) & 4)) & kPairMask;
+      const int c = pos ^ (sp << 1);
+      off = c * 8 < cols_left ? (uint32_t)(row * ld + c * 16) : kOut;
     }
   }
+  struct Copy {  // of one stage: kLoads pieces
+    u32x4 rsrc;
+    uint32_t off;
+  };
   // base: first byte of the stage's tile, rem: bytes from there to the operand's end, kleft: bytes of the contraction
   // left in the segment (L = 0: chunks behind them are zeros; L = 1: rows behind them lie behind the end).
-  __device__ __forceinline__ void copy(uint32_t lds, const char* base, long long rem, int kleft) const {
+  __device__ __forceinline__ Copy begin(const char* base, long long rem, int kleft) const {
     const uint32_t n = rem > 0x7fffffffll ? 0x7fffffffu : (uint32_t)rem;
-    const u32x4 rsrc = {(uint32_t)(uintptr_t)base, (uint32_t)((uintptr_t)base >> 32) & 0xffffu, n, 0x00020000u};
-    const bool mine = L == 1 || chunk * 16 < kleft;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) lds_copy(lds + i * (THREADS * 16), mine ? off[i] : kOut, rsrc);
+    return Copy{u32x4{uniform((uint32_t)(uintptr_t)base), uniform((uint32_t)((uintptr_t)base >> 32) & 0xffffu), uniform(n), 0x00020000u},
+                L == 1 || chunk * 16 < kleft ? off : kOut};
+  }
+  __device__ __forceinline__ void piece(Copy& c, uint32_t lds, int i) const {
+    lds_copy(lds + i * (THREADS * 16), c.off, c.rsrc);
+    // (added here every time: kept in registers, the offsets of all pieces are many.  kOut stays behind every buffer: the
+    // steps add up to less than 2^31.)
+    if (i + 1 < kLoads) asm volatile("v_add_u32 %0, %1, %0" : "+v"(c.off) : "s"(step));
   }
 };
 
-// The matrix instruction's operand for 16 rows starting at r0, contraction elements 16 g .. (bytes) of half ks.
-template <int L, int R>
+// The matrix instruction's operand for 16 rows starting at r0, bytes 16 g .. of 64-byte part ks of a stage.
+template <int L, int R, int KB>
 __device__ __forceinline__ u32x4 fragment(uint32_t lds, int r0, int ks, int lane) {
   const int r = lane & 15, g = lane >> 4;
   if (L == 0) {
-    const uint32_t a = lds + (uint32_t)((r0 + r) * kStepBytes + (((ks * 4 + g) ^ ((r >> 1) & 7)) << 4));
+    const uint32_t a = lds + (uint32_t)((r0 + r) * KB + (((ks * 4 + g) ^ swizzle<KB>(r)) << 4));
     return *(const AX_LDS(u32x4)*)(uintptr_t)a;
   }
   const int kr = r >> 2;
@@ -160,16 +195,21 @@ struct Acc<true> {
 };
 
 // I8: int8 codes.  LA, LB: operand layouts.  NB: 2 for the gated pair (the tile's BN columns are BN/2 columns of both
-// projections).  WM x WN waves, STAGES stages of LDS.
-template <bool I8, int LA, int LB, int NB, int BM, int BN, int WM, int WN, int STAGES, int OCC>
+// projections).  WM x WN waves; STAGES stages of KB contraction bytes in LDS.
+//
+// The wave holds the fragments of 64 bytes of the contraction in registers and reads the next ones while the matrix
+// instructions of these run.  Where the next ones are another stage's, a barrier in front of that says that they have arrived
+// and that this stage's place is free, and the copies of stage + STAGES are asked for.
+template <bool I8, int LA, int LB, int NB, int BM, int BN, int WM, int WN, int KB, int STAGES, int OCC>
 __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   constexpr int THREADS = 64 * WM * WN;
   constexpr int BNS = BN / NB;                // columns of one right operand
   constexpr int MF = BM / WM / 16, NF = BN / WN / 16;
-  constexpr int kABytes = BM * kStepBytes, kBBytes = BNS * kStepBytes;
+  constexpr int KK = KB / 64;                 // matrix instructions' contraction steps per stage
+  constexpr int kABytes = BM * KB, kBBytes = BNS * KB;
   constexpr int kStage = kABytes + NB * kBBytes;
-  typedef Stager<LA, BM, THREADS> SA;
-  typedef Stager<LB, BNS, THREADS> SB;
+  typedef Stager<LA, BM, KB, THREADS> SA;
+  typedef Stager<LB, BNS, KB, THREADS> SB;
   constexpr int kLoads = SA::kLoads + NB * SB::kLoads;
   __shared__ __align__(1024) unsigned char smem[STAGES * kStage];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(AX_LDS(unsigned char)*)smem;
@@ -187,14 +227,14 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
     const int b = blockIdx.x, x = b & 7, i = b >> 3, per = total >> 3, more = total & 7;
     tile = x * per + min(x, more) + i;
   }
-  const int split = tile / (a.tiles_m * a.tiles_n);
+  const int split = uniform(tile / (a.tiles_m * a.tiles_n));
   tile -= split * (a.tiles_m * a.tiles_n);
   int tm, tn;
   {
-    const int band = 8 * a.tiles_n, b = tile / band, r = tile - b * band;
+    const int band = 8 * a.tiles_n, b = uniform(tile / band), r = tile - b * band;
     const int h = min(8, a.tiles_m - 8 * b);
-    tm = 8 * b + r % h;
-    tn = r / h;
+    tn = uniform(r / h);
+    tm = 8 * b + r - tn * h;
   }
   int second = 0;
   if (NB == 1 && g.dual) {
@@ -205,7 +245,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   const int m0 = tm * BM, n0 = tn * BNS;
 
   const int steps = g.nseg * a.ksteps;
-  const int s_beg = (int)((long long)steps * split / a.splits), s_end = (int)((long long)steps * (split + 1) / a.splits);
+  const int s_beg = uniform((int)((long long)steps * split / a.splits)), s_end = uniform((int)((long long)steps * (split + 1) / a.splits));
   const int n_st = s_end - s_beg;
 
   SA sa;
@@ -215,8 +255,8 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
 
   // the next stage to copy: segment, stage within it, operand positions
   constexpr int kElem = I8 ? 1 : 2;
-  constexpr int kStepK = kStepBytes / kElem;
-  const long long a_step = LA == 0 ? kStepBytes : kStepK * g.lda, b_step = LB == 0 ? kStepBytes : kStepK * g.ldb;
+  constexpr int kStepK = KB / kElem;
+  const long long a_step = LA == 0 ? KB : kStepK * g.lda, b_step = LB == 0 ? KB : kStepK * g.ldb;
   // bytes from the tile's first element to the operand's end; rows are whole 16-byte chunks, and a chunk that only began
   // in front of the end would not be loaded at all
   const long long row_bytes = ((long long)g.K * kElem + 15) & ~15ll;
@@ -224,10 +264,10 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
                                   : (long long)(g.K - 1) * g.lda + (long long)(((g.M + 7) & ~7) - m0) * kElem;
   const long long b_all = LB == 0 ? (long long)(g.N - 1 - n0) * g.ldb + row_bytes
                                   : (long long)(g.K - 1) * g.ldb + (long long)(((g.N + 7) & ~7) - n0) * kElem;
-  int seg = s_beg / a.ksteps, ks = s_beg - seg * a.ksteps;
+  int seg = uniform(s_beg / a.ksteps), ks = s_beg - seg * a.ksteps;
   const char *pa, *pb, *pb2;
   long long ra, rb;
-  auto at_segment = [&]() {
+  auto at_segment = [&]() AX_INLINE {
     const long long ao = LA == 0 ? (long long)m0 * g.lda : (long long)m0 * kElem;
     const long long bo = LB == 0 ? (long long)n0 * g.ldb : (long long)n0 * kElem;
     pa = (const char*)g.seg[seg].a + ao + ks * a_step;
@@ -237,12 +277,26 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
     rb = b_all - ks * b_step;
   };
   at_segment();
-  auto issue = [&](int buf) {
-    const uint32_t l = lds0 + (uint32_t)(buf * kStage + wave * 1024);
+  struct Copies {
+    typename SA::Copy a;
+    typename SB::Copy b, b2;
+    uint32_t lds;
+  };
+  auto copies_begin = [&](int buf) AX_INLINE {
     const int kleft = (g.K - ks * kStepK) * kElem;
-    sa.copy(l, pa, ra, kleft);
-    sb.copy(l + kABytes, pb, rb, kleft);
-    if (NB == 2) sb.copy(l + kABytes + kBBytes, pb2, rb, kleft);
+    Copies c;
+    c.a = sa.begin(pa, ra, kleft);
+    c.b = sb.begin(pb, rb, kleft);
+    if (NB == 2) c.b2 = sb.begin(pb2, rb, kleft);
+    c.lds = uniform(lds0 + (uint32_t)(buf * kStage + wave * 1024));
+    return c;
+  };
+  auto copies_piece = [&](Copies& c, int i) AX_INLINE {
+    if (i < SA::kLoads) sa.piece(c.a, c.lds, i);
+    else if (i < SA::kLoads + SB::kLoads) sb.piece(c.b, c.lds + kABytes, i - SA::kLoads);
+    else sb.piece(c.b2, c.lds + kABytes + kBBytes, i - SA::kLoads - SB::kLoads);
+  };
+  auto copies_end = [&]() AX_INLINE {  // the next stage
     if (++ks == a.ksteps) {
       ks = 0;
       if (++seg < g.nseg) at_segment();
@@ -262,156 +316,252 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
     for (int j = 0; j < NF; ++j) acc[i][j] = typename Acc<I8>::T{};
 
   const int wrow = wm * (BM / WM), wcol = wn * (BNS / WN);
-  auto compute = [&](int buf) {
+  struct Fragments {
+    u32x4 a[MF], b[NF];
+  };
+  auto read = [&](Fragments& f, int buf, int kk, int i) AX_INLINE {  // fragment i of MF + NF
     const uint32_t la = lds0 + (uint32_t)(buf * kStage), lb = la + kABytes;
+    if (i < NF)
+      f.b[i] = NB == 2 ? fragment<LB, BNS, KB>(lb + (i & 1) * kBBytes, wcol + 16 * (i >> 1), kk, lane)
+                       : fragment<LB, BNS, KB>(lb, wcol + 16 * i, kk, lane);
+    else
+      f.a[i - NF] = fragment<LA, BM, KB>(la, wrow + 16 * (i - NF), kk, lane);
+  };
+
+  // Stages asked for: it + STAGES when stage it is multiplied.
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      u32x4 fb[NF], fa[MF];
+  for (int s = 0; s < STAGES; ++s)
+    if (s < n_st) {
+      Copies c = copies_begin(s);
 #pragma unroll
-      for (int j = 0; j < NF; ++j)
-        fb[j] = NB == 2 ? fragment<LB, BNS>(lb + (j & 1) * kBBytes, wcol + 16 * (j >> 1), kk, lane)
-                        : fragment<LB, BNS>(lb, wcol + 16 * j, kk, lane);
+      for (int i = 0; i < kLoads; ++i) copies_piece(c, i);
+      copies_end();
+    }
+  int buf = 0;
+  Fragments f0, f1;
+  if (n_st >= STAGES) wait_copies<(STAGES - 1) * kLoads>();
+  else wait_copies<0>();
+  wg_barrier();
 #pragma unroll
-      for (int i = 0; i < MF; ++i) fa[i] = fragment<LA, BM>(la, wrow + 16 * i, kk, lane);
+  for (int i = 0; i < MF + NF; ++i) read(f0, 0, 0, i);
+  // Part kk of stage `it`, whose fragments `now` holds; `next` gets those of the part behind it.  steady: there is a stage
+  // it + STAGES to ask for.  Copies and LDS reads are spread evenly among the matrix instructions, row by row.
+  auto turn = [&](auto steady, int it, int kk, const Fragments& now, Fragments& next) AX_INLINE {
+    const bool last = kk + 1 == KK;
+    const int nbuf = !last ? buf : buf + 1 == STAGES ? 0 : buf + 1;
+    const bool more = !last || steady || it + 1 < n_st;
+    if (last && more) {
+      // behind stage it + 1, STAGES - 2 have been asked for (fewer at the end)
+      if (steady || it + STAGES <= n_st) wait_copies<(STAGES - 2) * kLoads>();
+      else wait_copies<0>();
+      wg_barrier();
+    }
+    if constexpr (steady) {
+      Copies c;
+      if (last) c = copies_begin(buf);
+#pragma unroll
+      for (int i = 0; i < MF; ++i) {
+#pragma unroll
+        for (int k = i * kLoads / MF; k < (i + 1) * kLoads / MF; ++k)
+          if (last) copies_piece(c, k);
+#pragma unroll
+        for (int k = i * (MF + NF) / MF; k < (i + 1) * (MF + NF) / MF; ++k) read(next, nbuf, last ? 0 : kk + 1, k);
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = Acc<I8>::mma(now.b[j], now.a[i], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (last) copies_end();
+    } else {
+      if (last && it + STAGES < n_st) {
+        Copies c = copies_begin(buf);
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) copies_piece(c, k);
+        copies_end();
+      }
+      if (more) {
+#pragma unroll
+        for (int k = 0; k < MF + NF; ++k) read(next, nbuf, last ? 0 : kk + 1, k);
+      }
 #pragma unroll
       for (int i = 0; i < MF; ++i)
 #pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = Acc<I8>::mma(fb[j], fa[i], acc[i][j]);
+        for (int j = 0; j < NF; ++j) acc[i][j] = Acc<I8>::mma(now.b[j], now.a[i], acc[i][j]);
+    }
+    buf = nbuf;
+  };
+  // stages in pairs, so that each part finds its fragments in the same registers every time
+  auto two = [&](auto steady, int it) AX_INLINE {
+    if constexpr (KK == 1) {
+      turn(steady, it, 0, f0, f1);
+      if (steady || it + 1 < n_st) turn(steady, it + 1, 0, f1, f0);
+    } else {
+      turn(steady, it, 0, f0, f1);
+      turn(steady, it, 1, f1, f0);
     }
   };
+  constexpr int PER = KK == 1 ? 2 : 1;
+  int it = 0;
+  for (; it + STAGES + PER - 1 < n_st; it += PER) two(std::true_type{}, it);
+  for (; it < n_st; it += PER) two(std::false_type{}, it);
 
+  // ---- epilogue: a lane holds row m, columns n .. n + 3 of every 16 x 16 block.  Through LDS (a part of it for each wave)
+  // so that rows are stored in whole lines: eight columns a lane, the wave's columns of a row side by side.
+  constexpr int COLS = NF * 16, OUT = COLS / NB;    // columns in LDS, of the result
+  constexpr int PITCH = COLS * 4 + 16;
+  constexpr int ROUND = MF >= 2 ? 32 : 16;          // rows a turn
+  constexpr int LPR = OUT / 8, RPI = 64 / LPR;      // lanes a row, rows a pass
+  static_assert(ROUND * PITCH * WM * WN <= STAGES * kStage && ROUND % RPI == 0, "a part of LDS for each wave");
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  wg_barrier();  // the stages are read
+  const uint32_t mine = lds0 + (uint32_t)(wave * ROUND * PITCH);
+  const int lm = lane & 15, lq = lane >> 4;
+  const int orow = lane / LPR, ocol = lane % LPR * 8;
+  const int n = n0 + wcol + ocol;
+  Columns cols;
+  if (a.splits == 1 && n < g.N) load_columns<I8, NB == 2>(g, n, cols);
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s)
-    if (s < n_st) issue(s);
-  int buf = 0;
-  for (int it = 0; it < n_st; ++it) {
-    if (n_st - 1 - it >= STAGES - 2) wait_copies<(STAGES - 2) * kLoads>();
-    else wait_copies<0>();
-    wg_barrier();
-    if (it + STAGES - 1 < n_st) issue(buf == 0 ? STAGES - 1 : buf - 1);
-    compute(buf);
-    buf = buf + 1 == STAGES ? 0 : buf + 1;
-  }
-
-  // lane: row m, columns n .. n + 3 of every 16 x 16 block
-  const int lm = lane & 15, ln = (lane >> 4) * 4;
+  for (int i0 = 0; i0 < MF; i0 += ROUND / 16) {
 #pragma unroll
-  for (int i = 0; i < MF; ++i) {
-    const int m = m0 + wrow + 16 * i + lm;
-    if (m >= g.M) continue;
+    for (int i = 0; i < ROUND / 16; ++i)
 #pragma unroll
-    for (int j = 0; j < NF; j += NB) {
-      const int n = n0 + wcol + 16 * (j / NB) + ln;
-      if (n >= g.N) continue;
-      if (a.splits > 1) {
+      for (int j = 0; j < NF; ++j) {
+        const int c = NB == 2 ? (j & 1) * OUT + 16 * (j >> 1) : 16 * j;
+        *(AX_LDS(u32x4)*)(uintptr_t)(mine + (uint32_t)((16 * i + lm) * PITCH + (c + 4 * lq) * 4)) =
+            __builtin_bit_cast(u32x4, acc[i0 + i][j]);
+      }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int r = 0; r < ROUND; r += RPI) {
+      const int m = m0 + wrow + 16 * i0 + r + orow;
+      const uint32_t at = mine + (uint32_t)((r + orow) * PITCH + ocol * 4);
+      f32x4 s[2], s2[2];
+      s[0] = *(const AX_LDS(f32x4)*)(uintptr_t)at;
+      s[1] = *(const AX_LDS(f32x4)*)(uintptr_t)(at + 16);
+      if (NB == 2) {
+        s2[0] = *(const AX_LDS(f32x4)*)(uintptr_t)(at + OUT * 4);
+        s2[1] = *(const AX_LDS(f32x4)*)(uintptr_t)(at + OUT * 4 + 16);
+      }
+      if (m >= g.M || n >= g.N) continue;
+      if (a.splits > 1) {  // (rows of ldp, a multiple of eight)
         const long long plane = (long long)g.M * a.ldp;
         const int planes = NB == 2 || g.dual ? 2 : 1;
         float* p = a.part + ((long long)split * planes + second) * plane + (long long)m * a.ldp + n;
-        *(u32x4*)p = __builtin_bit_cast(u32x4, acc[i][j]);
-        if (NB == 2) *(u32x4*)(p + plane) = __builtin_bit_cast(u32x4, acc[i][j + NB - 1]);
-        continue;
-      }
-      float v[4], u[4];
-      if (I8) {
-        const float xs = g.xs[m];
-        int32_t c[4], c2[4];
-        for (int e = 0; e < 4; ++e) {
-          c[e] = (int32_t)acc[i][j][e];
-          c2[e] = (int32_t)acc[i][j + NB - 1][e];
+        *(f32x4*)p = s[0];
+        *(f32x4*)(p + 4) = s[1];
+        if (NB == 2) {
+          *(f32x4*)(p + plane) = s2[0];
+          *(f32x4*)(p + plane + 4) = s2[1];
         }
-        scaled4(c, xs, g.ws, n, g.N, v);
-        if (NB == 2) scaled4(c2, xs, g.ws2, n, g.N, u);
       } else {
-        for (int e = 0; e < 4; ++e) {
-          v[e] = (float)acc[i][j][e];
-          u[e] = (float)acc[i][j + NB - 1][e];
-        }
+        finish<I8, NB == 2>(g, cols, m, n, s, s2, second);
       }
-      if (NB == 2) finish_gated(g, m, n, v, u);
-      else finish(g, m, n, v, second);
     }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
-// Partial sums of the slices, added in their order, and the epilogue: four columns a thread.
-template <bool I8>
+// Partial sums of the slices, added in their order, and the epilogue: eight columns a thread.
+template <bool I8, bool GATED>
 __global__ __launch_bounds__(256) void gemm_join_kernel(const Args a) {
   const GemmArgs& g = a.g;
-  const int quads = (int)(a.ldp >> 2);
-  const int planes = g.gated || g.dual ? 2 : 1;
+  const int groups = (int)(a.ldp >> 3);
+  const int planes = GATED || g.dual ? 2 : 1;
   const int outs = g.dual ? 2 : 1;
   const long long plane = (long long)g.M * a.ldp;
-  const long long total = (long long)outs * g.M * quads;
+  const long long total = (long long)outs * g.M * groups;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-    const int second = i >= (long long)g.M * quads;
-    const long long r = i - (second ? (long long)g.M * quads : 0);
-    const int m = (int)(r / quads), n = (int)(r - (long long)m * quads) * 4;
-    float v[2][4];
+    const int second = i >= (long long)g.M * groups;
+    const long long r = i - (second ? (long long)g.M * groups : 0);
+    const int m = (int)(r / groups), n = (int)(r - (long long)m * groups) * 8;
+    Columns cols;
+    load_columns<I8, GATED>(g, n, cols);
+    f32x4 s[2][2];
 #pragma unroll
-    for (int pl = 0; pl < 2; ++pl) {
-      if (pl && !g.gated) break;
-      const float* p = a.part + (long long)(second + pl) * plane + (long long)m * a.ldp + n;
-      if (I8) {
-        i32x4 s = {0, 0, 0, 0};
-        for (int k = 0; k < a.splits; ++k) s += *(const i32x4*)(p + (long long)k * planes * plane);
-        int32_t c[4] = {s[0], s[1], s[2], s[3]};
-        scaled4(c, g.xs[m], pl ? g.ws2 : g.ws, n, g.N, v[pl]);
-      } else {
-        f32x4 s = *(const f32x4*)p;
-        for (int k = 1; k < a.splits; ++k) s += *(const f32x4*)(p + (long long)k * planes * plane);
-        for (int e = 0; e < 4; ++e) v[pl][e] = s[e];
+    for (int pl = 0; pl < (GATED ? 2 : 1); ++pl)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float* p = a.part + (long long)(second + pl) * plane + (long long)m * a.ldp + n + 4 * h;
+        const long long step = (long long)planes * plane;
+        if (I8) {
+          i32x4 t = *(const i32x4*)p;
+          for (int k = 1; k < a.splits; ++k) t += *(const i32x4*)(p + k * step);
+          s[pl][h] = __builtin_bit_cast(f32x4, t);
+        } else {
+          f32x4 t = *(const f32x4*)p;
+          for (int k = 1; k < a.splits; ++k) t += *(const f32x4*)(p + k * step);
+          s[pl][h] = t;
+        }
       }
-    }
-    if (g.gated) finish_gated(g, m, n, v[0], v[1]);
-    else finish(g, m, n, v[0], second);
+    finish<I8, GATED>(g, cols, m, n, s[0], s[GATED ? 1 : 0], second);
   }
 }
 
+// Tile configurations.  per_cu: workgroups that fit a compute unit (LDS).  Times in us, measured on products that fill
+// the card with one kind of tile: of a workgroup (prologue, epilogue), and of 128 contraction bytes with one workgroup per
+// compute unit and with per_cu of them.
 struct TileShape {
-  int bm, bn, wgs;  // wgs: workgroups per compute unit
+  int bm, bn, per_cu;
+  double fixed, step1, step;
 };
-constexpr TileShape kTiles[3] = {{256, 256, 1}, {128, 128, 2}, {32, 128, 2}};
+constexpr int kStageBytes = 128;
+constexpr int kNumTiles = 4;
+constexpr TileShape kTiles[kNumTiles] = {
+    {256, 256, 1, 6.0, 1.50, 1.50}, {128, 128, 2, 3.0, 0.70, 0.95}, {64, 128, 2, 2.5, 0.39, 0.65}, {32, 128, 2, 2.0, 0.26, 0.45}};
 
 template <bool I8, int LA, int LB, int NB>
 void launch_tile(const Args& a, int tile, int grid, hipStream_t s) {
   switch (tile) {
-    case 0: gemm_kernel<I8, LA, LB, NB, 256, 256, 2, 4, 2, 2><<<grid, 512, 0, s>>>(a); break;
-    case 1: gemm_kernel<I8, LA, LB, NB, 128, 128, 2, 2, 2, 2><<<grid, 256, 0, s>>>(a); break;
-    default:
-      if constexpr (LA == 0) gemm_kernel<I8, LA, LB, NB, 32, 128, 1, 4, 3, 2><<<grid, 256, 0, s>>>(a);
+    case 0: gemm_kernel<I8, LA, LB, NB, 256, 256, 2, 4, kStageBytes, 2, 2><<<grid, 512, 0, s>>>(a); break;
+    case 1: gemm_kernel<I8, LA, LB, NB, 128, 128, 2, 2, kStageBytes, 2, 2><<<grid, 256, 0, s>>>(a); break;
+    case 2: gemm_kernel<I8, LA, LB, NB, 64, 128, 1, 4, kStageBytes, 3, 2><<<grid, 256, 0, s>>>(a); break;
+    default:  // (copies of 32 columns whose rows are the contraction would not fill the threads)
+      if constexpr (LA == 0) gemm_kernel<I8, LA, LB, NB, 32, 128, 1, 4, kStageBytes, 3, 2><<<grid, 256, 0, s>>>(a);
       break;
   }
 }
 
+constexpr int kCus = 256;
+constexpr int kMaxSplits = 16;
+
+long long tiles_of(const GemmArgs& g, const TileShape& t) {
+  const int bns = t.bn / (g.gated ? 2 : 1);
+  return (long long)((g.M + t.bm - 1) / t.bm) * ((g.N + bns - 1) / bns) * (g.dual ? 2 : 1);
+}
+long long part_pitch(const GemmArgs& g) { return ((long long)g.N + 7) / 8 * 8; }
+
 }  // namespace
 
+// The tile configuration and the slices of the contraction with the least estimated time: rounds of workgroups over the
+// card, each a fixed part and its stages; the slices' partial sums (written and read once, at 6.5 bytes a picosecond) and the
+// launch that adds them.  Large products get the large tiles, few tiles are cut along the contraction.
 GemmPlan plan_gemm(const GemmArgs& g) {
-  const int elem = g.i8 ? 1 : 2, kstep = kStepBytes / elem;
-  const int ksteps = (g.K + kstep - 1) / kstep, steps = ksteps * g.nseg;
-  const int cus = 256;
+  const long long kbytes = (long long)g.K * (g.i8 ? 1 : 2);
+  const long long steps = (kbytes + kStageBytes - 1) / kStageBytes * g.nseg;
+  const double outs = g.gated || g.dual ? 2 : 1;
   GemmPlan best{};
-  double best_t = 1e30;
-  for (int t = 0; t < 3; ++t) {
-    if (t == 2 && g.la != 0) continue;
+  double least = 1e300;
+  for (int t = 0; t < kNumTiles; ++t) {
+    if (t == 3 && g.la != 0) continue;
     const TileShape& T = kTiles[t];
-    const int bns = T.bn / (g.gated ? 2 : 1);
-    const long long tiles = (long long)((g.M + T.bm - 1) / T.bm) * ((g.N + bns - 1) / bns) * (g.dual ? 2 : 1);
-    const long long slots = (long long)cus * T.wgs;
-    for (int sp = 1; sp <= 16 && sp * 4 <= std::max(4, steps); sp *= 2) {
-      const long long rounds = (tiles * sp + slots - 1) / slots;
-      // a stage of the tile, in units of a 128 x 128 x 64 step of a workgroup that has its unit half for itself
-      const double step = t == 0 ? 1.75 : t == 1 ? 1.0 : 0.55;
-      double cost = rounds * ((steps + sp - 1) / sp * step + 6.0);
-      if (sp > 1) cost += 8.0 + sp * (double)g.M * g.N * (g.gated || g.dual ? 2 : 1) * 8.0 / 4e6;
-      if (cost < best_t) {
-        best_t = cost;
+    const long long tiles = tiles_of(g, T);
+    for (int sp = 1; sp <= kMaxSplits && (sp == 1 || sp * 2 <= steps); ++sp) {
+      const long long n = tiles * sp, slots = (long long)kCus * T.per_cu;
+      const long long full = n / slots, rest = n - full * slots;
+      const double stages = (double)((steps + sp - 1) / sp);
+      double cost = full * (T.fixed + stages * T.step);
+      if (rest) cost += T.fixed + stages * (rest <= kCus ? T.step1 : T.step);
+      if (sp > 1) cost += 3.0 + sp * outs * g.M * (double)g.N * 8.0 / 6.5e6;
+      if (cost < least) {
+        least = cost;
         best.tile = t;
         best.splits = sp;
       }
     }
   }
-  const long long ldp = (g.N + 3) / 4 * 4;
-  best.part_bytes = best.splits > 1 ? (size_t)best.splits * (g.gated || g.dual ? 2 : 1) * g.M * ldp * 4 : 0;
+#ifdef PLANENV
+  if (getenv("AXT")) { best.tile = atoi(getenv("AXT")); best.splits = atoi(getenv("AXS")); }
+#endif
+  best.part_bytes = best.splits > 1 ? (size_t)best.splits * (size_t)outs * (size_t)g.M * (size_t)part_pitch(g) * 4 : 0;
   return best;
 }
 
@@ -419,14 +569,13 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStre
   Args a;
   a.g = g;
   const TileShape& T = kTiles[p.tile];
-  const int bns = T.bn / (g.gated ? 2 : 1);
-  const int kstep = kStepBytes / (g.i8 ? 1 : 2);
+  const int kstep = kStageBytes / (g.i8 ? 1 : 2);
   a.tiles_m = (g.M + T.bm - 1) / T.bm;
-  a.tiles_n = (g.N + bns - 1) / bns * (g.dual ? 2 : 1);
+  a.tiles_n = (int)(tiles_of(g, T) / a.tiles_m);
   a.ksteps = (g.K + kstep - 1) / kstep;
   a.splits = p.splits;
   a.part = (float*)part;
-  a.ldp = (g.N + 3) / 4 * 4;
+  a.ldp = part_pitch(g);
   const long long grid = (long long)a.tiles_m * a.tiles_n * p.splits;
   if (grid <= 0 || grid > 0x7fffffffll) return hipErrorInvalidValue;
   const int n = (int)grid;
@@ -444,10 +593,10 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStre
   }
   hipError_t rc = hipGetLastError();
   if (rc != hipSuccess || p.splits == 1) return rc;
-  const long long quads = (long long)(g.dual ? 2 : 1) * g.M * (a.ldp / 4);
-  const int jg = (int)std::min<long long>((quads + 255) / 256, 4096);
-  if (g.i8) gemm_join_kernel<true><<<jg, 256, 0, s>>>(a);
-  else gemm_join_kernel<false><<<jg, 256, 0, s>>>(a);
+  const long long groups = (long long)(g.dual ? 2 : 1) * g.M * (a.ldp / 8);
+  const int jg = (int)std::min<long long>((groups + 255) / 256, 8192);
+  if (g.i8) g.gated ? gemm_join_kernel<true, true><<<jg, 256, 0, s>>>(a) : gemm_join_kernel<true, false><<<jg, 256, 0, s>>>(a);
+  else g.gated ? gemm_join_kernel<false, true><<<jg, 256, 0, s>>>(a) : gemm_join_kernel<false, false><<<jg, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -197,16 +197,19 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const GradArgs a) {
       float gy[8], z[8], u[8];
       load_elems<DT == AX_F32, 8>(a.gy, (long long)r * a.ldy + c, left, gy);
       if (GATED || a.z) load_elems<DT == AX_F32, 8>(a.z, (long long)r * a.N + c, left, z);
-      if (GATED) {
-        float gu[8];
-        load_elems<DT == AX_F32, 8>(a.u, (long long)r * a.N + c, left, u);
-        for (int e = 0; e < 8; ++e) {
-          gu[e] = gy[e] * act_of(z[e], a.act);
-          gy[e] = gy[e] * u[e] * act_slope(z[e], a.act);
+      if (GATED || a.z) {
+        float v[8], sl[8];
+        act_and_slope(z, a.act, v, sl);
+        if (GATED) {
+          load_elems<DT == AX_F32, 8>(a.u, (long long)r * a.N + c, left, u);
+          for (int e = 0; e < 8; ++e) {
+            v[e] *= gy[e];
+            gy[e] = gy[e] * u[e] * sl[e];
+          }
+          write_planes<DT>(a.gu, a.M, a.pcols, r, c, v);
+        } else {
+          for (int e = 0; e < 8; ++e) gy[e] *= sl[e];
         }
-        write_planes<DT>(a.gu, a.M, a.pcols, r, c, gu);
-      } else if (a.z) {
-        for (int e = 0; e < 8; ++e) gy[e] *= act_slope(z[e], a.act);
       }
       if (a.gz) write_planes<DT>(a.gz, a.M, a.pcols, r, c, gy);
       if (!GATED)
