@@ -953,13 +953,13 @@ def _norm_desc(x, residual, sum_out, weight, eps, normalize) -> ax_norm_desc_t:
 def ax_rmsnorm(x, weight, residual=None, eps=1e-5, sum_out=None, y_out=None, rstd_out=None, stream=None):
     """Root-mean-square norm of rows: t = x + residual, y = t * rstd * weight.  Returns (y, t, rstd); t is None without
     a residual.  sum_out may be x or residual themselves; False skips t (or rstd)."""
-    if residual is not None and sum_out is None:
-        sum_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if y_out is None:
-        y_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if rstd_out is None:
-        rstd_out = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     key = ("rmsnorm", eps, _sig(x), _sig(weight), _sig(residual), _sig(sum_out), _sig(y_out), _sig(rstd_out))
+    if residual is not None and sum_out is None:
+        sum_out = torch.empty_like(x)
+    if y_out is None:
+        y_out = torch.empty_like(x)
+    if rstd_out is None:
+        rstd_out = x.new_empty(x.shape[:-1], dtype=torch.float32)
     d = _checked.get(key)
     if d is None:
         d = _norm_desc(x, residual, sum_out, weight, eps, True)
@@ -978,17 +978,16 @@ def ax_rmsnorm_q8(x, weight=None, residual=None, eps=1e-5, normalize=True, sum_o
     """The norm's output as int8 codes with a scale a row: y = codes * scales[:, None].  normalize False: the rows
     themselves (times weight).  Returns (codes, scales, t, values); values, the float32 values that the codes stand for,
     is None unless asked for."""
-    dev = x.device
-    if residual is not None and sum_out is None:
-        sum_out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-    if codes_out is None:
-        codes_out = torch.empty(x.shape, dtype=torch.int8, device=dev)
-    if scales_out is None:
-        scales_out = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
-    if values_out is None and values:
-        values_out = torch.empty(x.shape, dtype=torch.float32, device=dev)
     key = ("rmsnorm_q8", eps, normalize, _sig(x), _sig(weight), _sig(residual), _sig(sum_out), _sig(codes_out), _sig(scales_out),
            _sig(values_out))
+    if residual is not None and sum_out is None:
+        sum_out = torch.empty_like(x)
+    if codes_out is None:
+        codes_out = torch.empty_like(x, dtype=torch.int8, memory_format=torch.contiguous_format)
+    if scales_out is None:
+        scales_out = x.new_empty(x.shape[:-1], dtype=torch.float32)
+    if values_out is None and values:
+        values_out = torch.empty_like(x, dtype=torch.float32, memory_format=torch.contiguous_format)
     d = _checked.get(key)
     if d is None:
         d = _norm_desc(x, residual, sum_out, weight, eps, normalize)
@@ -1017,11 +1016,11 @@ def ax_rmsnorm_backward(gy, t, weight, rstd, gsum=None, gx_out=None, gw_out=None
     """Gradients of ax_rmsnorm: (gx, gw), gx for x and residual alike, gw float32.  t, rstd: what the forward pass
     returned (t = x without a residual); gsum: the gradient that reaches t from the residual stream.  False skips one."""
     L = lib()
-    if gx_out is None:
-        gx_out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-    if gw_out is None:
-        gw_out = torch.empty(weight.shape, dtype=torch.float32, device=t.device)
     key = ("rmsnorm_backward", _sig(gy), _sig(t), _sig(weight), _sig(rstd), _sig(gsum), _sig(gx_out), _sig(gw_out))
+    if gx_out is None:
+        gx_out = torch.empty_like(t)
+    if gw_out is None:
+        gw_out = torch.empty_like(weight, dtype=torch.float32)
     hit = _checked.get(key)
     if hit is None:
         rows, cols, ld = _mat(t, t.dtype, "t")
@@ -1089,13 +1088,14 @@ def ax_matmul(x, w, bias=None, residual=None, act="none", transposed=False, out_
     L = lib()
     dev = x.device
     out_dtype = x.dtype if out_dtype is None else out_dtype
-    if y_out is None:
-        y_out = torch.empty(x.shape[:-1] + (_columns(w, transposed),), dtype=out_dtype, device=dev)
-    if z_out is None and save:
-        z_out = torch.empty(y_out.shape, dtype=out_dtype, device=dev)
     xp, wp = x.data_ptr(), w.data_ptr()
     aligned = (xp | wp) % 16 == 0
-    key = ("matmul", act, transposed, out_dtype, aligned, _sig(x), _sig(w), _sig(bias), _sig(residual), _sig(y_out), _sig(z_out))
+    key = ("matmul", act, transposed, out_dtype, aligned, save, _sig(x), _sig(w), _sig(bias), _sig(residual), _sig(y_out),
+           _sig(z_out))
+    if y_out is None:
+        y_out = x.new_empty(x.shape[:-1] + (_columns(w, transposed),), dtype=out_dtype)
+    if z_out is None and save:
+        z_out = torch.empty_like(y_out, memory_format=torch.contiguous_format)
     hit = _checked.get(key)
     if hit is None:
         d = _matmul_desc(x, w, act, transposed, out_dtype, aligned)
@@ -1113,12 +1113,12 @@ def ax_matmul_q8(x, x_scales, w, w_scales, bias=None, residual=None, act="none",
     ax_rmsnorm_q8 returns), w [N,K] with a scale a row."""
     L = lib()
     dev = x.device
-    if y_out is None:
-        y_out = torch.empty(x.shape[:-1] + (_columns(w, True),), dtype=out_dtype, device=dev)
     xp, wp = x.data_ptr(), w.data_ptr()
     aligned = (xp | wp) % 16 == 0
     key = ("matmul_q8", act, out_dtype, aligned, _sig(x), _sig(x_scales), _sig(w), _sig(w_scales), _sig(bias), _sig(residual),
            _sig(y_out))
+    if y_out is None:
+        y_out = x.new_empty(x.shape[:-1] + (_columns(w, True),), dtype=out_dtype)
     hit = _checked.get(key)
     if hit is None:
         d = _matmul_desc(x, w, act, True, out_dtype, aligned)
@@ -1152,12 +1152,12 @@ def ax_matmul_backward(gy, x, w, z=None, act="none", transposed=False, gx_out=No
     """Gradients of ax_matmul: (gx, gw, gb), gb float32; False skips one.  z: the value before the activation."""
     L = lib()
     dev = x.device
-    gx_out, gw_out = _grad_out(gx_out, x), _grad_out(gw_out, w)
-    if gb_out is None:
-        gb_out = torch.empty(_columns(w, transposed), dtype=torch.float32, device=dev)
     gp, xp, wp = gy.data_ptr(), x.data_ptr(), w.data_ptr()
     aligned = (xp | wp | (gp if act == "none" else 0)) % 16 == 0
     key = ("matmul_backward", act, transposed, aligned, _sig(gy), _sig(x), _sig(w), _sig(z), _sig(gx_out), _sig(gw_out), _sig(gb_out))
+    gx_out, gw_out = _grad_out(gx_out, x), _grad_out(gw_out, w)
+    if gb_out is None:
+        gb_out = x.new_empty(_columns(w, transposed), dtype=torch.float32)
     hit = _checked.get(key)
     if hit is None:
         d = _matmul_desc(x, w, act, transposed, x.dtype, aligned)
@@ -1192,13 +1192,13 @@ def ax_gated(x, wg, wu, act="silu", out_dtype=None, save=False, h_out=None, g_ou
     L = lib()
     dev = x.device
     out_dtype = x.dtype if out_dtype is None else out_dtype
-    if h_out is None:
-        h_out = torch.empty(x.shape[:-1] + (_columns(wg, False),), dtype=out_dtype, device=dev)
-    if save:
-        g_out, u_out = (torch.empty(h_out.shape, dtype=out_dtype, device=dev) if o is None else o for o in (g_out, u_out))
     xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
     aligned = (xp | gp | up) % 16 == 0
-    key = ("gated", act, out_dtype, aligned, _sig(x), _sig(wg), _sig(wu), _sig(h_out), _sig(g_out), _sig(u_out))
+    key = ("gated", act, out_dtype, aligned, save, _sig(x), _sig(wg), _sig(wu), _sig(h_out), _sig(g_out), _sig(u_out))
+    if h_out is None:
+        h_out = x.new_empty(x.shape[:-1] + (_columns(wg, False),), dtype=out_dtype)
+    if save:
+        g_out, u_out = (torch.empty_like(h_out, memory_format=torch.contiguous_format) if o is None else o for o in (g_out, u_out))
     hit = _checked.get(key)
     if hit is None:
         d = _gated_desc(x, wg, wu, act, False, out_dtype, aligned)
@@ -1217,12 +1217,12 @@ def ax_gated_q8(x, x_scales, wg, wg_scales, wu, wu_scales, act="silu", out_dtype
     """The gated block on int8 codes: x [M,K] and wg, wu [F,K], each with a scale a row."""
     L = lib()
     dev = x.device
-    if h_out is None:
-        h_out = torch.empty(x.shape[:-1] + (_columns(wg, True),), dtype=out_dtype, device=dev)
     xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
     aligned = (xp | gp | up) % 16 == 0
     key = ("gated_q8", act, out_dtype, aligned, _sig(x), _sig(x_scales), _sig(wg), _sig(wg_scales), _sig(wu), _sig(wu_scales),
            _sig(h_out))
+    if h_out is None:
+        h_out = x.new_empty(x.shape[:-1] + (_columns(wg, True),), dtype=out_dtype)
     hit = _checked.get(key)
     if hit is None:
         d = _gated_desc(x, wg, wu, act, True, out_dtype, aligned)
@@ -1241,11 +1241,11 @@ def ax_gated_backward(gh, x, wg, wu, g, u, act="silu", gx_out=None, gwg_out=None
     """Gradients of ax_gated: (gx, gwg, gwu); gx_out False, or gwg_out and gwu_out False, skips them."""
     L = lib()
     dev = x.device
-    gx_out, gwg_out, gwu_out = _grad_out(gx_out, x), _grad_out(gwg_out, wg), _grad_out(gwu_out, wu)
     xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
     aligned = (xp | gp | up) % 16 == 0
     key = ("gated_backward", act, aligned, _sig(gh), _sig(x), _sig(wg), _sig(wu), _sig(g), _sig(u), _sig(gx_out), _sig(gwg_out),
            _sig(gwu_out))
+    gx_out, gwg_out, gwu_out = _grad_out(gx_out, x), _grad_out(gwg_out, wg), _grad_out(gwu_out, wu)
     hit = _checked.get(key)
     if hit is None:
         d = _gated_desc(x, wg, wu, act, False, x.dtype, aligned)

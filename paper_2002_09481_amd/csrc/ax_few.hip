@@ -1,0 +1,320 @@
+// Products with few rows on the left (a token, or a handful decoded together): every weight is read once and met by all rows.
+//
+// Bound by memory: 2 M operations for each weight.  So nothing is staged: a workgroup of 16 waves takes 16 to 64 columns
+// of the result, its waves take turns along the contraction, and a lane loads weights straight into the registers that the
+// matrix instruction wants (16 columns x 32 of the contraction, 64 for int8), several steps ahead of their use.  The
+// waves' sums meet in LDS, in the waves' order, and the epilogue follows there: one launch, no partial sums in memory.
+//
+// Weights [N, K]: a lane holds 8 (int8: 16) consecutive elements of a row, what the instruction wants.  Weights [K, N]: a
+// lane loads V neighbouring columns of eight rows, and the eight values of a column are put together by byte permutes;
+// lane r of a fragment then stands for columns V r .. V r + V - 1, one for each of V matrix instructions.  float32 operands
+// are cut into their three bf16 pieces in registers.
+#include <algorithm>
+
+#include "ax_float.h"
+#include "ax_gemm.h"
+
+namespace ax {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 16, kThreads = 64 * kWaves;
+enum Kind { kBf16, kInt8, kF32 };
+
+struct Args {
+  GemmArgs g;
+  int blocks;  // of the contraction, per segment
+};
+
+// One operand of the matrix instruction: bf16 or int8 as they are, float32 as three pieces.
+template <Kind KD>
+struct Frag {
+  u32x4 p[KD == kF32 ? 3 : 1];
+};
+
+// Eight float32 values in three pieces, smallest pieces last.
+__device__ __forceinline__ void pieces_of(const float (&v)[8], u32x4 (&p)[3]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    uint32_t a[3], b[3];
+    split3(v[2 * e], a[0], a[1], a[2]);
+    split3(v[2 * e + 1], b[0], b[1], b[2]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) p[k][e] = a[k] | (b[k] << 16);
+  }
+}
+
+template <Kind KD, typename Acc>
+__device__ __forceinline__ Acc mma(const Frag<KD>& a, const Frag<KD>& b, Acc c) {
+  if constexpr (KD == kInt8) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a.p[0]), __builtin_bit_cast(i32x4, b.p[0]), c, 0, 0, 0);
+  } else if constexpr (KD == kBf16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.p[0]), __builtin_bit_cast(bf16x8, b.p[0]), c, 0, 0, 0);
+  } else {
+    constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+    for (int i = 0; i < 6; ++i)
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.p[pa[i]]), __builtin_bit_cast(bf16x8, b.p[pb[i]]), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// A lane's share of a row with the contraction contiguous: raw bytes (32 for float32), `left` elements of them there.
+template <Kind KD>
+struct Along {
+  u32x4 q[KD == kF32 ? 2 : 1];
+  template <bool FULL>
+  __device__ __forceinline__ void load(const char* row, int k, int left) {
+    constexpr int E = KD == kInt8 ? 16 : 8, B = KD == kInt8 ? 1 : KD == kBf16 ? 2 : 4;
+    const char* p = row + (long long)k * B;
+    if (FULL || left >= E) {
+      q[0] = load_any<u32x4>(p);
+      if (KD == kF32) q[KD == kF32 ? 1 : 0] = load_any<u32x4>(p + 16);
+      return;
+    }
+#pragma unroll
+    for (int w = 0; w < E * B / 4; ++w) {
+      uint32_t v = 0;
+#pragma unroll
+      for (int e = 0; e < 4 / B; ++e) {
+        const int i = w * (4 / B) + e;
+        if (i < left) {
+          if (B == 1) v |= (uint32_t)((const uint8_t*)p)[i] << (8 * e);
+          else if (B == 2) v |= (uint32_t)((const uint16_t*)p)[i] << (16 * e);
+          else v = ((const uint32_t*)p)[i];
+        }
+      }
+      q[w >> 2][w & 3] = v;
+    }
+  }
+  __device__ __forceinline__ void fragment(Frag<KD>& f) const {
+    if constexpr (KD == kF32) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(q[e >> 2][e & 3]);
+      pieces_of(v, f.p);
+    } else {
+      f.p[0] = q[0];
+    }
+  }
+};
+
+// A lane's share of eight rows of V columns.
+template <Kind KD, int V>
+struct Across {
+  static constexpr int W = V * (KD == kF32 ? 4 : 2) / 4;  // words a row
+  uint32_t d[8][W];
+  // p: first row's first column; rows_left, cols_left: how many of each there are
+  template <bool FULL>
+  __device__ __forceinline__ void load(const char* p, long long ld, int rows_left, int cols_left) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const char* r = p + j * ld;
+      if (FULL) {
+        typedef uint32_t words __attribute__((ext_vector_type(W)));
+        const words v = load_any<words>(r);
+#pragma unroll
+        for (int w = 0; w < W; ++w) d[j][w] = W == 1 ? ((const uint32_t*)&v)[0] : v[w];
+        continue;
+      }
+#pragma unroll
+      for (int w = 0; w < W; ++w) d[j][w] = 0;
+#pragma unroll
+      for (int c = 0; c < V; ++c)
+        if (j < rows_left && c < cols_left) {
+          if (KD == kF32) d[j][c] = ((const uint32_t*)r)[c];
+          else d[j][c >> 1] |= (uint32_t)((const uint16_t*)r)[c] << (16 * (c & 1));
+        }
+    }
+  }
+  __device__ __forceinline__ void fragment(int v, Frag<KD>& f) const {
+    if constexpr (KD == kF32) {
+      float t[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = __uint_as_float(d[e][v]);
+      pieces_of(t, f.p);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        f.p[0][e] = __builtin_amdgcn_perm(d[2 * e + 1][v >> 1], d[2 * e][v >> 1], (v & 1) ? 0x07060302u : 0x05040100u);
+    }
+  }
+};
+
+// LB: 0 = weights [N, K], 1 = [K, N].  NB: 2 for the gated pair.  MFR: fragments of 16 rows.  CF: fragments of 16 columns
+// of one weight (LB = 1: neighbouring columns a lane).  U: steps of the contraction a wave loads at a time.
+template <Kind KD, int LB, int NB, int MFR, int CF, int U>
+__global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
+  constexpr int KS = KD == kInt8 ? 64 : 32, LANE = KS / 4;  // contraction of a step, of a lane
+  constexpr int ES = KD == kInt8 ? 1 : KD == kBf16 ? 2 : 4;
+  constexpr int COLS = 16 * CF;
+  typedef typename std::conditional<KD == kInt8, i32x4, f32x4>::type Acc;
+  __shared__ __align__(16) float part[kWaves][NB][16 * MFR][COLS + 4];
+  const GemmArgs& g = a.g;
+  const int t = threadIdx.x, lane = t & 63, r = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  // workgroups b, b + 8, ... share an XCD: they take neighbouring columns, which may share lines of memory
+  int tile;
+  {
+    const int b = blockIdx.x, x = b & 7, i = b >> 3, total = gridDim.x, per = total >> 3, more = total & 7;
+    tile = x * per + min(x, more) + i;
+  }
+  const int n0 = tile * COLS;
+
+  Acc acc[NB][MFR][CF];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < MFR; ++i)
+#pragma unroll
+      for (int j = 0; j < CF; ++j) acc[b][i][j] = Acc{};
+
+  const bool all_cols = n0 + COLS <= g.N;
+  const int groups = (a.blocks + U - 1) / U;
+  for (int it = wave; it < groups * g.nseg; it += kWaves) {
+    const int seg = __builtin_amdgcn_readfirstlane(g.nseg == 1 ? 0 : it / groups);
+    const int k0 = (it - seg * groups) * U * KS;
+    const char* x = (const char*)g.seg[seg].a;
+    const char* w[2] = {(const char*)g.seg[seg].b, (const char*)g.seg[seg].b2};
+    auto run = [&](auto full) __attribute__((always_inline)) {
+      Along<KD> xa[U][MFR];
+      typename std::conditional<LB == 0, Along<KD>, Across<KD == kInt8 ? kBf16 : KD, CF>>::type wa[U][NB][LB == 0 ? CF : 1];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = k0 + u * KS + LANE * q, left = g.K - k;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          if constexpr (LB == 0) {
+#pragma unroll
+            for (int j = 0; j < CF; ++j) {  // (rows behind the last: their results are not stored)
+              const int n = min(n0 + 16 * j + r, g.N - 1);
+              wa[u][b][j].template load<full>(w[b] + n * g.ldb, k, left);
+            }
+          } else {
+            const int c = n0 + CF * r;
+            wa[u][b][0].template load<full>(w[b] + k * g.ldb + (long long)c * ES, g.ldb, left, g.N - c);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < MFR; ++i) xa[u][i].template load<full>(x + min(16 * i + r, g.M - 1) * g.lda, k, left);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        Frag<KD> fx[MFR];
+#pragma unroll
+        for (int i = 0; i < MFR; ++i) xa[u][i].fragment(fx[i]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int j = 0; j < CF; ++j) {
+            Frag<KD> fw;
+            if constexpr (LB == 0) wa[u][b][j].fragment(fw);
+            else wa[u][b][0].fragment(j, *(Frag<KD == kInt8 ? kBf16 : KD>*)&fw);
+#pragma unroll
+            for (int i = 0; i < MFR; ++i) acc[b][i][j] = mma<KD>(fw, fx[i], acc[b][i][j]);
+          }
+      }
+    };
+    if (k0 + U * KS <= g.K && (LB == 0 || all_cols)) run(std::true_type{});
+    else run(std::false_type{});
+  }
+
+  // lane: row m = r of the fragment, weight rows 4 q .. 4 q + 3 of it
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < MFR; ++i)
+#pragma unroll
+      for (int j = 0; j < CF; ++j) {
+        const f32x4 v = __builtin_bit_cast(f32x4, acc[b][i][j]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[wave][b][16 * i + r][LB == 0 ? 16 * j + 4 * q + e : CF * (4 * q + e) + j] = v[e];
+      }
+  __syncthreads();
+  for (int o = t; o < 16 * MFR * COLS; o += kThreads) {
+    const int m = o / COLS, c = o - m * COLS, n = n0 + c;
+    if (m >= g.M || n >= g.N) continue;
+    float s[2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      if (KD == kInt8) {
+        int32_t v = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v += __float_as_int(part[w][b][m][c]);
+        s[b] = (float)v * (g.xs[m] * (b ? g.ws2 : g.ws)[n]);
+      } else {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v += part[w][b][m][c];
+        s[b] = v;
+      }
+    }
+    auto put = [&](void* p, long long i, float v) {
+      if (g.odt == AX_F32) ((float*)p)[i] = v;
+      else ((uint16_t*)p)[i] = (uint16_t)f32_to_bf16(v);
+    };
+    auto get = [&](const void* p, long long i) { return g.odt == AX_F32 ? ((const float*)p)[i] : bf16_to_f32(((const uint16_t*)p)[i]); };
+    float v[1] = {s[0]};
+    if (NB == 1 && g.bias) v[0] += get(g.bias, n);
+    if (g.z) put(g.z, (long long)m * g.N + n, v[0]);
+    if (NB == 2 && g.z2) put(g.z2, (long long)m * g.N + n, s[1]);
+    apply_act(v, g.act);
+    if (NB == 2) v[0] *= s[1];
+    if (NB == 1 && g.res) v[0] += get(g.res, (long long)m * g.ldr + n);
+    put(g.y, (long long)m * g.ldy + n, v[0]);
+  }
+}
+
+// Columns of a workgroup: as many as leave a workgroup for every compute unit (wider pieces of a line, fewer reads of x).
+template <Kind KD, int LB, int NB, int MFR>
+void launch_cols(const Args& a, hipStream_t s) {
+  constexpr int U = KD == kF32 ? 2 / NB : 4 / NB;  // (what 128 registers a lane hold)
+  auto go = [&](auto cf) {
+    constexpr int CF = decltype(cf)::value;
+    few_kernel<KD, LB, NB, MFR, CF, U><<<(a.g.N + 16 * CF - 1) / (16 * CF), kThreads, 0, s>>>(a);
+  };
+  if constexpr (LB == 0) {
+    if constexpr (MFR * NB < 4) {
+      if (a.g.N >= 8192) return go(std::integral_constant<int, 2>{});
+    }
+    go(std::integral_constant<int, 1>{});
+  } else {
+    if constexpr (KD == kBf16 && MFR * NB == 1) {
+      if (a.g.N >= 16384) return go(std::integral_constant<int, 4>{});
+    }
+    go(std::integral_constant<int, 2>{});
+  }
+}
+template <Kind KD, int LB, int NB>
+void launch_rows(const Args& a, hipStream_t s) {
+  if constexpr (KD != kF32) {
+    if (a.g.M > 16) return launch_cols<KD, LB, NB, 2>(a, s);
+  }
+  launch_cols<KD, LB, NB, 1>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_few(const GemmArgs& g, int dtype, hipStream_t s) {
+  Args a;
+  a.g = g;
+  const int ks = g.i8 ? 64 : 32;
+  a.blocks = (g.K + ks - 1) / ks;
+  if (g.i8) {
+    if (g.gated) launch_rows<kInt8, 0, 2>(a, s);
+    else launch_rows<kInt8, 0, 1>(a, s);
+  } else if (dtype == AX_BF16) {
+    if (g.gated) launch_rows<kBf16, 1, 2>(a, s);
+    else if (g.lb == 0) launch_rows<kBf16, 0, 1>(a, s);
+    else launch_rows<kBf16, 1, 1>(a, s);
+  } else {
+    if (g.gated) launch_rows<kF32, 1, 2>(a, s);
+    else if (g.lb == 0) launch_rows<kF32, 0, 1>(a, s);
+    else launch_rows<kF32, 1, 1>(a, s);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace ax

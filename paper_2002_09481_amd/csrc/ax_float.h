@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "ax_internal.h"
 
@@ -72,6 +73,24 @@ __device__ __forceinline__ void store_elems(void* p, long long i, int left, cons
       if (F32) ((float*)p)[i + e] = v[e];
       else ((uint16_t*)p)[i + e] = (uint16_t)f32_to_bf16(v[e]);
     }
+}
+
+// a = p0 + p1 + p2 exactly: each piece is what is left, cut after eight significant bits.  An infinity or a NaN goes into
+// the first piece alone; what it meets comes out as NaN or infinity (not always the one that float32 gives: a piece of the
+// other factor may be zero).
+__device__ __forceinline__ void split3(float a, uint32_t& p0, uint32_t& p1, uint32_t& p2) {
+  const uint32_t b = __float_as_uint(a);
+  if ((b & 0x7f800000u) == 0x7f800000u) {
+    p0 = (b >> 16) | ((b & 0x7fffffu) ? 0x40u : 0u);
+    p1 = p2 = 0;
+    return;
+  }
+  const float r1 = a - __uint_as_float(b & 0xffff0000u);
+  const uint32_t b1 = __float_as_uint(r1);
+  const float r2 = r1 - __uint_as_float(b1 & 0xffff0000u);
+  p0 = b >> 16;
+  p1 = b1 >> 16;
+  p2 = __float_as_uint(r2) >> 16;
 }
 
 // Activations in float32, with the fast exponential and reciprocal (a few units in the last place each), against results

@@ -460,6 +460,21 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   }
 }
 
+// The slices' sums in their order, four loads at a time.
+template <bool I8>
+__device__ __forceinline__ f32x4 sum_slices(const float* p, long long step, int n) {
+  typedef typename Acc<I8>::T T;
+  T t = *(const T*)p;
+  int k = 1;
+  for (; k + 4 <= n; k += 4) {
+    const T a = *(const T*)(p + k * step), b = *(const T*)(p + (k + 1) * step), c = *(const T*)(p + (k + 2) * step),
+            d = *(const T*)(p + (k + 3) * step);
+    t = t + a + b + c + d;
+  }
+  for (; k < n; ++k) t += *(const T*)(p + k * step);
+  return __builtin_bit_cast(f32x4, t);
+}
+
 // Partial sums of the slices, added in their order, and the epilogue: eight columns a thread.
 template <bool I8, bool GATED>
 __global__ __launch_bounds__(256) void gemm_join_kernel(const Args a) {
@@ -481,16 +496,7 @@ __global__ __launch_bounds__(256) void gemm_join_kernel(const Args a) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const float* p = a.part + (long long)(second + pl) * plane + (long long)m * a.ldp + n + 4 * h;
-        const long long step = (long long)planes * plane;
-        if (I8) {
-          i32x4 t = *(const i32x4*)p;
-          for (int k = 1; k < a.splits; ++k) t += *(const i32x4*)(p + k * step);
-          s[pl][h] = __builtin_bit_cast(f32x4, t);
-        } else {
-          f32x4 t = *(const f32x4*)p;
-          for (int k = 1; k < a.splits; ++k) t += *(const f32x4*)(p + k * step);
-          s[pl][h] = t;
-        }
+        s[pl][h] = sum_slices<I8>(p, (long long)planes * plane, a.splits);
       }
     finish<I8, GATED>(g, cols, m, n, s[0], s[GATED ? 1 : 0], second);
   }

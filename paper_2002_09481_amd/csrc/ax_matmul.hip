@@ -50,24 +50,6 @@ struct PackJob {
 };
 constexpr int kI8 = 2;
 
-// a = p0 + p1 + p2 exactly: each piece is what is left, cut after eight significant bits.  An infinity or a NaN goes into
-// the first piece alone; what it meets comes out as NaN or infinity (not always the one that float32 gives: a piece of the
-// other factor may be zero).
-__device__ __forceinline__ void split3(float a, uint32_t& p0, uint32_t& p1, uint32_t& p2) {
-  const uint32_t b = __float_as_uint(a);
-  if ((b & 0x7f800000u) == 0x7f800000u) {
-    p0 = (b >> 16) | ((b & 0x7fffffu) ? 0x40u : 0u);
-    p1 = p2 = 0;
-    return;
-  }
-  const float r1 = a - __uint_as_float(b & 0xffff0000u);
-  const uint32_t b1 = __float_as_uint(r1);
-  const float r2 = r1 - __uint_as_float(b1 & 0xffff0000u);
-  p0 = b >> 16;
-  p1 = b1 >> 16;
-  p2 = __float_as_uint(r2) >> 16;
-}
-
 // Rows copied into the form the products read: eight elements (16 bytes of output; int8: 16) a thread.  Bound by
 // memory: 4 bytes read and 6 written per float32 element.
 template <int DT>
@@ -281,17 +263,61 @@ bool ws_ok(const void* ws, size_t have, size_t need) {
 struct Forward {
   PackJob jobs[3];
   int njobs;
+  bool few;  // launch_few, on the operands themselves
+  int dtype;
   GemmArgs g;
   GemmPlan plan;
   void* part;
   size_t bytes;
 };
 
+// Whether a product of M rows is worth launch_few: one launch that reads the weights once, against tiles with slices of the
+// contraction and the launch that adds them.  Times in us at rows / K / N, weights from memory, few : tiles.
+//   float32 (no copies in pieces)       16/2048/2048 15 : 32     1/4096/4096 29 : 71
+//   weights [N, K]                      1/4096/4096 9.7 : 17.8   24/4096/4096 14.7 : 14.9   int8 32/4096/4096 9.3 : 12.8
+//   bf16 [K, N], rows of one workgroup far apart: short contractions, or up to four rows
+//                                       1/2048/2048 6.8 : 12.4   32/2048/8192 12.9 : 13.8   16/4096/8192 21.8 : 19.1
+//                                       1/4096/4096 14.9 : 16.2  16/4096/4096 17.8 : 14.7   1/8192/2048 23.7 : 16.6
+//   int8 gated, where one launch of tiles has enough of them
+//                                       1/4096/4096 7.8 : 14.7   16/2048/6000 8.9 : 9.0     17/4096/10240 23.3 : 17.3
+bool few_fits(int dtype, bool along, bool gated, long long M, long long N, long long K) {
+  if (dtype == AX_F32) return M <= 16;
+  if (M > 32) return false;
+  if (dtype == kI8 && gated) return N <= 8192 && M * N <= 98304;
+  return along || K <= 2048 || (M <= 4 && K <= 4096);
+}
+
+// x [M, K] times w as it lies.
+GemmArgs few_args(const ax_matmul_desc_t* d, bool q8, const void* x, const void* w, const void* w2) {
+  GemmArgs g{};
+  const int esz = q8 ? 1 : elem_bytes(d->dtype);
+  g.seg[g.nseg++] = GemmSeg{x, w, w2};
+  g.i8 = q8;
+  g.lb = d->w_transposed ? 0 : 1;
+  g.M = (int)d->M;
+  g.N = (int)d->N;
+  g.K = (int)d->K;
+  g.lda = d->x_ld * esz;
+  g.ldb = d->w_ld * esz;
+  g.odt = d->out_dtype;
+  g.act = d->act;
+  g.ldy = d->y_ld;
+  return g;
+}
+
 Forward make_forward(const ax_matmul_desc_t* d, bool q8, bool gated, const void* x, const void* w, const void* w2, void* ws) {
   Forward f{};
   Arena ar(ws);
   const int dt = q8 ? kI8 : d->dtype;
   const long long wr = d->w_transposed ? d->N : d->K, wc = d->w_transposed ? d->K : d->N;
+  f.dtype = dt;
+  f.few = few_fits(dt, d->w_transposed, gated, d->M, d->N, d->K);
+  if (f.few) {
+    f.g = few_args(d, q8, x, w, w2);
+    f.g.gated = gated;
+    f.g.ldr = d->residual_ld;
+    return f;
+  }
   const Operand a = make_operand(x, d->M, d->K, d->x_ld, dt, d->unaligned, ar, &f.jobs[0]);
   const Operand b = make_operand(w, wr, wc, d->w_ld, dt, d->unaligned, ar, &f.jobs[1]);
   Operand b2{};
@@ -320,6 +346,7 @@ Forward make_forward(const ax_matmul_desc_t* d, bool q8, bool gated, const void*
 }
 
 int run_forward(Forward& f, hipStream_t s) {
+  if (f.few) return launch_few(f.g, f.dtype, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
   for (int i = 0; i < f.njobs; ++i)
     if (run_pack(f.jobs[i], s) != hipSuccess) return AX_ERR_HIP;
   return launch_gemm(f.g, f.plan, f.part, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
@@ -333,6 +360,7 @@ struct Backward {
   bool elementwise;  // act_grad_kernel runs for the products (it runs for gb alone too)
   int row_blocks;
   float* part;       // of gb
+  bool few;          // gx by launch_few
   GemmArgs gx, gw;
   GemmPlan px, pw;
   void *partx, *partw;
@@ -346,9 +374,12 @@ Backward make_backward(const ax_matmul_desc_t* d, bool gated, const void* gy, co
   const int dt = d->dtype;
   const long long wr = d->w_transposed ? d->N : d->K, wc = d->w_transposed ? d->K : d->N;
   const Operand ox = make_operand(x, d->M, d->K, d->x_ld, dt, d->unaligned, ar, &b.jobs[0]);
-  const Operand ow = make_operand(w, wr, wc, d->w_ld, dt, d->unaligned, ar, &b.jobs[1]);
-  Operand ow2{};
-  if (gated) ow2 = make_operand(w2, wr, wc, d->w_ld, dt, d->unaligned, ar, &b.jobs[2]);
+  b.few = dt == AX_BF16 && few_fits(dt, !d->w_transposed, false, d->M, d->K, d->N);
+  Operand ow{}, ow2{};
+  if (!b.few) {
+    ow = make_operand(w, wr, wc, d->w_ld, dt, d->unaligned, ar, &b.jobs[1]);
+    if (gated) ow2 = make_operand(w2, wr, wc, d->w_ld, dt, d->unaligned, ar, &b.jobs[2]);
+  }
   // gz as an operand: gy itself where nothing is multiplied to it and it can be read in place
   PackJob unused;
   Operand oz{}, ou{};
@@ -379,18 +410,23 @@ Backward make_backward(const ax_matmul_desc_t* d, bool gated, const void* gy, co
   if (!gated) b.part = (float*)ar.take((size_t)b.row_blocks * d->N * 4);
 
   GemmArgs& gx = b.gx;  // gx [M, K] = gz [M, N] w^T
-  add_segments(&gx, oz, ow, nullptr);
-  if (gated) add_segments(&gx, ou, ow2, nullptr);
+  if (b.few) {
+    gx.seg[gx.nseg++] = GemmSeg{oz.p[0], w, nullptr};
+    if (gated) gx.seg[gx.nseg++] = GemmSeg{ou.p[0], w2, nullptr};
+  } else {
+    add_segments(&gx, oz, ow, nullptr);
+    if (gated) add_segments(&gx, ou, ow2, nullptr);
+  }
   gx.la = 0;
   gx.lb = d->w_transposed ? 1 : 0;
   gx.M = (int)d->M;
   gx.N = (int)d->K;
-  gx.K = (int)(d->w_transposed ? d->N : pcols);
+  gx.K = (int)(d->w_transposed || b.few ? d->N : pcols);
   gx.lda = oz.ld;
-  gx.ldb = ow.ld;
+  gx.ldb = b.few ? d->w_ld * 2 : ow.ld;
   gx.odt = dt;
   gx.ldy = d->x_ld;
-  b.px = plan_gemm(gx);
+  if (!b.few) b.px = plan_gemm(gx);
 
   GemmArgs& gw = b.gw;  // gw [K, N] = x^T gz, or [N, K] = gz^T x
   if (d->w_transposed) add_segments(&gw, oz, ox, nullptr);
@@ -440,8 +476,8 @@ int backward_common(const ax_matmul_desc_t* d, bool gated, const void* gy, const
   if (!ws_ok(ws, ws_bytes, b.bytes)) return AX_ERR_WORKSPACE;
   const bool products = gx_out || gw_out;
   if (gw_out && run_pack(b.jobs[0], s) != hipSuccess) return AX_ERR_HIP;
-  if (gx_out && run_pack(b.jobs[1], s) != hipSuccess) return AX_ERR_HIP;
-  if (gx_out && gated && run_pack(b.jobs[2], s) != hipSuccess) return AX_ERR_HIP;
+  if (gx_out && !b.few && run_pack(b.jobs[1], s) != hipSuccess) return AX_ERR_HIP;
+  if (gx_out && !b.few && gated && run_pack(b.jobs[2], s) != hipSuccess) return AX_ERR_HIP;
   if (gated) {
     if (run_act_grad<true>(b.ga, b.row_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
   } else if ((b.elementwise && products) || gb_out) {
@@ -454,7 +490,7 @@ int backward_common(const ax_matmul_desc_t* d, bool gated, const void* gy, const
   }
   if (gx_out) {
     b.gx.y = gx_out;
-    if (launch_gemm(b.gx, b.px, b.partx, s) != hipSuccess) return AX_ERR_HIP;
+    if ((b.few ? launch_few(b.gx, AX_BF16, s) : launch_gemm(b.gx, b.px, b.partx, s)) != hipSuccess) return AX_ERR_HIP;
   }
   if (gw_out) {
     b.gw.y = gw_out;

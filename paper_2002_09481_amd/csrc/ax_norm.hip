@@ -316,8 +316,17 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(const float* __restric
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
   const int c = blockIdx.x * 16 + x;
   float s = 0.f;
-  if (c < cols)
-    for (int r = y; r < rows; r += 64) s += part[(long long)r * cols + c];
+  if (c < cols) {
+    int r = y;
+    for (; r + 64 * 7 < rows; r += 64 * 8) {  // eight loads at a time
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = part[(long long)(r + 64 * k) * cols + c];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += v[k];
+    }
+    for (; r < rows; r += 64) s += part[(long long)r * cols + c];
+  }
   red[y][x] = s;
   __syncthreads();
   for (int h = 32; h > 0; h >>= 1) {
