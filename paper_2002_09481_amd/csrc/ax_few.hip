@@ -34,18 +34,6 @@ struct Frag {
   u32x4 p[KD == kF32 ? 3 : 1];
 };
 
-// Eight float32 values in three pieces, smallest pieces last.
-__device__ __forceinline__ void pieces_of(const float (&v)[8], u32x4 (&p)[3]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    uint32_t a[3], b[3];
-    split3(v[2 * e], a[0], a[1], a[2]);
-    split3(v[2 * e + 1], b[0], b[1], b[2]);
-#pragma unroll
-    for (int k = 0; k < 3; ++k) p[k][e] = a[k] | (b[k] << 16);
-  }
-}
-
 template <Kind KD, typename Acc>
 __device__ __forceinline__ Acc mma(const Frag<KD>& a, const Frag<KD>& b, Acc c) {
   if constexpr (KD == kInt8) {

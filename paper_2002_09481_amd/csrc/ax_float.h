@@ -93,6 +93,18 @@ __device__ __forceinline__ void split3(float a, uint32_t& p0, uint32_t& p1, uint
   p2 = __float_as_uint(r2) >> 16;
 }
 
+// Eight float32 values in three pieces, smallest pieces last.
+__device__ __forceinline__ void pieces_of(const float (&v)[8], u32x4 (&p)[3]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    uint32_t a[3], b[3];
+    split3(v[2 * e], a[0], a[1], a[2]);
+    split3(v[2 * e + 1], b[0], b[1], b[2]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) p[k][e] = a[k] | (b[k] << 16);
+  }
+}
+
 // Activations in float32, with the fast exponential and reciprocal (a few units in the last place each), against results
 // that are rounded to bf16 or compared in the norm.  The normal distribution function of gelu is 7.1.26 of Abramowitz and
 // Stegun's Handbook of Mathematical Functions: erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2) with t = 1 / (1 + 0.3275911 x),

@@ -15,16 +15,18 @@ struct GemmSeg {
   const void* b2;
 };
 
-constexpr int kMaxSegs = 12;  // float32: six pairs of pieces, and two factor pairs in the gated block's input gradient
+constexpr int kMaxSegs = 2;  // two in the gated block's input gradient
 
 // y[M,N] = epilogue(sum over the segments of a[M,K] b[K,N]).
 struct GemmArgs {
   GemmSeg seg[kMaxSegs];
   int nseg;
   int i8;         // 1: operands are int8 codes, sums int32; 0: bf16, sums float32
+  int pieces;     // 3: float32 operands as three bf16 matrices each, a_plane and b_plane bytes apart; else 1
   int la, lb;     // operand layouts: 0 = the contraction is contiguous (a [M,K], b [N,K]), 1 = it is the row index (a [K,M], b [K,N])
   int M, N, K;
   long long lda, ldb;  // row pitches in bytes, multiples of 16
+  long long a_plane, b_plane;
   int gated;      // h = act(a b) * (a b2)
   int dual;       // y = a b, y2 = a b2
   // epilogue

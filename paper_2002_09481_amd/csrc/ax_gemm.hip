@@ -200,17 +200,22 @@ struct Acc<true> {
 // The wave holds the fragments of 64 bytes of the contraction in registers and reads the next ones while the matrix
 // instructions of these run.  Where the next ones are another stage's, a barrier in front of that says that they have arrived
 // and that this stage's place is free, and the copies of stage + STAGES are asked for.
-template <bool I8, int LA, int LB, int NB, int BM, int BN, int WM, int WN, int KB, int STAGES, int OCC>
+//
+// P = 3: float32 operands as three bf16 pieces, a = a1 + a2 + a3 and b alike.  A stage holds all pieces of its part of both,
+// and each fragment is used in several of the six products of pieces that can reach 2^-24 of a b, the smallest added first:
+// half the copies and a third of the LDS reads that six passes over pairs of pieces would take.
+template <bool I8, int P, int LA, int LB, int NB, int BM, int BN, int WM, int WN, int KB, int STAGES, int OCC>
 __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   constexpr int THREADS = 64 * WM * WN;
   constexpr int BNS = BN / NB;                // columns of one right operand
   constexpr int MF = BM / WM / 16, NF = BN / WN / 16;
   constexpr int KK = KB / 64;                 // matrix instructions' contraction steps per stage
   constexpr int kABytes = BM * KB, kBBytes = BNS * KB;
-  constexpr int kStage = kABytes + NB * kBBytes;
+  constexpr int kBAt = P * kABytes;           // right operands: [weight][piece]
+  constexpr int kStage = P * (kABytes + NB * kBBytes);
   typedef Stager<LA, BM, KB, THREADS> SA;
   typedef Stager<LB, BNS, KB, THREADS> SB;
-  constexpr int kLoads = SA::kLoads + NB * SB::kLoads;
+  constexpr int kLoads = P * (SA::kLoads + NB * SB::kLoads);
   __shared__ __align__(1024) unsigned char smem[STAGES * kStage];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(AX_LDS(unsigned char)*)smem;
 
@@ -278,23 +283,30 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   };
   at_segment();
   struct Copies {
-    typename SA::Copy a;
-    typename SB::Copy b, b2;
+    typename SA::Copy a[P];
+    typename SB::Copy b[NB][P];
     uint32_t lds;
   };
   auto copies_begin = [&](int buf) AX_INLINE {
     const int kleft = (g.K - ks * kStepK) * kElem;
     Copies c;
-    c.a = sa.begin(pa, ra, kleft);
-    c.b = sb.begin(pb, rb, kleft);
-    if (NB == 2) c.b2 = sb.begin(pb2, rb, kleft);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      c.a[p] = sa.begin(pa + p * g.a_plane, ra, kleft);
+      c.b[0][p] = sb.begin(pb + p * g.b_plane, rb, kleft);
+      if (NB == 2) c.b[NB - 1][p] = sb.begin(pb2 + p * g.b_plane, rb, kleft);
+    }
     c.lds = uniform(lds0 + (uint32_t)(buf * kStage + wave * 1024));
     return c;
   };
   auto copies_piece = [&](Copies& c, int i) AX_INLINE {
-    if (i < SA::kLoads) sa.piece(c.a, c.lds, i);
-    else if (i < SA::kLoads + SB::kLoads) sb.piece(c.b, c.lds + kABytes, i - SA::kLoads);
-    else sb.piece(c.b2, c.lds + kABytes + kBBytes, i - SA::kLoads - SB::kLoads);
+    if (i < P * SA::kLoads) {
+      const int p = i / SA::kLoads;
+      sa.piece(c.a[p], c.lds + p * kABytes, i % SA::kLoads);
+    } else {
+      const int k = (i - P * SA::kLoads) / SB::kLoads;
+      sb.piece(c.b[k / P][k % P], c.lds + kBAt + k * kBBytes, (i - P * SA::kLoads) % SB::kLoads);
+    }
   };
   auto copies_end = [&]() AX_INLINE {  // the next stage
     if (++ks == a.ksteps) {
@@ -317,15 +329,27 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
 
   const int wrow = wm * (BM / WM), wcol = wn * (BNS / WN);
   struct Fragments {
-    u32x4 a[MF], b[NF];
+    u32x4 a[P][MF], b[P][NF];
   };
-  auto read = [&](Fragments& f, int buf, int kk, int i) AX_INLINE {  // fragment i of MF + NF
-    const uint32_t la = lds0 + (uint32_t)(buf * kStage), lb = la + kABytes;
-    if (i < NF)
-      f.b[i] = NB == 2 ? fragment<LB, BNS, KB>(lb + (i & 1) * kBBytes, wcol + 16 * (i >> 1), kk, lane)
-                       : fragment<LB, BNS, KB>(lb, wcol + 16 * i, kk, lane);
-    else
-      f.a[i - NF] = fragment<LA, BM, KB>(la, wrow + 16 * (i - NF), kk, lane);
+  constexpr int kFrags = P * (MF + NF);
+  auto read = [&](Fragments& f, int buf, int kk, int i) AX_INLINE {  // fragment i of kFrags
+    const uint32_t la = lds0 + (uint32_t)(buf * kStage), lb = la + kBAt;
+    if (i < P * NF) {
+      const int p = i / NF, j = i % NF;
+      f.b[p][j] = NB == 2 ? fragment<LB, BNS, KB>(lb + ((j & 1) * P + p) * kBBytes, wcol + 16 * (j >> 1), kk, lane)
+                          : fragment<LB, BNS, KB>(lb + p * kBBytes, wcol + 16 * j, kk, lane);
+    } else {  // (row by row: the first rows' products can start before the last rows' pieces are there)
+      const int k = i - P * NF;
+      f.a[k % P][k / P] = fragment<LA, BM, KB>(la + (k % P) * kABytes, wrow + 16 * (k / P), kk, lane);
+    }
+  };
+  auto multiply = [&](const Fragments& f, int i) AX_INLINE {  // row i of blocks
+    constexpr int kPairs = P == 1 ? 1 : 6;
+    constexpr int qa[6] = {P - 1, 0, P / 2, P / 2, 0, 0}, qb[6] = {0, P - 1, P / 2, 0, P / 2, 0};
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q)
+#pragma unroll
+      for (int j = 0; j < NF; ++j) acc[i][j] = Acc<I8>::mma(f.b[qb[q]][j], f.a[qa[q]][i], acc[i][j]);
   };
 
   // Stages asked for: it + STAGES when stage it is multiplied.
@@ -343,7 +367,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   else wait_copies<0>();
   wg_barrier();
 #pragma unroll
-  for (int i = 0; i < MF + NF; ++i) read(f0, 0, 0, i);
+  for (int i = 0; i < kFrags; ++i) read(f0, 0, 0, i);
   // Part kk of stage `it`, whose fragments `now` holds; `next` gets those of the part behind it.  steady: there is a stage
   // it + STAGES to ask for.  Copies and LDS reads are spread evenly among the matrix instructions, row by row.
   auto turn = [&](auto steady, int it, int kk, const Fragments& now, Fragments& next) AX_INLINE {
@@ -365,9 +389,8 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
         for (int k = i * kLoads / MF; k < (i + 1) * kLoads / MF; ++k)
           if (last) copies_piece(c, k);
 #pragma unroll
-        for (int k = i * (MF + NF) / MF; k < (i + 1) * (MF + NF) / MF; ++k) read(next, nbuf, last ? 0 : kk + 1, k);
-#pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = Acc<I8>::mma(now.b[j], now.a[i], acc[i][j]);
+        for (int k = i * kFrags / MF; k < (i + 1) * kFrags / MF; ++k) read(next, nbuf, last ? 0 : kk + 1, k);
+        multiply(now, i);
         __builtin_amdgcn_sched_barrier(0);
       }
       if (last) copies_end();
@@ -380,12 +403,10 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
       }
       if (more) {
 #pragma unroll
-        for (int k = 0; k < MF + NF; ++k) read(next, nbuf, last ? 0 : kk + 1, k);
+        for (int k = 0; k < kFrags; ++k) read(next, nbuf, last ? 0 : kk + 1, k);
       }
 #pragma unroll
-      for (int i = 0; i < MF; ++i)
-#pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = Acc<I8>::mma(now.b[j], now.a[i], acc[i][j]);
+      for (int i = 0; i < MF; ++i) multiply(now, i);
     }
     buf = nbuf;
   };
@@ -502,28 +523,37 @@ __global__ __launch_bounds__(256) void gemm_join_kernel(const Args a) {
   }
 }
 
-// Tile configurations.  per_cu: workgroups that fit a compute unit (LDS).  Times in us, measured on products that fill
-// the card with one kind of tile: of a workgroup (prologue, epilogue), and of 128 contraction bytes with one workgroup per
-// compute unit and with per_cu of them.
+// Tile configurations.  kb: contraction bytes (of a bf16 or int8 operand) per stage, per_cu: workgroups that fit a compute
+// unit (LDS).  Times in us, measured on products that fill the card with one kind of tile: of a workgroup (prologue,
+// epilogue), and of 128 contraction bytes with one workgroup per compute unit and with per_cu of them.
 struct TileShape {
-  int bm, bn, per_cu;
+  int bm, bn, kb, per_cu;
   double fixed, step1, step;
 };
-constexpr int kStageBytes = 128;
 constexpr int kNumTiles = 4;
-constexpr TileShape kTiles[kNumTiles] = {
-    {256, 256, 1, 6.0, 1.50, 1.50}, {128, 128, 2, 3.0, 0.70, 0.95}, {64, 128, 2, 2.5, 0.39, 0.65}, {32, 128, 2, 2.0, 0.26, 0.45}};
+constexpr TileShape kTiles[kNumTiles] = {{256, 256, 128, 1, 6.0, 1.50, 1.50},
+                                         {128, 128, 128, 2, 3.0, 0.70, 0.95},
+                                         {64, 128, 128, 2, 2.5, 0.39, 0.65},
+                                         {32, 128, 128, 2, 2.0, 0.26, 0.45}};
+// float32 operands (three pieces; six products in the time)
+constexpr int kNumTiles3 = 2;
+constexpr TileShape kTiles3[kNumTiles3] = {{128, 128, 64, 1, 5.0, 2.1, 2.1}, {64, 128, 64, 2, 4.0, 1.25, 2.1}};
 
 template <bool I8, int LA, int LB, int NB>
 void launch_tile(const Args& a, int tile, int grid, hipStream_t s) {
   switch (tile) {
-    case 0: gemm_kernel<I8, LA, LB, NB, 256, 256, 2, 4, kStageBytes, 2, 2><<<grid, 512, 0, s>>>(a); break;
-    case 1: gemm_kernel<I8, LA, LB, NB, 128, 128, 2, 2, kStageBytes, 2, 2><<<grid, 256, 0, s>>>(a); break;
-    case 2: gemm_kernel<I8, LA, LB, NB, 64, 128, 1, 4, kStageBytes, 3, 2><<<grid, 256, 0, s>>>(a); break;
+    case 0: gemm_kernel<I8, 1, LA, LB, NB, 256, 256, 2, 4, 128, 2, 2><<<grid, 512, 0, s>>>(a); break;
+    case 1: gemm_kernel<I8, 1, LA, LB, NB, 128, 128, 2, 2, 128, 2, 2><<<grid, 256, 0, s>>>(a); break;
+    case 2: gemm_kernel<I8, 1, LA, LB, NB, 64, 128, 1, 4, 128, 3, 2><<<grid, 256, 0, s>>>(a); break;
     default:  // (copies of 32 columns whose rows are the contraction would not fill the threads)
-      if constexpr (LA == 0) gemm_kernel<I8, LA, LB, NB, 32, 128, 1, 4, kStageBytes, 3, 2><<<grid, 256, 0, s>>>(a);
+      if constexpr (LA == 0) gemm_kernel<I8, 1, LA, LB, NB, 32, 128, 1, 4, 128, 3, 2><<<grid, 256, 0, s>>>(a);
       break;
   }
+}
+template <int LA, int LB, int NB>
+void launch_tile3(const Args& a, int tile, int grid, hipStream_t s) {
+  if (tile == 0) gemm_kernel<false, 3, LA, LB, NB, 128, 128, 2, 2, 64, 3, 1><<<grid, 256, 0, s>>>(a);
+  else gemm_kernel<false, 3, LA, LB, NB, 64, 128, 2, 2, 64, 2, 2><<<grid, 256, 0, s>>>(a);
 }
 
 constexpr int kCus = 256;
@@ -533,6 +563,7 @@ long long tiles_of(const GemmArgs& g, const TileShape& t) {
   const int bns = t.bn / (g.gated ? 2 : 1);
   return (long long)((g.M + t.bm - 1) / t.bm) * ((g.N + bns - 1) / bns) * (g.dual ? 2 : 1);
 }
+const TileShape& shape_of(const GemmArgs& g, int tile) { return g.pieces == 3 ? kTiles3[tile] : kTiles[tile]; }
 long long part_pitch(const GemmArgs& g) { return ((long long)g.N + 7) / 8 * 8; }
 
 }  // namespace
@@ -542,18 +573,19 @@ long long part_pitch(const GemmArgs& g) { return ((long long)g.N + 7) / 8 * 8; }
 // launch that adds them.  Large products get the large tiles, few tiles are cut along the contraction.
 GemmPlan plan_gemm(const GemmArgs& g) {
   const long long kbytes = (long long)g.K * (g.i8 ? 1 : 2);
-  const long long steps = (kbytes + kStageBytes - 1) / kStageBytes * g.nseg;
+  const bool three = g.pieces == 3;
   const double outs = g.gated || g.dual ? 2 : 1;
   GemmPlan best{};
   double least = 1e300;
-  for (int t = 0; t < kNumTiles; ++t) {
-    if (t == 3 && g.la != 0) continue;
-    const TileShape& T = kTiles[t];
+  for (int t = 0; t < (three ? kNumTiles3 : kNumTiles); ++t) {
+    const TileShape& T = shape_of(g, t);
+    if (T.bm == 32 && g.la != 0) continue;
+    const long long steps = (kbytes + T.kb - 1) / T.kb * g.nseg;
     const long long tiles = tiles_of(g, T);
     for (int sp = 1; sp <= kMaxSplits && (sp == 1 || sp * 2 <= steps); ++sp) {
       const long long n = tiles * sp, slots = (long long)kCus * T.per_cu;
       const long long full = n / slots, rest = n - full * slots;
-      const double stages = (double)((steps + sp - 1) / sp);
+      const double stages = (double)((steps + sp - 1) / sp) * T.kb / 128;
       double cost = full * (T.fixed + stages * T.step);
       if (rest) cost += T.fixed + stages * (rest <= kCus ? T.step1 : T.step);
       if (sp > 1) cost += 3.0 + sp * outs * g.M * (double)g.N * 8.0 / 6.5e6;
@@ -574,8 +606,8 @@ GemmPlan plan_gemm(const GemmArgs& g) {
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStream_t s) {
   Args a;
   a.g = g;
-  const TileShape& T = kTiles[p.tile];
-  const int kstep = kStageBytes / (g.i8 ? 1 : 2);
+  const TileShape& T = shape_of(g, p.tile);
+  const int kstep = T.kb / (g.i8 ? 1 : 2);
   a.tiles_m = (g.M + T.bm - 1) / T.bm;
   a.tiles_n = (int)(tiles_of(g, T) / a.tiles_m);
   a.ksteps = (g.K + kstep - 1) / kstep;
@@ -585,7 +617,12 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStre
   const long long grid = (long long)a.tiles_m * a.tiles_n * p.splits;
   if (grid <= 0 || grid > 0x7fffffffll) return hipErrorInvalidValue;
   const int n = (int)grid;
-  if (g.gated) {
+  if (g.pieces == 3) {
+    if (g.gated) launch_tile3<0, 1, 2>(a, p.tile, n, s);
+    else if (g.la == 0 && g.lb == 0) launch_tile3<0, 0, 1>(a, p.tile, n, s);
+    else if (g.la == 0) launch_tile3<0, 1, 1>(a, p.tile, n, s);
+    else launch_tile3<1, 1, 1>(a, p.tile, n, s);
+  } else if (g.gated) {
     if (g.i8) launch_tile<true, 0, 0, 2>(a, p.tile, n, s);
     else launch_tile<false, 0, 1, 2>(a, p.tile, n, s);
   } else if (g.i8) {

@@ -5,9 +5,8 @@
 //   g = x wg,  u = x wu,  h = act(g) u             gg = gh u act'(g),  gu = gh act(g),  gx = gg wg^T + gu wu^T, ...
 //
 // The matrix instructions take bf16 (or int8) operands.  float32 operands are cut into three bf16 pieces,
-// a = a1 + a2 + a3 exactly (eight significant bits each), and the product runs over the six pairs of pieces whose
-// product can reach 2^-24 of a b, smallest first, as six segments of one contraction: 6 / 16 of the cost of the float32
-// matrix instruction, at its precision.
+// a = a1 + a2 + a3 exactly (eight significant bits each), and six of the nine products of pieces are added: what is left out
+// is below 2^-24 of a b.  That is 6 / 16 of the cost of the float32 matrix instruction, at its precision.
 #include <algorithm>
 
 #include "ax_float.h"
@@ -35,9 +34,10 @@ inline int elem_bytes(int dtype) { return dtype == AX_F32 ? 4 : 2; }
 
 // A matrix as the products read it: planes of bf16 (or int8) rows whose length is a multiple of 16 bytes.
 struct Operand {
-  const void* p[3];
-  int planes;      // 3 for float32
-  long long ld;    // bytes
+  const void* p;
+  int planes;       // 3 for float32
+  long long plane;  // bytes from one to the next
+  long long ld;     // bytes
   long long cols;  // row length, rounded up to whole 16-byte chunks (zeros behind the given columns)
 };
 
@@ -45,62 +45,83 @@ struct PackJob {
   const void* src;
   void* dst;  // planes back to back; null: read in place
   long long rows, cols, ld;  // of the source, elements
-  long long pcols;
+  long long pcols;  // cols in whole chunks, zeros behind cols
+  long long pitch;  // of the copy, elements
   int dtype;  // AX_F32, AX_BF16, or kI8
 };
 constexpr int kI8 = 2;
 
-// Rows copied into the form the products read: eight elements (16 bytes of output; int8: 16) a thread.  Bound by
-// memory: 4 bytes read and 6 written per float32 element.
+// Rows copied into the form the products read: eight elements (16 bytes of output; int8: 16) a thread, all the operands of a
+// product in one launch.  Bound by memory: 4 bytes read and 6 written per float32 element.
+struct PackBatch {
+  PackJob job[3];
+  int first[3];  // workgroup that each job starts at
+  int blocks[3];
+};
 template <int DT>
-__global__ __launch_bounds__(256) void pack_kernel(const void* __restrict__ src, void* __restrict__ dst, long long rows,
-                                                    long long cols, long long ld, long long pcols) {
+__global__ __launch_bounds__(256) void pack_kernel(const PackBatch b) {
   constexpr int E = DT == kI8 ? 16 : 8;
-  const long long groups = pcols / E, total = rows * groups;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+  const int k = (int)blockIdx.x >= b.first[2] ? 2 : (int)blockIdx.x >= b.first[1] ? 1 : 0;
+  const PackJob& j = b.job[k];
+  const long long groups = j.pcols / E, total = j.rows * groups;
+  for (long long i = (long long)(blockIdx.x - b.first[k]) * 256 + threadIdx.x; i < total; i += (long long)b.blocks[k] * 256) {
     const long long r = i / groups, c = (i - r * groups) * E;
-    const long long left = cols - c;
+    const long long left = j.cols - c;
     if (DT == AX_F32) {
       float v[8];
-      load_elems<true, 8>(src, r * ld + c, (int)min(left, 8ll), v);
-      uint32_t q[3][4];
-      for (int e = 0; e < 4; ++e) {
-        uint32_t a[3], b[3];
-        split3(v[2 * e], a[0], a[1], a[2]);
-        split3(v[2 * e + 1], b[0], b[1], b[2]);
-        for (int k = 0; k < 3; ++k) q[k][e] = a[k] | (b[k] << 16);
-      }
-      for (int k = 0; k < 3; ++k)
-        *(uint4*)((uint16_t*)dst + (k * rows + r) * pcols + c) = make_uint4(q[k][0], q[k][1], q[k][2], q[k][3]);
+      load_elems<true, 8>(j.src, r * j.ld + c, (int)min(left, 8ll), v);
+      u32x4 q[3];
+      pieces_of(v, q);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) *(u32x4*)((uint16_t*)j.dst + (p * j.rows + r) * j.pitch + c) = q[p];
     } else if (DT == AX_BF16) {
-      const uint16_t* s = (const uint16_t*)src + r * ld + c;
+      const uint16_t* s = (const uint16_t*)j.src + r * j.ld + c;
       u32x4 q;
       if (left >= 8) q = load_any<u32x4>(s);
       else for (int e = 0; e < 4; ++e)
         q[e] = (2 * e < left ? (uint32_t)s[2 * e] : 0u) | ((2 * e + 1 < left ? (uint32_t)s[2 * e + 1] : 0u) << 16);
-      *(u32x4*)((uint16_t*)dst + r * pcols + c) = q;
+      *(u32x4*)((uint16_t*)j.dst + r * j.pitch + c) = q;
     } else {
-      const uint8_t* s = (const uint8_t*)src + r * ld + c;
+      const uint8_t* s = (const uint8_t*)j.src + r * j.ld + c;
       u32x4 q;
       if (left >= 16) q = load_any<u32x4>(s);
       else for (int e = 0; e < 4; ++e) {
         q[e] = 0;
-        for (int b = 0; b < 4; ++b) q[e] |= (4 * e + b < left ? (uint32_t)s[4 * e + b] : 0u) << (8 * b);
+        for (int x = 0; x < 4; ++x) q[e] |= (4 * e + x < left ? (uint32_t)s[4 * e + x] : 0u) << (8 * x);
       }
-      *(u32x4*)((uint8_t*)dst + r * pcols + c) = q;
+      *(u32x4*)((uint8_t*)j.dst + r * j.pitch + c) = q;
     }
   }
 }
 
 int grid_for(long long items) { return (int)std::max<long long>(1, std::min<long long>((items + 255) / 256, 8192)); }
 
-hipError_t run_pack(const PackJob& j, hipStream_t s) {
-  if (!j.dst || j.rows == 0) return hipSuccess;
-  const int grid = grid_for(j.rows * (j.pcols / (j.dtype == kI8 ? 16 : 8)));
-  if (j.dtype == AX_F32) pack_kernel<AX_F32><<<grid, 256, 0, s>>>(j.src, j.dst, j.rows, j.cols, j.ld, j.pcols);
-  else if (j.dtype == AX_BF16) pack_kernel<AX_BF16><<<grid, 256, 0, s>>>(j.src, j.dst, j.rows, j.cols, j.ld, j.pcols);
-  else pack_kernel<kI8><<<grid, 256, 0, s>>>(j.src, j.dst, j.rows, j.cols, j.ld, j.pcols);
+// The jobs of an operation that have something to copy (wanted[i]: whether job i is needed by this call).
+hipError_t run_pack(const PackJob* jobs, const bool* wanted, int n, hipStream_t s) {
+  PackBatch b{};
+  int k = 0, grid = 0;
+  for (int i = 0; i < 3; ++i) b.first[i] = 0x7fffffff;
+  for (int i = 0; i < n; ++i) {
+    const PackJob& j = jobs[i];
+    if (!wanted[i] || !j.dst || j.rows == 0) continue;
+    b.job[k] = j;
+    b.first[k] = grid;
+    b.blocks[k] = grid_for(j.rows * (j.pcols / (j.dtype == kI8 ? 16 : 8)));
+    grid += b.blocks[k++];
+  }
+  if (k == 0) return hipSuccess;
+  const int dtype = b.job[0].dtype;  // the same for all operands of an operation
+  if (dtype == AX_F32) pack_kernel<AX_F32><<<grid, 256, 0, s>>>(b);
+  else if (dtype == AX_BF16) pack_kernel<AX_BF16><<<grid, 256, 0, s>>>(b);
+  else pack_kernel<kI8><<<grid, 256, 0, s>>>(b);
   return hipGetLastError();
+}
+
+// Row pitch of a copy: whole lines of 128 bytes, and not a multiple of 2 KB, at which the pieces of one stage of a tile
+// fall on few channels (bf16 8192^3, both operands contiguous along the sum: 956 us at 16 KB, 863 us at 16 KB + 128).
+long long copy_pitch(long long cols, int esz) {
+  const long long line = 128 / esz, pitch = (cols + line - 1) / line * line;
+  return pitch * esz % 2048 ? pitch : pitch + line;
 }
 
 // Whether the matrix is read in place or copied is decided by its description alone, so that the workspace query knows.
@@ -108,30 +129,32 @@ Operand make_operand(const void* p, long long rows, long long cols, long long ld
   Operand o{};
   const int chunk = dtype == kI8 ? 16 : 8, esz = dtype == kI8 ? 1 : 2;
   const long long pcols = (cols + chunk - 1) / chunk * chunk;
-  *job = PackJob{p, nullptr, rows, cols, ld, pcols, dtype};
+  const long long pitch = copy_pitch(cols, esz);
+  *job = PackJob{p, nullptr, rows, cols, ld, pcols, pitch, dtype};
   o.cols = pcols;
   if (dtype != AX_F32 && !unaligned && pcols == cols && ld % chunk == 0) {
     o.planes = 1;
-    o.p[0] = p;
+    o.p = p;
     o.ld = ld * esz;
     return o;
   }
   o.planes = dtype == AX_F32 ? 3 : 1;
-  o.ld = pcols * esz;
-  const size_t plane = (size_t)rows * pcols * esz;
+  o.ld = pitch * esz;
+  const size_t plane = (size_t)rows * pitch * esz;
   job->dst = ar.take(plane * o.planes);
-  for (int k = 0; k < o.planes; ++k) o.p[k] = (const char*)job->dst + k * plane;
+  o.p = job->dst;
+  o.plane = (long long)plane;
   return o;
 }
 
-// Factor pairs of a product of two operands: one, or six pairs of pieces, smallest products first.
-void add_segments(GemmArgs* g, const Operand& a, const Operand& b, const Operand* b2) {
-  if (a.planes == 1) {
-    g->seg[g->nseg++] = GemmSeg{a.p[0], b.p[0], b2 ? b2->p[0] : nullptr};
-    return;
-  }
-  static const int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
-  for (int i = 0; i < 6; ++i) g->seg[g->nseg++] = GemmSeg{a.p[pa[i]], b.p[pb[i]], b2 ? b2->p[pb[i]] : nullptr};
+// A factor pair of a product (all pairs of a product have the same pitches).
+void add_segment(GemmArgs* g, const Operand& a, const Operand& b, const Operand* b2) {
+  g->seg[g->nseg++] = GemmSeg{a.p, b.p, b2 ? b2->p : nullptr};
+  g->pieces = a.planes;
+  g->lda = a.ld;
+  g->ldb = b.ld;
+  g->a_plane = a.plane;
+  g->b_plane = b.plane;
 }
 
 // ---- elementwise part of the gradients ---------------------------------------------------------------------------
@@ -145,24 +168,19 @@ struct GradArgs {
   void* gz;        // planes [M, pcols] (may be NULL: gy itself is read by the products)
   void* gu;        // GATED
   float* part;     // [row blocks][N] (may be NULL)
-  long long ldy, pcols;
+  long long ldy, pcols, pitch;  // pcols, pitch: of gz and gu
   int M, N, act, rows_per;
 };
 
 template <int DT>
-__device__ __forceinline__ void write_planes(void* dst, long long rows, long long pcols, long long r, long long c, const float (&v)[8]) {
+__device__ __forceinline__ void write_planes(void* dst, long long rows, long long pitch, long long r, long long c, const float (&v)[8]) {
   if (DT == AX_F32) {
-    uint32_t q[3][4];
-    for (int e = 0; e < 4; ++e) {
-      uint32_t a[3], b[3];
-      split3(v[2 * e], a[0], a[1], a[2]);
-      split3(v[2 * e + 1], b[0], b[1], b[2]);
-      for (int k = 0; k < 3; ++k) q[k][e] = a[k] | (b[k] << 16);
-    }
-    for (int k = 0; k < 3; ++k)
-      *(uint4*)((uint16_t*)dst + (k * rows + r) * pcols + c) = make_uint4(q[k][0], q[k][1], q[k][2], q[k][3]);
+    u32x4 q[3];
+    pieces_of(v, q);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *(u32x4*)((uint16_t*)dst + (k * rows + r) * pitch + c) = q[k];
   } else {
-    *(uint4*)((uint16_t*)dst + r * pcols + c) =
+    *(uint4*)((uint16_t*)dst + r * pitch + c) =
         make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
   }
 }
@@ -188,12 +206,12 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const GradArgs a) {
             v[e] *= gy[e];
             gy[e] = gy[e] * u[e] * sl[e];
           }
-          write_planes<DT>(a.gu, a.M, a.pcols, r, c, v);
+          write_planes<DT>(a.gu, a.M, a.pitch, r, c, v);
         } else {
           for (int e = 0; e < 8; ++e) gy[e] *= sl[e];
         }
       }
-      if (a.gz) write_planes<DT>(a.gz, a.M, a.pcols, r, c, gy);
+      if (a.gz) write_planes<DT>(a.gz, a.M, a.pitch, r, c, gy);
       if (!GATED)
         for (int e = 0; e < 8; ++e) sum[e] += gy[e];
     }
@@ -324,7 +342,7 @@ Forward make_forward(const ax_matmul_desc_t* d, bool q8, bool gated, const void*
   f.njobs = 2;
   if (gated) b2 = make_operand(w2, wr, wc, d->w_ld, dt, d->unaligned, ar, &f.jobs[f.njobs++]);
   GemmArgs& g = f.g;
-  add_segments(&g, a, b, gated ? &b2 : nullptr);
+  add_segment(&g, a, b, gated ? &b2 : nullptr);
   g.i8 = q8;
   g.la = 0;
   g.lb = d->w_transposed ? 0 : 1;
@@ -332,8 +350,6 @@ Forward make_forward(const ax_matmul_desc_t* d, bool q8, bool gated, const void*
   g.N = (int)d->N;
   // contraction: whole chunks where both operands have them contiguous (zeros behind the end), rows of w otherwise
   g.K = (int)(d->w_transposed ? a.cols : d->K);
-  g.lda = a.ld;
-  g.ldb = b.ld;
   g.gated = gated;
   g.odt = d->out_dtype;
   g.act = d->act;
@@ -347,8 +363,8 @@ Forward make_forward(const ax_matmul_desc_t* d, bool q8, bool gated, const void*
 
 int run_forward(Forward& f, hipStream_t s) {
   if (f.few) return launch_few(f.g, f.dtype, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
-  for (int i = 0; i < f.njobs; ++i)
-    if (run_pack(f.jobs[i], s) != hipSuccess) return AX_ERR_HIP;
+  const bool all[3] = {true, true, true};
+  if (run_pack(f.jobs, all, f.njobs, s) != hipSuccess) return AX_ERR_HIP;
   return launch_gemm(f.g, f.plan, f.part, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
 }
 
@@ -402,6 +418,7 @@ Backward make_backward(const ax_matmul_desc_t* d, bool gated, const void* gy, co
   b.ga.u = u;
   b.ga.ldy = d->y_ld;
   b.ga.pcols = pcols;
+  b.ga.pitch = oz.ld / 2;
   b.ga.M = (int)d->M;
   b.ga.N = (int)d->N;
   b.ga.act = d->act;
@@ -411,32 +428,32 @@ Backward make_backward(const ax_matmul_desc_t* d, bool gated, const void* gy, co
 
   GemmArgs& gx = b.gx;  // gx [M, K] = gz [M, N] w^T
   if (b.few) {
-    gx.seg[gx.nseg++] = GemmSeg{oz.p[0], w, nullptr};
-    if (gated) gx.seg[gx.nseg++] = GemmSeg{ou.p[0], w2, nullptr};
+    gx.seg[gx.nseg++] = GemmSeg{oz.p, w, nullptr};
+    if (gated) gx.seg[gx.nseg++] = GemmSeg{ou.p, w2, nullptr};
   } else {
-    add_segments(&gx, oz, ow, nullptr);
-    if (gated) add_segments(&gx, ou, ow2, nullptr);
+    add_segment(&gx, oz, ow, nullptr);
+    if (gated) add_segment(&gx, ou, ow2, nullptr);
   }
   gx.la = 0;
   gx.lb = d->w_transposed ? 1 : 0;
   gx.M = (int)d->M;
   gx.N = (int)d->K;
   gx.K = (int)(d->w_transposed || b.few ? d->N : pcols);
-  gx.lda = oz.ld;
-  gx.ldb = b.few ? d->w_ld * 2 : ow.ld;
+  if (b.few) {
+    gx.lda = oz.ld;
+    gx.ldb = d->w_ld * 2;
+  }
   gx.odt = dt;
   gx.ldy = d->x_ld;
   if (!b.few) b.px = plan_gemm(gx);
 
   GemmArgs& gw = b.gw;  // gw [K, N] = x^T gz, or [N, K] = gz^T x
-  if (d->w_transposed) add_segments(&gw, oz, ox, nullptr);
-  else add_segments(&gw, ox, oz, gated ? &ou : nullptr);
+  if (d->w_transposed) add_segment(&gw, oz, ox, nullptr);
+  else add_segment(&gw, ox, oz, gated ? &ou : nullptr);
   gw.la = gw.lb = 1;
   gw.M = (int)(d->w_transposed ? d->N : d->K);
   gw.N = (int)(d->w_transposed ? d->K : d->N);
   gw.K = (int)d->M;
-  gw.lda = d->w_transposed ? oz.ld : ox.ld;
-  gw.ldb = d->w_transposed ? ox.ld : oz.ld;
   gw.dual = gated;
   gw.odt = dt;
   gw.ldy = d->w_ld;
@@ -475,9 +492,9 @@ int backward_common(const ax_matmul_desc_t* d, bool gated, const void* gy, const
   Backward b = make_backward(d, gated, gy, x, w, w2, z, u, ws);
   if (!ws_ok(ws, ws_bytes, b.bytes)) return AX_ERR_WORKSPACE;
   const bool products = gx_out || gw_out;
-  if (gw_out && run_pack(b.jobs[0], s) != hipSuccess) return AX_ERR_HIP;
-  if (gx_out && !b.few && run_pack(b.jobs[1], s) != hipSuccess) return AX_ERR_HIP;
-  if (gx_out && !b.few && gated && run_pack(b.jobs[2], s) != hipSuccess) return AX_ERR_HIP;
+  const bool weights = gx_out && !b.few;
+  const bool wanted[3] = {gw_out != nullptr, weights, weights && gated};
+  if (run_pack(b.jobs, wanted, 3, s) != hipSuccess) return AX_ERR_HIP;
   if (gated) {
     if (run_act_grad<true>(b.ga, b.row_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
   } else if ((b.elementwise && products) || gb_out) {
