@@ -534,7 +534,7 @@ constexpr int kNumTiles = 4;
 constexpr TileShape kTiles[kNumTiles] = {{256, 256, 128, 1, 6.0, 1.50, 1.50},
                                          {128, 128, 128, 2, 3.0, 0.70, 0.95},
                                          {64, 128, 128, 2, 2.5, 0.39, 0.65},
-                                         {32, 128, 128, 2, 2.0, 0.26, 0.45}};
+                                         {32, 128, 128, 2, 2.0, 0.30, 0.45}};
 // float32 operands (three pieces; six products in the time)
 constexpr int kNumTiles3 = 2;
 constexpr TileShape kTiles3[kNumTiles3] = {{128, 128, 64, 1, 5.0, 2.1, 2.1}, {64, 128, 64, 2, 4.0, 1.25, 2.1}};
@@ -586,8 +586,9 @@ GemmPlan plan_gemm(const GemmArgs& g) {
       const long long n = tiles * sp, slots = (long long)kCus * T.per_cu;
       const long long full = n / slots, rest = n - full * slots;
       const double stages = (double)((steps + sp - 1) / sp) * T.kb / 128;
-      double cost = full * (T.fixed + stages * T.step);
-      if (rest) cost += T.fixed + stages * (rest <= kCus ? T.step1 : T.step);
+      const double fixed = T.fixed + (sp > 1 ? T.bm * T.bn * 4 / 20e3 : 0);  // (sums leave a compute unit at 20 KB a us)
+      double cost = full * (fixed + stages * T.step);
+      if (rest) cost += fixed + stages * (rest <= kCus ? T.step1 : T.step);
       if (sp > 1) cost += 3.0 + sp * outs * g.M * (double)g.N * 8.0 / 6.5e6;
       if (cost < least) {
         least = cost;
