@@ -402,7 +402,7 @@ size_t ax_conv2d_backward_workspace_bytes(const ax_conv_desc_t* desc);
  *   y = t * rstd * weight
  */
 typedef struct {
-  int64_t rows, cols; /* rows >= 0, 1 <= cols < 2^31                                            */
+  int64_t rows, cols; /* 0 <= rows < 2^31, 1 <= cols < 2^31 - 32768                             */
   int64_t x_ld, residual_ld, sum_ld, y_ld;
   int32_t dtype;      /* of x, residual, sum and y; in the backward pass of all the matrices    */
   int32_t w_dtype;    /* of weight                                                              */
@@ -447,16 +447,16 @@ size_t ax_rmsnorm_backward_workspace_bytes(const ax_norm_desc_t* desc);
  * Matrix product with its epilogue:  z = x w + bias,  y = act(z) + residual.
  *   x [M, K], w [K, N] (or [N, K] where w_transposed is 1), bias [N], residual and y [M, N],
  *   z_out (may be NULL) [M, N] with pitch N, kept for the backward pass
- * bias and residual may be NULL.  dtype is the type of x and w, out_dtype that of bias, residual, z
+ * bias and residual may be NULL; y_out may be residual itself, with its pitch.  dtype is the type of x and w, out_dtype that of bias, residual, z
  * and y.  AX_BF16 products are exact in float32 and summed there.  AX_F32 operands are taken as three
  * bf16 pieces each (exact together) and six of their nine products; what is dropped is below 2^-24
- * of a product, so results are those of a float32 product.
+ * of a product, so results are those of a float32 product (but an infinity in an operand may give NaN).
  * Operands that the kernels cannot read in place (AX_F32; rows that are not 16-byte aligned or whose
  * length is no multiple of 16 bytes) are copied into the workspace first.
  * workspace: ax_matmul_workspace_bytes(desc) bytes, 256-byte aligned.
  */
 typedef struct {
-  int64_t M, N, K;    /* M >= 0; N, K >= 1; each below 2^31, row pitches below 2^22 bytes        */
+  int64_t M, N, K;    /* M >= 0; N, K >= 1; each at most 2^30, row pitches below 2^22 bytes      */
   int64_t x_ld, w_ld, residual_ld, y_ld;
   int32_t dtype, out_dtype;
   int32_t act;
@@ -547,7 +547,7 @@ typedef struct {
   float* m_scale; /* 8 bits: one a block                                                       */
   float* v_scale;
   void* copy;     /* may be NULL: the updated parameters once more, rounded to bf16            */
-  int64_t n;      /* elements, >= 0                                                            */
+  int64_t n;      /* elements, >= 0, below 2^36                                                */
 } ax_adamw_tensor_t;
 
 typedef struct {

@@ -888,6 +888,15 @@ def _sig(t):
     return t.dtype, t.shape, t.stride(), t.device
 
 
+def _lend(stream, *tensors):
+    """Tensors allocated here belong to the current stream's pool: those a call on another stream uses are tied to that one
+    too, so that their memory is not handed out again while its kernels run."""
+    if stream is not None:
+        for t in tensors:
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
+
+
 def _mat(t, dtype, name: str) -> Tuple[int, int, int]:
     """(rows, columns, row pitch) of a matrix."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -968,6 +977,7 @@ def ax_rmsnorm(x, weight, residual=None, eps=1e-5, sum_out=None, y_out=None, rst
             _vec_of(rstd_out, torch.float32, d.rows, "rstd_out")
         _remember(key, d)
     sum_out, rstd_out = (None if o is False else o for o in (sum_out, rstd_out))
+    _lend(stream, y_out, sum_out, rstd_out)
     _check(lib().ax_rmsnorm(d, _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_out), _ptr(y_out), _ptr(rstd_out),
                             _stream_ptr(stream)))
     return y_out, sum_out, rstd_out
@@ -997,6 +1007,7 @@ def ax_rmsnorm_q8(x, weight=None, residual=None, eps=1e-5, normalize=True, sum_o
             _vec_of(values_out, torch.float32, d.rows * d.cols, "values_out")
         _remember(key, d)
     sum_out = None if sum_out is False else sum_out
+    _lend(stream, codes_out, scales_out, sum_out, values_out)
     _check(lib().ax_rmsnorm_q8(d, _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_out), _ptr(codes_out), _ptr(scales_out),
                                _ptr(values_out), _stream_ptr(stream)))
     return codes_out, scales_out, sum_out, values_out
@@ -1038,6 +1049,7 @@ def ax_rmsnorm_backward(gy, t, weight, rstd, gsum=None, gx_out=None, gw_out=None
     d, need = hit
     gx_out, gw_out = (None if o is False else o for o in (gx_out, gw_out))
     ws = _scratch(need, workspace, t.device, stream)
+    _lend(stream, gx_out, gw_out)
     _check(L.ax_rmsnorm_backward(d, _ptr(gy), _ptr(gsum), _ptr(t), _ptr(weight), _ptr(rstd), _ptr(gx_out), _ptr(gw_out),
                                  *_ws_args(ws), _stream_ptr(stream)))
     return gx_out, gw_out
@@ -1103,6 +1115,7 @@ def ax_matmul(x, w, bias=None, residual=None, act="none", transposed=False, out_
         hit = _remember(key, (d, int(L.ax_matmul_workspace_bytes(d))))
     d, need = hit
     ws = _scratch(need, workspace, dev, stream)
+    _lend(stream, y_out, z_out)
     _check(L.ax_matmul(d, xp, wp, _ptr(bias), _ptr(residual), y_out.data_ptr(), _ptr(z_out), *_ws_args(ws), _stream_ptr(stream)))
     return y_out, z_out
 
@@ -1127,6 +1140,7 @@ def ax_matmul_q8(x, x_scales, w, w_scales, bias=None, residual=None, act="none",
         hit = _remember(key, (d, int(L.ax_matmul_q8_workspace_bytes(d))))
     d, need = hit
     ws = _scratch(need, workspace, dev, stream)
+    _lend(stream, y_out)
     _check(L.ax_matmul_q8(d, xp, x_scales.data_ptr(), wp, w_scales.data_ptr(), _ptr(bias), _ptr(residual), y_out.data_ptr(),
                           *_ws_args(ws), _stream_ptr(stream)))
     return y_out
@@ -1174,6 +1188,7 @@ def ax_matmul_backward(gy, x, w, z=None, act="none", transposed=False, gx_out=No
     d, need = hit
     gx_out, gw_out, gb_out = (None if o is False else o for o in (gx_out, gw_out, gb_out))
     ws = _scratch(need, workspace, dev, stream)
+    _lend(stream, gx_out, gw_out, gb_out)
     _check(L.ax_matmul_backward(d, gp, xp, wp, _ptr(z), _ptr(gx_out), _ptr(gw_out), _ptr(gb_out), *_ws_args(ws), _stream_ptr(stream)))
     return gx_out, gw_out, gb_out
 
@@ -1208,6 +1223,7 @@ def ax_gated(x, wg, wu, act="silu", out_dtype=None, save=False, h_out=None, g_ou
         hit = _remember(key, (d, int(L.ax_gated_workspace_bytes(d))))
     d, need = hit
     ws = _scratch(need, workspace, dev, stream)
+    _lend(stream, h_out, g_out, u_out)
     _check(L.ax_gated(d, xp, gp, up, h_out.data_ptr(), _ptr(g_out), _ptr(u_out), *_ws_args(ws), _stream_ptr(stream)))
     return h_out, g_out, u_out
 
@@ -1232,6 +1248,7 @@ def ax_gated_q8(x, x_scales, wg, wg_scales, wu, wu_scales, act="silu", out_dtype
         hit = _remember(key, (d, int(L.ax_gated_q8_workspace_bytes(d))))
     d, need = hit
     ws = _scratch(need, workspace, dev, stream)
+    _lend(stream, h_out)
     _check(L.ax_gated_q8(d, xp, x_scales.data_ptr(), gp, wg_scales.data_ptr(), up, wu_scales.data_ptr(), h_out.data_ptr(),
                          *_ws_args(ws), _stream_ptr(stream)))
     return h_out
@@ -1258,6 +1275,7 @@ def ax_gated_backward(gh, x, wg, wu, g, u, act="silu", gx_out=None, gwg_out=None
     d, need = hit
     gx_out, gwg_out, gwu_out = (None if o is False else o for o in (gx_out, gwg_out, gwu_out))
     ws = _scratch(need, workspace, dev, stream)
+    _lend(stream, gx_out, gwg_out, gwu_out)
     _check(L.ax_gated_backward(d, gh.data_ptr(), xp, gp, up, g.data_ptr(), u.data_ptr(), _ptr(gx_out), _ptr(gwg_out), _ptr(gwu_out),
                                *_ws_args(ws), _stream_ptr(stream)))
     return gx_out, gwg_out, gwu_out
@@ -1342,6 +1360,7 @@ class AxAdamW:
         if self.bits == 32:
             return self.m, self.v
         out = [[torch.empty(t.shape, dtype=torch.float32, device=t.device) for t in self.params] for _ in range(2)]
+        _lend(stream, *out[0], *out[1])
         ptrs = [(ctypes.c_void_p * len(o))(*[t.data_ptr() for t in o]) for o in out]
         _check(lib().ax_adamw_states(self._t, len(self._t), ptrs[0], ptrs[1], _stream_ptr(stream)))
         return out[0], out[1]

@@ -190,7 +190,7 @@ long long fill_batch(Batch* b, const ax_adamw_tensor_t* t, int count, int* next,
   while (*next < count && k < AX_ADAMW_LAUNCH) {
     const ax_adamw_tensor_t& e = t[*next];
     const long long c = (e.n + kChunk - 1) / kChunk;
-    if (chunks > 0 && chunks + c > 0x7fffffffll) break;
+    if (chunks > 0 && chunks + c >= 1 << 24) break;  // (a launch counts its threads in 32 bits)
     if (e.n > 0) {
       b->t[k] = Tensor{m_out ? (void*)m_out[*next] : e.p, e.g, e.m, e.v, e.m_scale, e.v_scale,
                        v_out ? (void*)v_out[*next] : e.copy, (long long)e.n};
@@ -220,7 +220,7 @@ extern "C" int ax_adamw(const ax_adamw_desc_t* d, const ax_adamw_tensor_t* tenso
   const bool q8 = d->state_bits == 8;
   for (int i = 0; i < count; ++i) {
     const ax_adamw_tensor_t& t = tensors[i];
-    if (t.n < 0 || t.n > (1ll << 42)) return AX_ERR_SHAPE;
+    if (t.n < 0 || t.n >= 1ll << 36) return AX_ERR_SHAPE;
     if (t.n == 0) continue;
     if (!t.p || !t.g || !t.m || !t.v || (q8 && (!t.m_scale || !t.v_scale))) return AX_ERR_NULL;
     if ((uintptr_t)t.p % pe || (uintptr_t)t.g % ge || (uintptr_t)t.copy % 2) return AX_ERR_ALIGN;
@@ -254,7 +254,7 @@ extern "C" int ax_adamw_states(const ax_adamw_tensor_t* tensors, int count, floa
   if (count > 0 && (!tensors || !m_out || !v_out)) return AX_ERR_NULL;
   for (int i = 0; i < count; ++i) {
     const ax_adamw_tensor_t& t = tensors[i];
-    if (t.n < 0 || t.n > (1ll << 42)) return AX_ERR_SHAPE;
+    if (t.n < 0 || t.n >= 1ll << 36) return AX_ERR_SHAPE;
     if (t.n == 0) continue;
     if (!t.m || !t.v || !t.m_scale || !t.v_scale || !m_out[i] || !v_out[i]) return AX_ERR_NULL;
     if ((uintptr_t)t.m_scale % 4 || (uintptr_t)t.v_scale % 4 || (uintptr_t)m_out[i] % 4 || (uintptr_t)v_out[i] % 4) return AX_ERR_ALIGN;

@@ -558,6 +558,7 @@ void launch_tile3(const Args& a, int tile, int grid, hipStream_t s) {
 
 constexpr int kCus = 256;
 constexpr int kMaxSplits = 16;
+constexpr long long kMaxGrid = 1 << 22;  // workgroups: a launch counts its threads in 32 bits
 
 long long tiles_of(const GemmArgs& g, const TileShape& t) {
   const int bns = t.bn / (g.gated ? 2 : 1);
@@ -582,7 +583,9 @@ GemmPlan plan_gemm(const GemmArgs& g) {
     if (T.bm == 32 && g.la != 0) continue;
     const long long steps = (kbytes + T.kb - 1) / T.kb * g.nseg;
     const long long tiles = tiles_of(g, T);
+    if (t > 0 && tiles > kMaxGrid) continue;
     for (int sp = 1; sp <= kMaxSplits && (sp == 1 || sp * 2 <= steps); ++sp) {
+      if (sp > 1 && tiles * sp > kMaxGrid) break;
       const long long n = tiles * sp, slots = (long long)kCus * T.per_cu;
       const long long full = n / slots, rest = n - full * slots;
       const double stages = (double)((steps + sp - 1) / sp) * T.kb / 128;
@@ -616,7 +619,7 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStre
   a.part = (float*)part;
   a.ldp = part_pitch(g);
   const long long grid = (long long)a.tiles_m * a.tiles_n * p.splits;
-  if (grid <= 0 || grid > 0x7fffffffll) return hipErrorInvalidValue;
+  if (grid <= 0 || grid >= 1 << 23) return hipErrorInvalidValue;
   const int n = (int)grid;
   if (g.pieces == 3) {
     if (g.gated) launch_tile3<0, 1, 2>(a, p.tile, n, s);

@@ -245,7 +245,7 @@ int rows_per_block(int M, int N) {  // about eight workgroups per compute unit, 
 
 // ---- checks ------------------------------------------------------------------------------------------------------
 
-constexpr long long kMaxDim = 0x7fffffff, kMaxPitch = 1 << 22;
+constexpr long long kMaxDim = 1 << 30, kMaxPitch = 1 << 22;
 
 bool dtype_ok(int d) { return d == AX_F32 || d == AX_BF16; }
 bool pitch_ok(long long ld, long long cols, int esz) { return ld >= cols && ld * esz < kMaxPitch; }
@@ -299,8 +299,8 @@ struct Forward {
 //   int8 gated, where one launch of tiles has enough of them
 //                                       1/4096/4096 7.8 : 14.7   16/2048/6000 8.9 : 9.0     17/4096/10240 23.3 : 17.3
 bool few_fits(int dtype, bool along, bool gated, long long M, long long N, long long K) {
-  if (dtype == AX_F32) return M <= 16;
-  if (M > 32) return false;
+  if (dtype == AX_F32) return M <= 16 && N <= 1 << 20;
+  if (M > 32 || N > 1 << 20) return false;
   if (dtype == kI8 && gated) return N <= 8192 && M * N <= 98304;
   return along || K <= 2048 || (M <= 4 && K <= 4096);
 }

@@ -34,7 +34,7 @@ struct NormArgs {
   float* scales;
   float* values;  // may be null
   float* rstd;    // may be null
-  long long rows;
+  long long rows, row0;  // row0: first of this launch
   long long x_ld, r_ld, s_ld, y_ld;
   int cols, w_f32, normalize;
   float eps;
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const NormA
   constexpr int THREADS = TPR < 256 ? 256 : TPR;
   __shared__ float red[2 * (TPR / 64)];
   const int t = threadIdx.x % TPR;
-  const long long row = (long long)blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
+  const long long row = a.row0 + (long long)blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
   if (row >= a.rows) return;  // uniform over a row's lanes (and over the workgroup where it has one row)
   const long long xo = row * a.x_ld, ro = row * a.r_ld, so = row * a.s_ld, yo = row * a.y_ld, co = row * (long long)a.cols;
   const int iters = NV ? NV : (a.cols + TPR * 8 - 1) / (TPR * 8);
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(const NormA
   const float rstd = a.normalize ? 1.f / sqrtf(ss / (float)a.cols + a.eps) : 1.f;
   const float amax = __uint_as_float(top);
   const float inv = amax >= 0x1p-120f && top < 0x7f800000u ? 127.f / amax : 0.f;
-  const float scale = amax * rstd / 127.f;
+  const float scale = top ? amax * rstd / 127.f : 0.f;  // (rstd may be infinite)
   if (t == 0) {
     if (a.rstd) a.rstd[row] = rstd;
     if (MODE == kCodes) a.scales[row] = scale;
@@ -182,7 +182,7 @@ struct NormGradArgs {
   const float* rstd;
   void* gx;     // may be null
   float* part;  // [workgroups][cols], may be null
-  long long rows;
+  long long rows, row0;
   long long t_ld, gs_ld, gx_ld, gy_ld;
   int cols, w_f32;
 };
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const NormGradArgs
   constexpr int TPR = 1024;
   __shared__ float red[2 * (TPR / 64)];
   const int t = threadIdx.x;
-  const long long row = blockIdx.x;
+  const long long row = a.row0 + blockIdx.x;
   const float rstd = a.rstd[row];
   const int iters = (a.cols + TPR * 8 - 1) / (TPR * 8);
   float dot = 0.f;
@@ -314,26 +314,29 @@ __global__ __launch_bounds__(256) void norm_gw_long_kernel(const NormGradArgs a)
 __global__ __launch_bounds__(1024) void column_sum_kernel(const float* __restrict__ part, int rows, int cols, float* __restrict__ out) {
   __shared__ float red[64][17];
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
-  const int c = blockIdx.x * 16 + x;
-  float s = 0.f;
-  if (c < cols) {
-    int r = y;
-    for (; r + 64 * 7 < rows; r += 64 * 8) {  // eight loads at a time
-      float v[8];
+  for (long long c0 = blockIdx.x * 16ll; c0 < cols; c0 += gridDim.x * 16ll) {
+    const long long c = c0 + x;
+    float s = 0.f;
+    if (c < cols) {
+      int r = y;
+      for (; r + 64 * 7 < rows; r += 64 * 8) {  // eight loads at a time
+        float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = part[(long long)(r + 64 * k) * cols + c];
+        for (int k = 0; k < 8; ++k) v[k] = part[(long long)(r + 64 * k) * cols + c];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s += v[k];
+        for (int k = 0; k < 8; ++k) s += v[k];
+      }
+      for (; r < rows; r += 64) s += part[(long long)r * cols + c];
     }
-    for (; r < rows; r += 64) s += part[(long long)r * cols + c];
-  }
-  red[y][x] = s;
-  __syncthreads();
-  for (int h = 32; h > 0; h >>= 1) {
-    if (y < h) red[y][x] += red[y + h][x];
+    red[y][x] = s;
+    __syncthreads();
+    for (int h = 32; h > 0; h >>= 1) {
+      if (y < h) red[y][x] += red[y + h][x];
+      __syncthreads();
+    }
+    if (y == 0 && c < cols) out[c] = red[0][x];
     __syncthreads();
   }
-  if (y == 0 && c < cols) out[c] = red[0][x];
 }
 
 // ---- dispatch ----------------------------------------------------------------------------------------------------
@@ -351,11 +354,12 @@ Shape shape_of(long long rows, long long cols) {
   return {1024, 0};
 }
 
+constexpr int kMaxGrid = 1 << 21;  // workgroups of a launch, which counts its threads in 32 bits
+
 template <int MODE, bool F32>
-void norm_launch(const NormArgs& a, hipStream_t s) {
-  const Shape sh = shape_of(a.rows, a.cols);
+void norm_launch(const NormArgs& all, hipStream_t s) {
+  const Shape sh = shape_of(all.rows, all.cols);
   const int per = sh.tpr == 64 ? 4 : 1;
-  const unsigned grid = (unsigned)((a.rows + per - 1) / per);
   const int threads = sh.tpr < 256 ? 256 : sh.tpr;
 #define AX_NORM(T, V) norm_kernel<MODE, F32, T, V><<<grid, threads, 0, s>>>(a)
 #define AX_NORM_T(T)                         \
@@ -364,10 +368,14 @@ void norm_launch(const NormArgs& a, hipStream_t s) {
     case 2: AX_NORM(T, 2); break;            \
     default: AX_NORM(T, 4); break;           \
   }
-  if (sh.nv == 0) AX_NORM(1024, 0);
-  else if (sh.tpr == 64) AX_NORM_T(64)
-  else if (sh.tpr == 256) AX_NORM_T(256)
-  else AX_NORM_T(1024)
+  NormArgs a = all;
+  for (a.row0 = 0; a.row0 < a.rows; a.row0 += (long long)kMaxGrid * per) {
+    const unsigned grid = (unsigned)std::min<long long>((a.rows - a.row0 + per - 1) / per, kMaxGrid);
+    if (sh.nv == 0) AX_NORM(1024, 0);
+    else if (sh.tpr == 64) AX_NORM_T(64)
+    else if (sh.tpr == 256) AX_NORM_T(256)
+    else AX_NORM_T(1024)
+  }
 #undef AX_NORM_T
 #undef AX_NORM
 }
@@ -440,7 +448,7 @@ int norm_common(const ax_norm_desc_t* d, NormArgs& a, bool codes, hipStream_t s)
 }  // namespace
 
 hipError_t launch_column_sum(const float* part, int rows, int cols, float* out, hipStream_t s) {
-  column_sum_kernel<<<(cols + 15) / 16, 1024, 0, s>>>(part, rows, cols, out);
+  column_sum_kernel<<<std::min((cols + 15ll) / 16, 65536ll), 1024, 0, s>>>(part, rows, cols, out);
   return hipGetLastError();
 }
 
@@ -522,8 +530,11 @@ extern "C" int ax_rmsnorm_backward(const ax_norm_desc_t* d, const void* gy, cons
   const int groups = grad_groups(d->rows, d->cols);
   if (grad_is_long(sh)) {
     if (gx_out) {
-      if (f32) norm_grad_long_kernel<true><<<(unsigned)d->rows, 1024, 0, s>>>(a);
-      else norm_grad_long_kernel<false><<<(unsigned)d->rows, 1024, 0, s>>>(a);
+      for (a.row0 = 0; a.row0 < a.rows; a.row0 += kMaxGrid) {
+        const unsigned grid = (unsigned)std::min<long long>(a.rows - a.row0, kMaxGrid);
+        if (f32) norm_grad_long_kernel<true><<<grid, 1024, 0, s>>>(a);
+        else norm_grad_long_kernel<false><<<grid, 1024, 0, s>>>(a);
+      }
     }
     if (gw_out) {
       const dim3 grid((a.cols + 255) / 256, groups);

@@ -13,11 +13,17 @@ scale a row, weights are laid out once as [outputs, inputs] codes with a scale a
 
 from __future__ import annotations
 
+import contextlib
 import math
 
 import torch
 
 from . import binding as ax
+
+
+def _on(stream):
+    """The context in which everything, allocations included, belongs to `stream` (None: the current one)."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 class FeedForward:
@@ -46,10 +52,11 @@ class FeedForward:
     def forward(self, x, residual=None, train=False, stream=None):
         """y [rows, width]; with train, what backward needs is kept until it is called."""
         p = self.params
-        n, t, rstd = ax.ax_rmsnorm(x, p["norm"], residual=residual, eps=self.eps, rstd_out=None if train else False, stream=stream)
-        t = x if t is None else t
-        h, g, u = ax.ax_gated(n, p["wg"], p["wu"], act=self.act, save=train, stream=stream)
-        y, _ = ax.ax_matmul(h, p["wd"], bias=p["bias"], residual=t, stream=stream)
+        with _on(stream):
+            n, t, rstd = ax.ax_rmsnorm(x, p["norm"], residual=residual, eps=self.eps, rstd_out=None if train else False)
+            t = x if t is None else t
+            h, g, u = ax.ax_gated(n, p["wg"], p["wu"], act=self.act, save=train)
+            y, _ = ax.ax_matmul(h, p["wd"], bias=p["bias"], residual=t)
         if train:
             self._kept = (n, t, rstd, h, g, u)
         return y
@@ -61,9 +68,10 @@ class FeedForward:
         n, t, rstd, h, g, u = self._kept
         self._kept = None
         p, d = self.params, self.grads
-        gh, _, _ = ax.ax_matmul_backward(gy, h, p["wd"], gw_out=d["wd"], gb_out=d["bias"], stream=stream)
-        gn, _, _ = ax.ax_gated_backward(gh, n, p["wg"], p["wu"], g, u, act=self.act, gwg_out=d["wg"], gwu_out=d["wu"], stream=stream)
-        gx, _ = ax.ax_rmsnorm_backward(gn, t, p["norm"], rstd, gsum=gy, gw_out=d["norm"], stream=stream)
+        with _on(stream):
+            gh, _, _ = ax.ax_matmul_backward(gy, h, p["wd"], gw_out=d["wd"], gb_out=d["bias"])
+            gn, _, _ = ax.ax_gated_backward(gh, n, p["wg"], p["wu"], g, u, act=self.act, gwg_out=d["wg"], gwu_out=d["wu"])
+            gx, _ = ax.ax_rmsnorm_backward(gn, t, p["norm"], rstd, gsum=gy, gw_out=d["norm"])
         return gx
 
     def step(self, lr, weight_decay=0.0, grad_scale=None, stream=None, **betas):
@@ -82,15 +90,17 @@ class QuantizedFeedForward:
 
     def __init__(self, block: FeedForward, stream=None):
         self.act, self.eps, self.dtype = block.act, block.eps, block.dtype
-        self.norm, self.bias = block.params["norm"].clone(), block.params["bias"].clone()
-        self.w = {}
-        for name in ("wg", "wu", "wd"):  # [inputs, outputs] -> codes [outputs, inputs], a scale an output
-            codes, scales, _, _ = ax.ax_rmsnorm_q8(block.master[name].t().contiguous(), normalize=False, stream=stream)
-            self.w[name] = (codes, scales)
+        with _on(stream):
+            self.norm, self.bias = block.params["norm"].clone(), block.params["bias"].clone()
+            self.w = {}
+            for name in ("wg", "wu", "wd"):  # [inputs, outputs] -> codes [outputs, inputs], a scale an output
+                codes, scales, _, _ = ax.ax_rmsnorm_q8(block.master[name].t().contiguous(), normalize=False)
+                self.w[name] = (codes, scales)
 
     def forward(self, x, residual=None, stream=None):
-        codes, scales, t, _ = ax.ax_rmsnorm_q8(x, self.norm, residual=residual, eps=self.eps, stream=stream)
-        t = x if t is None else t
-        h = ax.ax_gated_q8(codes, scales, *self.w["wg"], *self.w["wu"], act=self.act, out_dtype=self.dtype, stream=stream)
-        hc, hs, _, _ = ax.ax_rmsnorm_q8(h, normalize=False, stream=stream)
-        return ax.ax_matmul_q8(hc, hs, *self.w["wd"], bias=self.bias, residual=t, out_dtype=self.dtype, stream=stream)
+        with _on(stream):
+            codes, scales, t, _ = ax.ax_rmsnorm_q8(x, self.norm, residual=residual, eps=self.eps)
+            t = x if t is None else t
+            h = ax.ax_gated_q8(codes, scales, *self.w["wg"], *self.w["wu"], act=self.act, out_dtype=self.dtype)
+            hc, hs, _, _ = ax.ax_rmsnorm_q8(h, normalize=False)
+            return ax.ax_matmul_q8(hc, hs, *self.w["wd"], bias=self.bias, residual=t, out_dtype=self.dtype)

@@ -209,6 +209,61 @@ def test_pitches_and_places(dt, offset, pad):
     assert torch.equal(ybuf, old)
 
 
+@pytest.mark.parametrize("M,K,N", [(3, 64, 40), (40, 4096, 72), (300, 72, 264)])
+def test_result_in_the_place_of_the_residual(M, K, N):
+    g = F.gen(M)
+    x, w, r = F.randn(g, (M, K), 1.0, torch.bfloat16).cuda(), F.randn(g, (K, N), K ** -0.5, torch.bfloat16).cuda(), F.randn(g, (M, N), 1.0, torch.bfloat16).cuda()
+    want, _ = ax.ax_matmul(x, w, residual=r, act="gelu")
+    y, _ = ax.ax_matmul(x, w, residual=r, act="gelu", y_out=r)
+    assert y is r and torch.equal(r, want)
+
+
+# both sides of the bounds between the kernel of few rows and the tiles, of its own fragments of 16 rows and 16, 32 or 64
+# columns, and of its waves' turns along the contraction
+@pytest.mark.parametrize("dt", ["f32", "bf16", "q8"])
+@pytest.mark.parametrize("M", [2, 15, 16, 17, 31, 32, 33])
+@pytest.mark.parametrize("K,N", [(1, 17), (30, 33), (129, 16), (2048, 48), (2050, 31), (4100, 70), (72, 8200), (40, 16400)])
+def test_few_rows(M, K, N, dt):
+    g = F.gen(M * K + N)
+    if dt == "q8":
+        (x, xs), (w, ws) = _codes(g, M, K), _codes(g, N, K)
+        y = ax.ax_matmul_q8(x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), out_dtype=torch.float32)
+        a = (x.double() @ w.double().t()) * xs.double()[:, None] * ws.double()
+        F.assert_within(y, a, a.abs() * 5 * F.U)
+        h = ax.ax_gated_q8(x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), w.cuda(), ws.cuda(), act="relu", out_dtype=torch.float32)
+        F.assert_within(h, torch.relu(a) * a, a * a * 12 * F.U)
+        return
+    dtype = F.DT[dt]
+    x, w, wt = F.randn(g, (M, K), 1.0, dtype), F.randn(g, (K, N), K ** -0.5, dtype), F.randn(g, (N, K), K ** -0.5, dtype)
+    b = F.randn(g, (N,), 1.0, torch.float32)
+    for v, vd, t in ((w, w.double(), False), (wt, wt.double().t(), True)):
+        zd, size = _product(x.double(), vd)
+        zd = zd + b.double()
+        y, z = ax.ax_matmul(x.cuda(), v.cuda(), bias=b.cuda(), transposed=t, act="silu", out_dtype=torch.float32, save=True)
+        zb = size * F.sum_bound(K, dt == "f32") + 2 * F.U * (zd.abs() + b.double().abs())
+        F.assert_within(z, zd, zb, "z")
+        F.assert_within(y, F.act(zd, "silu"), zb * F.ACT_LIP + F.act(zd, "silu").abs() * F.ACT_REL, "y")
+        gy = F.randn(g, (M, N), 1.0, dtype)
+        gx = ax.ax_matmul_backward(gy.cuda(), x.cuda(), v.cuda(), transposed=t, gw_out=False, gb_out=False)[0]
+        want, size = _product(gy.double(), vd.t())
+        F.assert_within(gx, want, size * F.sum_bound(N, dt == "f32") + want.abs() * F.store(dtype), "gx")
+
+
+def test_other_streams():
+    """Calls on a stream that is not the current one, their workspaces and results allocated inside."""
+    g = F.gen(8)
+    x, w, wu = F.randn(g, (257, 320)).cuda(), F.randn(g, (320, 136), 0.05).cuda(), F.randn(g, (320, 136), 0.05).cuda()
+    want = ax.ax_gated(x, w, wu, save=True)
+    grad = ax.ax_gated_backward(want[0], x, w, wu, want[1], want[2])
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        got = ax.ax_gated(x, w, wu, save=True, stream=s)
+        out = ax.ax_gated_backward(got[0], x, w, wu, got[1], got[2], stream=s)
+        s.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and all(torch.equal(a, b) for a, b in zip(out, grad))
+
+
 def test_gradients_inside_wider_buffers():
     g, M, K, N = F.gen(4), 40, 48, 56
     big = torch.full((K, N + 8), 3.0, device="cuda", dtype=torch.bfloat16)

@@ -151,6 +151,12 @@ def test_pitches_and_places(dt, offset, pad):
         assert torch.equal(b, old)
 
 
+def test_rows_of_zeros_without_eps():
+    x = torch.zeros((5, 70), device="cuda")
+    codes, scales, _, values = ax.ax_rmsnorm_q8(x, torch.ones(70, device="cuda"), eps=0.0, values=True)
+    assert not bool(codes.any()) and not bool(scales.any()) and not bool(values.any())
+
+
 def test_no_rows():
     x, w = torch.empty((0, 33), device="cuda"), torch.ones(33, device="cuda")
     y, t, rstd = ax.ax_rmsnorm(x, w)
