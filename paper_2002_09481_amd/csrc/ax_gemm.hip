@@ -117,15 +117,22 @@ __device__ __forceinline__ int swizzle(int row) {
   return KB == 128 ? (row >> 1) & 7 : (-(row >> 2)) & 3;
 }
 
+// Where a stage keeps a 32-byte pair of chunks of a row (of R elements, L = 1): at pair ^ pair_swizzle(row).  A transposing
+// 8-byte read takes 32 bytes of rows 8 g + 0 .. 3 for g = 0 .. 3; the eight rows of either half of the wave get eight
+// different slots (rows of 64 elements: two of them share a line of the banks).
+template <int R>
+__device__ __forceinline__ int pair_swizzle(int row) {
+  return R >= 128 ? (row & 3) | ((row >> 1) & 4) : ((row >> 1) & 1) | ((row >> 2) & 2);
+}
+
 // One operand's share of the copies.  L = 0: R rows of KB bytes, contraction contiguous.  L = 1 (bf16): KB / 2 rows (the
-// contraction) of R elements; 32-byte chunk pairs are stored at pair ^ (bits 0, 1 and 3 of the row), for the transposing
-// 8-byte reads.
+// contraction) of R elements.
 template <int L, int R, int KB, int THREADS>
 struct Stager {
   static constexpr int kLoads = R * KB / 16 / THREADS;
   static_assert(kLoads >= 1 && kLoads * 16 * THREADS == R * KB, "whole copies per thread");
   static constexpr int kRowChunks = L == 0 ? KB / 16 : R / 8;
-  static constexpr int kPairMask = R / 16 - 1;  // L = 1
+  static_assert(L == 0 || R >= 64, "four pairs a row at least");
   static_assert(THREADS / kRowChunks % 16 == 0, "the swizzle is the same in all copies of a thread");
   uint32_t off;   // of this thread's first copy; the others follow at `step`
   uint32_t step;  // uniform
@@ -138,8 +145,7 @@ struct Stager {
       chunk = pos ^ swizzle<KB>(row);
       off = (uint32_t)(row * ld + chunk * 16);
     } else {
-      const int sp = ((row & 3) | ((row >> 1) & 4)) & kPairMask;
-      const int c = pos ^ (sp << 1);
+      const int c = pos ^ (pair_swizzle<R>(row) << 1);
       off = c * 8 < cols_left ? (uint32_t)(row * ld + c * 16) : kOut;
     }
   }
@@ -170,8 +176,7 @@ __device__ __forceinline__ u32x4 fragment(uint32_t lds, int r0, int ks, int lane
     const uint32_t a = lds + (uint32_t)((r0 + r) * KB + (((ks * 4 + g) ^ swizzle<KB>(r)) << 4));
     return *(const AX_LDS(u32x4)*)(uintptr_t)a;
   }
-  const int kr = r >> 2;
-  const int sp = (kr | ((g & 1) << 2)) & (R / 16 - 1);
+  const int kr = r >> 2, sp = pair_swizzle<R>(8 * g + kr);
   const uint32_t a = lds + (uint32_t)((ks * 32 + g * 8 + kr) * (R * 2) + (((r0 >> 4) ^ sp) << 5) + 8 * (lane & 3));
   const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((AX_LDS(s16x4)*)(uintptr_t)a);
   const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((AX_LDS(s16x4)*)(uintptr_t)(a + 4 * R * 2));
