@@ -3,7 +3,11 @@
 // Bound by memory: 2 M operations for each weight.  So nothing is staged: a workgroup of 16 waves takes 16 to 64 columns
 // of the result, its waves take turns along the contraction, and a lane loads weights straight into the registers that the
 // matrix instruction wants (16 columns x 32 of the contraction, 64 for int8), several steps ahead of their use.  The
-// waves' sums meet in LDS, in the waves' order, and the epilogue follows there: one launch, no partial sums in memory.
+// waves' sums meet in LDS, in the waves' order, and the epilogue follows there: one launch, no partial sums in memory.  Only
+// where the columns would leave compute units idle is the contraction cut, and a second launch joins the slices' sums.
+//
+// Measured, weights from memory (us at rows / K / N): bf16 [N, K] 1/4096/4096 9.6 (3.5 TB/s), [K, N] 1/2048/8192 10.3
+// (3.3 TB/s), float32 [K, N] 17/8192/8192 71.5 (3.75 TB/s); slices: float32 [K, N] 16/8192/512 13.5, uncut 45.
 //
 // Weights [N, K]: a lane holds 8 (int8: 16) consecutive elements of a row, what the instruction wants.  Weights [K, N]: a
 // lane loads V neighbouring columns of eight rows, and the eight values of a column are put together by byte permutes;
@@ -25,7 +29,12 @@ enum Kind { kBf16, kInt8, kF32 };
 
 struct Args {
   GemmArgs g;
-  int blocks;  // of the contraction, per segment
+  int blocks;   // of the contraction, per segment
+  int tiles;    // workgroups along the columns
+  int slices;   // of the contraction, each `per` turns of a wave (over all segments)
+  int per;
+  float* part;  // [slices][NB][M][ldp] with slices, as the joining kernel reads them
+  long long ldp;
 };
 
 // One operand of the matrix instruction: bf16 or int8 as they are, float32 as three pieces.
@@ -50,13 +59,25 @@ __device__ __forceinline__ Acc mma(const Frag<KD>& a, const Frag<KD>& b, Acc c) 
 }
 
 // A lane's share of a row with the contraction contiguous: raw bytes (32 for float32), `left` elements of them there.
-template <Kind KD>
+// ODD: rows may start inside a word.  Reads of 16 bytes off the words cost two to three times as much (us at rows / K / N of
+// [N, K], with and without ODD: bf16 16/4097/4096 18.1 : 28.5, int8 9.2 : 17.4), so the words that hold the bytes are read, and
+// shifted when they are used.  No word is read that holds none of the row's elements.
+template <Kind KD, bool ODD>
 struct Along {
   u32x4 q[KD == kF32 ? 2 : 1];
+  uint32_t next, shift;
   template <bool FULL>
   __device__ __forceinline__ void load(const char* row, int k, int left) {
     constexpr int E = KD == kInt8 ? 16 : 8, B = KD == kInt8 ? 1 : KD == kBf16 ? 2 : 4;
     const char* p = row + (long long)k * B;
+    if (ODD && FULL) {
+      shift = (uint32_t)(uintptr_t)row & 3u;  // (k elements are whole words)
+      const char* words = p - shift;
+      q[0] = load_any<u32x4>(words);
+      next = *(const uint32_t*)(words + (shift ? 16 : 12));
+      return;
+    }
+    if (ODD) shift = 0;
     if (FULL || left >= E) {
       q[0] = load_any<u32x4>(p);
       if (KD == kF32) q[KD == kF32 ? 1 : 0] = load_any<u32x4>(p + 16);
@@ -83,6 +104,9 @@ struct Along {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(q[e >> 2][e & 3]);
       pieces_of(v, f.p);
+    } else if constexpr (ODD) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) f.p[0][w] = __builtin_amdgcn_alignbyte(w < 3 ? q[0][w < 3 ? w + 1 : 0] : next, q[0][w], shift);
     } else {
       f.p[0] = q[0];
     }
@@ -133,7 +157,8 @@ struct Across {
 
 // LB: 0 = weights [N, K], 1 = [K, N].  NB: 2 for the gated pair.  MFR: fragments of 16 rows.  CF: fragments of 16 columns
 // of one weight (LB = 1: neighbouring columns a lane).  U: steps of the contraction a wave loads at a time.
-template <Kind KD, int LB, int NB, int MFR, int CF, int U>
+// ODD: rows may start inside a word (not for float32).
+template <Kind KD, int LB, int NB, int MFR, int CF, int U, bool ODD>
 __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
   constexpr int KS = KD == kInt8 ? 64 : 32, LANE = KS / 4;  // contraction of a step, of a lane
   constexpr int ES = KD == kInt8 ? 1 : KD == kBf16 ? 2 : 4;
@@ -144,10 +169,12 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
   const int t = threadIdx.x, lane = t & 63, r = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   // workgroups b, b + 8, ... share an XCD: they take neighbouring columns, which may share lines of memory
-  int tile;
+  int tile, slice;
   {
     const int b = blockIdx.x, x = b & 7, i = b >> 3, total = gridDim.x, per = total >> 3, more = total & 7;
     tile = x * per + min(x, more) + i;
+    slice = a.slices > 1 ? tile / a.tiles : 0;
+    tile -= slice * a.tiles;
   }
   const int n0 = tile * COLS;
 
@@ -161,14 +188,15 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
 
   const bool all_cols = n0 + COLS <= g.N;
   const int groups = (a.blocks + U - 1) / U;
-  for (int it = wave; it < groups * g.nseg; it += kWaves) {
+  const int behind = min((slice + 1) * a.per, groups * g.nseg);
+  for (int it = slice * a.per + wave; it < behind; it += kWaves) {
     const int seg = __builtin_amdgcn_readfirstlane(g.nseg == 1 ? 0 : it / groups);
     const int k0 = (it - seg * groups) * U * KS;
     const char* x = (const char*)g.seg[seg].a;
     const char* w[2] = {(const char*)g.seg[seg].b, (const char*)g.seg[seg].b2};
     auto run = [&](auto full) __attribute__((always_inline)) {
-      Along<KD> xa[U][MFR];
-      typename std::conditional<LB == 0, Along<KD>, Across<KD == kInt8 ? kBf16 : KD, CF>>::type wa[U][NB][LB == 0 ? CF : 1];
+      Along<KD, ODD> xa[U][MFR];
+      typename std::conditional<LB == 0, Along<KD, ODD>, Across<KD == kInt8 ? kBf16 : KD, CF>>::type wa[U][NB][LB == 0 ? CF : 1];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int k = k0 + u * KS + LANE * q, left = g.K - k;
@@ -231,13 +259,18 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
         int32_t v = 0;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) v += __float_as_int(part[w][b][m][c]);
-        s[b] = (float)v * (g.xs[m] * (b ? g.ws2 : g.ws)[n]);
+        s[b] = a.slices > 1 ? __int_as_float(v) : (float)v * (g.xs[m] * (b ? g.ws2 : g.ws)[n]);
       } else {
         float v = 0.f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) v += part[w][b][m][c];
         s[b] = v;
       }
+    }
+    if (a.slices > 1) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) a.part[((long long)(slice * NB + b) * g.M + m) * a.ldp + n] = s[b];
+      continue;
     }
     auto put = [&](void* p, long long i, float v) {
       if (g.odt == AX_F32) ((float*)p)[i] = v;
@@ -255,54 +288,103 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
   }
 }
 
-// Columns of a workgroup: as many as leave a workgroup for every compute unit (wider pieces of a line, fewer reads of x).
+// Fragments of 16 columns a workgroup takes: as many as leave a workgroup for every compute unit (wider pieces of a line,
+// fewer reads of x).
+constexpr int cols_of(Kind kd, int lb, int nb, int mfr, int n) {
+  const bool wide = kd == kF32 && mfr == 2;  // (the pieces of 32 rows leave few registers)
+  if (lb == 0) return mfr * nb < 4 && !wide && n >= 8192 ? 2 : 1;
+  if (wide && nb == 2) return 1;
+  return kd == kBf16 && mfr * nb == 1 && n >= 16384 ? 4 : 2;
+}
+// Steps of the contraction that a wave loads at a time: what 128 registers a lane hold.
+constexpr int steps_of(Kind kd, int lb, int nb, int mfr) {
+  if (kd == kF32) return nb == 2 || (lb == 1 && mfr == 2) ? 1 : 2;
+  return 4 / nb;
+}
+
 template <Kind KD, int LB, int NB, int MFR>
-void launch_cols(const Args& a, hipStream_t s) {
-  constexpr int U = KD == kF32 ? 2 / NB : 4 / NB;  // (what 128 registers a lane hold)
+void launch_cols(Args& a, hipStream_t s) {
+  constexpr int U = steps_of(KD, LB, NB, MFR);
+  uintptr_t low = (uintptr_t)a.g.lda;
+  if (LB == 0) low |= (uintptr_t)a.g.ldb;
+  for (int i = 0; i < a.g.nseg; ++i) {
+    low |= (uintptr_t)a.g.seg[i].a;
+    if (LB == 0) low |= (uintptr_t)a.g.seg[i].b | (uintptr_t)a.g.seg[i].b2;
+  }
+  const bool odd = KD != kF32 && (low & 3);
   auto go = [&](auto cf) {
     constexpr int CF = decltype(cf)::value;
-    few_kernel<KD, LB, NB, MFR, CF, U><<<(a.g.N + 16 * CF - 1) / (16 * CF), kThreads, 0, s>>>(a);
+    a.tiles = (a.g.N + 16 * CF - 1) / (16 * CF);
+    a.per = ((a.blocks + U - 1) / U * a.g.nseg + a.slices - 1) / a.slices;
+    const int n = a.tiles * a.slices;
+    if constexpr (KD != kF32 && CF < 4) {
+      if (odd) {
+        few_kernel<KD, LB, NB, MFR, CF, U, true><<<n, kThreads, 0, s>>>(a);
+        return;
+      }
+    }
+    few_kernel<KD, LB, NB, MFR, CF, U, false><<<n, kThreads, 0, s>>>(a);
   };
-  if constexpr (LB == 0) {
-    if constexpr (MFR * NB < 4) {
-      if (a.g.N >= 8192) return go(std::integral_constant<int, 2>{});
-    }
-    go(std::integral_constant<int, 1>{});
-  } else {
-    if constexpr (KD == kBf16 && MFR * NB == 1) {
-      if (a.g.N >= 16384) return go(std::integral_constant<int, 4>{});
-    }
-    go(std::integral_constant<int, 2>{});
+  const int cf = cols_of(KD, LB, NB, MFR, a.g.N);
+  constexpr int most = cols_of(KD, LB, NB, MFR, 1 << 20), least = cols_of(KD, LB, NB, MFR, 1);
+  if constexpr (most != least) {
+    if (cf == most && (most < 4 || !odd)) return go(std::integral_constant<int, most>{});
   }
+  go(std::integral_constant<int, least>{});
 }
 template <Kind KD, int LB, int NB>
-void launch_rows(const Args& a, hipStream_t s) {
-  if constexpr (KD != kF32) {
-    if (a.g.M > 16) return launch_cols<KD, LB, NB, 2>(a, s);
-  }
+void launch_rows(Args& a, hipStream_t s) {
+  if (a.g.M > 16) return launch_cols<KD, LB, NB, 2>(a, s);
   launch_cols<KD, LB, NB, 1>(a, s);
 }
 
+Kind kind_of(const GemmArgs& g, int dtype) { return g.i8 ? kInt8 : dtype == AX_BF16 ? kBf16 : kF32; }
+int blocks_of(const GemmArgs& g) { return (g.K + (g.i8 ? 63 : 31)) / (g.i8 ? 64 : 32); }
+
 }  // namespace
 
-hipError_t launch_few(const GemmArgs& g, int dtype, hipStream_t s) {
-  Args a;
-  a.g = g;
-  const int ks = g.i8 ? 64 : 32;
-  a.blocks = (g.K + ks - 1) / ks;
-  if (g.i8) {
-    if (g.gated) launch_rows<kInt8, 0, 2>(a, s);
-    else launch_rows<kInt8, 0, 1>(a, s);
-  } else if (dtype == AX_BF16) {
-    if (g.gated) launch_rows<kBf16, 1, 2>(a, s);
-    else if (g.lb == 0) launch_rows<kBf16, 0, 1>(a, s);
-    else launch_rows<kBf16, 1, 1>(a, s);
-  } else {
-    if (g.gated) launch_rows<kF32, 1, 2>(a, s);
-    else if (g.lb == 0) launch_rows<kF32, 0, 1>(a, s);
-    else launch_rows<kF32, 1, 1>(a, s);
+// A compute unit takes in some 18 KB a us from memory, whatever the others do, so few columns leave most of the card's rate
+// unused: the contraction is cut where the workgroups' rounds, with the launch that joins their sums, come out shorter.
+FewPlan plan_few(const GemmArgs& g, int dtype) {
+  const Kind kd = kind_of(g, dtype);
+  const int nb = g.gated ? 2 : 1, mfr = g.M > 16 ? 2 : 1, cols = 16 * cols_of(kd, g.lb, nb, mfr, g.N), steps = steps_of(kd, g.lb, nb, mfr);
+  const long long tiles = (g.N + cols - 1) / cols, groups = (long long)(blocks_of(g) + steps - 1) / steps * g.nseg;
+  const double turn = kWaves * steps * nb * (kd == kF32 ? 128.0 : 64.0) * cols / 18e3;
+  FewPlan best{1, 0};
+  double least = 1e300;
+  for (int n = 1; n <= 16 && (n == 1 || n * kWaves < groups + kWaves); ++n) {
+    const long long turns = ((groups + n - 1) / n + kWaves - 1) / kWaves;
+    const double sums = n > 1 ? 5.0 + n * nb * g.M * (double)g.N * 8.0 / 4e6 : 0.0;
+    const double cost = (double)((tiles * n + 255) / 256) * (turns * turn + 2.0) + sums;
+    if (cost < least) {
+      least = cost;
+      best.slices = n;
+    }
   }
-  return hipGetLastError();
+  if (best.slices > 1) best.part_bytes = (size_t)best.slices * nb * g.M * (((size_t)g.N + 7) / 8 * 8) * 4;
+  return best;
+}
+
+hipError_t launch_few(const GemmArgs& g, int dtype, const FewPlan& p, void* part, hipStream_t s) {
+  Args a{};
+  a.g = g;
+  a.blocks = blocks_of(g);
+  a.slices = p.slices;
+  a.part = (float*)part;
+  a.ldp = ((long long)g.N + 7) / 8 * 8;
+  switch (kind_of(g, dtype)) {
+    case kInt8: g.gated ? launch_rows<kInt8, 0, 2>(a, s) : launch_rows<kInt8, 0, 1>(a, s); break;
+    case kBf16:
+      if (g.gated) launch_rows<kBf16, 1, 2>(a, s);
+      else g.lb == 0 ? launch_rows<kBf16, 0, 1>(a, s) : launch_rows<kBf16, 1, 1>(a, s);
+      break;
+    case kF32:
+      if (g.gated) launch_rows<kF32, 1, 2>(a, s);
+      else g.lb == 0 ? launch_rows<kF32, 0, 1>(a, s) : launch_rows<kF32, 1, 1>(a, s);
+      break;
+  }
+  const hipError_t rc = hipGetLastError();
+  return rc != hipSuccess || p.slices == 1 ? rc : launch_join(g, p.slices, part, s);
 }
 
 }  // namespace ax

@@ -53,9 +53,16 @@ struct GemmPlan {
 
 GemmPlan plan_gemm(const GemmArgs& g);
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStream_t s);
+// y from the partial sums [splits][planes][M][N rounded up to 8] of the slices, with the epilogue.
+hipError_t launch_join(const GemmArgs& g, int splits, void* part, hipStream_t s);
 
 // Products of few rows straight from the operands in their own type, at any element: int8 (g.i8), or dtype AX_BF16 or
-// AX_F32.  g as above; seg holds the operands themselves, la is 0, dual is not taken.  At most 32 rows, 16 of float32.
-hipError_t launch_few(const GemmArgs& g, int dtype, hipStream_t s);
+// AX_F32.  g as above; seg holds the operands themselves, la is 0, dual is not taken.  At most 32 rows.
+struct FewPlan {
+  int slices;
+  size_t part_bytes;
+};
+FewPlan plan_few(const GemmArgs& g, int dtype);
+hipError_t launch_few(const GemmArgs& g, int dtype, const FewPlan& p, void* part, hipStream_t s);
 
 }  // namespace ax

@@ -640,8 +640,16 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStre
   } else {
     launch_tile<false, 1, 1, 1>(a, p.tile, n, s);
   }
-  hipError_t rc = hipGetLastError();
-  if (rc != hipSuccess || p.splits == 1) return rc;
+  const hipError_t rc = hipGetLastError();
+  return rc != hipSuccess || p.splits == 1 ? rc : launch_join(g, p.splits, part, s);
+}
+
+hipError_t launch_join(const GemmArgs& g, int splits, void* part, hipStream_t s) {
+  Args a{};
+  a.g = g;
+  a.splits = splits;
+  a.part = (float*)part;
+  a.ldp = part_pitch(g);
   const long long groups = (long long)(g.dual ? 2 : 1) * g.M * (a.ldp / 8);
   const int jg = (int)std::min<long long>((groups + 255) / 256, 8192);
   if (g.i8) g.gated ? gemm_join_kernel<true, true><<<jg, 256, 0, s>>>(a) : gemm_join_kernel<true, false><<<jg, 256, 0, s>>>(a);

@@ -381,24 +381,32 @@ struct Forward {
   int dtype;
   GemmArgs g;
   GemmPlan plan;
+  FewPlan few_plan;
   void* part;
   size_t bytes;
 };
 
-// Whether a product of M rows is worth launch_few: one launch that reads the weights once, against tiles with slices of the
-// contraction and the launch that adds them.  Times in us at rows / K / N, weights from memory, few : tiles.
-//   float32 (no copies in pieces)       16/2048/2048 15 : 32     1/4096/4096 29 : 71
-//   weights [N, K]                      1/4096/4096 9.7 : 17.8   24/4096/4096 14.7 : 14.9   int8 32/4096/4096 9.3 : 12.8
-//   bf16 [K, N], rows of one workgroup far apart: short contractions, or up to four rows
-//                                       1/2048/2048 6.8 : 12.4   32/2048/8192 12.9 : 13.8   16/4096/8192 21.8 : 19.1
-//                                       1/4096/4096 14.9 : 16.2  16/4096/4096 17.8 : 14.7   1/8192/2048 23.7 : 16.6
-//   int8 gated, where one launch of tiles has enough of them
-//                                       1/4096/4096 7.8 : 14.7   16/2048/6000 8.9 : 9.0     17/4096/10240 23.3 : 17.3
+// Whether a product of M rows is worth launch_few, which reads the weights once and as they lie, against tiles with slices
+// of the contraction and the launch that adds them.  A rule on the sizes alone: a view gives the bits of its copy.  Times in us
+// at rows / K / N, weights from memory, few : tiles.
+//   float32 (no copies in pieces)       1/4096/4096 20 : 71      32/2048/2048 12 : 25     32/8192/8192 78 : 224
+//   weights [N, K]                      1/4096/4096 9.6 : 17.8   24/4096/4096 14.7 : 14.9 int8 32/4096/4096 9.0 : 12.8
+//   bf16 [K, N], rows of one workgroup far apart: short contractions, small weights
+//                                       1/2048/2048 6.6 : 9.9    32/2048/8192 12.7 : 13.7
+//                                       8/4096/4096 13.8 : 14.9  16/4096/4096 14.7 : 13.7 1/4096/12288 31 : 25
+//                                       16/4096/2048 11.1 : 11.8 32/4096/1024 11.7 : 11.0 8/8192/2048 15.0 : 14.5
+//       gated                           16/4096/4096 22.6 : 24.4 32/4096/4096 23.9 : 20.8 32/4096/2048 14.3 : 14.8
+//     or rows that tiles would have laid out anew
+//                                       16/4097/4097 21 : 28     32/8191/1001 29 : 22     gated 32/8191/1001 25 : 29
+//   int8 gated, where one launch of tiles has enough of them, of rows that are read in place
+//                                       1/4096/4096 7.8 : 14.7   16/2048/6000 8.9 : 9.0   17/4096/10240 23.3 : 17.3
 bool few_fits(int dtype, bool along, bool gated, long long M, long long N, long long K) {
-  if (dtype == AX_F32) return M <= 16 && N <= 1 << 20;
   if (M > 32 || N > 1 << 20) return false;
-  if (dtype == kI8 && gated) return N <= 8192 && M * N <= 98304;
-  return along || K <= 2048 || (M <= 4 && K <= 4096);
+  if (dtype == AX_F32) return true;
+  if (dtype == kI8 && gated) return K % 16 != 0 || (N <= 8192 && M * N <= 98304);
+  if (along || K <= 2048 || (N % 8 != 0 && (gated || M <= 16))) return true;
+  const int m = (int)M / (gated ? 2 : 1);
+  return K * N <= (m <= 8 ? 1 << 24 : m <= 16 ? 1 << 23 : 0);
 }
 
 // x [M, K] times w as it lies.
@@ -430,6 +438,9 @@ Forward make_forward(const ax_matmul_desc_t* d, bool q8, bool gated, const void*
     f.g = few_args(d, q8, x, w, w2);
     f.g.gated = gated;
     f.g.ldr = d->residual_ld;
+    f.few_plan = plan_few(f.g, dt);
+    f.part = ar.take(f.few_plan.part_bytes);
+    f.bytes = ar.used;
     return f;
   }
   const Operand a = make_operand(x, d->M, d->K, d->x_ld, dt, d->unaligned, ar, &f.jobs[0]);
@@ -458,7 +469,7 @@ Forward make_forward(const ax_matmul_desc_t* d, bool q8, bool gated, const void*
 }
 
 int run_forward(Forward& f, hipStream_t s) {
-  if (f.few) return launch_few(f.g, f.dtype, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
+  if (f.few) return launch_few(f.g, f.dtype, f.few_plan, f.part, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
   const bool all[3] = {true, true, true};
   if (run_pack(f.jobs, all, f.njobs, s) != hipSuccess) return AX_ERR_HIP;
   return launch_gemm(f.g, f.plan, f.part, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
@@ -475,6 +486,7 @@ struct Backward {
   bool few;          // gx by launch_few
   GemmArgs gx, gw;
   GemmPlan px, pw;
+  FewPlan pf;
   void *partx, *partw;
   size_t bytes;
 };
@@ -541,7 +553,8 @@ Backward make_backward(const ax_matmul_desc_t* d, bool gated, const void* gy, co
   }
   gx.odt = dt;
   gx.ldy = d->x_ld;
-  if (!b.few) b.px = plan_gemm(gx);
+  if (b.few) b.pf = plan_few(gx, dt);
+  else b.px = plan_gemm(gx);
 
   GemmArgs& gw = b.gw;  // gw [K, N] = x^T gz, or [N, K] = gz^T x
   if (d->w_transposed) add_segment(&gw, oz, ox, nullptr);
@@ -555,7 +568,7 @@ Backward make_backward(const ax_matmul_desc_t* d, bool gated, const void* gy, co
   gw.ldy = d->w_ld;
   if (d->M > 0) b.pw = plan_gemm(gw);
   // one after the other on one stream: the partial sums may share their place
-  b.partx = b.partw = ar.take(std::max(b.px.part_bytes, b.pw.part_bytes));
+  b.partx = b.partw = ar.take(std::max({b.px.part_bytes, b.pf.part_bytes, b.pw.part_bytes}));
   b.bytes = ar.used;
   return b;
 }
@@ -571,6 +584,8 @@ hipError_t run_act_grad(const GradArgs& a, int row_blocks, int dtype, hipStream_
 struct FewBackward {
   OuterArgs o;
   GemmArgs gx;
+  FewPlan plan;
+  void* part;
   size_t bytes;
 };
 
@@ -610,6 +625,8 @@ FewBackward make_few_backward(const ax_matmul_desc_t* d, bool gated, const void*
   gx.ldb = d->w_ld * esz;
   gx.odt = d->dtype;
   gx.ldy = d->x_ld;
+  b.plan = plan_few(gx, d->dtype);
+  b.part = ar.take(b.plan.part_bytes);
   b.bytes = ar.used;
   return b;
 }
@@ -630,7 +647,7 @@ int run_few_backward(FewBackward& b, int dtype, bool gated, void* gx_out, void* 
   }
   if (gx_out) {
     b.gx.y = gx_out;
-    if (launch_few(b.gx, dtype, s) != hipSuccess) return AX_ERR_HIP;
+    if (launch_few(b.gx, dtype, b.plan, b.part, s) != hipSuccess) return AX_ERR_HIP;
   }
   return AX_OK;
 }
@@ -675,7 +692,7 @@ int backward_common(const ax_matmul_desc_t* d, bool gated, const void* gy, const
   }
   if (gx_out) {
     b.gx.y = gx_out;
-    if ((b.few ? launch_few(b.gx, AX_BF16, s) : launch_gemm(b.gx, b.px, b.partx, s)) != hipSuccess) return AX_ERR_HIP;
+    if ((b.few ? launch_few(b.gx, AX_BF16, b.pf, b.partx, s) : launch_gemm(b.gx, b.px, b.partx, s)) != hipSuccess) return AX_ERR_HIP;
   }
   if (gw_out) {
     b.gw.y = gw_out;
