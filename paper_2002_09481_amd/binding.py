@@ -1332,6 +1332,11 @@ class AxAdamW:
                 e.m_scale, e.v_scale = self.m_scales[i].data_ptr(), self.v_scales[i].data_ptr()
             if self.copies is not None:
                 e.copy = self.copies[i].data_ptr()
+        # states(): the tensors' places in one buffer, whole lines apart
+        self._places, self._whole = [], 0
+        for t, k in zip(self.params, sizes):
+            self._places.append((t.shape, t.stride(), self._whole))
+            self._whole += -(-k // 64) * 64
         self.set_grads(grads)
 
     def set_grads(self, grads):
@@ -1356,14 +1361,16 @@ class AxAdamW:
         _check(lib().ax_adamw(d, self._t, len(self._t), _stream_ptr(stream)))
 
     def states(self, stream=None):
-        """(m, v) as lists of float32 tensors: the values that 8-bit states stand for, or the 32-bit states themselves."""
+        """(m, v) as lists of float32 tensors: the values that 8-bit states stand for (views of one new buffer for m and one
+        for v), or the 32-bit states themselves."""
         if self.bits == 32:
             return self.m, self.v
-        out = [[torch.empty(t.shape, dtype=torch.float32, device=t.device) for t in self.params] for _ in range(2)]
-        _lend(stream, *out[0], *out[1])
-        ptrs = [(ctypes.c_void_p * len(o))(*[t.data_ptr() for t in o]) for o in out]
+        bufs = [torch.empty(self._whole, dtype=torch.float32, device=self.params[0].device) for _ in range(2)]
+        _lend(stream, *bufs)
+        ptrs = [(ctypes.c_void_p * len(self._places))(*[b.data_ptr() + 4 * at for _, _, at in self._places]) for b in bufs]
         _check(lib().ax_adamw_states(self._t, len(self._t), ptrs[0], ptrs[1], _stream_ptr(stream)))
-        return out[0], out[1]
+        m, v = ([b.as_strided(*place) for place in self._places] for b in bufs)
+        return m, v
 
 
 def ax_probe_lds_gather(width_bytes: int, pattern: int, table_bytes: int, threads: int = 1024, iters: int = 2000,
