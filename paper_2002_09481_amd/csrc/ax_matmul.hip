@@ -230,12 +230,11 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const GradArgs a) {
 
 // ---- gradients of few rows -----------------------------------------------------------------------------------------
 //
-// With at most 16 rows the weight's gradient is a sum of that many outer products: bound by writing it, no work for the
-// matrix instructions.  outer_kernel computes gz where it needs it (GATED: gg for one weight, gu for the other,
-// blockIdx.z), and leaves it and its sum over the rows for the input's gradient and the bias's: two launches in all.
-// A workgroup has 32 rows of the gradient and 512 columns, a lane eight of each; both factors come from LDS.
-// 3 x 97 x 2920 in float32: 25 us by copies and tiles, 10 so.
-constexpr int kFewBackward = 16;
+// With few rows the weight's gradient is a sum of that many outer products: bound by writing it, no work for the matrix
+// instructions.  outer_kernel computes gz where it needs it (GATED: gg for one weight, gu for the other, blockIdx.z), and
+// leaves it and its sum over the rows for the input's gradient and the bias's: two launches in all.
+// A workgroup has 32 rows of the gradient and 512 columns, a lane eight of each; both factors come from LDS, which holds
+// ROWS rows (16 or 32) of them.
 struct OuterArgs {
   const void* x;   // [M, K]
   const void* gy;  // [M, N] (GATED: gh)
@@ -247,11 +246,11 @@ struct OuterArgs {
   long long x_ld, gy_ld, gw_ld;
   int M, N, K, act, transposed;
 };
-template <int DT, bool GATED>
+template <int DT, bool GATED, int ROWS>
 __global__ __launch_bounds__(256) void outer_kernel(const OuterArgs a) {
   constexpr bool F32 = DT == AX_F32;
   constexpr int R = 32, C = 512;
-  __shared__ __align__(16) float rows[kFewBackward][R], cols[kFewBackward][C];
+  __shared__ __align__(16) float rows[ROWS][R], cols[ROWS][C];
   const int which = GATED ? blockIdx.z : 0;
   const int r0 = blockIdx.y * R, c0 = blockIdx.x * C;
   const int nr = a.transposed ? a.N : a.K, nc = a.transposed ? a.K : a.N;
@@ -589,8 +588,13 @@ struct FewBackward {
   size_t bytes;
 };
 
+// Whether the gradients are those of few rows.  Times in us of all three at rows / K / N, few : tiles.
+//   float32    8/2048/2048 22 : 39   16/97/2920 20 : 25       32/2048/2048 36 : 39   20/512/8192 28 : 49   32/97/2920 31 : 26
+//   bf16       8/2048/1000 12 : 14   16/2048/2048 17.5 : 18.3 16/2048/1000 16.4 : 14.5                     32/4096/4096 53 : 39
 bool few_backward_fits(const ax_matmul_desc_t* d) {
-  return d->M <= kFewBackward && d->K <= 1 << 20 && d->N <= 1 << 20 && few_fits(d->dtype, !d->w_transposed, false, d->M, d->K, d->N);
+  if (d->K > 1 << 20 || d->N > 1 << 20 || !few_fits(d->dtype, !d->w_transposed, false, d->M, d->K, d->N)) return false;
+  if (d->dtype == AX_F32) return d->M <= (d->K * d->N >= 1 << 20 ? 32 : 16);
+  return d->M <= (d->K * d->N >= 1 << 22 ? 16 : 12);
 }
 
 FewBackward make_few_backward(const ax_matmul_desc_t* d, bool gated, const void* gy, const void* x, const void* w,
@@ -631,6 +635,17 @@ FewBackward make_few_backward(const ax_matmul_desc_t* d, bool gated, const void*
   return b;
 }
 
+template <int DT, bool GATED>
+void run_outer(const OuterArgs& o, dim3 grid, hipStream_t s) {
+  if constexpr (DT == AX_F32) {  // (bf16 does not come with more rows)
+    if (o.M > 16) {
+      outer_kernel<DT, GATED, 32><<<grid, 256, 0, s>>>(o);
+      return;
+    }
+  }
+  outer_kernel<DT, GATED, 16><<<grid, 256, 0, s>>>(o);
+}
+
 int run_few_backward(FewBackward& b, int dtype, bool gated, void* gx_out, void* gw_out, void* gw2_out, float* gb_out, hipStream_t s) {
   OuterArgs& o = b.o;
   o.gw[0] = gw_out;
@@ -641,8 +656,8 @@ int run_few_backward(FewBackward& b, int dtype, bool gated, void* gx_out, void* 
     // without the weight's gradient, one piece of the other factor
     const int nr = o.transposed ? o.N : o.K, nc = o.transposed ? o.K : o.N;
     const dim3 grid(gw_out || !o.transposed ? (nc + 511) / 512 : 1, gw_out || o.transposed ? (nr + 31) / 32 : 1, gated ? 2 : 1);
-    if (dtype == AX_F32) gated ? outer_kernel<AX_F32, true><<<grid, 256, 0, s>>>(o) : outer_kernel<AX_F32, false><<<grid, 256, 0, s>>>(o);
-    else gated ? outer_kernel<AX_BF16, true><<<grid, 256, 0, s>>>(o) : outer_kernel<AX_BF16, false><<<grid, 256, 0, s>>>(o);
+    if (dtype == AX_F32) gated ? run_outer<AX_F32, true>(o, grid, s) : run_outer<AX_F32, false>(o, grid, s);
+    else gated ? run_outer<AX_BF16, true>(o, grid, s) : run_outer<AX_BF16, false>(o, grid, s);
     if (hipGetLastError() != hipSuccess) return AX_ERR_HIP;
   }
   if (gx_out) {

@@ -341,16 +341,26 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(const float* __restric
 
 // ---- dispatch ----------------------------------------------------------------------------------------------------
 
-// Lanes a row and passes: as few lanes as hold the row in four passes; four times as many for few rows, whose time is one row's latency
-// rather than bandwidth.
+// Lanes a row and passes of the forward kernels: as few lanes as hold the row in four passes (bandwidth), four times as many
+// for few rows, whose time is one row's latency.  Times in us of codes of bf16 rows with a residual, at rows / columns, few
+// lanes : many:  1/2048 5.0 : 3.2   1024/2048 7.8 : 6.0   4096/2048 13.4 : 14.9   16/8192 5.8 : 4.2   512/8192 9.4 : 8.7
+// 1024/8192 13.5 : 16.0.  (2049 to 4096 columns would leave half of 1024 lanes idle: 512/4096 6.2 : 6.9.)
 struct Shape {
   int tpr, nv;
 };
 Shape shape_of(long long rows, long long cols) {
-  const bool few = rows <= 512;
-  if (cols <= (few ? 512 : 2048)) return {64, (int)((cols + 511) / 512)};
-  if (cols <= (few ? 2048 : 8192)) return {256, (int)((cols + 2047) / 2048)};
+  if (cols <= (rows <= 1024 ? 512 : 2048)) return {64, (int)((cols + 511) / 512)};
+  if (cols <= (rows <= 512 ? 4096 : 8192)) return {256, (int)((cols + 2047) / 2048)};
   if (cols <= 32768) return {1024, (int)((cols + 8191) / 8192)};
+  return {1024, 0};
+}
+
+// Of the gradient, which keeps four values a column in registers: many lanes at all row counts (float32, 64 lanes a row : 256:
+// 6007/1000 20.2 : 19.3, 4096/2048 26.9 : 22.9; 256 : 1024: 4096/8192 91 : 84).
+Shape grad_shape_of(long long cols) {
+  if (cols <= 512) return {64, 1};
+  if (cols <= 4096) return {256, (int)((cols + 2047) / 2048)};
+  if (cols <= 16384) return {1024, (int)((cols + 8191) / 8192)};
   return {1024, 0};
 }
 
@@ -381,30 +391,19 @@ void norm_launch(const NormArgs& all, hipStream_t s) {
 }
 template <bool F32>
 void norm_grad_launch(const NormGradArgs& a, const Shape& sh, int groups, hipStream_t s) {
-  const int threads = sh.tpr < 256 ? 256 : sh.tpr;
-#define AX_NG(T, V) norm_grad_kernel<F32, T, V><<<groups, threads, 0, s>>>(a)
-#define AX_NG_T(T)                           \
-  switch (sh.nv) {                           \
-    case 1: AX_NG(T, 1); break;              \
-    case 2: AX_NG(T, 2); break;              \
-    default: AX_NG(T, 4); break;             \
-  }
-  if (sh.tpr == 64) AX_NG_T(64)
-  else if (sh.tpr == 256) AX_NG_T(256)
-  else if (sh.nv == 1) AX_NG(1024, 1);
-  else AX_NG(1024, 2);
-#undef AX_NG_T
-#undef AX_NG
+  if (sh.tpr == 64) norm_grad_kernel<F32, 64, 1><<<groups, 256, 0, s>>>(a);
+  else if (sh.tpr == 256) sh.nv == 1 ? norm_grad_kernel<F32, 256, 1><<<groups, 256, 0, s>>>(a) : norm_grad_kernel<F32, 256, 2><<<groups, 256, 0, s>>>(a);
+  else sh.nv == 1 ? norm_grad_kernel<F32, 1024, 1><<<groups, 1024, 0, s>>>(a) : norm_grad_kernel<F32, 1024, 2><<<groups, 1024, 0, s>>>(a);
 }
 
-// The gradient keeps four values a column in registers: 1024 lanes hold 16384 columns.
-bool grad_is_long(const Shape& sh) { return sh.nv == 0 || (sh.tpr == 1024 && sh.nv > 2); }
-
+// Workgroups of the gradient, each with a row of sums to be added afterwards: four rows each (us with one, two, four and eight,
+// 1024/2048: 16.1, 11.9, 12.3, 14.3; 512/8192: 24.1, 18.1, 17.4, 17.2), and no fewer than 128 while there are rows.
 int grad_groups(long long rows, long long cols) {
-  const Shape sh = shape_of(rows, cols);
-  if (grad_is_long(sh)) return (int)std::min<long long>(rows, 64);
-  const long long per = sh.tpr == 64 ? 4 : 1;
-  return (int)std::min<long long>((rows + per - 1) / per, sh.tpr == 1024 ? 512 : 1024);
+  const Shape sh = grad_shape_of(cols);
+  if (sh.nv == 0) return (int)std::min<long long>(rows, 64);
+  const long long most = sh.tpr == 1024 ? 512 : 1024;
+  const long long least = sh.tpr == 64 ? 1 : std::min<long long>(rows, 128);
+  return (int)std::min(most, std::max((rows + 3) / 4, least));
 }
 
 int check_norm(const ax_norm_desc_t* d) {
@@ -526,9 +525,9 @@ extern "C" int ax_rmsnorm_backward(const ax_norm_desc_t* d, const void* gy, cons
   a.cols = (int)d->cols;
   a.w_f32 = d->w_dtype == AX_F32;
   const bool f32 = d->dtype == AX_F32;
-  const Shape sh = shape_of(d->rows, d->cols);
+  const Shape sh = grad_shape_of(d->cols);
   const int groups = grad_groups(d->rows, d->cols);
-  if (grad_is_long(sh)) {
+  if (sh.nv == 0) {
     if (gx_out) {
       for (a.row0 = 0; a.row0 < a.rows; a.row0 += kMaxGrid) {
         const unsigned grid = (unsigned)std::min<long long>(a.rows - a.row0, kMaxGrid);

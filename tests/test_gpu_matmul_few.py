@@ -94,3 +94,23 @@ def test_gated_input_gradient(M, K, N, dt):
         want = want + p @ w.double().t()
         bound = bound + one @ w.double().abs().t() + p.abs() @ w.double().abs().t() * F.sum_bound(2 * N, dt == "f32")
     F.assert_within(gx, want, bound + want.abs() * F.store(dtype), "gx")
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(12, 2048, 40), (13, 70, 300), (16, 2048, 2048), (17, 1030, 1021), (32, 1024, 1024), (31, 513, 2100), (33, 1024, 1030)])
+def test_gradients(M, K, N, dt, transposed):
+    dtype, g = F.DT[dt], F.gen(M + 5 * K + N)
+    x, w = F.randn(g, (M, K), 1.0, dtype), F.randn(g, (N, K) if transposed else (K, N), K ** -0.5, dtype)
+    gy, z = F.randn(g, (M, N), 1.0, dtype), F.randn(g, (M, N), 1.5, dtype)
+    wd = w.double().t() if transposed else w.double()
+    gz = gy.double() * F.slope(z.double(), "silu")
+    gx, gw, gb = ax.ax_matmul_backward(gy.cuda(), x.cuda(), w.cuda(), z.cuda(), act="silu", transposed=transposed)
+    one = 24 * F.U * gy.double().abs() + (gz.abs() * 2.0 ** -8 if dt == "bf16" else 0)
+    want = gz @ wd.t()
+    F.assert_within(gx, want, one @ wd.t().abs() + gz.abs() @ wd.t().abs() * F.sum_bound(N, dt == "f32") + want.abs() * F.store(dtype), "gx")
+    xt = x.double().t()
+    want, bound = xt @ gz, xt.abs() @ one + xt.abs() @ gz.abs() * F.sum_bound(M, dt == "f32")
+    bound = bound + want.abs() * F.store(dtype)
+    F.assert_within(gw, want.t() if transposed else want, bound.t() if transposed else bound, "gw")
+    F.assert_within(gb, gz.sum(dim=0), (24 * F.U * gy.double().abs()).sum(dim=0) + gz.abs().sum(dim=0) * (M / 8 + 80) * F.U, "gb")
