@@ -485,10 +485,9 @@ size_t ax_matmul_q8_workspace_bytes(const ax_matmul_desc_t* desc);
  * Gradients of ax_matmul (of its residual: gy itself).  With gz = gy * act'(z), act'(0) = 0 for relu:
  *   gx_out [M, K] = gz w^T     gw_out (the shape and pitch of w) = x^T gz     gb_out [N] float32 = sum of gz
  * gy and z [M, N] have the type desc->dtype and the pitches y_ld and N; gx_out (pitch x_ld) and gw_out
- * (pitch w_ld) too; desc->out_dtype must be desc->dtype.  z may be NULL where act is AX_ACT_NONE.  bf16: gz is rounded to bf16
- * for the two products (their matrix instructions take 16-bit operands), not for gb_out, nor for
- * gw_out of at most 16 rows.  Any output
- * may be NULL (not all).  workspace: ax_matmul_backward_workspace_bytes(desc) bytes.
+ * (pitch w_ld) too; desc->out_dtype must be desc->dtype.  z may be NULL where act is AX_ACT_NONE.  bf16: gz is
+ * rounded to bf16 for the two products (their matrix instructions take 16-bit operands), not for gb_out, nor
+ * for gw_out of at most 12 rows (16 where K N >= 2^22).  Any output may be NULL (not all).  workspace: ax_matmul_backward_workspace_bytes(desc) bytes.
  */
 int ax_matmul_backward(const ax_matmul_desc_t* desc, const void* gy, const void* x, const void* w,
                        const void* z, void* gx_out, void* gw_out, float* gb_out, void* workspace,

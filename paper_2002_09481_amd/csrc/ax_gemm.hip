@@ -1,4 +1,15 @@
 // Matrix products on the matrix cores: bf16 operands with float32 sums, int8 codes with int32 sums.
+//
+// A workgroup computes a tile of the result, 256 x 256 where the product is large: the two operands' parts of a stage meet
+// 256 times each, so that memory and L2 keep up.  Copies go from memory to LDS past the registers; LDS is laid out so that
+// neither plain nor transposing reads meet in a bank, which lets every operand be read as it lies.  Bound, large products: by
+// the power that the card draws with random operands (the matrix cores are busy 65 % of the time; zeros for operands run 1.2
+// times as fast, and so does the library's product of them).  Smaller ones: rounds of tiles that leave compute units idle,
+// and each tile's first stage and stores, during which nothing multiplies.
+//
+// Measured (us): bf16 8192^3 840 to 930 (1180 to 1310 TF), 4096^3 103 (1340 TF), gradient of a weight 8192^3 780 (1400 TF);
+// gated 8192 x 4096 -> 16384 with both projections stored 1735 to 1800 (1220 to 1270 TF); int8 8192^3 520 (2100 TOP);
+// float32 4096^3 583 (236 TF, six products each).
 #include <algorithm>
 #include <type_traits>
 
@@ -498,7 +509,8 @@ __device__ __forceinline__ f32x4 sum_slices(const float* p, long long step, int 
   return __builtin_bit_cast(f32x4, t);
 }
 
-// Partial sums of the slices, added in their order, and the epilogue: eight columns a thread.
+// Partial sums of the slices, added in their order, and the epilogue: eight columns a thread.  Bound by memory, a launch's
+// latency where the sums are few (333 x 2048 in five slices 5 us, 4101 x 2048 in three 29).
 template <bool I8, bool GATED>
 __global__ __launch_bounds__(256) void gemm_join_kernel(const Args a) {
   const GemmArgs& g = a.g;

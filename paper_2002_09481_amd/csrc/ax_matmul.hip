@@ -52,7 +52,8 @@ struct PackJob {
 constexpr int kI8 = 2;
 
 // Rows copied into the form the products read: eight elements (16 bytes of output; int8: 16) a thread, all the operands of a
-// product in one launch.  Bound by memory: 4 bytes read and 6 written per float32 element.
+// product in one launch.  Bound by memory: 4 bytes read and 6 written per float32 element (28 M of them 45 us, 6.3 TB/s with
+// part of it in the caches).
 struct PackBatch {
   PackJob job[3];
   int first[3];  // workgroup that each job starts at
@@ -160,7 +161,8 @@ void add_segment(GemmArgs* g, const Operand& a, const Operand& b, const Operand*
 // ---- elementwise part of the gradients ---------------------------------------------------------------------------
 //
 // gz = gy act'(z) (GATED: gg and gu) in the form the products read, and the sums of gz over blocks of rows.  A
-// workgroup takes 256 columns (eight a thread) and `rows_per` rows, eight at a time.  Bound by memory.
+// workgroup takes 256 columns (eight a thread) and `rows_per` rows, eight at a time.  Bound by memory: gated, 4101 x 5512
+// bf16, 226 MB in 46 us, 4.9 TB/s.
 struct GradArgs {
   const void* gy;  // [M, N], pitch ldy (GATED: gh)
   const void* z;   // [M, N], pitch N (may be NULL; GATED: the gate projection)
@@ -234,7 +236,7 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const GradArgs a) {
 // instructions.  outer_kernel computes gz where it needs it (GATED: gg for one weight, gu for the other, blockIdx.z), and
 // leaves it and its sum over the rows for the input's gradient and the bias's: two launches in all.
 // A workgroup has 32 rows of the gradient and 512 columns, a lane eight of each; both factors come from LDS, which holds
-// ROWS rows (16 or 32) of them.
+// ROWS rows (16 or 32) of them.  3 x 97 x 2920 float32: 5 us, of 8 x 616 x 11679 gated bf16 both 19.
 struct OuterArgs {
   const void* x;   // [M, K]
   const void* gy;  // [M, N] (GATED: gh)
