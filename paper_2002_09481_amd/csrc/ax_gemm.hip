@@ -3,8 +3,8 @@
 // A workgroup computes a tile of the result, 256 x 256 where the product is large: the two operands' parts of a stage meet
 // 256 times each, so that memory and L2 keep up.  Copies go from memory to LDS past the registers; LDS is laid out so that
 // neither plain nor transposing reads meet in a bank, which lets every operand be read as it lies.  Bound, large products: by
-// the power that the card draws with random operands (the matrix cores are busy 65 % of the time; zeros for operands run 1.2
-// times as fast, and so does the library's product of them).  Smaller ones: rounds of tiles that leave compute units idle,
+// the power that the card draws with random operands (the matrix cores are busy 65 % of the time; with zeros for operands
+// the same product takes 692 us instead of 843).  Smaller ones: rounds of tiles that leave compute units idle,
 // and each tile's first stage and stores, during which nothing multiplies.
 //
 // Measured (us): bf16 8192^3 840 to 930 (1180 to 1310 TF), 4096^3 103 (1340 TF), gradient of a weight 8192^3 780 (1400 TF);
@@ -549,9 +549,12 @@ constexpr TileShape kTiles[kNumTiles] = {{256, 256, 128, 1, 6.0, 1.50, 1.50},
                                          {128, 128, 128, 2, 3.0, 0.70, 0.95},
                                          {64, 128, 128, 2, 2.5, 0.39, 0.65},
                                          {32, 128, 128, 2, 2.0, 0.30, 0.45}};
-// float32 operands (three pieces; six products in the time)
+// float32 operands (three pieces; six products in the time).  Two of the small ones in a compute unit that read both operands
+// along the contraction: kStep3Along (1531 x 1000 -> 2048: 54.8 us a call with the large tile, 60.7 with the small one; 2000 x
+// 2048 -> 2048 101.8 and 121.6).
 constexpr int kNumTiles3 = 2;
 constexpr TileShape kTiles3[kNumTiles3] = {{128, 128, 64, 1, 5.0, 2.1, 2.1}, {64, 128, 64, 2, 4.0, 1.25, 2.1}};
+constexpr double kStep3Along = 2.6;
 
 template <bool I8, int LA, int LB, int NB>
 void launch_tile(const Args& a, int tile, int grid, hipStream_t s) {
@@ -600,6 +603,7 @@ GemmPlan plan_gemm(const GemmArgs& g) {
     if (T.bm == 32 && g.la != 0) continue;
     const long long steps = (kbytes + T.kb - 1) / T.kb * g.nseg;
     const long long tiles = tiles_of(g, T);
+    const double step = three && t == 1 && g.la == 0 && g.lb == 0 ? kStep3Along : T.step;
     if (t > 0 && tiles > kMaxGrid) continue;
     for (int sp = 1; sp <= kMaxSplits && (sp == 1 || sp * 2 <= steps); ++sp) {
       if (sp > 1 && tiles * sp > kMaxGrid) break;
@@ -607,8 +611,8 @@ GemmPlan plan_gemm(const GemmArgs& g) {
       const long long full = n / slots, rest = n - full * slots;
       const double stages = (double)((steps + sp - 1) / sp) * T.kb / 128;
       const double fixed = T.fixed + (sp > 1 ? T.bm * T.bn * 4 / 20e3 : 0);  // (sums leave a compute unit at 20 KB a us)
-      double cost = full * (fixed + stages * T.step);
-      if (rest) cost += fixed + stages * (rest <= kCus ? T.step1 : T.step);
+      double cost = full * (fixed + stages * step);
+      if (rest) cost += fixed + stages * (rest <= kCus ? T.step1 : step);
       if (sp > 1) cost += 3.0 + sp * outs * g.M * (double)g.N * 8.0 / 6.5e6;
       if (cost < least) {
         least = cost;
