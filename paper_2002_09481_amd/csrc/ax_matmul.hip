@@ -60,12 +60,12 @@ struct PackBatch {
   int blocks[3];
 };
 template <int DT>
-__global__ __launch_bounds__(256) void pack_kernel(const PackBatch b) {
+__device__ __forceinline__ void pack_rows(const PackBatch& b, int block) {
   constexpr int E = DT == kI8 ? 16 : 8;
-  const int k = (int)blockIdx.x >= b.first[2] ? 2 : (int)blockIdx.x >= b.first[1] ? 1 : 0;
+  const int k = block >= b.first[2] ? 2 : block >= b.first[1] ? 1 : 0;
   const PackJob& j = b.job[k];
   const long long groups = j.pcols / E, total = j.rows * groups;
-  for (long long i = (long long)(blockIdx.x - b.first[k]) * 256 + threadIdx.x; i < total; i += (long long)b.blocks[k] * 256) {
+  for (long long i = (long long)(block - b.first[k]) * 256 + threadIdx.x; i < total; i += (long long)b.blocks[k] * 256) {
     const long long r = i / groups, c = (i - r * groups) * E;
     const long long left = j.cols - c;
     if (DT == AX_F32) {
@@ -95,22 +95,30 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackBatch b) {
   }
 }
 
+template <int DT>
+__global__ __launch_bounds__(256) void pack_kernel(const PackBatch b) {
+  pack_rows<DT>(b, blockIdx.x);
+}
+
 int grid_for(long long items) { return (int)std::max<long long>(1, std::min<long long>((items + 255) / 256, 8192)); }
 
-// The jobs of an operation that have something to copy (wanted[i]: whether job i is needed by this call).
-hipError_t run_pack(const PackJob* jobs, const bool* wanted, int n, hipStream_t s) {
-  PackBatch b{};
+// The jobs of an operation that have something to copy (wanted[i]: whether job i is needed by this call); returns the
+// workgroups that they take.
+int fill_pack(PackBatch* b, const PackJob* jobs, const bool* wanted, int n) {
   int k = 0, grid = 0;
-  for (int i = 0; i < 3; ++i) b.first[i] = 0x7fffffff;
+  for (int i = 0; i < 3; ++i) b->first[i] = 0x7fffffff;
   for (int i = 0; i < n; ++i) {
     const PackJob& j = jobs[i];
     if (!wanted[i] || !j.dst || j.rows == 0) continue;
-    b.job[k] = j;
-    b.first[k] = grid;
-    b.blocks[k] = grid_for(j.rows * (j.pcols / (j.dtype == kI8 ? 16 : 8)));
-    grid += b.blocks[k++];
+    b->job[k] = j;
+    b->first[k] = grid;
+    b->blocks[k] = grid_for(j.rows * (j.pcols / (j.dtype == kI8 ? 16 : 8)));
+    grid += b->blocks[k++];
   }
-  if (k == 0) return hipSuccess;
+  return grid;
+}
+hipError_t run_pack(const PackBatch& b, int grid, hipStream_t s) {
+  if (grid == 0) return hipSuccess;
   const int dtype = b.job[0].dtype;  // the same for all operands of an operation
   if (dtype == AX_F32) pack_kernel<AX_F32><<<grid, 256, 0, s>>>(b);
   else if (dtype == AX_BF16) pack_kernel<AX_BF16><<<grid, 256, 0, s>>>(b);
@@ -172,6 +180,7 @@ struct GradArgs {
   float* part;     // [row blocks][N] (may be NULL)
   long long ldy, pcols, pitch;  // pcols, pitch: of gz and gu
   int M, N, act, rows_per;
+  int wide, blocks;  // workgroups along the columns, in all
 };
 
 template <int DT>
@@ -187,11 +196,18 @@ __device__ __forceinline__ void write_planes(void* dst, long long rows, long lon
   }
 }
 
+// The copies that the products need as well come in the same launch, behind: neither waits for the other (us of all gradients
+// at rows / K / N, together : in two launches: bf16 64/501/701 17.8 : 20.0, float32 333/2001/1003 48.0 : 51.9).
 template <int DT, bool GATED>
-__global__ __launch_bounds__(256) void act_grad_kernel(const GradArgs a) {
+__global__ __launch_bounds__(256) void act_grad_kernel(const GradArgs a, const PackBatch copies) {
+  if ((int)blockIdx.x >= a.blocks) {
+    pack_rows<DT>(copies, blockIdx.x - a.blocks);
+    return;
+  }
+  const int by = blockIdx.x / a.wide, bx = blockIdx.x - by * a.wide;
   const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
-  const long long c = ((long long)blockIdx.x * 32 + cx) * 8;
-  const int r0 = blockIdx.y * a.rows_per, r1 = min(a.M, r0 + a.rows_per);
+  const long long c = ((long long)bx * 32 + cx) * 8;
+  const int r0 = by * a.rows_per, r1 = min(a.M, r0 + a.rows_per);
   const int left = (int)max(0ll, min(8ll, a.N - c));
   float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   if (c < a.pcols) {
@@ -223,11 +239,11 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const GradArgs a) {
   for (int e = 0; e < 8; ++e) red[ry][cx][e] = sum[e];
   __syncthreads();
   const int x = threadIdx.x >> 3, e = threadIdx.x & 7;
-  const long long col = ((long long)blockIdx.x * 32 + x) * 8 + e;
+  const long long col = ((long long)bx * 32 + x) * 8 + e;
   if (col >= a.N) return;
   float t = 0.f;
   for (int y = 0; y < 8; ++y) t += red[y][x][e];
-  a.part[(long long)blockIdx.y * a.N + col] = t;
+  a.part[(long long)by * a.N + col] = t;
 }
 
 // ---- gradients of few rows -----------------------------------------------------------------------------------------
@@ -472,7 +488,9 @@ Forward make_forward(const ax_matmul_desc_t* d, bool q8, bool gated, const void*
 int run_forward(Forward& f, hipStream_t s) {
   if (f.few) return launch_few(f.g, f.dtype, f.few_plan, f.part, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
   const bool all[3] = {true, true, true};
-  if (run_pack(f.jobs, all, f.njobs, s) != hipSuccess) return AX_ERR_HIP;
+  PackBatch copies{};
+  const int copy_blocks = fill_pack(&copies, f.jobs, all, f.njobs);
+  if (run_pack(copies, copy_blocks, s) != hipSuccess) return AX_ERR_HIP;
   return launch_gemm(f.g, f.plan, f.part, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
 }
 
@@ -533,6 +551,8 @@ Backward make_backward(const ax_matmul_desc_t* d, bool gated, const void* gy, co
   b.ga.act = d->act;
   b.ga.rows_per = rows_per_block((int)d->M, (int)d->N);
   b.row_blocks = (int)((d->M + b.ga.rows_per - 1) / b.ga.rows_per);
+  b.ga.wide = (int)((pcols + 255) / 256);
+  b.ga.blocks = b.ga.wide * b.row_blocks;
   if (!gated) b.part = (float*)ar.take((size_t)b.row_blocks * d->N * 4);
 
   GemmArgs& gx = b.gx;  // gx [M, K] = gz [M, N] w^T
@@ -575,10 +595,10 @@ Backward make_backward(const ax_matmul_desc_t* d, bool gated, const void* gy, co
 }
 
 template <bool GATED>
-hipError_t run_act_grad(const GradArgs& a, int row_blocks, int dtype, hipStream_t s) {
-  const dim3 grid((unsigned)((a.pcols + 255) / 256), (unsigned)row_blocks);
-  if (dtype == AX_F32) act_grad_kernel<AX_F32, GATED><<<grid, 256, 0, s>>>(a);
-  else act_grad_kernel<AX_BF16, GATED><<<grid, 256, 0, s>>>(a);
+hipError_t run_act_grad(const GradArgs& a, const PackBatch& copies, int copy_blocks, int dtype, hipStream_t s) {
+  const int grid = a.blocks + copy_blocks;
+  if (dtype == AX_F32) act_grad_kernel<AX_F32, GATED><<<grid, 256, 0, s>>>(a, copies);
+  else act_grad_kernel<AX_BF16, GATED><<<grid, 256, 0, s>>>(a, copies);
   return hipGetLastError();
 }
 
@@ -696,16 +716,19 @@ int backward_common(const ax_matmul_desc_t* d, bool gated, const void* gy, const
   const bool products = gx_out || gw_out;
   const bool weights = gx_out && !b.few;
   const bool wanted[3] = {gw_out != nullptr, weights, weights && gated};
-  if (run_pack(b.jobs, wanted, 3, s) != hipSuccess) return AX_ERR_HIP;
+  PackBatch copies{};
+  const int copy_blocks = fill_pack(&copies, b.jobs, wanted, 3);
   if (gated) {
-    if (run_act_grad<true>(b.ga, b.row_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
+    if (run_act_grad<true>(b.ga, copies, copy_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
   } else if ((b.elementwise && products) || gb_out) {
     if (!products) b.ga.gz = nullptr;
     b.ga.part = gb_out ? b.part : nullptr;
-    if (run_act_grad<false>(b.ga, b.row_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
+    if (run_act_grad<false>(b.ga, copies, copy_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
     if (gb_out) {
       if (launch_column_sum(b.part, b.row_blocks, (int)d->N, gb_out, s) != hipSuccess) return AX_ERR_HIP;
     }
+  } else if (run_pack(copies, copy_blocks, s) != hipSuccess) {
+    return AX_ERR_HIP;
   }
   if (gx_out) {
     b.gx.y = gx_out;
