@@ -6,6 +6,8 @@
 // waves' sums meet in LDS, in the waves' order, and the epilogue follows there: one launch, no partial sums in memory.  Only
 // where the columns would leave compute units idle is the contraction cut, and a second launch joins the slices' sums.
 //
+// More than 32 rows (16 in one fragment) are several workgroups, neighbours, so that one reads what the other has brought to L2.
+//
 // Measured, weights from memory (us at rows / K / N): bf16 [N, K] 1/4096/4096 9.6 (3.5 TB/s), [K, N] 1/2048/8192 10.3
 // (3.3 TB/s), float32 [K, N] 17/8192/8192 71.5 (3.75 TB/s); slices: float32 [K, N] 16/8192/512 13.5, uncut 45.
 //
@@ -31,6 +33,7 @@ struct Args {
   GemmArgs g;
   int blocks;   // of the contraction, per segment
   int tiles;    // workgroups along the columns
+  int bands;    // of 16 MFR rows
   int slices;   // of the contraction, each `per` turns of a wave (over all segments)
   int per;
   float* part;  // [slices][NB][M][ldp] with slices, as the joining kernel reads them
@@ -169,10 +172,15 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
   const int t = threadIdx.x, lane = t & 63, r = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   // workgroups b, b + 8, ... share an XCD: they take neighbouring columns, which may share lines of memory
-  int tile, slice;
+  int tile, slice, m0 = 0;
   {
     const int b = blockIdx.x, x = b & 7, i = b >> 3, total = gridDim.x, per = total >> 3, more = total & 7;
     tile = x * per + min(x, more) + i;
+    if (a.bands > 1) {  // neighbours: the weights come from memory once
+      const int band = tile % a.bands;
+      tile /= a.bands;
+      m0 = band * 16 * MFR;
+    }
     slice = a.slices > 1 ? tile / a.tiles : 0;
     tile -= slice * a.tiles;
   }
@@ -214,7 +222,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
           }
         }
 #pragma unroll
-        for (int i = 0; i < MFR; ++i) xa[u][i].template load<full>(x + min(16 * i + r, g.M - 1) * g.lda, k, left);
+        for (int i = 0; i < MFR; ++i) xa[u][i].template load<full>(x + min(m0 + 16 * i + r, g.M - 1) * g.lda, k, left);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -250,7 +258,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
       }
   __syncthreads();
   for (int o = t; o < 16 * MFR * COLS; o += kThreads) {
-    const int m = o / COLS, c = o - m * COLS, n = n0 + c;
+    const int row = o / COLS, c = o - row * COLS, m = m0 + row, n = n0 + c;
     if (m >= g.M || n >= g.N) continue;
     float s[2];
 #pragma unroll
@@ -258,12 +266,12 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
       if (KD == kInt8) {
         int32_t v = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) v += __float_as_int(part[w][b][m][c]);
+        for (int w = 0; w < kWaves; ++w) v += __float_as_int(part[w][b][row][c]);
         s[b] = a.slices > 1 ? __int_as_float(v) : (float)v * (g.xs[m] * (b ? g.ws2 : g.ws)[n]);
       } else {
         float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) v += part[w][b][m][c];
+        for (int w = 0; w < kWaves; ++w) v += part[w][b][row][c];
         s[b] = v;
       }
     }
@@ -315,8 +323,9 @@ void launch_cols(Args& a, hipStream_t s) {
   auto go = [&](auto cf) {
     constexpr int CF = decltype(cf)::value;
     a.tiles = (a.g.N + 16 * CF - 1) / (16 * CF);
+    a.bands = (a.g.M + 16 * MFR - 1) / (16 * MFR);
     a.per = ((a.blocks + U - 1) / U * a.g.nseg + a.slices - 1) / a.slices;
-    const int n = a.tiles * a.slices;
+    const int n = a.tiles * a.slices * a.bands;
     if constexpr (KD != kF32 && CF < 4) {
       if (odd) {
         few_kernel<KD, LB, NB, MFR, CF, U, true><<<n, kThreads, 0, s>>>(a);
@@ -350,8 +359,8 @@ int blocks_of(const GemmArgs& g) { return (g.K + (g.i8 ? 63 : 31)) / (g.i8 ? 64 
 FewPlan plan_few(const GemmArgs& g, int dtype) {
   const Kind kd = kind_of(g, dtype);
   const int nb = g.gated ? 2 : 1, mfr = g.M > 16 ? 2 : 1, cols = 16 * cols_of(kd, g.lb, nb, mfr, g.N), steps = steps_of(kd, g.lb, nb, mfr);
-  const long long tiles = (g.N + cols - 1) / cols, groups = (long long)(blocks_of(g) + steps - 1) / steps * g.nseg;
-  const double turn = kWaves * steps * (kd == kF32 ? 128.0 : 64.0) * (nb * cols + 0.5 * g.M) / 18e3;  // (x from the caches)
+  const long long tiles = (long long)((g.N + cols - 1) / cols) * ((g.M + 16 * mfr - 1) / (16 * mfr)), groups = (long long)(blocks_of(g) + steps - 1) / steps * g.nseg;
+  const double turn = kWaves * steps * (kd == kF32 ? 128.0 : 64.0) * (nb * cols + 0.5 * std::min(g.M, 32)) / 18e3;  // (x from the caches)
   FewPlan best{1, 0};
   double least = 1e300;
   for (int n = 1; n <= 16 && (n == 1 || n * kWaves < groups + kWaves); ++n) {

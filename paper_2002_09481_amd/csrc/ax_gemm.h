@@ -57,7 +57,7 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStre
 hipError_t launch_join(const GemmArgs& g, int splits, void* part, hipStream_t s);
 
 // Products of few rows straight from the operands in their own type, at any element: int8 (g.i8), or dtype AX_BF16 or
-// AX_F32.  g as above; seg holds the operands themselves, la is 0, dual is not taken.  At most 32 rows.
+// AX_F32.  g as above; seg holds the operands themselves, la is 0, dual is not taken.  Meant for up to 64 rows.
 struct FewPlan {
   int slices;
   size_t part_bytes;

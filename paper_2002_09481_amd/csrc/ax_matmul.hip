@@ -407,6 +407,9 @@ struct Forward {
 // of the contraction and the launch that adds them.  A rule on the sizes alone: a view gives the bits of its copy.  Times in us
 // at rows / K / N, weights from memory, few : tiles.
 //   float32 (no copies in pieces)       1/4096/4096 20 : 71      32/2048/2048 12 : 25     32/8192/8192 78 : 224
+//                                       64/2048/2048 15 : 25     64/8192/8192 133 : 231   96/512/8192 gated 39 : 32
+//       [N, K]                          64/2048/2048 17 : 26     64/8192/8192 202 : 261   96/2048/2048 31 : 26
+//       [N, K], rows off 16 bytes       32/4097/4097 56 : 57     64/4097/4097 95 : 57
 //   weights [N, K]                      1/4096/4096 9.6 : 17.8   24/4096/4096 14.7 : 14.9 int8 32/4096/4096 9.0 : 12.8
 //   bf16 [K, N], rows of one workgroup far apart: short contractions, small weights
 //                                       1/2048/2048 6.6 : 9.9    32/2048/8192 12.7 : 13.7
@@ -418,8 +421,8 @@ struct Forward {
 //   int8 gated, where one launch of tiles has enough of them, of rows that are read in place
 //                                       1/4096/4096 7.8 : 14.7   16/2048/6000 8.9 : 9.0   17/4096/10240 23.3 : 17.3
 bool few_fits(int dtype, bool along, bool gated, long long M, long long N, long long K) {
-  if (M > 32 || N > 1 << 20) return false;
-  if (dtype == AX_F32) return true;
+  if (M > (dtype == AX_F32 ? 64 : 32) || N > 1 << 20) return false;
+  if (dtype == AX_F32) return M <= 32 || !along || K % 4 == 0;
   if (dtype == kI8 && gated) return K % 16 != 0 || (N <= 8192 && M * N <= 98304);
   if (along || K <= 2048 || (N % 8 != 0 && (gated || M <= 16))) return true;
   const int m = (int)M / (gated ? 2 : 1);

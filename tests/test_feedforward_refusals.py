@@ -95,9 +95,9 @@ def test_products_of_codes():
 
 def test_product_pointers():
     L = ax.lib()
-    d = mm(M=40, dtype=0, out_dtype=0)  # float32 operands go through the workspace (of more than a few rows)
+    d = mm(M=72, dtype=0, out_dtype=0)  # float32 operands go through the workspace (of more than a few rows)
     need = L.ax_matmul_workspace_bytes(R(d))
-    assert need >= 3 * 2 * (40 * 32 + 32 * 64)
+    assert need >= 3 * 2 * (72 * 32 + 32 * 64)
     assert L.ax_matmul(R(d), P, P, P, P, P, P, P, need - 1, None) == -5 and L.ax_matmul(R(d), P, P, P, P, P, P, None, need, None) == -5
     assert L.ax_matmul(R(d), P, P, P, P, P, P, ctypes.c_void_p(4096 + 64), need, None) == -5
     assert L.ax_matmul(None, P, P, P, P, P, P, P, need, None) == -1

@@ -114,3 +114,24 @@ def test_gradients(M, K, N, dt, transposed):
     bound = bound + want.abs() * F.store(dtype)
     F.assert_within(gw, want.t() if transposed else want, bound.t() if transposed else bound, "gw")
     F.assert_within(gb, gz.sum(dim=0), (24 * F.U * gy.double().abs()).sum(dim=0) + gz.abs().sum(dim=0) * (M / 8 + 80) * F.U, "gb")
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("M,K,N", [(33, 512, 130), (48, 6000, 64), (63, 333, 1001), (64, 2052, 96), (64, 2051, 96), (65, 512, 64)])
+def test_bands_of_rows(M, K, N, transposed):
+    """float32 rows of several workgroups, with and without slices; one row more goes through tiles."""
+    g = F.gen(M + K + N)
+    x, w, w2 = F.randn(g, (M, K)), F.randn(g, (N, K) if transposed else (K, N), K ** -0.5), F.randn(g, (K, N), K ** -0.5)
+    r, wd = F.randn(g, (M, N)), w.double().t() if transposed else w.double()
+    zd, zb = x.double() @ wd, x.double().abs() @ wd.abs() * F.sum_bound(K, True)
+    y, z = ax.ax_matmul(x.cuda(), w.cuda(), residual=r.cuda(), act="silu", transposed=transposed, save=True)
+    F.assert_within(z, zd, zb + zd.abs() * F.store(torch.float32), "z")
+    yd, bound = _bound(zd, zb, "silu", torch.float32)
+    yd = yd + r.double()
+    F.assert_within(y, yd, bound + 2 * F.U * (yd.abs() + r.double().abs()) + yd.abs() * F.store(torch.float32), "y")
+    if not transposed:
+        ud, ub = x.double() @ w2.double(), x.double().abs() @ w2.double().abs() * F.sum_bound(K, True)
+        h, _, u = ax.ax_gated(x.cuda(), w.cuda(), w2.cuda(), act="silu", save=True)
+        F.assert_within(u, ud, ub + ud.abs() * F.store(torch.float32), "u")
+        ad, ab = _bound(zd, zb, "silu", torch.float32)
+        F.assert_within(h, ad * ud, ab * (ud.abs() + ub) + ad.abs() * ub + (ad * ud).abs() * (2 * F.U + F.store(torch.float32)), "h")
