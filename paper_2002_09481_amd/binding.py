@@ -1055,13 +1055,13 @@ def ax_rmsnorm_backward(gy, t, weight, rstd, gsum=None, gx_out=None, gw_out=None
     return gx_out, gw_out
 
 
-def _matmul_desc(x, w, act, transposed, out_dtype, aligned, names=("x", "w")) -> ax_matmul_desc_t:
+def _matmul_desc(x, w, act, transposed, out_dtype, aligned, names=("x", "w"), codes=False) -> ax_matmul_desc_t:
+    dt = AX_BF16 if codes else _float_dtype(x, names[0])  # (of codes the library does not look at it)
     M, K, x_ld = _mat(x, x.dtype, names[0])
     wr, wc, w_ld = _mat(w, x.dtype, names[1])
     if w.dim() != 2 or (wc if transposed else wr) != K:
         raise ValueError("%s must be %s for %s [M,K]" % (names[1], "[N,K]" if transposed else "[K,N]", names[0]))
     N = wr if transposed else wc
-    dt = AX_BF16 if x.dtype == torch.int8 else _float_dtype(x, names[0])
     odt = _DT.get(out_dtype)
     if odt is None:
         raise TypeError("out_dtype must be float32 or bfloat16")
@@ -1134,7 +1134,7 @@ def ax_matmul_q8(x, x_scales, w, w_scales, bias=None, residual=None, act="none",
         y_out = x.new_empty(x.shape[:-1] + (_columns(w, True),), dtype=out_dtype)
     hit = _checked.get(key)
     if hit is None:
-        d = _matmul_desc(x, w, act, True, out_dtype, aligned)
+        d = _matmul_desc(x, w, act, True, out_dtype, aligned, codes=True)
         _codes_of(x, x_scales, w, w_scales, d.M, d.N)
         _epilogue_args(d, bias, residual, y_out, None, out_dtype)
         hit = _remember(key, (d, int(L.ax_matmul_q8_workspace_bytes(d))))
@@ -1193,8 +1193,8 @@ def ax_matmul_backward(gy, x, w, z=None, act="none", transposed=False, gx_out=No
     return gx_out, gw_out, gb_out
 
 
-def _gated_desc(x, wg, wu, act, transposed, out_dtype, aligned) -> ax_matmul_desc_t:
-    d = _matmul_desc(x, wg, act, transposed, out_dtype, aligned, ("x", "wg"))
+def _gated_desc(x, wg, wu, act, out_dtype, aligned, codes=False) -> ax_matmul_desc_t:
+    d = _matmul_desc(x, wg, act, codes, out_dtype, aligned, ("x", "wg"), codes)  # (codes are [F,K])
     wr, wc, ld = _mat(wu, x.dtype, "wu")
     if wu.shape != wg.shape or ld != d.w_ld:
         raise ValueError("wg and wu must have one shape and one row pitch")
@@ -1216,7 +1216,7 @@ def ax_gated(x, wg, wu, act="silu", out_dtype=None, save=False, h_out=None, g_ou
         g_out, u_out = (torch.empty_like(h_out, memory_format=torch.contiguous_format) if o is None else o for o in (g_out, u_out))
     hit = _checked.get(key)
     if hit is None:
-        d = _gated_desc(x, wg, wu, act, False, out_dtype, aligned)
+        d = _gated_desc(x, wg, wu, act, out_dtype, aligned)
         _epilogue_args(d, None, None, h_out, g_out, out_dtype, "h_out")
         if u_out is not None:
             _vec_of(u_out, out_dtype, d.M * d.N, "u_out")
@@ -1241,7 +1241,7 @@ def ax_gated_q8(x, x_scales, wg, wg_scales, wu, wu_scales, act="silu", out_dtype
         h_out = x.new_empty(x.shape[:-1] + (_columns(wg, True),), dtype=out_dtype)
     hit = _checked.get(key)
     if hit is None:
-        d = _gated_desc(x, wg, wu, act, True, out_dtype, aligned)
+        d = _gated_desc(x, wg, wu, act, out_dtype, aligned, codes=True)
         _codes_of(x, x_scales, wg, wg_scales, d.M, d.N)
         _codes_of(x, x_scales, wu, wu_scales, d.M, d.N)
         _epilogue_args(d, None, None, h_out, None, out_dtype, "h_out")
@@ -1265,7 +1265,7 @@ def ax_gated_backward(gh, x, wg, wu, g, u, act="silu", gx_out=None, gwg_out=None
     gx_out, gwg_out, gwu_out = _grad_out(gx_out, x), _grad_out(gwg_out, wg), _grad_out(gwu_out, wu)
     hit = _checked.get(key)
     if hit is None:
-        d = _gated_desc(x, wg, wu, act, False, x.dtype, aligned)
+        d = _gated_desc(x, wg, wu, act, x.dtype, aligned)
         d.y_ld = _mat_of(gh, x.dtype, d.M, d.N, "gh")
         _vec_of(g, x.dtype, d.M * d.N, "g")
         _vec_of(u, x.dtype, d.M * d.N, "u")
