@@ -301,6 +301,23 @@ def _stream_ptr(stream) -> int:
     return int(stream.cuda_stream)
 
 
+def _on_stream(call, stream, *args):
+    """call(*args) on `stream`, which is not None: what it allocates comes from that stream's pool, whose blocks are free in
+    that stream's order (one of the current stream's pool may have been freed with kernels still running there).  torch hands
+    a block on when its tensor dies, so the tensors that the call takes are tied to `stream`, and its results to the stream
+    that was current as well, where they will be used."""
+    before = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    for t in args:
+        if isinstance(t, torch.Tensor):
+            t.record_stream(stream)
+    for t in out if isinstance(out, tuple) else (out,):
+        if isinstance(t, torch.Tensor):
+            t.record_stream(before)
+    return out
+
+
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
@@ -888,15 +905,6 @@ def _sig(t):
     return t.dtype, t.shape, t.stride(), t.device
 
 
-def _lend(stream, *tensors):
-    """Tensors allocated here belong to the current stream's pool: those a call on another stream uses are tied to that one
-    too, so that their memory is not handed out again while its kernels run."""
-    if stream is not None:
-        for t in tensors:
-            if isinstance(t, torch.Tensor):
-                t.record_stream(stream)
-
-
 def _mat(t, dtype, name: str) -> Tuple[int, int, int]:
     """(rows, columns, row pitch) of a matrix."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -962,6 +970,8 @@ def _norm_desc(x, residual, sum_out, weight, eps, normalize) -> ax_norm_desc_t:
 def ax_rmsnorm(x, weight, residual=None, eps=1e-5, sum_out=None, y_out=None, rstd_out=None, stream=None):
     """Root-mean-square norm of rows: t = x + residual, y = t * rstd * weight.  Returns (y, t, rstd); t is None without
     a residual.  sum_out may be x or residual themselves; False skips t (or rstd)."""
+    if stream is not None:
+        return _on_stream(ax_rmsnorm, stream, x, weight, residual, eps, sum_out, y_out, rstd_out)
     key = ("rmsnorm", eps, _sig(x), _sig(weight), _sig(residual), _sig(sum_out), _sig(y_out), _sig(rstd_out))
     if residual is not None and sum_out is None:
         sum_out = torch.empty_like(x)
@@ -977,9 +987,8 @@ def ax_rmsnorm(x, weight, residual=None, eps=1e-5, sum_out=None, y_out=None, rst
             _vec_of(rstd_out, torch.float32, d.rows, "rstd_out")
         _remember(key, d)
     sum_out, rstd_out = (None if o is False else o for o in (sum_out, rstd_out))
-    _lend(stream, y_out, sum_out, rstd_out)
     _check(lib().ax_rmsnorm(d, _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_out), _ptr(y_out), _ptr(rstd_out),
-                            _stream_ptr(stream)))
+                            _stream_ptr(None)))
     return y_out, sum_out, rstd_out
 
 
@@ -988,6 +997,9 @@ def ax_rmsnorm_q8(x, weight=None, residual=None, eps=1e-5, normalize=True, sum_o
     """The norm's output as int8 codes with a scale a row: y = codes * scales[:, None].  normalize False: the rows
     themselves (times weight).  Returns (codes, scales, t, values); values, the float32 values that the codes stand for,
     is None unless asked for."""
+    if stream is not None:
+        return _on_stream(ax_rmsnorm_q8, stream, x, weight, residual, eps, normalize, sum_out, codes_out, scales_out,
+                          values_out, values)
     key = ("rmsnorm_q8", eps, normalize, _sig(x), _sig(weight), _sig(residual), _sig(sum_out), _sig(codes_out), _sig(scales_out),
            _sig(values_out))
     if residual is not None and sum_out is None:
@@ -1007,15 +1019,14 @@ def ax_rmsnorm_q8(x, weight=None, residual=None, eps=1e-5, normalize=True, sum_o
             _vec_of(values_out, torch.float32, d.rows * d.cols, "values_out")
         _remember(key, d)
     sum_out = None if sum_out is False else sum_out
-    _lend(stream, codes_out, scales_out, sum_out, values_out)
     _check(lib().ax_rmsnorm_q8(d, _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_out), _ptr(codes_out), _ptr(scales_out),
-                               _ptr(values_out), _stream_ptr(stream)))
+                               _ptr(values_out), _stream_ptr(None)))
     return codes_out, scales_out, sum_out, values_out
 
 
-def _scratch(need: int, workspace, device, stream):
+def _scratch(need: int, workspace, device):
     if workspace is None:
-        return _workspace(need, device, stream) if need else None
+        return _workspace(need, device, None) if need else None
     return _dev(workspace, torch.uint8, "workspace")
 
 
@@ -1026,6 +1037,8 @@ def _ws_args(ws):
 def ax_rmsnorm_backward(gy, t, weight, rstd, gsum=None, gx_out=None, gw_out=None, workspace=None, stream=None):
     """Gradients of ax_rmsnorm: (gx, gw), gx for x and residual alike, gw float32.  t, rstd: what the forward pass
     returned (t = x without a residual); gsum: the gradient that reaches t from the residual stream.  False skips one."""
+    if stream is not None:
+        return _on_stream(ax_rmsnorm_backward, stream, gy, t, weight, rstd, gsum, gx_out, gw_out, workspace)
     L = lib()
     key = ("rmsnorm_backward", _sig(gy), _sig(t), _sig(weight), _sig(rstd), _sig(gsum), _sig(gx_out), _sig(gw_out))
     if gx_out is None:
@@ -1048,10 +1061,9 @@ def ax_rmsnorm_backward(gy, t, weight, rstd, gsum=None, gx_out=None, gw_out=None
         hit = _remember(key, (d, int(L.ax_rmsnorm_backward_workspace_bytes(d))))
     d, need = hit
     gx_out, gw_out = (None if o is False else o for o in (gx_out, gw_out))
-    ws = _scratch(need, workspace, t.device, stream)
-    _lend(stream, gx_out, gw_out)
+    ws = _scratch(need, workspace, t.device)
     _check(L.ax_rmsnorm_backward(d, _ptr(gy), _ptr(gsum), _ptr(t), _ptr(weight), _ptr(rstd), _ptr(gx_out), _ptr(gw_out),
-                                 *_ws_args(ws), _stream_ptr(stream)))
+                                 *_ws_args(ws), _stream_ptr(None)))
     return gx_out, gw_out
 
 
@@ -1097,6 +1109,8 @@ def ax_matmul(x, w, bias=None, residual=None, act="none", transposed=False, out_
     """y = act(x w + bias) + residual.  x: [M,K]; w: [K,N], or [N,K] with transposed; float32 or bfloat16 both; bias,
     residual and the outputs have out_dtype (x's by default).  Returns (y, z): z, the value before the activation, with
     save or z_out, otherwise None."""
+    if stream is not None:
+        return _on_stream(ax_matmul, stream, x, w, bias, residual, act, transposed, out_dtype, save, y_out, z_out, workspace)
     L = lib()
     dev = x.device
     out_dtype = x.dtype if out_dtype is None else out_dtype
@@ -1114,9 +1128,8 @@ def ax_matmul(x, w, bias=None, residual=None, act="none", transposed=False, out_
         _epilogue_args(d, bias, residual, y_out, z_out, out_dtype)
         hit = _remember(key, (d, int(L.ax_matmul_workspace_bytes(d))))
     d, need = hit
-    ws = _scratch(need, workspace, dev, stream)
-    _lend(stream, y_out, z_out)
-    _check(L.ax_matmul(d, xp, wp, _ptr(bias), _ptr(residual), y_out.data_ptr(), _ptr(z_out), *_ws_args(ws), _stream_ptr(stream)))
+    ws = _scratch(need, workspace, dev)
+    _check(L.ax_matmul(d, xp, wp, _ptr(bias), _ptr(residual), y_out.data_ptr(), _ptr(z_out), *_ws_args(ws), _stream_ptr(None)))
     return y_out, z_out
 
 
@@ -1124,6 +1137,8 @@ def ax_matmul_q8(x, x_scales, w, w_scales, bias=None, residual=None, act="none",
                  workspace=None, stream=None):
     """y = act((x * x_scales) (w * w_scales)^T + bias) + residual on int8 codes: x [M,K] with a scale a row (what
     ax_rmsnorm_q8 returns), w [N,K] with a scale a row."""
+    if stream is not None:
+        return _on_stream(ax_matmul_q8, stream, x, x_scales, w, w_scales, bias, residual, act, out_dtype, y_out, workspace)
     L = lib()
     dev = x.device
     xp, wp = x.data_ptr(), w.data_ptr()
@@ -1139,10 +1154,9 @@ def ax_matmul_q8(x, x_scales, w, w_scales, bias=None, residual=None, act="none",
         _epilogue_args(d, bias, residual, y_out, None, out_dtype)
         hit = _remember(key, (d, int(L.ax_matmul_q8_workspace_bytes(d))))
     d, need = hit
-    ws = _scratch(need, workspace, dev, stream)
-    _lend(stream, y_out)
+    ws = _scratch(need, workspace, dev)
     _check(L.ax_matmul_q8(d, xp, x_scales.data_ptr(), wp, w_scales.data_ptr(), _ptr(bias), _ptr(residual), y_out.data_ptr(),
-                          *_ws_args(ws), _stream_ptr(stream)))
+                          *_ws_args(ws), _stream_ptr(None)))
     return y_out
 
 
@@ -1164,6 +1178,8 @@ def _check_grad(out, like, ld, name):
 def ax_matmul_backward(gy, x, w, z=None, act="none", transposed=False, gx_out=None, gw_out=None, gb_out=None, workspace=None,
                        stream=None):
     """Gradients of ax_matmul: (gx, gw, gb), gb float32; False skips one.  z: the value before the activation."""
+    if stream is not None:
+        return _on_stream(ax_matmul_backward, stream, gy, x, w, z, act, transposed, gx_out, gw_out, gb_out, workspace)
     L = lib()
     dev = x.device
     gp, xp, wp = gy.data_ptr(), x.data_ptr(), w.data_ptr()
@@ -1187,9 +1203,8 @@ def ax_matmul_backward(gy, x, w, z=None, act="none", transposed=False, gx_out=No
         hit = _remember(key, (d, int(L.ax_matmul_backward_workspace_bytes(d))))
     d, need = hit
     gx_out, gw_out, gb_out = (None if o is False else o for o in (gx_out, gw_out, gb_out))
-    ws = _scratch(need, workspace, dev, stream)
-    _lend(stream, gx_out, gw_out, gb_out)
-    _check(L.ax_matmul_backward(d, gp, xp, wp, _ptr(z), _ptr(gx_out), _ptr(gw_out), _ptr(gb_out), *_ws_args(ws), _stream_ptr(stream)))
+    ws = _scratch(need, workspace, dev)
+    _check(L.ax_matmul_backward(d, gp, xp, wp, _ptr(z), _ptr(gx_out), _ptr(gw_out), _ptr(gb_out), *_ws_args(ws), _stream_ptr(None)))
     return gx_out, gw_out, gb_out
 
 
@@ -1204,6 +1219,8 @@ def _gated_desc(x, wg, wu, act, out_dtype, aligned, codes=False) -> ax_matmul_de
 def ax_gated(x, wg, wu, act="silu", out_dtype=None, save=False, h_out=None, g_out=None, u_out=None, workspace=None, stream=None):
     """h = act(x wg) * (x wu).  x [M,K]; wg, wu [K,F]; float32 or bfloat16.  Returns (h, g, u): both projections with
     save (or g_out and u_out), otherwise None."""
+    if stream is not None:
+        return _on_stream(ax_gated, stream, x, wg, wu, act, out_dtype, save, h_out, g_out, u_out, workspace)
     L = lib()
     dev = x.device
     out_dtype = x.dtype if out_dtype is None else out_dtype
@@ -1222,15 +1239,16 @@ def ax_gated(x, wg, wu, act="silu", out_dtype=None, save=False, h_out=None, g_ou
             _vec_of(u_out, out_dtype, d.M * d.N, "u_out")
         hit = _remember(key, (d, int(L.ax_gated_workspace_bytes(d))))
     d, need = hit
-    ws = _scratch(need, workspace, dev, stream)
-    _lend(stream, h_out, g_out, u_out)
-    _check(L.ax_gated(d, xp, gp, up, h_out.data_ptr(), _ptr(g_out), _ptr(u_out), *_ws_args(ws), _stream_ptr(stream)))
+    ws = _scratch(need, workspace, dev)
+    _check(L.ax_gated(d, xp, gp, up, h_out.data_ptr(), _ptr(g_out), _ptr(u_out), *_ws_args(ws), _stream_ptr(None)))
     return h_out, g_out, u_out
 
 
 def ax_gated_q8(x, x_scales, wg, wg_scales, wu, wu_scales, act="silu", out_dtype=torch.bfloat16, h_out=None, workspace=None,
                 stream=None):
     """The gated block on int8 codes: x [M,K] and wg, wu [F,K], each with a scale a row."""
+    if stream is not None:
+        return _on_stream(ax_gated_q8, stream, x, x_scales, wg, wg_scales, wu, wu_scales, act, out_dtype, h_out, workspace)
     L = lib()
     dev = x.device
     xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
@@ -1247,15 +1265,16 @@ def ax_gated_q8(x, x_scales, wg, wg_scales, wu, wu_scales, act="silu", out_dtype
         _epilogue_args(d, None, None, h_out, None, out_dtype, "h_out")
         hit = _remember(key, (d, int(L.ax_gated_q8_workspace_bytes(d))))
     d, need = hit
-    ws = _scratch(need, workspace, dev, stream)
-    _lend(stream, h_out)
+    ws = _scratch(need, workspace, dev)
     _check(L.ax_gated_q8(d, xp, x_scales.data_ptr(), gp, wg_scales.data_ptr(), up, wu_scales.data_ptr(), h_out.data_ptr(),
-                         *_ws_args(ws), _stream_ptr(stream)))
+                         *_ws_args(ws), _stream_ptr(None)))
     return h_out
 
 
 def ax_gated_backward(gh, x, wg, wu, g, u, act="silu", gx_out=None, gwg_out=None, gwu_out=None, workspace=None, stream=None):
     """Gradients of ax_gated: (gx, gwg, gwu); gx_out False, or gwg_out and gwu_out False, skips them."""
+    if stream is not None:
+        return _on_stream(ax_gated_backward, stream, gh, x, wg, wu, g, u, act, gx_out, gwg_out, gwu_out, workspace)
     L = lib()
     dev = x.device
     xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
@@ -1274,10 +1293,9 @@ def ax_gated_backward(gh, x, wg, wu, g, u, act="silu", gx_out=None, gwg_out=None
         hit = _remember(key, (d, int(L.ax_gated_backward_workspace_bytes(d))))
     d, need = hit
     gx_out, gwg_out, gwu_out = (None if o is False else o for o in (gx_out, gwg_out, gwu_out))
-    ws = _scratch(need, workspace, dev, stream)
-    _lend(stream, gx_out, gwg_out, gwu_out)
+    ws = _scratch(need, workspace, dev)
     _check(L.ax_gated_backward(d, gh.data_ptr(), xp, gp, up, g.data_ptr(), u.data_ptr(), _ptr(gx_out), _ptr(gwg_out), _ptr(gwu_out),
-                               *_ws_args(ws), _stream_ptr(stream)))
+                               *_ws_args(ws), _stream_ptr(None)))
     return gx_out, gwg_out, gwu_out
 
 
@@ -1358,6 +1376,9 @@ class AxAdamW:
         if grad_scale is not None:
             _vec_of(grad_scale, torch.float32, 1, "grad_scale")
         d.grad_scale = _ptr(grad_scale)
+        if stream is not None:  # (the gradients may be exchanged, and the factor dropped, before the step has run)
+            for t in self.grads if grad_scale is None else self.grads + [grad_scale]:
+                t.record_stream(stream)
         _check(lib().ax_adamw(d, self._t, len(self._t), _stream_ptr(stream)))
 
     def states(self, stream=None):
@@ -1365,12 +1386,15 @@ class AxAdamW:
         for v), or the 32-bit states themselves."""
         if self.bits == 32:
             return self.m, self.v
-        bufs = [torch.empty(self._whole, dtype=torch.float32, device=self.params[0].device) for _ in range(2)]
-        _lend(stream, *bufs)
-        ptrs = [(ctypes.c_void_p * len(self._places))(*[b.data_ptr() + 4 * at for _, _, at in self._places]) for b in bufs]
-        _check(lib().ax_adamw_states(self._t, len(self._t), ptrs[0], ptrs[1], _stream_ptr(stream)))
+        bufs = self._states() if stream is None else _on_stream(self._states, stream)
         m, v = ([b.as_strided(*place) for place in self._places] for b in bufs)
         return m, v
+
+    def _states(self):
+        bufs = tuple(torch.empty(self._whole, dtype=torch.float32, device=self.params[0].device) for _ in range(2))
+        ptrs = [(ctypes.c_void_p * len(self._places))(*[b.data_ptr() + 4 * at for _, _, at in self._places]) for b in bufs]
+        _check(lib().ax_adamw_states(self._t, len(self._t), ptrs[0], ptrs[1], _stream_ptr(None)))
+        return bufs
 
 
 def ax_probe_lds_gather(width_bytes: int, pattern: int, table_bytes: int, threads: int = 1024, iters: int = 2000,

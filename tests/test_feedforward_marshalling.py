@@ -1,6 +1,8 @@
 """What the feed-forward entry points hand to the library, on the host: the C calls are replaced by ones that take notes, and the
 tensors are ordinary ones that say that they are on the GPU."""
 
+import contextlib
+
 import pytest
 import torch
 
@@ -77,3 +79,72 @@ def test_products_of_codes_take_codes_alone(notes):
     ax.ax_gated_q8(codes(4, 16), s, codes(8, 16), s16, codes(8, 16), s16)
     ax.ax_matmul(x, w, transposed=True)
     assert notes.calls == ["ax_matmul_q8", "ax_gated_q8", "ax_matmul"]
+
+
+class Side:
+    """A stream that is not the current one, for tensors on the host."""
+
+    device, cuda_stream = torch.device("cuda", 0), 7
+
+
+def _every_operator():
+    """(call, its arguments in their order) of every operator that allocates."""
+    f = lambda *s: floats(*s, dtype=torch.float32)  # noqa: E731
+    q, sc = codes(4, 16), f(4)
+    x, w, gy, v = f(4, 16), f(16, 16), f(4, 16), f(16)
+    opt = ax.AxAdamW([v], [f(16)], [codes(16)], [placed(torch.zeros(16, dtype=torch.uint8))], [f(1)], [f(1)])
+    return [(ax.ax_rmsnorm, (x, v, gy)), (ax.ax_rmsnorm_q8, (x, v, gy, 1e-5, True, None, None, None, None, True)),
+            (ax.ax_rmsnorm_backward, (gy, x, v, sc)), (ax.ax_matmul, (x, w, v, gy, "silu", False, None, True)),
+            (ax.ax_matmul_q8, (q, sc, q, sc)), (ax.ax_matmul_backward, (gy, x, w)), (ax.ax_gated, (x, w, w, "silu", None, True)),
+            (ax.ax_gated_q8, (q, sc, q, sc, q, sc)), (ax.ax_gated_backward, (gy, x, w, w, gy, gy)), (opt.states, ())]
+
+
+@pytest.mark.parametrize("k", range(10))
+def test_memory_of_calls_on_another_stream(notes, monkeypatch, k):
+    """What a call allocates belongs to its stream's pool; what it takes is tied to its stream, what it returns to the one
+    that was current."""
+    current, side, made, ties = [object()], Side(), [], []
+    main = current[0]
+
+    @contextlib.contextmanager
+    def on(s):
+        current.append(s)
+        yield
+        current.pop()
+
+    def factory(f):
+        def make(*a, **kw):
+            kw["device"] = None if "device" in kw else kw.get("device")
+            t = placed(f(*a, **{n: v for n, v in kw.items() if v is not None}))
+            made.append((t.data_ptr(), current[-1]))
+            return t
+        return make
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: current[-1])
+    monkeypatch.setattr(Placed, "record_stream", lambda t, s: ties.append((t.data_ptr(), s)), raising=False)
+    call, args = _every_operator()[k]
+    for name in ("empty", "empty_like", "empty_strided"):
+        monkeypatch.setattr(torch, name, factory(getattr(torch, name)))
+    monkeypatch.setattr(Placed, "new_empty", factory(torch.Tensor.new_empty), raising=False)
+    out = call(*args, stream=side)
+    results = [t for t in (out if isinstance(out, tuple) else (out,)) if isinstance(t, torch.Tensor)]
+    results += [t for ts in out if isinstance(ts, list) for t in ts[:1]] if isinstance(out, tuple) else []
+    assert len(notes.calls) == 1 and made and results
+    assert all(where is side for _, where in made) and current == [main]
+    for t in results:
+        assert (t.data_ptr(), main) in ties
+    for t in args:
+        if isinstance(t, torch.Tensor):
+            assert (t.data_ptr(), side) in ties
+
+
+def test_gradients_of_a_step_on_another_stream(notes, monkeypatch):
+    ties, side = [], Side()
+    monkeypatch.setattr(Placed, "record_stream", lambda t, s: ties.append((t.data_ptr(), s)), raising=False)
+    p, g, factor = (floats(n, dtype=torch.float32) for n in (16, 16, 1))
+    opt = ax.AxAdamW([p], [g], m=[floats(16, dtype=torch.float32)], v=[floats(16, dtype=torch.float32)])
+    opt.step(1e-3, 1, grad_scale=factor)
+    assert not ties
+    opt.step(1e-3, 2, grad_scale=factor, stream=side)
+    assert (g.data_ptr(), side) in ties and (factor.data_ptr(), side) in ties
