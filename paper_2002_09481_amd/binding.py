@@ -322,14 +322,9 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _workspace(need: int, device, stream) -> torch.Tensor:
-    """Temporary scratch for one call.  torch's allocator hands memory back to the current
-    stream's pool when the tensor dies: for a call on another stream the allocation is tied to
-    that stream as well, so that it is not reused while the kernels still run."""
-    ws = torch.empty(max(int(need), 256), dtype=torch.uint8, device=device)
-    if stream is not None:
-        ws.record_stream(stream)
-    return ws
+def _workspace(need: int, device) -> torch.Tensor:
+    """Temporary scratch for one call."""
+    return torch.empty(max(int(need), 256), dtype=torch.uint8, device=device)
 
 
 def _conv_desc(x_shape, w_shape, stride, pad, dilation=1, depthwise=False, signed=False, groups=1) -> ax_conv_desc_t:
@@ -382,6 +377,8 @@ def ax_conv2d(x, w, lut, stride, pad, q, acc_out=None, y_out=None, workspace=Non
     [65536] (bit pattern of the uint16 entries); acc_out: int32 [N,OH,OW,Cout]; y_out: float32.
     Missing outputs / workspace are allocated with torch (the C call itself never allocates).
     Returns (acc_out, y_out)."""
+    if stream is not None:
+        return _on_stream(ax_conv2d, stream, x, w, lut, stride, pad, q, acc_out, y_out, workspace)
     # Small layers are bound by this function, not by the device: the plain entry point takes the sizes as they are, no
     # descriptor is filled in and read back (16 x 16 x 8, 3 x 3: 13.5 us a call, 11.4 now; 6.5 on the device).
     L = lib()
@@ -399,10 +396,10 @@ def ax_conv2d(x, w, lut, stride, pad, q, acc_out=None, y_out=None, workspace=Non
         _check(-2)
     acc_out, y_out = _outs((N, OH, OW, Cout), x.device, acc_out, y_out)
     if workspace is None:  # (a workspace handed in is checked by the C call itself)
-        workspace = _workspace(ax_conv2d_workspace_bytes(xs, ws, stride, pad), x.device, stream)
+        workspace = _workspace(ax_conv2d_workspace_bytes(xs, ws, stride, pad), x.device)
     _dev(workspace, torch.uint8, "workspace")
     tail = (ctypes.byref(_quant(q)), _ptr(None if acc_out is False else acc_out), _ptr(None if y_out is False else y_out),
-            _ptr(workspace), workspace.numel(), _stream_ptr(stream))
+            _ptr(workspace), workspace.numel(), _stream_ptr(None))
     t = _tune_arg()
     if t is None:
         rc = L.ax_conv2d(_ptr(x), N, H, W, Cin, _ptr(w), KH, KW, Cout, _ptr(lut), sh, sw, ph, pw, *tail)
@@ -414,6 +411,8 @@ def ax_conv2d(x, w, lut, stride, pad, q, acc_out=None, y_out=None, workspace=Non
 
 def ax_dense(x, w, lut, q, acc_out=None, y_out=None, workspace=None, stream=None):
     """x: uint8 [M,K]; w: uint8 [K,N]; outputs [M,N]."""
+    if stream is not None:
+        return _on_stream(ax_dense, stream, x, w, lut, q, acc_out, y_out, workspace)
     L = lib()
     _dev(x, torch.uint8, "x")
     _dev(w, torch.uint8, "w")
@@ -424,12 +423,12 @@ def ax_dense(x, w, lut, q, acc_out=None, y_out=None, workspace=None, stream=None
     N = w.shape[1]
     acc_out, y_out = _outs((M, N), x.device, acc_out, y_out)
     if workspace is None:
-        workspace = _workspace(ax_dense_workspace_bytes(M, K, N), x.device, stream)
+        workspace = _workspace(ax_dense_workspace_bytes(M, K, N), x.device)
     _dev(workspace, torch.uint8, "workspace")
     qs = _quant(q)
     t = _tune_arg()
     tail = (ctypes.byref(qs), _ptr(None if acc_out is False else acc_out), _ptr(None if y_out is False else y_out),
-            _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(stream)))
+            _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(None)))
     if t is None:
         rc = L.ax_dense(_ptr(x), M, K, _ptr(w), N, _ptr(lut), *tail)
     else:
@@ -448,6 +447,8 @@ def ax_conv2d_multi_lut(x, w, luts, stride, pad, q, acc_out=None, y_out=None, wo
     """One layer against T tables.  luts: 16-bit integer CUDA tensor [T, 65536]; outputs
     [T, N, OH, OW, Cout].  Returns (acc_out, y_out); pass False to skip one of them.  With a
     default tune set the call goes through a layer handle (the one-call entry takes no tune)."""
+    if stream is not None:
+        return _on_stream(ax_conv2d_multi_lut, stream, x, w, luts, stride, pad, q, acc_out, y_out, workspace)
     L = lib()
     _dev(x, torch.uint8, "x")
     _dev(w, torch.uint8, "w")
@@ -465,16 +466,16 @@ def ax_conv2d_multi_lut(x, w, luts, stride, pad, q, acc_out=None, y_out=None, wo
     qs = _quant(q)
     if _tune_arg() is not None:
         with AxLayer(d, qs, T) as layer:
-            layer.prepare(w, luts, stream=stream)
-            layer.run(x, acc_out, y_out, workspace=workspace, stream=stream)
+            layer.prepare(w, luts)
+            layer.run(x, acc_out, y_out, workspace=workspace)
         return (None if acc_out is False else acc_out), (None if y_out is False else y_out)
     if workspace is None:
-        workspace = _workspace(ax_conv2d_multi_lut_workspace_bytes(x.shape, w.shape, T, stride, pad), x.device, stream)
+        workspace = _workspace(ax_conv2d_multi_lut_workspace_bytes(x.shape, w.shape, T, stride, pad), x.device)
     _dev(workspace, torch.uint8, "workspace")
     rc = L.ax_conv2d_multi_lut(_ptr(x), d.N, d.H, d.W, d.Cin, _ptr(w), d.KH, d.KW, d.Cout, _ptr(luts), T, d.stride_h,
                                d.stride_w, d.pad_h, d.pad_w, ctypes.byref(qs),
                                _ptr(None if acc_out is False else acc_out), _ptr(None if y_out is False else y_out),
-                               _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(stream)))
+                               _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(None)))
     _check(rc)
     return (None if acc_out is False else acc_out), (None if y_out is False else y_out)
 
@@ -484,6 +485,9 @@ def ax_conv2d_ex(x, w, lut, stride, pad, q, dilation=1, depthwise=False, acc_out
     """Operator variants.  Signed form: x, w int8 and lut int16 (chosen by x.dtype).  Depthwise:
     w is [KH,KW,Cin,mult].  Grouped: w is [KH,KW,Cin/groups,Cout].  q.pad_code None selects the
     zero point.  Returns (acc_out, y_out)."""
+    if stream is not None:
+        return _on_stream(ax_conv2d_ex, stream, x, w, lut, stride, pad, q, dilation, depthwise, acc_out, y_out, workspace, None,
+                          groups)
     L = lib()
     signed = x.dtype == torch.int8
     cdt = torch.int8 if signed else torch.uint8
@@ -499,12 +503,12 @@ def ax_conv2d_ex(x, w, lut, stride, pad, q, dilation=1, depthwise=False, acc_out
     acc_out, y_out = _outs((desc.N, OH, OW, desc.Cout), x.device, acc_out, y_out)
     t = _tune_arg()
     if workspace is None:
-        workspace = _workspace(int(L.ax_conv2d_ex_workspace_bytes(ctypes.byref(desc), t)), x.device, stream)
+        workspace = _workspace(int(L.ax_conv2d_ex_workspace_bytes(ctypes.byref(desc), t)), x.device)
     _dev(workspace, torch.uint8, "workspace")
     qs = _quant(q)
     rc = L.ax_conv2d_ex(ctypes.byref(desc), t, _ptr(x), _ptr(w), _ptr(lut), ctypes.byref(qs),
                         _ptr(None if acc_out is False else acc_out), _ptr(None if y_out is False else y_out),
-                        _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(stream)))
+                        _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(None)))
     _check(rc)
     return (None if acc_out is False else acc_out), (None if y_out is False else y_out)
 
@@ -513,6 +517,8 @@ def ax_conv2d_transpose(x, w, lut, stride, pad, q, dilation=1, acc_out=None, y_o
     """Transposed convolution by zero insertion.  x: codes [N,H,W,Cin] (uint8, or int8 for the
     signed form), w: [KH,KW,Cin,Cout].  Returns (acc_out, y_out) of shape [N,OH,OW,Cout] with
     OH = (H-1)*stride + 1 + dilation*(KH-1) - 2*pad."""
+    if stream is not None:
+        return _on_stream(ax_conv2d_transpose, stream, x, w, lut, stride, pad, q, dilation, acc_out, y_out, workspace)
     L = lib()
     signed = x.dtype == torch.int8
     cdt = torch.int8 if signed else torch.uint8
@@ -532,12 +538,12 @@ def ax_conv2d_transpose(x, w, lut, stride, pad, q, dilation=1, acc_out=None, y_o
         n = int(L.ax_conv2d_transpose_workspace_bytes(ctypes.byref(desc), t))
         if n == 0:
             _check(-2)
-        workspace = _workspace(n, x.device, stream)
+        workspace = _workspace(n, x.device)
     _dev(workspace, torch.uint8, "workspace")
     qs = _quant(q)
     rc = L.ax_conv2d_transpose(ctypes.byref(desc), t, _ptr(x), _ptr(w), _ptr(lut), ctypes.byref(qs),
                                _ptr(None if acc_out is False else acc_out), _ptr(None if y_out is False else y_out),
-                               _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(stream)))
+                               _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(None)))
     _check(rc)
     return (None if acc_out is False else acc_out), (None if y_out is False else y_out)
 
@@ -546,6 +552,8 @@ def ax_conv2d_backward(x, w, gy, stride, pad, q, dilation=1, gx_out=None, gw_out
     """Backward pass of a layer (straight-through).  x, w: codes (uint8, or int8 for the signed
     form); gy: float32 [N,OH,OW,Cout].  Returns (gx [N,H,W,Cin], gw [KH,KW,Cin,Cout]) as float32
     tensors; pass False to skip one of them."""
+    if stream is not None:
+        return _on_stream(ax_conv2d_backward, stream, x, w, gy, stride, pad, q, dilation, gx_out, gw_out, workspace)
     L = lib()
     signed = x.dtype == torch.int8
     cdt = torch.int8 if signed else torch.uint8
@@ -570,12 +578,12 @@ def ax_conv2d_backward(x, w, gy, stride, pad, q, dilation=1, gx_out=None, gw_out
             if o.numel() != ref.numel():
                 raise ValueError("%s has the wrong number of elements" % name)
     if workspace is None:
-        workspace = _workspace(int(L.ax_conv2d_backward_workspace_bytes(ctypes.byref(desc))), x.device, stream)
+        workspace = _workspace(int(L.ax_conv2d_backward_workspace_bytes(ctypes.byref(desc))), x.device)
     _dev(workspace, torch.uint8, "workspace")
     qs = _quant(q)
     _check(L.ax_conv2d_backward(ctypes.byref(desc), ctypes.byref(qs), _ptr(x), _ptr(w), _ptr(gy),
                                 _ptr(None if gx_out is False else gx_out), _ptr(None if gw_out is False else gw_out),
-                                _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(stream))))
+                                _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(None))))
     return (None if gx_out is False else gx_out), (None if gw_out is False else gw_out)
 
 
@@ -647,6 +655,8 @@ class AxLayer:
                 "tiles": tiles, "workgroups": workgroups, "threads": threads}
 
     def prepare(self, w, luts, prepared=None, stream=None):
+        if stream is not None:
+            return _on_stream(self.prepare, stream, w, luts, prepared)
         cdt = torch.int8 if self.desc.signed_codes else torch.uint8
         _dev(w, cdt, "w")
         _check_lut(luts, self.num_luts * 65536)
@@ -654,11 +664,11 @@ class AxLayer:
             prepared = torch.empty(max(self.prepared_bytes, 256), dtype=torch.uint8, device=w.device)
         _dev(prepared, torch.uint8, "prepared")
         _check(lib().ax_layer_prepare(self._h, _ptr(w), _ptr(luts), _ptr(prepared), prepared.numel(),
-                                      ctypes.c_void_p(_stream_ptr(stream))))
+                                      ctypes.c_void_p(_stream_ptr(None))))
         self._keep = (w, luts, prepared)
         return prepared
 
-    def _args(self, x, acc_out, y_out, workspace, stream):
+    def _args(self, x, acc_out, y_out, workspace):
         cdt = torch.int8 if self.desc.signed_codes else torch.uint8
         _dev(x, cdt, "x")
         acc_out, y_out = _outs(self.out_shape(), x.device, acc_out, y_out)
@@ -666,21 +676,26 @@ class AxLayer:
             if self._ws is None or self._ws.device != x.device:
                 self._ws = torch.empty(max(self.workspace_bytes, 256), dtype=torch.uint8, device=x.device)
             workspace = self._ws
-            if stream is not None:
-                workspace.record_stream(stream)
         _dev(workspace, torch.uint8, "workspace")
         return acc_out, y_out, workspace
 
     def run(self, x, acc_out=None, y_out=None, workspace=None, stream=None):
-        acc_out, y_out, workspace = self._args(x, acc_out, y_out, workspace, stream)
+        if stream is not None:
+            out = _on_stream(self.run, stream, x, acc_out, y_out, workspace)
+            if workspace is None:
+                self._ws.record_stream(stream)
+            return out
+        acc_out, y_out, workspace = self._args(x, acc_out, y_out, workspace)
         _check(lib().ax_layer_run(self._h, _ptr(x), _ptr(None if acc_out is False else acc_out),
                                   _ptr(None if y_out is False else y_out), _ptr(workspace), workspace.numel(),
-                                  ctypes.c_void_p(_stream_ptr(stream))))
+                                  ctypes.c_void_p(_stream_ptr(None))))
         return (None if acc_out is False else acc_out), (None if y_out is False else y_out)
 
     def run_static(self, x, acc_out, y_out, stream=None):
         """ax_layer_run_static: scratch from the library's static device array; nothing is
         allocated, so the outputs must be handed in (False skips one of them)."""
+        if stream is not None:
+            return _on_stream(self.run_static, stream, x, acc_out, y_out)
         cdt = torch.int8 if self.desc.signed_codes else torch.uint8
         _dev(x, cdt, "x")
         if acc_out is None or y_out is None:
@@ -688,17 +703,19 @@ class AxLayer:
         acc_out, y_out = _outs(self.out_shape(), x.device, acc_out, y_out)
         _check(lib().ax_layer_run_static(self._h, _ptr(x), _ptr(None if acc_out is False else acc_out),
                                          _ptr(None if y_out is False else y_out),
-                                         ctypes.c_void_p(_stream_ptr(stream))))
+                                         ctypes.c_void_p(_stream_ptr(None))))
         return (None if acc_out is False else acc_out), (None if y_out is False else y_out)
 
     def kernel_ms(self, x, acc_out=None, y_out=None, workspace=None, reps: int = 8, stream=None) -> float:
         """ax_probe_layer_kernel_ms: duration of one launch of the layer's main kernel."""
-        acc_out, y_out, workspace = self._args(x, acc_out, y_out, workspace, stream)
+        if stream is not None:
+            return _on_stream(self.kernel_ms, stream, x, acc_out, y_out, workspace, reps)
+        acc_out, y_out, workspace = self._args(x, acc_out, y_out, workspace)
         ms = ctypes.c_float(0.0)
         _check(lib().ax_probe_layer_kernel_ms(self._h, _ptr(x), _ptr(None if acc_out is False else acc_out),
                                               _ptr(None if y_out is False else y_out), _ptr(workspace),
                                               workspace.numel(), int(reps), ctypes.byref(ms),
-                                              ctypes.c_void_p(_stream_ptr(stream))))
+                                              ctypes.c_void_p(_stream_ptr(None))))
         return float(ms.value)
 
 
@@ -708,6 +725,8 @@ def ax_range_workspace_bytes(n: int) -> int:
 
 def ax_range_f32(x, relu=False, range_out=None, workspace=None, stream=None):
     """(min, max) of a float32 CUDA tensor into a float32 CUDA tensor of two."""
+    if stream is not None:
+        return _on_stream(ax_range_f32, stream, x, relu, range_out, workspace)
     L = lib()
     _dev(x, torch.float32, "x")
     if range_out is None:
@@ -717,7 +736,7 @@ def ax_range_f32(x, relu=False, range_out=None, workspace=None, stream=None):
         workspace = torch.empty(int(L.ax_range_workspace_bytes(x.numel())), dtype=torch.uint8, device=x.device)
     _dev(workspace, torch.uint8, "workspace")
     _check(L.ax_range_f32(_ptr(x), x.numel(), int(bool(relu)), _ptr(range_out), _ptr(workspace), workspace.numel(),
-                          ctypes.c_void_p(_stream_ptr(stream))))
+                          ctypes.c_void_p(_stream_ptr(None))))
     return range_out
 
 
@@ -725,6 +744,8 @@ def ax_quantize_f32(x, rng, relu=False, round_mode=0, codes_out=None, coeffs_out
     """Codes of a float32 CUDA tensor for the range `rng` (float32 CUDA tensor of two).
     coeffs_out: int32 CUDA tensor of two receiving the bit pattern of alpha and the value of
     beta (allocated when None).  Returns (codes_out, coeffs_out)."""
+    if stream is not None:
+        return _on_stream(ax_quantize_f32, stream, x, rng, relu, round_mode, codes_out, coeffs_out)
     L = lib()
     _dev(x, torch.float32, "x")
     _dev(rng, torch.float32, "range")
@@ -739,7 +760,7 @@ def ax_quantize_f32(x, rng, relu=False, round_mode=0, codes_out=None, coeffs_out
         coeffs_out = torch.empty(2, dtype=torch.int32, device=x.device)
     _dev(coeffs_out, torch.int32, "coeffs_out")
     _check(L.ax_quantize_f32(_ptr(x), x.numel(), _ptr(rng), int(bool(relu)), int(round_mode), _ptr(codes_out),
-                             _ptr(coeffs_out), ctypes.c_void_p(_stream_ptr(stream))))
+                             _ptr(coeffs_out), ctypes.c_void_p(_stream_ptr(None))))
     return codes_out, coeffs_out
 
 
@@ -789,17 +810,17 @@ def _outs(shape, device, acc_out, y_out):
     return acc_out, y_out
 
 
-def _f32_ex(desc, x, w, lut, x_range, w_range, relu, round_mode, acc_out, y_out, workspace, stream, out_shape):
+def _f32_ex(desc, x, w, lut, x_range, w_range, relu, round_mode, acc_out, y_out, workspace, out_shape):
     L = lib()
     acc_out, y_out = _outs(out_shape, x.device, acc_out, y_out)
     t = _tune_arg()
     if workspace is None:
-        workspace = _workspace(int(L.ax_conv2d_f32_ex_workspace_bytes(ctypes.byref(desc), t)), x.device, stream)
+        workspace = _workspace(int(L.ax_conv2d_f32_ex_workspace_bytes(ctypes.byref(desc), t)), x.device)
     _dev(workspace, torch.uint8, "workspace")
     rc = L.ax_conv2d_f32_ex(ctypes.byref(desc), t, _ptr(x), _ptr(w), _ptr(lut), _ptr(x_range), _ptr(w_range),
                             int(bool(relu)), int(round_mode), _ptr(None if acc_out is False else acc_out),
                             _ptr(None if y_out is False else y_out), _ptr(workspace), workspace.numel(),
-                            ctypes.c_void_p(_stream_ptr(stream)))
+                            ctypes.c_void_p(_stream_ptr(None)))
     _check(rc)
     return (None if acc_out is False else acc_out), (None if y_out is False else y_out)
 
@@ -808,6 +829,9 @@ def ax_conv2d_f32(x, w, lut, stride, pad, x_range=None, w_range=None, relu=False
                   workspace=None, stream=None):
     """Float layer.  x: float32 [N,H,W,Cin]; w: float32 [KH,KW,Cin,Cout]; ranges: float32 CUDA
     tensors of two, or None to let the layer take the range of that tensor.  Returns (acc_out, y_out); pass False to skip one of them."""
+    if stream is not None:
+        return _on_stream(ax_conv2d_f32, stream, x, w, lut, stride, pad, x_range, w_range, relu, round_mode, acc_out,
+                          y_out, workspace)
     L = lib()
     _f32_common(x, w, lut, x_range, w_range)
     if x.dim() != 4 or w.dim() != 4 or w.shape[2] != x.shape[3]:
@@ -817,16 +841,16 @@ def ax_conv2d_f32(x, w, lut, stride, pad, x_range=None, w_range=None, relu=False
     if OH <= 0 or OW <= 0:
         _check(-2)
     if _tune_arg() is not None:
-        return _f32_ex(d, x, w, lut, x_range, w_range, relu, round_mode, acc_out, y_out, workspace, stream,
+        return _f32_ex(d, x, w, lut, x_range, w_range, relu, round_mode, acc_out, y_out, workspace,
                        (d.N, OH, OW, d.Cout))
     acc_out, y_out = _outs((d.N, OH, OW, d.Cout), x.device, acc_out, y_out)
     if workspace is None:
-        workspace = _workspace(ax_conv2d_f32_workspace_bytes(x.shape, w.shape, stride, pad), x.device, stream)
+        workspace = _workspace(ax_conv2d_f32_workspace_bytes(x.shape, w.shape, stride, pad), x.device)
     _dev(workspace, torch.uint8, "workspace")
     rc = L.ax_conv2d_f32(_ptr(x), d.N, d.H, d.W, d.Cin, _ptr(w), d.KH, d.KW, d.Cout, _ptr(lut), d.stride_h, d.stride_w,
                          d.pad_h, d.pad_w, _ptr(x_range), _ptr(w_range), int(bool(relu)), int(round_mode),
                          _ptr(None if acc_out is False else acc_out), _ptr(None if y_out is False else y_out),
-                         _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(stream)))
+                         _ptr(workspace), workspace.numel(), ctypes.c_void_p(_stream_ptr(None)))
     _check(rc)
     return (None if acc_out is False else acc_out), (None if y_out is False else y_out)
 
@@ -835,6 +859,9 @@ def ax_conv2d_f32_ex(x, w, lut, stride, pad, x_range=None, w_range=None, relu=Fa
                      depthwise=False, signed=False, acc_out=None, y_out=None, workspace=None, stream=None, groups=1):
     """Float layer with dilation / signed codes / depthwise filters (w [KH,KW,Cin,mult]) / grouped
     filters (w [KH,KW,Cin/groups,Cout]).  Returns (acc_out, y_out); pass False to skip one of them."""
+    if stream is not None:
+        return _on_stream(ax_conv2d_f32_ex, stream, x, w, lut, stride, pad, x_range, w_range, relu, round_mode, dilation,
+                          depthwise, signed, acc_out, y_out, workspace, None, groups)
     _f32_common(x, w, lut, x_range, w_range)
     if x.dim() != 4 or w.dim() != 4 or w.shape[2] * int(groups) != x.shape[3]:
         raise ValueError("x must be [N,H,W,Cin] and w [KH,KW,Cin/groups,Cout] (or [KH,KW,Cin,mult])")
@@ -842,13 +869,15 @@ def ax_conv2d_f32_ex(x, w, lut, stride, pad, x_range=None, w_range=None, relu=Fa
     OH, OW = _out_hw(desc)
     if OH <= 0 or OW <= 0:
         _check(-2)
-    return _f32_ex(desc, x, w, lut, x_range, w_range, relu, round_mode, acc_out, y_out, workspace, stream,
+    return _f32_ex(desc, x, w, lut, x_range, w_range, relu, round_mode, acc_out, y_out, workspace,
                    (desc.N, OH, OW, desc.Cout))
 
 
 def ax_dense_f32(x, w, lut, x_range=None, w_range=None, relu=False, round_mode=0, acc_out=None, y_out=None, workspace=None,
                  stream=None):
     """x: float32 [M,K]; w: float32 [K,N]; outputs [M,N]."""
+    if stream is not None:
+        return _on_stream(ax_dense_f32, stream, x, w, lut, x_range, w_range, relu, round_mode, acc_out, y_out, workspace)
     L = lib()
     _f32_common(x, w, lut, x_range, w_range)
     if x.dim() != 2 or w.dim() != 2 or w.shape[0] != x.shape[1]:
@@ -857,15 +886,15 @@ def ax_dense_f32(x, w, lut, x_range=None, w_range=None, relu=False, round_mode=0
     N = w.shape[1]
     if _tune_arg() is not None:
         return _f32_ex(_dense_desc(M, K, N), x, w, lut, x_range, w_range, relu, round_mode, acc_out, y_out, workspace,
-                       stream, (M, N))
+                       (M, N))
     acc_out, y_out = _outs((M, N), x.device, acc_out, y_out)
     if workspace is None:
-        workspace = _workspace(ax_dense_f32_workspace_bytes(M, K, N), x.device, stream)
+        workspace = _workspace(ax_dense_f32_workspace_bytes(M, K, N), x.device)
     _dev(workspace, torch.uint8, "workspace")
     rc = L.ax_dense_f32(_ptr(x), M, K, _ptr(w), N, _ptr(lut), _ptr(x_range), _ptr(w_range), int(bool(relu)),
                         int(round_mode), _ptr(None if acc_out is False else acc_out),
                         _ptr(None if y_out is False else y_out), _ptr(workspace), workspace.numel(),
-                        ctypes.c_void_p(_stream_ptr(stream)))
+                        ctypes.c_void_p(_stream_ptr(None)))
     _check(rc)
     return (None if acc_out is False else acc_out), (None if y_out is False else y_out)
 
@@ -1026,7 +1055,7 @@ def ax_rmsnorm_q8(x, weight=None, residual=None, eps=1e-5, normalize=True, sum_o
 
 def _scratch(need: int, workspace, device):
     if workspace is None:
-        return _workspace(need, device, None) if need else None
+        return _workspace(need, device) if need else None
     return _dev(workspace, torch.uint8, "workspace")
 
 

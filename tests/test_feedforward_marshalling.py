@@ -99,44 +99,50 @@ def _every_operator():
             (ax.ax_gated_q8, (q, sc, q, sc, q, sc)), (ax.ax_gated_backward, (gy, x, w, w, gy, gy)), (opt.states, ())]
 
 
+class Streams:
+    """The current stream (a stack), and who allocated and tied what: made holds (address, current stream then), ties (address,
+    stream)."""
+
+    def __init__(self, monkeypatch):
+        self.main, self.side, self.made, self.ties = object(), Side(), [], []
+        self.current = [self.main]
+
+        @contextlib.contextmanager
+        def on(s):
+            self.current.append(s)
+            yield
+            self.current.pop()
+
+        def factory(f):
+            def make(*a, **kw):
+                t = placed(f(*a, **{n: v for n, v in kw.items() if n != "device"}))
+                self.made.append((t.data_ptr(), self.current[-1]))
+                return t
+            return make
+
+        monkeypatch.setattr(torch.cuda, "stream", on)
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: self.current[-1])
+        monkeypatch.setattr(Placed, "record_stream", lambda t, s: self.ties.append((t.data_ptr(), s)), raising=False)
+        for name in ("empty", "empty_like", "empty_strided"):
+            monkeypatch.setattr(torch, name, factory(getattr(torch, name)))
+        monkeypatch.setattr(Placed, "new_empty", factory(torch.Tensor.new_empty), raising=False)
+
+    def check(self, call, args):
+        """What a call allocates belongs to its stream's pool; what it takes is tied to its stream, what it returns to the one
+        that was current."""
+        out = call(*args, stream=self.side)
+        results = [t for t in (out if isinstance(out, tuple) else (out,)) if isinstance(t, torch.Tensor)]
+        results += [ts[0] for ts in out if isinstance(ts, list)] if isinstance(out, tuple) else []
+        assert self.made and results and all(where is self.side for _, where in self.made) and self.current == [self.main]
+        assert all((t.data_ptr(), self.main) in self.ties for t in results)
+        assert all((t.data_ptr(), self.side) in self.ties for t in args if isinstance(t, torch.Tensor))
+
+
 @pytest.mark.parametrize("k", range(10))
 def test_memory_of_calls_on_another_stream(notes, monkeypatch, k):
-    """What a call allocates belongs to its stream's pool; what it takes is tied to its stream, what it returns to the one
-    that was current."""
-    current, side, made, ties = [object()], Side(), [], []
-    main = current[0]
-
-    @contextlib.contextmanager
-    def on(s):
-        current.append(s)
-        yield
-        current.pop()
-
-    def factory(f):
-        def make(*a, **kw):
-            kw["device"] = None if "device" in kw else kw.get("device")
-            t = placed(f(*a, **{n: v for n, v in kw.items() if v is not None}))
-            made.append((t.data_ptr(), current[-1]))
-            return t
-        return make
-
-    monkeypatch.setattr(torch.cuda, "stream", on)
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: current[-1])
-    monkeypatch.setattr(Placed, "record_stream", lambda t, s: ties.append((t.data_ptr(), s)), raising=False)
     call, args = _every_operator()[k]
-    for name in ("empty", "empty_like", "empty_strided"):
-        monkeypatch.setattr(torch, name, factory(getattr(torch, name)))
-    monkeypatch.setattr(Placed, "new_empty", factory(torch.Tensor.new_empty), raising=False)
-    out = call(*args, stream=side)
-    results = [t for t in (out if isinstance(out, tuple) else (out,)) if isinstance(t, torch.Tensor)]
-    results += [t for ts in out if isinstance(ts, list) for t in ts[:1]] if isinstance(out, tuple) else []
-    assert len(notes.calls) == 1 and made and results
-    assert all(where is side for _, where in made) and current == [main]
-    for t in results:
-        assert (t.data_ptr(), main) in ties
-    for t in args:
-        if isinstance(t, torch.Tensor):
-            assert (t.data_ptr(), side) in ties
+    Streams(monkeypatch).check(call, args)
+    assert len(notes.calls) == 1
 
 
 def test_gradients_of_a_step_on_another_stream(notes, monkeypatch):

@@ -6,6 +6,7 @@ import torch
 
 import ff_common as F
 from paper_2002_09481_amd import binding as ax
+from paper_2002_09481_amd import inputs as I
 
 pytestmark = pytest.mark.gpu
 
@@ -77,3 +78,19 @@ def test_what_a_call_on_another_stream_took_may_be_dropped():
     junk = [torch.full((M, K), 7.0, device="cuda"), torch.full((K, N), 7.0, device="cuda")]
     s.synchronize()
     assert torch.equal(y, want) and bool((junk[0] == 7).all())
+
+
+def test_lookup_layers_on_another_stream_leave_freed_memory_alone():
+    x, w, q = I.make_operands(I.Layer("side", 4, 28, 28, 64, 3, 3, 72, 1, 1, x_dist="relu", w_dist="normal"), 1)
+    lut = ax.lut_to_device(I.lut_truncated(4))
+    xd, wd = torch.from_numpy(x).cuda(), torch.from_numpy(w).cuda()
+    acc, y = ax.ax_conv2d(xd, wd, lut, 1, 1, q)
+    gx, gw = ax.ax_conv2d_backward(xd, wd, y, 1, 1, q)
+    s = torch.cuda.Stream()
+    need = ax.ax_conv2d_workspace_bytes(x.shape, w.shape, 1, 1)
+    outs = [(acc.shape, torch.int32), (y.shape, torch.float32), ((need,), torch.uint8), (gx.shape, torch.float32), (gw.shape, torch.float32),
+            ((1 << 24,), torch.uint8)]
+    got = _while_the_current_stream_reads(outs, lambda: ax.ax_conv2d(xd, wd, lut, 1, 1, q, stream=s) +
+                                          ax.ax_conv2d_backward(xd, wd, y, 1, 1, q, stream=s))
+    assert torch.equal(got[0], acc) and torch.equal(got[1], y)
+    assert torch.equal(got[2], gx) and torch.equal(got[3], gw)
