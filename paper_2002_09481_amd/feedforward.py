@@ -21,11 +21,6 @@ import torch
 from . import binding as ax
 
 
-def _on(stream):
-    """The context in which everything, allocations included, belongs to `stream` (None: the current one)."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
-
-
 class FeedForward:
     """width: features of the stream; hidden: features between the projections; dtype: torch.bfloat16 or torch.float32;
     bits: of the optimizer's states (32 or 8)."""
@@ -50,28 +45,34 @@ class FeedForward:
         self._kept = None
 
     def forward(self, x, residual=None, train=False, stream=None):
-        """y [rows, width]; with train, what backward needs is kept until it is called."""
+        """y [rows, width]; with train, what backward needs is kept until it is called, in the place of what an earlier pass
+        left."""
+        if stream is not None:
+            return ax._on_stream(self.forward, stream, x, residual, train)
         p = self.params
-        with _on(stream):
-            n, t, rstd = ax.ax_rmsnorm(x, p["norm"], residual=residual, eps=self.eps, rstd_out=None if train else False)
-            t = x if t is None else t
-            h, g, u = ax.ax_gated(n, p["wg"], p["wu"], act=self.act, save=train)
-            y, _ = ax.ax_matmul(h, p["wd"], bias=p["bias"], residual=t)
+        n, t, rstd = ax.ax_rmsnorm(x, p["norm"], residual=residual, eps=self.eps, rstd_out=None if train else False)
+        t = x if t is None else t
+        h, g, u = ax.ax_gated(n, p["wg"], p["wu"], act=self.act, save=train)
+        y, _ = ax.ax_matmul(h, p["wd"], bias=p["bias"], residual=t)
         if train:
             self._kept = (n, t, rstd, h, g, u)
         return y
 
     def backward(self, gy, stream=None):
         """The gradient of x (and of the residual); those of the parameters are left in self.grads."""
+        if stream is not None:
+            return ax._on_stream(self.backward, stream, gy)
         if self._kept is None:
             raise RuntimeError("backward needs a forward pass with train=True first")
-        n, t, rstd, h, g, u = self._kept
+        n, t, rstd, h, g, u = kept = self._kept
         self._kept = None
+        here = torch.cuda.current_stream(gy.device)
+        for k in kept:  # (of the forward pass's stream; they die before this one has read them)
+            k.record_stream(here)
         p, d = self.params, self.grads
-        with _on(stream):
-            gh, _, _ = ax.ax_matmul_backward(gy, h, p["wd"], gw_out=d["wd"], gb_out=d["bias"])
-            gn, _, _ = ax.ax_gated_backward(gh, n, p["wg"], p["wu"], g, u, act=self.act, gwg_out=d["wg"], gwu_out=d["wu"])
-            gx, _ = ax.ax_rmsnorm_backward(gn, t, p["norm"], rstd, gsum=gy, gw_out=d["norm"])
+        gh, _, _ = ax.ax_matmul_backward(gy, h, p["wd"], gw_out=d["wd"], gb_out=d["bias"])
+        gn, _, _ = ax.ax_gated_backward(gh, n, p["wg"], p["wu"], g, u, act=self.act, gwg_out=d["wg"], gwu_out=d["wu"])
+        gx, _ = ax.ax_rmsnorm_backward(gn, t, p["norm"], rstd, gsum=gy, gw_out=d["norm"])
         return gx
 
     def step(self, lr, weight_decay=0.0, grad_scale=None, stream=None, **betas):
@@ -90,7 +91,7 @@ class QuantizedFeedForward:
 
     def __init__(self, block: FeedForward, stream=None):
         self.act, self.eps, self.dtype = block.act, block.eps, block.dtype
-        with _on(stream):
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
             self.norm, self.bias = block.params["norm"].clone(), block.params["bias"].clone()
             self.w = {}
             for name in ("wg", "wu", "wd"):  # [inputs, outputs] -> codes [outputs, inputs], a scale an output
@@ -98,9 +99,10 @@ class QuantizedFeedForward:
                 self.w[name] = (codes, scales)
 
     def forward(self, x, residual=None, stream=None):
-        with _on(stream):
-            codes, scales, t, _ = ax.ax_rmsnorm_q8(x, self.norm, residual=residual, eps=self.eps)
-            t = x if t is None else t
-            h = ax.ax_gated_q8(codes, scales, *self.w["wg"], *self.w["wu"], act=self.act, out_dtype=self.dtype)
-            hc, hs, _, _ = ax.ax_rmsnorm_q8(h, normalize=False)
-            return ax.ax_matmul_q8(hc, hs, *self.w["wd"], bias=self.bias, residual=t, out_dtype=self.dtype)
+        if stream is not None:
+            return ax._on_stream(self.forward, stream, x, residual)
+        codes, scales, t, _ = ax.ax_rmsnorm_q8(x, self.norm, residual=residual, eps=self.eps)
+        t = x if t is None else t
+        h = ax.ax_gated_q8(codes, scales, *self.w["wg"], *self.w["wu"], act=self.act, out_dtype=self.dtype)
+        hc, hs, _, _ = ax.ax_rmsnorm_q8(h, normalize=False)
+        return ax.ax_matmul_q8(hc, hs, *self.w["wd"], bias=self.bias, residual=t, out_dtype=self.dtype)

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2002_09481_amd import binding as ax
+from paper_2002_09481_amd.feedforward import FeedForward
 
 
 class Placed(torch.Tensor):
@@ -154,3 +155,34 @@ def test_gradients_of_a_step_on_another_stream(notes, monkeypatch):
     assert not ties
     opt.step(1e-3, 2, grad_scale=factor, stream=side)
     assert (g.data_ptr(), side) in ties and (factor.data_ptr(), side) in ties
+
+
+def _kept_block():
+    f = lambda *s: floats(*s, dtype=torch.float32)  # noqa: E731
+    b = FeedForward.__new__(FeedForward)
+    b.width, b.hidden, b.act, b.dtype, b.eps = 16, 24, "silu", torch.float32, 1e-5
+    b.params = {"wg": f(16, 24), "wu": f(16, 24), "wd": f(24, 16), "norm": f(16), "bias": f(16)}
+    b.grads = {n: torch.zeros_like(t) for n, t in b.params.items()}
+    b._kept = (f(4, 16), f(4, 16), f(4), f(4, 24), f(4, 24), f(4, 24))
+    return b
+
+
+@pytest.mark.parametrize("way", ["argument", "current"])
+def test_what_a_backward_pass_on_another_stream_drops(notes, monkeypatch, way):
+    """The forward pass left it in another stream's pool: it is tied to the stream that reads it before it dies."""
+    b, gy, s = _kept_block(), floats(4, 16, dtype=torch.float32), Streams(monkeypatch)
+    kept = [t.data_ptr() for t in b._kept]
+    if way == "argument":
+        gx = b.backward(gy, stream=s.side)
+        assert (gx.data_ptr(), s.main) in s.ties
+    else:
+        with torch.cuda.stream(s.side):
+            b.backward(gy)
+    assert b._kept is None and all((k, s.side) in s.ties for k in kept)
+    assert notes.calls == ["ax_matmul_backward", "ax_gated_backward", "ax_rmsnorm_backward"]
+
+
+def test_results_of_a_block_on_another_stream(notes, monkeypatch):
+    b, s = _kept_block(), Streams(monkeypatch)
+    x, r = floats(4, 16, dtype=torch.float32), floats(4, 16, dtype=torch.float32)
+    s.check(b.forward, (x, r))
