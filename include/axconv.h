@@ -449,8 +449,9 @@ size_t ax_rmsnorm_backward_workspace_bytes(const ax_norm_desc_t* desc);
  *   z_out (may be NULL) [M, N] with pitch N, kept for the backward pass
  * bias and residual may be NULL; y_out may be residual itself, with its pitch.  dtype is the type of x and w, out_dtype that of bias, residual, z
  * and y.  AX_BF16 products are exact in float32 and summed there.  AX_F32 operands are taken as three
- * bf16 pieces each (exact together) and six of their nine products; what is dropped is below 2^-24
- * of a product, so results are those of a float32 product (but an infinity in an operand may give NaN).
+ * bf16 pieces each (exact together, each rounded to nearest) and six of their nine products; what is
+ * dropped is within 2^-24 (1 + 2^-8) of a product and of either sign, so results are those of a float32
+ * product (but an infinity in an operand may give NaN).
  * Operands that the kernels cannot read in place (AX_F32; rows that are not 16-byte aligned or whose
  * length is no multiple of 16 bytes) are copied into the workspace first.
  * workspace: ax_matmul_workspace_bytes(desc) bytes, 256-byte aligned.

@@ -75,33 +75,41 @@ __device__ __forceinline__ void store_elems(void* p, long long i, int left, cons
     }
 }
 
-// a = p0 + p1 + p2 exactly: each piece is what is left, cut after eight significant bits.  An infinity or a NaN goes into
-// the first piece alone; what it meets comes out as NaN or infinity (not always the one that float32 gives: a piece of the
-// other factor may be zero).
-__device__ __forceinline__ void split3(float a, uint32_t& p0, uint32_t& p1, uint32_t& p2) {
-  const uint32_t b = __float_as_uint(a);
-  if ((b & 0x7f800000u) == 0x7f800000u) {
-    p0 = (b >> 16) | ((b & 0x7fffffu) ? 0x40u : 0u);
-    p1 = p2 = 0;
-    return;
-  }
-  const float r1 = a - __uint_as_float(b & 0xffff0000u);
-  const uint32_t b1 = __float_as_uint(r1);
-  const float r2 = r1 - __uint_as_float(b1 & 0xffff0000u);
-  p0 = b >> 16;
-  p1 = b1 >> 16;
-  p2 = __float_as_uint(r2) >> 16;
-}
-
-// Eight float32 values in three pieces, smallest pieces last.
+// Eight float32 values in three pieces, smallest pieces last: v = p0 + p1 + p2 exactly (down to 2^-133, the least that a bf16
+// holds), each piece what is left, rounded to nearest.  So the pieces of a product that are left out (p1 q2, p2 q1, p2 q2) are
+// within 2^-24 (1 + 2^-8) of it, of either sign: 2^-27 in the root mean square over normal factors.  (Pieces that are cut
+// instead have the value's sign: up to 7.8 2^-24 left out, 0.7 on average, always towards zero.)  A value that would round to
+// infinity has its first piece cut.  An infinity or a NaN goes into the first piece alone; what it meets comes out as NaN
+// or infinity (not always the one that float32 gives: a piece of the other factor may be zero).
 __device__ __forceinline__ void pieces_of(const float (&v)[8], u32x4 (&p)[3]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+  const bool plain = top < 0x7f7f8000u;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    uint32_t a[3], b[3];
-    split3(v[2 * e], a[0], a[1], a[2]);
-    split3(v[2 * e + 1], b[0], b[1], b[2]);
+    float r[2] = {v[2 * e], v[2 * e + 1]};
+    uint32_t q = pack_bf16(r[0], r[1]);
+    if (!plain) {
+      q = 0;
 #pragma unroll
-    for (int k = 0; k < 3; ++k) p[k][e] = a[k] | (b[k] << 16);
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t b = __float_as_uint(r[h]), a = b & 0x7fffffffu;
+        q |= (a < 0x7f7f8000u ? f32_to_bf16(r[h]) : (b >> 16) | (a > 0x7f800000u ? 0x40u : 0u)) << (16 * h);
+      }
+    }
+    p[0][e] = q;
+    r[0] -= __uint_as_float(q << 16);
+    r[1] -= __uint_as_float(q & 0xffff0000u);
+    if (!plain) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if ((__float_as_uint(v[2 * e + h]) & 0x7f800000u) == 0x7f800000u) r[h] = 0.f;
+    }
+    p[1][e] = q = pack_bf16(r[0], r[1]);
+    r[0] -= __uint_as_float(q << 16);
+    r[1] -= __uint_as_float(q & 0xffff0000u);
+    p[2][e] = (__float_as_uint(r[0]) >> 16) | (__float_as_uint(r[1]) & 0xffff0000u);
   }
 }
 

@@ -237,7 +237,7 @@ struct Acc<true> {
 // and that this stage's place is free, and the copies of stage + STAGES are asked for.
 //
 // P = 3: float32 operands as three bf16 pieces, a = a1 + a2 + a3 and b alike.  A stage holds all pieces of its part of both,
-// and each fragment is used in several of the six products of pieces that can reach 2^-24 of a b, the smallest added first:
+// and each fragment is used in several of the six products of pieces that can pass 2^-24 of a b, the smallest added first:
 // half the copies and a third of the LDS reads that six passes over pairs of pieces would take.
 template <bool I8, int P, int LA, int LB, int NB, int BM, int BN, int WM, int WN, int KB, int STAGES, int OCC>
 __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {

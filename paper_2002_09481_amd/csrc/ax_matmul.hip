@@ -6,7 +6,7 @@
 //
 // The matrix instructions take bf16 (or int8) operands.  float32 operands are cut into three bf16 pieces,
 // a = a1 + a2 + a3 exactly (eight significant bits each), and six of the nine products of pieces are added: what is left out
-// is below 2^-24 of a b.  That is 6 / 16 of the cost of the float32 matrix instruction, at its precision.
+// is within 2^-24 (1 + 2^-8) of a b, of either sign.  That is 6 / 16 of the cost of the float32 matrix instruction, at its precision.
 #include <algorithm>
 
 #include "ax_float.h"
