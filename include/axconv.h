@@ -394,6 +394,8 @@ size_t ax_conv2d_backward_workspace_bytes(const ax_conv_desc_t* desc);
 #define AX_ACT_RELU 1
 #define AX_ACT_SILU 2 /* z / (1 + exp(-z)) */
 #define AX_ACT_GELU 3 /* z * (1 + erf(z / sqrt 2)) / 2 */
+/* Float32 results are evaluated to within 14 2^-24 (gelu) and 8 2^-24 (silu) of themselves, the far tails of gelu
+ * included; results in bf16 to within 1.2e-4 and 1.2e-5 in front of their rounding. */
 
 /*
  * Root-mean-square norm of rows with the residual's addition in front:

@@ -289,7 +289,8 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
     if (NB == 1 && g.bias) v[0] += get(g.bias, n);
     if (g.z) put(g.z, (long long)m * g.N + n, v[0]);
     if (NB == 2 && g.z2) put(g.z2, (long long)m * g.N + n, s[1]);
-    apply_act(v, g.act);
+    if (g.odt == AX_F32) apply_act<true>(v, g.act);
+    else apply_act<false>(v, g.act);
     if (NB == 2) v[0] *= s[1];
     if (NB == 1 && g.res) v[0] += get(g.res, (long long)m * g.ldr + n);
     put(g.y, (long long)m * g.ldy + n, v[0]);

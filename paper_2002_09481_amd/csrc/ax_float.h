@@ -113,27 +113,72 @@ __device__ __forceinline__ void pieces_of(const float (&v)[8], u32x4 (&p)[3]) {
   }
 }
 
-// Activations in float32, with the fast exponential and reciprocal (a few units in the last place each), against results
-// that are rounded to bf16 or compared in the norm.  The normal distribution function of gelu is 7.1.26 of Abramowitz and
-// Stegun's Handbook of Mathematical Functions: erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2) with t = 1 / (1 + 0.3275911 x),
-// off by at most 1.5e-7 for x >= 0, here with the halves of the coefficients and x = |z| / sqrt 2.  (The library's erf
-// takes three times as many instructions: 17 us for a 256 x 256 tile of a compute unit, of 86 for the whole tile.)
-__device__ __forceinline__ float normal_cdf(float z, float gauss) {  // gauss = exp(-z^2 / 2)
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(fabsf(z), 0.231641888f, 1.0f));
-  float p = __builtin_fmaf(t, 0.5307027145f, -0.7265760135f);
-  p = __builtin_fmaf(t, p, 0.7107068705f);
-  p = __builtin_fmaf(t, p, -0.142248368f);
-  p = __builtin_fmaf(t, p, 0.127414796f);
+// Activations.  EXACT: for results in float32, otherwise for results that are rounded to bf16, with the fast exponential and
+// reciprocal: relative errors of 1.2e-4 at most, far out, where 2^-9 is half a unit.
+//
+// The normal distribution function of gelu is exp(-z^2 / 2) t P(t) for z < 0 and one minus that for z > 0, t = 1 / (1 + c |z|).
+// P is fitted to the scaled function over 0 <= |z| <= 14.2, so that the tail keeps its leading digits where it is far below one:
+// nine coefficients for the smallest largest relative error, 1.3e-8, and six within 5.4e-8 and, where that says less, relatively
+// within 1.1e-4.  Evaluated in float32, over -12.5 < z < 12.5: z times the long form within 7.7 2^-24 of it, the short form
+// within 2.2e-7 and relatively within 1.2e-4.  (The library's erf takes three times the instructions of the short form, and
+// 1 + erf has no digits left in the tail.)
+__device__ __forceinline__ float rcp_near(float d) {  // 1 / d of normal d, to within a unit in the last place
+  const float t = __builtin_amdgcn_rcpf(d);
+  return __builtin_fmaf(__builtin_fmaf(-d, t, 1.0f), t, t);
+}
+// exp(x + low) of a finite x <= 0 and a low below x's last place: 2^(x log2 e) with what the product loses put back.
+__device__ __forceinline__ float exp_near(float x, float low) {
+  const float q = x * 1.44269504f, r = __builtin_fmaf(x, 1.44269504f, -q);
+  const float e = __builtin_amdgcn_exp2f(q);
+  return __builtin_fmaf(e, __builtin_fmaf(x, 1.92596303e-8f * 0.693147181f, __builtin_fmaf(r, 0.693147181f, low)), e);
+}
+template <bool EXACT>
+__device__ __forceinline__ float gauss_of(float x) {  // exp(-x^2 / 2) of x >= 0 (EXACT: up to 64)
+  if (!EXACT) return __expf(-0.5f * x * x);
+  const float q = x * x;
+  return exp_near(-0.5f * q, -0.5f * __builtin_fmaf(x, x, -q));
+}
+template <bool EXACT>
+__device__ __forceinline__ float normal_cdf(float z, float& gauss) {  // gauss = exp(-z^2 / 2)
+  const float x = EXACT && fabsf(z) > 64.f ? 64.f : fabsf(z);  // (NaN stays; both are 0 or 1 from there on)
+  gauss = gauss_of<EXACT>(x);
+  float p;
+  const float d = __builtin_fmaf(x, EXACT ? 0.265f : 0.29f, 1.0f);
+  const float t = EXACT ? rcp_near(d) : __builtin_amdgcn_rcpf(d);
+  if (EXACT) {
+    p = __builtin_fmaf(t, 0.0307411347f, -0.143851921f);
+    p = __builtin_fmaf(t, p, 0.217057899f);
+    p = __builtin_fmaf(t, p, -0.115519196f);
+    p = __builtin_fmaf(t, p, 0.137384608f);
+    p = __builtin_fmaf(t, p, 0.0605500154f);
+    p = __builtin_fmaf(t, p, 0.102641486f);
+    p = __builtin_fmaf(t, p, 0.105254889f);
+    p = __builtin_fmaf(t, p, 0.105741084f);
+  } else {
+    p = __builtin_fmaf(t, -0.0892740786f, 0.286521465f);
+    p = __builtin_fmaf(t, p, -0.0954555646f);
+    p = __builtin_fmaf(t, p, 0.181015849f);
+    p = __builtin_fmaf(t, p, 0.100275196f);
+    p = __builtin_fmaf(t, p, 0.116917126f);
+  }
   const float tail = p * t * gauss;
   return z > 0.f ? 1.f - tail : tail;
 }
-__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
-__device__ __forceinline__ float gelu(float z) {
-  const float y = z * normal_cdf(z, __expf(-0.5f * z * z));
-  return z < -14.f ? -0.f : y;  // (-infinity times zero; the product is below float32 there)
+// 1 / (1 + exp(-z)), and one minus it
+template <bool EXACT>
+__device__ __forceinline__ float sigmoid(float z, float& rest) {
+  if (!EXACT) {
+    const float g = __builtin_amdgcn_rcpf(1.f + __expf(-z));
+    rest = 1.f - g;
+    return g;
+  }
+  const float x = fabsf(z) > 128.f ? 128.f : fabsf(z);  // (NaN stays; the exponential is 0 from there on)
+  const float e = exp_near(-x, 0.f), r = rcp_near(1.f + e), s = e * r;
+  rest = z > 0.f ? s : r;
+  return z > 0.f ? r : s;
 }
 
-template <int E>
+template <bool EXACT, int E>
 __device__ __forceinline__ void apply_act(float (&v)[E], int act) {
   switch (act) {
     case AX_ACT_RELU:
@@ -142,17 +187,24 @@ __device__ __forceinline__ void apply_act(float (&v)[E], int act) {
       break;
     case AX_ACT_SILU:
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] *= sigmoid(v[e]);
+      for (int e = 0; e < E; ++e) {
+        float rest;
+        v[e] *= sigmoid<EXACT>(v[e], rest);
+      }
       break;
     case AX_ACT_GELU:
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = gelu(v[e]);
+      for (int e = 0; e < E; ++e) {
+        float gauss;
+        const float y = v[e] * normal_cdf<EXACT>(v[e], gauss);
+        v[e] = v[e] < -14.2f ? -0.f : y;  // (-infinity times zero; the product is below float32 there)
+      }
       break;
     default: break;
   }
 }
 // v = act(z), s = act'(z)
-template <int E>
+template <bool EXACT, int E>
 __device__ __forceinline__ void act_and_slope(const float (&z)[E], int act, float (&v)[E], float (&s)[E]) {
   switch (act) {
     case AX_ACT_RELU:
@@ -165,17 +217,19 @@ __device__ __forceinline__ void act_and_slope(const float (&z)[E], int act, floa
     case AX_ACT_SILU:
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float g = sigmoid(z[e]);
+        float rest;
+        const float g = sigmoid<EXACT>(z[e], rest);
         v[e] = z[e] * g;
-        s[e] = g * (1.f + z[e] * (1.f - g));
+        s[e] = g * (1.f + z[e] * rest);
       }
       break;
     case AX_ACT_GELU:
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float x = __expf(-0.5f * z[e] * z[e]), c = normal_cdf(z[e], x);
-        v[e] = z[e] < -14.f ? -0.f : z[e] * c;
-        s[e] = c + (x > 0.f ? z[e] * x * 0.39894228040143268f : 0.f);
+        float gauss;
+        const float c = normal_cdf<EXACT>(z[e], gauss);
+        v[e] = z[e] < -14.2f ? -0.f : z[e] * c;
+        s[e] = c + (gauss > 0.f ? z[e] * gauss * 0.39894228040143268f : 0.f);
       }
       break;
     default:

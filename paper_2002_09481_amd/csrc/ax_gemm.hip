@@ -50,14 +50,20 @@ __device__ __forceinline__ void store8(void* p, long long i, int dt, int left, c
   else store_elems<false, 8>(p, i, left, v);
 }
 
+// Type of the results, known to the kernel or not.  It decides the form of the activation: with both forms in the epilogue of
+// a 256 x 256 tile the compiler no longer unrolls it, and the sums go through scratch memory.
+constexpr int kAnyOut = 2;
+template <int OT>
+__device__ __forceinline__ int out_type(const GemmArgs& g) { return OT == kAnyOut ? g.odt : OT; }
+
 // What the epilogue needs of eight columns, the same for all rows.
 struct Columns {
   float bias[8], ws[8], ws2[8];
 };
-template <bool I8, bool GATED>
+template <bool I8, bool GATED, int OT>
 __device__ __forceinline__ void load_columns(const GemmArgs& g, int n, Columns& c) {
   const int left = g.N - n;
-  if (!GATED && g.bias) load8(g.bias, n, g.odt, left, c.bias);
+  if (!GATED && g.bias) load8(g.bias, n, out_type<OT>(g), left, c.bias);
   if (I8) load_elems<true, 8>(g.ws, n, left, c.ws);
   if (I8 && GATED) load_elems<true, 8>(g.ws2, n, left, c.ws2);
 }
@@ -66,11 +72,11 @@ __device__ __forceinline__ void load_columns(const GemmArgs& g, int n, Columns& 
 struct Ahead {
   u32x4 q[2];
 };
-template <bool I8, bool GATED>
+template <bool I8, bool GATED, int OT>
 __device__ __forceinline__ void look_ahead(const GemmArgs& g, int m, int n, Ahead& a) {
   if (!I8 || GATED || !g.res || n + 8 > g.N) return;
   const long long i = (long long)m * g.ldr + n;
-  if (g.odt == AX_F32) {
+  if (out_type<OT>(g) == AX_F32) {
     a.q[0] = load_any<u32x4>((const float*)g.res + i);
     a.q[1] = load_any<u32x4>((const float*)g.res + i + 4);
   } else {
@@ -79,9 +85,9 @@ __device__ __forceinline__ void look_ahead(const GemmArgs& g, int m, int n, Ahea
 }
 // Columns n .. n + 7 of row m from their finished sums (GATED: of both projections; int8: sums as integers in s and s2).
 // second: the second output of a dual launch.
-template <bool I8, bool GATED>
+template <bool I8, bool GATED, int OT>
 __device__ __forceinline__ void finish(const GemmArgs& g, const Columns& c, const Ahead& a, int m, int n, const f32x4 (&s)[2], const f32x4 (&s2)[2], int second) {
-  const int left = g.N - n;
+  const int left = g.N - n, odt = out_type<OT>(g);
   float v[8], u[8];
   const float xs = I8 ? g.xs[m] : 1.f;
 #pragma unroll
@@ -93,25 +99,26 @@ __device__ __forceinline__ void finish(const GemmArgs& g, const Columns& c, cons
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += c.bias[e];
   }
-  if (g.z) store8(g.z, (long long)m * g.N + n, g.odt, left, v);
-  if (GATED && g.z2) store8(g.z2, (long long)m * g.N + n, g.odt, left, u);
-  apply_act(v, g.act);
+  if (g.z) store8(g.z, (long long)m * g.N + n, odt, left, v);
+  if (GATED && g.z2) store8(g.z2, (long long)m * g.N + n, odt, left, u);
+  if (odt == AX_F32) apply_act<true>(v, g.act);
+  else apply_act<false>(v, g.act);
   if (GATED) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= u[e];
   }
   if (!GATED && g.res) {
     if (!I8 || left < 8) {
-      load8(g.res, (long long)m * g.ldr + n, g.odt, left, u);
+      load8(g.res, (long long)m * g.ldr + n, odt, left, u);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        u[e] = g.odt == AX_F32 ? __uint_as_float(a.q[e >> 2][e & 3]) : bf16_to_f32((a.q[0][e >> 1] >> (16 * (e & 1))) & 0xffffu);
+        u[e] = odt == AX_F32 ? __uint_as_float(a.q[e >> 2][e & 3]) : bf16_to_f32((a.q[0][e >> 1] >> (16 * (e & 1))) & 0xffffu);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += u[e];
   }
-  store8(!GATED && second ? g.y2 : g.y, (long long)m * g.ldy + n, g.odt, left, v);
+  store8(!GATED && second ? g.y2 : g.y, (long long)m * g.ldy + n, odt, left, v);
 }
 
 // ---- main kernel -------------------------------------------------------------------------------
@@ -239,7 +246,8 @@ struct Acc<true> {
 // P = 3: float32 operands as three bf16 pieces, a = a1 + a2 + a3 and b alike.  A stage holds all pieces of its part of both,
 // and each fragment is used in several of the six products of pieces that can pass 2^-24 of a b, the smallest added first:
 // half the copies and a third of the LDS reads that six passes over pairs of pieces would take.
-template <bool I8, int P, int LA, int LB, int NB, int BM, int BN, int WM, int WN, int KB, int STAGES, int OCC>
+// OT: type of the results.
+template <bool I8, int P, int LA, int LB, int NB, int BM, int BN, int WM, int WN, int KB, int STAGES, int OCC, int OT>
 __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   constexpr int THREADS = 64 * WM * WN;
   constexpr int BNS = BN / NB;                // columns of one right operand
@@ -474,7 +482,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   const int orow = lane / LPR, ocol = lane % LPR * 8;
   const int n = n0 + wcol + ocol;
   Columns cols;
-  if (a.splits == 1 && n < g.N) load_columns<I8, NB == 2>(g, n, cols);
+  if (a.splits == 1 && n < g.N) load_columns<I8, NB == 2, OT>(g, n, cols);
 #pragma unroll
   for (int i0 = 0; i0 < MF; i0 += ROUND / 16) {
 #pragma unroll
@@ -489,7 +497,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
 #pragma unroll
     for (int r = 0; r < ROUND / RPI; ++r) {
       const int m = m0 + wrow + 16 * i0 + r * RPI + orow;
-      if (a.splits == 1 && m < g.M && n < g.N) look_ahead<I8, NB == 2>(g, m, n, ahead[r]);
+      if (a.splits == 1 && m < g.M && n < g.N) look_ahead<I8, NB == 2, OT>(g, m, n, ahead[r]);
     }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -515,7 +523,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
           *(f32x4*)(p + plane + 4) = s2[1];
         }
       } else {
-        finish<I8, NB == 2>(g, cols, ahead[r / RPI], m, n, s, s2, second);
+        finish<I8, NB == 2, OT>(g, cols, ahead[r / RPI], m, n, s, s2, second);
       }
     }
     __builtin_amdgcn_wave_barrier();
@@ -552,9 +560,9 @@ __global__ __launch_bounds__(256) void gemm_join_kernel(const Args a) {
     const long long r = i - (second ? (long long)g.M * groups : 0);
     const int m = (int)(r / groups), n = (int)(r - (long long)m * groups) * 8;
     Columns cols;
-    load_columns<I8, GATED>(g, n, cols);
+    load_columns<I8, GATED, kAnyOut>(g, n, cols);
     Ahead ahead;
-    look_ahead<I8, GATED>(g, m, n, ahead);
+    look_ahead<I8, GATED, kAnyOut>(g, m, n, ahead);
     f32x4 s[2][2];
 #pragma unroll
     for (int pl = 0; pl < (GATED ? 2 : 1); ++pl)
@@ -563,7 +571,7 @@ __global__ __launch_bounds__(256) void gemm_join_kernel(const Args a) {
         const float* p = a.part + (long long)(second + pl) * plane + (long long)m * a.ldp + n + 4 * h;
         s[pl][h] = sum_slices<I8>(p, (long long)planes * plane, a.splits);
       }
-    finish<I8, GATED>(g, cols, ahead, m, n, s[0], s[GATED ? 1 : 0], second);
+    finish<I8, GATED, kAnyOut>(g, cols, ahead, m, n, s[0], s[GATED ? 1 : 0], second);
   }
 }
 
@@ -586,24 +594,38 @@ constexpr int kNumTiles3 = 2;
 constexpr TileShape kTiles3[kNumTiles3] = {{128, 128, 64, 1, 5.0, 2.1, 2.1}, {64, 128, 64, 2, 4.0, 1.25, 2.1}};
 constexpr double kStep3Along = 2.6;
 
-template <bool I8, int LA, int LB, int NB>
-void launch_tile(const Args& a, int tile, int grid, hipStream_t s) {
+template <bool I8, int LA, int LB, int NB, int OT>
+void launch_out(const Args& a, int tile, int grid, hipStream_t s) {
   switch (tile) {
-    case 0: gemm_kernel<I8, 1, LA, LB, NB, 256, 256, 2, 4, 128, 2, 2><<<grid, 512, 0, s>>>(a); break;
-    case 1: gemm_kernel<I8, 1, LA, LB, NB, 128, 128, 2, 2, 128, 2, 2><<<grid, 256, 0, s>>>(a); break;
-    case 2: gemm_kernel<I8, 1, LA, LB, NB, 64, 128, 1, 4, 128, 3, 2><<<grid, 256, 0, s>>>(a); break;
+    case 0: gemm_kernel<I8, 1, LA, LB, NB, 256, 256, 2, 4, 128, 2, 2, OT><<<grid, 512, 0, s>>>(a); break;
+    case 1: gemm_kernel<I8, 1, LA, LB, NB, 128, 128, 2, 2, 128, 2, 2, OT><<<grid, 256, 0, s>>>(a); break;
+    case 2: gemm_kernel<I8, 1, LA, LB, NB, 64, 128, 1, 4, 128, 3, 2, OT><<<grid, 256, 0, s>>>(a); break;
     default:  // (copies of 32 columns whose rows are the contraction would not fill the threads)
-      if constexpr (LA == 0) gemm_kernel<I8, 1, LA, LB, NB, 32, 128, 1, 4, 128, 3, 2><<<grid, 256, 0, s>>>(a);
+      if constexpr (LA == 0) gemm_kernel<I8, 1, LA, LB, NB, 32, 128, 1, 4, 128, 3, 2, OT><<<grid, 256, 0, s>>>(a);
       break;
   }
 }
-template <int LA, int LB, int NB>
-void launch_tile3(const Args& a, int tile, int grid, hipStream_t s) {
+template <bool I8, int LA, int LB, int NB>
+void launch_tile(const Args& a, int tile, int grid, hipStream_t s) {
+  if constexpr (LA == 0) {  // (the weight's gradient has the operands' type)
+    if (a.g.odt == AX_F32) return launch_out<I8, LA, LB, NB, AX_F32>(a, tile, grid, s);
+  }
+  launch_out<I8, LA, LB, NB, AX_BF16>(a, tile, grid, s);
+}
+template <int LA, int LB, int NB, int OT>
+void launch_out3(const Args& a, int tile, int grid, hipStream_t s) {
   if (tile == 0) {
     // eight waves (4096^3: 583 us with its copies, 605 with four); the gated pair's 64 columns a weight do not fill their copies
-    if constexpr (NB == 1) gemm_kernel<false, 3, LA, LB, NB, 128, 128, 2, 4, 64, 3, 2><<<grid, 512, 0, s>>>(a);
-    else gemm_kernel<false, 3, LA, LB, NB, 128, 128, 2, 2, 64, 3, 1><<<grid, 256, 0, s>>>(a);
-  } else gemm_kernel<false, 3, LA, LB, NB, 64, 128, 2, 2, 64, 2, 2><<<grid, 256, 0, s>>>(a);
+    if constexpr (NB == 1) gemm_kernel<false, 3, LA, LB, NB, 128, 128, 2, 4, 64, 3, 2, OT><<<grid, 512, 0, s>>>(a);
+    else gemm_kernel<false, 3, LA, LB, NB, 128, 128, 2, 2, 64, 3, 1, OT><<<grid, 256, 0, s>>>(a);
+  } else gemm_kernel<false, 3, LA, LB, NB, 64, 128, 2, 2, 64, 2, 2, OT><<<grid, 256, 0, s>>>(a);
+}
+template <int LA, int LB, int NB>
+void launch_tile3(const Args& a, int tile, int grid, hipStream_t s) {
+  if constexpr (LA == 0) {
+    if (a.g.odt == AX_BF16) return launch_out3<LA, LB, NB, AX_BF16>(a, tile, grid, s);
+  }
+  launch_out3<LA, LB, NB, AX_F32>(a, tile, grid, s);
 }
 
 constexpr int kCus = 256;

@@ -217,7 +217,7 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const GradArgs a, const P
       if (GATED || a.z) load_elems<DT == AX_F32, 8>(a.z, (long long)r * a.N + c, left, z);
       if (GATED || a.z) {
         float v[8], sl[8];
-        act_and_slope(z, a.act, v, sl);
+        act_and_slope<DT == AX_F32>(z, a.act, v, sl);
         if (GATED) {
           load_elems<DT == AX_F32, 8>(a.u, (long long)r * a.N + c, left, u);
           for (int e = 0; e < 8; ++e) {
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(256) void outer_kernel(const OuterArgs a) {
     if (!a.z) return;
     float z[8], v[8], sl[8];
     load_elems<F32, 8>(a.z, (long long)m * a.N + i, left, z);
-    act_and_slope(z, a.act, v, sl);
+    act_and_slope<DT == AX_F32>(z, a.act, v, sl);
     if (GATED) {
       float u[8];
       load_elems<F32, 8>(a.u, (long long)m * a.N + i, left, u);
