@@ -9,7 +9,7 @@
 //
 // Measured (us): bf16 8192^3 840 to 930 (1180 to 1310 TF), 4096^3 103 (1340 TF), gradient of a weight 8192^3 780 (1400 TF);
 // gated 8192 x 4096 -> 16384 with both projections stored 1735 to 1800 (1220 to 1270 TF); int8 8192^3 520 (2100 TOP);
-// float32 4096^3 583 (236 TF, six products each).
+// float32 4096^3 690 to 700 (196 to 199 TF, six products each).
 #include <algorithm>
 #include <type_traits>
 
@@ -587,9 +587,9 @@ constexpr TileShape kTiles[kNumTiles] = {{256, 256, 128, 1, 6.0, 1.50, 1.50},
                                          {128, 128, 128, 2, 3.0, 0.70, 0.95},
                                          {64, 128, 128, 2, 2.5, 0.39, 0.65},
                                          {32, 128, 128, 2, 2.0, 0.30, 0.45}};
-// float32 operands (three pieces; six products in the time).  Two of the small ones in a compute unit that read both operands
-// along the contraction: kStep3Along (1531 x 1000 -> 2048: 54.8 us a call with the large tile, 60.7 with the small one; 2000 x
-// 2048 -> 2048 101.8 and 121.6).
+// float32 operands (three pieces; six products in the time).  Two of the small ones in a compute unit take the time of a large
+// one, which therefore pays only where they read both operands along the contraction: kStep3Along (1531 x 1000 -> 2048: 54.8 us
+// a call with the large tile, 60.7 with the small one; 2000 x 2048 -> 2048 101.8 and 121.6).
 constexpr int kNumTiles3 = 2;
 constexpr TileShape kTiles3[kNumTiles3] = {{128, 128, 64, 1, 5.0, 2.1, 2.1}, {64, 128, 64, 2, 4.0, 1.25, 2.1}};
 constexpr double kStep3Along = 2.6;
@@ -614,11 +614,13 @@ void launch_tile(const Args& a, int tile, int grid, hipStream_t s) {
 }
 template <int LA, int LB, int NB, int OT>
 void launch_out3(const Args& a, int tile, int grid, hipStream_t s) {
-  if (tile == 0) {
-    // eight waves (4096^3: 583 us with its copies, 605 with four); the gated pair's 64 columns a weight do not fill their copies
-    if constexpr (NB == 1) gemm_kernel<false, 3, LA, LB, NB, 128, 128, 2, 4, 64, 3, 2, OT><<<grid, 512, 0, s>>>(a);
-    else gemm_kernel<false, 3, LA, LB, NB, 128, 128, 2, 2, 64, 3, 1, OT><<<grid, 256, 0, s>>>(a);
-  } else gemm_kernel<false, 3, LA, LB, NB, 64, 128, 2, 2, 64, 2, 2, OT><<<grid, 256, 0, s>>>(a);
+  if constexpr (LA == 0 && LB == 0) {
+    if (tile == 0) {
+      gemm_kernel<false, 3, LA, LB, NB, 128, 128, 2, 4, 64, 3, 2, OT><<<grid, 512, 0, s>>>(a);
+      return;
+    }
+  }
+  gemm_kernel<false, 3, LA, LB, NB, 64, 128, 2, 2, 64, 2, 2, OT><<<grid, 256, 0, s>>>(a);
 }
 template <int LA, int LB, int NB>
 void launch_tile3(const Args& a, int tile, int grid, hipStream_t s) {
@@ -653,6 +655,7 @@ GemmPlan plan_gemm(const GemmArgs& g) {
   for (int t = 0; t < (three ? kNumTiles3 : kNumTiles); ++t) {
     const TileShape& T = shape_of(g, t);
     if (T.bm == 32 && g.la != 0) continue;
+    if (three && t == 0 && (g.la != 0 || g.lb != 0)) continue;
     const long long steps = (kbytes + T.kb - 1) / T.kb * g.nseg;
     const long long tiles = tiles_of(g, T);
     const double step = three && t == 1 && g.la == 0 && g.lb == 0 ? kStep3Along : T.step;
