@@ -72,6 +72,24 @@ int ax_probe_layer_kernel_ms(const ax_layer_t* layer, const void* x, int32_t* ac
 int ax_probe_layer_route(const ax_layer_t* layer, int* kernel, int* pixels, int* channels, int* tiles,
                          int* workgroups, int* threads);
 
+/*
+ * Which kernel a feed-forward product runs and how it is cut (host arithmetic only, nothing is launched).
+ *   product     AX_PRODUCT_*: the call, and of a gradient's call which of its products
+ *   kernel      0 = tiles in LDS, 1 = few rows straight from the operands, 2 = outer products of few rows
+ *   rows, cols  of a tile, the columns of both projections counted (0 for the other kernels)
+ *   slices      of the contraction, joined by a second launch where there are more than one
+ * Errors are those of the call for the same description.  Any output pointer may be NULL.
+ */
+#define AX_PRODUCT_MATMUL 0
+#define AX_PRODUCT_MATMUL_Q8 1
+#define AX_PRODUCT_GATED 2
+#define AX_PRODUCT_GATED_Q8 3
+#define AX_PRODUCT_MATMUL_GX 4
+#define AX_PRODUCT_MATMUL_GW 5
+#define AX_PRODUCT_GATED_GX 6
+#define AX_PRODUCT_GATED_GW 7
+int ax_probe_product_plan(const ax_matmul_desc_t* desc, int product, int* kernel, int* rows, int* cols, int* slices);
+
 #ifdef __cplusplus
 }
 #endif

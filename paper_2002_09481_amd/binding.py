@@ -57,7 +57,7 @@ EXPORTS = [  # include/axconv.h
 ]
 PROBE_EXPORTS = [  # include/axconv_probe.h
     "ax_probe_lds_gather", "ax_probe_copy", "ax_probe_mac", "ax_probe_layer_kernel_ms",
-    "ax_probe_layer_route",
+    "ax_probe_layer_route", "ax_probe_product_plan",
 ]
 
 
@@ -202,6 +202,7 @@ def lib():
             ("ax_adamw", [ctypes.POINTER(ax_adamw_desc_t), ctypes.POINTER(ax_adamw_tensor_t), ci, vp]),
             ("ax_adamw_states", [ctypes.POINTER(ax_adamw_tensor_t), ci, ctypes.POINTER(vp), ctypes.POINTER(vp), vp])):
         getattr(L, name).argtypes, getattr(L, name).restype = args, ci
+    L.ax_probe_product_plan.argtypes, L.ax_probe_product_plan.restype = [md, ci] + [ip] * 4, ci
     L.ax_rmsnorm_backward_workspace_bytes.argtypes, L.ax_rmsnorm_backward_workspace_bytes.restype = [nd], sz
     for name in ("ax_matmul", "ax_matmul_q8", "ax_matmul_backward", "ax_gated", "ax_gated_q8", "ax_gated_backward"):
         f = getattr(L, name + "_workspace_bytes")
@@ -1442,6 +1443,22 @@ def ax_probe_mac(mode: int, pattern: int = 1, iters: int = 200, wgs_per_cu: int 
     _check(lib().ax_probe_mac(mode, pattern, iters, wgs_per_cu, ctypes.byref(ops), ctypes.byref(sec),
                               ctypes.c_void_p(_stream_ptr(stream))))
     return {"ops": ops.value, "seconds": sec.value, "ops_per_s": ops.value / sec.value}
+
+
+PRODUCTS = ("matmul", "matmul_q8", "gated", "gated_q8", "matmul_gx", "matmul_gw", "gated_gx", "gated_gw")
+
+
+def ax_probe_product_plan(product: str, M: int, K: int, N: int, dtype=torch.bfloat16, out_dtype=None, transposed=False) -> dict:
+    """Which kernel a product of contiguous aligned matrices runs ("tiles", "few", "outer"), its tile and the slices of its
+    contraction.  M, K, N: of the call, also where the product is one of its gradients (matmul_gx, ...)."""
+    q8 = product.endswith("q8")
+    out_dtype = (torch.bfloat16 if q8 else dtype) if out_dtype is None else out_dtype
+    transposed = transposed or q8
+    d = ax_matmul_desc_t(M, N, K, K, K if transposed else N, N, N, AX_BF16 if q8 else _DT[dtype], _DT[out_dtype], 0, int(transposed), 0)
+    out = [ctypes.c_int(0) for _ in range(4)]
+    _check(lib().ax_probe_product_plan(d, PRODUCTS.index(product), *[ctypes.byref(o) for o in out]))
+    k, rows, cols, slices = [o.value for o in out]
+    return {"kernel": ("tiles", "few", "outer")[k], "tile": (rows, cols), "slices": slices}
 
 
 def ax_probe_copy(dst: torch.Tensor, src: torch.Tensor, stream=None) -> None:

@@ -52,6 +52,7 @@ struct GemmPlan {
 };
 
 GemmPlan plan_gemm(const GemmArgs& g);
+void tile_of(const GemmArgs& g, const GemmPlan& p, int* rows, int* cols);
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStream_t s);
 // y from the partial sums [splits][planes][M][N rounded up to 8] of the slices, with the epilogue.
 hipError_t launch_join(const GemmArgs& g, int splits, void* part, hipStream_t s);

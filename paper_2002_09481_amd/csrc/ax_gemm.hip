@@ -680,6 +680,12 @@ GemmPlan plan_gemm(const GemmArgs& g) {
   return best;
 }
 
+void tile_of(const GemmArgs& g, const GemmPlan& p, int* rows, int* cols) {
+  const TileShape& T = shape_of(g, p.tile);
+  *rows = T.bm;
+  *cols = T.bn;
+}
+
 hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStream_t s) {
   Args a;
   a.g = g;

@@ -12,6 +12,7 @@
 #include "ax_float.h"
 #include "ax_gemm.h"
 #include "ax_norm.h"
+#include "axconv_probe.h"
 
 namespace ax {
 namespace {
@@ -898,4 +899,34 @@ extern "C" int ax_gated_backward(const ax_matmul_desc_t* d, const void* gh, cons
     if (!aligned_to(p, e)) return AX_ERR_ALIGN;
   return backward_common(d, true, gh, x, wg, wu, g, u, gx_out, gwg_out, gwu_out, nullptr, workspace, workspace_bytes,
                          (hipStream_t)hip_stream);
+}
+
+extern "C" int ax_probe_product_plan(const ax_matmul_desc_t* d, int product, int* kernel, int* rows, int* cols, int* slices) {
+  if (product < AX_PRODUCT_MATMUL || product > AX_PRODUCT_GATED_GW) return AX_ERR_OPTION;
+  const bool q8 = product == AX_PRODUCT_MATMUL_Q8 || product == AX_PRODUCT_GATED_Q8, back = product >= AX_PRODUCT_MATMUL_GX;
+  const bool gated = product == AX_PRODUCT_GATED || product == AX_PRODUCT_GATED_Q8 || product >= AX_PRODUCT_GATED_GX;
+  if (int rc = check_desc(d, q8, back, gated)) return rc;
+  int k = 0, r = 0, c = 0, n = 1;
+  if (d->M > 0 && !back) {
+    const Forward f = make_forward(d, q8, gated, nullptr, nullptr, nullptr, nullptr);
+    k = f.few;
+    n = f.few ? f.few_plan.slices : f.plan.splits;
+    if (!f.few) tile_of(f.g, f.plan, &r, &c);
+  } else if (d->M > 0) {
+    const bool gx = product == AX_PRODUCT_MATMUL_GX || product == AX_PRODUCT_GATED_GX;
+    if (few_backward_fits(d)) {
+      k = gx ? 1 : 2;
+      if (gx) n = make_few_backward(d, gated, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr).plan.slices;
+    } else {
+      const Backward b = make_backward(d, gated, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
+      k = gx && b.few;
+      n = k ? b.pf.slices : gx ? b.px.splits : b.pw.splits;
+      if (!k) gx ? tile_of(b.gx, b.px, &r, &c) : tile_of(b.gw, b.pw, &r, &c);
+    }
+  }
+  if (kernel) *kernel = k;
+  if (rows) *rows = r;
+  if (cols) *cols = c;
+  if (slices) *slices = n;
+  return AX_OK;
 }
