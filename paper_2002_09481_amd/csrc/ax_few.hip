@@ -80,7 +80,7 @@ struct Along {
       next = *(const uint32_t*)(words + (shift ? 16 : 12));
       return;
     }
-    if (ODD) shift = 0;
+    if (ODD) shift = next = 0;
     if (FULL || left >= E) {
       q[0] = load_any<u32x4>(p);
       if (KD == kF32) q[KD == kF32 ? 1 : 0] = load_any<u32x4>(p + 16);

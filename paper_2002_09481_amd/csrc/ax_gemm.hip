@@ -128,7 +128,8 @@ template <typename T>
 __device__ __forceinline__ T uniform(T x) { return (T)__builtin_amdgcn_readfirstlane((int)x); }
 
 // 16 bytes per lane from memory to LDS at dst + 16 * lane (dst uniform over the wave).  Written as instructions: of a
-// copy that it knows, the compiler makes every later LDS read wait, since it cannot tell the stages apart.
+// copy that it knows, the compiler makes every later LDS read wait, since it cannot tell the stages apart.  (m0 is reserved: the
+// compiler keeps nothing there and sets it right in front of the instructions that read it, of which these kernels have no others.)
 __device__ __forceinline__ void lds_copy(uint32_t dst, uint32_t off, const u32x4& rsrc) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :: "s"(dst), "v"(off), "s"(rsrc) : "memory");
