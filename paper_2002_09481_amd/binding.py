@@ -903,7 +903,8 @@ def ax_dense_f32(x, w, lut, x_range=None, w_range=None, relu=False, round_mode=0
 # ---- feed-forward operators: norm, products, gated block, optimizer step -----------------------------------------------
 #
 # Matrices are torch tensors whose last dimension is contiguous; the leading dimensions are rows, at any pitch where there is
-# one of them, contiguous where there are more.  Outputs that are not handed in are allocated with torch.
+# one of them, contiguous where there are more.  Outputs that are not handed in are allocated with torch.  As with the lookup
+# layers, nothing here is recorded by autograd: gradients are calls of their own.
 
 
 _DT = {torch.float32: AX_F32, torch.bfloat16: AX_BF16}
@@ -1400,7 +1401,8 @@ class AxAdamW:
 
     def step(self, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, grad_scale=None, stream=None):
         """One step, the step-th (from 1).  grad_scale: None, or a float32 CUDA tensor of one element that multiplies the
-        gradients (what clipping by a norm that was computed on the device gives)."""
+        gradients (what clipping by a norm that was computed on the device gives).  lr and the factors of the step-th step are
+        the launch's arguments: a graph that holds it repeats that step."""
         d = self._d
         d.lr, d.beta1, d.beta2, d.eps, d.weight_decay, d.step = lr, beta1, beta2, eps, weight_decay, int(step)
         if grad_scale is not None:

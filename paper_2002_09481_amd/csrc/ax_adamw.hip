@@ -8,7 +8,7 @@
 // parameters, bf16 gradients and copies and 8-bit states.  All tensors in one launch, a workgroup for 4096 elements of one
 // of them: a step over many small tensors is one launch's latency.
 //
-// Measured: 302 M elements with 8-bit states 930 to 1040 us (4.8 GB; a copy moves 5.1 TB/s), their states as float32
+// Measured: 302 M elements with 8-bit states 930 to 1055 us (4.8 GB; a copy moves 5.1 TB/s), their states as float32
 // values 545 us (5.5 TB/s); 2.3 M elements of 15 tensors with float32 states 12.5 us (5.1 TB/s).
 #include <algorithm>
 #include <cmath>

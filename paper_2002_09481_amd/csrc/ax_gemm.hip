@@ -7,8 +7,9 @@
 // the same product takes 692 us instead of 843).  Smaller ones: rounds of tiles that leave compute units idle,
 // and each tile's first stage and stores, during which nothing multiplies.
 //
-// Measured (us): bf16 8192^3 840 to 930 (1180 to 1310 TF), 4096^3 103 (1340 TF), gradient of a weight 8192^3 780 (1400 TF);
-// gated 8192 x 4096 -> 16384 with both projections stored 1735 to 1800 (1220 to 1270 TF); int8 8192^3 520 (2100 TOP);
+// Measured (us): bf16 8192^3 815 to 930 (1180 to 1350 TF), 4096^3 103 to 110 (1250 to 1340 TF), gradient of a weight 8192^3 780 to
+// 805 (1365 to 1400 TF);
+// gated 8192 x 4096 -> 16384 with both projections stored 1735 to 1800 (1220 to 1270 TF); int8 8192^3 465 to 520 (2100 to 2370 TOP);
 // float32 4096^3 690 to 700 (196 to 199 TF, six products each).
 #include <algorithm>
 #include <type_traits>
