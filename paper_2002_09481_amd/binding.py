@@ -309,10 +309,12 @@ def _on_stream(call, stream, *args):
     that was current as well, where they will be used."""
     before = torch.cuda.current_stream(stream.device)
     with torch.cuda.stream(stream):
-        out = call(*args)
-    for t in args:
-        if isinstance(t, torch.Tensor):
-            t.record_stream(stream)
+        try:
+            out = call(*args)
+        finally:  # (a call that fails at its second launch has enqueued the first)
+            for t in args:
+                if isinstance(t, torch.Tensor) and t.is_cuda:
+                    t.record_stream(stream)
     for t in out if isinstance(out, tuple) else (out,):
         if isinstance(t, torch.Tensor):
             t.record_stream(before)

@@ -111,8 +111,10 @@ class Streams:
         @contextlib.contextmanager
         def on(s):
             self.current.append(s)
-            yield
-            self.current.pop()
+            try:
+                yield
+            finally:
+                self.current.pop()
 
         def factory(f):
             def make(*a, **kw):
@@ -186,3 +188,16 @@ def test_results_of_a_block_on_another_stream(notes, monkeypatch):
     b, s = _kept_block(), Streams(monkeypatch)
     x, r = floats(4, 16, dtype=torch.float32), floats(4, 16, dtype=torch.float32)
     s.check(b.forward, (x, r))
+
+
+def test_a_call_on_another_stream_that_fails(notes, monkeypatch):
+    """Its operands are tied to the stream all the same, and the current stream is the one that it was."""
+    s = Streams(monkeypatch)
+    x, w = floats(4, 16, dtype=torch.float32), floats(16, 16, dtype=torch.float32)
+    notes.ax_matmul = lambda *a: -6
+    monkeypatch.setattr(ax, "_check", lambda rc: (_ for _ in ()).throw(ax.AxError(rc, "")) if rc else None)
+    with pytest.raises(ax.AxError):
+        ax.ax_matmul(x, w, stream=s.side)
+    assert s.current == [s.main] and (x.data_ptr(), s.side) in s.ties and (w.data_ptr(), s.side) in s.ties
+    with pytest.raises(TypeError):  # nothing on the host is tied to a stream
+        ax.ax_matmul(torch.zeros((4, 16)), w, stream=s.side)
