@@ -199,5 +199,5 @@ def test_a_call_on_another_stream_that_fails(notes, monkeypatch):
     with pytest.raises(ax.AxError):
         ax.ax_matmul(x, w, stream=s.side)
     assert s.current == [s.main] and (x.data_ptr(), s.side) in s.ties and (w.data_ptr(), s.side) in s.ties
-    with pytest.raises(TypeError):  # nothing on the host is tied to a stream
-        ax.ax_matmul(torch.zeros((4, 16)), w, stream=s.side)
+    with pytest.raises(TypeError):  # nothing on the host is tied to a stream (other sizes: those above are known as checked)
+        ax.ax_matmul(torch.zeros((5, 16)), w, stream=s.side)
