@@ -574,6 +574,177 @@ int ax_adamw(const ax_adamw_desc_t* desc, const ax_adamw_tensor_t* tensors, int 
 int ax_adamw_states(const ax_adamw_tensor_t* tensors, int count, float* const* m_out, float* const* v_out,
                     void* hip_stream);
 
+/* ---- feed-forward blocks of experts ---------------------------------------------------------
+ *
+ * A block whose projections come in `experts` versions, of which every token takes k: the router's choice, the products
+ * of the tokens' rows with the matrix of their expert, and their sum; and, for serving, products with weights of 4 bits.  The conventions
+ * are those above.
+ *
+ * Rows.  Every choice of a token is a row of the products.  Rows lie in the order of their experts: expert e has the rows
+ * offsets[e] .. offsets[e + 1] - 1 (offsets [experts + 1], int32, device).  Sizes are ragged, an expert may have no rows;
+ * rows in front of offsets[0] and from offsets[experts] on belong to nobody and are left as they are in the outputs.  With
+ * offsets that descend or leave the rows the results are not defined, but no call reads or writes outside its arrays, whatever they hold.
+ */
+#define AX_MAX_EXPERTS 1024
+#define AX_MAX_CHOICES 16
+
+/*
+ * The router.  For every token the k largest logits, ties to the lowest expert, in descending order:
+ *   experts_out [tokens, k]  int32
+ *   weights_out [tokens, k]  float32: exp(l - m) / sum of exp(l - m), m the largest logit, summed over the chosen experts
+ *                            (normalize = 1) or over all (0)
+ *   offsets_out [experts + 1], rows_out [tokens, k], tokens_out [tokens * k], int32: the rows of the choices in the order
+ *                            (expert, token, choice): the row of every choice, and the token of every row
+ * A logit of minus infinity is never chosen (a mask); where fewer than k others are left, the choice is dropped: expert -1, weight 0, row
+ * -1, and as many rows at the end belong to nobody (their token is -1).  Infinite logits share the weight.  A NaN is never
+ * chosen either, and makes the weights of its token NaN.
+ * workspace: ax_route_workspace_bytes(desc) bytes, 256-byte aligned.
+ */
+typedef struct {
+  int64_t tokens;     /* tokens * k <= 2^30                                                     */
+  int64_t ld;         /* row pitch of the logits                                                */
+  int32_t experts;    /* 1 .. AX_MAX_EXPERTS                                                    */
+  int32_t k;          /* 1 .. min(experts, AX_MAX_CHOICES)                                      */
+  int32_t dtype;      /* of the logits and their gradient                                       */
+  int32_t normalize;
+} ax_route_desc_t;
+
+int ax_route(const ax_route_desc_t* desc, const void* logits, int32_t* experts_out, float* weights_out,
+             int32_t* offsets_out, int32_t* rows_out, int32_t* tokens_out, void* workspace,
+             size_t workspace_bytes, void* hip_stream);
+size_t ax_route_workspace_bytes(const ax_route_desc_t* desc);
+
+/*
+ * The gradient of the logits from that of the weights, through what the forward pass left.  With inner = sum over j of gw_j w_j:
+ *   normalize = 1: gl[e_j] = w_j (gw_j - inner), zero elsewhere (logits may be NULL)
+ *   normalize = 0: gl = p (g - inner), p the softmax over all experts, g_e_j = gw_j and zero elsewhere
+ * A dropped choice has no gradient.  glogits_out [tokens, experts] at pitch glogits_ld.  No workspace.
+ */
+int ax_route_backward(const ax_route_desc_t* desc, const float* gweights, const void* logits, const int32_t* experts,
+                      const float* weights, void* glogits_out, int64_t glogits_ld, void* hip_stream);
+
+/*
+ * Products of rows with the matrix of their expert.  Row r is row index[r] of x (an index outside x: a row of zeros), or row
+ * r of x where index is NULL and desc->indexed is 0; w holds the experts' matrices one behind the other, [experts, K, N] or
+ * [experts, N, K] (w_transposed), all rows at pitch w_ld:
+ *   z = x w_e,  y_out = act(z),  z_out (may be NULL, pitch N) kept for the backward pass
+ *   h_out = act(x wg_e) * (x wu_e),  g_out and u_out (both or neither NULL, pitch N) kept
+ * Types, sums and roundings as in ax_matmul and ax_gated.  Indexed rows may start at any element.
+ * workspace: ax_*_experts_workspace_bytes(desc) bytes, 256-byte aligned.
+ */
+typedef struct {
+  int64_t rows;       /* of the products, at most 2^30                                          */
+  int64_t x_rows;     /* of x; rows where it is not indexed                                     */
+  int64_t N, K;       /* experts * N and experts * K below 2^31                                 */
+  int64_t x_ld, w_ld, y_ld;
+  int64_t gx_ld;      /* of the rows' gradient                                                  */
+  int32_t experts;    /* 1 .. AX_MAX_EXPERTS                                                    */
+  int32_t dtype;      /* of all matrices                                                        */
+  int32_t act;
+  int32_t w_transposed; /* must be 0 for the gated pair                                         */
+  int32_t indexed;    /* 1: index is given                                                      */
+  int32_t unaligned;  /* as in ax_matmul_desc_t                                                 */
+} ax_experts_desc_t;
+
+int ax_matmul_experts(const ax_experts_desc_t* desc, const void* x, const int32_t* index, const int32_t* offsets,
+                      const void* w, void* y_out, void* z_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t ax_matmul_experts_workspace_bytes(const ax_experts_desc_t* desc);
+int ax_gated_experts(const ax_experts_desc_t* desc, const void* x, const int32_t* index, const int32_t* offsets,
+                     const void* wg, const void* wu, void* h_out, void* g_out, void* u_out, void* workspace,
+                     size_t workspace_bytes, void* hip_stream);
+size_t ax_gated_experts_workspace_bytes(const ax_experts_desc_t* desc);
+
+/*
+ * Their gradients.  gx_out [rows, K] (pitch gx_ld) is that of the rows of the products, in their order; the gradient of an indexed
+ * x is the sum over its rows (ax_combine without weights).  gw_out (gwg_out, gwu_out): the experts' matrices one behind the other, at
+ * the pitch of w; an expert without rows gets zeros.  Formulas, roundings and what may be NULL as in
+ * ax_matmul_backward and ax_gated_backward, without the bias; bf16: gz (gg, gu) is rounded to bf16 for all products.
+ */
+int ax_matmul_experts_backward(const ax_experts_desc_t* desc, const void* gy, const void* x, const int32_t* index,
+                               const int32_t* offsets, const void* w, const void* z, void* gx_out, void* gw_out,
+                               void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t ax_matmul_experts_backward_workspace_bytes(const ax_experts_desc_t* desc);
+int ax_gated_experts_backward(const ax_experts_desc_t* desc, const void* gh, const void* x, const int32_t* index,
+                              const int32_t* offsets, const void* wg, const void* wu, const void* g, const void* u,
+                              void* gx_out, void* gwg_out, void* gwu_out, void* workspace, size_t workspace_bytes,
+                              void* hip_stream);
+size_t ax_gated_experts_backward_workspace_bytes(const ax_experts_desc_t* desc);
+
+/*
+ * Back to the tokens: y_out[t] = residual[t] + sum over j of weights[t, j] * h[rows[t, j]], in float32 in the order of j.
+ *   h [h_rows, cols], rows [tokens, k] int32 (a row outside h is left out), weights [tokens, k] float32 (NULL: one each),
+ *   residual (may be NULL) and y_out [tokens, cols]; y_out may be residual itself, with its pitch
+ */
+typedef struct {
+  int64_t tokens;     /* tokens * k <= 2^30                                                     */
+  int64_t h_rows, cols;
+  int64_t h_ld, residual_ld, y_ld;
+  int64_t gh_ld;      /* of h's gradient                                                        */
+  int32_t k;          /* 1 .. AX_MAX_CHOICES                                                    */
+  int32_t dtype;      /* of h, residual, y and their gradients                                  */
+} ax_combine_desc_t;
+
+int ax_combine(const ax_combine_desc_t* desc, const void* h, const int32_t* rows, const float* weights,
+               const void* residual, void* y_out, void* hip_stream);
+
+/*
+ * Gradients: gh_out[rows[t, j]] = weights[t, j] * gy[t] (gy at pitch y_ld; rows must differ from one another; rows of gh_out that no
+ * choice names are left as they are), gweights_out[t, j] = sum over the columns of gy[t] * h[rows[t, j]], float32, zero for a row
+ * outside h.  Either may be NULL (not both); h is needed for gweights_out alone.  The residual's gradient is gy.
+ */
+int ax_combine_backward(const ax_combine_desc_t* desc, const void* gy, const void* h, const int32_t* rows,
+                        const float* weights, void* gh_out, float* gweights_out, void* hip_stream);
+
+/*
+ * Weights of 4 bits with a scale for every group of a row: w[n, k] = scale[n, k / group] * code[n, k], codes -8 .. 7, scales bf16,
+ * group 32, 64 or 128, [N, K] for each of `experts` matrices (1 for a plain one).  They are kept in a layout of the
+ * library's own, codes and scales apart, ax_q4_codes_bytes and ax_q4_scales_bytes bytes, 16-byte aligned, at most 2^24
+ * blocks of 16 x 128 in all.
+ *
+ * ax_quantize_q4: from float weights [experts * N, K] at pitch w_ld: scale = (largest |w| of the group / 7) rounded to bf16, code =
+ * w / scale rounded to nearest, ties to even, in -8 .. 7; a group whose scale is zero or not finite has codes zero.
+ * ax_pack_q4: from codes int8 [experts * N, K] (others are taken to the nearest of -8 .. 7) and scales bf16 [experts * N, ceil(K / group)].
+ * ax_q4_values: the weights, float32 [experts * N, K].
+ */
+size_t ax_q4_codes_bytes(int64_t experts, int64_t N, int64_t K);
+size_t ax_q4_scales_bytes(int64_t experts, int64_t N, int64_t K, int32_t group);
+int ax_quantize_q4(const void* w, int32_t dtype, int64_t w_ld, int64_t experts, int64_t N, int64_t K, int32_t group,
+                   uint8_t* codes_out, void* scales_out, void* hip_stream);
+int ax_pack_q4(const int8_t* codes, const void* scales, int64_t experts, int64_t N, int64_t K, int32_t group,
+               uint8_t* codes_out, void* scales_out, void* hip_stream);
+int ax_q4_values(const uint8_t* codes, const void* scales, int64_t experts, int64_t N, int64_t K, int32_t group,
+                 float* values_out, void* hip_stream);
+
+/*
+ * Products with such weights: y_out = act(x w^T + bias) + residual, h_out = act(x wg^T) * (x wu^T).  bias [N], residual and y_out
+ * [rows, N] (both may be NULL; y_out may be residual itself) have x's type.  With several experts the rows are grouped as above (index
+ * and offsets; offsets may be NULL for one expert, whose rows are then all).  Up to 64 rows an expert on the average
+ * the weights are exact: products with the codes are exact and summed in float32, each group's sum times its scale in float32.
+ * More rows of bf16: every weight is rounded to bf16 for the matrix instructions; float32: exact, as in ax_matmul.
+ * workspace: ax_*_q4_workspace_bytes(desc) bytes, 256-byte aligned.
+ */
+typedef struct {
+  int64_t rows;       /* of the products, at most 2^30                                          */
+  int64_t x_rows;     /* of x; rows where it is not indexed                                     */
+  int64_t N, K;
+  int64_t x_ld, residual_ld, y_ld;
+  int32_t experts;
+  int32_t group;
+  int32_t dtype;      /* of x, bias, residual and the output                                    */
+  int32_t act;
+  int32_t indexed;
+  int32_t unaligned;
+} ax_q4_desc_t;
+
+int ax_matmul_q4(const ax_q4_desc_t* desc, const void* x, const int32_t* index, const int32_t* offsets,
+                 const uint8_t* codes, const void* scales, const void* bias, const void* residual, void* y_out,
+                 void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t ax_matmul_q4_workspace_bytes(const ax_q4_desc_t* desc);
+int ax_gated_q4(const ax_q4_desc_t* desc, const void* x, const int32_t* index, const int32_t* offsets,
+                const uint8_t* g_codes, const void* g_scales, const uint8_t* u_codes, const void* u_scales, void* h_out,
+                void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t ax_gated_q4_workspace_bytes(const ax_q4_desc_t* desc);
+
 const char* ax_strerror(int code);
 
 /* Library version, major * 10000 + minor * 100 + patch. */

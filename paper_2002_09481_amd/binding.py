@@ -14,6 +14,7 @@ entry points that accept a tune (ax_conv2d_ex, ax_conv2d_f32_ex, the layer handl
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional, Tuple
 
@@ -54,6 +55,12 @@ EXPORTS = [  # include/axconv.h
     "ax_matmul_backward", "ax_matmul_backward_workspace_bytes", "ax_gated", "ax_gated_workspace_bytes",
     "ax_gated_q8", "ax_gated_q8_workspace_bytes", "ax_gated_backward", "ax_gated_backward_workspace_bytes",
     "ax_adamw", "ax_adamw_states",
+    "ax_route", "ax_route_workspace_bytes", "ax_route_backward", "ax_combine", "ax_combine_backward",
+    "ax_matmul_experts", "ax_matmul_experts_workspace_bytes", "ax_gated_experts", "ax_gated_experts_workspace_bytes",
+    "ax_matmul_experts_backward", "ax_matmul_experts_backward_workspace_bytes",
+    "ax_gated_experts_backward", "ax_gated_experts_backward_workspace_bytes",
+    "ax_quantize_q4", "ax_pack_q4", "ax_q4_values", "ax_q4_codes_bytes", "ax_q4_scales_bytes",
+    "ax_matmul_q4", "ax_matmul_q4_workspace_bytes", "ax_gated_q4", "ax_gated_q4_workspace_bytes",
 ]
 PROBE_EXPORTS = [  # include/axconv_probe.h
     "ax_probe_lds_gather", "ax_probe_copy", "ax_probe_mac", "ax_probe_layer_kernel_ms",
@@ -97,6 +104,26 @@ class ax_adamw_desc_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [
         ("step", ctypes.c_int64), ("grad_scale", ctypes.c_void_p)] + [
         (n, ctypes.c_int32) for n in ("p_dtype", "g_dtype", "state_bits", "reserved")]
+
+
+class ax_route_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("tokens", "ld")] + [
+        (n, ctypes.c_int32) for n in ("experts", "k", "dtype", "normalize")]
+
+
+class ax_experts_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "x_rows", "N", "K", "x_ld", "w_ld", "y_ld", "gx_ld")] + [
+        (n, ctypes.c_int32) for n in ("experts", "dtype", "act", "w_transposed", "indexed", "unaligned")]
+
+
+class ax_combine_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("tokens", "h_rows", "cols", "h_ld", "residual_ld", "y_ld", "gh_ld")] + [
+        (n, ctypes.c_int32) for n in ("k", "dtype")]
+
+
+class ax_q4_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "x_rows", "N", "K", "x_ld", "residual_ld", "y_ld")] + [
+        (n, ctypes.c_int32) for n in ("experts", "group", "dtype", "act", "indexed", "unaligned")]
 
 
 def lib():
@@ -207,6 +234,23 @@ def lib():
     for name in ("ax_matmul", "ax_matmul_q8", "ax_matmul_backward", "ax_gated", "ax_gated_q8", "ax_gated_backward"):
         f = getattr(L, name + "_workspace_bytes")
         f.argtypes, f.restype = [md], sz
+    rd, ed, cd, qd = (ctypes.POINTER(t) for t in (ax_route_desc_t, ax_experts_desc_t, ax_combine_desc_t, ax_q4_desc_t))
+    i64, i32 = ctypes.c_int64, ctypes.c_int32
+    for name, args, workspace in (
+            ("ax_route", [rd] + [vp] * 7 + [sz, vp], rd), ("ax_route_backward", [rd] + [vp] * 5 + [i64, vp], None),
+            ("ax_matmul_experts", [ed] + [vp] * 7 + [sz, vp], ed), ("ax_gated_experts", [ed] + [vp] * 9 + [sz, vp], ed),
+            ("ax_matmul_experts_backward", [ed] + [vp] * 9 + [sz, vp], ed),
+            ("ax_gated_experts_backward", [ed] + [vp] * 12 + [sz, vp], ed),
+            ("ax_combine", [cd] + [vp] * 6, None), ("ax_combine_backward", [cd] + [vp] * 7, None),
+            ("ax_quantize_q4", [vp, i32] + [i64] * 4 + [i32] + [vp] * 3, None),
+            ("ax_pack_q4", [vp] * 2 + [i64] * 3 + [i32] + [vp] * 3, None), ("ax_q4_values", [vp] * 2 + [i64] * 3 + [i32] + [vp] * 2, None),
+            ("ax_matmul_q4", [qd] + [vp] * 9 + [sz, vp], qd), ("ax_gated_q4", [qd] + [vp] * 9 + [sz, vp], qd)):
+        getattr(L, name).argtypes, getattr(L, name).restype = args, ci
+        if workspace is not None:
+            f = getattr(L, name + "_workspace_bytes")
+            f.argtypes, f.restype = [workspace], sz
+    L.ax_q4_codes_bytes.argtypes, L.ax_q4_codes_bytes.restype = [i64] * 3, sz
+    L.ax_q4_scales_bytes.argtypes, L.ax_q4_scales_bytes.restype = [i64] * 3 + [i32], sz
     _lib = L
     return L
 
@@ -312,13 +356,21 @@ def _on_stream(call, stream, *args):
         try:
             out = call(*args)
         finally:  # (a call that fails at its second launch has enqueued the first)
-            for t in args:
-                if isinstance(t, torch.Tensor) and t.is_cuda:
+            for t in _tensors_of(args):
+                if t.is_cuda:
                     t.record_stream(stream)
-    for t in out if isinstance(out, tuple) else (out,):
-        if isinstance(t, torch.Tensor):
-            t.record_stream(before)
+    for t in _tensors_of(out if isinstance(out, tuple) else (out,)):
+        t.record_stream(before)
     return out
+
+
+def _tensors_of(things):
+    for t in things:
+        if isinstance(t, torch.Tensor):
+            yield t
+        elif isinstance(t, AxQ4):
+            yield t.codes
+            yield t.scales
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -1330,6 +1382,496 @@ def ax_gated_backward(gh, x, wg, wu, g, u, act="silu", gx_out=None, gwg_out=None
     _check(L.ax_gated_backward(d, gh.data_ptr(), xp, gp, up, g.data_ptr(), u.data_ptr(), _ptr(gx_out), _ptr(gwg_out), _ptr(gwu_out),
                                *_ws_args(ws), _stream_ptr(None)))
     return gx_out, gwg_out, gwu_out
+
+
+# ---- feed-forward blocks of experts ------------------------------------------------------------------------------------
+#
+# Rows are grouped by expert: offsets [experts + 1] and tokens [rows], both int32 on the device, are what ax_route returns.
+# Weights are [experts, inputs, outputs] (or [experts, outputs, inputs] with transposed), the experts' matrices one behind the
+# other.  Tensors of a call share a device, the current one.
+
+
+def _same_device(*tensors):
+    dev = tensors[0].device
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.device != dev:
+            raise ValueError("all tensors must be on one device")
+
+
+def _current_device(t):
+    if t.is_cuda and t.device.type == "cuda" and t.device.index != torch._C._cuda_getDevice():
+        raise ValueError("the tensors are on %s, which is not the current device" % t.device)
+
+
+def _whole(t, n: int, name: str) -> None:
+    """A vector of n whole numbers."""
+    _dev(t, torch.int32, name)
+    if n >= 0 and t.numel() != n:
+        raise ValueError("%s must have %d elements" % (name, n))
+
+
+def _weights(t, dtype, name: str):
+    """(experts, rows, columns, row pitch) of the experts' matrices."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % name)
+    if t.dtype != dtype:
+        raise TypeError("%s must have dtype %s, got %s" % (name, dtype, t.dtype))
+    if t.dim() != 3:
+        raise ValueError("%s must be [experts, rows, columns]" % name)
+    e, r, c = t.shape
+    ld = t.stride(1) if r > 1 else t.stride(0) if e > 1 else c
+    if (c > 1 and t.stride(2) != 1) or ld < c or (e > 1 and t.stride(0) != r * ld):
+        raise ValueError("%s must have contiguous rows at one pitch, the experts' matrices one behind the other" % name)
+    return e, r, c, ld
+
+
+def ax_route(logits, k, normalize=True, experts_out=None, weights_out=None, offsets_out=None, rows_out=None, tokens_out=None,
+             workspace=None, stream=None):
+    """Each token's k largest logits and the order of its choices by expert.  logits: [tokens, experts].  Returns (experts
+    [tokens, k], weights [tokens, k], offsets [experts + 1], rows [tokens, k], tokens [tokens * k]): weights float32, the softmax
+    over the chosen experts (normalize) or over all; the others int32."""
+    if stream is not None:
+        return _on_stream(ax_route, stream, logits, k, normalize, experts_out, weights_out, offsets_out, rows_out, tokens_out, workspace)
+    L = lib()
+    key = ("route", k, normalize, _sig(logits), _sig(experts_out), _sig(weights_out), _sig(offsets_out), _sig(rows_out), _sig(tokens_out))
+    hit = _checked.get(key)
+    if hit is None:
+        T, E, ld = _mat(logits, logits.dtype, "logits")
+        d = ax_route_desc_t(T, ld, E, int(k), _float_dtype(logits, "logits"), int(bool(normalize)))
+        if not 1 <= d.k <= E:
+            raise ValueError("k must be between 1 and the number of experts")
+        for t, n, dt, name in ((experts_out, T * d.k, torch.int32, "experts_out"), (weights_out, T * d.k, torch.float32, "weights_out"),
+                               (offsets_out, E + 1, torch.int32, "offsets_out"), (rows_out, T * d.k, torch.int32, "rows_out"),
+                               (tokens_out, T * d.k, torch.int32, "tokens_out")):
+            if t is not None:
+                _vec_of(t, dt, n, name)
+        _same_device(logits, experts_out, weights_out, offsets_out, rows_out, tokens_out)
+        hit = _remember(key, (d, int(L.ax_route_workspace_bytes(d)), logits.shape[:-1] + (d.k,), T * d.k))
+    d, need, shape, n = hit
+    _current_device(logits)
+    if experts_out is None:
+        experts_out = logits.new_empty(shape, dtype=torch.int32)
+    if weights_out is None:
+        weights_out = logits.new_empty(shape, dtype=torch.float32)
+    if offsets_out is None:
+        offsets_out = logits.new_empty(d.experts + 1, dtype=torch.int32)
+    if rows_out is None:
+        rows_out = logits.new_empty(shape, dtype=torch.int32)
+    if tokens_out is None:
+        tokens_out = logits.new_empty(n, dtype=torch.int32)
+    ws = _scratch(need, workspace, logits.device)
+    _check(L.ax_route(d, _ptr(logits), _ptr(experts_out), _ptr(weights_out), _ptr(offsets_out), _ptr(rows_out), _ptr(tokens_out),
+                      *_ws_args(ws), _stream_ptr(None)))
+    return experts_out, weights_out, offsets_out, rows_out, tokens_out
+
+
+def ax_route_backward(gweights, logits, experts, weights, normalize=True, glogits_out=None, stream=None):
+    """The gradient of the logits from that of the weights [tokens, k] (float32); experts and weights as ax_route returned them."""
+    if stream is not None:
+        return _on_stream(ax_route_backward, stream, gweights, logits, experts, weights, normalize, glogits_out)
+    L = lib()
+    key = ("route_backward", normalize, _sig(gweights), _sig(logits), _sig(experts), _sig(weights), _sig(glogits_out))
+    if glogits_out is None:
+        glogits_out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    hit = _checked.get(key)
+    if hit is None:
+        T, E, ld = _mat(logits, logits.dtype, "logits")
+        if experts.dim() < 1 or experts.numel() != T * experts.shape[-1]:
+            raise ValueError("experts must be [tokens, k]")
+        k = experts.shape[-1]
+        d = ax_route_desc_t(T, ld, E, k, _float_dtype(logits, "logits"), int(bool(normalize)))
+        _whole(experts, T * k, "experts")
+        _vec_of(weights, torch.float32, T * k, "weights")
+        _vec_of(gweights, torch.float32, T * k, "gweights")
+        _same_device(logits, gweights, experts, weights, glogits_out)
+        hit = _remember(key, (d, _mat_of(glogits_out, logits.dtype, T, E, "glogits_out")))
+    d, ld = hit
+    _current_device(logits)
+    _check(L.ax_route_backward(d, _ptr(gweights), _ptr(logits), _ptr(experts), _ptr(weights), _ptr(glogits_out), ld, _stream_ptr(None)))
+    return glogits_out
+
+
+def _experts_desc(x, weights, names, offsets, tokens, act, transposed, aligned) -> ax_experts_desc_t:
+    n, K, x_ld = _mat(x, x.dtype, "x")
+    w = weights[0]
+    E, wr, wc, w_ld = _weights(w, x.dtype, names[0])
+    for other, name in zip(weights[1:], names[1:]):
+        if _weights(other, x.dtype, name) != (E, wr, wc, w_ld):
+            raise ValueError("%s and %s must have one shape and one row pitch" % (names[0], name))
+    if (wc if transposed else wr) != K:
+        raise ValueError("%s must be %s for x [rows,K]" % (names[0], "[experts,N,K]" if transposed else "[experts,K,N]"))
+    _whole(offsets, E + 1, "offsets")
+    if tokens is not None:
+        _whole(tokens, -1, "tokens")
+    N = wr if transposed else wc
+    return ax_experts_desc_t(n if tokens is None else tokens.numel(), n, N, K, x_ld, w_ld, N, K, E, _float_dtype(x, "x"), _act_code(act),
+                             int(bool(transposed)), int(tokens is not None), int(not aligned))
+
+
+def _expert_columns(w, transposed) -> int:
+    if w.dim() != 3:
+        raise ValueError("the experts' weights must be [experts, rows, columns]")
+    return w.shape[1] if transposed else w.shape[2]
+
+
+def _rows_of(x, tokens):
+    return x.shape[:-1] if tokens is None else (tokens.numel(),)
+
+
+def ax_matmul_experts(x, w, offsets, tokens=None, act="none", transposed=False, save=False, y_out=None, z_out=None, workspace=None,
+                      stream=None):
+    """y = act(x w_e) for rows grouped by expert: row r is row tokens[r] of x (row r without tokens).  w: [experts,K,N], or
+    [experts,N,K] with transposed; float32 or bfloat16.  Returns (y, z): z, the value before the activation, with save or z_out,
+    otherwise None.  Rows that belong to no expert are not written."""
+    if stream is not None:
+        return _on_stream(ax_matmul_experts, stream, x, w, offsets, tokens, act, transposed, save, y_out, z_out, workspace)
+    L = lib()
+    xp, wp = x.data_ptr(), w.data_ptr()
+    aligned = (wp | (xp if tokens is None else 0)) % 16 == 0
+    key = ("matmul_experts", act, transposed, aligned, save, _sig(x), _sig(w), _sig(offsets), _sig(tokens), _sig(y_out), _sig(z_out))
+    if y_out is None:
+        y_out = x.new_empty(_rows_of(x, tokens) + (_expert_columns(w, transposed),))
+    if z_out is None and save:
+        z_out = torch.empty_like(y_out, memory_format=torch.contiguous_format)
+    hit = _checked.get(key)
+    if hit is None:
+        d = _experts_desc(x, (w,), ("w",), offsets, tokens, act, transposed, aligned)
+        d.y_ld = _mat_of(y_out, x.dtype, d.rows, d.N, "y_out")
+        if z_out is not None:
+            _vec_of(z_out, x.dtype, d.rows * d.N, "z_out")
+        _same_device(x, w, offsets, tokens, y_out, z_out)
+        hit = _remember(key, (d, int(L.ax_matmul_experts_workspace_bytes(d))))
+    d, need = hit
+    _current_device(x)
+    ws = _scratch(need, workspace, x.device)
+    _check(L.ax_matmul_experts(d, xp, _ptr(tokens), offsets.data_ptr(), wp, y_out.data_ptr(), _ptr(z_out), *_ws_args(ws), _stream_ptr(None)))
+    return y_out, z_out
+
+
+def _rows_grad(out, rows, x):
+    return x.new_empty((rows, x.shape[-1])) if out is None else out
+
+
+def _check_weight_grad(out, like, name):
+    if out is not False and _weights(out, like.dtype, name) != _weights(like, like.dtype, name):
+        raise ValueError("%s must have the shape and the row pitch of its tensor" % name)
+
+
+def ax_matmul_experts_backward(gy, x, w, offsets, tokens=None, z=None, act="none", transposed=False, gx_out=None, gw_out=None,
+                               workspace=None, stream=None):
+    """Gradients of ax_matmul_experts: (gx, gw); False skips one.  gx is that of the rows of the products, [rows,K] (with tokens,
+    x's own is their sum: ax_combine without weights); z: the value before the activation."""
+    if stream is not None:
+        return _on_stream(ax_matmul_experts_backward, stream, gy, x, w, offsets, tokens, z, act, transposed, gx_out, gw_out, workspace)
+    L = lib()
+    gp, xp, wp = gy.data_ptr(), x.data_ptr(), w.data_ptr()
+    aligned = (wp | (xp if tokens is None else 0) | (gp if act == "none" else 0)) % 16 == 0
+    key = ("matmul_experts_backward", act, transposed, aligned, _sig(gy), _sig(x), _sig(w), _sig(offsets), _sig(tokens), _sig(z),
+           _sig(gx_out), _sig(gw_out))
+    hit = _checked.get(key)
+    if hit is None:
+        d = _experts_desc(x, (w,), ("w",), offsets, tokens, act, transposed, aligned)
+        d.y_ld = _mat_of(gy, x.dtype, d.rows, d.N, "gy")
+        if z is not None:
+            _vec_of(z, x.dtype, d.rows * d.N, "z")
+        elif d.act:
+            raise ValueError("the gradient of an activation needs z")
+        if gx_out is not None and gx_out is not False:
+            d.gx_ld = _mat_of(gx_out, x.dtype, d.rows, d.K, "gx_out")
+        if gw_out is not None:
+            _check_weight_grad(gw_out, w, "gw_out")
+        _same_device(x, gy, w, offsets, tokens, z, gx_out, gw_out)
+        hit = _remember(key, (d, int(L.ax_matmul_experts_backward_workspace_bytes(d))))
+    d, need = hit
+    _current_device(x)
+    gx_out, gw_out = _rows_grad(gx_out, d.rows, x), _grad_out(gw_out, w)
+    gx_out, gw_out = (None if o is False else o for o in (gx_out, gw_out))
+    ws = _scratch(need, workspace, x.device)
+    _check(L.ax_matmul_experts_backward(d, gp, xp, _ptr(tokens), offsets.data_ptr(), wp, _ptr(z), _ptr(gx_out), _ptr(gw_out),
+                                        *_ws_args(ws), _stream_ptr(None)))
+    return gx_out, gw_out
+
+
+def ax_gated_experts(x, wg, wu, offsets, tokens=None, act="silu", save=False, h_out=None, g_out=None, u_out=None, workspace=None,
+                     stream=None):
+    """h = act(x wg_e) * (x wu_e) for rows grouped by expert, as ax_matmul_experts; wg, wu [experts,K,F].  Returns (h, g, u): both
+    projections with save (or g_out and u_out), otherwise None."""
+    if stream is not None:
+        return _on_stream(ax_gated_experts, stream, x, wg, wu, offsets, tokens, act, save, h_out, g_out, u_out, workspace)
+    L = lib()
+    xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
+    aligned = (gp | up | (xp if tokens is None else 0)) % 16 == 0
+    key = ("gated_experts", act, aligned, save, _sig(x), _sig(wg), _sig(wu), _sig(offsets), _sig(tokens), _sig(h_out), _sig(g_out), _sig(u_out))
+    if h_out is None:
+        h_out = x.new_empty(_rows_of(x, tokens) + (_expert_columns(wg, False),))
+    if save:
+        g_out, u_out = (torch.empty_like(h_out, memory_format=torch.contiguous_format) if o is None else o for o in (g_out, u_out))
+    hit = _checked.get(key)
+    if hit is None:
+        d = _experts_desc(x, (wg, wu), ("wg", "wu"), offsets, tokens, act, False, aligned)
+        d.y_ld = _mat_of(h_out, x.dtype, d.rows, d.N, "h_out")
+        for t, name in ((g_out, "g_out"), (u_out, "u_out")):
+            if t is not None:
+                _vec_of(t, x.dtype, d.rows * d.N, name)
+        _same_device(x, wg, wu, offsets, tokens, h_out, g_out, u_out)
+        hit = _remember(key, (d, int(L.ax_gated_experts_workspace_bytes(d))))
+    d, need = hit
+    _current_device(x)
+    ws = _scratch(need, workspace, x.device)
+    _check(L.ax_gated_experts(d, xp, _ptr(tokens), offsets.data_ptr(), gp, up, h_out.data_ptr(), _ptr(g_out), _ptr(u_out), *_ws_args(ws),
+                              _stream_ptr(None)))
+    return h_out, g_out, u_out
+
+
+def ax_gated_experts_backward(gh, x, wg, wu, g, u, offsets, tokens=None, act="silu", gx_out=None, gwg_out=None, gwu_out=None,
+                              workspace=None, stream=None):
+    """Gradients of ax_gated_experts: (gx, gwg, gwu), gx that of the rows as in ax_matmul_experts_backward; gx_out False, or gwg_out
+    and gwu_out False, skips them."""
+    if stream is not None:
+        return _on_stream(ax_gated_experts_backward, stream, gh, x, wg, wu, g, u, offsets, tokens, act, gx_out, gwg_out, gwu_out, workspace)
+    L = lib()
+    xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
+    aligned = (gp | up | (xp if tokens is None else 0)) % 16 == 0
+    key = ("gated_experts_backward", act, aligned, _sig(gh), _sig(x), _sig(wg), _sig(wu), _sig(g), _sig(u), _sig(offsets), _sig(tokens),
+           _sig(gx_out), _sig(gwg_out), _sig(gwu_out))
+    hit = _checked.get(key)
+    if hit is None:
+        d = _experts_desc(x, (wg, wu), ("wg", "wu"), offsets, tokens, act, False, aligned)
+        d.y_ld = _mat_of(gh, x.dtype, d.rows, d.N, "gh")
+        _vec_of(g, x.dtype, d.rows * d.N, "g")
+        _vec_of(u, x.dtype, d.rows * d.N, "u")
+        if gx_out is not None and gx_out is not False:
+            d.gx_ld = _mat_of(gx_out, x.dtype, d.rows, d.K, "gx_out")
+        for o, like, name in ((gwg_out, wg, "gwg_out"), (gwu_out, wu, "gwu_out")):
+            if o is not None:
+                _check_weight_grad(o, like, name)
+        _same_device(x, gh, wg, wu, g, u, offsets, tokens, gx_out, gwg_out, gwu_out)
+        hit = _remember(key, (d, int(L.ax_gated_experts_backward_workspace_bytes(d))))
+    d, need = hit
+    _current_device(x)
+    gx_out, gwg_out, gwu_out = _rows_grad(gx_out, d.rows, x), _grad_out(gwg_out, wg), _grad_out(gwu_out, wu)
+    gx_out, gwg_out, gwu_out = (None if o is False else o for o in (gx_out, gwg_out, gwu_out))
+    ws = _scratch(need, workspace, x.device)
+    _check(L.ax_gated_experts_backward(d, gh.data_ptr(), xp, _ptr(tokens), offsets.data_ptr(), gp, up, g.data_ptr(), u.data_ptr(),
+                                       _ptr(gx_out), _ptr(gwg_out), _ptr(gwu_out), *_ws_args(ws), _stream_ptr(None)))
+    return gx_out, gwg_out, gwu_out
+
+
+def _combine_desc(h, rows, weights, y, name) -> ax_combine_desc_t:
+    """y: what has a row for every token."""
+    n, cols, ld = _mat(h, h.dtype, "h")
+    _whole(rows, -1, "rows")
+    if rows.dim() < 2:
+        raise ValueError("rows must be [tokens, k]")
+    k = rows.shape[-1]
+    T = math.prod(rows.shape[:-1])
+    if weights is not None:
+        _vec_of(weights, torch.float32, T * k, "weights")
+    y_ld = _mat_of(y, h.dtype, T, cols, name)
+    return ax_combine_desc_t(T, n, cols, ld, cols, y_ld, cols, k, _float_dtype(h, "h"))
+
+
+def ax_combine(h, rows, weights=None, residual=None, y_out=None, stream=None):
+    """y[t] = residual[t] + sum over j of weights[t,j] * h[rows[t,j]]: the tokens' sums of their experts' rows.  rows [tokens,k] int32
+    as ax_route returned them (one outside h is left out), weights [tokens,k] float32 (one each without them).  y_out may be the residual
+    itself."""
+    if stream is not None:
+        return _on_stream(ax_combine, stream, h, rows, weights, residual, y_out)
+    key = ("combine", _sig(h), _sig(rows), _sig(weights), _sig(residual), _sig(y_out))
+    if y_out is None:
+        y_out = h.new_empty(rows.shape[:-1] + h.shape[-1:])
+    d = _checked.get(key)
+    if d is None:
+        d = _combine_desc(h, rows, weights, y_out, "y_out")
+        if residual is not None:
+            d.residual_ld = _mat_of(residual, h.dtype, d.tokens, d.cols, "residual")
+        _same_device(h, rows, weights, residual, y_out)
+        _remember(key, d)
+    _current_device(h)
+    _check(lib().ax_combine(d, h.data_ptr(), rows.data_ptr(), _ptr(weights), _ptr(residual), y_out.data_ptr(), _stream_ptr(None)))
+    return y_out
+
+
+def ax_combine_backward(gy, h, rows, weights=None, gh_out=None, gweights_out=None, stream=None):
+    """Gradients of ax_combine: (gh, gweights); False skips one.  Rows of gh that no choice names are not written; the residual's
+    gradient is gy."""
+    if stream is not None:
+        return _on_stream(ax_combine_backward, stream, gy, h, rows, weights, gh_out, gweights_out)
+    key = ("combine_backward", _sig(gy), _sig(h), _sig(rows), _sig(weights), _sig(gh_out), _sig(gweights_out))
+    if gh_out is None:
+        gh_out = torch.empty_like(h, memory_format=torch.contiguous_format)
+    if gweights_out is None:
+        gweights_out = rows.new_empty(rows.shape, dtype=torch.float32)
+    d = _checked.get(key)
+    if d is None:
+        d = _combine_desc(h, rows, weights, gy, "gy")
+        if gh_out is not False:
+            d.gh_ld = _mat_of(gh_out, h.dtype, d.h_rows, d.cols, "gh_out")
+        if gweights_out is not False:
+            _vec_of(gweights_out, torch.float32, d.tokens * d.k, "gweights_out")
+        _same_device(h, gy, rows, weights, gh_out, gweights_out)
+        _remember(key, d)
+    _current_device(h)
+    gh_out, gweights_out = (None if o is False else o for o in (gh_out, gweights_out))
+    _check(lib().ax_combine_backward(d, gy.data_ptr(), h.data_ptr(), rows.data_ptr(), _ptr(weights), _ptr(gh_out), _ptr(gweights_out),
+                                     _stream_ptr(None)))
+    return gh_out, gweights_out
+
+
+# ---- weights of 4 bits -------------------------------------------------------------------------------------------------
+
+
+class AxQ4:
+    """Weights of 4 bits with a scale for every group of a row, in the library's layout: made once by ax_quantize_q4 or
+    ax_pack_q4, read by ax_matmul_q4 and ax_gated_q4.  rows and cols are those of one matrix (outputs and inputs); experts is
+    None for a single one."""
+
+    def __init__(self, rows, cols, group, experts, device):
+        L = lib()
+        self.rows, self.cols, self.group, self.experts = int(rows), int(cols), int(group), experts
+        if self.group not in (32, 64, 128):
+            raise ValueError("group must be 32, 64 or 128")
+        n = (experts or 1, self.rows, self.cols)
+        c, s = int(L.ax_q4_codes_bytes(*n)), int(L.ax_q4_scales_bytes(*n, self.group))
+        if not c or not s:
+            _check(-2)
+        self.codes = torch.empty(c, dtype=torch.uint8, device=device)
+        self.scales = torch.empty(s // 2, dtype=torch.bfloat16, device=device)
+
+    @property
+    def shape(self):
+        """[outputs, inputs], or [experts, outputs, inputs]."""
+        return ((self.experts,) if self.experts else ()) + (self.rows, self.cols)
+
+    def _sizes(self):
+        return self.experts or 1, self.rows, self.cols, self.group
+
+    def values(self, stream=None):
+        """The weights that the codes and scales stand for, float32."""
+        return _q4_values(self) if stream is None else _on_stream(_q4_values, stream, self)
+
+
+def _q4_values(w):
+    _current_device(w.codes)
+    out = torch.empty(w.shape, dtype=torch.float32, device=w.codes.device)
+    _check(lib().ax_q4_values(w.codes.data_ptr(), w.scales.data_ptr(), *w._sizes(), out.data_ptr(), _stream_ptr(None)))
+    return out
+
+
+def ax_quantize_q4(w, group=128, stream=None) -> AxQ4:
+    """Float weights [outputs, inputs], or [experts, outputs, inputs], in 4 bits: of every `group` inputs of a row the scale is the
+    largest |w| / 7 (bfloat16), the codes w / scale rounded, -8 .. 7."""
+    if stream is not None:
+        return _on_stream(ax_quantize_q4, stream, w, group)
+    dt = _float_dtype(w, "w")
+    if w.dim() == 3:
+        E, r, c, ld = _weights(w, w.dtype, "w")
+    else:
+        E, (r, c, ld) = None, _mat(w, w.dtype, "w")
+        if w.dim() != 2:
+            raise ValueError("w must be [outputs, inputs] or [experts, outputs, inputs]")
+    _current_device(w)
+    q = AxQ4(r, c, group, E, w.device)
+    _check(lib().ax_quantize_q4(w.data_ptr(), dt, ld, *q._sizes(), q.codes.data_ptr(), q.scales.data_ptr(), _stream_ptr(None)))
+    return q
+
+
+def ax_pack_q4(codes, scales, group=128, stream=None) -> AxQ4:
+    """Codes and scales from elsewhere: codes int8 [outputs, inputs] or [experts, outputs, inputs], -8 .. 7; scales bfloat16 of the
+    same shape with one for every `group` inputs."""
+    if stream is not None:
+        return _on_stream(ax_pack_q4, stream, codes, scales, group)
+    _dev(codes, torch.int8, "codes")
+    _dev(scales, torch.bfloat16, "scales")
+    if codes.dim() not in (2, 3) or group not in (32, 64, 128):
+        raise ValueError("codes must be [outputs, inputs] or [experts, outputs, inputs], group 32, 64 or 128")
+    if scales.shape != codes.shape[:-1] + (-(-codes.shape[-1] // group),):
+        raise ValueError("scales must have one for every group of a row")
+    _same_device(codes, scales)
+    _current_device(codes)
+    q = AxQ4(codes.shape[-2], codes.shape[-1], group, codes.shape[0] if codes.dim() == 3 else None, codes.device)
+    _check(lib().ax_pack_q4(codes.data_ptr(), scales.data_ptr(), *q._sizes(), q.codes.data_ptr(), q.scales.data_ptr(), _stream_ptr(None)))
+    return q
+
+
+def _q4_desc(x, weights, offsets, tokens, act, aligned) -> ax_q4_desc_t:
+    w = weights[0]
+    n, K, x_ld = _mat(x, x.dtype, "x")
+    for other in weights:
+        if not isinstance(other, AxQ4):
+            raise TypeError("weights must be AxQ4")
+        if other.shape != w.shape or other.group != w.group:
+            raise ValueError("both weights must have one shape and one group")
+    if K != w.cols:
+        raise ValueError("x must be [rows, %d] for these weights" % w.cols)
+    E = w.experts or 1
+    if offsets is not None:
+        _whole(offsets, E + 1, "offsets")
+    elif E > 1:
+        raise ValueError("weights of several experts need offsets")
+    if tokens is not None:
+        _whole(tokens, -1, "tokens")
+    return ax_q4_desc_t(n if tokens is None else tokens.numel(), n, w.rows, K, x_ld, w.rows, w.rows, E, w.group, _float_dtype(x, "x"),
+                        _act_code(act), int(tokens is not None), int(not aligned))
+
+
+def _q4_sig(w):
+    return (w.experts, w.rows, w.cols, w.group, w.codes.device) if isinstance(w, AxQ4) else None
+
+
+def ax_matmul_q4(x, w, bias=None, residual=None, act="none", offsets=None, tokens=None, y_out=None, workspace=None, stream=None):
+    """y = act(x w^T + bias) + residual with weights of 4 bits (AxQ4).  x: [rows, inputs], float32 or bfloat16, as bias, residual and
+    y are.  Weights of several experts: rows grouped by them, as in ax_matmul_experts."""
+    if stream is not None:
+        return _on_stream(ax_matmul_q4, stream, x, w, bias, residual, act, offsets, tokens, y_out, workspace)
+    L = lib()
+    xp = x.data_ptr()
+    aligned = tokens is not None or xp % 16 == 0
+    key = ("matmul_q4", act, aligned, _sig(x), _q4_sig(w), _sig(bias), _sig(residual), _sig(offsets), _sig(tokens), _sig(y_out))
+    hit = _checked.get(key)
+    if hit is None:
+        d = _q4_desc(x, (w,), offsets, tokens, act, aligned)
+        if bias is not None:
+            _vec_of(bias, x.dtype, d.N, "bias")
+        if residual is not None:
+            d.residual_ld = _mat_of(residual, x.dtype, d.rows, d.N, "residual")
+        if y_out is not None:
+            d.y_ld = _mat_of(y_out, x.dtype, d.rows, d.N, "y_out")
+        _same_device(x, w.codes, bias, residual, offsets, tokens, y_out)
+        hit = _remember(key, (d, int(L.ax_matmul_q4_workspace_bytes(d))))
+    d, need = hit
+    _current_device(x)
+    if y_out is None:
+        y_out = x.new_empty(_rows_of(x, tokens) + (w.rows,))
+    ws = _scratch(need, workspace, x.device)
+    _check(L.ax_matmul_q4(d, xp, _ptr(tokens), _ptr(offsets), w.codes.data_ptr(), w.scales.data_ptr(), _ptr(bias), _ptr(residual),
+                          y_out.data_ptr(), *_ws_args(ws), _stream_ptr(None)))
+    return y_out
+
+
+def ax_gated_q4(x, wg, wu, act="silu", offsets=None, tokens=None, h_out=None, workspace=None, stream=None):
+    """h = act(x wg^T) * (x wu^T) with weights of 4 bits (AxQ4), as ax_matmul_q4."""
+    if stream is not None:
+        return _on_stream(ax_gated_q4, stream, x, wg, wu, act, offsets, tokens, h_out, workspace)
+    L = lib()
+    xp = x.data_ptr()
+    aligned = tokens is not None or xp % 16 == 0
+    key = ("gated_q4", act, aligned, _sig(x), _q4_sig(wg), _q4_sig(wu), _sig(offsets), _sig(tokens), _sig(h_out))
+    hit = _checked.get(key)
+    if hit is None:
+        d = _q4_desc(x, (wg, wu), offsets, tokens, act, aligned)
+        if h_out is not None:
+            d.y_ld = _mat_of(h_out, x.dtype, d.rows, d.N, "h_out")
+        _same_device(x, wg.codes, wu.codes, offsets, tokens, h_out)
+        hit = _remember(key, (d, int(L.ax_gated_q4_workspace_bytes(d))))
+    d, need = hit
+    _current_device(x)
+    if h_out is None:
+        h_out = x.new_empty(_rows_of(x, tokens) + (wg.rows,))
+    ws = _scratch(need, workspace, x.device)
+    _check(L.ax_gated_q4(d, xp, _ptr(tokens), _ptr(offsets), wg.codes.data_ptr(), wg.scales.data_ptr(), wu.codes.data_ptr(),
+                         wu.scales.data_ptr(), h_out.data_ptr(), *_ws_args(ws), _stream_ptr(None)))
+    return h_out
 
 
 class AxAdamW:

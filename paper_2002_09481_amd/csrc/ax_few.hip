@@ -19,6 +19,7 @@
 
 #include "ax_float.h"
 #include "ax_gemm.h"
+#include "ax_group.h"
 
 namespace ax {
 namespace {
@@ -38,6 +39,10 @@ struct Args {
   int per;
   float* part;  // [slices][NB][M][ldp] with slices, as the joining kernel reads them
   long long ldp;
+  Groups e;                // rows grouped by expert
+  const int32_t* index;    // of the grouped rows into those of x (null: the same)
+  int x_rows;
+  long long next;          // bytes from one expert's weights to the next one's
 };
 
 // One operand of the matrix instruction: bf16 or int8 as they are, float32 as three pieces.
@@ -101,6 +106,10 @@ struct Along {
       q[w >> 2][w & 3] = v;
     }
   }
+  __device__ __forceinline__ void clear() {
+    q[0] = u32x4{0, 0, 0, 0};
+    if (KD == kF32) q[KD == kF32 ? 1 : 0] = q[0];
+  }
   __device__ __forceinline__ void fragment(Frag<KD>& f) const {
     if constexpr (KD == kF32) {
       float v[8];
@@ -160,8 +169,8 @@ struct Across {
 
 // LB: 0 = weights [N, K], 1 = [K, N].  NB: 2 for the gated pair.  MFR: fragments of 16 rows.  CF: fragments of 16 columns
 // of one weight (LB = 1: neighbouring columns a lane).  U: steps of the contraction a wave loads at a time.
-// ODD: rows may start inside a word (not for float32).
-template <Kind KD, int LB, int NB, int MFR, int CF, int U, bool ODD>
+// ODD: rows may start inside a word (not for float32).  GR: rows grouped by expert; a workgroup has up to 16 MFR of one expert.
+template <Kind KD, int LB, int NB, int MFR, int CF, int U, bool ODD, bool GR = false>
 __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
   constexpr int KS = KD == kInt8 ? 64 : 32, LANE = KS / 4;  // contraction of a step, of a lane
   constexpr int ES = KD == kInt8 ? 1 : KD == kBf16 ? 2 : 4;
@@ -172,8 +181,18 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
   const int t = threadIdx.x, lane = t & 63, r = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   // workgroups b, b + 8, ... share an XCD: they take neighbouring columns, which may share lines of memory
-  int tile, slice, m0 = 0;
-  {
+  int tile, slice = 0, m0 = 0, M = g.M, row_at = 0;
+  long long w_at = 0;
+  if constexpr (GR) {  // (the columns of one expert: workgroups of an XCD take neighbours)
+    GroupTile e;
+    if (!find_tile(a.e.offsets, a.e.experts, a.e.rows, 16 * MFR, a.tiles, blockIdx.x, e)) return;
+    const int bands = e.tiles / a.tiles, k = xcd_run(e.tile, e.tiles);
+    m0 = __builtin_amdgcn_readfirstlane(k % bands) * 16 * MFR;
+    tile = __builtin_amdgcn_readfirstlane(k / bands);
+    M = __builtin_amdgcn_readfirstlane(e.count);
+    row_at = __builtin_amdgcn_readfirstlane(e.first);
+    w_at = __builtin_amdgcn_readfirstlane(e.expert) * a.next;
+  } else {
     const int b = blockIdx.x, x = b & 7, i = b >> 3, total = gridDim.x, per = total >> 3, more = total & 7;
     tile = x * per + min(x, more) + i;
     if (a.bands > 1) {  // neighbours: the weights come from memory once
@@ -194,6 +213,18 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
 #pragma unroll
       for (int j = 0; j < CF; ++j) acc[b][i][j] = Acc{};
 
+  // grouped: where this lane's rows of x are
+  long long x_at[GR ? MFR : 1];
+  bool there[GR ? MFR : 1];
+  if constexpr (GR) {
+#pragma unroll
+    for (int i = 0; i < MFR; ++i) {
+      const int m = row_at + min(m0 + 16 * i + r, M - 1), k = a.index ? a.index[m] : m;
+      there[i] = k >= 0 && k < a.x_rows;  // (another index stands for a row of zeros)
+      x_at[i] = there[i] ? k * g.lda : 0;
+    }
+  }
+
   const bool all_cols = n0 + COLS <= g.N;
   const int groups = (a.blocks + U - 1) / U;
   const int behind = min((slice + 1) * a.per, groups * g.nseg);
@@ -201,7 +232,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
     const int seg = __builtin_amdgcn_readfirstlane(g.nseg == 1 ? 0 : it / groups);
     const int k0 = (it - seg * groups) * U * KS;
     const char* x = (const char*)g.seg[seg].a;
-    const char* w[2] = {(const char*)g.seg[seg].b, (const char*)g.seg[seg].b2};
+    const char* w[2] = {(const char*)g.seg[seg].b + w_at, (const char*)g.seg[seg].b2 + w_at};
     auto run = [&](auto full) __attribute__((always_inline)) {
       Along<KD, ODD> xa[U][MFR];
       typename std::conditional<LB == 0, Along<KD, ODD>, Across<KD == kInt8 ? kBf16 : KD, CF>>::type wa[U][NB][LB == 0 ? CF : 1];
@@ -222,13 +253,21 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
           }
         }
 #pragma unroll
-        for (int i = 0; i < MFR; ++i) xa[u][i].template load<full>(x + min(m0 + 16 * i + r, g.M - 1) * g.lda, k, left);
+        for (int i = 0; i < MFR; ++i) {
+          if constexpr (GR) xa[u][i].template load<full>(x + x_at[i], k, left);
+          else xa[u][i].template load<full>(x + min(m0 + 16 * i + r, g.M - 1) * g.lda, k, left);
+        }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         Frag<KD> fx[MFR];
 #pragma unroll
-        for (int i = 0; i < MFR; ++i) xa[u][i].fragment(fx[i]);
+        for (int i = 0; i < MFR; ++i) {
+          if constexpr (GR) {
+            if (!there[i]) xa[u][i].clear();
+          }
+          xa[u][i].fragment(fx[i]);
+        }
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -258,8 +297,8 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
       }
   __syncthreads();
   for (int o = t; o < 16 * MFR * COLS; o += kThreads) {
-    const int row = o / COLS, c = o - row * COLS, m = m0 + row, n = n0 + c;
-    if (m >= g.M || n >= g.N) continue;
+    const int row = o / COLS, c = o - row * COLS, n = n0 + c, m = row_at + m0 + row;
+    if (m0 + row >= M || n >= g.N) continue;
     float s[2];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -348,6 +387,21 @@ void launch_rows(Args& a, hipStream_t s) {
   launch_cols<KD, LB, NB, 1>(a, s);
 }
 
+// Grouped: 16 rows of an expert a workgroup, or 32 where an expert can expect more.
+template <Kind KD, int LB, int NB, int MFR>
+void launch_group(Args& a, hipStream_t s) {
+  constexpr int U = steps_of(KD, LB, NB, MFR), CF = cols_of(KD, LB, NB, MFR, 1);
+  a.tiles = (a.g.N + 16 * CF - 1) / (16 * CF);
+  a.per = (a.blocks + U - 1) / U;
+  const long long grid = (a.e.rows / (16 * MFR) + std::min(a.e.experts, a.e.rows)) * (long long)a.tiles;
+  few_kernel<KD, LB, NB, MFR, CF, U, false, true><<<(int)grid, kThreads, 0, s>>>(a);
+}
+template <Kind KD, int LB, int NB>
+void launch_group_rows(Args& a, hipStream_t s) {
+  if (a.e.rows > 16 * std::min(a.e.experts, a.e.rows)) return launch_group<KD, LB, NB, 2>(a, s);
+  launch_group<KD, LB, NB, 1>(a, s);
+}
+
 Kind kind_of(const GemmArgs& g, int dtype) { return g.i8 ? kInt8 : dtype == AX_BF16 ? kBf16 : kF32; }
 int blocks_of(const GemmArgs& g) { return (g.K + (g.i8 ? 63 : 31)) / (g.i8 ? 64 : 32); }
 
@@ -397,6 +451,25 @@ hipError_t launch_few(const GemmArgs& g, int dtype, const FewPlan& p, void* part
   }
   const hipError_t rc = hipGetLastError();
   return rc != hipSuccess || p.slices == 1 ? rc : launch_join(g, p.slices, part, s);
+}
+
+hipError_t launch_few_experts(const GemmArgs& g, int dtype, const Groups& e, const int32_t* index, int x_rows, hipStream_t s) {
+  Args a{};
+  a.g = g;
+  a.blocks = blocks_of(g);
+  a.slices = 1;
+  a.e = e;
+  a.index = index;
+  a.x_rows = x_rows;
+  a.next = (long long)(g.lb == 0 ? g.N : g.K) * g.ldb;
+  if (kind_of(g, dtype) == kBf16) {
+    if (g.gated) launch_group_rows<kBf16, 1, 2>(a, s);
+    else g.lb == 0 ? launch_group_rows<kBf16, 0, 1>(a, s) : launch_group_rows<kBf16, 1, 1>(a, s);
+  } else {
+    if (g.gated) launch_group_rows<kF32, 1, 2>(a, s);
+    else g.lb == 0 ? launch_group_rows<kF32, 0, 1>(a, s) : launch_group_rows<kF32, 1, 1>(a, s);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace ax

@@ -57,6 +57,18 @@ hipError_t launch_gemm(const GemmArgs& g, const GemmPlan& p, void* part, hipStre
 // y from the partial sums [splits][planes][M][N rounded up to 8] of the slices, with the epilogue.
 hipError_t launch_join(const GemmArgs& g, int splits, void* part, hipStream_t s);
 
+// Products of rows grouped by expert (ax_gemm_experts.hip).  offsets [experts + 1] (device; null: one expert, all rows) are the
+// experts' first rows; the experts' right operands lie one behind the other.  sums false: rows of a times the matrix of their
+// expert, g.M = rows.  sums true: for every expert a^T b over its rows, g.K = rows, results one behind the other.  No slices,
+// bf16 operands or pieces, results of the operands' type.
+struct Groups {
+  const int32_t* offsets;
+  int experts, rows;
+};
+int plan_experts(const GemmArgs& g, const Groups& e, bool sums);  // the tile configuration
+void tile_of_experts(const GemmArgs& g, int tile, int* rows, int* cols);
+hipError_t launch_gemm_experts(const GemmArgs& g, const Groups& e, bool sums, int tile, hipStream_t s);
+
 // Products of few rows straight from the operands in their own type, at any element: int8 (g.i8), or dtype AX_BF16 or
 // AX_F32.  g as above; seg holds the operands themselves, la is 0, dual is not taken.  Meant for up to 64 rows.
 struct FewPlan {
@@ -65,5 +77,8 @@ struct FewPlan {
 };
 FewPlan plan_few(const GemmArgs& g, int dtype);
 hipError_t launch_few(const GemmArgs& g, int dtype, const FewPlan& p, void* part, hipStream_t s);
+
+// Few rows an expert, forward only: rows index[r] of x (null: row r; x_rows there are) straight from the operands.  g.M = rows.
+hipError_t launch_few_experts(const GemmArgs& g, int dtype, const Groups& e, const int32_t* index, int x_rows, hipStream_t s);
 
 }  // namespace ax

@@ -1,0 +1,78 @@
+// Rows grouped by expert: where the tile of a workgroup lies.
+//
+// The experts' sizes are known on the device alone (the router has just counted them), so a launch has as many workgroups as
+// there can be tiles, and each looks its own up in the offsets: 64 experts at a time, a lane each, summed over the wave.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "axconv.h"
+
+namespace ax {
+
+constexpr int kMaxExperts = AX_MAX_EXPERTS;
+
+// Rows of an expert, within the rows that there are whatever the offsets hold.
+struct Span {
+  int first, count;
+};
+__device__ __forceinline__ Span span_of(const int32_t* offsets, int e, int rows) {
+  const int lo = min(max(offsets[e], 0), rows), hi = min(max(offsets[e + 1], lo), rows);
+  return Span{lo, hi - lo};
+}
+
+struct GroupTile {
+  int expert, first, count;  // its rows
+  int tile, tiles;           // of the expert's tiles
+  int total;                 // tiles of all experts
+};
+
+// Tile `want` of all experts' tiles, `per` for every (begun) `height` rows; false where there are not as many.  Without offsets
+// all rows are those of one expert.  height and per are above zero.
+__device__ __forceinline__ bool find_tile(const int32_t* offsets, int experts, int rows, int height, int per, int want, GroupTile& g) {
+  if (!offsets) {
+    g = GroupTile{0, 0, rows, want, (rows + height - 1) / height * per, 0};
+    g.total = g.tiles;
+    return want < g.tiles;
+  }
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  bool found = false;
+  g = GroupTile{};
+  for (int base = 0; base < experts; base += 64) {
+    Span s{0, 0};
+    if (base + lane < experts) s = span_of(offsets, base + lane, rows);
+    const int mine = (s.count + height - 1) / height * per;
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int v = __shfl_up(upto, d);
+      if (lane >= d) upto += v;
+    }
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    if (!found && want - before < all) {
+      const unsigned long long behind = __ballot(want - before < upto);
+      if (behind) {
+        const int l = __builtin_ctzll(behind);
+        found = true;
+        g.expert = base + l;
+        g.first = __builtin_amdgcn_readlane(s.first, l);
+        g.count = __builtin_amdgcn_readlane(s.count, l);
+        g.tiles = __builtin_amdgcn_readlane(mine, l);
+        g.tile = want - before - (__builtin_amdgcn_readlane(upto, l) - g.tiles);
+      }
+    }
+    before += all;
+  }
+  g.total = before;
+  return found && g.tile >= 0 && g.tile < g.tiles;  // (sums that leave 32 bits: only with offsets that do not ascend)
+}
+
+// Workgroups b, b + 8, ... share an XCD and its L2: item b of n in an order in which they take neighbouring ones.
+__device__ __forceinline__ int xcd_run(int b, int n) {
+  const int x = b & 7, i = b >> 3;
+  return x * (n >> 3) + min(x, n & 7) + i;
+}
+
+}  // namespace ax

@@ -10,56 +10,16 @@
 #include <algorithm>
 
 #include "ax_float.h"
-#include "ax_gemm.h"
 #include "ax_norm.h"
+#include "ax_operand.h"
 #include "axconv_probe.h"
 
 namespace ax {
 namespace {
 
-constexpr size_t kAlign = 256;
-
-// Hands out pieces of the workspace; with base 0 it only counts.
-struct Arena {
-  uintptr_t base;
-  size_t used = 0;
-  explicit Arena(void* p) : base((uintptr_t)p) {}
-  void* take(size_t bytes) {
-    void* p = (void*)(base + used);
-    used += (bytes + kAlign - 1) / kAlign * kAlign;
-    return p;
-  }
-};
-
-inline int elem_bytes(int dtype) { return dtype == AX_F32 ? 4 : 2; }
-
-// A matrix as the products read it: planes of bf16 (or int8) rows whose length is a multiple of 16 bytes.
-struct Operand {
-  const void* p;
-  int planes;       // 3 for float32
-  long long plane;  // bytes from one to the next
-  long long ld;     // bytes
-  long long cols;  // row length, rounded up to whole 16-byte chunks (zeros behind the given columns)
-};
-
-struct PackJob {
-  const void* src;
-  void* dst;  // planes back to back; null: read in place
-  long long rows, cols, ld;  // of the source, elements
-  long long pcols;  // cols in whole chunks, zeros behind cols
-  long long pitch;  // of the copy, elements
-  int dtype;  // AX_F32, AX_BF16, or kI8
-};
-constexpr int kI8 = 2;
-
 // Rows copied into the form the products read: eight elements (16 bytes of output; int8: 16) a thread, all the operands of a
 // product in one launch.  Bound by memory: 4 bytes read and 6 written per float32 element (28 M of them 45 us, 6.3 TB/s with
 // part of it in the caches).
-struct PackBatch {
-  PackJob job[3];
-  int first[3];  // workgroup that each job starts at
-  int blocks[3];
-};
 template <int DT>
 __device__ __forceinline__ void pack_rows(const PackBatch& b, int block) {
   constexpr int E = DT == kI8 ? 16 : 8;
@@ -101,10 +61,8 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackBatch b) {
   pack_rows<DT>(b, blockIdx.x);
 }
 
-int grid_for(long long items) { return (int)std::max<long long>(1, std::min<long long>((items + 255) / 256, 8192)); }
+}  // namespace
 
-// The jobs of an operation that have something to copy (wanted[i]: whether job i is needed by this call); returns the
-// workgroups that they take.
 int fill_pack(PackBatch* b, const PackJob* jobs, const bool* wanted, int n) {
   int k = 0, grid = 0;
   for (int i = 0; i < 3; ++i) b->first[i] = 0x7fffffff;
@@ -127,45 +85,7 @@ hipError_t run_pack(const PackBatch& b, int grid, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Row pitch of a copy: whole lines of 128 bytes, and not a multiple of 2 KB, at which the pieces of one stage of a tile
-// fall on few channels (bf16 8192^3, both operands contiguous along the sum: 956 us at 16 KB, 863 us at 16 KB + 128).
-long long copy_pitch(long long cols, int esz) {
-  const long long line = 128 / esz, pitch = (cols + line - 1) / line * line;
-  return pitch * esz % 2048 ? pitch : pitch + line;
-}
-
-// Whether the matrix is read in place or copied is decided by its description alone, so that the workspace query knows.
-Operand make_operand(const void* p, long long rows, long long cols, long long ld, int dtype, bool unaligned, Arena& ar, PackJob* job) {
-  Operand o{};
-  const int chunk = dtype == kI8 ? 16 : 8, esz = dtype == kI8 ? 1 : 2;
-  const long long pcols = (cols + chunk - 1) / chunk * chunk;
-  const long long pitch = copy_pitch(cols, esz);
-  *job = PackJob{p, nullptr, rows, cols, ld, pcols, pitch, dtype};
-  o.cols = pcols;
-  if (dtype != AX_F32 && !unaligned && pcols == cols && ld % chunk == 0) {
-    o.planes = 1;
-    o.p = p;
-    o.ld = ld * esz;
-    return o;
-  }
-  o.planes = dtype == AX_F32 ? 3 : 1;
-  o.ld = pitch * esz;
-  const size_t plane = (size_t)rows * pitch * esz;
-  job->dst = ar.take(plane * o.planes);
-  o.p = job->dst;
-  o.plane = (long long)plane;
-  return o;
-}
-
-// A factor pair of a product (all pairs of a product have the same pitches).
-void add_segment(GemmArgs* g, const Operand& a, const Operand& b, const Operand* b2) {
-  g->seg[g->nseg++] = GemmSeg{a.p, b.p, b2 ? b2->p : nullptr};
-  g->pieces = a.planes;
-  g->lda = a.ld;
-  g->ldb = b.ld;
-  g->a_plane = a.plane;
-  g->b_plane = b.plane;
-}
+namespace {
 
 // ---- elementwise part of the gradients ---------------------------------------------------------------------------
 //
@@ -176,18 +96,6 @@ void add_segment(GemmArgs* g, const Operand& a, const Operand& b, const Operand*
 // bf16: gz is rounded to bf16, since the matrix instructions take 16-bit operands.  The products' error grows from that of their
 // results' own rounding, 1.7e-3 in the 2-norm, to 2.3e-3 (gated gradients, 4101 x 2048 -> 5512); as two pieces gz would double
 // both products (380 of 460 us).  The sums of gz, and outer_kernel's weight gradients, take it unrounded.
-struct GradArgs {
-  const void* gy;  // [M, N], pitch ldy (GATED: gh)
-  const void* z;   // [M, N], pitch N (may be NULL; GATED: the gate projection)
-  const void* u;   // GATED
-  void* gz;        // planes [M, pcols] (may be NULL: gy itself is read by the products)
-  void* gu;        // GATED
-  float* part;     // [row blocks][N] (may be NULL)
-  long long ldy, pcols, pitch;  // pcols, pitch: of gz and gu
-  int M, N, act, rows_per;
-  int wide, blocks;  // workgroups along the columns, in all
-};
-
 template <int DT>
 __device__ __forceinline__ void write_planes(void* dst, long long rows, long long pitch, long long r, long long c, const float (&v)[8]) {
   if (DT == AX_F32) {
@@ -355,18 +263,7 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(uint8_t* p, long long ro
   }
 }
 
-int rows_per_block(int M, int N) {  // about eight workgroups per compute unit, at least eight rows each
-  const long long cols = (N + 255) / 256;
-  const long long want = std::max(1ll, 2048 / cols);
-  return (int)std::max(8ll, ((M + want - 1) / want + 7) / 8 * 8);
-}
-
 // ---- checks ------------------------------------------------------------------------------------------------------
-
-constexpr long long kMaxDim = 1 << 30, kMaxPitch = 1 << 22;
-
-bool dtype_ok(int d) { return d == AX_F32 || d == AX_BF16; }
-bool pitch_ok(long long ld, long long cols, int esz) { return ld >= cols && ld * esz < kMaxPitch; }
 
 int check_desc(const ax_matmul_desc_t* d, bool q8, bool backward, bool gated) {
   if (!d) return AX_ERR_NULL;
@@ -382,18 +279,6 @@ int check_desc(const ax_matmul_desc_t* d, bool q8, bool backward, bool gated) {
   if (q8 && d->K > 131071) return AX_ERR_K_OVERFLOW;  // 131072 * 128 * 128 = 2^31
   return AX_OK;
 }
-// 16-byte operands where the description promises them, element alignment otherwise.
-bool operand_aligned(const void* p, int esz, bool unaligned, long long cols, long long ld, int dtype) {
-  if ((uintptr_t)p % esz) return false;
-  const int chunk = 16 / esz;
-  const bool in_place = dtype != AX_F32 && !unaligned && cols % chunk == 0 && ld % chunk == 0;
-  return !in_place || (uintptr_t)p % 16 == 0;
-}
-bool aligned_to(const void* p, int esz) { return (uintptr_t)p % esz == 0; }
-bool ws_ok(const void* ws, size_t have, size_t need) {
-  return need == 0 || (ws && (uintptr_t)ws % kAlign == 0 && have >= need);
-}
-
 // ---- forward -----------------------------------------------------------------------------------------------------
 
 struct Forward {
@@ -603,12 +488,20 @@ Backward make_backward(const ax_matmul_desc_t* d, bool gated, const void* gy, co
 }
 
 template <bool GATED>
-hipError_t run_act_grad(const GradArgs& a, const PackBatch& copies, int copy_blocks, int dtype, hipStream_t s) {
-  const int grid = a.blocks + copy_blocks;
+void run_act_grad(const GradArgs& a, const PackBatch& copies, int grid, int dtype, hipStream_t s) {
   if (dtype == AX_F32) act_grad_kernel<AX_F32, GATED><<<grid, 256, 0, s>>>(a, copies);
   else act_grad_kernel<AX_BF16, GATED><<<grid, 256, 0, s>>>(a, copies);
+}
+
+}  // namespace
+
+hipError_t launch_act_grad(const GradArgs& a, bool gated, const PackBatch& copies, int copy_blocks, int dtype, hipStream_t s) {
+  const int grid = a.blocks + copy_blocks;
+  gated ? run_act_grad<true>(a, copies, grid, dtype, s) : run_act_grad<false>(a, copies, grid, dtype, s);
   return hipGetLastError();
 }
+
+namespace {
 
 struct FewBackward {
   OuterArgs o;
@@ -697,10 +590,14 @@ int run_few_backward(FewBackward& b, int dtype, bool gated, void* gx_out, void* 
   return AX_OK;
 }
 
+}  // namespace
+
 hipError_t zero_rows(void* p, long long rows, long long cols, long long ld, int esz, hipStream_t s) {
   zero_rows_kernel<<<grid_for(rows * cols * esz / 2), 256, 0, s>>>((uint8_t*)p, rows, cols * esz, ld * esz);
   return hipGetLastError();
 }
+
+namespace {
 
 int backward_common(const ax_matmul_desc_t* d, bool gated, const void* gy, const void* x, const void* w, const void* w2,
                     const void* z, const void* u, void* gx_out, void* gw_out, void* gw2_out, float* gb_out, void* ws,
@@ -727,11 +624,11 @@ int backward_common(const ax_matmul_desc_t* d, bool gated, const void* gy, const
   PackBatch copies{};
   const int copy_blocks = fill_pack(&copies, b.jobs, wanted, 3);
   if (gated) {
-    if (run_act_grad<true>(b.ga, copies, copy_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
+    if (launch_act_grad(b.ga, true, copies, copy_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
   } else if ((b.elementwise && products) || gb_out) {
     if (!products) b.ga.gz = nullptr;
     b.ga.part = gb_out ? b.part : nullptr;
-    if (run_act_grad<false>(b.ga, copies, copy_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
+    if (launch_act_grad(b.ga, false, copies, copy_blocks, d->dtype, s) != hipSuccess) return AX_ERR_HIP;
     if (gb_out) {
       if (launch_column_sum(b.part, b.row_blocks, (int)d->N, gb_out, s) != hipSuccess) return AX_ERR_HIP;
     }
