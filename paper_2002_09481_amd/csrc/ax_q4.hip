@@ -5,13 +5,18 @@
 //
 // Layout.  A block holds 16 rows and 128 columns of the weights in 1 KB, as the matrix instruction wants them: lane (r, q) of a wave
 // has 16 bytes, word s of which holds columns 32 s + 8 q .. + 7 of row r, the first in the low bits.  Blocks of a row of
-// blocks follow one another, then those of the next 16 rows, then those of the next expert.  Scales: [16 rows][groups], the 16 rows of a
-// group side by side.  What lies behind the last row or column has codes and scales of zero.
+// blocks follow one another, then those of the next 16 rows, then those of the next expert.  Scales in the same order of blocks:
+// [4 quads of rows][groups of the block][4 rows], a quad's side by side for the lanes that hold its sums.  What lies behind the last
+// row or column has codes and scales of zero.
 //
 // Few rows of x (q4_kernel).  Bound by reading the weights once, half a byte each.  A wave reads whole blocks, 1 KB at
 // a time, and turns words into operands of the matrix instruction in registers: codes are whole numbers that bf16 holds, so
 // the products with x (float32: its three bf16 pieces) are exact, and each group's sum in float32 is multiplied by its
-// scale in float32.  No weight is rounded.  The waves of a workgroup share the contraction and meet in LDS.
+// scale in float32.  No weight is rounded.  The waves of a workgroup share the contraction and meet in LDS.  Measured (us at rows / K / N,
+// group, back to back; in brackets the bytes at the rate of a large copy): bf16 1/4096/4096, 128 5.0 (1.7), 8/8192/8192, 32 15.2 (7.4), gated
+// 1/4096/14336, 128 19.8 (11.8), 64/4096/4096, 128 18.0 (1.9), 256/4096/4096, 128 25.2 (2.5); float32 1/4096/4096, 128 7.5 (1.7); gated, 68 rows of
+// 32 experts, 2048/1409, 32 28 (20.3).  What is left: a workgroup's way from its launch to its first block, and the meeting at its end; from 64
+// rows on the conversion of codes, 20 instructions for eight.
 //
 // Many rows.  The weights are written out once, in the workspace, and multiplied by tiles (ax_gemm_experts.hip): bf16 rounds each
 // weight, scale times code, to nearest (2^-9 of it at most; codes and scales have eleven significant bits together), an
@@ -44,6 +49,9 @@ inline Shape shape_of(long long N, long long K, int group) {
   return s;
 }
 
+// Scale of row r of a tile of rows for group g of block `at` (tile * blocks + block), per groups a block.
+__device__ __forceinline__ long long scale_at(long long at, int per, int g, int r) { return (at * per * 4 + (r >> 2) * per + g) * 4 + (r & 3); }
+
 // Eight codes of a word as bf16.  (The conversion takes a code for sixteenths: what comes out is c / 16.)
 __device__ __forceinline__ u32x4 widen(uint32_t d) {
   u32x4 v;
@@ -71,18 +79,36 @@ struct Args {
   int wide;                   // workgroups along the columns
 };
 
+// Eight float32 values in three pieces of bf16, cut instead of rounded: all products of the pieces with a code are taken, so their sum is
+// exact either way, and cutting is a quarter of the instructions.  (An infinity leaves a NaN in the later pieces.)
+__device__ __forceinline__ void cut_in_pieces(const float (&v)[8], u32x4 (&p)[3]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo = v[2 * i], hi = v[2 * i + 1];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      p[k][i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+      if (k < 2) {
+        lo -= __uint_as_float(__float_as_uint(lo) & 0xffff0000u);
+        hi -= __uint_as_float(__float_as_uint(hi) & 0xffff0000u);
+      }
+    }
+  }
+}
+
 // Eight elements of x at any alignment, `left` of them there, as operands: themselves, or three pieces.
 template <bool F32>
 struct XPart {
   u32x4 p[F32 ? 3 : 1];
+  template <bool FULL>
   __device__ __forceinline__ void load(const void* x, long long i, int left) {
     if constexpr (F32) {
       float v[8];
-      load_elems<true, 8>(x, i, left, v);
-      pieces_of(v, p);
+      load_elems<true, 8>(x, i, FULL ? 8 : left, v);
+      cut_in_pieces(v, p);
     } else {
       const uint16_t* s = (const uint16_t*)x + i;
-      if (left >= 8) {
+      if (FULL || left >= 8) {
         p[0] = load_any<u32x4>(s);
       } else {
 #pragma unroll
@@ -118,12 +144,13 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(const Args a) {
   const int expert = __builtin_amdgcn_readfirstlane(e.expert);
 
   long long x_at[MFR];
-  bool there[MFR];
+  bool there[MFR], all = true;
 #pragma unroll
   for (int i = 0; i < MFR; ++i) {
     const int m = row_at + min(m0 + 16 * i + r, M - 1), row = a.index ? a.index[m] : m;
     there[i] = row >= 0 && row < a.x_rows;  // (another index stands for a row of zeros)
     x_at[i] = there[i] ? row * a.lda : 0;
+    all = all && __ballot(there[i]) == ~0ull;
   }
 
   f32x4 acc[NB][MFR][CF];
@@ -134,25 +161,24 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(const Args a) {
 #pragma unroll
       for (int j = 0; j < CF; ++j) acc[b][i][j] = f32x4{0, 0, 0, 0};
 
-  for (int kb = wave; kb < a.blocks; kb += WAVES) {
+  auto run = [&](int kb, auto full) __attribute__((always_inline)) {
     u32x4 w[NB][CF];
-    u32x2 sc[NB][CF][SCALES];
+    typedef uint32_t Scales __attribute__((ext_vector_type(2 * SCALES)));
+    Scales sc[NB][CF];
+    XPart<F32> x[4][MFR];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int j = 0; j < CF; ++j) {
         const long long row = (long long)expert * a.tiles + min(tile + j, a.tiles - 1);  // (tiles behind the last: not stored)
         w[b][j] = *(const u32x4*)(a.codes[b] + (row * a.blocks + kb) * kBlockBytes + lane * 16);
-#pragma unroll
-        for (int g = 0; g < SCALES; ++g)
-          sc[b][j][g] = *(const u32x2*)(a.scales[b] + (row * a.groups + kb * SCALES + g) * 16 + 4 * q);
+        sc[b][j] = *(const Scales*)(a.scales[b] + scale_at(row * a.blocks + kb, SCALES, 0, 4 * q));
       }
-    XPart<F32> x[4][MFR];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       const int c = kb * kBlockCols + 32 * s + 8 * q;
 #pragma unroll
-      for (int i = 0; i < MFR; ++i) x[s][i].load(a.x, x_at[i] + c, there[i] ? a.K - c : 0);
+      for (int i = 0; i < MFR; ++i) x[s][i].template load<full>(a.x, x_at[i] + c, there[i] ? a.K - c : 0);
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -163,13 +189,13 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(const Args a) {
         for (int s = 0; s < 4; ++s) {
           const u32x4 v = widen(w[b][j][s]);
           const bool first = s % (G / 32) == 0, last = (s + 1) % (G / 32) == 0;
-          const u32x2 g2 = sc[b][j][s * 32 / G];
+          const uint32_t g0 = sc[b][j][s * 32 / G * 2], g1 = sc[b][j][s * 32 / G * 2 + 1];
           f32x4 g;
           if (last) {
-            g[0] = bf16_to_f32(g2[0] & 0xffffu);
-            g[1] = __uint_as_float(g2[0] & 0xffff0000u);
-            g[2] = bf16_to_f32(g2[1] & 0xffffu);
-            g[3] = __uint_as_float(g2[1] & 0xffff0000u);
+            g[0] = bf16_to_f32(g0 & 0xffffu);
+            g[1] = __uint_as_float(g0 & 0xffff0000u);
+            g[2] = bf16_to_f32(g1 & 0xffffu);
+            g[3] = __uint_as_float(g1 & 0xffff0000u);
           }
 #pragma unroll
           for (int i = 0; i < MFR; ++i) {
@@ -181,7 +207,11 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(const Args a) {
           }
         }
       }
-  }
+  };
+  const int whole = all ? a.K / kBlockCols : 0;  // blocks that x has whole
+  int kb = wave;
+  for (; kb < whole; kb += WAVES) run(kb, std::true_type{});
+  for (; kb < a.blocks; kb += WAVES) run(kb, std::false_type{});
 
   // lane: row r of a fragment of x, columns 4 q .. 4 q + 3 of a tile
 #pragma unroll
@@ -274,7 +304,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const LayoutArgs a) {
       d |= ((uint32_t)(int)c & 15u) << (4 * i);
     }
     words[s] = d;
-    if (q == 0 && s % per == 0) a.scales[(tile * a.groups + kb * (4 / per) + s / per) * 16 + r] = (uint16_t)half;
+    if (q == 0 && s % per == 0) a.scales[scale_at(at, 4 / per, s / per, r)] = (uint16_t)half;
   }
   *(u32x4*)(a.codes + at * kBlockBytes + lane * 16) = words;
 }
@@ -303,7 +333,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const LayoutArgs a) {
     words[s] = d;
     if (q == 0 && s % per == 0) {
       const int g = kb * (4 / per) + s / per;
-      a.scales[(tile * a.groups + g) * 16 + r] = n < a.N && g < a.given ? a.scales_in[row * a.given + g] : 0;
+      a.scales[scale_at(at, 4 / per, s / per, r)] = n < a.N && g < a.given ? a.scales_in[row * a.given + g] : 0;
     }
   }
   *(u32x4*)(a.codes + at * kBlockBytes + lane * 16) = words;
@@ -327,7 +357,7 @@ __global__ __launch_bounds__(256) void unpack_kernel(const LayoutArgs a) {
   for (int s = 0; s < 4; ++s) {
     const int c = kb * kBlockCols + 32 * s + 8 * q;
     if (c >= a.K) continue;
-    const float scale = bf16_to_f32(a.scales[(tile * a.groups + c / a.group) * 16 + r]);
+    const float scale = bf16_to_f32(a.scales[scale_at(at, kBlockCols / a.group, c % kBlockCols / a.group, r)]);
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (float)((int)(words[s] << (28 - 4 * i)) >> 28) * scale;
@@ -392,11 +422,14 @@ struct Plan {
   size_t bytes;
 };
 
-// Rows that q4_kernel takes at a time, and whether it is the one.
+// Whether q4_kernel is the one: where writing the weights out costs more than turning codes into operands once for every 64 rows.  us at
+// rows / K / N, q4_kernel : tiles: bf16 256/4096/4096 26 : 36, 300/4096/4096 42 : 36; 4100 rows of 32 experts, 2048/1408 81 : 113; float32
+// 256/4096/4096 79 : 119, 4100 rows of 32 experts 259 : 472.
 bool few_fits(const ax_q4_desc_t* d) {
   const long long used = std::max<long long>(1, std::min<long long>(d->experts, d->rows));
   const long long tiles = (d->N + 15) / 16;
-  return d->rows <= 64 * used && (d->rows / 16 + used) * tiles < 1 << 21;  // (a launch counts its threads in 32 bits)
+  const bool f32 = d->dtype == AX_F32;
+  return d->rows <= (d->experts == 1 ? (f32 ? 384 : 256) : (f32 ? 256 : 192) * used) && (d->rows / 16 + used) * tiles < 1 << 21;  // (threads of a launch: 32 bits)
 }
 
 Plan make_plan(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* offsets, void* ws) {
@@ -424,6 +457,11 @@ Plan make_plan(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* 
   return p;
 }
 
+// A workgroup's columns, 16, 32 or 64 of them: as many as leave work for two thirds of the compute units, since each reads all
+// rows of x (us with 16 / 32 / 64: 64/2048/11264 26 / 23 / 18, 64/4096/4096 18 / 19 / 24, 256/4096/4096 61 / 36 / 25).  Its waves:
+// 16 where there are few workgroups and many blocks (1/4096/4096 5.0, eight waves 5.7), else eight (32 experts, 2048/1409 28, sixteen 39: two
+// blocks a wave are over before the next workgroup has started).
+constexpr long long kLeast = 170;
 template <bool F32, int NB, int G>
 void launch_rows(Args& a, hipStream_t s) {
   const long long used = std::max(1, a.e.offsets ? std::min(a.e.experts, a.e.rows) : 1), rows = a.e.rows;
@@ -433,9 +471,30 @@ void launch_rows(Args& a, hipStream_t s) {
     const long long bands = a.e.offsets ? rows / (16 * MFR) + used : (rows + 16 * MFR - 1) / (16 * MFR);
     q4_kernel<F32, NB, MFR, CF, G, WAVES><<<(int)(bands * a.wide), 64 * WAVES, 0, s>>>(a);
   };
-  if (rows <= 16 * used) go(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{});
-  else if (rows <= 32 * used) go(std::integral_constant<int, 2>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
-  else go(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
+  constexpr auto one = std::integral_constant<int, 1>{};
+  constexpr auto two = std::integral_constant<int, 2>{};
+  constexpr auto four = std::integral_constant<int, 4>{};
+  constexpr auto eight = std::integral_constant<int, 8>{};
+  constexpr auto sixteen = std::integral_constant<int, 16>{};
+  // tiles of 16 columns by bands of rows that there can be expected
+  const int height = rows <= 16 * used ? 16 : F32 || rows <= 32 * used ? 32 : 64;  // (three pieces of 64 rows leave no registers)
+  const long long work = a.tiles * used * ((rows + height * used - 1) / (height * used));
+  const bool deep = a.blocks >= 32;
+  if (height == 16) {
+    if (deep && work >= 512) go(one, two, eight);
+    else if (deep && work <= 256) go(one, one, sixteen);
+    else go(one, one, eight);
+  } else if (height == 32) {
+    if (work >= 2 * kLeast) go(two, two, eight);
+    else if (deep && !F32) go(two, one, std::integral_constant<int, F32 ? 8 : 16>{});
+    else go(two, one, eight);
+  } else if constexpr (!F32) {
+    if constexpr (NB == 1) {
+      if (work >= 4 * kLeast) return go(four, four, four);
+    }
+    if (work >= 2 * kLeast) go(four, two, eight);
+    else go(four, one, eight);
+  }
 }
 template <bool F32, int NB>
 hipError_t launch_group(Args& a, int group, hipStream_t s) {

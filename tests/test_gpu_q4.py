@@ -82,7 +82,7 @@ def _weights(g, shape, group):
 
 def _rounded(M, dtype, used=1):
     """Half a unit of a weight, where they are rounded to bf16 for the tiles."""
-    return 2.0 ** -8 * 1.01 if dtype == torch.bfloat16 and M > 64 * used else 0.0
+    return 2.0 ** -8 * 1.01 if dtype == torch.bfloat16 and M > (192 * used if used > 1 else 256) else 0.0
 
 
 def _check(y, zd, size, K, weight, act, r, dtype, what):
