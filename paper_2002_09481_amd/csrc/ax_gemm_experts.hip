@@ -1,5 +1,11 @@
 // Matrix products of rows grouped by expert: the tiles of ax_gemm_tile.h, each of which looks up whose rows it has.
 //
+// Bound: few experts with many rows as ax_gemm.hip's tiles.  Many with few: sums by the stores of the weights' gradients, rows by tiles that
+// the experts' ends leave partly empty.  Measured (us, bf16, experts / rows / inputs / outputs, sizes that differ up to 20 times): rows
+// 8/16384/2048/4096 275 (1000 TF), 32/8192/1024/1408 50; sums 8/16384/2048/4096 247 (1110 TF), 32/8192/1024/1408 47 (92 MB
+// of results; 3 workgroups a compute unit, with tiles of 256 x 256 54, two workgroups of 128 x 128 56), 32/32768/1024/1408 118 (in the order of
+// the experts, larger or not, 160: the launch ends with the tiles of a large one).
+//
 // Rows by rows (kRows): a tile never spans two experts, so one of 256 rows wastes half of itself at an expert's end on the
 // average; the tile's height goes by the rows that an expert can expect.  Sums over rows (kSums, the weights' gradients): one
 // product for each expert, with its rows for the contraction; an expert without rows writes zeros.  Nothing is cut along the
@@ -11,6 +17,12 @@
 namespace ax {
 namespace {
 
+// Configurations of their own: tiles of which three fit a compute unit.  Rows by rows: between the others where one more round of
+// two would be needed.  Sums: contractions are short, a workgroup mostly waits for its first stage and for its stores.
+constexpr TileShape kThreeRows = {64, 128, 128, 3, 2.5, 0.60, 0.93};
+constexpr TileShape kThreeSums = {128, 128, 64, 3, 3.0, 0.90, 1.40};
+constexpr int kThree = 4;
+
 template <int LA, int LB, int NB, Grouping GR>
 void launch_bf16(const Args& a, int tile, int grid, hipStream_t s) {
   constexpr int OT = AX_BF16;
@@ -18,6 +30,10 @@ void launch_bf16(const Args& a, int tile, int grid, hipStream_t s) {
     case 0: gemm_kernel<false, 1, LA, LB, NB, 256, 256, 2, 4, 128, 2, 2, OT, GR><<<grid, 512, 0, s>>>(a); break;
     case 1: gemm_kernel<false, 1, LA, LB, NB, 128, 128, 2, 2, 128, 2, 2, OT, GR><<<grid, 256, 0, s>>>(a); break;
     case 2: gemm_kernel<false, 1, LA, LB, NB, 64, 128, 1, 4, 128, 3, 2, OT, GR><<<grid, 256, 0, s>>>(a); break;
+    case kThree:
+      if constexpr (GR == kRows) gemm_kernel<false, 1, LA, LB, NB, 64, 128, 1, 4, 128, 2, 3, OT, GR><<<grid, 256, 0, s>>>(a);
+      else gemm_kernel<false, 1, LA, LB, NB, 128, 128, 2, 2, 64, 3, 3, OT, GR><<<grid, 256, 0, s>>>(a);
+      break;
     default:
       if constexpr (LA == 0) gemm_kernel<false, 1, LA, LB, NB, 32, 128, 1, 4, 128, 3, 2, OT, GR><<<grid, 256, 0, s>>>(a);
       break;
@@ -40,7 +56,10 @@ void launch_tiles(const Args& a, int tile, int grid, hipStream_t s) {
   else launch_bf16<LA, LB, NB, GR>(a, tile, grid, s);
 }
 
-const TileShape& shape_of(const GemmArgs& g, int tile) { return g.pieces == 3 ? kTiles3[tile] : kTiles[tile]; }
+const TileShape& shape_of(const GemmArgs& g, bool sums, int tile) {
+  if (g.pieces == 3) return kTiles3[tile];
+  return tile < kThree ? kTiles[tile] : sums ? kThreeSums : kThreeRows;
+}
 long long tiles_across(const GemmArgs& g, const TileShape& T) {
   const int bns = T.bn / (g.gated ? 2 : 1);
   return (long long)((g.N + bns - 1) / bns) * (g.dual ? 2 : 1);
@@ -62,8 +81,8 @@ int plan_experts(const GemmArgs& g, const Groups& e, bool sums) {
   const double kbytes = 2.0 * (sums ? rows / experts : (double)g.K);
   int best = three ? 1 : 0;
   double least = 1e300;
-  for (int t = 0; t < (three ? kNumTiles3 : kNumTiles); ++t) {
-    const TileShape& T = shape_of(g, t);
+  for (int t = 0; t < (three ? kNumTiles3 : kThree + 1); ++t) {
+    const TileShape& T = shape_of(g, sums, t);
     if (T.bm == 32 && g.la != 0) continue;
     if (three && t == 0 && (g.la != 0 || g.lb != 0 || g.gated)) continue;
     if (t > 0 && grid_of(g, e, sums, T) > kMaxGrid) continue;
@@ -72,8 +91,9 @@ int plan_experts(const GemmArgs& g, const Groups& e, bool sums) {
     const double step = three && t == 1 && g.la == 0 && g.lb == 0 ? kStep3Along : T.step;
     const double stages = ((kbytes + T.kb - 1) / T.kb) * g.nseg * T.kb / 128;
     const long long slots = (long long)kCus * T.per_cu, full = n / slots, rest = n - full * slots;
-    double cost = full * (T.fixed + stages * step);
-    if (rest) cost += T.fixed + stages * (rest <= kCus ? T.step1 : step);
+    const double fixed = T.fixed + (sums && !three ? T.per_cu * T.bm * T.bn * 2 / 28e3 : 0);  // (results leave a compute unit at 28 KB a us)
+    double cost = full * (fixed + stages * step);
+    if (rest) cost += fixed + stages * (rest <= kCus ? T.step1 : step);
     if (cost < least) {
       least = cost;
       best = t;
@@ -82,15 +102,15 @@ int plan_experts(const GemmArgs& g, const Groups& e, bool sums) {
   return best;
 }
 
-void tile_of_experts(const GemmArgs& g, int tile, int* rows, int* cols) {
-  *rows = shape_of(g, tile).bm;
-  *cols = shape_of(g, tile).bn;
+void tile_of_experts(const GemmArgs& g, bool sums, int tile, int* rows, int* cols) {
+  *rows = shape_of(g, sums, tile).bm;
+  *cols = shape_of(g, sums, tile).bn;
 }
 
 hipError_t launch_gemm_experts(const GemmArgs& g, const Groups& e, bool sums, int tile, hipStream_t s) {
   Args a{};
   a.g = g;
-  const TileShape& T = shape_of(g, tile);
+  const TileShape& T = shape_of(g, sums, tile);
   const int kstep = T.kb / 2;
   a.tiles_m = sums ? (g.M + T.bm - 1) / T.bm : 1;  // (kRows: each expert's own)
   a.tiles_n = (int)tiles_across(g, T);

@@ -289,9 +289,11 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
     a_at = row_at * g.lda;
     b_at = (long long)uniform(e.expert) * (LB == 0 ? g.N : g.K) * g.ldb;
   } else {
-    const int per = a.tiles_m * a.tiles_n, e = uniform(blockIdx.x / per);
-    tile = xcd_run(blockIdx.x - e * per, per);
-    const Span rows = span_of(a.offsets, e, a.rows);
+    // (the experts with most rows begin first: the launch does not end with them)
+    const int per = a.tiles_m * a.tiles_n, i = uniform(blockIdx.x / per);
+    Span rows;
+    const int e = uniform(by_size(a.offsets, a.experts, a.rows, i, rows));
+    tile = xcd_run(blockIdx.x - i * per, per);
     K = uniform(rows.count);
     ksteps = (K + kStepK - 1) / kStepK;
     row_at = e * M;

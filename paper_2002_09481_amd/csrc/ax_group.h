@@ -69,6 +69,35 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, int experts, i
   return found && g.tile >= 0 && g.tile < g.tiles;  // (sums that leave 32 bits: only with offsets that do not ascend)
 }
 
+// The i-th expert by size, the larger ones first, and its rows.  By powers of two, those of one power in their order; up to 64
+// experts (a lane each), more in their order.
+__device__ __forceinline__ int by_size(const int32_t* offsets, int experts, int rows, int i, Span& s) {
+  if (experts > 64) {
+    s = span_of(offsets, i, rows);
+    return i;
+  }
+  const int lane = threadIdx.x & 63;
+  Span mine{0, 0};
+  int power = -1;
+  if (lane < experts) {
+    mine = span_of(offsets, lane, rows);
+    power = 32 - __clz(mine.count);  // (no rows: 0)
+  }
+  int before = 0, e = i;
+  for (int p = 32 - __clz(rows); p >= 0; --p) {
+    const unsigned long long all = __ballot(power == p);
+    const int n = __popcll(all);
+    if (i < before + n) {
+      const int rank = __popcll(all & ((1ull << lane) - 1));
+      e = __builtin_ctzll(__ballot(power == p && rank == i - before));
+      break;
+    }
+    before += n;
+  }
+  s = Span{__builtin_amdgcn_readlane(mine.first, e), __builtin_amdgcn_readlane(mine.count, e)};
+  return e;
+}
+
 // Workgroups b, b + 8, ... share an XCD and its L2: item b of n in an order in which they take neighbouring ones.
 __device__ __forceinline__ int xcd_run(int b, int n) {
   const int x = b & 7, i = b >> 3;
