@@ -276,3 +276,41 @@ def test_non_finite_operands_show_in_their_rows_alone():
             want = torch.ones((R, 72), dtype=torch.bool)
             want[3], want[R // 2:, 30] = False, False
             assert torch.equal(ok, want)
+
+
+def test_more_elements_than_32_bits_count():
+    """Rows of x, of the products and of a sum beyond 2^31 elements."""
+    T, K, N, dtype = (1 << 20) + 70, 2112, 16, torch.bfloat16
+    x = torch.zeros((T, K), dtype=dtype, device="cuda")
+    x[-70:] = F.randn(F.gen(1), (70, K), 1.0, dtype).cuda()
+    w = F.randn(F.gen(2), (2, K, N), 0.02, dtype).cuda()
+    xd, wd = x[-70:].cpu().double(), w.cpu().double()
+    # few rows and many, found at the end of x
+    for R in (20, 70):
+        index = torch.arange(T - R, T, dtype=torch.int32).cuda()
+        o = torch.tensor([0, 5, R], dtype=torch.int32).cuda()
+        y, _ = ax.ax_matmul_experts(x, w, o, index)
+        want, size = _grouped(xd[70 - R:], w.cpu(), torch.tensor([0] * 5 + [1] * (R - 5)))
+        F.assert_within(y, want, size * F.sum_bound(K) + want.abs() * F.store(dtype))
+    # all rows: the last expert's at the end
+    o = torch.tensor([0, T - 70, T], dtype=torch.int32).cuda()
+    y, _ = ax.ax_matmul_experts(x, w, o)
+    want = xd @ wd[1]
+    F.assert_within(y[-70:], want, (xd.abs() @ wd[1].abs()) * F.sum_bound(K) + want.abs() * F.store(dtype))
+    assert not bool(y[:-70].any())
+    gy = F.randn(F.gen(3), (T, N), 1.0, dtype).cuda()
+    gx, gw = ax.ax_matmul_experts_backward(gy, x, w, o)
+    gd = gy[-70:].cpu().double()
+    want = gd @ wd[1].t()
+    F.assert_within(gx[-70:], want, (gd.abs() @ wd[1].t().abs()) * F.sum_bound(N) + want.abs() * F.store(dtype), "gx")
+    want = xd.t() @ gd
+    F.assert_within(gw[1], want, (xd.t().abs() @ gd.abs()) * F.sum_bound(70) + want.abs() * F.store(dtype), "gw")
+    assert not bool(gw[0].any())
+    rows = torch.tensor([[T - 1, 0], [T - 3, T - 1]], dtype=torch.int32).cuda()
+    assert torch.equal(ax.ax_combine(x, rows), torch.stack((x[-1], (x[-3].float() + x[-1].float()).to(dtype))))
+    two = x[-2:].clone()
+    gh, gr = ax.ax_combine_backward(two, x, rows[:, :1].contiguous())
+    assert torch.equal(gh[T - 1], two[0]) and torch.equal(gh[T - 3], two[1])
+    want = torch.stack((two[0].double() @ x[-1].double(), two[1].double() @ x[-3].double()))[:, None].cpu()
+    size = torch.stack((two[0].double().abs() @ x[-1].double().abs(), two[1].double().abs() @ x[-3].double().abs()))[:, None].cpu()
+    F.assert_within(gr, want, size * (K / 64 + 24) * 2 * F.U)
