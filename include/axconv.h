@@ -629,7 +629,7 @@ int ax_route_backward(const ax_route_desc_t* desc, const float* gweights, const 
  * [experts, N, K] (w_transposed), all rows at pitch w_ld:
  *   z = x w_e,  y_out = act(z),  z_out (may be NULL, pitch N) kept for the backward pass
  *   h_out = act(x wg_e) * (x wu_e),  g_out and u_out (both or neither NULL, pitch N) kept
- * Types, sums and roundings as in ax_matmul and ax_gated.  Indexed rows may start at any element.
+ * Types, sums and roundings as in ax_matmul and ax_gated.
  * workspace: ax_*_experts_workspace_bytes(desc) bytes, 256-byte aligned.
  */
 typedef struct {

@@ -1527,7 +1527,7 @@ def ax_matmul_experts(x, w, offsets, tokens=None, act="none", transposed=False, 
         return _on_stream(ax_matmul_experts, stream, x, w, offsets, tokens, act, transposed, save, y_out, z_out, workspace)
     L = lib()
     xp, wp = x.data_ptr(), w.data_ptr()
-    aligned = (wp | (xp if tokens is None else 0)) % 16 == 0
+    aligned = (wp | xp) % 16 == 0
     key = ("matmul_experts", act, transposed, aligned, save, _sig(x), _sig(w), _sig(offsets), _sig(tokens), _sig(y_out), _sig(z_out))
     if y_out is None:
         y_out = x.new_empty(_rows_of(x, tokens) + (_expert_columns(w, transposed),))
@@ -1565,7 +1565,7 @@ def ax_matmul_experts_backward(gy, x, w, offsets, tokens=None, z=None, act="none
         return _on_stream(ax_matmul_experts_backward, stream, gy, x, w, offsets, tokens, z, act, transposed, gx_out, gw_out, workspace)
     L = lib()
     gp, xp, wp = gy.data_ptr(), x.data_ptr(), w.data_ptr()
-    aligned = (wp | (xp if tokens is None else 0) | (gp if act == "none" else 0)) % 16 == 0
+    aligned = (wp | xp | (gp if act == "none" else 0)) % 16 == 0
     key = ("matmul_experts_backward", act, transposed, aligned, _sig(gy), _sig(x), _sig(w), _sig(offsets), _sig(tokens), _sig(z),
            _sig(gx_out), _sig(gw_out))
     hit = _checked.get(key)
@@ -1600,7 +1600,7 @@ def ax_gated_experts(x, wg, wu, offsets, tokens=None, act="silu", save=False, h_
         return _on_stream(ax_gated_experts, stream, x, wg, wu, offsets, tokens, act, save, h_out, g_out, u_out, workspace)
     L = lib()
     xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
-    aligned = (gp | up | (xp if tokens is None else 0)) % 16 == 0
+    aligned = (gp | up | xp) % 16 == 0
     key = ("gated_experts", act, aligned, save, _sig(x), _sig(wg), _sig(wu), _sig(offsets), _sig(tokens), _sig(h_out), _sig(g_out), _sig(u_out))
     if h_out is None:
         h_out = x.new_empty(_rows_of(x, tokens) + (_expert_columns(wg, False),))
@@ -1631,7 +1631,7 @@ def ax_gated_experts_backward(gh, x, wg, wu, g, u, offsets, tokens=None, act="si
         return _on_stream(ax_gated_experts_backward, stream, gh, x, wg, wu, g, u, offsets, tokens, act, gx_out, gwg_out, gwu_out, workspace)
     L = lib()
     xp, gp, up = x.data_ptr(), wg.data_ptr(), wu.data_ptr()
-    aligned = (gp | up | (xp if tokens is None else 0)) % 16 == 0
+    aligned = (gp | up | xp) % 16 == 0
     key = ("gated_experts_backward", act, aligned, _sig(gh), _sig(x), _sig(wg), _sig(wu), _sig(g), _sig(u), _sig(offsets), _sig(tokens),
            _sig(gx_out), _sig(gwg_out), _sig(gwu_out))
     hit = _checked.get(key)

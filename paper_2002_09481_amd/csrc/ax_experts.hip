@@ -65,9 +65,15 @@ hipError_t launch_gather(const PackJob& j, const int32_t* index, int x_rows, hip
 
 namespace {
 
-// x as the tiles read it: in place, or copied (job; gathered where it is indexed).
-Operand make_rows(const ax_experts_desc_t* d, const void* x, Arena& ar, PackJob* job) {
-  return make_operand(x, d->rows, d->K, d->x_ld, d->dtype, d->unaligned || d->indexed, ar, job);
+// Whether the tiles find indexed rows themselves (forward): where they could read x in place, and count its bytes in 31 bits.  us at
+// experts / rows / inputs / outputs of a gated pair, found : copied first: 8/16384/2048/8192 1107 : 1127, 32/8192/1024/1416 90 : 106,
+// 16/1024/2048/1408 40 : 46.
+bool found_in_place(const ax_experts_desc_t* d) {
+  return d->indexed && d->dtype == AX_BF16 && !d->unaligned && d->K % 8 == 0 && d->x_ld % 8 == 0 && d->x_rows * d->x_ld * 2 < 1ll << 31;
+}
+// x as the tiles read it: in place, or copied (job; gathered where it is indexed and not found).
+Operand make_rows(const ax_experts_desc_t* d, bool found, const void* x, Arena& ar, PackJob* job) {
+  return make_operand(x, found ? d->x_rows : d->rows, d->K, d->x_ld, d->dtype, d->unaligned || (d->indexed && !found), ar, job);
 }
 
 int check_experts(const ax_experts_desc_t* d, bool backward, bool gated) {
@@ -90,7 +96,7 @@ long long weight_cols(const ax_experts_desc_t* d) { return d->w_transposed ? d->
 // ---- forward -----------------------------------------------------------------------------------
 
 struct Forward {
-  bool few;
+  bool few, found;
   PackJob jobs[3];  // x, w, wu
   GemmArgs g;
   Groups e;
@@ -98,11 +104,19 @@ struct Forward {
   size_t bytes;
 };
 
-// Whether the experts have few rows each: as many as a workgroup of launch_few_experts takes at a time.
+// Whether the experts' rows are so few that launch_few_experts, which reads the weights as they lie, is worth it.  us at experts /
+// inputs / outputs (rows an expert), few : tiles.
+//   bf16, in place: while its workgroups (32 columns of an expert each) are few as well, since it reads all x in each of them
+//     64/1024/1024 (1) 17 : 14, (4) 29 : 22, (14) 44 : 26   8/2048/4096 (0.3) 8.4 : 17, (8) 30 : 28   4/4096/2048 (8) 17 : 27, (20) 26 : 27
+//   bf16, weights that the tiles copy first: 16/1001/777 gated (4) 24 : 30, (14) 38 : 33   [N, K] (8) 19 : 22, (20) 34 : 23
+//   float32, weights that the tiles take in copied pieces: 64/1024/1024 (30) 131 : 238, (60) 204 : 249   [N, K] (20) 167 : 214, (60) 360 : 260
+//     8/2048/4096 (60) 173 : 245   [N, K] (30) 152 : 253, (60) 285 : 269   32/256/512 [N, K] (20) 25 : 27, (30) 33 : 28
 bool few_fits(const ax_experts_desc_t* d) {
-  const long long used = std::min<long long>(d->experts, d->rows);
-  const long long tiles = (d->N + 15) / 16;
-  return d->rows <= 16 * used && (d->rows / 16 + used) * tiles < 1 << 21;  // (a launch counts its threads in 32 bits)
+  const long long used = std::min<long long>(d->experts, d->rows), tiles = (d->N + 31) / 32;
+  if ((d->rows / 16 + used) * 2 * tiles >= 1 << 21) return false;  // (a launch counts its threads in 32 bits)
+  if (d->dtype == AX_F32) return d->rows <= (d->w_transposed ? 28 : 48) * used;
+  const bool in_place = !d->unaligned && weight_cols(d) % 8 == 0 && d->w_ld % 8 == 0;
+  return in_place ? d->rows <= 8 * used && used * tiles <= 512 : d->rows <= 12 * used;
 }
 
 Forward make_forward(const ax_experts_desc_t* d, bool gated, const void* x, const int32_t* offsets, const void* w, const void* w2, void* ws) {
@@ -110,7 +124,7 @@ Forward make_forward(const ax_experts_desc_t* d, bool gated, const void* x, cons
   Arena ar(ws);
   GemmArgs& g = f.g;
   const long long wr = weight_rows(d), wc = weight_cols(d);
-  f.e = Groups{offsets, d->experts, (int)d->rows};
+  f.e = Groups{offsets, d->experts, (int)d->rows, nullptr, 0};
   f.few = few_fits(d);
   if (f.few) {
     const int esz = elem_bytes(d->dtype);
@@ -119,7 +133,8 @@ Forward make_forward(const ax_experts_desc_t* d, bool gated, const void* x, cons
     g.lda = d->x_ld * esz;
     g.ldb = d->w_ld * esz;
   } else {
-    const Operand a = make_rows(d, x, ar, &f.jobs[0]);
+    f.found = found_in_place(d);
+    const Operand a = make_rows(d, f.found, x, ar, &f.jobs[0]);
     const Operand b = make_operand(w, d->experts * wr, wc, d->w_ld, d->dtype, d->unaligned, ar, &f.jobs[1]);
     Operand b2{};
     if (gated) b2 = make_operand(w2, d->experts * wr, wc, d->w_ld, d->dtype, d->unaligned, ar, &f.jobs[2]);
@@ -140,7 +155,12 @@ Forward make_forward(const ax_experts_desc_t* d, bool gated, const void* x, cons
 
 int run_forward(Forward& f, const ax_experts_desc_t* d, const int32_t* index, hipStream_t s) {
   if (f.few) return launch_few_experts(f.g, d->dtype, f.e, index, (int)d->x_rows, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
-  if (d->indexed && launch_gather(f.jobs[0], index, (int)d->x_rows, s) != hipSuccess) return AX_ERR_HIP;
+  if (f.found) {
+    f.e.index = index;
+    f.e.x_rows = (int)d->x_rows;
+  } else if (d->indexed && launch_gather(f.jobs[0], index, (int)d->x_rows, s) != hipSuccess) {
+    return AX_ERR_HIP;
+  }
   const bool wanted[3] = {!d->indexed, true, f.g.gated != 0};
   PackBatch copies{};
   const int blocks = fill_pack(&copies, f.jobs, wanted, 3);
@@ -166,8 +186,8 @@ Backward make_backward(const ax_experts_desc_t* d, bool gated, const void* gy, c
   Arena ar(ws);
   const int dt = d->dtype;
   const long long wr = weight_rows(d), wc = weight_cols(d);
-  b.e = Groups{offsets, d->experts, (int)d->rows};
-  const Operand ox = make_rows(d, x, ar, &b.jobs[0]);
+  b.e = Groups{offsets, d->experts, (int)d->rows, nullptr, 0};
+  const Operand ox = make_rows(d, false, x, ar, &b.jobs[0]);
   const Operand ow = make_operand(w, d->experts * wr, wc, d->w_ld, dt, d->unaligned, ar, &b.jobs[1]);
   Operand ow2{}, oz{}, ou{};
   if (gated) ow2 = make_operand(w2, d->experts * wr, wc, d->w_ld, dt, d->unaligned, ar, &b.jobs[2]);
@@ -262,8 +282,7 @@ int backward_common(const ax_experts_desc_t* d, bool gated, const void* gy, cons
 int check_rows(const ax_experts_desc_t* d, const void* x, bool need_x, const int32_t* index, const int32_t* offsets) {
   if (!offsets || (d->indexed != 0) != (index != nullptr) || (need_x && !x && d->x_rows > 0)) return AX_ERR_NULL;
   if (!aligned_to(offsets, 4) || !aligned_to(index, 4)) return AX_ERR_ALIGN;
-  // (indexed rows are read at any alignment)
-  return operand_aligned(x, elem_bytes(d->dtype), d->unaligned || d->indexed, d->K, d->x_ld, d->dtype) ? AX_OK : AX_ERR_ALIGN;
+  return operand_aligned(x, elem_bytes(d->dtype), d->unaligned, d->K, d->x_ld, d->dtype) ? AX_OK : AX_ERR_ALIGN;
 }
 int check_weight(const ax_experts_desc_t* d, const void* w) {
   return operand_aligned(w, elem_bytes(d->dtype), d->unaligned, weight_cols(d), d->w_ld, d->dtype) ? AX_OK : AX_ERR_ALIGN;

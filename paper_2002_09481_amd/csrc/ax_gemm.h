@@ -61,9 +61,12 @@ hipError_t launch_join(const GemmArgs& g, int splits, void* part, hipStream_t s)
 // experts' first rows; the experts' right operands lie one behind the other.  sums false: rows of a times the matrix of their
 // expert, g.M = rows.  sums true: for every expert a^T b over its rows, g.K = rows, results one behind the other.  No slices,
 // bf16 operands or pieces, results of the operands' type.
+// index (rows by rows of bf16 alone; null: none): row of a for each of the rows, a has x_rows of them, in less than 2 GB.
 struct Groups {
   const int32_t* offsets;
   int experts, rows;
+  const int32_t* index;
+  int x_rows;
 };
 int plan_experts(const GemmArgs& g, const Groups& e, bool sums);  // the tile configuration
 void tile_of_experts(const GemmArgs& g, bool sums, int tile, int* rows, int* cols);

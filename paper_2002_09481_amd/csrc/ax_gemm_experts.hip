@@ -31,7 +31,7 @@ void launch_bf16(const Args& a, int tile, int grid, hipStream_t s) {
     case 1: gemm_kernel<false, 1, LA, LB, NB, 128, 128, 2, 2, 128, 2, 2, OT, GR><<<grid, 256, 0, s>>>(a); break;
     case 2: gemm_kernel<false, 1, LA, LB, NB, 64, 128, 1, 4, 128, 3, 2, OT, GR><<<grid, 256, 0, s>>>(a); break;
     case kThree:
-      if constexpr (GR == kRows) gemm_kernel<false, 1, LA, LB, NB, 64, 128, 1, 4, 128, 2, 3, OT, GR><<<grid, 256, 0, s>>>(a);
+      if constexpr (GR != kSums) gemm_kernel<false, 1, LA, LB, NB, 64, 128, 1, 4, 128, 2, 3, OT, GR><<<grid, 256, 0, s>>>(a);
       else gemm_kernel<false, 1, LA, LB, NB, 128, 128, 2, 2, 64, 3, 3, OT, GR><<<grid, 256, 0, s>>>(a);
       break;
     default:
@@ -52,6 +52,9 @@ void launch_f32(const Args& a, int tile, int grid, hipStream_t s) {
 }
 template <int LA, int LB, int NB, Grouping GR>
 void launch_tiles(const Args& a, int tile, int grid, hipStream_t s) {
+  if constexpr (GR == kRows) {
+    if (a.index) return launch_bf16<LA, LB, NB, kFound>(a, tile, grid, s);
+  }
   if (a.g.pieces == 3) launch_f32<LA, LB, NB, GR>(a, tile, grid, s);
   else launch_bf16<LA, LB, NB, GR>(a, tile, grid, s);
 }
@@ -119,6 +122,8 @@ hipError_t launch_gemm_experts(const GemmArgs& g, const Groups& e, bool sums, in
   a.offsets = e.offsets;
   a.experts = e.experts;
   a.rows = e.rows;
+  a.index = e.index;
+  a.x_rows = e.x_rows;
   const long long grid = grid_of(g, e, sums, T);
   if (grid <= 0 || grid >= 1 << 23) return hipErrorInvalidValue;
   const int n = (int)grid;

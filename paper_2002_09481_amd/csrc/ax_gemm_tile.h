@@ -30,11 +30,14 @@ struct Args {
   long long ldp;
   const int32_t* offsets;  // rows grouped by expert: [experts + 1], of their first rows (null: one expert, all rows)
   int experts, rows;
+  const int32_t* index;    // kFound: row of the left operand for each row, of x_rows
+  int x_rows;
 };
 
-// What a launch's tiles belong to: one product, or products of rows grouped by expert, each with its own right operand (kRows),
-// or the experts' weight gradients, each a sum over its own rows (kSums: the contraction is grouped).
-enum Grouping { kWhole, kRows, kSums };
+// What a launch's tiles belong to: one product, or products of rows grouped by expert, each with its own right operand (kRows;
+// kFound: its rows of the left operand are found through an index), or the experts' weight gradients, each a sum over its own rows
+// (kSums: the contraction is grouped).
+enum Grouping { kWhole, kRows, kFound, kSums };
 
 // ---- epilogue ----------------------------------------------------------------------------------
 
@@ -204,6 +207,36 @@ struct Stager {
   }
 };
 
+// The left operand's share of the copies where its rows are found through an index: like L = 0, with an offset for each piece.
+template <int R, int KB, int THREADS>
+struct RowStager {
+  static constexpr int kLoads = R * KB / 16 / THREADS, kRowChunks = KB / 16, kStep = THREADS / kRowChunks;
+  static_assert(kLoads >= 1 && kLoads * 16 * THREADS == R * KB && kStep % 16 == 0, "whole copies, one swizzle per thread");
+  uint32_t off[kLoads];
+  int chunk;
+  // rows `first` .. of the product, `left` of them this tile's
+  __device__ __forceinline__ void init(int t, long long ld, const int32_t* index, int x_rows, int first, int left) {
+    const int row = t / kRowChunks;
+    chunk = (t % kRowChunks) ^ swizzle<KB>(row);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = row + i * kStep;
+      const int k = r < left ? index[first + r] : -1;
+      off[i] = k >= 0 && k < x_rows ? (uint32_t)(k * ld + chunk * 16) : kOut;
+    }
+  }
+  struct Copy {
+    u32x4 rsrc;
+    bool in;
+  };
+  __device__ __forceinline__ Copy begin(const char* base, long long rem, int kleft) const {
+    const uint32_t n = rem > 0x7fffffffll ? 0x7fffffffu : (uint32_t)rem;
+    return Copy{u32x4{uniform((uint32_t)(uintptr_t)base), uniform((uint32_t)((uintptr_t)base >> 32) & 0xffffu), uniform(n), 0x00020000u},
+                chunk * 16 < kleft};
+  }
+  __device__ __forceinline__ void piece(Copy& c, uint32_t lds, int i) const { lds_copy(lds + i * (THREADS * 16), c.in ? off[i] : kOut, c.rsrc); }
+};
+
 // The matrix instruction's operand for 16 rows starting at r0, bytes 16 g .. of 64-byte part ks of a stage.
 template <int L, int R, int KB>
 __device__ __forceinline__ u32x4 fragment(uint32_t lds, int r0, int ks, int lane) {
@@ -256,7 +289,8 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   constexpr int kABytes = BM * KB, kBBytes = BNS * KB;
   constexpr int kBAt = P * kABytes;           // right operands: [weight][piece]
   constexpr int kStage = P * (kABytes + NB * kBBytes);
-  typedef Stager<LA, BM, KB, THREADS> SA;
+  constexpr bool kIndexed = GR == kFound;
+  typedef typename std::conditional<kIndexed, RowStager<BM, KB, THREADS>, Stager<LA, BM, KB, THREADS>>::type SA;
   typedef Stager<LB, BNS, KB, THREADS> SB;
   constexpr int kLoads = P * (SA::kLoads + NB * SB::kLoads);
   __shared__ __align__(1024) unsigned char smem[STAGES * kStage];
@@ -279,14 +313,14 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
     tile = xcd_run(blockIdx.x, a.tiles_m * a.tiles_n * a.splits);
     split = uniform(tile / (a.tiles_m * a.tiles_n));
     tile -= split * (a.tiles_m * a.tiles_n);
-  } else if constexpr (GR == kRows) {
+  } else if constexpr (GR == kRows || GR == kFound) {
     GroupTile e;
     if (!find_tile(a.offsets, a.experts, a.rows, BM, a.tiles_n, blockIdx.x, e)) return;
     tile = uniform(xcd_run(e.tile, e.tiles));
     M = uniform(e.count);
     row_at = uniform(e.first);
     tiles_m = uniform((M + BM - 1) / BM);
-    a_at = row_at * g.lda;
+    a_at = kIndexed ? 0 : row_at * g.lda;
     b_at = (long long)uniform(e.expert) * (LB == 0 ? g.N : g.K) * g.ldb;
   } else {
     // (the experts with most rows begin first: the launch does not end with them)
@@ -321,7 +355,8 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
 
   SA sa;
   SB sb;
-  sa.init(t, g.lda, M - m0);
+  if constexpr (kIndexed) sa.init(t, g.lda, a.index, a.x_rows, row_at + m0, M - m0);
+  else sa.init(t, g.lda, M - m0);
   sb.init(t, g.ldb, g.N - n0);
 
   // the next stage to copy: segment, stage within it, operand positions
@@ -329,7 +364,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   // bytes from the tile's first element to the operand's end; rows are whole 16-byte chunks, and a chunk that only began
   // in front of the end would not be loaded at all
   const long long row_bytes = ((long long)K * kElem + 15) & ~15ll;
-  const long long a_all = LA == 0 ? (long long)(M - 1 - m0) * g.lda + row_bytes
+  const long long a_all = LA == 0 ? (long long)(kIndexed ? a.x_rows - 1 : M - 1 - m0) * g.lda + row_bytes
                                   : (long long)(K - 1) * g.lda + (long long)(((M + 7) & ~7) - m0) * kElem;
   const long long b_all = LB == 0 ? (long long)(g.N - 1 - n0) * g.ldb + row_bytes
                                   : (long long)(K - 1) * g.ldb + (long long)(((g.N + 7) & ~7) - n0) * kElem;
@@ -337,7 +372,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   const char *pa, *pb, *pb2;
   long long ra, rb;
   auto at_segment = [&]() AX_INLINE {
-    const long long ao = LA == 0 ? (long long)m0 * g.lda : (long long)m0 * kElem;
+    const long long ao = LA == 0 ? (kIndexed ? 0 : (long long)m0 * g.lda) : (long long)m0 * kElem;
     const long long bo = LB == 0 ? (long long)n0 * g.ldb : (long long)n0 * kElem;
     pa = (const char*)g.seg[seg].a + a_at + ao + ks * a_step;
     pb = (const char*)(second ? g.seg[seg].b2 : g.seg[seg].b) + b_at + bo + ks * b_step;

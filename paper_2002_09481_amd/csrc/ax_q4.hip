@@ -436,7 +436,7 @@ Plan make_plan(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* 
   Plan p{};
   Arena ar(ws);
   p.few = few_fits(d);
-  p.e = Groups{offsets, d->experts, (int)d->rows};
+  p.e = Groups{offsets, d->experts, (int)d->rows, nullptr, 0};
   if (p.few) return p;
   p.x = make_operand(x, d->rows, d->K, d->x_ld, d->dtype, d->unaligned || d->indexed, ar, &p.job);
   PackJob unused;
