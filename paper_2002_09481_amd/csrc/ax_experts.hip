@@ -6,7 +6,8 @@
 //   h = act(x wg_e) (x wu_e)              gg = gh u act'(g),  gu = gh act(g),  gx = gg wg_e^T + gu wu_e^T, ...
 //
 // Two forms: few rows an expert (launch_few_experts: weights read once, straight into registers, rows found through the index)
-// and tiles (launch_gemm_experts), which read x in rows that lie one behind the other: indexed rows are copied first.
+// and tiles (launch_gemm_experts), which find rows that they can read in place through the index as well; others, and those of
+// the weights' gradients, where rows are the contraction, are copied first.
 #include <algorithm>
 
 #include "ax_float.h"
@@ -17,63 +18,20 @@
 namespace ax {
 namespace {
 
-// Rows of x in the order of the products, in the form that the tiles read: eight elements a thread.  A row whose index is
-// outside x becomes zeros.  Bound by memory.
-struct GatherArgs {
-  PackJob j;
-  const int32_t* index;
-  int x_rows;
-};
-template <bool F32>
-__global__ __launch_bounds__(256) void gather_kernel(const GatherArgs a) {
-  const PackJob& j = a.j;
-  const long long groups = j.pcols / 8, total = j.rows * groups;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-    const long long r = i / groups, c = (i - r * groups) * 8;
-    const int k = a.index[r];
-    const int left = k >= 0 && k < a.x_rows ? (int)min(8ll, j.cols - c) : 0;
-    float v[8];
-    if constexpr (F32) {
-      load_elems<true, 8>(j.src, k * j.ld + c, left, v);
-      u32x4 q[3];
-      pieces_of(v, q);
-#pragma unroll
-      for (int p = 0; p < 3; ++p) *(u32x4*)((uint16_t*)j.dst + (p * j.rows + r) * j.pitch + c) = q[p];
-    } else {
-      u32x4 q{0, 0, 0, 0};
-      const uint16_t* s = (const uint16_t*)j.src + k * j.ld + c;
-      if (left >= 8) {
-        q = load_any<u32x4>(s);
-      } else {
-        for (int e = 0; e < 4; ++e)
-          q[e] = (2 * e < left ? (uint32_t)s[2 * e] : 0u) | ((2 * e + 1 < left ? (uint32_t)s[2 * e + 1] : 0u) << 16);
-      }
-      *(u32x4*)((uint16_t*)j.dst + r * j.pitch + c) = q;
-    }
-  }
-}
-
-}  // namespace
-
-hipError_t launch_gather(const PackJob& j, const int32_t* index, int x_rows, hipStream_t s) {
-  const GatherArgs a{j, index, x_rows};
-  const int grid = grid_for(j.rows * (j.pcols / 8));
-  if (j.dtype == AX_F32) gather_kernel<true><<<grid, 256, 0, s>>>(a);
-  else gather_kernel<false><<<grid, 256, 0, s>>>(a);
-  return hipGetLastError();
-}
-
-namespace {
-
 // Whether the tiles find indexed rows themselves (forward): where they could read x in place, and count its bytes in 31 bits.  us at
 // experts / rows / inputs / outputs of a gated pair, found : copied first: 8/16384/2048/8192 1107 : 1127, 32/8192/1024/1416 90 : 106,
 // 16/1024/2048/1408 40 : 46.
 bool found_in_place(const ax_experts_desc_t* d) {
   return d->indexed && d->dtype == AX_BF16 && !d->unaligned && d->K % 8 == 0 && d->x_ld % 8 == 0 && d->x_rows * d->x_ld * 2 < 1ll << 31;
 }
-// x as the tiles read it: in place, or copied (job; gathered where it is indexed and not found).
-Operand make_rows(const ax_experts_desc_t* d, bool found, const void* x, Arena& ar, PackJob* job) {
-  return make_operand(x, found ? d->x_rows : d->rows, d->K, d->x_ld, d->dtype, d->unaligned || (d->indexed && !found), ar, job);
+// x as the tiles read it: in place, or copied, in the order of the products where it is indexed and not found.
+Operand make_rows(const ax_experts_desc_t* d, bool found, const void* x, const int32_t* index, Arena& ar, PackJob* job) {
+  const Operand o = make_operand(x, found ? d->x_rows : d->rows, d->K, d->x_ld, d->dtype, d->unaligned || (d->indexed && !found), ar, job);
+  if (!found) {
+    job->index = index;
+    job->src_rows = (int)d->x_rows;
+  }
+  return o;
 }
 
 int check_experts(const ax_experts_desc_t* d, bool backward, bool gated) {
@@ -119,7 +77,8 @@ bool few_fits(const ax_experts_desc_t* d) {
   return in_place ? d->rows <= 8 * used && used * tiles <= 512 : d->rows <= 12 * used;
 }
 
-Forward make_forward(const ax_experts_desc_t* d, bool gated, const void* x, const int32_t* offsets, const void* w, const void* w2, void* ws) {
+Forward make_forward(const ax_experts_desc_t* d, bool gated, const void* x, const int32_t* index, const int32_t* offsets, const void* w,
+                     const void* w2, void* ws) {
   Forward f{};
   Arena ar(ws);
   GemmArgs& g = f.g;
@@ -134,7 +93,7 @@ Forward make_forward(const ax_experts_desc_t* d, bool gated, const void* x, cons
     g.ldb = d->w_ld * esz;
   } else {
     f.found = found_in_place(d);
-    const Operand a = make_rows(d, f.found, x, ar, &f.jobs[0]);
+    const Operand a = make_rows(d, f.found, x, index, ar, &f.jobs[0]);
     const Operand b = make_operand(w, d->experts * wr, wc, d->w_ld, d->dtype, d->unaligned, ar, &f.jobs[1]);
     Operand b2{};
     if (gated) b2 = make_operand(w2, d->experts * wr, wc, d->w_ld, d->dtype, d->unaligned, ar, &f.jobs[2]);
@@ -158,10 +117,8 @@ int run_forward(Forward& f, const ax_experts_desc_t* d, const int32_t* index, hi
   if (f.found) {
     f.e.index = index;
     f.e.x_rows = (int)d->x_rows;
-  } else if (d->indexed && launch_gather(f.jobs[0], index, (int)d->x_rows, s) != hipSuccess) {
-    return AX_ERR_HIP;
   }
-  const bool wanted[3] = {!d->indexed, true, f.g.gated != 0};
+  const bool wanted[3] = {true, true, f.g.gated != 0};
   PackBatch copies{};
   const int blocks = fill_pack(&copies, f.jobs, wanted, 3);
   if (run_pack(copies, blocks, s) != hipSuccess) return AX_ERR_HIP;
@@ -180,14 +137,14 @@ struct Backward {
   size_t bytes;
 };
 
-Backward make_backward(const ax_experts_desc_t* d, bool gated, const void* gy, const void* x, const int32_t* offsets, const void* w,
-                       const void* w2, const void* z, const void* u, void* ws) {
+Backward make_backward(const ax_experts_desc_t* d, bool gated, const void* gy, const void* x, const int32_t* index, const int32_t* offsets,
+                       const void* w, const void* w2, const void* z, const void* u, void* ws) {
   Backward b{};
   Arena ar(ws);
   const int dt = d->dtype;
   const long long wr = weight_rows(d), wc = weight_cols(d);
   b.e = Groups{offsets, d->experts, (int)d->rows, nullptr, 0};
-  const Operand ox = make_rows(d, false, x, ar, &b.jobs[0]);
+  const Operand ox = make_rows(d, false, x, index, ar, &b.jobs[0]);
   const Operand ow = make_operand(w, d->experts * wr, wc, d->w_ld, dt, d->unaligned, ar, &b.jobs[1]);
   Operand ow2{}, oz{}, ou{};
   if (gated) ow2 = make_operand(w2, d->experts * wr, wc, d->w_ld, dt, d->unaligned, ar, &b.jobs[2]);
@@ -255,10 +212,9 @@ int backward_common(const ax_experts_desc_t* d, bool gated, const void* gy, cons
       if (p && rc == hipSuccess) rc = zero_rows(p, d->experts * weight_rows(d), weight_cols(d), d->w_ld, esz, s);
     return rc == hipSuccess ? AX_OK : AX_ERR_HIP;
   }
-  Backward b = make_backward(d, gated, gy, x, offsets, w, w2, z, u, ws);
+  Backward b = make_backward(d, gated, gy, x, index, offsets, w, w2, z, u, ws);
   if (!ws_ok(ws, ws_bytes, b.bytes)) return AX_ERR_WORKSPACE;
-  if (gw_out && d->indexed && launch_gather(b.jobs[0], index, (int)d->x_rows, s) != hipSuccess) return AX_ERR_HIP;
-  const bool wanted[3] = {gw_out && !d->indexed, gx_out != nullptr, gx_out && gated};
+  const bool wanted[3] = {gw_out != nullptr, gx_out != nullptr, gx_out && gated};
   PackBatch copies{};
   const int blocks = fill_pack(&copies, b.jobs, wanted, 3);
   if (b.elementwise) {
@@ -295,7 +251,7 @@ using namespace ax;
 
 extern "C" size_t ax_matmul_experts_workspace_bytes(const ax_experts_desc_t* d) {
   if (check_experts(d, false, false) != AX_OK || d->rows == 0) return 0;
-  return make_forward(d, false, nullptr, nullptr, nullptr, nullptr, nullptr).bytes;
+  return make_forward(d, false, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr).bytes;
 }
 
 extern "C" int ax_matmul_experts(const ax_experts_desc_t* d, const void* x, const int32_t* index, const int32_t* offsets, const void* w,
@@ -307,7 +263,7 @@ extern "C" int ax_matmul_experts(const ax_experts_desc_t* d, const void* x, cons
   if (int rc = check_weight(d, w)) return rc;
   for (const void* p : {(const void*)y_out, (const void*)z_out})
     if (!aligned_to(p, elem_bytes(d->dtype))) return AX_ERR_ALIGN;
-  Forward f = make_forward(d, false, x, offsets, w, nullptr, workspace);
+  Forward f = make_forward(d, false, x, index, offsets, w, nullptr, workspace);
   if (!ws_ok(workspace, workspace_bytes, f.bytes)) return AX_ERR_WORKSPACE;
   f.g.y = y_out;
   f.g.z = z_out;
@@ -316,7 +272,7 @@ extern "C" int ax_matmul_experts(const ax_experts_desc_t* d, const void* x, cons
 
 extern "C" size_t ax_gated_experts_workspace_bytes(const ax_experts_desc_t* d) {
   if (check_experts(d, false, true) != AX_OK || d->rows == 0) return 0;
-  return make_forward(d, true, nullptr, nullptr, nullptr, nullptr, nullptr).bytes;
+  return make_forward(d, true, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr).bytes;
 }
 
 extern "C" int ax_gated_experts(const ax_experts_desc_t* d, const void* x, const int32_t* index, const int32_t* offsets, const void* wg,
@@ -331,7 +287,7 @@ extern "C" int ax_gated_experts(const ax_experts_desc_t* d, const void* x, const
     if (int rc = check_weight(d, p)) return rc;
   for (const void* p : {(const void*)h_out, (const void*)g_out, (const void*)u_out})
     if (!aligned_to(p, elem_bytes(d->dtype))) return AX_ERR_ALIGN;
-  Forward f = make_forward(d, true, x, offsets, wg, wu, workspace);
+  Forward f = make_forward(d, true, x, index, offsets, wg, wu, workspace);
   if (!ws_ok(workspace, workspace_bytes, f.bytes)) return AX_ERR_WORKSPACE;
   f.g.y = h_out;
   f.g.z = g_out;
@@ -341,7 +297,7 @@ extern "C" int ax_gated_experts(const ax_experts_desc_t* d, const void* x, const
 
 extern "C" size_t ax_matmul_experts_backward_workspace_bytes(const ax_experts_desc_t* d) {
   if (check_experts(d, true, false) != AX_OK || d->rows == 0) return 0;
-  return make_backward(d, false, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr).bytes;
+  return make_backward(d, false, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr).bytes;
 }
 
 extern "C" int ax_matmul_experts_backward(const ax_experts_desc_t* d, const void* gy, const void* x, const int32_t* index,
@@ -364,7 +320,7 @@ extern "C" int ax_matmul_experts_backward(const ax_experts_desc_t* d, const void
 
 extern "C" size_t ax_gated_experts_backward_workspace_bytes(const ax_experts_desc_t* d) {
   if (check_experts(d, true, true) != AX_OK || d->rows == 0) return 0;
-  return make_backward(d, true, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr).bytes;
+  return make_backward(d, true, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr).bytes;
 }
 
 extern "C" int ax_gated_experts_backward(const ax_experts_desc_t* d, const void* gh, const void* x, const int32_t* index,

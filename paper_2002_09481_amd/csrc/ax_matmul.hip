@@ -28,23 +28,27 @@ __device__ __forceinline__ void pack_rows(const PackBatch& b, int block) {
   const long long groups = j.pcols / E, total = j.rows * groups;
   for (long long i = (long long)(block - b.first[k]) * 256 + threadIdx.x; i < total; i += (long long)b.blocks[k] * 256) {
     const long long r = i / groups, c = (i - r * groups) * E;
-    const long long left = j.cols - c;
+    long long left = j.cols - c, from = r;
+    if (j.index) {
+      from = j.index[r];
+      if (from < 0 || from >= j.src_rows) from = left = 0;
+    }
     if (DT == AX_F32) {
       float v[8];
-      load_elems<true, 8>(j.src, r * j.ld + c, (int)min(left, 8ll), v);
+      load_elems<true, 8>(j.src, from * j.ld + c, (int)min(left, 8ll), v);
       u32x4 q[3];
       pieces_of(v, q);
 #pragma unroll
       for (int p = 0; p < 3; ++p) *(u32x4*)((uint16_t*)j.dst + (p * j.rows + r) * j.pitch + c) = q[p];
     } else if (DT == AX_BF16) {
-      const uint16_t* s = (const uint16_t*)j.src + r * j.ld + c;
+      const uint16_t* s = (const uint16_t*)j.src + from * j.ld + c;
       u32x4 q;
       if (left >= 8) q = load_any<u32x4>(s);
       else for (int e = 0; e < 4; ++e)
         q[e] = (2 * e < left ? (uint32_t)s[2 * e] : 0u) | ((2 * e + 1 < left ? (uint32_t)s[2 * e + 1] : 0u) << 16);
       *(u32x4*)((uint16_t*)j.dst + r * j.pitch + c) = q;
     } else {
-      const uint8_t* s = (const uint8_t*)j.src + r * j.ld + c;
+      const uint8_t* s = (const uint8_t*)j.src + from * j.ld + c;
       u32x4 q;
       if (left >= 16) q = load_any<u32x4>(s);
       else for (int e = 0; e < 4; ++e) {

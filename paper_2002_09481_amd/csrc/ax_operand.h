@@ -39,6 +39,8 @@ struct PackJob {
   long long pcols;  // cols in whole chunks, zeros behind cols
   long long pitch;  // of the copy, elements
   int dtype;  // AX_F32, AX_BF16, or kI8
+  const int32_t* index;  // row of the source for each row (null: the same); one outside its src_rows stands for zeros
+  int src_rows;
 };
 constexpr int kI8 = 2;
 
@@ -67,7 +69,7 @@ inline Operand make_operand(const void* p, long long rows, long long cols, long 
   const int chunk = dtype == kI8 ? 16 : 8, esz = dtype == kI8 ? 1 : 2;
   const long long pcols = (cols + chunk - 1) / chunk * chunk;
   const long long pitch = copy_pitch(cols, esz);
-  *job = PackJob{p, nullptr, rows, cols, ld, pcols, pitch, dtype};
+  *job = PackJob{p, nullptr, rows, cols, ld, pcols, pitch, dtype, nullptr, 0};
   o.cols = pcols;
   if (dtype != AX_F32 && !unaligned && pcols == cols && ld % chunk == 0) {
     o.planes = 1;
@@ -113,8 +115,6 @@ inline int rows_per_block(int M, int N) {  // about eight workgroups per compute
   return (int)std::max(8ll, ((M + want - 1) / want + 7) / 8 * 8);
 }
 
-// A job whose row r is row index[r] of src (zeros where that is outside its x_rows).
-hipError_t launch_gather(const PackJob& j, const int32_t* index, int x_rows, hipStream_t s);
 // The elementwise part, with the copies of `copies` (copy_blocks workgroups) in the same launch.
 hipError_t launch_act_grad(const GradArgs& a, bool gated, const PackBatch& copies, int copy_blocks, int dtype, hipStream_t s);
 // rows x cols elements of esz bytes at pitch ld set to zero.

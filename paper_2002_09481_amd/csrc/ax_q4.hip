@@ -536,14 +536,12 @@ int run(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* index, 
                               : (gated ? launch_group<false, 2>(a, d->group, s) : launch_group<false, 1>(a, d->group, s));
     return rc == hipSuccess ? AX_OK : AX_ERR_HIP;
   }
-  if (d->indexed) {
-    if (launch_gather(p.job, index, (int)d->x_rows, s) != hipSuccess) return AX_ERR_HIP;
-  } else {
-    const bool wanted[1] = {true};
-    PackBatch copies{};
-    const int blocks = fill_pack(&copies, &p.job, wanted, 1);
-    if (run_pack(copies, blocks, s) != hipSuccess) return AX_ERR_HIP;
-  }
+  p.job.index = index;
+  p.job.src_rows = (int)d->x_rows;
+  const bool wanted[1] = {true};
+  PackBatch copies{};
+  const int blocks = fill_pack(&copies, &p.job, wanted, 1);
+  if (run_pack(copies, blocks, s) != hipSuccess) return AX_ERR_HIP;
   for (int b = 0; b < (gated ? 2 : 1); ++b) {
     LayoutArgs l = layout_args(d->experts, d->N, d->K, d->group);
     l.codes = (uint8_t*)codes[b];
