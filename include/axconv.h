@@ -718,9 +718,9 @@ int ax_q4_values(const uint8_t* codes, const void* scales, int64_t experts, int6
 /*
  * Products with such weights: y_out = act(x w^T + bias) + residual, h_out = act(x wg^T) * (x wu^T).  bias [N], residual and y_out
  * [rows, N] (both may be NULL; y_out may be residual itself) have x's type.  With several experts the rows are grouped as above (index
- * and offsets; offsets may be NULL for one expert, whose rows are then all).  Up to 64 rows an expert on the average
- * the weights are exact: products with the codes are exact and summed in float32, each group's sum times its scale in float32.
- * More rows of bf16: every weight is rounded to bf16 for the matrix instructions; float32: exact, as in ax_matmul.
+ * and offsets; offsets may be NULL for one expert, whose rows are then all).  The weights are exact: products with the
+ * codes are exact and summed in float32, each group's sum times its scale in float32 (some sums of bf16 rows run over codes with 24 added, taken
+ * off again in float32).  Only for more than 600 bf16 rows an expert on the average, every weight is rounded to bf16 for the matrix instructions.
  * workspace: ax_*_q4_workspace_bytes(desc) bytes, 256-byte aligned.
  */
 typedef struct {

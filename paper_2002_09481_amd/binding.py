@@ -1826,7 +1826,7 @@ def ax_matmul_q4(x, w, bias=None, residual=None, act="none", offsets=None, token
         return _on_stream(ax_matmul_q4, stream, x, w, bias, residual, act, offsets, tokens, y_out, workspace)
     L = lib()
     xp = x.data_ptr()
-    aligned = tokens is not None or xp % 16 == 0
+    aligned = xp % 16 == 0
     key = ("matmul_q4", act, aligned, _sig(x), _q4_sig(w), _sig(bias), _sig(residual), _sig(offsets), _sig(tokens), _sig(y_out))
     hit = _checked.get(key)
     if hit is None:
@@ -1855,7 +1855,7 @@ def ax_gated_q4(x, wg, wu, act="silu", offsets=None, tokens=None, h_out=None, wo
         return _on_stream(ax_gated_q4, stream, x, wg, wu, act, offsets, tokens, h_out, workspace)
     L = lib()
     xp = x.data_ptr()
-    aligned = tokens is not None or xp % 16 == 0
+    aligned = xp % 16 == 0
     key = ("gated_q4", act, aligned, _sig(x), _q4_sig(wg), _q4_sig(wu), _sig(offsets), _sig(tokens), _sig(h_out))
     hit = _checked.get(key)
     if hit is None:

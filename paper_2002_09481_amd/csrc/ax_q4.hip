@@ -1,10 +1,10 @@
 // Products with weights of 4 bits and a scale for every group of a row:
 //
-//   w[n, k] = scale[n, k / group] c[n, k],  c in -8 .. 7 (two's complement), scale bf16, group 32, 64 or 128
+//   w[n, k] = scale[n, k / group] c[n, k],  c in -8 .. 7, scale bf16, group 32, 64 or 128
 //   y = act(x w^T + bias) + residual        h = act(x wg^T) (x wu^T)
 //
 // Layout.  A block holds 16 rows and 128 columns of the weights in 1 KB, as the matrix instruction wants them: lane (r, q) of a wave
-// has 16 bytes, word s of which holds columns 32 s + 8 q .. + 7 of row r, the first in the low bits.  Blocks of a row of
+// has 16 bytes, word s of which holds columns 32 s + 8 q .. + 7 of row r (in the order of q4_shift).  Blocks of a row of
 // blocks follow one another, then those of the next 16 rows, then those of the next expert.  Scales in the same order of blocks:
 // [4 quads of rows][groups of the block][4 rows], a quad's side by side for the lanes that hold its sums.  What lies behind the last
 // row or column has codes and scales of zero.
@@ -18,16 +18,17 @@
 // 32 experts, 2048/1409, 32 28 (20.3).  What is left: a workgroup's way from its launch to its first block, and the meeting at its end; from 64
 // rows on the conversion of codes, 20 instructions for eight.
 //
-// Many rows.  The weights are written out once, in the workspace, and multiplied by tiles (ax_gemm_experts.hip): bf16 rounds each
-// weight, scale times code, to nearest (2^-9 of it at most; codes and scales have eleven significant bits together), an
-// error of 1.1e-3 of a result's root mean square, where the rounding of the result alone gives 1.7e-3.  With float32 x the weights
-// are exact (three pieces).
+// More rows: ax_q4_tile.hip, with the weights exact as well.  Very many rows of bf16: the weights are written out once, in the
+// workspace, and multiplied by the tiles of ax_gemm_experts.hip, which lose nothing to scales and codes: every weight, scale
+// times code, is rounded to bf16 (2^-9 of it at most; codes and scales have eleven significant bits together), an error of 1.1e-3 of a result's
+// root mean square, where the rounding of the result alone gives 1.7e-3.
 #include <algorithm>
 #include <type_traits>
 
 #include "ax_float.h"
 #include "ax_group.h"
 #include "ax_operand.h"
+#include "ax_q4.h"
 
 namespace ax {
 namespace {
@@ -52,22 +53,9 @@ inline Shape shape_of(long long N, long long K, int group) {
 // Scale of row r of a tile of rows for group g of block `at` (tile * blocks + block), per groups a block.
 __device__ __forceinline__ long long scale_at(long long at, int per, int g, int r) { return (at * per * 4 + (r >> 2) * per + g) * 4 + (r & 3); }
 
-// Eight codes of a word as bf16.  (The conversion takes a code for sixteenths: what comes out is c / 16.)
-__device__ __forceinline__ u32x4 widen(uint32_t d) {
-  u32x4 v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(d >> (8 * i))));
-    const uint32_t hi = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(d >> (8 * i + 4))));
-    v[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);  // (the upper halves: four significant bits)
-  }
-  return v;
-}
-
 struct Args {
   const void* x;
-  const uint8_t* codes[2];
-  const uint16_t* scales[2];
+  Q4Weights w;
   const void* bias;
   const void* res;
   void* y;
@@ -75,8 +63,7 @@ struct Args {
   Groups e;
   long long lda, ldr, ldy;  // elements
   int N, K, x_rows, act;
-  int tiles, blocks, groups;  // of an expert's weights
-  int wide;                   // workgroups along the columns
+  int wide;  // workgroups along the columns
 };
 
 // Eight float32 values in three pieces of bf16, cut instead of rounded: all products of the pieces with a code are taken, so their sum is
@@ -170,9 +157,9 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(const Args a) {
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int j = 0; j < CF; ++j) {
-        const long long row = (long long)expert * a.tiles + min(tile + j, a.tiles - 1);  // (tiles behind the last: not stored)
-        w[b][j] = *(const u32x4*)(a.codes[b] + (row * a.blocks + kb) * kBlockBytes + lane * 16);
-        sc[b][j] = *(const Scales*)(a.scales[b] + scale_at(row * a.blocks + kb, SCALES, 0, 4 * q));
+        const long long row = (long long)expert * a.w.tiles + min(tile + j, a.w.tiles - 1);  // (tiles behind the last: not stored)
+        w[b][j] = *(const u32x4*)(a.w.codes[b] + (row * a.w.blocks + kb) * kBlockBytes + lane * 16);
+        sc[b][j] = *(const Scales*)(a.w.scales[b] + scale_at(row * a.w.blocks + kb, SCALES, 0, 4 * q));
       }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -211,7 +198,7 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(const Args a) {
   const int whole = all ? a.K / kBlockCols : 0;  // blocks that x has whole
   int kb = wave;
   for (; kb < whole; kb += WAVES) run(kb, std::true_type{});
-  for (; kb < a.blocks; kb += WAVES) run(kb, std::false_type{});
+  for (; kb < a.w.blocks; kb += WAVES) run(kb, std::false_type{});
 
   // lane: row r of a fragment of x, columns 4 q .. 4 q + 3 of a tile
 #pragma unroll
@@ -251,10 +238,10 @@ struct LayoutArgs {
   const uint16_t* scales_in;  // pack: [experts N, groups given]
   uint8_t* codes;
   uint16_t* scales;
-  void* out;              // values (float32), or operands of the products
-  long long ld, pitch, plane_rows;
+  void* out;              // values, or operands of the products at `pitch`
+  long long ld, pitch;
   long long tiles_all;    // of all experts
-  int N, K, group, tiles, blocks, groups, given;
+  int N, K, group, tiles, blocks, given;
 };
 
 // A wave a block: lane (r, q) of it has columns 32 s + 8 q .. + 7 of row r.  The largest of a group is that of 4 lanes of the
@@ -301,7 +288,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const LayoutArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float c = sound ? fminf(7.f, fmaxf(-8.f, rintf(v[s][i] / scale))) : 0.f;
-      d |= ((uint32_t)(int)c & 15u) << (4 * i);
+      d |= (uint32_t)((int)c + 8) << q4_shift(i);
     }
     words[s] = d;
     if (q == 0 && s % per == 0) a.scales[scale_at(at, 4 / per, s / per, r)] = (uint16_t)half;
@@ -328,7 +315,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const LayoutArgs a) {
     for (int i = 0; i < 8; ++i) {
       int v = n < a.N && c + i < a.K ? a.codes_in[row * a.K + c + i] : 0;
       v = min(7, max(-8, v));
-      d |= ((uint32_t)v & 15u) << (4 * i);
+      d |= (uint32_t)(v + 8) << q4_shift(i);
     }
     words[s] = d;
     if (q == 0 && s % per == 0) {
@@ -339,9 +326,8 @@ __global__ __launch_bounds__(256) void pack_kernel(const LayoutArgs a) {
   *(u32x4*)(a.codes + at * kBlockBytes + lane * 16) = words;
 }
 
-// The weights written out: float32 [rows, K] (VALUES), or rows as the tiles read them, bf16 or three pieces.  Bound by memory.
-enum Written { kValues, kHalf, kPieces };
-template <Written W>
+// The weights, float32 [rows, K] (VALUES), or bf16 as the tiles read them.  Bound by memory.
+template <bool VALUES>
 __global__ __launch_bounds__(256) void unpack_kernel(const LayoutArgs a) {
   const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (at >= a.tiles_all * a.blocks) return;
@@ -360,18 +346,12 @@ __global__ __launch_bounds__(256) void unpack_kernel(const LayoutArgs a) {
     const float scale = bf16_to_f32(a.scales[scale_at(at, kBlockCols / a.group, c % kBlockCols / a.group, r)]);
     float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)((int)(words[s] << (28 - 4 * i)) >> 28) * scale;
-    if constexpr (W == kValues) {
-      store_elems<true, 8>(a.out, row * a.pitch + c, a.K - c, v);
-    } else if constexpr (W == kHalf) {
-      // (rounded to bf16 for the matrix instruction; whole chunks: the codes behind the last column are zero)
+    for (int i = 0; i < 8; ++i) v[i] = (float)((int)(words[s] >> q4_shift(i) & 15u) - 8) * scale;
+    if constexpr (VALUES) {
+      store_elems<true, 8>(a.out, row * a.K + c, a.K - c, v);
+    } else {  // (rounded for the matrix instruction; whole chunks: the codes behind the last column are zero)
       *(u32x4*)((uint16_t*)a.out + row * a.pitch + c) =
           u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-    } else {
-      u32x4 p[3];
-      pieces_of(v, p);
-#pragma unroll
-      for (int k = 0; k < 3; ++k) *(u32x4*)((uint16_t*)a.out + (k * a.plane_rows + row) * a.pitch + c) = p[k];
     }
   }
 }
@@ -385,7 +365,6 @@ LayoutArgs layout_args(long long experts, long long N, long long K, int group) {
   a.group = group;
   a.tiles = (int)s.tiles;
   a.blocks = (int)s.blocks;
-  a.groups = s.groups;
   a.given = (int)((K + group - 1) / group);
   return a;
 }
@@ -411,48 +390,57 @@ int check_q4(const ax_q4_desc_t* d, bool gated, bool residual) {
   return AX_OK;
 }
 
+enum Way { kFew, kTiles, kWritten };
 struct Plan {
-  bool few;
-  // many rows
-  Operand x, w[2];
-  PackJob job;
+  Way way;
+  bool found;   // more rows: through the index, in place
+  PackJob job;  // or copied
+  Operand w[2];  // kWritten
+  int tile;
   GemmArgs g;
   Groups e;
-  int tile;
   size_t bytes;
 };
 
-// Whether q4_kernel is the one: where writing the weights out costs more than turning codes into operands once for every 64 rows.  us at
-// rows / K / N, q4_kernel : tiles: bf16 256/4096/4096 26 : 36, 300/4096/4096 42 : 36; 4100 rows of 32 experts, 2048/1408 81 : 113; float32
-// 256/4096/4096 79 : 119, 4100 rows of 32 experts 259 : 472.
-bool few_fits(const ax_q4_desc_t* d) {
-  const long long used = std::max<long long>(1, std::min<long long>(d->experts, d->rows));
-  const long long tiles = (d->N + 15) / 16;
-  const bool f32 = d->dtype == AX_F32;
-  return d->rows <= (d->experts == 1 ? (f32 ? 384 : 256) : (f32 ? 256 : 192) * used) && (d->rows / 16 + used) * tiles < 1 << 21;  // (threads of a launch: 32 bits)
+// us at rows / K / N, q4_kernel : q4_tile_kernel : written out.  A few units of 64 rows by 16 columns, or few rows of an expert: the first, which
+// needs none of the others' stages.
+//   256/4096/4096 25 : 42 : 36      300/4096/4096 41 : 42 : 45   700/1000/777 12 : 13     gated 256/4096/4096 43 : 43
+//   8 experts, 2048/1408: 512 rows 20 : 23, 2048 rows 45 : 32    32 experts, 2048 rows 50 : 34   float32 256/4096/4096 79 : 75, 300/4096/4096 97 : 75
+// Many rows of an expert: the weights pay for being written once.
+//   512/4096/4096 43 : 43 : 46      1027/4096/4096 88 : 77 : 65  2048/4096/4096 151 : 87 : 78  8192/4096/4096 626 : 330 : 230
+//   32 experts, 2048/1408: 4096 rows 76 : 47 : 113
+// float32 is never written out, in pieces: 2048/4096/4096 228, the six products of pieces alone would be 340.
+Way way_of(const ax_q4_desc_t* d, bool gated) {
+  const long long used = std::max<long long>(1, std::min<long long>(d->experts, d->rows)), tiles = (d->N + 15) / 16;
+  const long long units = used * ((d->rows + 64 * used - 1) / (64 * used)) * tiles * (gated ? 2 : 1);
+  if ((d->rows <= 32 * used || units <= 1024) && (d->rows / 16 + used) * tiles < 1 << 21) return kFew;  // (a launch counts its threads in 32 bits)
+  if (d->dtype == AX_BF16 && d->rows > 600 * used) return kWritten;
+  return kTiles;
 }
 
 Plan make_plan(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* offsets, void* ws) {
   Plan p{};
   Arena ar(ws);
-  p.few = few_fits(d);
+  p.way = way_of(d, gated);
   p.e = Groups{offsets, d->experts, (int)d->rows, nullptr, 0};
-  if (p.few) return p;
-  p.x = make_operand(x, d->rows, d->K, d->x_ld, d->dtype, d->unaligned || d->indexed, ar, &p.job);
-  PackJob unused;
-  const long long n = (long long)d->experts * d->N;
-  for (int b = 0; b < (gated ? 2 : 1); ++b) p.w[b] = make_operand(nullptr, n, d->K, d->K, d->dtype, true, ar, &unused);
+  if (p.way == kFew) return p;
+  p.found = d->indexed && d->dtype == AX_BF16 && !d->unaligned && d->K % 8 == 0 && d->x_ld % 8 == 0 && d->x_rows * d->x_ld * 2 < 1ll << 31;
+  const Operand a = make_operand(x, p.found ? d->x_rows : d->rows, d->K, d->x_ld, d->dtype, d->unaligned || (d->indexed && !p.found), ar, &p.job);
   GemmArgs& g = p.g;
-  add_segment(&g, p.x, p.w[0], gated ? &p.w[1] : nullptr);
+  if (p.way == kWritten) {
+    PackJob unused;
+    for (int b = 0; b < (gated ? 2 : 1); ++b) p.w[b] = make_operand(nullptr, d->experts * d->N, d->K, d->K, AX_BF16, true, ar, &unused);
+  }
+  add_segment(&g, a, p.w[0], gated ? &p.w[1] : nullptr);
   g.M = (int)d->rows;
   g.N = (int)d->N;
-  g.K = (int)p.x.cols;
+  g.K = (int)a.cols;
   g.gated = gated;
   g.odt = d->dtype;
   g.act = d->act;
   g.ldy = d->y_ld;
   g.ldr = d->residual_ld;
-  p.tile = plan_experts(g, p.e, false);
+  if (p.way == kWritten) p.tile = plan_experts(g, p.e, false);
   p.bytes = ar.used;
   return p;
 }
@@ -467,7 +455,7 @@ void launch_rows(Args& a, hipStream_t s) {
   const long long used = std::max(1, a.e.offsets ? std::min(a.e.experts, a.e.rows) : 1), rows = a.e.rows;
   auto go = [&](auto mfr, auto cf, auto waves) {
     constexpr int MFR = decltype(mfr)::value, CF = decltype(cf)::value, WAVES = decltype(waves)::value;
-    a.wide = (a.tiles + CF - 1) / CF;
+    a.wide = (a.w.tiles + CF - 1) / CF;
     const long long bands = a.e.offsets ? rows / (16 * MFR) + used : (rows + 16 * MFR - 1) / (16 * MFR);
     q4_kernel<F32, NB, MFR, CF, G, WAVES><<<(int)(bands * a.wide), 64 * WAVES, 0, s>>>(a);
   };
@@ -478,8 +466,8 @@ void launch_rows(Args& a, hipStream_t s) {
   constexpr auto sixteen = std::integral_constant<int, 16>{};
   // tiles of 16 columns by bands of rows that there can be expected
   const int height = rows <= 16 * used ? 16 : F32 || rows <= 32 * used ? 32 : 64;  // (three pieces of 64 rows leave no registers)
-  const long long work = a.tiles * used * ((rows + height * used - 1) / (height * used));
-  const bool deep = a.blocks >= 32;
+  const long long work = a.w.tiles * used * ((rows + height * used - 1) / (height * used));
+  const bool deep = a.w.blocks >= 32;
   if (height == 16) {
     if (deep && work >= 512) go(one, two, eight);
     else if (deep && work <= 256) go(one, one, sixteen);
@@ -509,14 +497,19 @@ int run(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* index, 
   Plan p = make_plan(d, gated, x, offsets, ws);
   if (!ws_ok(ws, ws_bytes, p.bytes)) return AX_ERR_WORKSPACE;
   const bool f32 = d->dtype == AX_F32;
-  if (p.few) {
-    const Shape sh = shape_of(d->N, d->K, d->group);
+  const Shape sh = shape_of(d->N, d->K, d->group);
+  Q4Weights w{};
+  for (int b = 0; b < 2; ++b) {
+    w.codes[b] = codes[b];
+    w.scales[b] = (const uint16_t*)scales[b];
+  }
+  w.tiles = (int)sh.tiles;
+  w.blocks = (int)sh.blocks;
+  w.group = d->group;
+  if (p.way == kFew) {
     Args a{};
     a.x = x;
-    for (int b = 0; b < 2; ++b) {
-      a.codes[b] = codes[b];
-      a.scales[b] = (const uint16_t*)scales[b];
-    }
+    a.w = w;
     a.bias = bias;
     a.res = residual;
     a.y = y;
@@ -529,33 +522,34 @@ int run(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* index, 
     a.K = (int)d->K;
     a.x_rows = (int)d->x_rows;
     a.act = d->act;
-    a.tiles = (int)sh.tiles;
-    a.blocks = (int)sh.blocks;
-    a.groups = sh.groups;
     const hipError_t rc = f32 ? (gated ? launch_group<true, 2>(a, d->group, s) : launch_group<true, 1>(a, d->group, s))
                               : (gated ? launch_group<false, 2>(a, d->group, s) : launch_group<false, 1>(a, d->group, s));
     return rc == hipSuccess ? AX_OK : AX_ERR_HIP;
   }
-  p.job.index = index;
-  p.job.src_rows = (int)d->x_rows;
+  if (p.found) {
+    p.e.index = index;
+    p.e.x_rows = (int)d->x_rows;
+  } else {
+    p.job.index = index;
+    p.job.src_rows = (int)d->x_rows;
+  }
   const bool wanted[1] = {true};
   PackBatch copies{};
   const int blocks = fill_pack(&copies, &p.job, wanted, 1);
   if (run_pack(copies, blocks, s) != hipSuccess) return AX_ERR_HIP;
+  p.g.y = y;
+  p.g.bias = bias;
+  p.g.res = residual;
+  if (p.way == kTiles) return launch_q4_tiles(p.g, p.e, w, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
   for (int b = 0; b < (gated ? 2 : 1); ++b) {
     LayoutArgs l = layout_args(d->experts, d->N, d->K, d->group);
     l.codes = (uint8_t*)codes[b];
     l.scales = (uint16_t*)scales[b];
     l.out = (void*)p.w[b].p;
     l.pitch = p.w[b].ld / 2;
-    l.plane_rows = (long long)d->experts * d->N;
-    if (f32) unpack_kernel<kPieces><<<grid_of(l), 256, 0, s>>>(l);
-    else unpack_kernel<kHalf><<<grid_of(l), 256, 0, s>>>(l);
+    unpack_kernel<false><<<grid_of(l), 256, 0, s>>>(l);
     if (hipGetLastError() != hipSuccess) return AX_ERR_HIP;
   }
-  p.g.y = y;
-  p.g.bias = bias;
-  p.g.res = residual;
   return launch_gemm_experts(p.g, p.e, false, p.tile, s) == hipSuccess ? AX_OK : AX_ERR_HIP;
 }
 
@@ -563,7 +557,7 @@ int run(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* index, 
 int check_rows(const ax_q4_desc_t* d, const void* x, const int32_t* index, const int32_t* offsets) {
   if ((d->indexed != 0) != (index != nullptr) || (!x && d->x_rows > 0) || (!offsets && d->experts > 1)) return AX_ERR_NULL;
   if (!aligned_to(offsets, 4) || !aligned_to(index, 4)) return AX_ERR_ALIGN;
-  return operand_aligned(x, elem_bytes(d->dtype), d->unaligned || d->indexed, d->K, d->x_ld, d->dtype) ? AX_OK : AX_ERR_ALIGN;
+  return operand_aligned(x, elem_bytes(d->dtype), d->unaligned, d->K, d->x_ld, d->dtype) ? AX_OK : AX_ERR_ALIGN;
 }
 
 }  // namespace
@@ -623,8 +617,7 @@ extern "C" int ax_q4_values(const uint8_t* codes, const void* scales, int64_t ex
   a.codes = (uint8_t*)codes;
   a.scales = (uint16_t*)scales;
   a.out = values_out;
-  a.pitch = K;
-  unpack_kernel<kValues><<<grid_of(a), 256, 0, (hipStream_t)hip_stream>>>(a);
+  unpack_kernel<true><<<grid_of(a), 256, 0, (hipStream_t)hip_stream>>>(a);
   return hipGetLastError() == hipSuccess ? AX_OK : AX_ERR_HIP;
 }
 

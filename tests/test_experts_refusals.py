@@ -179,9 +179,12 @@ def test_4_bit_product_pointers():
     go = lambda *a: L.ax_matmul_q4(R(d), *a, P, BIG, None)  # noqa: E731
     null_each(go, 8, skip=(5, 6))
     odd_each(go, 8)
-    need = L.ax_matmul_q4_workspace_bytes(R(d))
-    assert need > 4 * 64 * 32 * 2 and L.ax_matmul_q4(R(d), *[P] * 8, P, need - 1, None) == -5
-    assert L.ax_matmul_q4_workspace_bytes(R(q4(rows=8))) == 0
+    copied = q4(unaligned=1, rows=2000, N=4096, y_ld=4096, residual_ld=4096)
+    need = L.ax_matmul_q4_workspace_bytes(R(copied))
+    assert need >= 2000 * 64 and L.ax_matmul_q4(R(copied), *[P] * 8, P, need - 1, None) == -5
+    copied.unaligned = 0  # (rows found through the index, in place)
+    assert L.ax_matmul_q4_workspace_bytes(R(copied)) == 0 and L.ax_matmul_q4_workspace_bytes(R(q4(rows=8, unaligned=1))) == 0
+    assert L.ax_matmul_q4_workspace_bytes(R(q4(N=4096, y_ld=4096, residual_ld=4096))) >= 4 * 4096 * 64  # weights written out
     assert L.ax_matmul_q4(R(q4(residual_ld=3)), *[P] * 9, BIG, None) == -2
     gated = lambda *a: L.ax_gated_q4(R(d), *a, P, BIG, None)  # noqa: E731
     null_each(gated, 8)

@@ -75,18 +75,31 @@ def test_groups_that_are_not_finite():
 
 
 def _weights(g, shape, group):
+    """(weights, their values, an absolute bound of what is summed in their place where bf16 rows meet codes with 24 added: those are 31 at
+    most, and 24 is taken off again)."""
     codes = torch.randint(-8, 8, shape, generator=g, dtype=torch.int8)
     scales = ((torch.rand(shape[:-1] + (-(-shape[-1] // group),), generator=g) + 0.1) * shape[-1] ** -0.5 / 4).to(torch.bfloat16)
-    return ax.ax_pack_q4(codes.cuda(), scales.cuda(), group=group), values(codes, scales, group)
+    return ax.ax_pack_q4(codes.cuda(), scales.cuda(), group=group), values(codes, scales, group), values(torch.ones_like(codes), scales, group) * 55
 
 
-def _rounded(M, dtype, used=1):
-    """Half a unit of a weight, where they are rounded to bf16 for the tiles."""
-    return 2.0 ** -8 * 1.01 if dtype == torch.bfloat16 and M > (192 * used if used > 1 else 256) else 0.0
+def _way(rows, N, used=1, gated=False, dtype=torch.bfloat16):
+    """Which kernel a call takes: few rows, tiles, or weights written out."""
+    units = used * -(-rows // (64 * used)) * -(-N // 16) * (2 if gated else 1)
+    if rows <= 32 * used or units <= 1024:
+        return "few"
+    return "written" if dtype == torch.bfloat16 and rows > 600 * used else "tiles"
 
 
-def _check(y, zd, size, K, weight, act, r, dtype, what):
-    zb = size * (F.sum_bound(K, dtype == torch.float32) + weight)
+def _sums(xd, w, most, K, way, dtype):
+    """Bound of a product's sum: of its terms, or of what is summed in their place; half a unit of every weight where they are rounded."""
+    a = xd.abs()
+    size = a @ w.abs().t()
+    if way == "tiles" and dtype == torch.bfloat16:
+        return (a @ most.t()) * F.sum_bound(K)
+    return size * (F.sum_bound(K, dtype == torch.float32) + (2.0 ** -8 * 1.01 if way == "written" else 0))
+
+
+def _check(y, zd, zb, act, r, dtype, what):
     yd = F.act(zd, act)
     bound = zb * F.ACT_LIP + yd.abs() * F.ACT_REL + F.U * zd.abs()
     if r is not None:
@@ -97,42 +110,50 @@ def _check(y, zd, size, K, weight, act, r, dtype, what):
 
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("M,K,N", [(1, 1, 1), (1, 4096, 130), (2, 128, 16), (3, 31, 17), (15, 200, 33), (16, 1000, 48), (17, 129, 64), (31, 2049, 5),
-                                   (33, 256, 100), (64, 640, 31), (65, 130, 129), (130, 333, 72), (300, 1024, 264), (700, 96, 40)])
-def test_matmul(M, K, N, dt, group):
+@pytest.mark.parametrize("M,K,N,way", [(1, 1, 1, "few"), (1, 4096, 130, "few"), (2, 128, 16, "few"), (3, 31, 17, "few"), (15, 200, 33, "few"),
+                                       (16, 1000, 48, "few"), (17, 129, 64, "few"), (31, 2049, 5, "few"), (33, 256, 100, "few"), (64, 640, 31, "few"),
+                                       (65, 130, 129, "few"), (130, 333, 72, "few"), (300, 1024, 264, "few"), (700, 96, 40, "few"), (8, 64, 9000, "few"),
+                                       (70, 65, 8300, "tiles"), (33, 1, 16400, "tiles"), (129, 130, 6000, "tiles"), (300, 520, 3601, "tiles"),
+                                       (600, 63, 1700, "tiles"), (601, 31, 1650, None), (650, 264, 1601, None)])
+def test_matmul(M, K, N, way, dt, group):
     dtype, g = F.DT[dt], F.gen(M + K + N + group)
+    assert way in (None, _way(M, N, dtype=dtype))
+    way = _way(M, N, dtype=dtype)
     x, b, r = F.randn(g, (M, K), 1.0, dtype), F.randn(g, (N,), 1.0, dtype), F.randn(g, (M, N), 1.0, dtype)
-    q, w = _weights(g, (N, K), group)
-    zd, size = x.double() @ w.t(), x.double().abs() @ w.abs().t()
+    q, w, most = _weights(g, (N, K), group)
+    xd = x.double()
+    zd, zb = xd @ w.t(), _sums(xd, w, most, K, way, dtype)
     y = ax.ax_matmul_q4(x.cuda(), q)
-    _check(y, zd, size, K, _rounded(M, dtype), "none", None, dtype, "plain")
-    zd, size = zd + b.double(), size + F.U * (zd.abs() + b.double().abs()) / F.sum_bound(K)
+    _check(y, zd, zb, "none", None, dtype, "plain")
+    zd = zd + b.double()
+    zb = zb + F.U * (zd.abs() + b.double().abs())
     for i, act in enumerate(ACTS):
         y = ax.ax_matmul_q4(x.cuda(), q, bias=b.cuda(), residual=r.cuda() if i % 2 else None, act=act)
-        _check(y, zd, size, K, _rounded(M, dtype), act, r.double() if i % 2 else None, dtype, act)
+        _check(y, zd, zb, act, r.double() if i % 2 else None, dtype, act)
 
 
 @pytest.mark.parametrize("act", ACTS)
-@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("M,K,N", [(1, 64, 33), (16, 1000, 48), (20, 300, 17), (50, 256, 80), (100, 200, 130)])
+@pytest.mark.parametrize("M,K,N", [(1, 64, 33), (16, 1000, 48), (20, 300, 17), (50, 256, 80), (100, 200, 130), (300, 200, 1901), (40, 129, 8200), (700, 96, 903)])
 def test_gated(M, K, N, dt, group, act):
     dtype, g = F.DT[dt], F.gen(M + K + N + group)
     x = F.randn(g, (M, K), 1.0, dtype)
-    (qg, wg), (qu, wu) = _weights(g, (N, K), group), _weights(g, (N, K), group)
-    xd = x.double()
-    gd, gs, ud, us = xd @ wg.t(), xd.abs() @ wg.abs().t(), xd @ wu.t(), xd.abs() @ wu.abs().t()
-    s = F.sum_bound(K, dt == "f32") + _rounded(M, dtype)
+    (qg, wg, mg), (qu, wu, mu) = _weights(g, (N, K), group), _weights(g, (N, K), group)
+    xd, way = x.double(), _way(M, N, gated=True, dtype=dtype)
+    gd, ud, gb, ub = xd @ wg.t(), xd @ wu.t(), _sums(xd, wg, mg, K, way, dtype), _sums(xd, wu, mu, K, way, dtype)
     hd = F.act(gd, act) * ud
-    hb = F.ACT_LIP * gs * s * (ud.abs() + us * s) + F.act(gd, act).abs() * us * s + hd.abs() * (F.ACT_REL + 2 * F.U + F.store(dtype))
+    hb = F.ACT_LIP * gb * (ud.abs() + ub) + F.act(gd, act).abs() * ub + hd.abs() * (F.ACT_REL + 2 * F.U + F.store(dtype))
     F.assert_within(ax.ax_gated_q4(x.cuda(), qg, qu, act=act), hd, hb)
 
 
 @pytest.mark.parametrize("gated", [False, True])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("sizes", [[1], [0, 2, 0, 1], [16, 0, 17, 31], [3, 1, 2, 0, 0, 40], [100, 0, 90], [70, 64, 0, 65, 129]])
-def test_experts(sizes, dt, gated):
-    dtype, g, E, K, N, group = F.DT[dt], F.gen(sum(sizes)), len(sizes), 200, 72, 64
+@pytest.mark.parametrize("sizes,K,N", [([1], 200, 72), ([0, 2, 0, 1], 200, 72), ([16, 0, 17, 31], 200, 72), ([3, 1, 2, 0, 0, 40], 200, 72),
+                                       ([100, 0, 90], 200, 72), ([70, 64, 0, 65, 129], 200, 2101), ([300, 0, 513, 2, 400], 136, 2100), ([0, 0, 777], 65, 1000),
+                                       ([1500, 2, 1100], 64, 400), ([40, 31, 0, 64, 33, 1], 72, 4096)])
+def test_experts(sizes, K, N, dt, gated):
+    dtype, g, E, group = F.DT[dt], F.gen(sum(sizes)), len(sizes), 64
     R, T = sum(sizes), max(1, sum(sizes) // 2)
     x = F.randn(g, (T, K), 1.0, dtype)
     index = torch.randint(0, T, (R + 2,), generator=g).to(torch.int32)
@@ -140,35 +161,34 @@ def test_experts(sizes, dt, gated):
     if R > 3:
         index[1] = T
     offsets = torch.tensor([sum(sizes[:e]) for e in range(E + 1)], dtype=torch.int32)
-    (q, w), (qu, wu) = _weights(g, (E, N, K), group), _weights(g, (E, N, K), group)
+    (q, w, most), (qu, wu, mostu) = _weights(g, (E, N, K), group), _weights(g, (E, N, K), group)
     in_x = (index[:R] >= 0) & (index[:R] < T)
     xd = x.double()[index[:R].long().clamp(0, T - 1)] * in_x[:, None]
-    expert = torch.repeat_interleave(torch.arange(E), torch.tensor(sizes))
-    z = lambda v, t: torch.einsum("rk,rnk->rn", t, v[expert])  # noqa: E731
+    way = _way(R + 2, N, min(E, R + 2), gated, dtype)
+    parts = lambda v, m: [torch.cat(t) for t in zip(*[(p @ v[e].t(), _sums(p, v[e], m[e], K, way, dtype)) for e, p in enumerate(xd.split(sizes))])]  # noqa: E731
     out = torch.full((R + 2, N), 7.0, dtype=dtype, device="cuda")
-    s = F.sum_bound(K, dt == "f32") + _rounded(R + 2, dtype, min(E, R + 2))
-    gd, gs = z(w, xd), z(w.abs(), xd.abs())
+    gd, gb = parts(w, most)
     dev = dict(offsets=offsets.cuda(), tokens=index.cuda())
     if gated:
-        ud, us = z(wu, xd), z(wu.abs(), xd.abs())
+        ud, ub = parts(wu, mostu)
         ax.ax_gated_q4(x.cuda(), q, qu, act="silu", h_out=out, **dev)
         yd = F.act(gd, "silu") * ud
-        bound = F.ACT_LIP * gs * s * (ud.abs() + us * s) + F.act(gd, "silu").abs() * us * s + yd.abs() * (F.ACT_REL + 2 * F.U + F.store(dtype))
+        bound = F.ACT_LIP * gb * (ud.abs() + ub) + F.act(gd, "silu").abs() * ub + yd.abs() * (F.ACT_REL + 2 * F.U + F.store(dtype))
     else:
         ax.ax_matmul_q4(x.cuda(), q, y_out=out, **dev)
-        yd, bound = gd, gs * s + gd.abs() * F.store(dtype)
+        yd, bound = gd, gb + gd.abs() * F.store(dtype)
     F.assert_within(out[:R], yd, bound)
     assert bool((out[R:] == 7).all())
 
 
-@pytest.mark.parametrize("M", [5, 200])
+@pytest.mark.parametrize("M,N", [(5, 80), (500, 2100), (700, 1600)])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("offset,pad", [(0, 8), (1, 6), (3, 2)])
-def test_pitches_and_places(M, dt, offset, pad):
-    g, K, N, dtype = F.gen(4), 264, 80, F.DT[dt]
+def test_pitches_and_places(M, N, dt, offset, pad):
+    g, K, dtype = F.gen(4), 264, F.DT[dt]
     wide = lambda r, c: F.randn(g, (r, c + offset + pad), 1.0, dtype).cuda()  # noqa: E731
     inner = lambda t: t[:, offset:t.shape[1] - pad]  # noqa: E731
-    q, _ = _weights(g, (N, K), 128)
+    q, _, _ = _weights(g, (N, K), 128)
     x, r, buf = inner(wide(M, K)), inner(wide(M, N)), wide(M, N)
     old = buf.clone()
     want = ax.ax_matmul_q4(x.contiguous(), q, residual=r.contiguous(), act="silu")
@@ -183,7 +203,7 @@ def test_pitches_and_places(M, dt, offset, pad):
 
 def test_no_rows_and_no_x():
     g = F.gen(0)
-    q, _ = _weights(g, (40, 64), 32)
+    q, _, _ = _weights(g, (40, 64), 32)
     assert ax.ax_matmul_q4(torch.empty((0, 64), device="cuda"), q).shape == (0, 40)
     assert ax.ax_gated_q4(torch.empty((0, 64), device="cuda"), q, q).shape == (0, 40)
     y = ax.ax_matmul_q4(torch.empty((0, 64), device="cuda"), q, tokens=torch.zeros(3, dtype=torch.int32, device="cuda"))
@@ -193,18 +213,20 @@ def test_no_rows_and_no_x():
 def test_what_lies_behind_a_row_is_not_looked_at():
     """NaN behind the last column of x, in the same buffer, and between its rows."""
     g = F.gen(2)
-    q, w = _weights(g, (30, 100), 32)
-    for M in (3, 100):
-        buf = torch.full((M, 128), float("nan"), device="cuda")
-        buf[:, :100] = F.randn(g, (M, 100)).cuda()
-        xd = buf[:, :100].cpu().double()
-        zd = xd @ w.t()
-        F.assert_within(ax.ax_matmul_q4(buf[:, :100], q), zd, (xd.abs() @ w.abs().t()) * F.sum_bound(100, True) + zd.abs() * F.store(torch.float32))
+    for M, N in ((3, 30), (300, 3700), (700, 1650)):
+        q, w, most = _weights(g, (N, 100), 32)
+        for dtype in (torch.float32, torch.bfloat16):
+            for cols in (100, 104):  # (of the buffer: rows of whole 16 bytes or not)
+                buf = torch.full((M, cols + 28), float("nan"), device="cuda", dtype=dtype)
+                buf[:, :100] = F.randn(g, (M, 100), 1.0, dtype).cuda()
+                xd = buf[:, :100].cpu().double()
+                zd = xd @ w.t()
+                F.assert_within(ax.ax_matmul_q4(buf[:, :100], q), zd, _sums(xd, w, most, 100, _way(M, N, dtype=dtype), dtype) + zd.abs() * F.store(dtype))
 
 
 def test_experts_of_one_matrix_take_all_rows_without_offsets():
     g = F.gen(7)
-    q, w = _weights(g, (1, 24, 64), 32)
+    q, _, _ = _weights(g, (1, 24, 64), 32)
     x = F.randn(g, (9, 64)).cuda()
     o = torch.tensor([2, 7], dtype=torch.int32).cuda()
     y = ax.ax_matmul_q4(x, q)
