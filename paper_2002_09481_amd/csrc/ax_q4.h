@@ -22,10 +22,13 @@ __host__ __device__ __forceinline__ int q4_shift(int i) { return (i >> 1) * 4 + 
 __device__ __forceinline__ q4_words widen(uint32_t d) {
   q4_words v;
   d ^= 0x88888888u;
+  uint32_t odd = d >> 4;
+  asm("" : "+v"(odd));  // (kept as it is: the conversions then take bytes of the two words as they lie)
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(d >> (4 * i))));
-    const uint32_t hi = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(d >> (4 * i + 16))));
+    const uint32_t b = (i & 1 ? odd : d) >> (8 * (i >> 1));
+    const uint32_t lo = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(b & 0xffu)));
+    const uint32_t hi = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(b >> 16 & 0xffu)));
     v[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);  // (the upper halves: four significant bits)
   }
   return v;

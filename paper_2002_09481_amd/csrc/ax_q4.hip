@@ -13,10 +13,11 @@
 // a time, and turns words into operands of the matrix instruction in registers: codes are whole numbers that bf16 holds, so
 // the products with x (float32: its three bf16 pieces) are exact, and each group's sum in float32 is multiplied by its
 // scale in float32.  No weight is rounded.  The waves of a workgroup share the contraction and meet in LDS.  Measured (us at rows / K / N,
-// group, back to back; in brackets the bytes at the rate of a large copy): bf16 1/4096/4096, 128 5.0 (1.7), 8/8192/8192, 32 15.2 (7.4), gated
-// 1/4096/14336, 128 19.8 (11.8), 64/4096/4096, 128 18.0 (1.9), 256/4096/4096, 128 25.2 (2.5); float32 1/4096/4096, 128 7.5 (1.7); gated, 68 rows of
-// 32 experts, 2048/1409, 32 28 (20.3).  What is left: a workgroup's way from its launch to its first block, and the meeting at its end; from 64
-// rows on the conversion of codes, 20 instructions for eight.
+// group, back to back; in brackets the bytes at the rate of a large copy): bf16 1/4096/4096, 128 5.0 (1.7), 8/8192/8192, 32 12.4 (7.4), gated
+// 1/4096/14336, 128 14.4 (11.8), gated 68 rows of 32 experts, 2048/1409, 32 22 (20.3; calls back to back 28), 64/4096/4096, 128 17.4 (1.7),
+// 256/4096/4096, 128 23.8 (1.7); float32 1/4096/4096, 128 6.4 (1.7), gated 68 rows of 32 experts 53 (20.3).  What is left: a workgroup's way
+// from its launch to its first block, and the meeting at its end; from 64 rows on the conversion of codes, 14 instructions for eight;
+// float32: x cut in pieces once for 16 to 64 columns.
 //
 // More rows: ax_q4_tile.hip, with the weights exact as well.  Very many rows of bf16: the weights are written out once, in the
 // workspace, and multiplied by the tiles of ax_gemm_experts.hip, which lose nothing to scales and codes: every weight, scale
@@ -404,7 +405,7 @@ struct Plan {
 
 // us at rows / K / N, q4_kernel : q4_tile_kernel : written out.  A few units of 64 rows by 16 columns, or few rows of an expert: the first, which
 // needs none of the others' stages.
-//   256/4096/4096 25 : 42 : 36      300/4096/4096 41 : 42 : 45   700/1000/777 12 : 13     gated 256/4096/4096 43 : 43
+//   256/4096/4096 25 : 42 : 36      300/4096/4096 41 : 42 : 45   700/1000/777 12 : 13     gated 256/4096/4096 42 : 43
 //   8 experts, 2048/1408: 512 rows 20 : 23, 2048 rows 45 : 32    32 experts, 2048 rows 50 : 34   float32 256/4096/4096 79 : 75, 300/4096/4096 97 : 75
 // Many rows of an expert: the weights pay for being written once.
 //   512/4096/4096 43 : 43 : 46      1027/4096/4096 88 : 77 : 65  2048/4096/4096 151 : 87 : 78  8192/4096/4096 626 : 330 : 230
@@ -469,7 +470,9 @@ void launch_rows(Args& a, hipStream_t s) {
   const long long work = a.w.tiles * used * ((rows + height * used - 1) / (height * used));
   const bool deep = a.w.blocks >= 32;
   if (height == 16) {
-    if (deep && work >= 512) go(one, two, eight);
+    // (float32 pays for the pieces of x in each workgroup: 68 rows of 16 experts, 1024/4096 30 / 21 / 17 with 16 / 32 / 64 columns)
+    if (F32 && NB == 1 && work >= 2048) go(one, four, eight);
+    else if ((deep || F32) && work >= 512) go(one, two, eight);
     else if (deep && work <= 256) go(one, one, sixteen);
     else go(one, one, eight);
   } else if (height == 32) {
