@@ -90,6 +90,23 @@ int ax_probe_layer_route(const ax_layer_t* layer, int* kernel, int* pixels, int*
 #define AX_PRODUCT_GATED_GW 7
 int ax_probe_product_plan(const ax_matmul_desc_t* desc, int product, int* kernel, int* rows, int* cols, int* slices);
 
+/*
+ * The same of a product grouped by expert: kernel 0 = tiles, 1 = few rows an expert straight from the operands.
+ *   product     as above, without the products of int8 codes
+ *   per_cu      workgroups that a compute unit holds (0 for kernel 1)
+ *   found       1 where tiles look up the rows of an index themselves, 0 where there is none or they are copied first
+ */
+int ax_probe_experts_plan(const ax_experts_desc_t* desc, int product, int* kernel, int* rows, int* cols, int* per_cu,
+                          int* found);
+
+/*
+ * The same of a product with 4-bit weights.
+ *   kernel      0 = few rows, 1 = tiles of codes, 2 = the weights are written out in bf16 for the tiles of the other products
+ *   rows, cols  that a workgroup computes (gated, kernels 0 and 1: columns of each weight)
+ *   waves       of a workgroup of kernel 0, which share the contraction (0 for the others)
+ */
+int ax_probe_q4_plan(const ax_q4_desc_t* desc, int gated, int* kernel, int* rows, int* cols, int* waves);
+
 #ifdef __cplusplus
 }
 #endif

@@ -64,7 +64,7 @@ EXPORTS = [  # include/axconv.h
 ]
 PROBE_EXPORTS = [  # include/axconv_probe.h
     "ax_probe_lds_gather", "ax_probe_copy", "ax_probe_mac", "ax_probe_layer_kernel_ms",
-    "ax_probe_layer_route", "ax_probe_product_plan",
+    "ax_probe_layer_route", "ax_probe_product_plan", "ax_probe_experts_plan", "ax_probe_q4_plan",
 ]
 
 
@@ -230,6 +230,8 @@ def lib():
             ("ax_adamw_states", [ctypes.POINTER(ax_adamw_tensor_t), ci, ctypes.POINTER(vp), ctypes.POINTER(vp), vp])):
         getattr(L, name).argtypes, getattr(L, name).restype = args, ci
     L.ax_probe_product_plan.argtypes, L.ax_probe_product_plan.restype = [md, ci] + [ip] * 4, ci
+    L.ax_probe_experts_plan.argtypes, L.ax_probe_experts_plan.restype = [ctypes.POINTER(ax_experts_desc_t), ci] + [ip] * 5, ci
+    L.ax_probe_q4_plan.argtypes, L.ax_probe_q4_plan.restype = [ctypes.POINTER(ax_q4_desc_t), ci] + [ip] * 4, ci
     L.ax_rmsnorm_backward_workspace_bytes.argtypes, L.ax_rmsnorm_backward_workspace_bytes.restype = [nd], sz
     for name in ("ax_matmul", "ax_matmul_q8", "ax_matmul_backward", "ax_gated", "ax_gated_q8", "ax_gated_backward"):
         f = getattr(L, name + "_workspace_bytes")
@@ -2005,6 +2007,30 @@ def ax_probe_product_plan(product: str, M: int, K: int, N: int, dtype=torch.bflo
     _check(lib().ax_probe_product_plan(d, PRODUCTS.index(product), *[ctypes.byref(o) for o in out]))
     k, rows, cols, slices = [o.value for o in out]
     return {"kernel": ("tiles", "few", "outer")[k], "tile": (rows, cols), "slices": slices}
+
+
+def _plan(f, results, desc, *args) -> list:
+    out = [ctypes.c_int(0) for _ in range(results)]
+    _check(f(ctypes.byref(desc), *args, *[ctypes.byref(o) for o in out]))
+    return [o.value for o in out]
+
+
+def ax_probe_experts_plan(product: str, rows: int, experts: int, K: int, N: int, dtype=torch.bfloat16, transposed=False, x_rows=None,
+                          unaligned=False) -> dict:
+    """Which kernel a product grouped by expert runs ("tiles", "few"), its tile, its workgroups a compute unit, and whether it looks up the
+    rows of an index (of x_rows rows) itself.  Contiguous operands."""
+    d = ax_experts_desc_t(rows, rows if x_rows is None else x_rows, N, K, K, K if transposed else N, N, K, experts, _DT[dtype], 0,
+                          int(transposed), int(x_rows is not None), int(unaligned))
+    k, r, c, per_cu, found = _plan(lib().ax_probe_experts_plan, 5, d, PRODUCTS.index(product))
+    return {"kernel": ("tiles", "few")[k], "tile": (r, c), "per_cu": per_cu, "found": bool(found)}
+
+
+def ax_probe_q4_plan(gated: bool, rows: int, experts: int, K: int, N: int, group=128, dtype=torch.bfloat16, x_rows=None) -> dict:
+    """Which kernel a product with 4-bit weights runs ("few", "tiles", "written"), rows and columns of its workgroups, and of "few" their
+    waves.  Contiguous aligned operands."""
+    d = ax_q4_desc_t(rows, rows if x_rows is None else x_rows, N, K, K, N, N, experts, group, _DT[dtype], 0, int(x_rows is not None), 0)
+    k, r, c, waves = _plan(lib().ax_probe_q4_plan, 4, d, int(gated))
+    return {"kernel": ("few", "tiles", "written")[k], "tile": (r, c), "waves": waves}
 
 
 def ax_probe_copy(dst: torch.Tensor, src: torch.Tensor, stream=None) -> None:

@@ -341,3 +341,28 @@ extern "C" int ax_gated_experts_backward(const ax_experts_desc_t* d, const void*
   return backward_common(d, true, gh, x, index, offsets, wg, wu, g, u, gx_out, gwg_out, gwu_out, workspace, workspace_bytes,
                          (hipStream_t)hip_stream);
 }
+
+extern "C" int ax_probe_experts_plan(const ax_experts_desc_t* d, int product, int* kernel, int* rows, int* cols, int* per_cu,
+                                     int* found) {
+  const bool gated = product == AX_PRODUCT_GATED || product == AX_PRODUCT_GATED_GX || product == AX_PRODUCT_GATED_GW;
+  const bool gx = product == AX_PRODUCT_MATMUL_GX || product == AX_PRODUCT_GATED_GX;
+  const bool gw = product == AX_PRODUCT_MATMUL_GW || product == AX_PRODUCT_GATED_GW;
+  if (!gx && !gw && product != AX_PRODUCT_MATMUL && product != AX_PRODUCT_GATED) return AX_ERR_OPTION;
+  if (int rc = check_experts(d, gx || gw, gated)) return rc;
+  int k = 0, r = 0, c = 0, n = 0, at = 0;
+  if (d->rows > 0 && (gx || gw)) {
+    const Backward b = make_backward(d, gated, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
+    gx ? tile_of_experts(b.gx, false, b.tile_x, &r, &c, &n) : tile_of_experts(b.gw, true, b.tile_w, &r, &c, &n);
+  } else if (d->rows > 0) {
+    const Forward f = make_forward(d, gated, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
+    k = f.few;
+    at = f.found;
+    if (!f.few) tile_of_experts(f.g, false, f.tile, &r, &c, &n);
+  }
+  if (kernel) *kernel = k;
+  if (rows) *rows = r;
+  if (cols) *cols = c;
+  if (per_cu) *per_cu = n;
+  if (found) *found = at;
+  return AX_OK;
+}

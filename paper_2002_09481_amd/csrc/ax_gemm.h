@@ -69,7 +69,7 @@ struct Groups {
   int x_rows;
 };
 int plan_experts(const GemmArgs& g, const Groups& e, bool sums);  // the tile configuration
-void tile_of_experts(const GemmArgs& g, bool sums, int tile, int* rows, int* cols);
+void tile_of_experts(const GemmArgs& g, bool sums, int tile, int* rows, int* cols, int* per_cu);
 hipError_t launch_gemm_experts(const GemmArgs& g, const Groups& e, bool sums, int tile, hipStream_t s);
 
 // Products of few rows straight from the operands in their own type, at any element: int8 (g.i8), or dtype AX_BF16 or

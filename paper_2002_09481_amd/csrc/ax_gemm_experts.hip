@@ -105,9 +105,10 @@ int plan_experts(const GemmArgs& g, const Groups& e, bool sums) {
   return best;
 }
 
-void tile_of_experts(const GemmArgs& g, bool sums, int tile, int* rows, int* cols) {
+void tile_of_experts(const GemmArgs& g, bool sums, int tile, int* rows, int* cols, int* per_cu) {
   *rows = shape_of(g, sums, tile).bm;
   *cols = shape_of(g, sums, tile).bn;
+  *per_cu = shape_of(g, sums, tile).per_cu;
 }
 
 hipError_t launch_gemm_experts(const GemmArgs& g, const Groups& e, bool sums, int tile, hipStream_t s) {

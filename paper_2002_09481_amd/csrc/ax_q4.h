@@ -47,6 +47,7 @@ __device__ __forceinline__ q4_words widen_more(uint32_t d) {
 constexpr uint32_t kQ4Less = 0xc1c0c1c0u;  // -24, twice
 
 // Many rows of x (ax_q4_tile.hip).  g as for launch_gemm_experts, without right operands; N columns of each weight.
+int q4_tile_rows(const GemmArgs& g, const Groups& e);  // of a workgroup
 hipError_t launch_q4_tiles(const GemmArgs& g, const Groups& e, const Q4Weights& w, hipStream_t s);
 
 }  // namespace ax

@@ -30,6 +30,7 @@
 #include "ax_group.h"
 #include "ax_operand.h"
 #include "ax_q4.h"
+#include "axconv_probe.h"
 
 namespace ax {
 namespace {
@@ -447,15 +448,38 @@ Plan make_plan(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* 
 }
 
 // A workgroup's columns, 16, 32 or 64 of them: as many as leave work for two thirds of the compute units, since each reads all
-// rows of x (us with 16 / 32 / 64: 64/2048/11264 26 / 23 / 18, 64/4096/4096 18 / 19 / 24, 256/4096/4096 61 / 36 / 25).  Its waves:
-// 16 where there are few workgroups and many blocks (1/4096/4096 5.0, eight waves 5.7), else eight (32 experts, 2048/1409 28, sixteen 39: two
-// blocks a wave are over before the next workgroup has started).
+// rows of x (us with 16 / 32 / 64: 64/2048/11264 26 / 23 / 18, 64/4096/4096 18 / 19 / 24, 256/4096/4096 61 / 36 / 25).  float32 pays for the
+// pieces of x in each workgroup as well: 68 rows of 16 experts, 1024/4096 30 / 21 / 17, gated 32 experts, 2048/1409 55 / 53 / 50, 8 experts,
+// 2048/4096 30 / 25 / 27.  Its waves: 16 where there are few workgroups and many blocks (1/4096/4096 5.0, eight waves 5.7), else eight
+// (32 experts, 2048/1409 28, sixteen 39: two blocks a wave are over before the next workgroup has started).
 constexpr long long kLeast = 170;
+struct FewShape {
+  int bands, cols, waves;  // rows and columns by 16
+};
+FewShape few_shape(bool f32, bool gated, const Groups& e, const Q4Weights& w) {
+  const long long used = std::max(1, e.offsets ? std::min(e.experts, e.rows) : 1), rows = e.rows;
+  const int bands = rows <= 16 * used ? 1 : f32 || rows <= 32 * used ? 2 : 4;  // (three pieces of 64 rows leave no registers)
+  // tiles of 16 columns by bands of rows that there can be expected
+  const long long work = w.tiles * used * ((rows + 16 * bands * used - 1) / (16 * bands * used));
+  const bool deep = w.blocks >= 32;
+  if (bands == 1) {
+    if (f32 && !gated && work >= 2048) return {1, 4, 8};
+    if ((deep || f32) && work >= 512) return {1, 2, 8};
+    return {1, 1, deep && work <= 256 ? 16 : 8};
+  }
+  if (bands == 2) {
+    if (work >= 2 * kLeast) return {2, 2, 8};
+    return {2, 1, deep && !f32 ? 16 : 8};
+  }
+  if (!gated && work >= 4 * kLeast) return {4, 4, 4};
+  return {4, work >= 2 * kLeast ? 2 : 1, 8};
+}
 template <bool F32, int NB, int G>
 void launch_rows(Args& a, hipStream_t s) {
-  const long long used = std::max(1, a.e.offsets ? std::min(a.e.experts, a.e.rows) : 1), rows = a.e.rows;
+  const FewShape f = few_shape(F32, NB == 2, a.e, a.w);
   auto go = [&](auto mfr, auto cf, auto waves) {
     constexpr int MFR = decltype(mfr)::value, CF = decltype(cf)::value, WAVES = decltype(waves)::value;
+    const long long used = std::max(1, a.e.offsets ? std::min(a.e.experts, a.e.rows) : 1), rows = a.e.rows;
     a.wide = (a.w.tiles + CF - 1) / CF;
     const long long bands = a.e.offsets ? rows / (16 * MFR) + used : (rows + 16 * MFR - 1) / (16 * MFR);
     q4_kernel<F32, NB, MFR, CF, G, WAVES><<<(int)(bands * a.wide), 64 * WAVES, 0, s>>>(a);
@@ -465,25 +489,24 @@ void launch_rows(Args& a, hipStream_t s) {
   constexpr auto four = std::integral_constant<int, 4>{};
   constexpr auto eight = std::integral_constant<int, 8>{};
   constexpr auto sixteen = std::integral_constant<int, 16>{};
-  // tiles of 16 columns by bands of rows that there can be expected
-  const int height = rows <= 16 * used ? 16 : F32 || rows <= 32 * used ? 32 : 64;  // (three pieces of 64 rows leave no registers)
-  const long long work = a.w.tiles * used * ((rows + height * used - 1) / (height * used));
-  const bool deep = a.w.blocks >= 32;
-  if (height == 16) {
-    // (float32 pays for the pieces of x in each workgroup: 68 rows of 16 experts, 1024/4096 30 / 21 / 17 with 16 / 32 / 64 columns)
-    if (F32 && NB == 1 && work >= 2048) go(one, four, eight);
-    else if ((deep || F32) && work >= 512) go(one, two, eight);
-    else if (deep && work <= 256) go(one, one, sixteen);
+  if (f.bands == 1) {
+    if constexpr (F32 && NB == 1) {
+      if (f.cols == 4) return go(one, four, eight);
+    }
+    if (f.cols == 2) go(one, two, eight);
+    else if (f.waves == 16) go(one, one, sixteen);
     else go(one, one, eight);
-  } else if (height == 32) {
-    if (work >= 2 * kLeast) go(two, two, eight);
-    else if (deep && !F32) go(two, one, std::integral_constant<int, F32 ? 8 : 16>{});
+  } else if (f.bands == 2) {
+    if constexpr (!F32) {
+      if (f.waves == 16) return go(two, one, sixteen);
+    }
+    if (f.cols == 2) go(two, two, eight);
     else go(two, one, eight);
   } else if constexpr (!F32) {
     if constexpr (NB == 1) {
-      if (work >= 4 * kLeast) return go(four, four, four);
+      if (f.cols == 4) return go(four, four, four);
     }
-    if (work >= 2 * kLeast) go(four, two, eight);
+    if (f.cols == 2) go(four, two, eight);
     else go(four, one, eight);
   }
 }
@@ -495,11 +518,7 @@ hipError_t launch_group(Args& a, int group, hipStream_t s) {
   return hipGetLastError();
 }
 
-int run(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* index, const int32_t* offsets, const uint8_t* const (&codes)[2],
-        const void* const (&scales)[2], const void* bias, const void* residual, void* y, void* ws, size_t ws_bytes, hipStream_t s) {
-  Plan p = make_plan(d, gated, x, offsets, ws);
-  if (!ws_ok(ws, ws_bytes, p.bytes)) return AX_ERR_WORKSPACE;
-  const bool f32 = d->dtype == AX_F32;
+Q4Weights weights_of(const ax_q4_desc_t* d, const uint8_t* const (&codes)[2], const void* const (&scales)[2]) {
   const Shape sh = shape_of(d->N, d->K, d->group);
   Q4Weights w{};
   for (int b = 0; b < 2; ++b) {
@@ -509,6 +528,15 @@ int run(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* index, 
   w.tiles = (int)sh.tiles;
   w.blocks = (int)sh.blocks;
   w.group = d->group;
+  return w;
+}
+
+int run(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* index, const int32_t* offsets, const uint8_t* const (&codes)[2],
+        const void* const (&scales)[2], const void* bias, const void* residual, void* y, void* ws, size_t ws_bytes, hipStream_t s) {
+  Plan p = make_plan(d, gated, x, offsets, ws);
+  if (!ws_ok(ws, ws_bytes, p.bytes)) return AX_ERR_WORKSPACE;
+  const bool f32 = d->dtype == AX_F32;
+  const Q4Weights w = weights_of(d, codes, scales);
   if (p.way == kFew) {
     Args a{};
     a.x = x;
@@ -660,4 +688,31 @@ extern "C" int ax_gated_q4(const ax_q4_desc_t* d, const void* x, const int32_t* 
   if (!aligned_to(h_out, elem_bytes(d->dtype))) return AX_ERR_ALIGN;
   return run(d, true, x, index, offsets, {g_codes, u_codes}, {g_scales, u_scales}, nullptr, nullptr, h_out, workspace, workspace_bytes,
              (hipStream_t)hip_stream);
+}
+
+extern "C" int ax_probe_q4_plan(const ax_q4_desc_t* d, int gated, int* kernel, int* rows, int* cols, int* waves) {
+  if (gated & ~1) return AX_ERR_OPTION;
+  if (int rc = check_q4(d, gated != 0, false)) return rc;
+  int k = 0, r = 0, c = 0, n = 0, unused;
+  if (d->rows > 0) {
+    static const int32_t grouped = 0;  // (asked only whether there are any)
+    const Plan p = make_plan(d, gated != 0, nullptr, d->experts > 1 ? &grouped : nullptr, nullptr);
+    k = p.way;
+    if (k == kFew) {
+      const FewShape f = few_shape(d->dtype == AX_F32, gated != 0, p.e, weights_of(d, {nullptr, nullptr}, {nullptr, nullptr}));
+      r = 16 * f.bands;
+      c = 16 * f.cols;
+      n = f.waves;
+    } else if (k == kTiles) {
+      r = q4_tile_rows(p.g, p.e);
+      c = gated ? 128 : 256;
+    } else {
+      tile_of_experts(p.g, false, p.tile, &r, &c, &unused);
+    }
+  }
+  if (kernel) *kernel = k;
+  if (rows) *rows = r;
+  if (cols) *cols = c;
+  if (waves) *waves = n;
+  return AX_OK;
 }

@@ -223,20 +223,25 @@ void launch_group(const TileArgs& a, int grid, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_q4_tiles(const GemmArgs& g, const Groups& e, const Q4Weights& w, hipStream_t s) {
-  TileArgs a{g, e, w, wide_of(g.N, g.gated != 0)};
+// 64 rows a workgroup or 32: rounds of workgroups over the card, in us for 4096 columns of the contraction.  (300/4096/4096 64 : 32 rows 58 : 42,
+// 1027/4096/4096 80 : 77, 2048/4096/4096 87 : 108, 2048 rows of 32 experts, 2048/1408 44 : 34; float32 512/4096/4096 107 : 77, 2048/4096/4096 228 : 285.)
+int q4_tile_rows(const GemmArgs& g, const Groups& e) {
   const bool f32 = g.pieces == 3;
-  // 64 rows a workgroup or 32: rounds of workgroups over the card, in us for 4096 columns of the contraction.  (300/4096/4096 64 : 32 rows 58 : 42,
-  // 1027/4096/4096 80 : 77, 2048/4096/4096 87 : 108, 2048 rows of 32 experts, 2048/1408 44 : 34; float32 512/4096/4096 107 : 77, 2048/4096/4096 228 : 285.)
+  const int wide = wide_of(g.N, g.gated != 0);
   const double experts = (double)std::max(1, e.offsets ? std::min(e.experts, e.rows) : 1), each = e.rows / experts;
   auto count = [&](int height) {
-    return (long long)(a.wide * (e.experts == 1 ? std::ceil(each / height) : experts * std::max(1.0, each / height + 0.5)));
+    return (long long)(wide * (e.experts == 1 ? std::ceil(each / height) : experts * std::max(1.0, each / height + 0.5)));
   };
   auto rounds = [](long long n, long long slots) { return (double)((n + slots - 1) / slots); };
   const long long n4 = count(64), n2 = count(32);
   const double cost4 = f32 ? 100 * rounds(n4, 256) : n4 <= 256 ? 57 : 84 * rounds(n4, 512);
   const double cost2 = f32 ? 70 * rounds(n2, 256) : n2 <= 256 ? 42 : 76 * rounds(n2, 768);
-  const bool low = cost2 < cost4;
+  return cost2 < cost4 ? 32 : 64;
+}
+
+hipError_t launch_q4_tiles(const GemmArgs& g, const Groups& e, const Q4Weights& w, hipStream_t s) {
+  TileArgs a{g, e, w, wide_of(g.N, g.gated != 0)};
+  const bool f32 = g.pieces == 3, low = q4_tile_rows(g, e) == 32;
   const long long grid = grid_of(e, low ? 32 : 64, a.wide);
   if (grid <= 0 || grid >= 1 << 23) return hipErrorInvalidValue;
   const int n = (int)grid;
