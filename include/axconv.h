@@ -720,7 +720,7 @@ int ax_q4_values(const uint8_t* codes, const void* scales, int64_t experts, int6
  * [rows, N] (both may be NULL; y_out may be residual itself) have x's type.  With several experts the rows are grouped as above (index
  * and offsets; offsets may be NULL for one expert, whose rows are then all).  The weights are exact: products with the
  * codes are exact and summed in float32, each group's sum times its scale in float32 (some sums of bf16 rows run over codes with 24 added, taken
- * off again in float32).  Only for more than 600 bf16 rows an expert on the average, every weight is rounded to bf16 for the matrix instructions.
+ * off again in float32; an infinity in x may come out as a NaN).  Only for more than 600 bf16 rows an expert on the average, every weight is rounded to bf16 for the matrix instructions.
  * workspace: ax_*_q4_workspace_bytes(desc) bytes, 256-byte aligned.
  */
 typedef struct {

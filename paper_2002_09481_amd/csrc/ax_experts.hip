@@ -22,7 +22,8 @@ namespace {
 // experts / rows / inputs / outputs of a gated pair, found : copied first: 8/16384/2048/8192 1107 : 1127, 32/8192/1024/1416 90 : 106,
 // 16/1024/2048/1408 40 : 46.
 bool found_in_place(const ax_experts_desc_t* d) {
-  return d->indexed && d->dtype == AX_BF16 && !d->unaligned && d->K % 8 == 0 && d->x_ld % 8 == 0 && d->x_rows * d->x_ld * 2 < 1ll << 31;
+  return d->indexed && d->x_rows > 0 && d->dtype == AX_BF16 && !d->unaligned && d->K % 8 == 0 && d->x_ld % 8 == 0 &&
+         d->x_rows * d->x_ld * 2 < 1ll << 31;
 }
 // x as the tiles read it: in place, or copied, in the order of the products where it is indexed and not found.
 Operand make_rows(const ax_experts_desc_t* d, bool found, const void* x, const int32_t* index, Arena& ar, PackJob* job) {
@@ -70,6 +71,7 @@ struct Forward {
 //   float32, weights that the tiles take in copied pieces: 64/1024/1024 (30) 131 : 238, (60) 204 : 249   [N, K] (20) 167 : 214, (60) 360 : 260
 //     8/2048/4096 (60) 173 : 245   [N, K] (30) 152 : 253, (60) 285 : 269   32/256/512 [N, K] (20) 25 : 27, (30) 33 : 28
 bool few_fits(const ax_experts_desc_t* d) {
+  if (d->x_rows == 0) return false;  // (it reads some row of x for an index outside)
   const long long used = std::min<long long>(d->experts, d->rows), tiles = (d->N + 31) / 32;
   if ((d->rows / 16 + used) * 2 * tiles >= 1 << 21) return false;  // (a launch counts its threads in 32 bits)
   if (d->dtype == AX_F32) return d->rows <= (d->w_transposed ? 28 : 48) * used;

@@ -426,7 +426,8 @@ Plan make_plan(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* 
   p.way = way_of(d, gated);
   p.e = Groups{offsets, d->experts, (int)d->rows, nullptr, 0};
   if (p.way == kFew) return p;
-  p.found = d->indexed && d->dtype == AX_BF16 && !d->unaligned && d->K % 8 == 0 && d->x_ld % 8 == 0 && d->x_rows * d->x_ld * 2 < 1ll << 31;
+  p.found = d->indexed && d->x_rows > 0 && d->dtype == AX_BF16 && !d->unaligned && d->K % 8 == 0 && d->x_ld % 8 == 0 &&
+            d->x_rows * d->x_ld * 2 < 1ll << 31;
   const Operand a = make_operand(x, p.found ? d->x_rows : d->rows, d->K, d->x_ld, d->dtype, d->unaligned || (d->indexed && !p.found), ar, &p.job);
   GemmArgs& g = p.g;
   if (p.way == kWritten) {

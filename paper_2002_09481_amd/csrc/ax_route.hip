@@ -580,15 +580,22 @@ extern "C" int ax_route_backward(const ax_route_desc_t* d, const float* gweights
   if (!aligned_to(logits, elem_bytes(d->dtype)) || !aligned_to(glogits_out, elem_bytes(d->dtype))) return AX_ERR_ALIGN;
   for (const void* p : {(const void*)gweights, (const void*)experts, (const void*)weights})
     if (!aligned_to(p, 4)) return AX_ERR_ALIGN;
-  const RouteGradArgs a{gweights, logits, experts, weights, glogits_out, d->ld, glogits_ld, (int)d->tokens, d->experts, d->k, d->normalize};
   const hipStream_t s = (hipStream_t)hip_stream;
-  by_experts(d->experts, [&](auto l, auto v) {
-    constexpr int L = decltype(l)::value, V = decltype(v)::value;
-    const int grid = (int)((d->tokens + 256 / L - 1) / (256 / L));
-    if (d->dtype == AX_F32) route_grad_kernel<true, L, V><<<grid, 256, 0, s>>>(a);
-    else route_grad_kernel<false, L, V><<<grid, 256, 0, s>>>(a);
-  });
-  return hipGetLastError() == hipSuccess ? AX_OK : AX_ERR_HIP;
+  const int e = elem_bytes(d->dtype);
+  const int64_t most = 1 << 24;  // (a launch counts its threads in 32 bits)
+  for (int64_t t0 = 0; t0 < d->tokens; t0 += most) {
+    const int n = (int)std::min(most, d->tokens - t0);
+    const RouteGradArgs a{gweights + t0 * d->k, logits ? (const char*)logits + t0 * d->ld * e : nullptr, experts + t0 * d->k,
+                          weights + t0 * d->k, (char*)glogits_out + t0 * glogits_ld * e, d->ld, glogits_ld, n, d->experts, d->k, d->normalize};
+    by_experts(d->experts, [&](auto l, auto v) {
+      constexpr int L = decltype(l)::value, V = decltype(v)::value;
+      const int grid = (n + 256 / L - 1) / (256 / L);
+      if (d->dtype == AX_F32) route_grad_kernel<true, L, V><<<grid, 256, 0, s>>>(a);
+      else route_grad_kernel<false, L, V><<<grid, 256, 0, s>>>(a);
+    });
+    if (hipGetLastError() != hipSuccess) return AX_ERR_HIP;
+  }
+  return AX_OK;
 }
 
 extern "C" int ax_combine(const ax_combine_desc_t* d, const void* h, const int32_t* rows, const float* weights, const void* residual,

@@ -55,6 +55,13 @@ def test_few_rows_and_rows_that_are_copied():
     assert not plan("gated", 4000, 2, 8192, 64, x_rows=1 << 17)["found"]  # 2 GB of x: copied
 
 
+def test_an_empty_x_is_not_read():
+    """Rows of an x that has none, all of zeros: only the copies know what to do with those."""
+    for rows, dt in ((4, "bf16"), (4, "f32"), (4000, "bf16"), (4000, "f32")):
+        plan = ax.ax_probe_experts_plan("matmul", rows, 2, 1000, 1000, F.DT[dt], x_rows=0)
+        assert plan["kernel"] == "tiles" and not plan["found"]
+
+
 def test_refusals():
     L, R, none = ax.lib(), ctypes.byref, [None] * 5
     d = ax.ax_experts_desc_t(4, 4, 64, 32, 32, 64, 64, 32, 2, 1, 0, 0, 0, 0)

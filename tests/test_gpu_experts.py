@@ -223,6 +223,22 @@ def test_no_rows():
     assert not bool(ax.ax_matmul_experts_backward(y, x, w, o, gw_out=full())[1].any())
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [3, 700])
+def test_rows_of_an_empty_x(rows, dt):
+    """Every index lies outside: rows of zeros."""
+    K, N, kw = 264, 520, dict(dtype=F.DT[dt], device="cuda")
+    x, w, gy = torch.empty((0, K), **kw), torch.ones((2, K, N), **kw), torch.ones((rows, N), **kw)
+    o, t = torch.tensor([0, 1, rows], dtype=torch.int32).cuda(), torch.arange(-1, rows - 1, dtype=torch.int32, device="cuda")
+    for transposed in (False, True):
+        v = w.transpose(1, 2).contiguous() if transposed else w
+        y, z = ax.ax_matmul_experts(x, v, o, t, transposed=transposed, save=True)
+        assert y.shape == (rows, N) and not bool(y.any()) and not bool(z.any())
+        gx, gw = ax.ax_matmul_experts_backward(gy, x, v, o, t, transposed=transposed, gw_out=torch.ones_like(v))
+        assert bool((gx == N).all()) and not bool(gw.any())
+    assert not any(bool(v.any()) for v in ax.ax_gated_experts(x, w, w, o, t, save=True))
+
+
 def test_many_experts():
     """More than a wave looks up at a time."""
     g, E, K, N = F.gen(11), 1024, 16, 24

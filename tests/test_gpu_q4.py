@@ -210,6 +210,16 @@ def test_no_rows_and_no_x():
     assert y.shape == (3, 40) and not bool(y.any())
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,N", [(3, 40), (300, 3700), (700, 1650)])
+def test_rows_of_an_empty_x(rows, N, dt):
+    """Every index lies outside: rows of zeros, whichever kernel."""
+    q, _, _ = _weights(F.gen(1), (N, 264), 64)
+    x, t = torch.empty((0, 264), dtype=F.DT[dt], device="cuda"), torch.arange(-1, rows - 1, dtype=torch.int32, device="cuda")
+    b = torch.ones(N, dtype=F.DT[dt], device="cuda")
+    assert bool((ax.ax_matmul_q4(x, q, bias=b, tokens=t) == 1).all()) and not bool(ax.ax_gated_q4(x, q, q, tokens=t).any())
+
+
 def test_what_lies_behind_a_row_is_not_looked_at():
     """NaN behind the last column of x, in the same buffer, and between its rows."""
     g = F.gen(2)

@@ -187,6 +187,15 @@ def test_route_gradient_against_differences():
         assert abs(float(got.sum()) - slope) <= e * e * third + 1e-15 * T / e + float(got.abs().sum()) * 200 * F.U
 
 
+def test_route_gradient_of_very_many_tokens():
+    """More than a launch can count the threads of."""
+    T, kw = (1 << 28) + 5, dict(device="cuda")
+    logits, experts = torch.zeros((T, 1), dtype=torch.bfloat16, **kw), torch.zeros((T, 1), dtype=torch.int32, **kw)
+    weights, gw = torch.full((T, 1), 0.5, **kw), torch.full((T, 1), 2.0, **kw)
+    out = ax.ax_route_backward(gw, logits, experts, weights, glogits_out=torch.full_like(logits, 7.0))
+    assert int((out == 0.5).sum()) == T  # 0.5 (2 - 1)
+
+
 def test_route_gradient_of_nan_shows():
     x = torch.zeros((3, 20))
     x[1, 4] = float("nan")
