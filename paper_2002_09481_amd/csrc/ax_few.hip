@@ -185,8 +185,8 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
   long long w_at = 0;
   if constexpr (GR) {  // (the columns of one expert: workgroups of an XCD take neighbours)
     GroupTile e;
-    if (!find_tile(a.e.offsets, a.e.experts, a.e.rows, 16 * MFR, a.tiles, blockIdx.x, e)) return;
-    const int bands = e.tiles / a.tiles, k = xcd_run(e.tile, e.tiles);
+    if (!find_tile<false>(a.e.offsets, a.e.experts, a.e.rows, 16 * MFR, a.tiles, blockIdx.x, e)) return;
+    const int bands = e.tiles / a.tiles, k = e.tile;
     m0 = __builtin_amdgcn_readfirstlane(k % bands) * 16 * MFR;
     tile = __builtin_amdgcn_readfirstlane(k / bands);
     M = __builtin_amdgcn_readfirstlane(e.count);

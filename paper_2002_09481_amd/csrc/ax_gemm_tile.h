@@ -315,8 +315,8 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
     tile -= split * (a.tiles_m * a.tiles_n);
   } else if constexpr (GR == kRows || GR == kFound) {
     GroupTile e;
-    if (!find_tile(a.offsets, a.experts, a.rows, BM, a.tiles_n, blockIdx.x, e)) return;
-    tile = uniform(xcd_run(e.tile, e.tiles));
+    if (!find_tile<true>(a.offsets, a.experts, a.rows, BM, a.tiles_n, blockIdx.x, e)) return;
+    tile = uniform(e.tile);
     M = uniform(e.count);
     row_at = uniform(e.first);
     tiles_m = uniform((M + BM - 1) / BM);

@@ -22,51 +22,78 @@ __device__ __forceinline__ Span span_of(const int32_t* offsets, int e, int rows)
   return Span{lo, hi - lo};
 }
 
+// Workgroups b, b + 8, ... share an XCD and its L2: item b of n in an order in which they take neighbouring ones.
+__device__ __forceinline__ int xcd_run(int b, int n) {
+  const int x = b & 7, i = b >> 3;
+  return x * (n >> 3) + min(x, n & 7) + i;
+}
+
 struct GroupTile {
   int expert, first, count;  // its rows
   int tile, tiles;           // of the expert's tiles
-  int total;                 // tiles of all experts
 };
 
-// Tile `want` of all experts' tiles, `per` for every (begun) `height` rows; false where there are not as many.  Without offsets
-// all rows are those of one expert.  height and per are above zero.
-__device__ __forceinline__ bool find_tile(const int32_t* offsets, int experts, int rows, int height, int per, int want, GroupTile& g) {
+// Tile of workgroup b among all experts' tiles, `per` for every (begun) `height` rows; false where there are not as many.  Without
+// offsets all rows are those of one expert.  height and per are above zero.  Tiles are dealt out in runs (xcd_run): all of them, so
+// that an XCD has few experts, or (RUNS false) those of each expert.
+template <bool RUNS>
+__device__ __forceinline__ bool find_tile(const int32_t* offsets, int experts, int rows, int height, int per, int b, GroupTile& g) {
   if (!offsets) {
-    g = GroupTile{0, 0, rows, want, (rows + height - 1) / height * per, 0};
-    g.total = g.tiles;
-    return want < g.tiles;
+    g = GroupTile{0, 0, rows, b, (rows + height - 1) / height * per};
+    if (b >= g.tiles) return false;
+    g.tile = xcd_run(b, g.tiles);
+    return true;
   }
   const int lane = threadIdx.x & 63;
-  int before = 0;
-  bool found = false;
-  g = GroupTile{};
-  for (int base = 0; base < experts; base += 64) {
-    Span s{0, 0};
+  Span s;
+  int mine, upto;
+  auto look = [&](int base) __attribute__((always_inline)) {  // 64 experts from base on; returns their tiles
+    s = Span{0, 0};
     if (base + lane < experts) s = span_of(offsets, base + lane, rows);
-    const int mine = (s.count + height - 1) / height * per;
-    int upto = mine;
+    mine = (s.count + height - 1) / height * per;
+    upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const int v = __shfl_up(upto, d);
       if (lane >= d) upto += v;
     }
-    const int all = __builtin_amdgcn_readlane(upto, 63);
-    if (!found && want - before < all) {
-      const unsigned long long behind = __ballot(want - before < upto);
-      if (behind) {
-        const int l = __builtin_ctzll(behind);
-        found = true;
-        g.expert = base + l;
-        g.first = __builtin_amdgcn_readlane(s.first, l);
-        g.count = __builtin_amdgcn_readlane(s.count, l);
-        g.tiles = __builtin_amdgcn_readlane(mine, l);
-        g.tile = want - before - (__builtin_amdgcn_readlane(upto, l) - g.tiles);
-      }
+    return __builtin_amdgcn_readlane(upto, 63);
+  };
+  auto take = [&](int base, int want) __attribute__((always_inline)) {  // the want-th of those
+    const unsigned long long behind = __ballot(want < upto);
+    if (!behind) return false;
+    const int l = __builtin_ctzll(behind);
+    g.expert = base + l;
+    g.first = __builtin_amdgcn_readlane(s.first, l);
+    g.count = __builtin_amdgcn_readlane(s.count, l);
+    g.tiles = __builtin_amdgcn_readlane(mine, l);
+    g.tile = want - (__builtin_amdgcn_readlane(upto, l) - g.tiles);
+    return g.tile >= 0 && g.tile < g.tiles;  // (sums that leave 32 bits: only with offsets that do not ascend)
+  };
+  g = GroupTile{};
+  bool found;
+  int all = look(0);
+  if (experts <= 64) {
+    found = b < all && take(0, RUNS ? xcd_run(b, all) : b);
+  } else {
+    int want = b;
+    if (RUNS) {
+      int total = all;
+      for (int base = 64; base < experts; base += 64) total += look(base);
+      if (b >= total) return false;
+      want = xcd_run(b, total);
+      all = look(0);
     }
-    before += all;
+    int base = 0;
+    while (want >= all && base + 64 < experts) {
+      want -= all;
+      base += 64;
+      all = look(base);
+    }
+    found = want < all && take(base, want);
   }
-  g.total = before;
-  return found && g.tile >= 0 && g.tile < g.tiles;  // (sums that leave 32 bits: only with offsets that do not ascend)
+  if (!RUNS) g.tile = found ? xcd_run(g.tile, g.tiles) : 0;
+  return found;
 }
 
 // The i-th expert by size, the larger ones first, and its rows.  By powers of two, those of one power in their order; up to 64
@@ -96,12 +123,6 @@ __device__ __forceinline__ int by_size(const int32_t* offsets, int experts, int 
   }
   s = Span{__builtin_amdgcn_readlane(mine.first, e), __builtin_amdgcn_readlane(mine.count, e)};
   return e;
-}
-
-// Workgroups b, b + 8, ... share an XCD and its L2: item b of n in an order in which they take neighbouring ones.
-__device__ __forceinline__ int xcd_run(int b, int n) {
-  const int x = b & 7, i = b >> 3;
-  return x * (n >> 3) + min(x, n & 7) + i;
 }
 
 }  // namespace ax
