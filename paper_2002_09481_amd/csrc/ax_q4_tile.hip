@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256, P == 3 ? 1 : 2) void q4_tile_kernel(const Tile
   const int t = threadIdx.x, lane = t & 63, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   GroupTile e;
-  if (!find_tile<false>(a.e.offsets, a.e.experts, a.e.rows, BM, a.wide, blockIdx.x, e)) return;
+  if (!find_tile<true>(a.e.offsets, a.e.experts, a.e.rows, BM, a.wide, blockIdx.x, e)) return;
   // (neighbouring workgroups of an XCD: all rows of the same columns)
   const int bands = e.tiles / a.wide, k = e.tile;
   const int m0 = uniform(k % bands) * BM, n0 = uniform(k / bands) * (64 * PER);
