@@ -19,8 +19,8 @@ namespace ax {
 namespace {
 
 // Whether the tiles find indexed rows themselves (forward): where they could read x in place, and count its bytes in 31 bits.  us at
-// experts / rows / inputs / outputs of a gated pair, found : copied first: 8/16384/2048/8192 1107 : 1127, 32/8192/1024/1416 90 : 106,
-// 16/1024/2048/1408 40 : 46.
+// experts / rows / inputs / outputs of a gated pair, found : copied first: 8/16384/2048/8192 904 : 929, 32/8192/1024/1416 63 : 69,
+// 16/1024/2048/1408 31 : 35.
 bool found_in_place(const ax_experts_desc_t* d) {
   return d->indexed && d->x_rows > 0 && d->dtype == AX_BF16 && !d->unaligned && d->K % 8 == 0 && d->x_ld % 8 == 0 &&
          d->x_rows * d->x_ld * 2 < 1ll << 31;
@@ -64,19 +64,19 @@ struct Forward {
 };
 
 // Whether the experts' rows are so few that launch_few_experts, which reads the weights as they lie, is worth it.  us at experts /
-// inputs / outputs (rows an expert), few : tiles.
+// inputs / outputs (rows of each expert), few : tiles.
 //   bf16, in place: while its workgroups (32 columns of an expert each) are few as well, since it reads all x in each of them
-//     64/1024/1024 (1) 17 : 14, (4) 29 : 22, (14) 44 : 26   8/2048/4096 (0.3) 8.4 : 17, (8) 30 : 28   4/4096/2048 (8) 17 : 27, (20) 26 : 27
-//   bf16, weights that the tiles copy first: 16/1001/777 gated (4) 24 : 30, (14) 38 : 33   [N, K] (8) 19 : 22, (20) 34 : 23
-//   float32, weights that the tiles take in copied pieces: 64/1024/1024 (30) 131 : 238, (60) 204 : 249   [N, K] (20) 167 : 214, (60) 360 : 260
-//     8/2048/4096 (60) 173 : 245   [N, K] (30) 152 : 253, (60) 285 : 269   32/256/512 [N, K] (20) 25 : 27, (30) 33 : 28
+//     64/1024/1024 (1) 30 : 22, (14) 35 : 23   8/2048/4096 (one row of two) 9 : 14, (8) 27 : 22   4/4096/2048 (8) 16 : 23, (20) 17 : 23
+//   bf16, weights that the tiles copy first: 16/1001/777 gated (4) 30 : 29, (14) 32 : 29   [N, K] (8) 17 : 23, (20) 29 : 23
+//   float32, weights that the tiles take in copied pieces: 64/1024/1024 (30) 96 : 212, (60) 174 : 220   [N, K] (20) 140 : 214, (60) 295 : 230
+//     8/2048/4096 (60) 146 : 213   [N, K] (30) 127 : 213, (60) 245 : 219   32/256/512 [N, K] (20) 21 : 27, (30) 23 : 27
 bool few_fits(const ax_experts_desc_t* d) {
   if (d->x_rows == 0) return false;  // (it reads some row of x for an index outside)
   const long long used = std::min<long long>(d->experts, d->rows), tiles = (d->N + 31) / 32;
   if ((d->rows / 16 + used) * 2 * tiles >= 1 << 21) return false;  // (a launch counts its threads in 32 bits)
-  if (d->dtype == AX_F32) return d->rows <= (d->w_transposed ? 28 : 48) * used;
+  if (d->dtype == AX_F32) return d->rows <= (d->w_transposed ? 40 : 64) * used;
   const bool in_place = !d->unaligned && weight_cols(d) % 8 == 0 && d->w_ld % 8 == 0;
-  return in_place ? d->rows <= 8 * used && used * tiles <= 512 : d->rows <= 12 * used;
+  return d->rows <= (!in_place ? 12 : used * tiles <= 256 ? 20 : used * tiles <= 512 ? 8 : 0) * used;
 }
 
 Forward make_forward(const ax_experts_desc_t* d, bool gated, const void* x, const int32_t* index, const int32_t* offsets, const void* w,

@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const Args a) {
   long long w_at = 0;
   if constexpr (GR) {  // (the columns of one expert: workgroups of an XCD take neighbours)
     GroupTile e;
-    if (!find_tile<false>(a.e.offsets, a.e.experts, a.e.rows, 16 * MFR, a.tiles, blockIdx.x, e)) return;
+    if (!find_tile(a.e.offsets, a.e.experts, a.e.rows, 16 * MFR, a.tiles, blockIdx.x, e)) return;
     const int bands = e.tiles / a.tiles, k = e.tile;
     m0 = __builtin_amdgcn_readfirstlane(k % bands) * 16 * MFR;
     tile = __builtin_amdgcn_readfirstlane(k / bands);

@@ -1,10 +1,11 @@
 // Matrix products of rows grouped by expert: the tiles of ax_gemm_tile.h, each of which looks up whose rows it has.
 //
-// Bound: few experts with many rows as ax_gemm.hip's tiles.  Many with few: sums by the stores of the weights' gradients, rows by tiles that
-// the experts' ends leave partly empty.  Measured (us, bf16, experts / rows / inputs / outputs, sizes that differ up to 20 times): rows
-// 8/16384/2048/4096 275 (1000 TF), 32/8192/1024/1408 50; sums 8/16384/2048/4096 247 (1110 TF), 32/8192/1024/1408 47 (92 MB
-// of results; 3 workgroups a compute unit, with tiles of 256 x 256 54, two workgroups of 128 x 128 56), 32/32768/1024/1408 118 (in the order of
-// the experts, larger or not, 160: the launch ends with the tiles of a large one).
+// Bound: few experts with many rows as ax_gemm.hip's tiles.  Many with few: sums by the stores of the weights' gradients, rows by what the
+// compute units fetch, and by tiles that the experts' ends leave partly empty.  Measured (us, bf16, experts / rows / inputs / outputs, sizes
+// that differ up to 20 times): rows 8/16384/2048/4096 266 (1030 TF), 32/8192/1024/1408 39 (600 TF); sums 8/16384/2048/4096 245 (1120 TF),
+// 32/8192/1024/1408 47 (92 MB of results; 3 workgroups a compute unit, with tiles of 256 x 256 54, two workgroups of 128 x 128 56),
+// 32/32768/1024/1408 110 (in the order of the experts, larger or not, 160: the launch ends with the tiles of a large one; whole experts an
+// XCD, by size in turn, 3 to 8 % faster with 32 or 64 of them and 25 % slower with eight).
 //
 // Rows by rows (kRows): a tile never spans two experts, so one of 256 rows wastes half of itself at an expert's end on the
 // average; the tile's height goes by the rows that an expert can expect.  Sums over rows (kSums, the weights' gradients): one

@@ -301,8 +301,8 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave % WM, wn = wave / WM;
 
-  // Tiles XCD by XCD: workgroups b, b + 8, ... share an XCD (and its L2) and take a contiguous run of tiles (grouped: of each
-  // expert's tiles); runs go down blocks of eight row tiles before they move to the next column tile.
+  // Tiles XCD by XCD: workgroups b, b + 8, ... share an XCD (and its L2) and take a contiguous run of tiles (of all
+  // experts' tiles; the weights' gradients: of each expert's); runs go down blocks of eight row tiles before they move to the next column tile.
   constexpr int kElem = I8 ? 1 : 2;
   constexpr int kStepK = KB / kElem;
   int M = g.M, K = g.K, ksteps = a.ksteps, tiles_m = a.tiles_m;
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) void gemm_kernel(const Args a) {
     tile -= split * (a.tiles_m * a.tiles_n);
   } else if constexpr (GR == kRows || GR == kFound) {
     GroupTile e;
-    if (!find_tile<true>(a.offsets, a.experts, a.rows, BM, a.tiles_n, blockIdx.x, e)) return;
+    if (!find_tile(a.offsets, a.experts, a.rows, BM, a.tiles_n, blockIdx.x, e)) return;
     tile = uniform(e.tile);
     M = uniform(e.count);
     row_at = uniform(e.first);

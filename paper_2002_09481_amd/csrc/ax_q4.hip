@@ -125,7 +125,7 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(const Args a) {
   const int t = threadIdx.x, lane = t & 63, r = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   GroupTile e;
-  if (!find_tile<false>(a.e.offsets, a.e.experts, a.e.rows, 16 * MFR, a.wide, blockIdx.x, e)) return;
+  if (!find_tile(a.e.offsets, a.e.experts, a.e.rows, 16 * MFR, a.wide, blockIdx.x, e)) return;
   // (workgroups of an XCD take neighbouring columns, and all rows of these)
   const int bands = e.tiles / a.wide, k = e.tile;
   const int m0 = __builtin_amdgcn_readfirstlane(k % bands) * 16 * MFR, tile = __builtin_amdgcn_readfirstlane(k / bands) * CF;

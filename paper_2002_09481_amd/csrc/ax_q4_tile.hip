@@ -10,7 +10,7 @@
 //
 // Bound: vector instructions (widening, scales) and matrix instructions, 63 and 49 % of the cycles at 8192/4096/4096, next to each
 // other only in part.  Measured (us at rows / K / N, group): bf16 300/4096/4096, 64 42, 1027/4096/4096, 64 77, 2048/4096/4096, 128 87,
-// 2048 rows of 32 experts, 2048/1408, 64 34; float32 512/4096/4096, 128 77.  Dropped: parts read a turn ahead in registers (they spill, or gain
+// 2048 rows of 32 experts, 2048/1408, 64 32; float32 512/4096/4096, 128 77.  Dropped: parts read a turn ahead in registers (they spill, or gain
 // nothing), three to six stages (0 to 50 % slower: fewer workgroups a compute unit), 128 rows a workgroup (one wave a SIMD, twice the time).
 #include <algorithm>
 #include <cmath>
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256, P == 3 ? 1 : 2) void q4_tile_kernel(const Tile
   const int t = threadIdx.x, lane = t & 63, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   GroupTile e;
-  if (!find_tile<true>(a.e.offsets, a.e.experts, a.e.rows, BM, a.wide, blockIdx.x, e)) return;
+  if (!find_tile(a.e.offsets, a.e.experts, a.e.rows, BM, a.wide, blockIdx.x, e)) return;
   // (neighbouring workgroups of an XCD: all rows of the same columns)
   const int bands = e.tiles / a.wide, k = e.tile;
   const int m0 = uniform(k % bands) * BM, n0 = uniform(k / bands) * (64 * PER);
