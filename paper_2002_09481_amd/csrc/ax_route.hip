@@ -230,7 +230,8 @@ __device__ __forceinline__ void lay_out(const RouteArgs& a, int count, bool writ
 }
 
 // Choices of a block of tokens, and how many each expert gets of them; one block finishes the order as well (a few tokens
-// decoded together: one launch).  16 lanes a token, four tokens a wave: bound by instructions, mostly the k searches.
+// decoded together: one launch).  16 lanes a token, four tokens a wave: bound by instructions, mostly the k searches.  16384 tokens of
+// 128 bf16 logits, 8 chosen: 6.0 us; one token of 64, 6 chosen, 4.7 us.
 template <bool F32, int L, int V>
 __global__ __launch_bounds__(kThreads) void route_kernel(const RouteArgs a) {
   __shared__ Shared s;
@@ -258,7 +259,8 @@ __global__ __launch_bounds__(kThreads) void route_kernel(const RouteArgs a) {
   place(a, t0, t1, s);
 }
 
-// Rows of a block's choices: the counts of all blocks say where its own begin.
+// Rows of a block's choices: the counts of all blocks say where its own begin.  16384 tokens of 128 experts, 8 chosen: 7.9 us, a chain
+// of latencies (256 counts of each expert, two sums over the workgroup, the places).
 __global__ __launch_bounds__(kThreads) void place_kernel(const RouteArgs a) {
   __shared__ Shared s;
   const int t = threadIdx.x, blocks = gridDim.x, mine = blockIdx.x;
@@ -299,7 +301,8 @@ __global__ __launch_bounds__(kThreads) void place_kernel(const RouteArgs a) {
 // ---- gradient of the logits --------------------------------------------------------------------
 //
 // inner = sum over j of gw_j w_j.  Over the chosen: gl[e_j] = w_j (gw_j - inner), zero elsewhere.  Over all, with p the softmax:
-// gl = p (g - inner), g the gradient of a chosen expert's weight and zero elsewhere.  Bound by memory.
+// gl = p (g - inner), g the gradient of a chosen expert's weight and zero elsewhere.  Bound by memory (6007 tokens of 60 float32
+// logits: 3.9 us, mostly the launch).
 struct RouteGradArgs {
   const float* gw;
   const void* logits;
@@ -373,7 +376,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteGradArgs a) 
 // ---- the way back ------------------------------------------------------------------------------
 //
 // y_t = residual_t + sum over j of w_tj h[row_tj], in float32 in the order of the choices; a row outside h (a choice that
-// was dropped) counts nothing.  Eight columns a thread, all rows asked for before the first is used.  Bound by memory.
+// was dropped) counts nothing.  Eight columns a thread, all rows asked for before the first is used.  Bound by memory: two rows and a residual of 8192 x 4096 bf16 48 us, 5.6 TB/s.
 struct CombineArgs {
   const void* h;
   const int32_t* rows;
@@ -421,7 +424,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
 }
 
 // gh[row_tj] = w_tj gy_t, gw_tj = the product of gy_t and h[row_tj] over the columns, summed in a fixed order.  T threads a
-// token, four choices at a time.
+// token, four choices at a time.  Bound by memory: four rows of 3001 x 1000 bf16 12.4 us, 4.4 TB/s.
 template <bool F32, int T>
 __global__ __launch_bounds__(256) void combine_grad_kernel(const CombineArgs a) {
   __shared__ float part[kAtOnce][4];
