@@ -630,6 +630,7 @@ int ax_route_backward(const ax_route_desc_t* desc, const float* gweights, const 
  *   z = x w_e,  y_out = act(z),  z_out (may be NULL, pitch N) kept for the backward pass
  *   h_out = act(x wg_e) * (x wu_e),  g_out and u_out (both or neither NULL, pitch N) kept
  * Types, sums and roundings as in ax_matmul and ax_gated.
+ * More than 2^23 tiles (2^29 float32 rows, say) are refused: AX_ERR_SHAPE, as in the gradients and in the products with 4-bit weights.
  * workspace: ax_*_experts_workspace_bytes(desc) bytes, 256-byte aligned.
  */
 typedef struct {

@@ -215,6 +215,7 @@ int backward_common(const ax_experts_desc_t* d, bool gated, const void* gy, cons
     return rc == hipSuccess ? AX_OK : AX_ERR_HIP;
   }
   Backward b = make_backward(d, gated, gy, x, index, offsets, w, w2, z, u, ws);
+  if ((gx_out && !experts_fit(b.gx, b.e, false, b.tile_x)) || (gw_out && !experts_fit(b.gw, b.e, true, b.tile_w))) return AX_ERR_SHAPE;
   if (!ws_ok(ws, ws_bytes, b.bytes)) return AX_ERR_WORKSPACE;
   const bool wanted[3] = {gw_out != nullptr, gx_out != nullptr, gx_out && gated};
   PackBatch copies{};
@@ -266,6 +267,7 @@ extern "C" int ax_matmul_experts(const ax_experts_desc_t* d, const void* x, cons
   for (const void* p : {(const void*)y_out, (const void*)z_out})
     if (!aligned_to(p, elem_bytes(d->dtype))) return AX_ERR_ALIGN;
   Forward f = make_forward(d, false, x, index, offsets, w, nullptr, workspace);
+  if (!f.few && !experts_fit(f.g, f.e, false, f.tile)) return AX_ERR_SHAPE;
   if (!ws_ok(workspace, workspace_bytes, f.bytes)) return AX_ERR_WORKSPACE;
   f.g.y = y_out;
   f.g.z = z_out;
@@ -290,6 +292,7 @@ extern "C" int ax_gated_experts(const ax_experts_desc_t* d, const void* x, const
   for (const void* p : {(const void*)h_out, (const void*)g_out, (const void*)u_out})
     if (!aligned_to(p, elem_bytes(d->dtype))) return AX_ERR_ALIGN;
   Forward f = make_forward(d, true, x, index, offsets, wg, wu, workspace);
+  if (!f.few && !experts_fit(f.g, f.e, false, f.tile)) return AX_ERR_SHAPE;
   if (!ws_ok(workspace, workspace_bytes, f.bytes)) return AX_ERR_WORKSPACE;
   f.g.y = h_out;
   f.g.z = g_out;

@@ -69,6 +69,7 @@ struct Groups {
   int x_rows;
 };
 int plan_experts(const GemmArgs& g, const Groups& e, bool sums);  // the tile configuration
+bool experts_fit(const GemmArgs& g, const Groups& e, bool sums, int tile);  // whether its tiles are as many as one launch can have
 void tile_of_experts(const GemmArgs& g, bool sums, int tile, int* rows, int* cols, int* per_cu);
 hipError_t launch_gemm_experts(const GemmArgs& g, const Groups& e, bool sums, int tile, hipStream_t s);
 

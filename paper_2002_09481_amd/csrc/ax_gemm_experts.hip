@@ -106,6 +106,8 @@ int plan_experts(const GemmArgs& g, const Groups& e, bool sums) {
   return best;
 }
 
+bool experts_fit(const GemmArgs& g, const Groups& e, bool sums, int tile) { return grid_of(g, e, sums, shape_of(g, sums, tile)) < 1 << 23; }
+
 void tile_of_experts(const GemmArgs& g, bool sums, int tile, int* rows, int* cols, int* per_cu) {
   *rows = shape_of(g, sums, tile).bm;
   *cols = shape_of(g, sums, tile).bn;
@@ -126,9 +128,7 @@ hipError_t launch_gemm_experts(const GemmArgs& g, const Groups& e, bool sums, in
   a.rows = e.rows;
   a.index = e.index;
   a.x_rows = e.x_rows;
-  const long long grid = grid_of(g, e, sums, T);
-  if (grid <= 0 || grid >= 1 << 23) return hipErrorInvalidValue;
-  const int n = (int)grid;
+  const int n = (int)grid_of(g, e, sums, T);
   if (sums) launch_tiles<1, 1, 1, kSums>(a, tile, n, s);
   else if (g.gated) g.lb == 0 ? launch_tiles<0, 0, 2, kRows>(a, tile, n, s) : launch_tiles<0, 1, 2, kRows>(a, tile, n, s);
   else g.lb == 0 ? launch_tiles<0, 0, 1, kRows>(a, tile, n, s) : launch_tiles<0, 1, 1, kRows>(a, tile, n, s);

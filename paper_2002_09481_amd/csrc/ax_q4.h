@@ -48,6 +48,7 @@ constexpr uint32_t kQ4Less = 0xc1c0c1c0u;  // -24, twice
 
 // Many rows of x (ax_q4_tile.hip).  g as for launch_gemm_experts, without right operands; N columns of each weight.
 int q4_tile_rows(const GemmArgs& g, const Groups& e);  // of a workgroup
+bool q4_tiles_fit(const GemmArgs& g, const Groups& e);  // whether they are as many as one launch can have
 hipError_t launch_q4_tiles(const GemmArgs& g, const Groups& e, const Q4Weights& w, hipStream_t s);
 
 }  // namespace ax

@@ -535,6 +535,7 @@ Q4Weights weights_of(const ax_q4_desc_t* d, const uint8_t* const (&codes)[2], co
 int run(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* index, const int32_t* offsets, const uint8_t* const (&codes)[2],
         const void* const (&scales)[2], const void* bias, const void* residual, void* y, void* ws, size_t ws_bytes, hipStream_t s) {
   Plan p = make_plan(d, gated, x, offsets, ws);
+  if ((p.way == kTiles && !q4_tiles_fit(p.g, p.e)) || (p.way == kWritten && !experts_fit(p.g, p.e, false, p.tile))) return AX_ERR_SHAPE;
   if (!ws_ok(ws, ws_bytes, p.bytes)) return AX_ERR_WORKSPACE;
   const bool f32 = d->dtype == AX_F32;
   const Q4Weights w = weights_of(d, codes, scales);

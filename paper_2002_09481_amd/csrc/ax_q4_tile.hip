@@ -239,12 +239,12 @@ int q4_tile_rows(const GemmArgs& g, const Groups& e) {
   return cost2 < cost4 ? 32 : 64;
 }
 
+bool q4_tiles_fit(const GemmArgs& g, const Groups& e) { return grid_of(e, q4_tile_rows(g, e), wide_of(g.N, g.gated != 0)) < 1 << 23; }
+
 hipError_t launch_q4_tiles(const GemmArgs& g, const Groups& e, const Q4Weights& w, hipStream_t s) {
   TileArgs a{g, e, w, wide_of(g.N, g.gated != 0)};
   const bool f32 = g.pieces == 3, low = q4_tile_rows(g, e) == 32;
-  const long long grid = grid_of(e, low ? 32 : 64, a.wide);
-  if (grid <= 0 || grid >= 1 << 23) return hipErrorInvalidValue;
-  const int n = (int)grid;
+  const int n = (int)grid_of(e, low ? 32 : 64, a.wide);
   auto go = [&](auto p, auto nb, auto found) {
     constexpr int P = decltype(p)::value, NB = decltype(nb)::value;
     low ? launch_group<P, NB, 2, decltype(found)::value>(a, n, s) : launch_group<P, NB, 4, decltype(found)::value>(a, n, s);

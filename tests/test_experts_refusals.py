@@ -202,3 +202,14 @@ def test_python_side():
                  lambda: ax.ax_gated_q4(x, x, x)):
         with pytest.raises(TypeError):  # not on the GPU, or not of the type: no fallback
             call()
+
+
+def test_more_tiles_than_a_launch_has():
+    L, many = ax.lib(), dict(rows=1 << 30, x_rows=1 << 30, N=1, K=1, x_ld=1, y_ld=1, dtype=0, indexed=0)
+    d = experts(w_ld=1, gx_ld=1, **many)
+    assert L.ax_matmul_experts(R(d), P, None, P, P, P, None, P, BIG, None) == -2
+    assert L.ax_gated_experts(R(d), P, None, P, P, P, P, None, None, P, BIG, None) == -2
+    assert L.ax_matmul_experts_backward(R(d), P, P, None, P, P, None, P, P, P, BIG, None) == -2
+    assert L.ax_gated_experts_backward(R(d), P, P, None, P, P, P, P, P, P, P, P, P, BIG, None) == -2
+    assert L.ax_matmul_q4(R(q4(residual_ld=1, **many)), P, None, P, P, P, None, None, P, P, BIG, None) == -2
+    assert L.ax_gated_q4(R(q4(residual_ld=1, **many)), P, None, P, P, P, P, P, P, P, BIG, None) == -2
