@@ -1431,7 +1431,8 @@ def ax_route(logits, k, normalize=True, experts_out=None, weights_out=None, offs
              workspace=None, stream=None):
     """Each token's k largest logits and the order of its choices by expert.  logits: [tokens, experts].  Returns (experts
     [tokens, k], weights [tokens, k], offsets [experts + 1], rows [tokens, k], tokens [tokens * k]): weights float32, the softmax
-    over the chosen experts (normalize) or over all; the others int32."""
+    over the chosen experts (normalize) or over all; the others int32.  Where none of those for the choices is given they are from one
+    allocation."""
     if stream is not None:
         return _on_stream(ax_route, stream, logits, k, normalize, experts_out, weights_out, offsets_out, rows_out, tokens_out, workspace)
     L = lib()
@@ -1451,6 +1452,9 @@ def ax_route(logits, k, normalize=True, experts_out=None, weights_out=None, offs
         hit = _remember(key, (d, int(L.ax_route_workspace_bytes(d)), logits.shape[:-1] + (d.k,), T * d.k))
     d, need, shape, n = hit
     _current_device(logits)
+    if experts_out is weights_out is rows_out is tokens_out is None:  # (one allocation: for a token or two they are most of a call)
+        experts_out, rows_out, tokens_out, weights_out = logits.new_empty((4,) + shape, dtype=torch.int32).unbind(0)
+        tokens_out, weights_out = tokens_out.view(-1), weights_out.view(torch.float32)
     if experts_out is None:
         experts_out = logits.new_empty(shape, dtype=torch.int32)
     if weights_out is None:
