@@ -93,6 +93,35 @@ def test_serving_in_4_bits(tokens):
     assert near(s.forward(x, r), want) <= 8 * 2.0 ** -8
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_a_batch_of_sequences(dt):
+    """[batch, length, width] gives the bits of its rows."""
+    b, g = _block(F.DT[dt]), F.gen(5)
+    x, gy = (F.randn(g, (3, 7, 96), 1.0, F.DT[dt]).cuda() for _ in range(2))
+    y, flat = b.forward(x, train=True), lambda t: t.view(21, -1)  # noqa: E731
+    gx, grads = b.backward(gy), {k: v.clone() for k, v in b.grads.items()}
+    assert y.shape == gx.shape == x.shape
+    assert torch.equal(flat(y), b.forward(flat(x), train=True)) and torch.equal(flat(gx), b.backward(flat(gy)))
+    assert all(torch.equal(v, b.grads[k]) for k, v in grads.items())
+    q = b.quantized(group=64)
+    assert torch.equal(flat(q.forward(x)), q.forward(flat(x)))
+
+
+def test_two_calls_at_once():
+    """One block's weights, two streams, other tokens and other choices on each."""
+    b, g = _block(torch.bfloat16), F.gen(6)
+    q = b.quantized(group=32)
+    xs = [F.randn(g, (n, 96), 1.0, torch.bfloat16).cuda() for n in (700, 333)]
+    want = [(b.forward(x), q.forward(x)) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    out = [[(b.forward(x, stream=s), q.forward(x, stream=s)) for x, s in zip(xs, streams)] for _ in range(5)]
+    torch.cuda.synchronize()
+    for both in out:
+        for got, w in zip(both, want):
+            assert all(torch.equal(a, e) for a, e in zip(got, w))
+
+
 def test_refused_bits():
     with pytest.raises(ValueError):
         FeedForward(32, 32).quantized(bits=5)
