@@ -406,11 +406,11 @@ struct Plan {
 
 // us at rows / K / N, q4_kernel : q4_tile_kernel : written out.  A few units of 64 rows by 16 columns, or few rows of an expert: the first, which
 // needs none of the others' stages.
-//   256/4096/4096 25 : 42 : 36      300/4096/4096 41 : 42 : 45   700/1000/777 12 : 13     gated 256/4096/4096 42 : 43
-//   8 experts, 2048/1408: 512 rows 20 : 23, 2048 rows 45 : 32    32 experts, 2048 rows 50 : 34   float32 256/4096/4096 79 : 75, 300/4096/4096 97 : 75
+//   256/4096/4096 26 : 43 : 39      350/4096/4096 41 : 43 : 42   gated 256/4096/4096 42 : 43     500/2048/11264 58 : 42 : 47
+//   8 experts, 2048/1408: 512 rows 17 : 23, 4096 rows 68 : 47 : 49   600/1024/3000 17 : 14 : 20  float32 256/4096/4096 74 : 75, 300/4096/4096 97 : 75
 // Many rows of an expert: the weights pay for being written once.
-//   512/4096/4096 43 : 43 : 46      1027/4096/4096 88 : 77 : 65  2048/4096/4096 151 : 87 : 78  8192/4096/4096 626 : 330 : 230
-//   32 experts, 2048/1408: 4096 rows 76 : 47 : 113
+//   512/4096/4096 41 : 42 : 42      600/4096/4096 62 : 58 : 51   1027/4096/4096 86 : 75 : 56     2048/4096/4096 151 : 85 : 75
+//   16 experts, 2048/1408: 4096 rows 64 : 45 : 56
 // float32 is never written out, in pieces: 2048/4096/4096 228, the six products of pieces alone would be 340.
 Way way_of(const ax_q4_desc_t* d, bool gated) {
   const long long used = std::max<long long>(1, std::min<long long>(d->experts, d->rows)), tiles = (d->N + 15) / 16;

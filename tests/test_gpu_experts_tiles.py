@@ -16,16 +16,16 @@ pytestmark = pytest.mark.gpu
 CASES = [
     ("matmul", "bf16", False, False, 131, 2, 1000, 129, 32, 2), ("matmul", "bf16", False, False, 16411, 3, 72, 41, 64, 2),
     ("matmul", "bf16", False, False, 333, 16, 264, 4100, 64, 3), ("matmul", "bf16", False, False, 8197, 64, 136, 523, 128, 2),
-    ("matmul", "bf16", False, False, 8197, 2, 136, 1003, 256, 1),
+    ("matmul", "bf16", False, False, 8197, 2, 136, 1003, 96, 2),
     ("matmul", "bf16", False, True, 131, 2, 1000, 129, 32, 2), ("matmul", "bf16", False, True, 16411, 3, 72, 41, 64, 2),
     ("matmul", "bf16", False, True, 333, 16, 264, 4100, 64, 3), ("matmul", "bf16", False, True, 8197, 64, 136, 523, 128, 2),
-    ("matmul", "bf16", False, True, 8197, 2, 136, 1003, 256, 1),
+    ("matmul", "bf16", False, True, 8197, 2, 136, 1003, 96, 2),
     ("matmul", "bf16", True, False, 131, 2, 1000, 129, 32, 2), ("matmul", "bf16", True, False, 16411, 3, 72, 41, 64, 2),
     ("matmul", "bf16", True, False, 333, 16, 264, 4100, 64, 3), ("matmul", "bf16", True, False, 8197, 64, 136, 523, 128, 2),
-    ("matmul", "bf16", True, False, 8197, 2, 136, 1003, 256, 1),
+    ("matmul", "bf16", True, False, 8197, 2, 136, 1003, 96, 2),
     ("matmul", "bf16", True, True, 131, 2, 1000, 129, 32, 2), ("matmul", "bf16", True, True, 16411, 3, 72, 41, 64, 2),
     ("matmul", "bf16", True, True, 333, 16, 264, 4100, 64, 3), ("matmul", "bf16", True, True, 8197, 64, 136, 523, 128, 2),
-    ("matmul", "bf16", True, True, 8197, 2, 136, 1003, 256, 1),
+    ("matmul", "bf16", True, True, 8197, 2, 136, 1003, 96, 2),
     ("matmul", "f32", False, False, 131, 2, 520, 129, 64, 2), ("matmul", "f32", True, False, 131, 2, 520, 129, 64, 2),
     ("matmul", "f32", True, False, 16411, 2, 265, 43, 128, 1),
     ("gated", "bf16", False, False, 131, 2, 1000, 129, 32, 2), ("gated", "bf16", False, False, 16411, 3, 72, 41, 64, 2),
@@ -36,15 +36,15 @@ CASES = [
     ("gated", "bf16", False, True, 1531, 2, 136, 4100, 256, 1), ("gated", "f32", False, False, 131, 2, 520, 129, 64, 2),
     ("matmul_gx", "bf16", False, False, 131, 2, 129, 1003, 32, 2), ("matmul_gx", "bf16", False, False, 16411, 3, 41, 72, 64, 2),
     ("matmul_gx", "bf16", False, False, 67, 33, 2049, 264, 64, 3), ("matmul_gx", "bf16", False, False, 8197, 64, 523, 137, 128, 2),
-    ("matmul_gx", "bf16", False, False, 8197, 2, 1003, 136, 256, 1),
+    ("matmul_gx", "bf16", False, False, 8197, 2, 1003, 136, 96, 2),
     ("matmul_gx", "bf16", True, False, 131, 2, 129, 1003, 32, 2), ("matmul_gx", "bf16", True, False, 16411, 3, 41, 72, 64, 2),
     ("matmul_gx", "bf16", True, False, 67, 33, 2049, 264, 64, 3), ("matmul_gx", "bf16", True, False, 8197, 64, 523, 137, 128, 2),
-    ("matmul_gx", "bf16", True, False, 8197, 2, 1003, 136, 256, 1),
+    ("matmul_gx", "bf16", True, False, 8197, 2, 1003, 136, 96, 2),
     ("matmul_gx", "f32", False, False, 131, 2, 129, 520, 64, 2), ("matmul_gx", "f32", False, False, 16411, 2, 43, 265, 128, 1),
     ("matmul_gx", "f32", True, False, 131, 2, 129, 520, 64, 2),
     ("gated_gx", "bf16", False, False, 131, 2, 129, 1003, 32, 2), ("gated_gx", "bf16", False, False, 16411, 3, 41, 72, 64, 2),
     ("gated_gx", "bf16", False, False, 67, 33, 2049, 41, 64, 3), ("gated_gx", "bf16", False, False, 8197, 64, 523, 137, 128, 2),
-    ("gated_gx", "bf16", False, False, 8197, 2, 1003, 136, 256, 1),
+    ("gated_gx", "bf16", False, False, 8197, 2, 1003, 136, 96, 2),
     ("gated_gx", "f32", False, False, 131, 2, 129, 520, 64, 2), ("gated_gx", "f32", False, False, 16411, 2, 43, 265, 128, 1),
     ("matmul_gw", "bf16", False, False, 133, 2, 43, 41, 64, 2), ("matmul_gw", "bf16", False, False, 131, 64, 523, 41, 128, 2),
     ("matmul_gw", "bf16", False, False, 133, 33, 41, 2049, 128, 3), ("matmul_gw", "bf16", False, False, 700, 64, 1003, 129, 256, 1),
@@ -54,6 +54,11 @@ CASES = [
     ("gated_gw", "bf16", False, False, 133, 2, 43, 41, 64, 2), ("gated_gw", "bf16", False, False, 131, 33, 523, 41, 128, 2),
     ("gated_gw", "bf16", False, False, 133, 64, 41, 523, 128, 3), ("gated_gw", "bf16", False, False, 333, 8, 1003, 1003, 256, 1),
     ("gated_gw", "f32", False, False, 333, 3, 131, 131, 64, 2),
+    ("matmul", "bf16", False, False, 16411, 2, 136, 521, 256, 1), ("matmul", "bf16", False, True, 16411, 2, 136, 521, 256, 1),
+    ("matmul_gx", "bf16", False, False, 16411, 2, 521, 136, 256, 1), ("matmul", "bf16", True, False, 16411, 2, 136, 521, 256, 1),
+    ("matmul", "bf16", True, True, 16411, 2, 136, 521, 256, 1), ("matmul_gx", "bf16", True, False, 16411, 2, 521, 136, 256, 1),
+    ("gated_gx", "bf16", False, False, 16411, 2, 521, 72, 256, 1), ("gated", "bf16", False, False, 1027, 2, 136, 4100, 96, 2),
+    ("gated", "bf16", False, True, 1027, 2, 136, 4100, 96, 2),
 ]
 # (gated, type, rows, experts, K, N, kernel, its rows, its columns, its waves)
 Q4_CASES = [
@@ -64,7 +69,7 @@ Q4_CASES = [
     (False, "bf16", 257, 2, 300, 2049, "few", 64, 64, 4), (False, "bf16", 131, 2, 300, 4099, "tiles", 32, 256, 0),
     (False, "bf16", 4099, 8, 300, 265, "tiles", 64, 256, 0), (False, "bf16", 1531, 1, 300, 4099, "written", 128, 128, 0),
     (False, "bf16", 1531, 1, 300, 8203, "written", 256, 256, 0), (False, "bf16", 1301, 2, 300, 1003, "written", 32, 128, 0),
-    (False, "bf16", 2051, 1, 300, 1003, "written", 64, 128, 0),
+    (False, "bf16", 2051, 1, 300, 1003, "written", 96, 128, 0), (False, "bf16", 8197, 1, 300, 265, "written", 64, 128, 0),
     (False, "f32", 3, 1, 4107, 41, "few", 16, 16, 16), (False, "f32", 5, 2, 300, 41, "few", 16, 16, 8),
     (False, "f32", 3, 1, 300, 8203, "few", 16, 32, 8), (False, "f32", 33, 33, 300, 1003, "few", 16, 64, 8),
     (False, "f32", 33, 2, 300, 41, "few", 32, 16, 8), (False, "f32", 2051, 64, 300, 41, "few", 32, 32, 8),
@@ -75,7 +80,8 @@ Q4_CASES = [
     (True, "bf16", 67, 2, 300, 41, "few", 64, 16, 8), (True, "bf16", 4099, 64, 300, 41, "few", 64, 32, 8),
     (True, "bf16", 131, 2, 300, 2049, "tiles", 32, 128, 0), (True, "bf16", 4099, 8, 300, 131, "tiles", 64, 128, 0),
     (True, "bf16", 1531, 1, 300, 2049, "written", 128, 128, 0), (True, "bf16", 1531, 1, 300, 4099, "written", 256, 256, 0),
-    (True, "bf16", 1301, 2, 300, 523, "written", 32, 128, 0), (True, "bf16", 1301, 2, 300, 1003, "written", 64, 128, 0),
+    (True, "bf16", 1301, 2, 300, 523, "written", 32, 128, 0), (True, "bf16", 1301, 2, 300, 1003, "written", 96, 128, 0),
+    (True, "bf16", 8197, 1, 300, 131, "written", 64, 128, 0),
     (True, "f32", 3, 1, 4107, 41, "few", 16, 16, 16), (True, "f32", 5, 2, 300, 41, "few", 16, 16, 8),
     (True, "f32", 3, 1, 300, 8203, "few", 16, 32, 8), (True, "f32", 33, 2, 300, 41, "few", 32, 16, 8),
     (True, "f32", 2051, 64, 300, 41, "few", 32, 32, 8), (True, "f32", 131, 2, 300, 2049, "tiles", 32, 128, 0),
