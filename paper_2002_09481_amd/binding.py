@@ -348,17 +348,18 @@ def _stream_ptr(stream) -> int:
     return int(stream.cuda_stream)
 
 
-def _on_stream(call, stream, *args):
+def _on_stream(call, stream, *args, held=()):
     """call(*args) on `stream`, which is not None: what it allocates comes from that stream's pool, whose blocks are free in
     that stream's order (one of the current stream's pool may have been freed with kernels still running there).  torch hands
     a block on when its tensor dies, so the tensors that the call takes are tied to `stream`, and its results to the stream
-    that was current as well, where they will be used."""
+    that was current as well, where they will be used.  held: what the call uses besides its arguments, tensors of the object
+    that it is a method of, which may be dropped with work under way as well."""
     before = torch.cuda.current_stream(stream.device)
     with torch.cuda.stream(stream):
         try:
             out = call(*args)
         finally:  # (a call that fails at its second launch has enqueued the first)
-            for t in _tensors_of(args):
+            for t in _tensors_of((args, held)):
                 if t.is_cuda:
                     t.record_stream(stream)
     for t in _tensors_of(out if isinstance(out, tuple) else (out,)):
@@ -367,12 +368,14 @@ def _on_stream(call, stream, *args):
 
 
 def _tensors_of(things):
-    for t in things:
+    for t in things.values() if isinstance(things, dict) else things:
         if isinstance(t, torch.Tensor):
             yield t
         elif isinstance(t, AxQ4):
             yield t.codes
             yield t.scales
+        elif isinstance(t, (tuple, list, dict)):
+            yield from _tensors_of(t)
 
 
 def _ptr(t: Optional[torch.Tensor]):

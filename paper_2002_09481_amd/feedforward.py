@@ -56,7 +56,7 @@ class FeedForward:
         """y [rows, width]; with train, what backward needs is kept until it is called, in the place of what an earlier pass
         left."""
         if stream is not None:
-            return ax._on_stream(self.forward, stream, x, residual, train)
+            return ax._on_stream(self.forward, stream, x, residual, train, held=(self.params,))
         p = self.params
         n, t, rstd = ax.ax_rmsnorm(x, p["norm"], residual=residual, eps=self.eps, rstd_out=None if train else False)
         t = x if t is None else t
@@ -69,7 +69,7 @@ class FeedForward:
     def backward(self, gy, stream=None):
         """The gradient of x (and of the residual); those of the parameters are left in self.grads."""
         if stream is not None:
-            return ax._on_stream(self.backward, stream, gy)
+            return ax._on_stream(self.backward, stream, gy, held=(self.params, self.grads))
         if self._kept is None:
             raise RuntimeError("backward needs a forward pass with train=True first")
         n, t, rstd, h, g, u = kept = self._kept
@@ -111,7 +111,7 @@ class QuantizedFeedForward:
 
     def forward(self, x, residual=None, stream=None):
         if stream is not None:
-            return ax._on_stream(self.forward, stream, x, residual)
+            return ax._on_stream(self.forward, stream, x, residual, held=(self.norm, self.bias, self.w))
         if self.bits == 4:
             n, t, _ = ax.ax_rmsnorm(x, self.norm, residual=residual, eps=self.eps, rstd_out=False)
             h = ax.ax_gated_q4(n, self.w["wg"], self.w["wu"], act=self.act)
@@ -152,7 +152,7 @@ class ExpertsFeedForward:
         """y [tokens, width]; with train, what backward needs is kept until it is called, in the place of what an earlier pass
         left."""
         if stream is not None:
-            return ax._on_stream(self.forward, stream, x, residual, train)
+            return ax._on_stream(self.forward, stream, x, residual, train, held=(self.params,))
         p = self.params
         n, t, rstd = ax.ax_rmsnorm(x, p["norm"], residual=residual, eps=self.eps, rstd_out=None if train else False)
         t = x if t is None else t
@@ -168,7 +168,7 @@ class ExpertsFeedForward:
     def backward(self, gy, stream=None):
         """The gradient of x (and of the residual); those of the parameters are left in self.grads."""
         if stream is not None:
-            return ax._on_stream(self.backward, stream, gy)
+            return ax._on_stream(self.backward, stream, gy, held=(self.params, self.grads))
         if self._kept is None:
             raise RuntimeError("backward needs a forward pass with train=True first")
         n, t, rstd, logits, experts, weights, offsets, rows, tokens, h, g, u, d = kept = self._kept
@@ -211,7 +211,7 @@ class QuantizedExperts:
 
     def forward(self, x, residual=None, stream=None):
         if stream is not None:
-            return ax._on_stream(self.forward, stream, x, residual)
+            return ax._on_stream(self.forward, stream, x, residual, held=(self.norm, self.router, self.w))
         n, t, _ = ax.ax_rmsnorm(x, self.norm, residual=residual, eps=self.eps, rstd_out=False)
         logits, _ = ax.ax_matmul(n, self.router, out_dtype=torch.float32)
         _, weights, offsets, rows, tokens = ax.ax_route(logits, self.k, normalize=self.normalize)

@@ -1,0 +1,63 @@
+"""Objects that are dropped while another stream still has to read what they hold: the memory must not be handed out before."""
+
+import pytest
+import torch
+
+import ff_common as F
+from paper_2002_09481_amd.feedforward import ExpertsFeedForward, FeedForward
+
+pytestmark = pytest.mark.gpu
+
+BUSY = 40_000_000  # cycles that the other stream is held: tens of milliseconds
+
+
+def _dropped(make, use):
+    """use(make(), stream) with what was made dropped at once; returns the results, after the current stream has filled whatever memory
+    of those sizes it gets."""
+    s = torch.cuda.Stream()
+    held, shapes = make()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(BUSY)
+    out = use(held, s)
+    del held
+    junk = [torch.full(sh, 7, dtype=d, device="cuda") for sh, d in shapes for _ in range(2)]
+    torch.cuda.synchronize()
+    assert all(bool((j == 7).all()) for j in junk)
+    return out
+
+
+def _tensors(b):
+    w = [t for v in b.w.values() for t in ((v.codes, v.scales) if hasattr(v, "codes") else v)]
+    return [(t.shape, t.dtype) for t in w]
+
+
+@pytest.mark.parametrize("kind", [8, 4, "experts"])
+def test_served_block_is_dropped(kind):
+    g = F.gen(11)
+    b = ExpertsFeedForward(256, 512, 4, 2, seed=1) if kind == "experts" else FeedForward(256, 1024, seed=1)
+    x = F.randn(g, (40, 256), 1.0, torch.bfloat16).cuda()
+    laid = lambda: b.quantized() if kind == "experts" else b.quantized(bits=kind)  # noqa: E731
+    want = laid().forward(x)
+
+    def make():
+        q = laid()
+        return q, _tensors(q)
+
+    assert torch.equal(_dropped(make, lambda q, s: q.forward(x, stream=s)), want)
+
+
+@pytest.mark.parametrize("experts", [False, True])
+def test_trained_block_is_dropped(experts):
+    g = F.gen(12)
+    new = lambda: ExpertsFeedForward(256, 512, 4, 2, seed=2) if experts else FeedForward(256, 1024, seed=2)  # noqa: E731
+    x, gy = (F.randn(g, (300, 256), 1.0, torch.bfloat16).cuda() for _ in range(2))
+    b = new()
+    want = b.forward(x, train=True), b.backward(gy)
+
+    def make():
+        b = new()
+        return b, [(t.shape, t.dtype) for d in (b.params, b.grads, b.master) for t in d.values()]
+
+    got = _dropped(make, lambda b, s: (b.forward(x, train=True, stream=s), b.backward(gy, stream=s)))
+    assert all(torch.equal(a, c) for a, c in zip(got, want))

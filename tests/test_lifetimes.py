@@ -1,0 +1,62 @@
+"""What objects hold and use on another stream than the current one, on the host: it is tied to that stream, since the object may be
+dropped with the work under way."""
+
+import pytest
+import torch
+
+from paper_2002_09481_amd import binding as ax
+from paper_2002_09481_amd.feedforward import ExpertsFeedForward, FeedForward, QuantizedExperts, QuantizedFeedForward
+from test_experts_marshalling import f32, notes, weights4, whole  # noqa: F401
+from test_feedforward_marshalling import Streams, codes
+
+
+def _block(cls, weights, kept=()):
+    b = cls.__new__(cls)
+    b.act, b.dtype, b.eps, b.k, b.normalize, b._kept = "silu", torch.float32, 1e-5, 2, True, kept
+    b.params = {n: f32(*s) for n, s in weights.items()}
+    b.grads = {n: f32(*s) for n, s in weights.items()}
+    return b
+
+
+def _plain():
+    return _block(FeedForward, {"wg": (16, 24), "wu": (16, 24), "wd": (24, 16), "norm": (16,), "bias": (16,)},
+                  (f32(4, 16), f32(4, 16), f32(4), f32(4, 24), f32(4, 24), f32(4, 24)))
+
+
+def _experts():
+    return _block(ExpertsFeedForward, {"router": (16, 3), "wg": (3, 16, 24), "wu": (3, 16, 24), "wd": (3, 24, 16), "norm": (16,)},
+                  (f32(4, 16), f32(4, 16), f32(4), f32(4, 3), whole(4, 2), f32(4, 2), whole(4), whole(4, 2), whole(8), f32(8, 24), f32(8, 24),
+                   f32(8, 24), f32(8, 16)))
+
+
+def _served(kind):
+    b = (QuantizedExperts if kind == "experts" else QuantizedFeedForward).__new__(QuantizedExperts if kind == "experts" else QuantizedFeedForward)
+    b.act, b.eps, b.dtype, b.k, b.normalize, b.norm = "silu", 1e-5, torch.float32, 2, True, f32(16)
+    if kind == "experts":
+        b.router, b.w = f32(16, 3), {"wg": weights4(3), "wu": weights4(3), "wd": weights4(3)}
+        return b, [b.norm, b.router]
+    b.bits, b.bias = kind, f32(16)
+    b.w = {n: weights4() if kind == 4 else (codes(16, 16), f32(16)) for n in ("wg", "wu", "wd")}
+    return b, [b.norm, b.bias]
+
+
+def _tied(s, tensors):
+    return all((t.data_ptr(), s.side) in s.ties for t in tensors)
+
+
+@pytest.mark.parametrize("make", [_plain, _experts])
+def test_parameters_and_gradients_of_a_block(notes, monkeypatch, make):  # noqa: F811
+    b, s = make(), Streams(monkeypatch)
+    b.forward(f32(4, 16), stream=s.side)
+    assert _tied(s, b.params.values()) and not _tied(s, b.grads.values())
+    s.ties.clear()
+    b.backward(f32(4, 16), stream=s.side)
+    assert _tied(s, b.params.values()) and _tied(s, b.grads.values())
+
+
+@pytest.mark.parametrize("kind", [8, 4, "experts"])
+def test_weights_of_a_served_block(notes, monkeypatch, kind):  # noqa: F811
+    (b, vectors), s = _served(kind), Streams(monkeypatch)
+    b.forward(f32(4, 16), stream=s.side)
+    held = [t for w in b.w.values() for t in ((w.codes, w.scales) if isinstance(w, ax.AxQ4) else w)]
+    assert len(held) == 6 and _tied(s, vectors + held)
