@@ -21,7 +21,6 @@ with the rows of the choices grouped by expert between the router and the sum.
 
 from __future__ import annotations
 
-import contextlib
 import math
 
 import torch
@@ -94,6 +93,11 @@ class FeedForward:
         return QuantizedFeedForward(self, stream=stream, bits=bits, group=group)
 
 
+def _reading(block, stream, call):
+    """call(), which reads the block's parameters, on `stream`."""
+    return call() if stream is None else ax._on_stream(call, stream, held=(block.params, block.master))
+
+
 class QuantizedFeedForward:
     """The block on int8 codes (bits = 8), or with weights of 4 bits (4: a scale for every `group` inputs); forward only.  The
     residual stream keeps the block's type."""
@@ -102,12 +106,15 @@ class QuantizedFeedForward:
         if bits not in (8, 4):
             raise ValueError("bits must be 8 or 4")
         self.act, self.eps, self.dtype, self.bits = block.act, block.eps, block.dtype, bits
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            self.norm, self.bias = block.params["norm"].clone(), block.params["bias"].clone()
-            self.w = {}
+
+        def lay_out():
+            w = {}
             for name in ("wg", "wu", "wd"):  # [inputs, outputs] -> codes [outputs, inputs], a scale an output (or group)
-                w = block.master[name].t().contiguous()
-                self.w[name] = ax.ax_quantize_q4(w, group=group) if bits == 4 else ax.ax_rmsnorm_q8(w, normalize=False)[:2]
+                t = block.master[name].t().contiguous()
+                w[name] = ax.ax_quantize_q4(t, group=group) if bits == 4 else ax.ax_rmsnorm_q8(t, normalize=False)[:2]
+            return block.params["norm"].clone(), block.params["bias"].clone(), w
+
+        self.norm, self.bias, self.w = _reading(block, stream, lay_out)
 
     def forward(self, x, residual=None, stream=None):
         if stream is not None:
@@ -205,9 +212,12 @@ class QuantizedExperts:
 
     def __init__(self, block: ExpertsFeedForward, stream=None, group=128):
         self.act, self.eps, self.dtype, self.k, self.normalize = block.act, block.eps, block.dtype, block.k, block.normalize
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            self.norm, self.router = block.params["norm"].clone(), block.params["router"].clone()
-            self.w = {name: ax.ax_quantize_q4(block.master[name].transpose(1, 2).contiguous(), group=group) for name in ("wg", "wu", "wd")}
+
+        def lay_out():
+            w = {name: ax.ax_quantize_q4(block.master[name].transpose(1, 2).contiguous(), group=group) for name in ("wg", "wu", "wd")}
+            return block.params["norm"].clone(), block.params["router"].clone(), w
+
+        self.norm, self.router, self.w = _reading(block, stream, lay_out)
 
     def forward(self, x, residual=None, stream=None):
         if stream is not None:

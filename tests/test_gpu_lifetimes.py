@@ -11,10 +11,10 @@ pytestmark = pytest.mark.gpu
 BUSY = 40_000_000  # cycles that the other stream is held: tens of milliseconds
 
 
-def _dropped(make, use):
+def _dropped(make, use, s=None):
     """use(make(), stream) with what was made dropped at once; returns the results, after the current stream has filled whatever memory
     of those sizes it gets."""
-    s = torch.cuda.Stream()
+    s = s or torch.cuda.Stream()
     held, shapes = make()
     torch.cuda.synchronize()
     with torch.cuda.stream(s):
@@ -61,3 +61,28 @@ def test_trained_block_is_dropped(experts):
 
     got = _dropped(make, lambda b, s: (b.forward(x, train=True, stream=s), b.backward(gy, stream=s)))
     assert all(torch.equal(a, c) for a, c in zip(got, want))
+
+
+@pytest.mark.parametrize("kind", [8, 4, "experts"])
+def test_block_is_dropped_after_its_weights_are_laid_out(kind):
+    """The masters die with the block that they are laid out from; what is made on the other stream is used and dropped on this one."""
+    g = F.gen(13)
+    new = lambda: ExpertsFeedForward(256, 512, 4, 2, seed=3) if kind == "experts" else FeedForward(256, 1024, seed=3)  # noqa: E731
+    laid = lambda b, s: b.quantized(stream=s) if kind == "experts" else b.quantized(stream=s, bits=kind)  # noqa: E731
+    x = F.randn(g, (40, 256), 1.0, torch.bfloat16).cuda()
+    want = laid(new(), None).forward(x)
+
+    def make():
+        b = new()
+        return b, [(t.shape, t.dtype) for d in (b.params, b.master) for t in d.values()]
+
+    s = torch.cuda.Stream()
+    q = _dropped(make, laid, s)
+    shapes = _tensors(q)
+    torch.cuda._sleep(BUSY)
+    y = q.forward(x)
+    del q
+    with torch.cuda.stream(s):
+        junk = [torch.full(sh, 7, dtype=d, device="cuda") for sh, d in shapes for _ in range(2)]
+    torch.cuda.synchronize()
+    assert torch.equal(y, want) and all(bool((j == 7).all()) for j in junk)

@@ -60,3 +60,16 @@ def test_weights_of_a_served_block(notes, monkeypatch, kind):  # noqa: F811
     b.forward(f32(4, 16), stream=s.side)
     held = [t for w in b.w.values() for t in ((w.codes, w.scales) if isinstance(w, ax.AxQ4) else w)]
     assert len(held) == 6 and _tied(s, vectors + held)
+
+
+@pytest.mark.parametrize("kind", [8, 4, "experts"])
+def test_weights_laid_out_on_another_stream(notes, monkeypatch, kind):  # noqa: F811
+    """What is read belongs to the block, what is made to whoever uses it next."""
+    b = _experts() if kind == "experts" else _plain()
+    b.master = {n: f32(*t.shape) for n, t in b.params.items()}
+    s = Streams(monkeypatch)
+    q = b.quantized(stream=s.side) if kind == "experts" else b.quantized(stream=s.side, bits=kind)
+    assert _tied(s, [b.master[n] for n in ("wg", "wu", "wd")] + [b.params[n] for n in (("norm", "router") if kind == "experts" else ("norm", "bias"))])
+    made = [q.norm, q.router if kind == "experts" else q.bias]
+    made += [t for w in q.w.values() for t in ((w.codes, w.scales) if isinstance(w, ax.AxQ4) else w)]
+    assert len(made) == 8 and all((t.data_ptr(), s.main) in s.ties for t in made) and s.current == [s.main]
