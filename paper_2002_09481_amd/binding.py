@@ -1892,6 +1892,7 @@ class AxAdamW:
     The tensors are held, and their addresses used, until the object is dropped; set_grads exchanges the gradients."""
 
     def __init__(self, params, grads, m=None, v=None, m_scales=None, v_scales=None, copies=None, bits=32):
+        self._streams = set()  # that steps were enqueued on
         self.params, self.copies = list(params), None if copies is None else list(copies)
         n = len(self.params)
         if not n:
@@ -1941,6 +1942,18 @@ class AxAdamW:
             self._whole += -(-k // 64) * 64
         self.set_grads(grads)
 
+    def _held(self):
+        return self.params, self.m, self.v, self.m_scales or (), self.v_scales or (), self.copies or ()
+
+    def __del__(self):
+        # (tied here, not in every step: hundreds of tensors, and until now nobody could drop the last of any)
+        try:
+            for s in self._streams:
+                for t in _tensors_of(self._held()):
+                    t.record_stream(s)
+        except Exception:  # interpreter shutdown: the module's globals may be gone
+            pass
+
     def set_grads(self, grads):
         grads = list(grads)
         if len(grads) != len(self.params):
@@ -1964,6 +1977,7 @@ class AxAdamW:
         if stream is not None:  # (the gradients may be exchanged, and the factor dropped, before the step has run)
             for t in self.grads if grad_scale is None else self.grads + [grad_scale]:
                 t.record_stream(stream)
+            self._streams.add(stream)
         _check(lib().ax_adamw(d, self._t, len(self._t), _stream_ptr(stream)))
 
     def states(self, stream=None):
@@ -1971,7 +1985,7 @@ class AxAdamW:
         for v), or the 32-bit states themselves."""
         if self.bits == 32:
             return self.m, self.v
-        bufs = self._states() if stream is None else _on_stream(self._states, stream)
+        bufs = self._states() if stream is None else _on_stream(self._states, stream, held=self._held())
         m, v = ([b.as_strided(*place) for place in self._places] for b in bufs)
         return m, v
 

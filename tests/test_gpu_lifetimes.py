@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import ff_common as F
+from paper_2002_09481_amd import binding as ax
 from paper_2002_09481_amd.feedforward import ExpertsFeedForward, FeedForward
 
 pytestmark = pytest.mark.gpu
@@ -86,3 +87,32 @@ def test_block_is_dropped_after_its_weights_are_laid_out(kind):
         junk = [torch.full(sh, 7, dtype=d, device="cuda") for sh, d in shapes for _ in range(2)]
     torch.cuda.synchronize()
     assert torch.equal(y, want) and all(bool((j == 7).all()) for j in junk)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_optimizer_is_dropped(bits):
+    """Parameters and states die with the optimizer, right after a step; the copies are what is looked at."""
+    g = F.gen(14)
+    p, gr = F.randn(g, (1 << 20,)).cuda(), F.randn(g, (1 << 20,)).cuda()
+    copy = torch.zeros(1 << 20, dtype=torch.bfloat16, device="cuda")
+
+    def make():
+        opt = ax.AxAdamW([p.clone()], [gr], copies=[copy], bits=bits)
+        return opt, [(t.shape, t.dtype) for t in opt.params + opt.m + opt.v + (opt.m_scales or []) + (opt.v_scales or [])]
+
+    make()[0].step(1e-2, 1, weight_decay=0.1)
+    want = copy.clone()
+    copy.zero_()
+    _dropped(make, lambda opt, s: opt.step(1e-2, 1, weight_decay=0.1, stream=s))
+    assert torch.equal(copy, want)
+    opt = make()[0]
+    opt.step(1e-2, 1)
+    want = [t.clone() for t in opt.states()[1]]
+
+    def stepped():
+        opt, shapes = make()
+        opt.step(1e-2, 1)
+        return opt, shapes
+
+    if bits == 8:
+        assert torch.equal(_dropped(stepped, lambda opt, s: opt.states(stream=s))[1][0], want[0])

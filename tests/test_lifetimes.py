@@ -7,7 +7,7 @@ import torch
 from paper_2002_09481_amd import binding as ax
 from paper_2002_09481_amd.feedforward import ExpertsFeedForward, FeedForward, QuantizedExperts, QuantizedFeedForward
 from test_experts_marshalling import f32, notes, weights4, whole  # noqa: F401
-from test_feedforward_marshalling import Streams, codes
+from test_feedforward_marshalling import Streams, codes, placed
 
 
 def _block(cls, weights, kept=()):
@@ -73,3 +73,27 @@ def test_weights_laid_out_on_another_stream(notes, monkeypatch, kind):  # noqa: 
     made = [q.norm, q.router if kind == "experts" else q.bias]
     made += [t for w in q.w.values() for t in ((w.codes, w.scales) if isinstance(w, ax.AxQ4) else w)]
     assert len(made) == 8 and all((t.data_ptr(), s.main) in s.ties for t in made) and s.current == [s.main]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_parameters_and_states_of_an_optimizer(notes, monkeypatch, bits):  # noqa: F811
+    """A step's are tied when the optimizer, which holds them, is dropped; those that states() reads in the call."""
+    p, g, copy = f32(16), f32(16), placed(torch.zeros(16, dtype=torch.bfloat16))
+    m, v = (codes(16), placed(torch.zeros(16, dtype=torch.uint8))) if bits == 8 else (f32(16), f32(16))
+    scales = [f32(1), f32(1)] if bits == 8 else []
+    opt = ax.AxAdamW([p], [g], [m], [v], *([t] for t in scales), copies=[copy])
+    s = Streams(monkeypatch)
+    if bits == 8:
+        opt.states(stream=s.side)
+        assert _tied(s, [m, v] + scales)
+        s.ties.clear()
+    opt.step(1e-3, 1, stream=s.side)
+    opt.step(1e-3, 2)
+    assert _tied(s, [g])
+    del opt
+    assert _tied(s, [p, m, v, copy] + scales) and not [t for t, where in s.ties if where is not s.side]
+    s.ties.clear()
+    opt = ax.AxAdamW([p], [g], [m], [v], *([t] for t in scales), copies=[copy])
+    opt.step(1e-3, 1)
+    del opt
+    assert not s.ties
