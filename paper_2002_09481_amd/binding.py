@@ -728,6 +728,9 @@ class AxLayer:
         self._keep = (w, luts, prepared)
         return prepared
 
+    def _held(self):
+        return (self._keep or ()) + (self._ws,)
+
     def _args(self, x, acc_out, y_out, workspace):
         cdt = torch.int8 if self.desc.signed_codes else torch.uint8
         _dev(x, cdt, "x")
@@ -741,9 +744,10 @@ class AxLayer:
 
     def run(self, x, acc_out=None, y_out=None, workspace=None, stream=None):
         if stream is not None:
-            out = _on_stream(self.run, stream, x, acc_out, y_out, workspace)
-            if workspace is None:
-                self._ws.record_stream(stream)
+            out = _on_stream(self.run, stream, x, acc_out, y_out, workspace, held=self._held())
+            if workspace is None:  # (of the pool of the first stream that runs the layer, this one or the current one among them)
+                for s in (stream, torch.cuda.current_stream(stream.device)):
+                    self._ws.record_stream(s)
             return out
         acc_out, y_out, workspace = self._args(x, acc_out, y_out, workspace)
         _check(lib().ax_layer_run(self._h, _ptr(x), _ptr(None if acc_out is False else acc_out),
@@ -755,7 +759,7 @@ class AxLayer:
         """ax_layer_run_static: scratch from the library's static device array; nothing is
         allocated, so the outputs must be handed in (False skips one of them)."""
         if stream is not None:
-            return _on_stream(self.run_static, stream, x, acc_out, y_out)
+            return _on_stream(self.run_static, stream, x, acc_out, y_out, held=self._held())
         cdt = torch.int8 if self.desc.signed_codes else torch.uint8
         _dev(x, cdt, "x")
         if acc_out is None or y_out is None:
@@ -769,7 +773,7 @@ class AxLayer:
     def kernel_ms(self, x, acc_out=None, y_out=None, workspace=None, reps: int = 8, stream=None) -> float:
         """ax_probe_layer_kernel_ms: duration of one launch of the layer's main kernel."""
         if stream is not None:
-            return _on_stream(self.kernel_ms, stream, x, acc_out, y_out, workspace, reps)
+            return _on_stream(self.kernel_ms, stream, x, acc_out, y_out, workspace, reps, held=self._held())
         acc_out, y_out, workspace = self._args(x, acc_out, y_out, workspace)
         ms = ctypes.c_float(0.0)
         _check(lib().ax_probe_layer_kernel_ms(self._h, _ptr(x), _ptr(None if acc_out is False else acc_out),

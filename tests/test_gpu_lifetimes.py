@@ -5,6 +5,7 @@ import torch
 
 import ff_common as F
 from paper_2002_09481_amd import binding as ax
+from paper_2002_09481_amd import inputs as I
 from paper_2002_09481_amd.feedforward import ExpertsFeedForward, FeedForward
 
 pytestmark = pytest.mark.gpu
@@ -116,3 +117,19 @@ def test_optimizer_is_dropped(bits):
 
     if bits == 8:
         assert torch.equal(_dropped(stepped, lambda opt, s: opt.states(stream=s))[1][0], want[0])
+
+
+def test_lookup_layer_is_dropped():
+    layer = I.Layer("drop", 4, 28, 28, 64, 3, 3, 72, 1, 1, x_dist="relu", w_dist="normal")
+    x, w, q = I.make_operands(layer, 15)
+    lut, desc = I.lut_truncated(4), ax._conv_desc(x.shape, w.shape, 1, 1)
+    xd = torch.from_numpy(x).cuda()
+
+    def make():
+        h = ax.AxLayer(desc, q)
+        p = h.prepare(torch.from_numpy(w).cuda(), ax.lut_to_device(lut))
+        return h, [(p.shape, p.dtype), (w.shape, torch.uint8), ((65536,), torch.int16)]
+
+    want = make()[0].run(xd)
+    got = _dropped(make, lambda h, s: h.run(xd, stream=s))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

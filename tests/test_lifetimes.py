@@ -97,3 +97,18 @@ def test_parameters_and_states_of_an_optimizer(notes, monkeypatch, bits):  # noq
     opt.step(1e-3, 1)
     del opt
     assert not s.ties
+
+
+def test_what_a_lookup_layer_was_prepared_from(notes, monkeypatch):  # noqa: F811
+    """Filters, tables and the prepared block are tied to each stream that runs the layer, its workspace to the current one too."""
+    u8 = lambda *s: placed(torch.zeros(s, dtype=torch.uint8))  # noqa: E731
+    w, luts, x, acc, y = u8(3, 3, 16, 16), placed(torch.zeros(65536, dtype=torch.int16)), u8(1, 8, 8, 16), whole(1, 8, 8, 16), f32(1, 8, 8, 16)
+    layer = ax.AxLayer(ax.ax_conv_desc_t(1, 8, 8, 16, 3, 3, 16, 1, 1, 1, 1, 1, 1, 0, 0), ax.ax_quant_t(1.0, 0, 1.0, 0, -1))
+    prepared = placed(layer.prepare(w, luts, prepared=u8(512)))
+    s = Streams(monkeypatch)
+    for call in (lambda: layer.run(x, stream=s.side), lambda: layer.run_static(x, acc, y, stream=s.side), lambda: layer.kernel_ms(x, stream=s.side)):
+        s.ties.clear()
+        call()
+        assert _tied(s, [w, luts, prepared])
+    layer.run(x, stream=s.side)
+    assert _tied(s, [layer._ws]) and (layer._ws.data_ptr(), s.main) in s.ties
