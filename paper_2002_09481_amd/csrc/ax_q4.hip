@@ -69,7 +69,9 @@ struct Args {
 };
 
 // Eight float32 values in three pieces of bf16, cut instead of rounded: all products of the pieces with a code are taken, so their sum is
-// exact either way, and cutting is a quarter of the instructions.  (An infinity leaves a NaN in the later pieces.)
+// exact either way, and cutting is a quarter of the instructions.  An infinity is its first piece alone, so that it comes out as the product
+// of a float32 infinity does; a NaN is in one of them.  (Float32 calls take 2 to 10 % longer for it, 1/4096/4096 8.5 us instead of 7.7; with
+// a branch on all eight values 10 to 40 %.)
 __device__ __forceinline__ void cut_in_pieces(const float (&v)[8], u32x4 (&p)[3]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -80,6 +82,10 @@ __device__ __forceinline__ void cut_in_pieces(const float (&v)[8], u32x4 (&p)[3]
       if (k < 2) {
         lo -= __uint_as_float(__float_as_uint(lo) & 0xffff0000u);
         hi -= __uint_as_float(__float_as_uint(hi) & 0xffff0000u);
+        if (k == 0) {
+          lo = __builtin_isinf(v[2 * i]) ? 0.f : lo;
+          hi = __builtin_isinf(v[2 * i + 1]) ? 0.f : hi;
+        }
       }
     }
   }
