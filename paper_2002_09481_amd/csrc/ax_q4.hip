@@ -457,9 +457,11 @@ Plan make_plan(const ax_q4_desc_t* d, bool gated, const void* x, const int32_t* 
 // A workgroup's columns, 16, 32 or 64 of them: as many as leave work for two thirds of the compute units, since each reads all
 // rows of x (us with 16 / 32 / 64: 64/2048/11264 26 / 23 / 18, 64/4096/4096 18 / 19 / 24, 256/4096/4096 61 / 36 / 25).  float32 pays for the
 // pieces of x in each workgroup as well: 68 rows of 16 experts, 1024/4096 30 / 21 / 17, gated 32 experts, 2048/1409 55 / 53 / 50, 8 experts,
-// 2048/4096 30 / 25 / 27.  Its waves: 16 where there are few workgroups and many blocks (1/4096/4096 5.0, eight waves 5.7), else eight
-// (32 experts, 2048/1409 28, sixteen 39: two blocks a wave are over before the next workgroup has started).
-constexpr long long kLeast = 170;
+// 2048/4096 30 / 25 / 27.  Its waves: 16 where a wave of eight would have four blocks or more and no compute unit gets a second workgroup,
+// else eight.  (us with 8 : 16, one row, K / N: 2048/4096 3.8 : 4.1, 4096/2048 4.5 : 4.6, 4096/4096 5.2 : 5.1, 5120/4096 5.8 : 5.4, 8192/4096
+// 7.3 : 6.7, 16384/2048 10.7 : 9.6, float32 8192/1024 12.2 : 11.5; 320 workgroups, which sixteen waves each would take in two turns: 2048/5120
+// 4.6 : 5.7, 4096/5120 6.5 : 7.6, 16384/5120 15.6 : 16.6; 20 rows, 4096/2048 8.5 : 8.7, 16384/4096 25.6 : 26.0, 4096/5120 14.6 : 15.5.)
+constexpr long long kLeast = 170, kUnits = 256;  // two thirds of the compute units, all
 struct FewShape {
   int bands, cols, waves;  // rows and columns by 16
 };
@@ -472,11 +474,11 @@ FewShape few_shape(bool f32, bool gated, const Groups& e, const Q4Weights& w) {
   if (bands == 1) {
     if (f32 && !gated && work >= 2048) return {1, 4, 8};
     if ((deep || f32) && work >= 512) return {1, 2, 8};
-    return {1, 1, deep && work <= 256 ? 16 : 8};
+    return {1, 1, deep && work <= kUnits ? 16 : 8};
   }
   if (bands == 2) {
     if (work >= 2 * kLeast) return {2, 2, 8};
-    return {2, 1, deep && !f32 ? 16 : 8};
+    return {2, 1, deep && !f32 && work <= kUnits ? 16 : 8};
   }
   if (!gated && work >= 4 * kLeast) return {4, 4, 4};
   return {4, work >= 2 * kLeast ? 2 : 1, 8};
