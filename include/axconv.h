@@ -659,7 +659,8 @@ size_t ax_gated_experts_workspace_bytes(const ax_experts_desc_t* desc);
  * Their gradients.  gx_out [rows, K] (pitch gx_ld) is that of the rows of the products, in their order; the gradient of an indexed
  * x is the sum over its rows (ax_combine without weights).  gw_out (gwg_out, gwu_out): the experts' matrices one behind the other, at
  * the pitch of w; an expert without rows gets zeros.  Formulas, roundings and what may be NULL as in
- * ax_matmul_backward and ax_gated_backward, without the bias; bf16: gz (gg, gu) is rounded to bf16 for all products.
+ * ax_matmul_backward and ax_gated_backward, without the bias; bf16: gz (gg, gu) is rounded to bf16 for all products.  Without rows
+ * gx_out may be NULL whatever else is.
  */
 int ax_matmul_experts_backward(const ax_experts_desc_t* desc, const void* gy, const void* x, const int32_t* index,
                                const int32_t* offsets, const void* w, const void* z, void* gx_out, void* gw_out,
@@ -691,7 +692,7 @@ int ax_combine(const ax_combine_desc_t* desc, const void* h, const int32_t* rows
 /*
  * Gradients: gh_out[rows[t, j]] = weights[t, j] * gy[t] (gy at pitch y_ld; rows must differ from one another; rows of gh_out that no
  * choice names are left as they are), gweights_out[t, j] = sum over the columns of gy[t] * h[rows[t, j]], float32, zero for a row
- * outside h.  Either may be NULL (not both); h is needed for gweights_out alone.  The residual's gradient is gy.
+ * outside h.  Either may be NULL (not both, where there are tokens); h is needed for gweights_out alone.  The residual's gradient is gy.
  */
 int ax_combine_backward(const ax_combine_desc_t* desc, const void* gy, const void* h, const int32_t* rows,
                         const float* weights, void* gh_out, float* gweights_out, void* hip_stream);

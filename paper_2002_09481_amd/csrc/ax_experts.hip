@@ -309,7 +309,7 @@ extern "C" int ax_matmul_experts_backward(const ax_experts_desc_t* d, const void
                                           const int32_t* offsets, const void* w, const void* z, void* gx_out, void* gw_out,
                                           void* workspace, size_t workspace_bytes, void* hip_stream) {
   if (int rc = check_experts(d, true, false)) return rc;
-  if (!gx_out && !gw_out) return AX_ERR_NULL;
+  if (d->rows > 0 && !gx_out && !gw_out) return AX_ERR_NULL;  // (a gradient of no rows may be NULL)
   const int e = elem_bytes(d->dtype);
   if (d->rows > 0) {
     if (int rc = check_rows(d, x, gw_out != nullptr, index, offsets)) return rc;
@@ -333,7 +333,7 @@ extern "C" int ax_gated_experts_backward(const ax_experts_desc_t* d, const void*
                                          void* gx_out, void* gwg_out, void* gwu_out, void* workspace, size_t workspace_bytes,
                                          void* hip_stream) {
   if (int rc = check_experts(d, true, true)) return rc;
-  if ((!gwg_out != !gwu_out) || (!gx_out && !gwg_out)) return AX_ERR_NULL;
+  if ((!gwg_out != !gwu_out) || (d->rows > 0 && !gx_out && !gwg_out)) return AX_ERR_NULL;
   const int e = elem_bytes(d->dtype);
   if (d->rows > 0) {
     if (int rc = check_rows(d, x, gwg_out != nullptr, index, offsets)) return rc;

@@ -634,8 +634,8 @@ extern "C" int ax_combine(const ax_combine_desc_t* d, const void* h, const int32
 extern "C" int ax_combine_backward(const ax_combine_desc_t* d, const void* gy, const void* h, const int32_t* rows, const float* weights,
                                    void* gh_out, float* gweights_out, void* hip_stream) {
   if (int rc = check_combine(d, true, false)) return rc;
-  if (!gh_out && !gweights_out) return AX_ERR_NULL;
   if (d->tokens == 0) return AX_OK;
+  if (!gh_out && !gweights_out) return AX_ERR_NULL;
   if (!gy || !rows || (gweights_out && d->h_rows > 0 && !h)) return AX_ERR_NULL;
   const int e = elem_bytes(d->dtype);
   if (!aligned_to(gy, e) || !aligned_to(h, e) || !aligned_to(gh_out, e) || !aligned_to(rows, 4) || !aligned_to(weights, 4) ||
