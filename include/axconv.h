@@ -437,7 +437,7 @@ int ax_rmsnorm_q8(const ax_norm_desc_t* desc, const void* x, const void* residua
  *   gx_out = rstd * (q - h * mean over the row of (q * h)) + gsum       for x and residual alike
  *   gw_out [cols] float32 = sum over the rows of gy * h
  * Pitches: desc->x_ld (t), residual_ld (gsum), sum_ld (gx_out), y_ld (gy).  gx_out may be gsum.
- * Either output may be NULL (not both).  The sum over rows is taken in a fixed order.
+ * Either output may be NULL (not both, where there are rows).  The sum over rows is taken in a fixed order.
  * workspace: ax_rmsnorm_backward_workspace_bytes(desc) bytes, 256-byte aligned.
  */
 int ax_rmsnorm_backward(const ax_norm_desc_t* desc, const void* gy, const void* gsum, const void* t,
@@ -491,7 +491,7 @@ size_t ax_matmul_q8_workspace_bytes(const ax_matmul_desc_t* desc);
  * (pitch w_ld) too; desc->out_dtype must be desc->dtype.  z may be NULL where act is AX_ACT_NONE.  bf16: gz is
  * rounded to bf16 for the two products (their matrix instructions take 16-bit operands), not for gb_out, nor
  * for gw_out of at most 12 rows (16 where K N >= 2^22): errors of 2.3e-3 in the 2-norm where the rounding of the
- * results alone gives 1.7e-3.  Float32 operands have no such rounding.  Any output may be NULL (not all).
+ * results alone gives 1.7e-3.  Float32 operands have no such rounding.  Any output may be NULL (not all, where there are rows).
  * workspace: ax_matmul_backward_workspace_bytes(desc) bytes.
  */
 int ax_matmul_backward(const ax_matmul_desc_t* desc, const void* gy, const void* x, const void* w,

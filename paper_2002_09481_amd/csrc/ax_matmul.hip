@@ -720,7 +720,7 @@ extern "C" int ax_matmul_backward(const ax_matmul_desc_t* d, const void* gy, con
                                   void* gx_out, void* gw_out, float* gb_out, void* workspace, size_t workspace_bytes,
                                   void* hip_stream) {
   if (int rc = check_desc(d, false, true, false)) return rc;
-  if (!gx_out && !gw_out && !gb_out) return AX_ERR_NULL;
+  if (d->M > 0 && !gx_out && !gw_out && !gb_out) return AX_ERR_NULL;  // (a gradient of no rows may be NULL)
   if (d->M > 0 && (!gy || (gw_out && !x) || (gx_out && !w) || (d->act != AX_ACT_NONE && !z))) return AX_ERR_NULL;
   const int e = elem_bytes(d->dtype);
   if (!operand_aligned(x, e, d->unaligned, d->K, d->x_ld, d->dtype) ||
@@ -794,7 +794,7 @@ extern "C" int ax_gated_backward(const ax_matmul_desc_t* d, const void* gh, cons
                                  const void* g, const void* u, void* gx_out, void* gwg_out, void* gwu_out, void* workspace,
                                  size_t workspace_bytes, void* hip_stream) {
   if (int rc = check_desc(d, false, true, true)) return rc;
-  if ((!gwg_out != !gwu_out) || (!gx_out && !gwg_out)) return AX_ERR_NULL;
+  if ((!gwg_out != !gwu_out) || (d->M > 0 && !gx_out && !gwg_out)) return AX_ERR_NULL;
   if (d->M > 0 && (!gh || !g || !u || (gwg_out && !x) || (gx_out && (!wg || !wu)))) return AX_ERR_NULL;
   const int e = elem_bytes(d->dtype);
   if (!operand_aligned(x, e, d->unaligned, d->K, d->x_ld, d->dtype)) return AX_ERR_ALIGN;

@@ -499,7 +499,7 @@ extern "C" int ax_rmsnorm_backward(const ax_norm_desc_t* d, const void* gy, cons
                                    void* hip_stream) {
   if (int rc = check_norm(d)) return rc;
   if (!d->normalize) return AX_ERR_OPTION;
-  if (!gx_out && !gw_out) return AX_ERR_NULL;
+  if (d->rows > 0 && !gx_out && !gw_out) return AX_ERR_NULL;  // (a gradient of no rows may be NULL)
   if (d->x_ld < d->cols || d->y_ld < d->cols || (gsum && d->residual_ld < d->cols) || (gx_out && d->sum_ld < d->cols))
     return AX_ERR_SHAPE;
   const int e = d->dtype == AX_F32 ? 4 : 2, we = d->w_dtype == AX_F32 ? 4 : 2;

@@ -38,3 +38,16 @@ def test_gradients_of_no_rows_by_experts(dt):
         gh, gweights = ax.ax_combine_backward(y, h, rows, p)
         assert gh.shape == h.shape and gweights.shape == (0, 2)
         assert ax.ax_combine_backward(y, h, rows, p, gh_out=False)[1].shape == (0, 2)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_gradients_of_no_rows(dt):
+    dtype = F.DT[dt]
+    x, y, w = torch.empty((0, 64), device="cuda", dtype=dtype), torch.empty((0, 96), device="cuda", dtype=dtype), torch.ones((64, 96), device="cuda", dtype=dtype)
+    for skip in (False, None):
+        gx, *rest = ax.ax_matmul_backward(y, x, w, gw_out=skip, gb_out=skip)
+        assert gx.shape == (0, 64) and all(g is None if skip is False else not bool(g.any()) for g in rest)
+        gx, *rest = ax.ax_gated_backward(y, x, w, w, y, y, gwg_out=skip, gwu_out=skip)
+        assert gx.shape == (0, 64) and all(g is None if skip is False else not bool(g.any()) for g in rest)
+        gx, gw = ax.ax_rmsnorm_backward(x, x, w[:, 0].contiguous(), torch.empty(0, device="cuda"), gw_out=skip)
+        assert gx.shape == (0, 64) and (gw is None if skip is False else not bool(gw.any()))
