@@ -20,7 +20,9 @@ namespace {
 
 // Configurations of their own.  Tiles of which three fit a compute unit; rows by rows: between the others where one more round of
 // two would be needed.  Sums: contractions are short, a workgroup mostly waits for its first stage and for its stores.  And a height between 64
-// and 128 rows, where it saves a compute unit its third or fourth tile (1027/4096/4096 in one piece 56 to 50 us).
+// and 128 rows, where it saves a compute unit its third or fourth tile: 184 products and gradients of 128 to 16384 rows, 1 to 64 experts, 256 to 8192
+// inputs and outputs, drawn among those that it is chosen for, take 0.97 of the time without it on the average (101 of them less by more than
+// 2 %, 38 more; 0.73 to 1.38, the worst a few hundred rows with weights read in place at a pitch of 8 KB).
 constexpr TileShape kThreeRows = {64, 128, 128, 3, 2.5, 0.60, 0.93};
 constexpr TileShape kThreeSums = {128, 128, 64, 3, 3.0, 0.90, 1.40};
 constexpr TileShape kMiddleRows = {96, 128, 128, 2, 3.0, 0.55, 0.80};

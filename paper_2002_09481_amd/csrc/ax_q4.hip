@@ -13,16 +13,17 @@
 // a time, and turns words into operands of the matrix instruction in registers: codes are whole numbers that bf16 holds, so
 // the products with x (float32: its three bf16 pieces) are exact, and each group's sum in float32 is multiplied by its
 // scale in float32.  No weight is rounded.  The waves of a workgroup share the contraction and meet in LDS.  Measured (us at rows / K / N,
-// group, back to back; in brackets the bytes at the rate of a large copy): bf16 1/4096/4096, 128 5.0 (1.7), 8/8192/8192, 32 12.4 (7.4), gated
-// 1/4096/14336, 128 14.4 (11.8), gated 68 rows of 32 experts, 2048/1409, 32 22 (20.3; calls back to back 28), 64/4096/4096, 128 17.4 (1.7),
-// 256/4096/4096, 128 23.8 (1.7); float32 1/4096/4096, 128 6.4 (1.7), gated 68 rows of 32 experts 53 (20.3).  What is left: a workgroup's way
-// from its launch to its first block, and the meeting at its end; from 64 rows on the conversion of codes, 14 instructions for eight;
-// float32: x cut in pieces once for 16 to 64 columns.
+// group, a replayed graph over four sets of weights; in brackets the bytes at the rate of a large copy): bf16 1/4096/4096, 128 5.1 (1.7),
+// 8/8192/8192, 32 13.3 (7.4), gated 1/4096/14336, 128 16.2 (11.8), gated 68 rows of 32 experts, 28 of them with rows, 2048/1409, 32 32.6 (18), 22 with rows
+// 23.8 (14), 64/4096/4096, 128 18.6 (1.9), 256/4096/4096, 128 25.1 (2.5); float32 1/4096/4096, 128 7.9 (1.7), 64/4096/4096 22 (2.1), 256/4096/4096 80 (3.3), gated
+// 68 rows of 28 experts 60 (18).  What is left: a workgroup's way from its launch to its first block, and the meeting at its end (the gated pair
+// of many experts: two blocks a wave between them); from 64 rows on the conversion of codes, 14 instructions for eight; float32: x cut in
+// pieces once for 16 to 64 columns.
 //
 // More rows: ax_q4_tile.hip, with the weights exact as well.  Very many rows of bf16: the weights are written out once, in the
 // workspace, and multiplied by the tiles of ax_gemm_experts.hip, which lose nothing to scales and codes: every weight, scale
 // times code, is rounded to bf16 (2^-9 of it at most; codes and scales have eleven significant bits together), an error of 1.1e-3 of a result's
-// root mean square, where the rounding of the result alone gives 1.7e-3.
+// root mean square, where the rounding of the result alone gives 1.7e-3.  A row's result then depends on how many rows its call has.
 #include <algorithm>
 #include <type_traits>
 
@@ -253,7 +254,8 @@ struct LayoutArgs {
 };
 
 // A wave a block: lane (r, q) of it has columns 32 s + 8 q .. + 7 of row r.  The largest of a group is that of 4 lanes of the
-// row and one, two or four words.
+// row and one, two or four words.  4096 x 4096, group 128: float32 21.5 us (14.8 at the rate of a large copy), bf16 17.8 (8.2), 32 matrices of
+// 1408 x 2048 in float32 96 (81).
 template <bool F32>
 __global__ __launch_bounds__(256) void quantize_kernel(const LayoutArgs a) {
   const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -304,6 +306,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const LayoutArgs a) {
   *(u32x4*)(a.codes + at * kBlockBytes + lane * 16) = words;
 }
 
+// Bound by its loads of single codes: 33 us for 4096 x 4096, where the bytes would take 5.  Once in a weight's life.
 __global__ __launch_bounds__(256) void pack_kernel(const LayoutArgs a) {
   const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (at >= a.tiles_all * a.blocks) return;
@@ -334,7 +337,8 @@ __global__ __launch_bounds__(256) void pack_kernel(const LayoutArgs a) {
   *(u32x4*)(a.codes + at * kBlockBytes + lane * 16) = words;
 }
 
-// The weights, float32 [rows, K] (VALUES), or bf16 as the tiles read them.  Bound by memory.
+// The weights, float32 [rows, K] (VALUES), or bf16 as the tiles read them.  Bound by memory: 4096 x 4096 in float32 18 us (14.8 at the rate of a
+// large copy), in bf16 11 (8.2).
 template <bool VALUES>
 __global__ __launch_bounds__(256) void unpack_kernel(const LayoutArgs a) {
   const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -413,7 +417,7 @@ struct Plan {
 // us at rows / K / N, q4_kernel : q4_tile_kernel : written out.  A few units of 64 rows by 16 columns, or few rows of an expert: the first, which
 // needs none of the others' stages.
 //   256/4096/4096 26 : 43 : 39      350/4096/4096 41 : 43 : 42   gated 256/4096/4096 42 : 43     500/2048/11264 58 : 42 : 47
-//   8 experts, 2048/1408: 512 rows 17 : 23, 4096 rows 68 : 47 : 49   600/1024/3000 17 : 14 : 20  float32 256/4096/4096 74 : 75, 300/4096/4096 97 : 75
+//   8 experts, 2048/1408: 512 rows 17 : 23, 4096 rows 68 : 47 : 49   600/1024/3000 17 : 14 : 20  float32 256/4096/4096 80 : 79, 300/4096/4096 100 : 79
 // Many rows of an expert: the weights pay for being written once.
 //   512/4096/4096 41 : 42 : 42      600/4096/4096 62 : 58 : 51   1027/4096/4096 86 : 75 : 56     2048/4096/4096 151 : 85 : 75
 //   16 experts, 2048/1408: 4096 rows 64 : 45 : 56

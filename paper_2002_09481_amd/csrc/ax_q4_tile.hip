@@ -9,8 +9,8 @@
 // stands in front of every sum; sums round as those of terms up to six times as large.  float32: x in its three pieces, codes as they are.
 //
 // Bound: vector instructions (widening, scales) and matrix instructions, 63 and 49 % of the cycles at 8192/4096/4096, next to each
-// other only in part.  Measured (us at rows / K / N, group): bf16 300/4096/4096, 64 42, 1027/4096/4096, 64 75, 2048/4096/4096, 128 85,
-// 2048 rows of 32 experts, 2048/1408, 64 32; float32 512/4096/4096, 128 77.  Dropped: parts read a turn ahead in registers (they spill, or gain
+// other only in part.  Measured (us at rows / K / N, group): bf16 300/4096/4096, 64 43, 512/4096/4096 44, 600/4096/4096 59, 1027/4096/4096, 64 75,
+// 2048/4096/4096, 128 85, 2048 rows of 32 experts, 2048/1408, 64 33, 4096 of them 47; float32 512/4096/4096, 128 81, 2048/4096/4096 244.  Dropped: parts read a turn ahead in registers (they spill, or gain
 // nothing), three to six stages (0 to 50 % slower: fewer workgroups a compute unit), 128 rows a workgroup (one wave a SIMD, twice the time).
 #include <algorithm>
 #include <cmath>
